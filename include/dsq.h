@@ -354,6 +354,76 @@ ds_status ds_bench_copy(void* dst_dev, const void* src_dev, uint64_t bytes, void
  * DS_EINVAL for bytes >= 64 GiB. */
 ds_status ds_bench_stream(void* x_dev, void* delta_dev, const void* g_dev, uint64_t bytes, void* hip_stream);
 
+/* ---- answers: a model used as it lies in a message, and the gradient of learning from a neighbour's answers ---------
+ *
+ * A DS_COMP_QUANT_MAXABS message of bits = 4 is a 4-bit copy of the sender's model.  These calls use it without unpacking
+ * it, and make the gradients of learning from what it answers.  They keep no handle and share nothing: every array is the caller's,
+ * device memory of the current HIP device; the work is enqueued on hip_stream (a hipStream_t, NULL = the default stream) with
+ * nothing allocated, copied, cleared or synchronised, so a stream capture of a call gives a graph that repeats it on what the arrays
+ * then hold.  work_dev: scratch of at least the bytes the matching ds_..._work_bytes names, 16-byte aligned (NULL where that is 0);
+ * its contents need not be set and mean nothing afterwards; calls that may run at the same time must not share it.  Apart from
+ * in-place forms that are named, the address ranges of outputs and inputs must not overlap.  errbuf (may be NULL) receives the reason of a failure.
+ * A call with no rows to write (tokens or rows = 0) does nothing. */
+typedef enum { DS_F32 = 0, DS_BF16 = 1, DS_F16 = 2 } ds_dtype;
+
+/* A matrix held as messages: row r is laid out as worker r's message of DS_COMP_QUANT_MAXABS with bits = 4, N = cols and this
+ * block (see ds_message_bytes), the rows one behind the other.  Where cols is a multiple of block, that is also how any
+ * rows * cols consecutive parameters lie inside one worker's message, if the first of them starts a block. */
+typedef struct {
+    uint64_t rows, cols;      /* of the matrix, each >= 1 and < 2^31                             */
+    uint64_t tokens;          /* vectors it is multiplied with, < 2^31                           */
+    int32_t  block;           /* power of two, 64 <= block <= 2048                               */
+    int32_t  dtype;           /* ds_dtype of x, y, dy and dx                                     */
+} ds_matrix;
+
+/* Bytes of such a matrix (tokens and dtype are not looked at); 0 if rows, cols or block is invalid. */
+uint64_t ds_matrix_bytes(const ds_matrix* m);
+
+/* y[t][r] = sum over blocks (scale / 15) * sum over c of the block (2 code - 15) * x[t][c]: `tokens` vectors through the matrix.
+ * msg_dev: ds_matrix_bytes(m) bytes, 4-byte aligned.  x_dev: tokens rows of pitch x_ld >= cols elements; y_dev: tokens rows of
+ * pitch y_ld >= rows elements (columns behind `rows` are left as they were); both of m->dtype and aligned to their elements.  Products are summed in fp32 and
+ * rounded once to dtype.  Infinities and NaN in x go where the formula takes them. */
+uint64_t ds_product_work_bytes(const ds_matrix* m);
+ds_status ds_product(const ds_matrix* m, const void* msg_dev, const void* x_dev, uint64_t x_ld, void* y_dev, uint64_t y_ld,
+                     void* work_dev, uint64_t work_bytes, void* hip_stream, char* errbuf, uint64_t errbuf_len);
+
+/* dx[t][c] = sum over r of dy[t][r] * (scale(r, c) / 15) * (2 code(r, c) - 15): the gradient of ds_product with respect to x.
+ * dy_dev: tokens rows of pitch dy_ld >= rows elements; dx_dev: tokens rows of pitch dx_ld >= cols elements; otherwise as ds_product. */
+uint64_t ds_product_gradient_work_bytes(const ds_matrix* m);
+ds_status ds_product_gradient(const ds_matrix* m, const void* msg_dev, const void* dy_dev, uint64_t dy_ld, void* dx_dev,
+                              uint64_t dx_ld, void* work_dev, uint64_t work_bytes, void* hip_stream, char* errbuf, uint64_t errbuf_len);
+
+/* Rows of logits and, for each row, k pairs (u32 index, f32 value) as in a DS_COMP_TOPK message. */
+typedef struct {
+    uint64_t rows;            /* < 2^31                                                          */
+    uint64_t vocab;           /* logits per row, 1 <= vocab < 2^31                               */
+    int32_t  k;               /* pairs per row, 1 <= k <= 256 (ds_top_logits: and k <= vocab)    */
+    int32_t  dtype;           /* ds_dtype of the logits and of their gradient                    */
+    float    temperature;     /* logits are divided by it; finite, > 0                           */
+    int32_t  reserved;        /* must be 0                                                       */
+} ds_logits;
+
+/* What a teacher sends: the k largest logits of each row, ties to the lower index (+0 and -0 tie, NaN is larger than
+ * anything), as pairs in ascending index order, and lse[i] = ln sum_v exp(z[i][v] / temperature).
+ * z_dev: rows of pitch z_ld >= vocab elements of dtype, aligned to its elements; pairs_dev: rows * k * 8 bytes, 8-byte aligned; lse_dev: rows floats or NULL. */
+uint64_t ds_top_logits_work_bytes(const ds_logits* l);
+ds_status ds_top_logits(const ds_logits* l, const void* z_dev, uint64_t z_ld, void* pairs_dev, float* lse_dev, void* work_dev,
+                        uint64_t work_bytes, void* hip_stream, char* errbuf, uint64_t errbuf_len);
+
+/* The loss of a student's logits z against a teacher's pairs (index i_j, logit a_j), and its gradient.  Per row, T = temperature:
+ *   p_j  = exp(a_j / T - A),  A = ln sum_j exp(a_j / T), or the row's teacher_lse (what ds_top_logits gave, at the same T)
+ *   Z    = ln sum_v exp(z_v / T),   loss = weight * sum_j p_j (ln p_j - z[i_j] / T + Z)      (terms with p_j = 0 are 0)
+ *   dz_v = weight / T * (exp(z_v / T - Z) * sum_j p_j  -  sum of p_j over the j with i_j = v)
+ * An index >= vocab is no entry (0xFFFFFFFF pads short lists); an index may occur more than once.  A row of weight 0, or without
+ * an entry of p_j != 0, has loss 0 and gradient 0 whatever its logits hold.  Logits of minus infinity have probability 0.
+ * pairs_dev: rows * k * 8 bytes, 8-byte aligned, any order; teacher_lse_dev, weight_dev: rows floats each or NULL (weight 1);
+ * loss_dev: rows floats or NULL; dz_dev: rows of pitch dz_ld >= vocab elements of dtype, or NULL; not both NULL.  dz_dev may be
+ * z_dev with dz_ld = z_ld.  Columns behind vocab are left as they were. */
+uint64_t ds_distill_work_bytes(const ds_logits* l);
+ds_status ds_distill(const ds_logits* l, const void* z_dev, uint64_t z_ld, const void* pairs_dev, const float* teacher_lse_dev,
+                     const float* weight_dev, float* loss_dev, void* dz_dev, uint64_t dz_ld, void* work_dev, uint64_t work_bytes,
+                     void* hip_stream, char* errbuf, uint64_t errbuf_len);
+
 /* Frees everything the handle owns (synchronises first).  NULL is a no-op. */
 void ds_destroy(ds_handle* h);
 

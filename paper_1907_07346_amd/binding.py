@@ -26,7 +26,9 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdsq.so")
 EXPORTS = ["ds_validate_config", "ds_build_topology", "ds_message_bytes", "ds_init", "ds_step",
            "ds_read_state", "ds_write_state", "ds_read_messages", "ds_state_ptrs", "ds_message_ptr",
            "ds_step_count", "ds_plan_name", "ds_last_error", "ds_destroy", "ds_bench_copy",
-           "ds_topk_candidate_rows", "ds_set_mixing", "ds_diagnostics", "ds_set_rates", "ds_workload_gradient", "ds_bench_stream", "ds_build_id", "ds_step_static", "ds_init_ex"]
+           "ds_topk_candidate_rows", "ds_set_mixing", "ds_diagnostics", "ds_set_rates", "ds_workload_gradient", "ds_bench_stream", "ds_build_id", "ds_step_static", "ds_init_ex",
+           "ds_matrix_bytes", "ds_product", "ds_product_work_bytes", "ds_product_gradient", "ds_product_gradient_work_bytes",
+           "ds_top_logits", "ds_top_logits_work_bytes", "ds_distill", "ds_distill_work_bytes"]
 
 
 # torch's current stream as the pointer the library takes.  torch.cuda.current_stream() makes a Stream object for it: 2.9 us of
@@ -63,6 +65,16 @@ class ds_config(ctypes.Structure):
                 ("W_rowptr", ctypes.c_void_p), ("W_col", ctypes.c_void_p), ("W_val", ctypes.c_void_p),
                 ("comp", ds_comp), ("gamma", ctypes.c_float), ("eta", ctypes.c_float),
                 ("seed", ctypes.c_uint64), ("algo", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class ds_matrix(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64), ("tokens", ctypes.c_uint64), ("block", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class ds_logits(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_uint64), ("vocab", ctypes.c_uint64), ("k", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("temperature", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
 class DsqError(RuntimeError):
@@ -111,6 +123,16 @@ def lib() -> ctypes.CDLL:
         L.ds_destroy.argtypes, L.ds_destroy.restype = [vp], None
         L.ds_bench_copy.argtypes, L.ds_bench_copy.restype = [vp, vp, u64, vp], i32
         L.ds_bench_stream.argtypes, L.ds_bench_stream.restype = [vp, vp, vp, u64, vp], i32
+        mp, lp = ctypes.POINTER(ds_matrix), ctypes.POINTER(ds_logits)
+        err = [ctypes.c_char_p, u64]
+        for name, shape in (("ds_matrix_bytes", mp), ("ds_product_work_bytes", mp), ("ds_product_gradient_work_bytes", mp),
+                            ("ds_top_logits_work_bytes", lp), ("ds_distill_work_bytes", lp)):
+            getattr(L, name).argtypes, getattr(L, name).restype = [shape], u64
+        L.ds_product.argtypes = L.ds_product_gradient.argtypes = [mp, vp, vp, u64, vp, u64, vp, u64, vp] + err
+        L.ds_top_logits.argtypes = [lp, vp, u64, vp, vp, vp, u64, vp] + err
+        L.ds_distill.argtypes = [lp, vp, u64, vp, vp, vp, vp, vp, u64, vp, u64, vp] + err
+        for name in ("ds_product", "ds_product_gradient", "ds_top_logits", "ds_distill"):
+            getattr(L, name).restype = i32
         _lib = L
     return _lib
 
@@ -210,6 +232,147 @@ def ds_step_static(cfg: ds_config, x: "torch.Tensor", delta: "torch.Tensor", g: 
         raise DsqError(st, "ds_step_static", buf.value.decode())
 
 
+# ---- answers: products with messages, logits (include/dsq.h says what each computes) -------------------------------
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _refuse(where: str, why: str):
+    raise DsqError(DS_EINVAL, where, why)
+
+
+def _on_device(where: str, **tensors):
+    here = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if t is not None and not (t.is_cuda and t.get_device() == here):
+            _refuse(where, f"{name} must be on the current CUDA device")
+
+
+def _rows_of(where: str, name: str, t: "torch.Tensor"):
+    """(rows, columns, pitch) of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.dtype not in _DTYPES:
+        _refuse(where, f"{name} must be a matrix of float32, bfloat16 or float16")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        _refuse(where, f"{name} must have unit column stride")
+    return rows, cols, t.stride(0) if rows > 1 else cols
+
+
+def _vector(where: str, name: str, t: "Optional[torch.Tensor]", rows: int):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != rows or not t.is_contiguous():
+        _refuse(where, f"{name} must be a contiguous float32 vector of {rows}")
+    return t.data_ptr()
+
+
+def _new(stream, shape, dtype):
+    """A tensor whose memory belongs to the stream that the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device="cuda")
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device="cuda")
+
+
+def _answer(name: str, shape, args, stream):
+    """Calls `name` with scratch memory of the call's stream; the reason of a refusal goes into the exception."""
+    L = lib()
+    size = getattr(L, name + "_work_bytes")(shape)
+    work = _new(stream, (size,), torch.uint8) if size else None
+    args = [shape, *args, work.data_ptr() if size else None, size, _stream_pointer(stream)]
+    st = getattr(L, name)(*args, None, 0)
+    if st == DS_EINVAL:                                   # (checks only: nothing has been enqueued)
+        buf = ctypes.create_string_buffer(256)
+        getattr(L, name)(*args, buf, 256)
+        raise DsqError(st, name, buf.value.decode())
+    if st != DS_OK:
+        raise DsqError(st, name)
+
+
+def ds_matrix_bytes(rows: int, cols: int, block: int) -> int:
+    return int(lib().ds_matrix_bytes(ctypes.byref(ds_matrix(rows, cols, 0, block, 0))))
+
+
+def _through(name: str, msg: "torch.Tensor", x: "torch.Tensor", rows: int, cols: int, block: int, out: "Optional[torch.Tensor]",
+             stream: Optional["torch.cuda.Stream"]):
+    width, out_width = (cols, rows) if name == "ds_product" else (rows, cols)
+    tokens, got, pitch = _rows_of(name, "the input", x)
+    if got != width:
+        _refuse(name, f"the input must have {width} columns")
+    m = ds_matrix(rows, cols, tokens, block, _DTYPES[x.dtype])
+    if msg.dtype != torch.uint8 or not msg.is_contiguous() or msg.numel() < lib().ds_matrix_bytes(ctypes.byref(m)):
+        _refuse(name, "msg must be a contiguous uint8 tensor that holds the matrix")
+    _on_device(name, msg=msg, x=x, out=out)
+    if out is None:
+        out = _new(stream, (tokens, out_width), x.dtype)
+    elif out.dtype != x.dtype or tuple(out.shape) != (tokens, out_width):
+        _refuse(name, f"out must be ({tokens}, {out_width}) and of the input's dtype")
+    out_pitch = _rows_of(name, "out", out)[2]
+    if tokens:
+        _answer(name, ctypes.byref(m), [msg.data_ptr(), x.data_ptr(), pitch, out.data_ptr(), out_pitch], stream)
+    return out
+
+
+def ds_product(msg: "torch.Tensor", x: "torch.Tensor", rows: int, block: int, out: "Optional[torch.Tensor]" = None,
+               stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
+    """x (tokens, cols) through the matrix of `rows` rows held as 4-bit messages in msg (uint8): (tokens, rows) of x's dtype."""
+    return _through("ds_product", msg, x, rows, x.shape[-1], block, out, stream)
+
+
+def ds_product_gradient(msg: "torch.Tensor", dy: "torch.Tensor", cols: int, block: int, out: "Optional[torch.Tensor]" = None,
+                        stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
+    """The gradient of ds_product with respect to x: dy (tokens, rows) gives (tokens, cols) of dy's dtype."""
+    return _through("ds_product_gradient", msg, dy, dy.shape[-1], cols, block, out, stream)
+
+
+def ds_top_logits(z: "torch.Tensor", k: int, temperature: float = 1.0, stream: Optional["torch.cuda.Stream"] = None):
+    """The k largest logits of each row of z: (pairs, lse), pairs int32 (rows, k, 2) of index and float32 bits, ascending index."""
+    rows, vocab, pitch = _rows_of("ds_top_logits", "z", z)
+    _on_device("ds_top_logits", z=z)
+    if not 1 <= k <= 256:
+        _refuse("ds_top_logits", "k must be between 1 and 256")
+    pairs, lse = _new(stream, (rows, k, 2), torch.int32), _new(stream, (rows,), torch.float32)
+    if rows:
+        _answer("ds_top_logits", ctypes.byref(ds_logits(rows, vocab, k, _DTYPES[z.dtype], temperature, 0)),
+                [z.data_ptr(), pitch, pairs.data_ptr(), lse.data_ptr()], stream)
+    return pairs, lse
+
+
+def ds_distill(z: "torch.Tensor", pairs: "torch.Tensor", temperature: float = 1.0, teacher_lse: "Optional[torch.Tensor]" = None,
+               weight: "Optional[torch.Tensor]" = None, want_loss: bool = True, want_gradient: bool = True,
+               dz: "Optional[torch.Tensor]" = None, stream: Optional["torch.cuda.Stream"] = None):
+    """The loss of each row of z against the teacher's pairs (as ds_top_logits gives them) and its gradient: (loss, dz), None for
+    what is not wanted.  dz may be given, also as z itself."""
+    rows, vocab, pitch = _rows_of("ds_distill", "z", z)
+    if pairs.dtype != torch.int32 or pairs.dim() != 3 or pairs.shape[0] != rows or pairs.shape[2] != 2 or not pairs.is_contiguous():
+        _refuse("ds_distill", f"pairs must be a contiguous int32 tensor ({rows}, k, 2)")
+    _on_device("ds_distill", z=z, pairs=pairs, teacher_lse=teacher_lse, weight=weight, dz=dz)
+    given = [_vector("ds_distill", "teacher_lse", teacher_lse, rows), _vector("ds_distill", "weight", weight, rows)]
+    loss = _new(stream, (rows,), torch.float32) if want_loss else None
+    dz_pitch = 0
+    if want_gradient:
+        if dz is None:
+            dz = _new(stream, (rows, vocab), z.dtype)
+        elif dz.dtype != z.dtype or dz.shape != z.shape:
+            _refuse("ds_distill", "dz must have z's shape and dtype")
+        dz_pitch = _rows_of("ds_distill", "dz", dz)[2]
+    elif dz is not None:
+        _refuse("ds_distill", "dz is given but no gradient is wanted")
+    if rows:
+        _answer("ds_distill", ctypes.byref(ds_logits(rows, vocab, pairs.shape[1], _DTYPES[z.dtype], temperature, 0)),
+                [z.data_ptr(), pitch, pairs.data_ptr(), *given, loss.data_ptr() if want_loss else None,
+                 dz.data_ptr() if want_gradient else None, dz_pitch], stream)
+    return loss, dz
+
+
+class _Lent:
+    """Bytes of the library's device memory for torch.as_tensor: no copy, and the owner lives as long as the tensor."""
+
+    def __init__(self, pointer: int, size: int, owner):
+        self.owner = owner
+        self.__cuda_array_interface__ = {"shape": (size,), "typestr": "|u1", "data": (pointer, False), "version": 2}
+
+
 class DeepSqueeze:
     """Owner of one ds_handle. Methods are the C calls with the same names."""
 
@@ -228,6 +391,7 @@ class DeepSqueeze:
         if st != DS_OK:
             raise DsqError(st, "ds_init", buf.value.decode())
         self.n, self.N = int(cfg.n), int(cfg.N)
+        self._stepped = False
 
     @classmethod
     def from_workload(cls, w: Config, plan: Optional[dict] = None) -> "DeepSqueeze":
@@ -244,8 +408,10 @@ class DeepSqueeze:
         assert g.stride(1) == 1 and g.shape[1] >= self.N
         self._check(lib().ds_step(self._h, g.data_ptr(), g.stride(0) if self.n > 1 else max(g.stride(0), g.shape[1]),
                                   _stream_pointer(stream)), "ds_step")
+        self._stepped = True
 
     def ds_step_raw(self, g_ptr: int, g_ld: int, stream_ptr: int = 0) -> int:
+        self._stepped = True
         return lib().ds_step(self._h, g_ptr, g_ld, stream_ptr)
 
     def ds_set_mixing(self, W_csr):
@@ -291,6 +457,33 @@ class DeepSqueeze:
         p, b = ctypes.c_void_p(), ctypes.c_uint64()
         self._check(lib().ds_message_ptr(self._h, ctypes.byref(p), ctypes.byref(b)), "ds_message_ptr")
         return p.value, b.value
+
+    def ds_product(self, worker: int, x: "torch.Tensor", rows: int, first: int = 0, out: "Optional[torch.Tensor]" = None,
+                   stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
+        """x (tokens, cols) through parameters first .. first + rows * cols - 1 of `worker` as the message of the last ds_step holds
+        them (4-bit QUANT_MAXABS; first and cols multiples of the block).  Some launch plans alternate between two message buffers:
+        the call then waits for the last ds_step (see ds_message_ptr)."""
+        return self._through_message("ds_product", worker, x, rows, x.shape[-1], first, out, stream)
+
+    def ds_product_gradient(self, worker: int, dy: "torch.Tensor", cols: int, first: int = 0, out: "Optional[torch.Tensor]" = None,
+                            stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
+        """The gradient of ds_product (same worker and parameters) with respect to x."""
+        return self._through_message("ds_product_gradient", worker, dy, dy.shape[-1], cols, first, out, stream)
+
+    def _through_message(self, name, worker, x, rows, cols, first, out, stream):
+        comp = self.cfg.comp
+        if comp.kind != KIND_QUANT_MAXABS or comp.bits != 4:
+            _refuse(name, "messages of the 4-bit block quantiser only")
+        if not self._stepped:
+            raise DsqError(DS_ESTATE, name, "no step has been taken yet")
+        if not 0 <= worker < self.n:
+            _refuse(name, f"there is no worker {worker}")
+        if first < 0 or first % comp.block or cols % comp.block or rows < 1 or cols < 1 or first + rows * cols > self.N:
+            _refuse(name, "first and cols must be multiples of the block and the matrix must lie inside the worker's parameters")
+        msg, total = self.ds_message_ptr()
+        lo = worker * (total // self.n) + first // comp.block * (4 + comp.block // 2)
+        view = torch.as_tensor(_Lent(msg + lo, ds_matrix_bytes(rows, cols, comp.block), self), device="cuda")
+        return _through(name, view, x, rows, cols, comp.block, out, stream)
 
     def ds_diagnostics(self) -> dict:
         out = (ctypes.c_double * 4)()

@@ -1,0 +1,491 @@
+"""The operators on messages and logits against plain implementations in 64 bits, at the sizes, types, masks and strides where
+they can go wrong, and a run of them together over messages that ds_step made.
+
+Tolerances.  U = 2^-24 is half a unit in the last place of fp32, in which sums are held.
+  products    A sum of n terms is rounded n times or so; each rounding is off by U times the partial sum it rounds, and their signs are
+              random: 8 U S covers it, S = sum |term| with every code taken as 31 (codes are summed as q + 16 and 23.5 x is taken off).
+              The gradient rounds dy * scale / 15 to two bf16 pieces of 8 bits, 2^-17 relative, for dtypes of 16 bits.
+  logits      exp2 of d = (z - max) log2(e) / T: the product is off by 2 U |d|, exp2 itself by 2 U or so; sums as above.
+Then comes the rounding to the output's type (answers_plain.rounding).
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1907_07346_amd import binding as b
+from paper_1907_07346_amd import workloads as wl
+from tests import answers_plain as plain
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+INF, NAN = float("inf"), float("nan")
+
+
+def normal(rng, shape, dtype=F32, scale=1.0):
+    return torch.from_numpy(rng.standard_normal(shape) * scale).to(dtype)
+
+
+def check(got, want, tol, what):
+    got, want = got.detach().cpu().double(), want.double()
+    same = (got == want) | (torch.isnan(got) & torch.isnan(want))
+    err = torch.where(same, torch.zeros_like(got), (got - want).abs())
+    bad = ~(err <= tol)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, first at {bad.nonzero()[0].tolist()}: {got[bad][0]} for {want[bad][0]}"
+
+
+# ---- products ------------------------------------------------------------------------------------
+
+def product_tolerance(want, x, unit, dtype):
+    """x (tokens, n) and unit (n, outputs), both float64: see above."""
+    spread = x.abs() @ unit.abs() * 31.0
+    return (8 * U + (2.0 ** -17 if dtype != F32 else 0.0)) * spread + plain.rounding(want, dtype)
+
+
+def units(scales, block, cols):
+    return torch.from_numpy(np.repeat(scales.astype(np.float64), block, axis=1)[:, :cols] / 15.0)
+
+
+SHAPES = [(1, 1, 1, 64), (1, 17, 63, 64), (2, 16, 64, 64), (3, 5, 65, 128), (5, 33, 129, 64), (7, 31, 8, 2048), (16, 129, 333, 128),
+          (17, 100, 1000, 256), (33, 64, 512, 512), (64, 70, 2049, 2048), (65, 40, 4100, 512), (130, 19, 300, 64), (1, 300, 5001, 1024),
+          (4, 1000, 127, 128), (9, 257, 2500, 64), (15, 513, 896, 256), (48, 1030, 640, 128), (1, 2048, 2048, 512)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("tokens,rows,cols,block", SHAPES)
+def test_product_and_its_gradient(tokens, rows, cols, block, dtype):
+    rng = np.random.default_rng(tokens * 1000003 + rows * 1009 + cols)
+    msg, codes, scales = plain.random_message(rows, cols, block, rng)
+    m, unit = plain.dense(codes, scales, block), units(scales, block, cols)
+    x, dy = normal(rng, (tokens, cols), dtype), normal(rng, (tokens, rows), dtype)
+    msg_dev = msg.cuda()
+    y = b.ds_product(msg_dev, x.cuda(), rows, block)
+    want = x.double() @ m.t().contiguous()
+    check(y, want, product_tolerance(want, x.double(), unit.t().contiguous(), dtype), "y")
+    dx = b.ds_product_gradient(msg_dev, dy.cuda(), cols, block)
+    want = dy.double() @ m
+    check(dx, want, product_tolerance(want, dy.double(), unit, dtype), "dx")
+    assert y.dtype == dx.dtype == dtype
+    # the same call gives the same bits
+    assert torch.equal(y, b.ds_product(msg_dev, x.cuda(), rows, block)) and torch.equal(dx, b.ds_product_gradient(msg_dev, dy.cuda(), cols, block))
+
+
+def test_gradient_is_the_transpose_and_matches_differences():
+    """<dy, product(x)> = <gradient(dy), x>, and the product is linear: a difference of it along e_c is the gradient's column."""
+    rng = np.random.default_rng(5)
+    rows, cols, block = 70, 390, 64
+    msg, codes, scales = plain.random_message(rows, cols, block, rng)
+    x, dy = normal(rng, (6, cols)).cuda(), normal(rng, (6, rows)).cuda()
+    y, dx = b.ds_product(msg.cuda(), x, rows, block), b.ds_product_gradient(msg.cuda(), dy, cols, block)
+    left, right = (dy.double() * y.double()).sum(dim=1), (dx.double() * x.double()).sum(dim=1)
+    size = (dy.double().abs() @ (plain.dense(codes, scales, block).abs().cuda()) * x.double().abs()).sum(dim=1)
+    assert ((left - right).abs() <= 64 * U * size).all()
+    step = torch.zeros_like(x)
+    for c in (0, 63, 64, 127, 389):
+        step.zero_()
+        step[:, c] = 1.0
+        d = (b.ds_product(msg.cuda(), x + step, rows, block).double() - b.ds_product(msg.cuda(), x - step, rows, block).double()) / 2
+        slope = (dy.double() * d).sum(dim=1)
+        assert ((slope - dx[:, c].double()).abs() <= 64 * U * size + 1e-9).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_products_with_pitches_offsets_and_neighbours(dtype):
+    """Inputs and outputs inside larger arrays that start at odd elements; what lies around the outputs stays."""
+    rng = np.random.default_rng(9)
+    tokens, rows, cols, block = 19, 77, 515, 128
+    msg, codes, scales = plain.random_message(rows, cols, block, rng)
+    m, unit = plain.dense(codes, scales, block), units(scales, block, cols)
+    big = torch.cat([torch.zeros(4, dtype=torch.uint8), msg, torch.full((64,), 255, dtype=torch.uint8)]).cuda()
+    here = big[4:4 + msg.numel()]                                  # starts at an odd word
+    for name, width, out_width, mat, un in (("ds_product", cols, rows, m.t().contiguous(), unit.t().contiguous()), ("ds_product_gradient", rows, cols, m, unit)):
+        for shift, pitch, out_shift, out_pitch in ((1, width + 3, 3, out_width + 5), (0, width, 0, out_width + 1), (5, width + 8, 1, out_width)):
+            store = torch.full((tokens * pitch + 16,), NAN, dtype=dtype)
+            x = normal(rng, (tokens, width), dtype)
+            store[shift:shift + tokens * pitch].view(tokens, pitch)[:, :width] = x
+            xs = store.cuda()[shift:shift + tokens * pitch].view(tokens, pitch)[:, :width]
+            out = torch.full((tokens * out_pitch + 16,), 123.0, dtype=dtype, device="cuda")
+            ys = out[out_shift:out_shift + tokens * out_pitch].view(tokens, out_pitch)[:, :out_width]
+            back = getattr(b, name)(here, xs, rows if name == "ds_product" else cols, block, out=ys)
+            assert back.data_ptr() == ys.data_ptr()
+            want = x.double() @ mat
+            check(ys, want, product_tolerance(want, x.double(), un, dtype), name)
+            ys.fill_(123.0)
+            assert (out == 123.0).all(), "memory around the output was written"
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("tokens,rows,cols,block", [(5, 40, 300, 64), (18, 33, 700, 256)])
+def test_products_with_infinities_nan_and_zero_scales(tokens, rows, cols, block, dtype):
+    """No code stands for 0, so an infinity in x reaches every y with the sign of the code, two of them may meet as NaN, and a block of
+    scale 0 makes NaN of them; finite rows are not touched by their neighbours."""
+    rng = np.random.default_rng(11)
+    zero_block = lambda shape, r: np.where(r.random(shape) < 0.2, 0.0, r.random(shape) + 0.01)
+    msg, codes, scales = plain.random_message(rows, cols, block, rng, zero_block)
+    m, unit = plain.dense(codes, scales, block), units(scales, block, cols)
+    for name, width, mat, un, other in (("ds_product", cols, m.t().contiguous(), unit.t().contiguous(), rows), ("ds_product_gradient", rows, m, unit, cols)):
+        x = normal(rng, (tokens, width), dtype)
+        x[0, 3], x[1, 5], x[1, 17], x[2, 20], x[3, 0], x[3, width - 1] = INF, -INF, INF, NAN, INF, INF
+        if dtype == F32:
+            x[4, 7] = 3e38                                         # finite, but 31 times as much is not
+        terms = x.double()[:, :, None] * mat[None]
+        want = terms.sum(dim=1)
+        got = getattr(b, name)(msg.cuda(), x.cuda(), other, block).cpu().double()
+        size = torch.where(torch.isfinite(x.double()), x.double(), torch.zeros(1, dtype=torch.float64))
+        tol = product_tolerance(torch.where(torch.isfinite(want), want, torch.zeros_like(want)), size, un, dtype)
+        if dtype == F32:                                           # where a sum of fp32 may or may not pass the largest number
+            edge = want[4].abs() > 1e38
+            got[4], want[4] = torch.where(edge, torch.zeros_like(got[4]), got[4]), torch.where(edge, torch.zeros_like(want[4]), want[4])
+        check(got, want, tol, name)
+
+
+def test_products_of_no_tokens_and_refusals():
+    msg = torch.zeros(2 * 36, dtype=torch.uint8, device="cuda")
+    x = torch.zeros((0, 64), device="cuda")
+    assert tuple(b.ds_product(msg, x, 2, 64).shape) == (0, 2)
+    assert tuple(b.ds_product_gradient(msg, torch.zeros((0, 2), device="cuda"), 64, 64).shape) == (0, 64)
+    x = torch.zeros((3, 64), device="cuda")
+    for call in (lambda: b.ds_product(msg.cpu(), x, 2, 64), lambda: b.ds_product(msg, x.double(), 2, 64), lambda: b.ds_product(msg, x, 3, 64),
+                 lambda: b.ds_product(msg, x.t(), 2, 64), lambda: b.ds_product(msg, x, 2, 48), lambda: b.ds_product(msg, x[:1].expand(3, 64), 2, 64),
+                 lambda: b.ds_product(msg, x, 2, 64, out=torch.zeros((3, 3), device="cuda")),
+                 lambda: b.ds_product(msg, x, 2, 64, out=x.bfloat16()[:, :2])):
+        with pytest.raises(b.DsqError) as e:
+            call()
+        assert e.value.status == b.DS_EINVAL
+    with pytest.raises(b.DsqError, match="overlaps"):
+        b.ds_product(msg, x, 2, 64, out=x[:, :2])
+
+
+def test_product_reads_a_message_of_more_than_four_gigabytes():
+    """Rows whose bytes lie past 2^32 of the message."""
+    rows, cols, block = 300_000, 32768, 256
+    per = plain.row_bytes(cols, block)
+    assert per * rows > 1 << 32
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    msg = torch.empty(rows * per, dtype=torch.uint8, device="cuda")
+    words = msg.view(torch.int32).view(rows, cols // block, 1 + block // 8)
+    for lo in range(0, rows, 50_000):
+        part = words[lo:lo + 50_000]
+        part[:] = torch.randint(-2 ** 31, 2 ** 31, part.shape, device="cuda", dtype=torch.int64, generator=gen).to(torch.int32)
+        part[:, :, 0] = torch.rand(part.shape[:2], device="cuda", generator=gen).view(torch.int32)
+    rng = np.random.default_rng(1)
+    x, dy = normal(rng, (2, cols), BF16), torch.zeros((2, rows), dtype=BF16)
+    some = [0, 1, 123_457, rows // 2, rows - 17, rows - 2, rows - 1]
+    m = plain.decode(msg.view(rows, per)[some].cpu().numpy(), len(some), cols, block)
+    y = b.ds_product(msg, x.cuda(), rows, block)
+    want = x.double() @ m.t().contiguous()
+    tol = product_tolerance(want, x.double(), m.t().contiguous(), BF16)
+    check(y[:, some], want, tol, "y")
+    dy[:, some] = normal(rng, (2, len(some)), BF16)
+    want = dy[:, some].double() @ m
+    check(b.ds_product_gradient(msg, dy.cuda(), cols, block), want, product_tolerance(want, dy[:, some].double(), m.abs() + 0.07, BF16), "dx")
+
+
+# ---- the largest logits ----------------------------------------------------------------------------
+
+def check_top(z, k, temperature=1.0):
+    pairs, lse = b.ds_top_logits(z.cuda(), k, temperature)
+    pairs, lse, z = pairs.cpu(), lse.cpu(), z.cpu()
+    want = plain.top(z, k)
+    assert torch.equal(pairs[..., 0].long(), want), "indices differ"
+    value, expected = pairs.view(F32)[..., 1], z.float().gather(1, want)
+    assert torch.equal(torch.nan_to_num(value, nan=7e30), torch.nan_to_num(expected, nan=7e30)), "values differ"
+    exact = plain.lse(z.double() / temperature)
+    finite = torch.where(torch.isfinite(z), z, torch.zeros_like(z)).double().abs().amax(dim=1) / temperature
+    # the sum's logarithm, its roundings at the size of the largest logit and of ln V, and the spread of exp2's error over the sum
+    check(lse, exact, U * (8 + 2 * finite + 4 * math.log(z.shape[1] + 1)), "lse")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,vocab,k", [(1, 1, 1), (3, 2, 2), (5, 63, 1), (4, 64, 64), (7, 300, 256), (2, 256, 256), (9, 1000, 17),
+                                          (33, 4097, 100), (3, 32003, 256), (2, 131072, 64), (1, 262147, 128), (600, 513, 8), (1, 9000, 255)])
+def test_top_logits(rows, vocab, k, dtype):
+    check_top(normal(np.random.default_rng(rows * 7 + vocab), (rows, vocab), dtype, 3.0), k, 1.0 if k % 2 else 2.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab,k", [(5000, 100), (70001, 256), (40000, 7)])
+def test_top_logits_of_rows_that_are_hard_to_select_from(vocab, k, dtype):
+    rng = np.random.default_rng(vocab)
+    rows = [np.zeros(vocab), np.arange(vocab) / vocab, -np.arange(vocab) / vocab, np.full(vocab, -INF), rng.integers(0, 3, vocab),
+            np.where(rng.random(vocab) < 0.5, 0.0, -0.0), np.where(np.arange(vocab) % 3 == 0, INF, rng.standard_normal(vocab)),
+            np.where(rng.random(vocab) < 0.001, NAN, rng.standard_normal(vocab)), np.full(vocab, NAN),
+            np.where(np.arange(vocab) < vocab - k // 2, -INF, 1.0), np.sort(rng.standard_normal(vocab)), np.full(vocab, -3.0e38)]
+    last = np.full(vocab, -1.0)
+    last[-k:] = 2.0
+    rows.append(last)
+    check_top(torch.from_numpy(np.stack(rows)).to(dtype), k)
+
+
+def test_top_logits_of_strided_rows_and_none():
+    rng = np.random.default_rng(2)
+    store = normal(rng, (20, 1111), BF16, 3.0)
+    dev = store.cuda()
+    pairs, lse = b.ds_top_logits(dev[3:17, 5:1000], 33)
+    want, lse_want = b.ds_top_logits(dev[3:17, 5:1000].contiguous(), 33)
+    assert torch.equal(pairs, want) and torch.equal(lse, lse_want)
+    assert torch.equal(pairs[..., 0].cpu().long(), plain.top(store[3:17, 5:1000], 33))
+    pairs, lse = b.ds_top_logits(dev[:0], 4)
+    assert tuple(pairs.shape) == (0, 4, 2) and tuple(lse.shape) == (0,)
+    for call in (lambda: b.ds_top_logits(dev, 0), lambda: b.ds_top_logits(dev, 257), lambda: b.ds_top_logits(dev[:, :3], 4),
+                 lambda: b.ds_top_logits(dev, 4, 0.0), lambda: b.ds_top_logits(dev, 4, NAN), lambda: b.ds_top_logits(dev.cpu(), 4),
+                 lambda: b.ds_top_logits(dev.t(), 4), lambda: b.ds_top_logits(dev.int(), 4)):
+        with pytest.raises(b.DsqError) as e:
+            call()
+        assert e.value.status == b.DS_EINVAL
+
+
+# ---- distillation ----------------------------------------------------------------------------------
+
+def teacher(rng, rows, vocab, k, shuffled=False):
+    """Distinct indices (as far as there are that many) and their logits."""
+    index = np.stack([np.sort(rng.permutation(vocab)[:k]) if k <= vocab else np.concatenate([np.arange(vocab), np.full(k - vocab, -1)])
+                      for _ in range(rows)])
+    if shuffled:
+        index = rng.permuted(index, axis=1)
+    return torch.from_numpy(index).long(), normal(rng, (rows, k), F32, 2.0)
+
+
+def pack_pairs(index, value):
+    return torch.stack([index.to(torch.int32), value.float().contiguous().view(torch.int32)], dim=2).contiguous()
+
+
+def distill_tolerances(z, index, value, temperature, want_loss, want, teacher_lse, weight):
+    """(of the loss, of dz)."""
+    zs = torch.where(torch.isfinite(z), z, torch.zeros_like(z)).double() / temperature
+    rel = U * (16 + 4 * (zs.amax(dim=1) - zs.amin(dim=1)))                                 # of a probability, see above
+    v = torch.where(torch.isfinite(value), value, torch.zeros_like(value)).double() / temperature
+    rel_p = U * (16 + 4 * (v.amax(dim=1) - v.amin(dim=1)) + (0 if teacher_lse is None else 4 * (v.abs().amax(dim=1) + teacher_lse.double().abs())))
+    p = torch.exp(v - (torch.logsumexp(v, dim=1) if teacher_lse is None else teacher_lse.double())[:, None]).sum(dim=1)
+    w = torch.ones(z.shape[0], dtype=torch.float64) if weight is None else weight.double().abs()
+    size = v.abs().amax(dim=1) + 2 * zs.abs().amax(dim=1) + math.log(z.shape[1] + 1) + 40
+    loss = w * p * (rel_p * size + rel) + 4 * U * want_loss.abs()
+    dense = (w / temperature * p)[:, None] * torch.nan_to_num(plain.log_softmax(z.double() / temperature).exp())
+    grad = (rel + rel_p)[:, None] * (dense + want.abs()) + plain.rounding(want, z.dtype)
+    return torch.nan_to_num(loss), torch.nan_to_num(grad)
+
+
+def check_distill(z, index, value, temperature=1.0, teacher_lse=None, weight=None, **kw):
+    dev = lambda t: None if t is None else t.cuda()
+    loss, dz = b.ds_distill(z.cuda(), pack_pairs(index, value).cuda(), temperature, dev(teacher_lse), dev(weight), **kw)
+    want_loss, want = plain.distill(z, index, value, temperature, teacher_lse, weight)
+    tol_loss, tol = distill_tolerances(z, index, value, temperature, torch.nan_to_num(want_loss), torch.nan_to_num(want), teacher_lse, weight)
+    if loss is not None:
+        check(loss, want_loss, tol_loss, "loss")
+    if dz is not None:
+        assert dz.dtype == z.dtype
+        check(dz, want, tol, "dz")
+    return loss, dz
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,vocab,k", [(1, 1, 1), (3, 2, 5), (5, 63, 1), (4, 64, 64), (7, 300, 256), (9, 1000, 17), (33, 4097, 100),
+                                          (3, 32003, 256), (2, 131072, 64), (1, 262147, 128), (600, 513, 8), (300, 2049, 16), (2, 70001, 3)])
+def test_distill(rows, vocab, k, dtype):
+    rng = np.random.default_rng(rows * 11 + vocab)
+    z = normal(rng, (rows, vocab), dtype, 3.0)
+    index, value = teacher(rng, rows, vocab, k, shuffled=k % 2 == 1)
+    check_distill(z, index, value)
+    weight = torch.from_numpy(rng.random(rows)).float() * 100
+    lse = (torch.logsumexp(value.double() / 2.0, dim=1) + 0.3).float()
+    loss, dz = check_distill(z, index, value, 2.0, lse, weight)
+    # either output alone, the gradient in place, the same bits again
+    loss_only, none = check_distill(z, index, value, 2.0, lse, weight, want_gradient=False)
+    assert none is None and torch.equal(loss_only, loss)
+    none, dz_only = check_distill(z, index, value, 2.0, lse, weight, want_loss=False)
+    assert none is None and torch.equal(dz_only, dz)
+    zd = z.cuda()
+    loss_in, dz_in = b.ds_distill(zd, pack_pairs(index, value).cuda(), 2.0, lse.cuda(), weight.cuda(), dz=zd)
+    assert dz_in.data_ptr() == zd.data_ptr() and torch.equal(dz_in, dz) and torch.equal(loss_in, loss)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab,rows", [(50, 12), (1000, 12), (30001, 12), (200003, 12), (999, 300)])
+def test_distill_masks_padding_and_repeated_indices(vocab, rows, dtype):
+    rng = np.random.default_rng(vocab)
+    k = 24
+    z = normal(rng, (rows, vocab), dtype, 2.0)
+    index, value = teacher(rng, rows, vocab, k)
+    weight = torch.ones(rows)
+    index[0, 5:] = -1                                              # a short list
+    index[1, :] = -1                                               # an empty one
+    index[2, :] = 7                                                # the same index in every entry
+    index[3, 3], index[3, 20], index[3, 21] = 1, 1, 1              # some of them
+    index[4, 2], index[4, 9] = vocab, 2 ** 31 - 1                  # behind the vocabulary
+    value[5, 1:] = -INF                                            # no mass but in one
+    value[6, :] = -INF                                             # no mass at all
+    z[7, :], weight[7] = NAN, 0.0                                  # a padded token
+    z[8, :] = -INF
+    z[8, index[8]] = 1.0                                           # a mask that leaves the listed columns
+    z[9, ::3] = -INF                                               # ... and one that takes some of them away: an infinite loss
+    z[10, :] = -INF                                                # nothing is left
+    z[11, 3] = NAN
+    for lse in (None, torch.full((rows,), 5.0)):
+        check_distill(z, index, value, 1.0, lse, weight)
+    low = torch.finfo(dtype).min                                   # masks of the type's lowest value
+    z = torch.where(torch.isfinite(z), z, torch.full_like(z, low))
+    z[7] = 0.0
+    check_distill(z, index, value, 1.0, None, weight)
+
+
+def test_distill_against_differences():
+    """Central differences of the loss the kernel returns: h = 2^-6 leaves h^2 / 6 times a third derivative (below 1) and the loss's own error over h."""
+    rng = np.random.default_rng(4)
+    rows, vocab, k, h = 6, 40, 10, 2.0 ** -6
+    z = normal(rng, (rows, vocab), F32)
+    index, value = teacher(rng, rows, vocab, k)
+    index[0, 4] = index[0, 5]
+    pairs, weight = pack_pairs(index, value).cuda(), torch.from_numpy(rng.random(rows) + 0.5).float().cuda()
+    _, dz = b.ds_distill(z.cuda(), pairs, 2.0, weight=weight)
+    for v in range(vocab):
+        step = torch.zeros_like(z)
+        step[:, v] = h
+        up, _ = b.ds_distill((z + step).cuda(), pairs, 2.0, weight=weight, want_gradient=False)
+        down, _ = b.ds_distill((z - step).cuda(), pairs, 2.0, weight=weight, want_gradient=False)
+        slope = (up.double() - down.double()) / (2 * h)
+        assert ((slope - dz[:, v].double()).abs() <= 1.5 * (h * h / 6 + 64 * U / h)).all()
+
+
+def test_distill_with_pitches_and_neighbours():
+    rng = np.random.default_rng(6)
+    for dtype in (F32, BF16, F16):
+        for rows, vocab in ((9, 1003), (130, 5001), (2, 70001)):
+            index, value = teacher(rng, rows, vocab, 12)
+            pairs = pack_pairs(index, value).cuda()
+            for shift, pitch, out_shift, out_pitch in ((1, vocab + 2, 3, vocab + 6), (0, vocab, 1, vocab), (8, vocab + 5, 8, vocab + 5)):
+                store = normal(rng, (rows * pitch + 16,), dtype, 2.0).cuda()
+                z = store[shift:shift + rows * pitch].view(rows, pitch)[:, :vocab]
+                out = torch.full((rows * out_pitch + 16,), 55.0, dtype=dtype, device="cuda")
+                dz = out[out_shift:out_shift + rows * out_pitch].view(rows, out_pitch)[:, :vocab]
+                loss, back = b.ds_distill(z, pairs, dz=dz)
+                loss_want, want = b.ds_distill(z.contiguous(), pairs)
+                assert torch.equal(dz, want) and torch.equal(loss, loss_want) and back.data_ptr() == dz.data_ptr()
+                dz.fill_(55.0)
+                assert (out == 55.0).all(), "memory around the gradient was written"
+    z = torch.zeros((4, 100), device="cuda")
+    pairs = torch.zeros((4, 3, 2), dtype=torch.int32, device="cuda")
+    for call in (lambda: b.ds_distill(z, pairs[:3]), lambda: b.ds_distill(z, pairs.long()), lambda: b.ds_distill(z, pairs, -1.0),
+                 lambda: b.ds_distill(z, pairs, weight=torch.ones(3, device="cuda")), lambda: b.ds_distill(z, pairs, weight=torch.ones(4)),
+                 lambda: b.ds_distill(z, pairs, dz=torch.zeros((4, 99), device="cuda")), lambda: b.ds_distill(z, pairs, want_loss=False, want_gradient=False),
+                 lambda: b.ds_distill(z, torch.zeros((4, 257, 2), dtype=torch.int32, device="cuda")), lambda: b.ds_distill(z[:, 1:], pairs, dz=z[:, :99]),
+                 lambda: b.ds_distill(z, pairs, dz=torch.zeros_like(z), want_gradient=False)):
+        with pytest.raises(b.DsqError) as e:
+            call()
+        assert e.value.status == b.DS_EINVAL
+    loss, dz = b.ds_distill(z[:0], pairs[:0])
+    assert tuple(loss.shape) == (0,) and tuple(dz.shape) == (0, 100)
+
+
+# ---- streams, graphs, all together -----------------------------------------------------------------
+
+def calls(rng, tokens, rows, cols, block, vocab, dtype):
+    """Each operator on inputs of its own: (inputs, function of them)."""
+    msg = plain.random_message(rows, cols, block, rng)[0].cuda()
+    x, dy = normal(rng, (tokens, cols), dtype).cuda(), normal(rng, (tokens, rows), dtype).cuda()
+    z = normal(rng, (tokens, vocab), dtype, 3.0).cuda()
+    pairs = pack_pairs(*teacher(rng, tokens, vocab, 20)).cuda()
+    return [((msg, x), lambda m, v, **kw: (b.ds_product(m, v, rows, block, **kw),)),
+            ((msg, dy), lambda m, v, **kw: (b.ds_product_gradient(m, v, cols, block, **kw),)),
+            ((z,), lambda v, **kw: b.ds_top_logits(v, 50, **kw)),
+            ((z, pairs), lambda v, p, **kw: b.ds_distill(v, p, **kw))]
+
+
+@pytest.mark.parametrize("tokens,rows,cols,block,vocab", [(1, 500, 1000, 64, 131072), (20, 300, 4000, 256, 9000), (200, 64, 512, 512, 2100)])
+def test_captured_calls_repeat_themselves_on_what_the_arrays_hold(tokens, rows, cols, block, vocab):
+    for dtype in (F32, BF16):
+        for inputs, f in calls(np.random.default_rng(tokens), tokens, rows, cols, block, vocab, dtype):
+            f(*inputs)                                             # (loads the kernels)
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                out = f(*inputs)
+            for turn in range(3):
+                if turn:
+                    last = inputs[-1] if inputs[-1].dtype == dtype else inputs[0]
+                    last.copy_(last.flip(0).flip(1) * 1.25)
+                graph.replay()
+                torch.cuda.synchronize()
+                want = f(*inputs)
+                torch.cuda.synchronize()
+                for got, w in zip(out, want):
+                    assert torch.equal(got, w), f"replay {turn} differs"
+
+
+def test_calls_on_two_streams_share_nothing():
+    first = calls(np.random.default_rng(1), 30, 400, 3000, 128, 40000, BF16)
+    second = calls(np.random.default_rng(2), 2, 900, 2000, 64, 131072, F32)
+    want = [[f(*inputs) for inputs, f in side] for side in (first, second)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for turn in range(5):
+        for q in range(4):
+            for s, side in enumerate((first, second)):
+                inputs, f = side[q]
+                got[s].append(f(*inputs, stream=streams[s]))
+    torch.cuda.synchronize()
+    for s in range(2):
+        for n, outs in enumerate(got[s]):
+            for a, w in zip(outs, want[s][n % 4]):
+                assert torch.equal(a, w)
+
+
+@pytest.mark.parametrize("variant", [0, 1])
+def test_learning_from_a_neighbours_message(variant):
+    """The operators as a run uses them: each worker's model is a matrix (classes x features) that answers with logits.  Worker i's right-hand
+    neighbour answers out of its message of the last step, its largest logits are what i learns from, and the gradient goes into ds_step.
+    Every result is compared with 64 bits from the messages and the state themselves."""
+    n, V, D, tokens, k, T = 5, 160, 128, 24, 16, 2.0
+    cfg, keep = b.make_config(n, V * D + 37, wl.TOPO_RING, wl.KIND_QUANT_MAXABS, 0.05, 0.3, bits=4, block=64, seed=3)
+    ds = b.DeepSqueeze(cfg, keep, {"variant": variant})
+    rng = np.random.default_rng(8)
+    with pytest.raises(b.DsqError) as e:
+        ds.ds_product(0, torch.zeros((1, D), device="cuda"), V)
+    assert e.value.status == b.DS_ESTATE
+    x0 = (rng.standard_normal((n, V * D + 37)) * 0.1).astype(np.float32)
+    ds.ds_write_state(x0, np.zeros_like(x0), 0)
+    g = torch.zeros((n, (V * D + 37 + 3) // 4 * 4), device="cuda")
+    ds.ds_step(g)
+    features = normal(rng, (tokens, D), F32)
+    fd = features.cuda()
+    for step in range(3):
+        messages = ds.ds_read_messages().reshape(n, -1)
+        state, _ = ds.ds_read_state()
+        g.zero_()
+        for i in range(n):
+            j = (i + 1) % n
+            answers = ds.ds_product(j, fd, V)
+            m = plain.decode(messages[j][:b.ds_matrix_bytes(V, D, 64)], V, D, 64)
+            want = features.double() @ m.t().contiguous()
+            check(answers, want, product_tolerance(want, features.double(), m.t().abs().contiguous() + 0.02, F32), "answers")
+            pairs, lse = b.ds_top_logits(answers, k, T)
+            assert torch.equal(pairs[..., 0].cpu().long(), plain.top(answers.cpu(), k))
+            mine = torch.from_numpy(state[i, :V * D].reshape(V, D))
+            z = (features @ mine.t()).contiguous()
+            index, value = pairs[..., 0].cpu().long(), pairs.view(F32)[..., 1].cpu()
+            loss, dz = check_distill(z, index, value, T, lse.cpu(), torch.full((tokens,), 1.0 / tokens))
+            back = ds.ds_product_gradient(j, dz, D)                # ... and through the neighbour's packed layer
+            want = dz.cpu().double() @ m
+            check(back, want, product_tolerance(want, dz.cpu().double(), m.abs() + 0.02, F32), "gradient through the message")
+            g[i, :V * D] = (dz.t().contiguous() @ fd).reshape(-1)
+        ds.ds_step(g)
+    # a part of the vector that starts at a later block, and what is refused
+    messages = ds.ds_read_messages().reshape(n, -1)
+    y = ds.ds_product(2, fd[:3, :64].contiguous(), 11, first=64 * 5)
+    m = plain.decode(messages[2][36 * 5:36 * 16], 11, 64, 64)
+    want = features[:3, :64].double() @ m.t().contiguous()
+    check(y, want, product_tolerance(want, features[:3, :64].double(), m.t().abs().contiguous() + 0.02, F32), "part")
+    for call in (lambda: ds.ds_product(n, fd, V), lambda: ds.ds_product(-1, fd, V), lambda: ds.ds_product(0, fd, V, first=32),
+                 lambda: ds.ds_product(0, fd, V + 1), lambda: ds.ds_product(0, fd[:, :100].contiguous(), 3), lambda: ds.ds_product(0, fd, V, first=-64)):
+        with pytest.raises(b.DsqError) as e:
+            call()
+        assert e.value.status == b.DS_EINVAL
+    ds.ds_destroy()
+    other, keep = b.make_config(4, 1000, wl.TOPO_RING, wl.KIND_QUANT_MAXABS, 0.05, 0.3, bits=2, block=64)
+    ds = b.DeepSqueeze(other, keep)
+    with pytest.raises(b.DsqError) as e:
+        ds.ds_product(0, fd[:, :64].contiguous(), 2)
+    assert e.value.status == b.DS_EINVAL
+    ds.ds_destroy()
