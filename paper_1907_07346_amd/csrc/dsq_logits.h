@@ -19,6 +19,9 @@ __device__ __forceinline__ uint32_t logit_key(float z) {
 __device__ __forceinline__ uint64_t logit_rank(float z, uint32_t index) { return (uint64_t)logit_key(z) << 32 | (uint32_t)~index; }
 __device__ __forceinline__ uint32_t rank_index(uint64_t rank) { return ~(uint32_t)rank; }
 
+// 2^x as the hardware has it: results below 2^-126 are 0.
+__device__ __forceinline__ float power2(float x) { return __builtin_amdgcn_exp2f(x); }
+
 // sum over some logits of 2^(scale (z - max)), with scale = log2(e) / temperature.  The maximum that is subtracted is taken as 0 where it
 // is infinite: a row of minus infinities has sum 0, one with plus infinity has an infinite sum.
 struct Spread {
