@@ -1,48 +1,82 @@
 // Products with a matrix that is held as messages (ds_product): y = x M^T, M's rows as 4-bit codes with a scale per block.
 //
-// What bounds it is reading the message, 0.53 bytes a weight, as long as 64 tokens or fewer share it.  So the codes go
-// straight from memory into matrix instructions: a wave takes 16 (or 32) rows and 128 columns at a time, lane l holds 32 codes of row
-// l % 16 (one 16-byte load) and its block's scale, and each word of eight codes becomes an operand with eight instructions (dsq_codes.h).  With the tokens as
-// the other operand a lane's results all belong to its own row, so the block's scale is one factor per lane.
-//   x is laid out once per workgroup, in LDS, as the operands need it: units of eight columns in the order in which a word's codes come
-// out, zero behind the last column.  The waves of a workgroup share it; they split its rows, and, where there are few rows, its columns,
-// too (joined in LDS).  Columns are also split over workgroups where x does not fit into LDS; then fp32 partial sums go through work_dev and a
-// second launch adds them, in the order of the columns.
+// Reading the message, 0.53 bytes a weight, is what cannot be done without, and leaves time for some four vector instructions a weight's
+// share of a lane.  Codes are bytes after half an instruction each, so x is made of bytes, too, and the products are integers: per token
+// and 128 columns ("chunk"; 64 where a block is 64), x = 2^e v with integers v of 16 bits (24 for fp32), written as two (three) signed bytes, most of which an i8 matrix instruction
+// takes as rows of their own.  All sums inside a chunk are exact; 15 sum v, which takes codes 0 .. 15 to 2 code - 15, is where they start.  What is rounded is v:
+// 2^-15 (2^-23) of the largest |x| next to it at most, which the same block's scale multiplies and no code drops, against the 2^-8 or 2^-11 of
+// y's own rounding for 16-bit types (2^-24 for fp32).
+//   A wave takes 16 (or 32) rows and a chunk at a time: lane (n, j) = (l % 16, l / 16) holds 32 codes of row n (one 16-byte load) and the scale of its
+// block, which is one factor for all of the lane's results.  x's bytes lie in LDS in the order in which codes come out of a word.  Up to 8 tokens (4 for
+// fp32) each workgroup makes them itself; for more, a launch before makes them once, in work_dev.  The waves of a workgroup split its rows and, where there are few, its
+// columns (joined in LDS); where there are too few rows for the GPU, workgroups split the columns, too, and one more launch adds their sums.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
 
 namespace dsq {
 namespace {
 
-constexpr int kWaves = 8, kChunk = 128;                           // waves of a workgroup; columns a wave takes at a time
+constexpr int kWaves = 8, kThreads = kWaves * 64, kChunk = 128;   // of a workgroup; columns a wave takes at a time
 constexpr uint32_t kPanel = 64 * 1024;                            // bytes of LDS for x: two workgroups fit on a compute unit
 constexpr uint64_t kTokens = 64;                                  // of a launch
 constexpr uint64_t kGroupsOfLaunch = 1u << 22;                    // a launch dimension holds fewer than 2^32 work-items
 
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
+// How x is written as bytes: `digits` rows of a matrix instruction per token, of which `stride` are set aside.
+template <typename T>
+struct Digits {
+    static constexpr int digits = 2, stride = 2, exponent = 14;   // |v| <= 127 * 256 + 127, below 2^15
+    static constexpr float most = 32639.f;
+};
+template <>
+struct Digits<float> {
+    static constexpr int digits = 3, stride = 4, exponent = 22;   // |v| <= 127 (2^16 + 2^8 + 1), below 2^23
+    static constexpr float most = 8355711.f;
+};
+template <typename T>
+constexpr int kTileTokens = 16 / Digits<T>::stride;               // tokens of a matrix instruction
+
 struct ProductPlan {
     uint32_t row_waves;                                           // waves side by side; the other kWaves / row_waves split the columns
     uint32_t parts, part_chunks;                                  // workgroups that split the columns, and the chunks of each
-    uint32_t panel_chunks;                                        // chunks of x that are in LDS at a time
+    uint32_t stage_chunks;                                        // chunks of x that are in LDS at a time
+    uint32_t wave_rows;                                           // one token: rows of a wave
 };
 
 struct ProductShape : ProductArgs {
     ProductPlan plan;
     uint64_t row0;
+    const uint8_t* panel;                                         // x as bytes, one record per chunk (see Record), or nullptr
     float* partial;                                               // parts x tokens x rows, or nullptr
+};
+
+// One chunk of x: the digits, [matrix instruction][j][row][16 columns]; the sums the products start from, -15 times the digits' sum, [block][row]
+// (two blocks where a block is 64 columns); and per token what v counts, 2^e.  Rows: digit d of token t is row stride t + d.
+template <typename T, int TT, bool NARROW>
+struct Record {
+    static constexpr uint32_t H = NARROW ? 2 : 1, sums = H * TT * 64, units = H * TT * 32;
+    __host__ __device__ static uint32_t rows(uint32_t tokens) { return tokens * Digits<T>::stride; }
+    __host__ __device__ static uint32_t bytes(uint32_t tokens) { return 128 * rows(tokens) + sums + units; }
+    __device__ static i32x4* digits(uint8_t* r) { return reinterpret_cast<i32x4*>(r); }
+    __device__ static int32_t* start(uint8_t* r, uint32_t tokens) { return reinterpret_cast<int32_t*>(r + 128 * rows(tokens)); }
+    __device__ static float* unit(uint8_t* r, uint32_t tokens) { return reinterpret_cast<float*>(r + 128 * rows(tokens) + sums); }
 };
 
 // One weight after the other, as the formula has it: for a result that is not finite.
 template <typename T>
-__device__ __noinline__ float product_in_order(const ProductArgs& a, uint64_t r, uint64_t t) {
+__device__ __forceinline__ float product_in_order(const ProductArgs& a, uint64_t r, uint64_t t) {
     const uint8_t* row = a.msg + r * a.row_bytes;
     const T* x = static_cast<const T*>(a.in) + t * a.in_ld;
     const uint32_t per = a.block / 8;
     float sum = 0.f;
+#pragma unroll 1
     for (uint64_t w = 0; 8 * w < a.cols; ++w) {
         const uint8_t* block = row + w / per * (4 + a.block / 2);
         const float unit = *reinterpret_cast<const float*>(block) * (16.f / 15.f);
         const uint32_t word = *reinterpret_cast<const uint32_t*>(block + 4 + 4 * (w % per));
         float part = 0.f;                                         // a code counts as (2 code - 15) / 16: no sum is infinite before y is
+#pragma unroll 1
         for (int e = 0; e < 8; ++e)
             if (8 * w + e < a.cols) part = fmaf((float)(2 * (int)(word >> (4 * e) & 15u) - 15) * 0.0625f, (float)x[8 * w + e], part);
         sum = fmaf(unit, part, sum);
@@ -58,8 +92,8 @@ __device__ __forceinline__ void product_store(const ProductArgs& a, uint64_t r, 
 }
 
 // 128 columns of a lane's row: four words and the scales of the block they lie in (of the two blocks, where a block is 64 columns).
-// Word t goes with words t of the other lanes of the row, lanes j = 0 .. 3, into one matrix instruction, and instructions must not mix blocks:
-// word t of lane j starts at column 32 j + 8 t, or at 64 floor(t / 2) + 16 j + 8 (t % 2) where a block is 64 columns.
+// Words 2 h and 2 h + 1 of all lanes j of the row go into matrix instruction h, which must not mix blocks: word t of lane j starts at
+// column 32 j + 8 t, or at 64 floor(t / 2) + 16 j + 8 (t % 2) where a block is 64 columns.
 template <bool NARROW>
 struct Codes {
     uint32_t w[4];
@@ -67,9 +101,6 @@ struct Codes {
 };
 template <bool NARROW>
 __device__ __forceinline__ uint32_t word_column(uint32_t t, uint32_t j) { return NARROW ? 64 * (t / 2) + 16 * j + 8 * (t % 2) : 32 * j + 8 * t; }
-// ... and the other way: (t, j) of the eight columns that start at 8 u.
-template <bool NARROW>
-__device__ __forceinline__ uint32_t column_place(uint32_t u) { return NARROW ? (u / 8 * 2 + u % 2) * 4 + u % 8 / 2 : u % 4 * 4 + u / 4; }
 
 template <bool NARROW>
 __device__ __forceinline__ void load_codes(Codes<NARROW>& c, const uint8_t* row, uint32_t block_log2, uint64_t col, uint32_t j) {
@@ -101,14 +132,91 @@ __device__ __forceinline__ void load_codes_tail(Codes<NARROW>& c, const uint8_t*
     }
 }
 
-template <typename T, int TT, int RT, bool NARROW>
-__global__ void __launch_bounds__(kWaves * 64, 2) product_kernel(ProductShape a) {
-    using O = typename Operand<T>::type;
-    constexpr int P = Operand<T>::pieces;
-    extern __shared__ __align__(16) uint8_t lds[];
-    Eight<O>* panel = reinterpret_cast<Eight<O>*>(lds);           // [chunk][t][piece][j][token]
+// 2^p, for p from -126 to 127.
+__device__ __forceinline__ float power2_of(int p) { return __uint_as_float((uint32_t)(p + 127) << 23); }
+// The largest p for which 2^p x is below 2^(exponent + 1) and at most `limit`, of an |x| with these bits (not above 127: what is lost there is
+// below 2^-127).
+__device__ __forceinline__ int power_of(uint32_t bits, int exponent, float limit) {
+    const int p = exponent + 127 - (int)(bits >> 23), q = p > 126 ? 126 : p;
+    return __uint_as_float(bits) * power2_of(q) > limit ? q - 1 : q;
+}
+
+// Sixteen adjacent lanes, lane u with columns 8 u .. 8 u + 7 of a chunk, write a token's part of the chunk's record.
+template <typename T, int TT, bool NARROW>
+__device__ void make_digits(const ProductArgs& a, uint64_t chunk, uint32_t tok, uint32_t u, uint8_t* record) {
+    using D = Digits<T>;
+    using R = Record<T, TT, NARROW>;
+    constexpr int LANES = NARROW ? 8 : 16;                        // of a block
     const uint32_t tokens = (uint32_t)a.tokens;
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, n = lane & 15, j = lane >> 4;
+    const uint64_t col = chunk * kChunk + 8 * u;
+    const T* x = static_cast<const T*>(a.in) + tok * a.in_ld + col;
+    float v[8];
+    if (col + 8 <= a.cols) {
+        typedef T Raw __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+        const Raw raw = *reinterpret_cast<const Raw*>(x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)raw[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = col + e < a.cols ? (float)x[e] : 0.f;
+    }
+    uint32_t most = 0;                                            // the bits of the largest |x|; NaN is above all
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t bits = __float_as_uint(v[e]) & 0x7FFFFFFFu;
+        most = bits > most ? bits : most;
+    }
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) {
+        const uint32_t other = (uint32_t)__shfl_xor((int)most, o);
+        most = other > most ? other : most;
+    }
+    const int power = power_of(most, D::exponent, D::most);
+    const bool finite = most < 0x7F800000u;
+    const float to = power2_of(power);
+    uint32_t bytes[D::digits][2];
+    int32_t sum[D::digits];
+#pragma unroll
+    for (int d = 0; d < D::digits; ++d) bytes[d][0] = bytes[d][1] = 0, sum[d] = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        int32_t rest = finite ? (int32_t)rintf(v[e] * to) : 0;
+#pragma unroll
+        for (int d = D::digits - 1; d >= 0; --d) {                // the last digit is the lowest
+            const int32_t digit = d ? (int32_t)(int8_t)rest : rest;
+            rest = (rest - digit) >> 8;
+            sum[d] += digit;
+            bytes[d][e % 2] |= ((uint32_t)digit & 255u) << (8 * (e / 2));
+        }
+    }
+    const uint32_t t = NARROW ? u / 8 * 2 + u % 2 : u % 4, j = NARROW ? u % 8 / 2 : u / 4, rows = R::rows(tokens);
+#pragma unroll
+    for (int d = 0; d < D::digits; ++d) {
+        const uint32_t at = (((t / 2) * 4 + j) * rows + tok * D::stride + d) * 16 + 8 * (t % 2);
+        *reinterpret_cast<u32x2*>(record + at) = u32x2{bytes[d][0], bytes[d][1]};
+#pragma unroll
+        for (int o = 1; o < LANES; o <<= 1) sum[d] += __shfl_xor(sum[d], o);
+        if (u % LANES == 0) R::start(record, tokens)[u / LANES * (TT * 16) + tok * D::stride + d] = -15 * sum[d];
+    }
+    if (u % LANES == 0) R::unit(record, tokens)[u / LANES * (TT * 8) + tok] = finite ? power2_of(-power) : __builtin_nanf("");
+}
+
+// x as bytes, for all workgroups: 16 threads per chunk and token.
+template <typename T, int TT, bool NARROW>
+__global__ void __launch_bounds__(256) product_digits_kernel(ProductShape a, uint8_t* panel) {
+    const uint64_t chunk = blockIdx.x;
+    for (uint32_t tok = threadIdx.x / 16 + 16 * blockIdx.y; tok < a.tokens; tok += 16 * gridDim.y)
+        make_digits<T, TT, NARROW>(a, chunk, tok, threadIdx.x % 16, panel + chunk * Record<T, TT, NARROW>::bytes((uint32_t)a.tokens));
+}
+
+template <typename T, int TT, int RT, bool NARROW>
+__global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
+    using D = Digits<T>;
+    using R = Record<T, TT, NARROW>;
+    constexpr int H = NARROW ? 2 : 1, PER = 4 / D::stride;        // blocks of a chunk; tokens of a lane and matrix instruction
+    extern __shared__ __align__(16) uint8_t lds[];
+    const uint32_t tokens = (uint32_t)a.tokens, x_rows = R::rows(tokens), record = R::bytes(tokens);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane & 15, j = lane >> 4;
     const uint32_t row_waves = a.plan.row_waves, col_waves = kWaves / row_waves;
     const uint32_t rw = wave % row_waves, cw = wave / row_waves;
     const uint64_t c0 = (uint64_t)blockIdx.y * a.plan.part_chunks, all_chunks = (a.cols + kChunk - 1) / kChunk;
@@ -122,104 +230,96 @@ __global__ void __launch_bounds__(kWaves * 64, 2) product_kernel(ProductShape a)
         const uint64_t at = first + 16 * r + n;
         row[r] = a.msg + (at < a.rows ? at : a.rows - 1) * a.row_bytes;
     }
-    uint32_t tok_at[TT];
+    uint32_t x_at[TT];                                            // the lane's row of x in each tile; rows that are not there repeat the last
 #pragma unroll
-    for (int t = 0; t < TT; ++t) tok_at[t] = 16 * t + n < tokens ? 16 * t + n : tokens - 1;
-    f32x4 sum[RT][TT];
+    for (int t = 0; t < TT; ++t) x_at[t] = j * x_rows + (16 * t + n < x_rows ? 16 * t + n : x_rows - 1);
+    float sum[RT][TT][PER];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int t = 0; t < TT; ++t) sum[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) sum[r][t][i] = 0.f;
 
     auto use = [&](const Codes<NARROW> (&c)[RT], uint32_t chunk) {
+        uint8_t* rec = lds + chunk * record;
+        const i32x4* digits = R::digits(rec);
+        i32x4 codes[RT][2];
+        float unit[RT][H];
 #pragma unroll
-        for (int h = 0; h < (NARROW ? 2 : 1); ++h) {
-            f32x4 part[RT][TT];
+        for (int r = 0; r < RT; ++r) {
 #pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                f32x4 off = {0.f, 0.f, 0.f, 0.f};
-                constexpr int words = NARROW ? 2 : 4;
+            for (int h = 0; h < 2; ++h)
+                codes[r][h] = i32x4{(int)(c[r].w[2 * h] << 1 & 0x1E1E1E1Eu), (int)(c[r].w[2 * h] >> 3 & 0x1E1E1E1Eu),
+                                    (int)(c[r].w[2 * h + 1] << 1 & 0x1E1E1E1Eu), (int)(c[r].w[2 * h + 1] >> 3 & 0x1E1E1E1Eu)};
 #pragma unroll
-                for (int w = 0; w < words; ++w)
+            for (int b = 0; b < H; ++b) unit[r][b] = c[r].scale[b] * (1.f / 15.f);
+        }
 #pragma unroll
-                    for (int p = 0; p < P; ++p)
-                        off = matrix_fma(panel[(((chunk * 4 + h * words + w) * P + p) * 4 + j) * tokens + tok_at[t]], centre_operand<O>(), off);
-                off = -off;
+        for (int t = 0; t < TT; ++t) {
+            const i32x4 x0 = digits[x_at[t]], x1 = digits[4 * x_rows + x_at[t]];
 #pragma unroll
-                for (int r = 0; r < RT; ++r) part[r][t] = off;
-            }
+            for (int b = 0; b < H; ++b) {
+                float count[PER];
 #pragma unroll
-            for (int w = 0; w < (NARROW ? 2 : 4); ++w) {
-                Eight<O> codes[RT];
+                for (int i = 0; i < PER; ++i) count[i] = R::unit(rec, tokens)[b * (TT * 8) + (4 * t + j) * PER + i];
+                const i32x4 start = *reinterpret_cast<const i32x4*>(R::start(rec, tokens) + b * (TT * 16) + 16 * t + 4 * j);
 #pragma unroll
-                for (int r = 0; r < RT; ++r) codes[r] = code_operand<O>(c[r].w[(NARROW ? 2 * h : 0) + w]);
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int t = 0; t < TT; ++t) {
-                        const Eight<O> x = panel[(((chunk * 4 + (NARROW ? 2 * h : 0) + w) * P + p) * 4 + j) * tokens + tok_at[t]];
-#pragma unroll
-                        for (int r = 0; r < RT; ++r) part[r][t] = matrix_fma(x, codes[r], part[r][t]);
+                for (int r = 0; r < RT; ++r) {
+                    i32x4 p;
+                    if constexpr (NARROW) {
+                        p = __builtin_amdgcn_mfma_i32_16x16x64_i8(b ? x1 : x0, codes[r][b], start, 0, 0, 0);
+                    } else {
+                        p = __builtin_amdgcn_mfma_i32_16x16x64_i8(x0, codes[r][0], start, 0, 0, 0);
+                        p = __builtin_amdgcn_mfma_i32_16x16x64_i8(x1, codes[r][1], p, 0, 0, 0);
                     }
-            }
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const float unit = c[r].scale[h] * kPerCode;
-#pragma unroll
-                for (int t = 0; t < TT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[r][t][i] = fmaf(unit, part[r][t][i], sum[r][t][i]);
+                    for (int i = 0; i < PER; ++i) {
+                        float v;
+                        if constexpr (D::digits == 2) v = (float)((p[2 * i] << 8) + p[2 * i + 1]);
+                        else v = fmaf(fmaf((float)p[0], 256.f, (float)p[1]), 256.f, (float)p[2]);
+                        sum[r][t][i] = fmaf(unit[r][b] * count[i], v, sum[r][t][i]);
+                    }
+                }
             }
         }
     };
-    // x goes through LDS in stages of panel_chunks; codes of the next chunks are under way while these are multiplied
-    constexpr int AHEAD = 2;
+    // x goes through LDS in stages; codes of the next chunks are under way while these are multiplied
+    constexpr int AHEAD = RT == 1 ? 4 : 2;
     Codes<NARROW> ring[AHEAD][RT];
-    for (uint32_t from = 0; from < chunks; from += a.plan.panel_chunks) {
-        const uint32_t count = chunks - from < a.plan.panel_chunks ? chunks - from : a.plan.panel_chunks;
+    for (uint32_t from = 0; from < chunks; from += a.plan.stage_chunks) {
+        const uint32_t count = chunks - from < a.plan.stage_chunks ? chunks - from : a.plan.stage_chunks;
         const uint64_t col0 = (c0 + from) * kChunk;
         const uint32_t whole = (uint32_t)(a.cols / kChunk - (c0 + from) < count ? a.cols / kChunk - (c0 + from) : count);   // chunks without a ragged end
+        const uint32_t mine = cw < whole ? (whole - cw + col_waves - 1) / col_waves : 0;   // of this wave
+        auto fetch = [&](Codes<NARROW> (&c)[RT], uint32_t q) {    // the wave's q-th chunk, or again its last: no branch, so that loads can be counted
+            const uint32_t chunk = cw + (q < mine ? q : mine - 1) * col_waves;
 #pragma unroll
-        for (int s = 0; s < AHEAD; ++s)
-            if (cw + s * col_waves < whole)
+            for (int r = 0; r < RT; ++r) load_codes<NARROW>(c[r], row[r], block_log2, col0 + (uint64_t)chunk * kChunk, j);
+        };
+        if (mine)
 #pragma unroll
-                for (int r = 0; r < RT; ++r) load_codes<NARROW>(ring[s][r], row[r], block_log2, col0 + (uint64_t)(cw + s * col_waves) * kChunk, j);
+            for (int s = 0; s < AHEAD; ++s) fetch(ring[s], s);
         if (from) __syncthreads();
-        // x as operands: a thread takes eight columns of a token at a time
-        for (uint32_t q = threadIdx.x; q < count * 16 * tokens; q += kWaves * 64) {
-            const uint32_t tok = q / (count * 16), u = q % (count * 16);
-            const uint64_t col = (c0 + from) * kChunk + 8 * u;
-            const T* x = static_cast<const T*>(a.in) + tok * a.in_ld + col;
-            float v[8];
-            if (col + 8 <= a.cols) {
-                typedef T Raw __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-                const Raw raw = *reinterpret_cast<const Raw*>(x);
-    #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = (float)raw[e / 2 + 4 * (e % 2)];
-            } else {
-    #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = col + e / 2 + 4 * (e % 2) < a.cols ? (float)x[e / 2 + 4 * (e % 2)] : 0.f;
+        if (TT == 1) {
+            for (uint32_t q = threadIdx.x / 16; q < count * tokens; q += kThreads / 16) {
+                const uint32_t tok = q / count, chunk = q % count;
+                make_digits<T, TT, NARROW>(a, c0 + from + chunk, tok, threadIdx.x % 16, lds + chunk * record);
             }
-            Eight<O> out[P];
-            split_operand<O, P>(v, out);
-            const uint32_t place = column_place<NARROW>(u % 16), base = (u / 16 * 4 + place / 4) * P;
-    #pragma unroll
-            for (int p = 0; p < P; ++p) panel[((base + p) * 4 + place % 4) * tokens + tok] = out[p];
+        } else {
+            const u32x4* src = reinterpret_cast<const u32x4*>(a.panel + (c0 + from) * record);
+            for (uint32_t q = threadIdx.x; q < count * record / 16; q += kThreads) reinterpret_cast<u32x4*>(lds)[q] = src[q];
         }
         __syncthreads();
-        for (uint32_t c = cw; c < whole; c += AHEAD * col_waves) {
+        for (uint32_t q = 0; q < mine; q += AHEAD) {
 #pragma unroll
             for (int s = 0; s < AHEAD; ++s) {
-                const uint32_t here = c + s * col_waves;
-                if (here >= whole) break;
+                if (q + s >= mine) break;
                 Codes<NARROW> now[RT];
 #pragma unroll
                 for (int r = 0; r < RT; ++r) now[r] = ring[s][r];
-                if (here + AHEAD * col_waves < whole)
-#pragma unroll
-                    for (int r = 0; r < RT; ++r)
-                        load_codes<NARROW>(ring[s][r], row[r], block_log2, col0 + (uint64_t)(here + AHEAD * col_waves) * kChunk, j);
-                use(now, here);
+                fetch(ring[s], q + s + AHEAD);
+                use(now, cw + (q + s) * col_waves);
             }
         }
         if (whole < count && whole % col_waves == cw) {
@@ -233,31 +333,212 @@ __global__ void __launch_bounds__(kWaves * 64, 2) product_kernel(ProductShape a)
     // the waves that split the columns: join in LDS
     if (col_waves > 1) {
         __syncthreads();
-        f32x4* joined = reinterpret_cast<f32x4*>(lds);
+        float* joined = reinterpret_cast<float*>(lds);            // [wave][tile of rows][tile of tokens][token][lane]
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int t = 0; t < TT; ++t) joined[((wave * RT + r) * TT + t) * 64 + lane] = sum[r][t];
+            for (int t = 0; t < TT; ++t)
+#pragma unroll
+                for (int i = 0; i < PER; ++i) joined[(((wave * RT + r) * TT + t) * PER + i) * 64 + lane] = sum[r][t][i];
         __syncthreads();
         if (cw != 0) return;
         for (uint32_t c = 1; c < col_waves; ++c)
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
-                for (int t = 0; t < TT; ++t) sum[r][t] += joined[(((c * row_waves + rw) * RT + r) * TT + t) * 64 + lane];
+                for (int t = 0; t < TT; ++t)
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) sum[r][t][i] += joined[((((c * row_waves + rw) * RT + r) * TT + t) * PER + i) * 64 + lane];
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int t = 0; t < TT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < PER; ++i) {
                 const uint64_t at = first + 16 * r + n;
-                const uint32_t tok = 16 * t + 4 * j + i;
+                const uint32_t tok = (4 * t + j) * PER + i;
                 if (at >= a.rows || tok >= tokens) continue;
                 if (a.partial) a.partial[((uint64_t)blockIdx.y * tokens + tok) * a.rows + at] = sum[r][t][i];
                 else product_store<T>(a, at, tok, sum[r][t][i]);
             }
+}
+
+// One token: rows of codes are read whole, which costs the memory pipeline a third of what sixteen rows of 64 bytes cost a load, and meet x in
+// registers.  A lane keeps 32 columns of x for all the rows of its wave, G lanes hold a row, and a load takes 64 / G rows of 32 G columns.  x is
+// written in digits of four bits here, 16^d apart, 4 of them (6 for fp32), with an exponent per 32 columns: eight codes (less 8, so that they are
+// signed) meet eight digits in one instruction, 0.6 instructions a weight.  The lanes of a row are joined by a tree of lane shifts.
+constexpr uint32_t kLaneCols = 32;
+template <typename T>
+struct Nibbles {
+    static constexpr int digits = 4, exponent = 14;
+    static constexpr float most = 30583.f;                        // 7 (16^3 + 16^2 + 16 + 1)
+};
+template <>
+struct Nibbles<float> {
+    static constexpr int digits = 6, exponent = 22;
+    static constexpr float most = 7829367.f;
+};
+
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ float add_shifted(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROW_MASK, 0xF, false));
+}
+// The sum over G adjacent lanes, in the last of them.
+template <int G>
+__device__ __forceinline__ float lanes_total(float v) {
+    v = add_shifted<0x111, 0xF>(v);
+    v = add_shifted<0x112, 0xF>(v);
+    if constexpr (G >= 16) {
+        v = add_shifted<0x114, 0xF>(v);
+        v = add_shifted<0x118, 0xF>(v);
+    }
+    if constexpr (G >= 32) v = add_shifted<0x142, 0xA>(v);
+    if constexpr (G >= 64) v = add_shifted<0x143, 0xC>(v);
+    return v;
+}
+
+template <typename T, int G>
+__global__ void __launch_bounds__(kThreads) product_one_kernel(ProductShape a) {
+    using D = Nibbles<T>;
+    constexpr int AT_ONCE = 64 / G, AHEAD = 4;                    // rows of a load, loads under way
+    extern __shared__ __align__(16) uint8_t lds[];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / G, l = lane % G;
+    const uint32_t row_waves = a.plan.row_waves, col_waves = kWaves / row_waves, rw = wave % row_waves, cw = wave / row_waves;
+    const uint32_t wave_rows = a.plan.wave_rows, rows_here = row_waves * wave_rows, loads = wave_rows / AT_ONCE;
+    const uint64_t first = a.row0 + (uint64_t)blockIdx.x * rows_here;
+    const uint32_t block_log2 = 31 - __builtin_clz(a.block), pitch = 4 + a.block / 2;
+    const uint32_t lanes = col_waves * G;                         // lanes that hold different columns ...
+    i32x4* digits = reinterpret_cast<i32x4*>(lds);                // ... and their digits, [digit][lane]; then sum v and what v counts
+    int32_t* sums = reinterpret_cast<int32_t*>(digits + D::digits * lanes);
+    float* units = reinterpret_cast<float*>(sums + lanes);
+    float* totals = units + lanes;                                // [column wave][row of the workgroup]
+    float* mine = totals + cw * rows_here + rw * wave_rows;
+    const T* x = static_cast<const T*>(a.in);
+    for (uint64_t slice = 0; slice < a.cols; slice += lanes * kLaneCols) {
+        const uint64_t col = slice + (cw * G + l) * kLaneCols;
+        // Lanes behind the last column read words of the first, and count for nothing.  The last lane with columns may have fewer than four
+        // words: it reads the four that end with the row instead, and has digits for its own.  (A row has four: cols > 24.)
+        const bool some = col < a.cols;
+        const uint64_t from_col = some ? col : slice;
+        auto missing_words = [&](uint64_t c) { return c < a.cols && c + 24 >= a.cols ? 4 - (uint32_t)((a.cols - c + 7) / 8) : 0u; };
+        const uint64_t scale_at = (from_col >> block_log2) * pitch;
+        const uint64_t codes_at = scale_at + 4 + (from_col & (a.block - 1)) / 2 - 4 * missing_words(col);
+        struct Load {
+            u32x4 w;
+            float scale;
+        };
+        auto fetch = [&](Load& v, uint32_t q) {                   // the q-th rows, or again the last: no branch, so that loads can be counted
+            const uint64_t at = first + rw * wave_rows + (q < loads ? q : loads - 1) * AT_ONCE + g, row = at < a.rows ? at : a.rows - 1;
+            const uint8_t* p = a.msg + row * a.row_bytes;
+            v.scale = *reinterpret_cast<const float*>(p + scale_at);
+            v.w = *reinterpret_cast<const u32x4_at4*>(p + codes_at);
+        };
+        Load ring[AHEAD];
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) fetch(ring[s], s);
+
+        // the workgroup writes this stretch of x in digits: a thread takes eight columns, four threads a lane's 32
+        if (slice) __syncthreads();
+        for (uint32_t w = threadIdx.x; w < lanes * 4; w += kThreads) {
+            const uint64_t at = slice + 8 * w;
+            float v[8];
+            if (at + 8 <= a.cols) {
+                typedef T Raw __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+                const Raw raw = *reinterpret_cast<const Raw*>(x + at);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = (float)raw[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = at + e < a.cols ? (float)x[at + e] : 0.f;
+            }
+            uint32_t most = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t bits = __float_as_uint(v[e]) & 0x7FFFFFFFu;
+                most = bits > most ? bits : most;
+            }
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) {
+                const uint32_t other = (uint32_t)__shfl_xor((int)most, o);
+                most = other > most ? other : most;
+            }
+            const int power = power_of(most, D::exponent, D::most);
+            const bool finite = most < 0x7F800000u;
+            const float to = power2_of(power);
+            uint32_t out[D::digits];
+            int32_t sum = 0;
+#pragma unroll
+            for (int d = 0; d < D::digits; ++d) out[d] = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                int32_t rest = finite ? (int32_t)rintf(v[e] * to) : 0;
+                sum += rest;
+#pragma unroll
+                for (int d = 0; d < D::digits; ++d) {             // the first digit is the lowest; signed, [-8, 7]
+                    const int32_t digit = rest << 28 >> 28;
+                    rest = (rest - digit) >> 4;
+                    out[d] |= ((uint32_t)digit & 15u) << (4 * e);
+                }
+            }
+            const uint32_t place = (w % 4 + missing_words(slice + w / 4 * kLaneCols)) % 4;
+#pragma unroll
+            for (int d = 0; d < D::digits; ++d) reinterpret_cast<uint32_t*>(digits + d * lanes + w / 4)[place] = out[d];
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) sum += __shfl_xor(sum, o);
+            if (w % 4 == 0) {
+                sums[w / 4] = sum;
+                units[w / 4] = finite ? power2_of(-power) * (1.f / 15.f) : __builtin_nanf("");
+            }
+        }
+        __syncthreads();
+        i32x4 own[D::digits];
+#pragma unroll
+        for (int d = 0; d < D::digits; ++d) own[d] = digits[d * lanes + cw * G + l];
+        const int32_t start = sums[cw * G + l];
+        const float unit = units[cw * G + l];
+
+        auto use = [&](const Load& v, uint32_t q) {
+            int32_t codes[4], dot[D::digits];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) codes[w] = (int32_t)(v.w[w] ^ 0x88888888u);         // code - 8
+#pragma unroll
+            for (int d = 0; d < D::digits; ++d) {
+                dot[d] = 0;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) dot[d] = __builtin_amdgcn_sdot8(codes[w], own[d][w], dot[d], false);
+            }
+            float sum;                                            // sum (2 code - 15) v = 2 sum (code - 8) v + sum v
+            if constexpr (D::digits == 4) {
+                sum = (float)(2 * ((((dot[3] * 16 + dot[2]) * 16 + dot[1]) * 16) + dot[0]) + start);
+            } else {
+                const int32_t high = (dot[5] * 16 + dot[4]) * 16 + dot[3], low = (dot[2] * 16 + dot[1]) * 16 + dot[0];
+                sum = fmaf((float)high, 8192.f, (float)(2 * low + start));
+            }
+            sum = lanes_total<G>((some ? v.scale : 0.f) * unit * sum);
+            if (l == G - 1) {
+                float* to = mine + q * AT_ONCE + g;
+                *to = slice ? *to + sum : sum;
+            }
+        };
+        for (uint32_t q = 0; q < loads; q += AHEAD) {
+#pragma unroll
+            for (int s = 0; s < AHEAD; ++s) {
+                if (q + s >= loads) break;
+                const Load now = ring[s];
+                fetch(ring[s], q + s + AHEAD);
+                use(now, q + s);
+            }
+        }
+    }
+    __syncthreads();
+    for (uint32_t q = threadIdx.x; q < rows_here; q += kThreads) {
+        const uint64_t at = first + q;
+        if (at >= a.rows) break;
+        float v = totals[q];
+        for (uint32_t c = 1; c < col_waves; ++c) v += totals[c * rows_here + q];
+        product_store<T>(a, at, 0, v);
+    }
 }
 
 // Adds the parts.  A thread per row and token.
@@ -265,60 +546,139 @@ template <typename T>
 __global__ void __launch_bounds__(256) product_join_kernel(ProductShape a) {
     const uint64_t r = a.row0 + (uint64_t)blockIdx.x * 256 + threadIdx.x, t = blockIdx.y;
     if (r >= a.rows) return;
+    const float* from = a.partial + t * a.rows + r;
+    const uint64_t step = a.tokens * a.rows;
     float v = 0.f;
-    for (uint32_t p = 0; p < a.plan.parts; ++p) v += a.partial[(p * a.tokens + t) * a.rows + r];
+    for (uint32_t p = 0; p < a.plan.parts; p += 4) {
+        float w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = p + q < a.plan.parts ? from[(p + q) * step] : 0.f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v += w[q];
+    }
     product_store<T>(a, r, t, v);
 }
 
 template <typename T>
-uint32_t panel_bytes_of_chunk(uint64_t tokens) { return (uint32_t)(tokens * kChunk * 2 * Operand<T>::pieces); }
+int product_tiles(uint64_t tokens) {
+    int tiles = 1;
+    while ((uint64_t)tiles * kTileTokens<T> < tokens) tiles *= 2;
+    return tiles;
+}
 
-uint32_t rows_of_wave(uint64_t tokens) { return tokens > 16 ? 32 : 16; }
+// f(std::integral_constant<int, tiles>(), std::bool_constant<narrow>())
+template <typename T, typename F>
+void by_tiles(int tiles, bool narrow, F f) {
+    auto with = [&](auto t) {
+        if (narrow) f(t, std::true_type());
+        else f(t, std::false_type());
+    };
+    if (tiles == 1) with(std::integral_constant<int, 1>());
+    else if (tiles == 2) with(std::integral_constant<int, 2>());
+    else if (tiles == 4) with(std::integral_constant<int, 4>());
+    else if (tiles == 8) with(std::integral_constant<int, 8>());
+    else if constexpr (sizeof(T) == 4) with(std::integral_constant<int, 16>());
+}
 
 template <typename T>
-ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens) {
+uint32_t record_bytes(uint64_t tokens, bool narrow) {
+    uint32_t bytes = 0;
+    by_tiles<T>(product_tiles<T>(tokens), narrow, [&](auto t, auto n) { bytes = Record<T, decltype(t)::value, decltype(n)::value>::bytes((uint32_t)tokens); });
+    return bytes;
+}
+
+template <typename T>
+constexpr int kRowTiles(int tiles) { return tiles >= 4 ? 2 : 1; }  // of 16 rows, in a wave
+
+template <typename T>
+ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens, bool narrow) {
     ProductPlan p{};
-    const uint64_t chunks = (cols + kChunk - 1) / kChunk, tiles = (rows + rows_of_wave(tokens) - 1) / rows_of_wave(tokens);
+    const int tiles = product_tiles<T>(tokens);
+    const uint64_t chunks = (cols + kChunk - 1) / kChunk, height = 16 * kRowTiles<T>(tiles), row_tiles = (rows + height - 1) / height;
+    const uint32_t record = record_bytes<T>(tokens, narrow);
     // A workgroup reads all of x for the rows it has: not more bytes of it than of codes, as far as eight waves of rows go.
     p.row_waves = 1;
-    while (p.row_waves < kWaves && (tokens * 4 * Operand<T>::pieces > rows_of_wave(tokens) * p.row_waves || tiles / (2 * p.row_waves) >= 512)) p.row_waves *= 2;
-    const uint64_t groups = (tiles + p.row_waves - 1) / p.row_waves, col_waves = kWaves / p.row_waves;
+    while (p.row_waves < kWaves && (record > 64 * height * p.row_waves || row_tiles / (2 * p.row_waves) >= 512)) p.row_waves *= 2;
+    const uint64_t groups = (row_tiles + p.row_waves - 1) / p.row_waves, col_waves = kWaves / p.row_waves;
     p.parts = 1;
     while (groups * p.parts < 256 && chunks >= 8 * p.parts * col_waves && p.parts < 32) p.parts *= 2;
     p.part_chunks = (uint32_t)((chunks + p.parts - 1) / p.parts);
     p.parts = (uint32_t)((chunks + p.part_chunks - 1) / p.part_chunks);
-    const uint32_t fit = kPanel / panel_bytes_of_chunk<T>(tokens);
-    p.panel_chunks = p.part_chunks < fit ? p.part_chunks : fit;
+    const uint32_t fit = kPanel / record;
+    p.stage_chunks = p.part_chunks < fit ? p.part_chunks : fit;
     return p;
 }
 
-template <typename T, int TT, int RT, bool NARROW>
-void launch_product_kernel(const ProductShape& a, hipStream_t stream) {
-    const uint32_t join = a.plan.row_waves == kWaves ? 0 : kWaves * RT * TT * 64 * 16;
-    const uint32_t panel = a.plan.panel_chunks * panel_bytes_of_chunk<T>(a.tokens), bytes = panel > join ? panel : join;
-    const uint64_t groups = (a.rows + 16 * RT * a.plan.row_waves - 1) / (16 * RT * a.plan.row_waves);
+// Scratch: the panel, then the partial sums.
+template <typename T>
+uint64_t panel_bytes(uint64_t cols, uint64_t tokens, bool narrow) {
+    return product_tiles<T>(tokens) == 1 ? 0 : (cols + kChunk - 1) / kChunk * record_bytes<T>(tokens, narrow);
+}
+template <typename T>
+uint64_t scratch_bytes(uint64_t rows, uint64_t cols, uint64_t tokens, bool narrow) {
+    const uint64_t parts = product_plan<T>(rows, cols, tokens, narrow).parts;
+    return panel_bytes<T>(cols, tokens, narrow) + (parts > 1 ? parts * tokens * rows * sizeof(float) : 0);
+}
+
+template <typename T, int TT, bool NARROW>
+void launch_product_kernels(const ProductShape& a, hipStream_t stream) {
+    constexpr int RT = kRowTiles<T>(TT);
+    using R = Record<T, TT, NARROW>;
+    const uint32_t tokens = (uint32_t)a.tokens, join = a.plan.row_waves == kWaves ? 0 : kThreads * RT * TT * (4 / Digits<T>::stride) * 4;
+    const uint32_t panel = a.plan.stage_chunks * R::bytes(tokens), bytes = panel > join ? panel : join;
     ProductShape b = a;
+    if (TT > 1) {
+        const unsigned chunks = (unsigned)((a.cols + kChunk - 1) / kChunk);
+        hipLaunchKernelGGL((product_digits_kernel<T, TT, NARROW>), dim3(chunks, (tokens + 15) / 16), dim3(256), 0, stream, b, static_cast<uint8_t*>(a.work));
+        b.panel = static_cast<const uint8_t*>(a.work);
+    }
+    const uint64_t height = 16 * RT * a.plan.row_waves, groups = (a.rows + height - 1) / height;
     for (uint64_t g = 0; g < groups; g += kGroupsOfLaunch) {
-        b.row0 = g * 16 * RT * a.plan.row_waves;
+        b.row0 = g * height;
         const uint64_t here = groups - g < kGroupsOfLaunch ? groups - g : kGroupsOfLaunch;
-        hipLaunchKernelGGL((product_kernel<T, TT, RT, NARROW>), dim3((unsigned)here, a.plan.parts), dim3(kWaves * 64), bytes, stream, b);
+        hipLaunchKernelGGL((product_kernel<T, TT, RT, NARROW>), dim3((unsigned)here, a.plan.parts), dim3(kThreads), bytes, stream, b);
+    }
+}
+
+template <typename T, int G>
+void launch_product_one(ProductShape a, hipStream_t stream) {
+    constexpr uint32_t AT_ONCE = 64 / G;
+    const uint64_t slices = (a.cols + G * kLaneCols - 1) / (G * kLaneCols);
+    uint32_t col_waves = 1;
+    while (col_waves < kWaves && col_waves < slices) col_waves *= 2;
+    a.plan.row_waves = kWaves / col_waves;
+    // Rows enough to be worth writing x in digits for, as long as there is a workgroup for every compute unit: 65536 x 4096, bf16, 8 rows a wave 32.6 us,
+    // 16: 27.9, 32: 28.2, 64: 28.6; 4096 x 16384 8: 15.4 (512 workgroups), 16: 13.2, 32: 16.8 (128); 2048 x 2048 1: 4.1, 4: 4.7, 16: 7.6.
+    const uint64_t each = a.rows / (256ull * a.plan.row_waves) / AT_ONCE * AT_ONCE;
+    a.plan.wave_rows = (uint32_t)(each < AT_ONCE ? AT_ONCE : each > 32 ? 32 : each);
+    const uint64_t rows_here = (uint64_t)a.plan.row_waves * a.plan.wave_rows, groups = (a.rows + rows_here - 1) / rows_here;
+    const uint32_t bytes = col_waves * G * (Nibbles<T>::digits * 16 + 8) + kWaves * a.plan.wave_rows * 4;
+    for (uint64_t q = 0; q < groups; q += kGroupsOfLaunch) {
+        a.row0 = q * rows_here;
+        const uint64_t here = groups - q < kGroupsOfLaunch ? groups - q : kGroupsOfLaunch;
+        hipLaunchKernelGGL((product_one_kernel<T, G>), dim3((unsigned)here), dim3(kThreads), bytes, stream, a);
     }
 }
 
 template <typename T>
 void launch_product_of(const ProductArgs& args, hipStream_t stream) {
+    const bool narrow = args.block == 64;
     for (uint64_t t0 = 0; t0 < args.tokens; t0 += kTokens) {
         ProductShape a{};
         static_cast<ProductArgs&>(a) = args;
         a.tokens = args.tokens - t0 < kTokens ? args.tokens - t0 : kTokens;
         a.in = static_cast<const T*>(args.in) + t0 * args.in_ld;
         a.out = static_cast<T*>(args.out) + t0 * args.out_ld;
-        a.plan = product_plan<T>(a.rows, a.cols, a.tokens);
-        a.partial = a.plan.parts > 1 ? static_cast<float*>(a.work) : nullptr;
-        const bool narrow = a.block == 64;
-        if (a.tokens <= 16) narrow ? launch_product_kernel<T, 1, 1, true>(a, stream) : launch_product_kernel<T, 1, 1, false>(a, stream);
-        else if (a.tokens <= 32) narrow ? launch_product_kernel<T, 2, 2, true>(a, stream) : launch_product_kernel<T, 2, 2, false>(a, stream);
-        else narrow ? launch_product_kernel<T, 4, 2, true>(a, stream) : launch_product_kernel<T, 4, 2, false>(a, stream);
+        if (a.tokens == 1 && a.cols > 24) {                         // (see the kernel)
+            if (a.cols <= 4 * kLaneCols) launch_product_one<T, 4>(a, stream);
+            else if (a.cols <= 16 * kLaneCols) launch_product_one<T, 16>(a, stream);
+            else if (a.cols <= 32 * kLaneCols) launch_product_one<T, 32>(a, stream);
+            else launch_product_one<T, 64>(a, stream);
+            continue;
+        }
+        a.plan = product_plan<T>(a.rows, a.cols, a.tokens, narrow);
+        if (a.plan.parts > 1) a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(a.work) + panel_bytes<T>(a.cols, a.tokens, narrow));
+        by_tiles<T>(product_tiles<T>(a.tokens), narrow, [&](auto t, auto n) { launch_product_kernels<T, decltype(t)::value, decltype(n)::value>(a, stream); });
         if (!a.partial) continue;
         const uint64_t groups = (a.rows + 255) / 256;
         for (uint64_t g = 0; g < groups; g += kGroupsOfLaunch) {
@@ -332,15 +692,14 @@ void launch_product_of(const ProductArgs& args, hipStream_t stream) {
 }  // namespace
 
 uint64_t product_work_bytes(const ds_matrix& m) {
-    const uint64_t tokens = m.tokens < kTokens ? m.tokens : kTokens;
-    uint64_t parts = 1;
     uint64_t bytes = 0;
-    auto most = [&](uint64_t of) {                                // of the launches: whole ones and the last
-        by_dtype(m.dtype, [&](auto kind) { parts = product_plan<decltype(kind)>(m.rows, m.cols, of).parts; });
-        const uint64_t here = parts > 1 ? parts * of * m.rows * sizeof(float) : 0;
-        if (here > bytes) bytes = here;
+    auto most = [&](uint64_t tokens) {                            // of the launches: whole ones and the last
+        by_dtype(m.dtype, [&](auto kind) {
+            const uint64_t here = scratch_bytes<decltype(kind)>(m.rows, m.cols, tokens, m.block == 64);
+            if (here > bytes) bytes = here;
+        });
     };
-    most(tokens);
+    if (m.tokens >= kTokens) most(kTokens);
     if (m.tokens % kTokens) most(m.tokens % kTokens);
     return bytes;
 }
