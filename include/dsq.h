@@ -370,7 +370,7 @@ typedef enum { DS_F32 = 0, DS_BF16 = 1, DS_F16 = 2 } ds_dtype;
  * block (see ds_message_bytes), the rows one behind the other.  Where cols is a multiple of block, that is also how any
  * rows * cols consecutive parameters lie inside one worker's message, if the first of them starts a block. */
 typedef struct {
-    uint64_t rows, cols;      /* of the matrix, each >= 1 and < 2^31                             */
+    uint64_t rows, cols;      /* of the matrix, each >= 1 and < 2^28                             */
     uint64_t tokens;          /* vectors it is multiplied with, < 2^31                           */
     int32_t  block;           /* power of two, 64 <= block <= 2048                               */
     int32_t  dtype;           /* ds_dtype of x, y, dy and dx                                     */

@@ -7,7 +7,7 @@
 
 namespace {
 
-constexpr uint64_t kMost = 1ull << 31;
+constexpr uint64_t kMost = 1ull << 31, kMostSide = 1ull << 28;   // of a matrix: 32 rows apart is less than 2^32 bytes
 
 struct Report {
     char* buf;
@@ -33,8 +33,8 @@ bool known(int32_t dtype) { return dtype == DS_F32 || dtype == DS_BF16 || dtype 
 
 const char* matrix_fault(const ds_matrix* m) {
     if (!m) return "the matrix is NULL";
-    if (m->rows < 1 || m->rows >= kMost) return "rows must be at least 1 and below 2^31";
-    if (m->cols < 1 || m->cols >= kMost) return "cols must be at least 1 and below 2^31";
+    if (m->rows < 1 || m->rows >= kMostSide) return "rows must be at least 1 and below 2^28";
+    if (m->cols < 1 || m->cols >= kMostSide) return "cols must be at least 1 and below 2^28";
     if (m->block < 64 || m->block > 2048 || (m->block & (m->block - 1))) return "block must be a power of two between 64 and 2048";
     return nullptr;
 }

@@ -12,24 +12,26 @@
 namespace dsq {
 namespace {
 
-constexpr int kWaves = 8, kChunk = 128, kStep = 32;               // waves of a workgroup; columns and rows a wave takes at a time
+constexpr int kWaves = 8, kThreads = kWaves * 64, kChunk = 128, kStep = 32;   // of a workgroup; columns and rows a wave takes at a time
+constexpr uint32_t kBlockRows = kWaves * kStep;                   // rows the workgroup takes at a time
 constexpr uint64_t kTokens = 64;                                  // of a launch
 constexpr uint64_t kGroupsOfLaunch = 1u << 22;                    // a launch dimension holds fewer than 2^32 work-items
 
 struct GradientShape : ProductArgs {
     uint32_t parts;                                               // workgroups that split the rows
-    uint64_t part_rows;                                           // a multiple of kStep
+    uint64_t part_rows;                                           // a multiple of kBlockRows
     uint64_t chunks, chunk0;
     float* partial;                                               // parts x tokens x cols, or nullptr
 };
 
 // One weight after the other, as the formula has it: for a result that is not finite.
 template <typename T>
-__device__ __noinline__ float gradient_in_order(const ProductArgs& a, uint64_t c, uint64_t t) {
+__device__ __forceinline__ float gradient_in_order(const ProductArgs& a, uint64_t c, uint64_t t) {
     const uint8_t* block = a.msg + c / a.block * (4 + a.block / 2);
     const uint32_t at = c % a.block / 8, by = c % 8 * 4;
     const T* dy = static_cast<const T*>(a.in) + t * a.in_ld;
     float sum = 0.f;
+#pragma unroll 1
     for (uint64_t r = 0; r < a.rows; ++r, block += a.row_bytes) {
         const float d = (float)dy[r] * (*reinterpret_cast<const float*>(block) / 15.f);
         const uint32_t word = *reinterpret_cast<const uint32_t*>(block + 4 + 4 * at);
@@ -45,23 +47,26 @@ __device__ __forceinline__ void gradient_store(const ProductArgs& a, uint64_t c,
     static_cast<T*>(a.out)[t * a.out_ld + c] = (T)v;
 }
 
-// What a wave needs of 32 rows.  A matrix instruction's columns must share a block: with blocks of 64 a lane takes four columns of either
+// What a wave needs of the matrix in 32 rows.  A matrix instruction's columns must share a block: with blocks of 64 a lane takes four columns of either
 // block, half of word n / 2, and its column c is 64 floor(c / 4) + 4 n + c % 4 instead of 8 n + c.
-template <typename T, int TT, bool NARROW>
+template <bool NARROW>
 struct Rows {
     static constexpr int H = NARROW ? 2 : 1;
     uint32_t w[H][8];
     float scale[H][8];
-    typedef T Eights __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-    Eights dy[TT];
 };
 
 template <typename T, int TT, bool NARROW>
-__global__ void __launch_bounds__(kWaves * 64, 2) product_gradient_kernel(GradientShape a) {
+__global__ void __launch_bounds__(kThreads, 2) product_gradient_kernel(GradientShape a) {
     constexpr int P = sizeof(T) == 4 ? 3 : 2, H = NARROW ? 2 : 1;
-    using R = Rows<T, TT, NARROW>;
+    constexpr uint32_t E = 16 / sizeof(T), PER = kBlockRows / E, PIECES = TT * 16 * PER / kThreads;   // 16-byte pieces of dy: elements, of a token, of a thread
+    constexpr uint32_t kPitch = kBlockRows + E;                   // of a token's dy in LDS, elements
+    using R = Rows<NARROW>;
+    typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+    typedef T Eights __attribute__((ext_vector_type(8), aligned(16)));
     extern __shared__ __align__(16) uint8_t lds[];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, n = lane & 15, j = lane >> 4;
+    T* staged = reinterpret_cast<T*>(lds);                        // [buffer][token][row]
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane & 15, j = lane >> 4;
     const uint32_t tokens = (uint32_t)a.tokens;
     // Workgroups go round the eight XCDs: those of the same rows, which share cache lines, onto one of them.
     uint64_t chunk = blockIdx.x, part = blockIdx.y;
@@ -71,23 +76,40 @@ __global__ void __launch_bounds__(kWaves * 64, 2) product_gradient_kernel(Gradie
         chunk = q % gridDim.x;
     }
     const uint64_t col0 = (a.chunk0 + chunk) * kChunk;
-    const uint64_t r_end = (part + 1) * a.part_rows < a.rows ? (part + 1) * a.part_rows : a.rows;
+    const uint64_t r_begin = part * a.part_rows, r_end = r_begin + a.part_rows < a.rows ? r_begin + a.part_rows : a.rows;
+    const uint32_t blocks = (uint32_t)((r_end - r_begin + kBlockRows - 1) / kBlockRows);
 
     const uint32_t pitch = 4 + a.block / 2;
     const uint8_t* block[H];                                      // in row 0: the blocks, and the lane's word in them
     uint32_t at[H];
-    bool there[H];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
         const uint64_t col = col0 + 64 * h, mine = NARROW ? col + n / 2 * 8 : col + 8 * n;
         block[h] = a.msg + (col < a.cols ? col : 0) / a.block * pitch;
-        there[h] = mine < a.cols;
-        at[h] = there[h] ? 4 + (uint32_t)(mine % a.block) / 2 : 4;
+        at[h] = mine < a.cols ? 4 + (uint32_t)(mine % a.block) / 2 : 4;
     }
-    auto load = [&](R& v, uint64_t r0) {
+    uint32_t scale_at[H], word_at[H];                             // of the lane's first row, from the block's (rows 24 apart: below 2^32)
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        scale_at[h] = 8 * j * (uint32_t)a.row_bytes;
+        word_at[h] = scale_at[h] + at[h];
+    }
+    auto fetch = [&](R& v, uint32_t b) {                          // all 256 rows are there
+        const uint64_t r0 = r_begin + (uint64_t)b * kBlockRows + wave * kStep;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+                const uint8_t* p = block[h] + (r0 + e) * a.row_bytes;
+                v.scale[h][e] = *reinterpret_cast<const float*>(p + scale_at[h]);
+                v.w[h][e] = *reinterpret_cast<const uint32_t*>(p + word_at[h]);
+            }
+    };
+    auto fetch_tail = [&](R& v, uint32_t b) {                     // rows behind the last repeat it (dy is 0 there)
+        const uint64_t r0 = r_begin + (uint64_t)b * kBlockRows + wave * kStep + 8 * j;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint64_t r = r0 + 8 * j + e, row = r < a.rows ? r : a.rows - 1;      // rows behind the last: dy counts as 0 there
+            const uint64_t row = r0 + e < a.rows ? r0 + e : a.rows - 1;
 #pragma unroll
             for (int h = 0; h < H; ++h) {
                 const uint8_t* p = block[h] + row * a.row_bytes;
@@ -95,14 +117,32 @@ __global__ void __launch_bounds__(kWaves * 64, 2) product_gradient_kernel(Gradie
                 v.w[h][e] = *reinterpret_cast<const uint32_t*>(p + at[h]);
             }
         }
+    };
+    const T* dy_at[PIECES];                                       // of the thread's pieces, in row 0
 #pragma unroll
-        for (int t = 0; t < TT; ++t) {
-            const uint32_t tok = 16 * t + n < tokens ? 16 * t + n : tokens - 1;
-            const T* dy = static_cast<const T*>(a.in) + tok * a.in_ld + r0 + 8 * j;
-            if (r0 + kStep <= a.rows) v.dy[t] = *reinterpret_cast<const typename R::Eights*>(dy);
-            else
+    for (uint32_t q = 0; q < PIECES; ++q) {
+        const uint32_t piece = q * kThreads + threadIdx.x, tok = piece / PER < tokens ? piece / PER : tokens - 1;
+        dy_at[q] = static_cast<const T*>(a.in) + tok * a.in_ld + piece % PER * E;
+    }
+    auto fetch_dy = [&](Piece (&v)[PIECES], uint32_t b) {
+        const uint64_t r0 = r_begin + (uint64_t)b * kBlockRows;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v.dy[t][e] = r0 + 8 * j + e < a.rows ? dy[e] : (T)0.f;
+        for (uint32_t q = 0; q < PIECES; ++q) v[q] = *reinterpret_cast<const Piece*>(dy_at[q] + r0);
+    };
+    auto fetch_dy_tail = [&](Piece (&v)[PIECES], uint32_t b) {
+        const uint64_t r0 = r_begin + (uint64_t)b * kBlockRows;
+#pragma unroll
+        for (uint32_t q = 0; q < PIECES; ++q) {
+            const uint64_t r = r0 + (q * kThreads + threadIdx.x) % PER * E;
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) v[q][e] = r + e < a.rows ? dy_at[q][r0 + e] : (T)0.f;
+        }
+    };
+    auto stage_dy = [&](const Piece (&v)[PIECES], uint32_t buffer) {
+#pragma unroll
+        for (uint32_t q = 0; q < PIECES; ++q) {
+            const uint32_t piece = q * kThreads + threadIdx.x;
+            *reinterpret_cast<u32x4*>(staged + (buffer * TT * 16 + piece / PER) * kPitch + piece % PER * E) = __builtin_bit_cast(u32x4, v[q]);
         }
     };
 
@@ -114,60 +154,87 @@ __global__ void __launch_bounds__(kWaves * 64, 2) product_gradient_kernel(Gradie
 #pragma unroll
         for (int h = 0; h < H; ++h) off[t][h] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    auto use = [&](const R& v, uint64_t r0) {
-        const bool ragged = r0 + kStep > a.rows;
+    const CodeMasks masks = code_masks<__bf16>();
+    auto use = [&](const R& v, uint32_t buffer, bool ragged, uint64_t r0) {
 #pragma unroll
         for (int h = 0; h < H; ++h) {
-            Eight<__bf16> left[TT][P];
+            constexpr int COLS = NARROW ? 4 : 8;
+            Eight<__bf16> right[COLS];
+#pragma unroll
+            for (int g = 0; g < COLS / 4; ++g) {
+                uint32_t pair[4];                                 // four columns of rows 2 q and 2 q + 1
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t select = NARROW ? (n % 2 ? 0x07060302u : 0x05040100u) : g ? 0x07060302u : 0x05040100u;
+                    pair[q] = __builtin_amdgcn_perm(v.w[h][2 * q + 1], v.w[h][2 * q], select);
+                }
+                auto column = [&](auto which) {
+                    constexpr int N = decltype(which)::value;
+                    const u32x4 codes = {code_pair<__bf16, N>(pair[0], masks), code_pair<__bf16, N>(pair[1], masks), code_pair<__bf16, N>(pair[2], masks),
+                                         code_pair<__bf16, N>(pair[3], masks)};
+                    right[4 * g + N] = __builtin_bit_cast(Eight<__bf16>, codes);
+                };
+                column(std::integral_constant<int, 0>());
+                column(std::integral_constant<int, 1>());
+                column(std::integral_constant<int, 2>());
+                column(std::integral_constant<int, 3>());
+            }
+            float unit[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) unit[e] = v.scale[h][e] * kPerCode;
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
+                const T* from = staged + (buffer * TT * 16 + 16 * t + n) * kPitch + wave * kStep + 8 * j;
+                const Eights raw = *reinterpret_cast<const Eights*>(from);
                 float d[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    d[e] = (float)v.dy[t][e] * (v.scale[h][e] * kPerCode);
-                    if (ragged && r0 + 8 * j + e >= a.rows) d[e] = 0.f;
+                for (int e = 0; e < 8; ++e) d[e] = (float)raw[e] * unit[e];
+                if (ragged)                                       // (a scale of the last row may be infinite)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) d[e] = r0 + 8 * j + e < a.rows ? d[e] : 0.f;
+                Eight<__bf16> left[P];
+                split_operand<P>(d, left);
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    off[t][h] = matrix_fma(left[p], centre_operand<__bf16>(), off[t][h]);
+#pragma unroll
+                    for (int c = 0; c < COLS; ++c) sum[t][COLS * h + c] = matrix_fma(left[p], right[c], sum[t][COLS * h + c]);
                 }
-                split_operand<__bf16, P>(d, left[t]);
-#pragma unroll
-                for (int p = 0; p < P; ++p) off[t][h] = matrix_fma(left[t][p], centre_operand<__bf16>(), off[t][h]);
-            }
-            uint32_t pair[H == 2 ? 1 : 2][4];                     // columns 0 .. 3 (and 4 .. 7) of rows 2 q and 2 q + 1
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if constexpr (NARROW) {
-                    pair[0][q] = __builtin_amdgcn_perm(v.w[h][2 * q + 1], v.w[h][2 * q], n % 2 ? 0x07060302u : 0x05040100u);
-                } else {
-                    pair[0][q] = __builtin_amdgcn_perm(v.w[0][2 * q + 1], v.w[0][2 * q], 0x05040100u);
-                    pair[1][q] = __builtin_amdgcn_perm(v.w[0][2 * q + 1], v.w[0][2 * q], 0x07060302u);
-                }
-            }
-            auto column = [&](auto which, int g) {                // column `which` of the four, of pair[g]
-                constexpr int N = decltype(which)::value;
-                const u32x4 codes = {code_pair<__bf16, N>(pair[g][0]), code_pair<__bf16, N>(pair[g][1]), code_pair<__bf16, N>(pair[g][2]),
-                                     code_pair<__bf16, N>(pair[g][3])};
-                const Eight<__bf16> right = __builtin_bit_cast(Eight<__bf16>, codes);
-                const int c = (NARROW ? 4 * h : 4 * g) + N;
-#pragma unroll
-                for (int t = 0; t < TT; ++t)
-#pragma unroll
-                    for (int p = 0; p < P; ++p) sum[t][c] = matrix_fma(left[t][p], right, sum[t][c]);
-            };
-#pragma unroll
-            for (int g = 0; g < (NARROW ? 1 : 2); ++g) {
-                column(std::integral_constant<int, 0>(), g);
-                column(std::integral_constant<int, 1>(), g);
-                column(std::integral_constant<int, 2>(), g);
-                column(std::integral_constant<int, 3>(), g);
             }
         }
     };
-    uint64_t r0 = part * a.part_rows + wave * kStep;
-    R next;
-    if (r0 < r_end) load(next, r0);
-    for (; r0 < r_end; r0 += kWaves * kStep) {
-        const R now = next;
-        if (r0 + kWaves * kStep < r_end) load(next, r0 + kWaves * kStep);
-        use(now, r0);
+    // Whole blocks of rows, each read while the one before is multiplied (the last once more: no branch, so that loads can be counted), ...
+    const uint32_t whole = (uint32_t)((r_end - r_begin) / kBlockRows);
+    Piece dy[PIECES];
+    if (whole) {
+        R rows[2];
+        fetch_dy(dy, 0);
+        fetch(rows[0], 0);
+        stage_dy(dy, 0);
+        __syncthreads();
+        auto step = [&](const R& now, R& next, uint32_t b) {
+            const uint32_t ahead = b + 1 < whole ? b + 1 : b;
+            fetch_dy(dy, ahead);
+            fetch(next, ahead);
+            use(now, b & 1, false, 0);
+            stage_dy(dy, (b + 1) & 1);
+            __syncthreads();
+        };
+        for (uint32_t b = 0; b < whole; b += 2) {
+            step(rows[0], rows[1], b);
+            if (b + 1 >= whole) break;
+            step(rows[1], rows[0], b + 1);
+        }
+    }
+    if (whole < blocks) {                                         // ... and the rows that are left
+        R rows;
+        fetch_dy_tail(dy, whole);
+        fetch_tail(rows, whole);
+        stage_dy(dy, 0);
+        __syncthreads();
+        const uint64_t r0 = r_begin + (uint64_t)whole * kBlockRows + wave * kStep;
+        use(rows, 0, true, r0);
+        __syncthreads();
     }
 #pragma unroll
     for (int t = 0; t < TT; ++t)
@@ -196,7 +263,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) product_gradient_kernel(Gradie
         }
     }
     __syncthreads();
-    for (uint32_t q = threadIdx.x; q < tokens * kChunk; q += kWaves * 64) {
+    for (uint32_t q = threadIdx.x; q < tokens * kChunk; q += kThreads) {
         const uint32_t tok = q / kChunk, c = q % kChunk;
         if (col0 + c >= a.cols) continue;
         const float v = line[tok * (kChunk + 4) + c];
@@ -210,29 +277,38 @@ template <typename T>
 __global__ void __launch_bounds__(256) product_gradient_join_kernel(GradientShape a) {
     const uint64_t c = (a.chunk0 * (uint64_t)gridDim.x + blockIdx.x) * 256 + threadIdx.x, t = blockIdx.y;
     if (c >= a.cols) return;
+    const float* from = a.partial + t * a.cols + c;
+    const uint64_t step = a.tokens * a.cols;
     float v = 0.f;
-    for (uint32_t p = 0; p < a.parts; ++p) v += a.partial[(p * a.tokens + t) * a.cols + c];
+    for (uint32_t p = 0; p < a.parts; p += 8) {
+        float w[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) w[q] = p + q < a.parts ? from[(p + q) * step] : 0.f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v += w[q];
+    }
     gradient_store<T>(a, c, t, v);
 }
 
 void gradient_plan(uint64_t rows, uint64_t cols, uint32_t& parts, uint64_t& part_rows) {
-    const uint64_t chunks = (cols + kChunk - 1) / kChunk, steps = (rows + kStep - 1) / kStep;
+    const uint64_t chunks = (cols + kChunk - 1) / kChunk, blocks = (rows + kBlockRows - 1) / kBlockRows;
     uint64_t p = 1;
-    while (chunks * p < 256 && steps >= 2 * p * kWaves && p < 64) p *= 2;
-    const uint64_t each = (steps + p - 1) / p;
-    part_rows = each * kStep;
-    parts = (uint32_t)((steps + each - 1) / each);
+    while (chunks * p < 256 && blocks >= 2 * p && p < 64) p *= 2;
+    const uint64_t each = (blocks + p - 1) / p;
+    part_rows = each * kBlockRows;
+    parts = (uint32_t)((blocks + each - 1) / each);
 }
 
 template <typename T, int TT, bool NARROW>
 void launch_gradient_kernel(const GradientShape& a, hipStream_t stream) {
-    constexpr uint32_t bytes = kWaves * 8 * 64 * 16 + 16 * TT * (kChunk + 4) * 4;
+    constexpr uint32_t join = kWaves * 8 * 64 * 16 + 16 * TT * (kChunk + 4) * 4, stage = 2 * TT * 16 * (kBlockRows * sizeof(T) + 16);
+    constexpr uint32_t bytes = join > stage ? join : stage;
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(product_gradient_kernel<T, TT, NARROW>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     GradientShape b = a;
     for (uint64_t g = 0; g < a.chunks; g += kGroupsOfLaunch) {
         b.chunk0 = g;
         const uint64_t here = a.chunks - g < kGroupsOfLaunch ? a.chunks - g : kGroupsOfLaunch;
-        hipLaunchKernelGGL((product_gradient_kernel<T, TT, NARROW>), dim3((unsigned)here, a.parts), dim3(kWaves * 64), bytes, stream, b);
+        hipLaunchKernelGGL((product_gradient_kernel<T, TT, NARROW>), dim3((unsigned)here, a.parts), dim3(kThreads), bytes, stream, b);
     }
 }
 
