@@ -1,9 +1,10 @@
 // The loss of a row of logits against a teacher's (index, logit) pairs, and its gradient (ds_distill).
 //
 // Bound by reading the logits once and writing their gradient once.  A row stays in the registers of its workgroup between the sum of exponentials
-// and the gradient (up to 256 KB: 1024 threads of 64 registers); the threads' number follows the row's length.  A wave's reduction and two barriers
-// join the threads' sums.  Where rows are longer, or too few to fill the GPU, they are split: a first launch sums the parts, a second one
-// reads the logits again (out of the memory-side cache, mostly) and writes the gradient.
+// and the gradient (up to 256 KB: 1024 threads of 64 registers); the threads' number follows the row's length.  A workgroup takes one row after the other,
+// and asks for the next row's logits as it writes: 16 bytes of gradient, and the registers they came from wait for 16 bytes of logits.  Where rows
+// are longer, or too few to fill the GPU, they are split: a first launch sums the parts, a second one reads the logits again (out of the
+// memory-side cache, mostly) and writes the gradient.
 //   The listed columns are written once more, after the dense part, by the thread that has the first of the entries with that index.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
@@ -16,6 +17,7 @@ constexpr uint64_t kRowsOfLaunch = 1u << 21;                      // a launch di
 
 struct DistillShape : LogitsArgs {
     uint64_t row0;
+    uint64_t rows_here;                                           // rows of the launch, from row0 on
     uint32_t parts;                                               // workgroups of a row
     uint64_t part_logits;                                         // a multiple of what a workgroup takes at a time
     float2* spreads;                                              // [row][part]
@@ -38,8 +40,9 @@ __device__ __forceinline__ float workgroup_total(float v, float* sums) {
     __syncthreads();
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x / 64] = v;
     __syncthreads();
-    v = 0.f;
-    for (int w = 0; w < WAVES; ++w) v += sums[w];
+    v = sums[threadIdx.x & (WAVES - 1)];                          // (WAVES is a power of two)
+#pragma unroll
+    for (int o = 1; o < WAVES; o <<= 1) v += __shfl_xor(v, o);
     return v;
 }
 
@@ -58,123 +61,158 @@ __device__ Teacher read_teacher(const LogitsArgs& a, uint64_t row, uint2 pair, f
         e.log_p = logit / a.temperature - a.teacher_lse[row];
     } else {
         const Spread s = workgroup_spread<WAVES>(e.listed ? spread_of(logit) : kNoSpread, scale, sums);
-        e.log_p = (logit - reference(s.max)) / a.temperature - kLn2 * log2f(s.sum);
+        const LogSum l = log_sum(s, scale);
+        e.log_p = (logit - l.from) / a.temperature - l.rest;
     }
     e.p = e.listed && logit != -__builtin_huge_valf() ? expf(e.log_p) : 0.f;
     e.mass = workgroup_total<WAVES>(e.p, sums);
     return e;
 }
 
-__device__ __forceinline__ float listed_term(const Teacher& e, float top, float temperature) {
-    return e.p != 0.f ? e.p * (e.log_p - (e.z - top) / temperature) : 0.f;
+// The entry's share of the loss.
+__device__ __forceinline__ float listed_term(const Teacher& e, LogSum l, float temperature) {
+    return e.p != 0.f ? e.p * (e.log_p - (e.z - l.from) / temperature + l.rest) : 0.f;
 }
 
-// dz of the listed columns in [begin, end): each from the thread that holds the first of its entries.  Called when the dense part is written.
-// index, prob: 256 of LDS each, which hold the entries since the last barrier.
-template <typename T>
-__device__ void write_listed(const Teacher& e, uint32_t k, const uint32_t* index, const float* prob, float each, float c, float top, float scale,
-                             uint64_t begin, uint64_t end, T* dz) {
-    if (!e.listed || e.index < begin || e.index >= end) return;
-    float all = 0.f;
-    bool mine = true;
-    for (uint32_t i = 0; i < k; ++i)
-        if (index[i] == e.index) {
-            mine = mine && i >= threadIdx.x;
-            all += prob[i];
-        }
-    if (mine) dz[e.index] = (T)(each * power2((e.z - top) * scale) - c * all);
-}
-
-template <typename T>
-struct Pieces {
-    static constexpr uint32_t E = 16 / sizeof(T);
-    typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+// The row's entries in LDS.
+struct Listed {
+    uint32_t index[kMaxTop];
+    float p[kMaxTop];
+    uint32_t mixed;                                               // an index is not above the one before: some may be the same
 };
+__device__ __forceinline__ void keep_listed(const Teacher& e, uint32_t k, Listed& listed) {
+    if (threadIdx.x == 0) listed.mixed = 0;
+    if (threadIdx.x < k) {
+        listed.index[threadIdx.x] = e.index;
+        listed.p[threadIdx.x] = e.p;
+    }
+    __syncthreads();
+    if (threadIdx.x && threadIdx.x < k && listed.index[threadIdx.x - 1] >= e.index) listed.mixed = 1;
+}
 
-// A workgroup per row, N 16-byte pieces of it in each thread's registers.
+// What a row's gradient is made of: dz = each 2^(exponent of z) - c (sum of the column's p).
+struct Gradient {
+    Exponents e;
+    float each, c;
+};
+template <typename T>
+__device__ __forceinline__ typename Pieces<T>::Piece gradient_piece(const Gradient& g, typename Pieces<T>::Piece z) {
+    typename Pieces<T>::Piece out;
+#pragma unroll
+    for (uint32_t i = 0; i < Pieces<T>::E; ++i) out[i] = (T)(g.each * g.e((float)z[i]));
+    return out;
+}
+// dz of the listed columns in [begin, end), when the dense part is written.
+template <typename T>
+__device__ __forceinline__ void write_listed(const Gradient& g, const Teacher& e, const Listed& listed, uint32_t k, uint64_t begin, uint64_t end, T* dz) {
+    if (!e.listed || e.index < begin || e.index >= end) return;
+    float all = e.p;
+    if (listed.mixed) {
+        all = 0.f;
+#pragma unroll 8
+        for (uint32_t i = 0; i < k; ++i) {
+            if (listed.index[i] != e.index) continue;
+            if (i < threadIdx.x) return;                          // the first of them writes
+            all += listed.p[i];
+        }
+    }
+    dz[e.index] = (T)(g.each * g.e(e.z) - g.c * all);
+}
+
+// A workgroup per row at a time, N 16-byte pieces of it in each thread's registers.
 template <typename T, int THREADS, int N>
 __global__ void __launch_bounds__(THREADS) distill_row_kernel(DistillShape a) {
     constexpr int WAVES = THREADS / 64;
     constexpr uint32_t E = Pieces<T>::E;
     using Piece = typename Pieces<T>::Piece;
     __shared__ float sums[2 * WAVES];
-    __shared__ uint32_t index[kMaxTop];
-    __shared__ float prob[kMaxTop];
-    const uint64_t row = a.row0 + blockIdx.x;
-    const T* z = static_cast<const T*>(a.z) + row * a.z_ld;
-    T* dz = a.dz ? static_cast<T*>(a.dz) + row * a.dz_ld : nullptr;
-    const float scale = kLog2e / a.temperature, weight = a.weight ? a.weight[row] : 1.f;
+    __shared__ Listed listed;
+    const float scale = kLog2e / a.temperature;
     const uint32_t vocab = (uint32_t)a.vocab, whole = vocab / E;   // pieces without the ragged end
-    const T zero = (T)0.f;
-
-    if (weight == 0.f) {                                          // a padded token: its logits are not read
-        if (a.loss && threadIdx.x == 0) a.loss[row] = 0.f;
-        if (!dz) return;
-        Piece none;
-#pragma unroll
-        for (uint32_t e = 0; e < E; ++e) none[e] = zero;
-        for (uint32_t p = threadIdx.x; p < whole; p += THREADS) *reinterpret_cast<Piece*>(dz + (uint64_t)p * E) = none;
-        for (uint32_t v = whole * E + threadIdx.x; v < vocab; v += THREADS) dz[v] = zero;
-        return;
-    }
-    const uint2 pair = teacher_pair(a, row);
-    const float listed = pair.x < vocab ? (float)z[pair.x] : 0.f;
+    const bool rest = whole * E + threadIdx.x < vocab;            // the thread has a column of it
     u32x4 raw[N];                                                 // (bits: as numbers the compiler would keep them in fp32, twice as many registers)
+    float last = -kInf;
+    Piece nothing;
 #pragma unroll
-    for (int p = 0; p < N; ++p) {
-        const uint32_t at = p * THREADS + threadIdx.x;
-        Piece v;
-        if (at < whole) v = *reinterpret_cast<const Piece*>(z + (uint64_t)at * E);
-        else {
+    for (uint32_t e = 0; e < E; ++e) nothing[e] = (T)-kInf;
+    auto load = [&](const T* z, int p) {
+        raw[p] = __builtin_bit_cast(u32x4, nothing);
+        if (p * THREADS + threadIdx.x < whole)                    // (an address for all, and the thread's 32 bits)
+            raw[p] = __builtin_bit_cast(u32x4, *reinterpret_cast<const Piece*>(reinterpret_cast<const uint8_t*>(z) + p * (THREADS * 16) + threadIdx.x * 16u));
+    };
+    auto logits = [&](uint64_t r) { return static_cast<const T*>(a.z) + r * a.z_ld; };
+    uint64_t row = a.row0 + blockIdx.x;
+    const uint64_t end = a.row0 + a.rows_here;
+    auto weight_of = [&](uint64_t r) { return a.weight ? a.weight[r] : 1.f; };
+    float weight = row < end ? weight_of(row) : 0.f;
+    if (weight != 0.f) {
 #pragma unroll
-            for (uint32_t e = 0; e < E; ++e) v[e] = at == whole && at * E + e < vocab ? z[at * E + e] : (T)-__builtin_huge_valf();
+        for (int p = 0; p < N; ++p) load(logits(row), p);
+        if (rest) last = (float)logits(row)[whole * E + threadIdx.x];
+    }
+    for (; row < end; row += gridDim.x) {
+        T* dz = a.dz ? static_cast<T*>(a.dz) + row * a.dz_ld : nullptr;
+        const uint64_t next = row + gridDim.x;
+        const float next_weight = next < end ? weight_of(next) : 0.f;
+        Gradient g{{0.f, 0.f}, 0.f, 0.f};
+        bool skip = weight == 0.f;                                // a padded token: its logits are not read
+        Teacher teacher{};
+        if (!skip) {
+            const uint2 pair = teacher_pair(a, row);
+            const float at_pair = pair.x < vocab ? (float)logits(row)[pair.x] : 0.f;
+            teacher = read_teacher<WAVES>(a, row, pair, at_pair, scale, sums);
+            keep_listed(teacher, a.k, listed);
+            Spread s = kNoSpread;
+#pragma unroll
+            for (int p = 0; p < N; p += N > 1 ? 2 : 1) {          // as the pieces arrive
+                constexpr int M = N > 1 ? 2 : 1;
+                float v[M][E], most[M];
+#pragma unroll
+                for (int m = 0; m < M; ++m) {
+                    u32x4 bits = raw[p + m];
+                    asm volatile("" : "+v"(bits), "+v"(s.sum));   // when the pieces before are done
+                    const Piece piece = __builtin_bit_cast(Piece, bits);
+#pragma unroll
+                    for (uint32_t e = 0; e < E; ++e) v[m][e] = (float)piece[e];
+                    most[m] = largest_of(v[m]);
+                }
+                add_logits(s, v, largest_of(most), scale);
+            }
+            s = join(s, spread_of(last), scale);
+            s = workgroup_spread<WAVES>(s, scale, sums);
+            const LogSum l = log_sum(s, scale);
+            if (a.loss) {
+                const float terms = workgroup_total<WAVES>(listed_term(teacher, l, a.temperature), sums);
+                if (threadIdx.x == 0) a.loss[row] = teacher.mass == 0.f ? 0.f : weight * terms;
+            }
+            g = {exponents(s.max, scale), weight / a.temperature * teacher.mass / s.sum, weight / a.temperature};
+            skip = teacher.mass == 0.f;
+        } else if (a.loss && threadIdx.x == 0) {
+            a.loss[row] = 0.f;
         }
-        raw[p] = __builtin_bit_cast(u32x4, v);
-    }
-    const Teacher teacher = read_teacher<WAVES>(a, row, pair, listed, scale, sums);
-    if (threadIdx.x < a.k) {
-        index[threadIdx.x] = teacher.index;
-        prob[threadIdx.x] = teacher.p;
-    }
-    Spread s = kNoSpread;
+        const bool more = next_weight != 0.f;
+        const T* z_next = logits(more ? next : row);
 #pragma unroll
-    for (int p = 0; p < N; ++p) {                                 // as the pieces arrive
-        const Piece v = __builtin_bit_cast(Piece, raw[p]);
-        float m = s.max;
+        for (int p = 0; p < N; ++p) {
+            asm volatile("" : "+v"(raw[p]) : : "memory");         // one after the other: all exponentials at once would take as many registers again
+            if (dz && p * THREADS + threadIdx.x < whole) {
+                Piece out;
+                if (skip) {
 #pragma unroll
-        for (uint32_t e = 0; e < E; ++e) m = fmaxf(m, (float)v[e]);
-        const float r = reference(m);
-        float total = s.sum == 0.f ? 0.f : s.sum * power2((reference(s.max) - r) * scale);
-#pragma unroll
-        for (uint32_t e = 0; e < E; ++e) total += power2(((float)v[e] - r) * scale);
-        s = {m, total};
-        asm volatile("" : "+v"(raw[p]));
-    }
-    s = workgroup_spread<WAVES>(s, scale, sums);
-    const float top = reference(s.max), log_sum = kLn2 * log2f(s.sum);
-    if (a.loss) {
-        const float terms = workgroup_total<WAVES>(listed_term(teacher, top, a.temperature), sums);
-        if (threadIdx.x == 0) a.loss[row] = teacher.mass == 0.f ? 0.f : weight * (terms + teacher.mass * log_sum);
-    }
-    if (!dz) return;
-    const float c = weight / a.temperature, each = c * teacher.mass / s.sum;
-    const bool skip = teacher.mass == 0.f;
-#pragma unroll
-    for (int p = 0; p < N; ++p) {
-        const uint32_t at = p * THREADS + threadIdx.x;
-        const Piece v = __builtin_bit_cast(Piece, raw[p]);
-        Piece out;
-#pragma unroll
-        for (uint32_t e = 0; e < E; ++e) out[e] = skip ? zero : (T)(each * power2(((float)v[e] - top) * scale));
-        if (at < whole) *reinterpret_cast<Piece*>(dz + (uint64_t)at * E) = out;
-        else if (at == whole) {
-#pragma unroll
-            for (uint32_t e = 0; e < E; ++e)
-                if (at * E + e < vocab) dz[at * E + e] = out[e];
+                    for (uint32_t e = 0; e < E; ++e) out[e] = (T)0.f;
+                } else {
+                    out = gradient_piece<T>(g, __builtin_bit_cast(Piece, raw[p]));
+                }
+                *reinterpret_cast<Piece*>(reinterpret_cast<uint8_t*>(dz) + p * (THREADS * 16) + threadIdx.x * 16u) = out;
+            }
+            if (more) load(z_next, p);
         }
+        if (dz && rest) dz[whole * E + threadIdx.x] = skip ? (T)0.f : (T)(g.each * g.e(last));
+        if (more && rest) last = (float)z_next[whole * E + threadIdx.x];
+        __syncthreads();
+        if (dz && !skip) write_listed(g, teacher, listed, a.k, 0, vocab, dz);
+        weight = next_weight;
     }
-    __syncthreads();
-    if (!skip) write_listed(teacher, a.k, index, prob, each, c, top, scale, 0, vocab, dz);
 }
 
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPartPieces = 4;
@@ -193,29 +231,28 @@ __global__ void __launch_bounds__(kPartThreads) distill_sum_kernel(DistillShape 
     const uint64_t begin = (uint64_t)blockIdx.y * a.part_logits, end = begin + a.part_logits < a.vocab ? begin + a.part_logits : a.vocab;
     Spread s = kNoSpread;
     for (uint64_t at = begin; at < end; at += kStretch) {
-        Piece raw[kPartPieces];
+        float v[kPartPieces][E], most[kPartPieces];
         const uint64_t mine = at + (uint64_t)threadIdx.x * E;
+        if (at + kStretch <= end) {
+            Piece raw[kPartPieces];
 #pragma unroll
-        for (int p = 0; p < kPartPieces; ++p) {
-            const uint64_t c = mine + (uint64_t)p * kPartThreads * E;
-            if (c + E <= end) raw[p] = *reinterpret_cast<const Piece*>(z + c);
-            else
+            for (int p = 0; p < kPartPieces; ++p) raw[p] = *reinterpret_cast<const Piece*>(z + mine + (uint64_t)p * kPartThreads * E);
 #pragma unroll
-                for (uint32_t e = 0; e < E; ++e) raw[p][e] = c + e < end ? z[c + e] : (T)-__builtin_huge_valf();
+            for (int p = 0; p < kPartPieces; ++p)
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) v[p][e] = (float)raw[p][e];
+        } else {
+#pragma unroll
+            for (int p = 0; p < kPartPieces; ++p)
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) {
+                    const uint64_t c = mine + (uint64_t)p * kPartThreads * E + e;
+                    v[p][e] = c < end ? (float)z[c] : -kInf;
+                }
         }
-        float m = s.max;
 #pragma unroll
-        for (int p = 0; p < kPartPieces; ++p)
-#pragma unroll
-            for (uint32_t e = 0; e < E; ++e) m = fmaxf(m, (float)raw[p][e]);
-        const float r = reference(m);
-        float total = 0.f;
-#pragma unroll
-        for (int p = 0; p < kPartPieces; ++p)
-#pragma unroll
-            for (uint32_t e = 0; e < E; ++e) total += power2(((float)raw[p][e] - r) * scale);
-        if (s.sum != 0.f) total = fmaf(s.sum, exp2f((reference(s.max) - r) * scale), total);
-        s = {m, total};
+        for (int p = 0; p < kPartPieces; ++p) most[p] = largest_of(v[p]);
+        add_logits(s, v, largest_of(most), scale);
     }
     s = workgroup_spread<kPartWaves>(s, scale, sums);
     if (threadIdx.x == 0) a.spreads[row * a.parts + blockIdx.y] = make_float2(s.max, s.sum);
@@ -230,8 +267,7 @@ __global__ void __launch_bounds__(kPartThreads) distill_part_kernel(DistillShape
     constexpr uint32_t E = Pieces<T>::E, kStretch = kPartThreads * kPartPieces * E;
     using Piece = typename Pieces<T>::Piece;
     __shared__ float sums[2 * kPartWaves];
-    __shared__ uint32_t index[kMaxTop];
-    __shared__ float prob[kMaxTop];
+    __shared__ Listed listed;
     const uint64_t row = a.row0 + blockIdx.x;
     const T* z = static_cast<const T*>(a.z) + row * a.z_ld;
     T* dz = a.dz ? static_cast<T*>(a.dz) + row * a.dz_ld : nullptr;
@@ -239,36 +275,31 @@ __global__ void __launch_bounds__(kPartThreads) distill_part_kernel(DistillShape
     const uint64_t begin = (uint64_t)blockIdx.y * a.part_logits, end = begin + a.part_logits < a.vocab ? begin + a.part_logits : a.vocab;
     bool skip = weight == 0.f;
     Teacher teacher{};
-    float top = 0.f, c = 0.f, each = 0.f;
+    Gradient g{{0.f, 0.f}, 0.f, 0.f};
     if (!skip) {
         teacher = read_teacher<kPartWaves>(a, row, teacher_pair(a, row), threadIdx.x < a.k ? a.listed[row * a.k + threadIdx.x] : 0.f, scale, sums);
-        if (threadIdx.x < a.k) {
-            index[threadIdx.x] = teacher.index;
-            prob[threadIdx.x] = teacher.p;
-        }
+        keep_listed(teacher, a.k, listed);
         Spread s = kNoSpread;
         for (uint32_t p = threadIdx.x; p < a.parts; p += kPartThreads) {
             const float2 v = a.spreads[row * a.parts + p];
             s = join(s, Spread{v.x, v.y}, scale);
         }
         s = workgroup_spread<kPartWaves>(s, scale, sums);
-        top = reference(s.max);
-        c = weight / a.temperature;
-        each = c * teacher.mass / s.sum;
+        const LogSum l = log_sum(s, scale);
         skip = teacher.mass == 0.f;
         if (a.loss && blockIdx.y == 0) {
-            const float terms = workgroup_total<kPartWaves>(listed_term(teacher, top, a.temperature), sums);
-            if (threadIdx.x == 0) a.loss[row] = skip ? 0.f : weight * (terms + teacher.mass * (kLn2 * log2f(s.sum)));
+            const float terms = workgroup_total<kPartWaves>(listed_term(teacher, l, a.temperature), sums);
+            if (threadIdx.x == 0) a.loss[row] = skip ? 0.f : weight * terms;
         }
+        g = {exponents(s.max, scale), weight / a.temperature * teacher.mass / s.sum, weight / a.temperature};
     } else if (a.loss && blockIdx.y == 0 && threadIdx.x == 0) {
         a.loss[row] = 0.f;
     }
     if (!dz) return;
     for (uint64_t at = begin; at < end; at += kStretch) {
-        const uint64_t mine = at + (uint64_t)threadIdx.x * E;
 #pragma unroll
         for (int p = 0; p < kPartPieces; ++p) {
-            const uint64_t col = mine + (uint64_t)p * kPartThreads * E;
+            const uint64_t col = at + (uint64_t)(p * kPartThreads + threadIdx.x) * E;
             if (col >= end) break;
             Piece raw, out;
             const bool whole = col + E <= end;
@@ -280,8 +311,7 @@ __global__ void __launch_bounds__(kPartThreads) distill_part_kernel(DistillShape
                 else
 #pragma unroll
                     for (uint32_t e = 0; e < E; ++e) raw[e] = col + e < end ? z[col + e] : (T)0.f;
-#pragma unroll
-                for (uint32_t e = 0; e < E; ++e) out[e] = (T)(each * power2(((float)raw[e] - top) * scale));
+                out = gradient_piece<T>(g, raw);
             }
             if (whole) *reinterpret_cast<Piece*>(dz + col) = out;
             else
@@ -291,7 +321,7 @@ __global__ void __launch_bounds__(kPartThreads) distill_part_kernel(DistillShape
         }
     }
     __syncthreads();
-    if (!skip) write_listed(teacher, a.k, index, prob, each, c, top, scale, begin, end, dz);
+    if (!skip) write_listed(g, teacher, listed, a.k, begin, end, dz);
 }
 
 constexpr uint64_t kRowBytes = 1024 * 16 * 16;                    // of the longest row that stays in registers
@@ -312,7 +342,9 @@ void distill_plan(uint64_t rows, uint64_t vocab, uint64_t size, uint32_t& parts,
 
 template <typename T, int THREADS, int N>
 void launch_rows(const DistillShape& a, unsigned here, hipStream_t stream) {
-    hipLaunchKernelGGL((distill_row_kernel<T, THREADS, N>), dim3(here), dim3(THREADS), 0, stream, a);
+    // as many workgroups as run at once (or a few more, where they are small): each goes through rows of its own
+    constexpr unsigned AT_ONCE = 256 * (2048 / THREADS);
+    hipLaunchKernelGGL((distill_row_kernel<T, THREADS, N>), dim3(here < AT_ONCE ? here : AT_ONCE), dim3(THREADS), 0, stream, a);
 }
 
 template <typename T>
@@ -325,6 +357,7 @@ void launch_distill_of(const LogitsArgs& args, hipStream_t stream) {
     for (uint64_t r = 0; r < a.rows; r += kRowsOfLaunch) {
         a.row0 = r;
         const unsigned here = (unsigned)(a.rows - r < kRowsOfLaunch ? a.rows - r : kRowsOfLaunch);
+        a.rows_here = here;
         if (a.parts) {
             hipLaunchKernelGGL(distill_sum_kernel<T>, dim3(here, a.parts), dim3(kPartThreads), 0, stream, a);
             hipLaunchKernelGGL(distill_part_kernel<T>, dim3(here, a.parts), dim3(kPartThreads), 0, stream, a);

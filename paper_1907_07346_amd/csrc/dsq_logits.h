@@ -21,21 +21,54 @@ __device__ __forceinline__ uint32_t rank_index(uint64_t rank) { return ~(uint32_
 
 // 2^x as the hardware has it: results below 2^-126 are 0.
 __device__ __forceinline__ float power2(float x) { return __builtin_amdgcn_exp2f(x); }
+// The larger one; NaN if there is one.
+__device__ __forceinline__ float max_or_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// sum over some logits of 2^(scale (z - max)), with scale = log2(e) / temperature.  The maximum that is subtracted is taken as 0 where it
-// is infinite: a row of minus infinities has sum 0, one with plus infinity has an infinite sum.
+// sum over some logits z of 2^(scale z - at), with scale = log2(e) / temperature, and the largest of them.  `at` is the largest times scale, as rounded: terms
+// and sum share it, whatever it is, and one multiply-add makes an exponent of a logit.  NaN anywhere makes all of it NaN.
+constexpr float kInf = __builtin_huge_valf();
 struct Spread {
     float max, sum;
 };
-constexpr Spread kNoSpread{-__builtin_huge_valf(), 0.f};
-__device__ __forceinline__ float reference(float max) { return fabsf(max) == __builtin_huge_valf() ? 0.f : max; }
-__device__ __forceinline__ Spread spread_of(float z) { return {z, z == -__builtin_huge_valf() ? 0.f : z == __builtin_huge_valf() ? z : 1.f}; }
+constexpr Spread kNoSpread{-kInf, 0.f};
+// What exponents are made with.  Where the largest is infinite they count from 0: a row of minus infinities has sum 0, one with plus infinity an infinite
+// sum.  Where the largest is finite but not with the factor, numbers lie so far apart that only those equal to it count, with any factor.
+struct Exponents {
+    float scale, at;
+    __device__ float operator()(float z) const { return power2(fmaf(z, scale, -at)); }
+};
+__device__ __forceinline__ Exponents exponents(float max, float scale) {
+    const float at = max * scale;
+    if (fabsf(at) != kInf) return {scale, at};
+    if (fabsf(max) == kInf) return {scale, 0.f};
+    return {1.f, max};
+}
+__device__ __forceinline__ Spread spread_of(float z) { return {z, z == -kInf ? 0.f : z == kInf ? z : z == z ? 1.f : z}; }
 __device__ __forceinline__ Spread join(Spread a, Spread b, float scale) {
-    const float m = fmaxf(a.max, b.max), r = reference(m);
-    // (An empty or all-masked side has sum 0 and a reference of 0, which may lie far above the other's maximum.)
-    const float sa = a.sum == 0.f ? 0.f : a.sum * exp2f((reference(a.max) - r) * scale);
-    const float sb = b.sum == 0.f ? 0.f : b.sum * exp2f((reference(b.max) - r) * scale);
+    const float m = max_or_nan(a.max, b.max), at = exponents(m, scale).at;
+    // (An empty or all-masked side has sum 0 and counts from 0, which may lie far above the other's largest.)
+    const float sa = a.sum == 0.f ? 0.f : a.sum * power2(exponents(a.max, scale).at - at);
+    const float sb = b.sum == 0.f ? 0.f : b.sum * power2(exponents(b.max, scale).at - at);
     return {m, sa + sb};
+}
+// Adds M times N logits whose largest is `most` (-inf counts for nothing).
+template <int M, int N>
+__device__ __forceinline__ void add_logits(Spread& s, const float (&z)[M][N], float most, float scale) {
+    const float m = max_or_nan(s.max, most);
+    const Exponents e = exponents(m, scale);
+    float total = s.sum == 0.f ? 0.f : s.sum * power2(exponents(s.max, scale).at - e.at);
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int k = 0; k < N; ++k) total += e(z[i][k]);
+    s = {m, total};
+}
+template <int N>
+__device__ __forceinline__ float largest_of(const float (&z)[N]) {
+    float m = z[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) m = max_or_nan(m, z[e]);
+    return m;
 }
 // Joins the spreads of a workgroup's WAVES * 64 threads, in an order that is always the same; every thread gets the result.  sums: 2 * WAVES floats of LDS.
 template <int WAVES>
@@ -49,12 +82,28 @@ __device__ Spread workgroup_spread(Spread s, float scale, float* sums) {
         sums[2 * (threadIdx.x / 64) + 1] = s.sum;
     }
     __syncthreads();
-    s = kNoSpread;
-    for (int w = 0; w < WAVES; ++w) s = join(s, Spread{sums[2 * w], sums[2 * w + 1]}, scale);
+    const int w = threadIdx.x & (WAVES - 1);                      // (WAVES is a power of two)
+    s = Spread{sums[2 * w], sums[2 * w + 1]};
+#pragma unroll
+    for (int o = 1; o < WAVES; o <<= 1) s = join(s, Spread{__shfl_xor(s.max, o), __shfl_xor(s.sum, o)}, scale);
     return s;
 }
-// ln of the sum of exp(z / temperature).
-__device__ __forceinline__ float spread_lse(Spread s, float temperature) { return reference(s.max) / temperature + kLn2 * log2f(s.sum); }
+// ln of the sum of exp(z / temperature) is base + rest: the largest (0 where that is infinite) and, for what `at` was rounded to, the sum.
+struct LogSum {
+    float from, rest;                                             // base = from / temperature
+};
+__device__ __forceinline__ LogSum log_sum(Spread s, float scale) {
+    const Exponents e = exponents(s.max, scale);
+    const float from = fabsf(s.max) == kInf ? 0.f : s.max;
+    return {from, kLn2 * (log2f(s.sum) - fmaf(from, e.scale, -e.at))};
+}
+
+// 16 bytes of logits, at any element's address.
+template <typename T>
+struct Pieces {
+    static constexpr uint32_t E = 16 / sizeof(T);
+    typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+};
 
 }  // namespace
 }  // namespace dsq
