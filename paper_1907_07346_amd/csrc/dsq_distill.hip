@@ -273,17 +273,29 @@ __global__ void __launch_bounds__(kPartThreads) distill_part_kernel(DistillShape
     T* dz = a.dz ? static_cast<T*>(a.dz) + row * a.dz_ld : nullptr;
     const float scale = kLog2e / a.temperature, weight = a.weight ? a.weight[row] : 1.f;
     const uint64_t begin = (uint64_t)blockIdx.y * a.part_logits, end = begin + a.part_logits < a.vocab ? begin + a.part_logits : a.vocab;
+    Piece raw[kPartPieces];
+    auto load = [&](uint64_t at) {
+#pragma unroll
+        for (int p = 0; p < kPartPieces; ++p) {
+            const uint64_t col = at + (uint64_t)(p * kPartThreads + threadIdx.x) * E;
+            if (col + E <= end) raw[p] = *reinterpret_cast<const Piece*>(z + col);
+            else
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) raw[p][e] = col + e < end ? z[col + e] : (T)0.f;
+        }
+    };
+    // all that is read without knowing more is asked for at once
+    if (dz && weight != 0.f) load(begin);
+    const uint2 pair = teacher_pair(a, row);
+    const float z_pair = threadIdx.x < a.k ? a.listed[row * a.k + threadIdx.x] : 0.f;
+    const float2 of_part = threadIdx.x < a.parts ? a.spreads[row * a.parts + threadIdx.x] : make_float2(-kInf, 0.f);   // (parts <= 256)
     bool skip = weight == 0.f;
     Teacher teacher{};
     Gradient g{{0.f, 0.f}, 0.f, 0.f};
     if (!skip) {
-        teacher = read_teacher<kPartWaves>(a, row, teacher_pair(a, row), threadIdx.x < a.k ? a.listed[row * a.k + threadIdx.x] : 0.f, scale, sums);
+        teacher = read_teacher<kPartWaves>(a, row, pair, z_pair, scale, sums);
         keep_listed(teacher, a.k, listed);
-        Spread s = kNoSpread;
-        for (uint32_t p = threadIdx.x; p < a.parts; p += kPartThreads) {
-            const float2 v = a.spreads[row * a.parts + p];
-            s = join(s, Spread{v.x, v.y}, scale);
-        }
+        Spread s = {of_part.x, of_part.y};
         s = workgroup_spread<kPartWaves>(s, scale, sums);
         const LogSum l = log_sum(s, scale);
         skip = teacher.mass == 0.f;
@@ -297,21 +309,18 @@ __global__ void __launch_bounds__(kPartThreads) distill_part_kernel(DistillShape
     }
     if (!dz) return;
     for (uint64_t at = begin; at < end; at += kStretch) {
+        if (at > begin && !skip) load(at);
 #pragma unroll
         for (int p = 0; p < kPartPieces; ++p) {
             const uint64_t col = at + (uint64_t)(p * kPartThreads + threadIdx.x) * E;
             if (col >= end) break;
-            Piece raw, out;
+            Piece out;
             const bool whole = col + E <= end;
             if (skip) {
 #pragma unroll
                 for (uint32_t e = 0; e < E; ++e) out[e] = (T)0.f;
             } else {
-                if (whole) raw = *reinterpret_cast<const Piece*>(z + col);
-                else
-#pragma unroll
-                    for (uint32_t e = 0; e < E; ++e) raw[e] = col + e < end ? z[col + e] : (T)0.f;
-                out = gradient_piece<T>(g, raw);
+                out = gradient_piece<T>(g, raw[p]);
             }
             if (whole) *reinterpret_cast<Piece*>(dz + col) = out;
             else
@@ -330,7 +339,9 @@ constexpr uint64_t kRowBytes = 1024 * 16 * 16;                    // of the long
 void distill_plan(uint64_t rows, uint64_t vocab, uint64_t size, uint32_t& parts, uint64_t& part_logits) {
     parts = 0;
     part_logits = vocab;
-    if (vocab * size <= kRowBytes && (rows >= 128 || vocab * size <= 16384)) return;
+    // One launch where it holds up: rows 8 x 32003 f32 11.3 us, and 5.0 + 7.3 split; 1 x 65536 bf16 13.3 and 4.1 + 7.1; 1 x 131072 bf16 20.9 and 4.5 + 7.1; 64 x
+    // 131072 24.5 and 9.2 + 10.5; 200 x 131072 30.8 and 13.2 + 20.1.
+    if (vocab * size <= kRowBytes && (rows >= 128 || vocab * size <= kRowBytes / 2)) return;
     const uint64_t stretch = kPartThreads * kPartPieces * (16 / size), stretches = (vocab + stretch - 1) / stretch;
     uint64_t p = rows >= 1024 ? 1 : 1024 / rows;
     if (p > stretches) p = stretches;
@@ -340,11 +351,14 @@ void distill_plan(uint64_t rows, uint64_t vocab, uint64_t size, uint32_t& parts,
     parts = (uint32_t)((stretches + each - 1) / each);
 }
 
-template <typename T, int THREADS, int N>
+// Few threads with much of a row each, so that a compute unit has several rows under way: 4096 x 32000 bf16 with 256 threads 112 us, 512 128, 1024 184;
+// 1023 x 50001 f16 with 512 50, 1024 65.  As many workgroups as run at once, each with rows of its own (RESIDENT a compute unit): 1023 x 50001 50 us, and 58 with
+// one for each row.  Where a compute unit holds one row it gains nothing, and rows of weight 0 leave some with less to do than others (RESIDENT = 0: one for
+// each row): 4096 x 131072 bf16 480 us, and 502.
+template <typename T, int THREADS, int N, int RESIDENT>
 void launch_rows(const DistillShape& a, unsigned here, hipStream_t stream) {
-    // as many workgroups as run at once (or a few more, where they are small): each goes through rows of its own
-    constexpr unsigned AT_ONCE = 256 * (2048 / THREADS);
-    hipLaunchKernelGGL((distill_row_kernel<T, THREADS, N>), dim3(here < AT_ONCE ? here : AT_ONCE), dim3(THREADS), 0, stream, a);
+    constexpr unsigned most = 256 * RESIDENT;
+    hipLaunchKernelGGL((distill_row_kernel<T, THREADS, N>), dim3(RESIDENT && here > most ? most : here), dim3(THREADS), 0, stream, a);
 }
 
 template <typename T>
@@ -364,13 +378,13 @@ void launch_distill_of(const LogitsArgs& args, hipStream_t stream) {
             continue;
         }
         const uint64_t bytes = a.vocab * sizeof(T);
-        if (bytes <= 4096) launch_rows<T, 256, 1>(a, here, stream);
-        else if (bytes <= 8192) launch_rows<T, 256, 2>(a, here, stream);
-        else if (bytes <= 16384) launch_rows<T, 256, 4>(a, here, stream);
-        else if (bytes <= 32768) launch_rows<T, 256, 8>(a, here, stream);
-        else if (bytes <= 65536) launch_rows<T, 512, 8>(a, here, stream);
-        else if (bytes <= 131072) launch_rows<T, 1024, 8>(a, here, stream);
-        else launch_rows<T, 1024, 16>(a, here, stream);
+        if (bytes <= 4096) launch_rows<T, 256, 1, 7>(a, here, stream);
+        else if (bytes <= 8192) launch_rows<T, 256, 2, 7>(a, here, stream);
+        else if (bytes <= 16384) launch_rows<T, 256, 4, 6>(a, here, stream);
+        else if (bytes <= 32768) launch_rows<T, 256, 8, 5>(a, here, stream);
+        else if (bytes <= 65536) launch_rows<T, 256, 16, 4>(a, here, stream);
+        else if (bytes <= 131072) launch_rows<T, 512, 16, 2>(a, here, stream);
+        else launch_rows<T, 1024, 16, 0>(a, here, stream);
     }
 }
 

@@ -30,8 +30,9 @@ struct TopShape : LogitsArgs {
     Part* found;                                                  // [row][part]
 };
 
+template <uint32_t ROOM>
 struct TopLds {
-    uint64_t list[kRoom];
+    uint64_t list[ROOM];
     uint32_t bins[256];
     uint64_t edges[2][kWaves];
     uint32_t totals[kWaves];
@@ -40,46 +41,41 @@ struct TopLds {
     uint32_t bin, above, inside;                                  // kth_rank: the k-th's bin, ranks in higher ones and in it
 };
 
-__device__ __forceinline__ uint64_t wave_max_rank(uint64_t v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint64_t other = __shfl_xor((unsigned long long)v, o);
-        v = other > v ? other : v;
-    }
-    return v;
-}
-
-// A number that exactly k of the list's n > k ranks reach.  Eight bits at a time from the first in which ranks differ: a histogram of those that agree with
-// what is known of the k-th, and the bin in which the k-th lies.
-__device__ uint64_t kth_rank(TopLds& s, uint32_t n, uint32_t k) {
+// A number that exactly k of the list's n > k ranks reach.  Up to eight bits at a time, of those in which ranks differ: a histogram of the ranks that agree
+// with what is known of the k-th, and the bin in which the k-th lies.
+template <uint32_t ROOM>
+__device__ uint64_t kth_rank(TopLds<ROOM>& s, uint32_t n, uint32_t k) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    uint64_t mine[kRoom / kThreads], high = 0, low = ~0ull;
+    uint64_t mine[ROOM / kThreads], some = 0, all = ~0ull;
 #pragma unroll
-    for (uint32_t q = 0; q < kRoom / kThreads; ++q) {
+    for (uint32_t q = 0; q < ROOM / kThreads; ++q) {
         const uint32_t at = q * kThreads + threadIdx.x;
         mine[q] = at < n ? s.list[at] : 0;                        // (0 is no rank)
-        high = mine[q] > high ? mine[q] : high;
-        if (at < n) low = mine[q] < low ? mine[q] : low;
+        some |= mine[q];
+        all &= at < n ? mine[q] : ~0ull;
     }
-    high = wave_max_rank(high);
-    low = ~wave_max_rank(~low);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        some |= __shfl_xor((unsigned long long)some, o);
+        all &= __shfl_xor((unsigned long long)all, o);
+    }
     if (lane == 0) {
-        s.edges[0][wave] = high;
-        s.edges[1][wave] = low;
+        s.edges[0][wave] = some;
+        s.edges[1][wave] = all;
     }
     s.bins[threadIdx.x] = 0;
     __syncthreads();
     for (int w = 0; w < kWaves; ++w) {
-        high = s.edges[0][w] > high ? s.edges[0][w] : high;
-        low = s.edges[1][w] < low ? s.edges[1][w] : low;
+        some |= s.edges[0][w];
+        all &= s.edges[1][w];
     }
-    int shift = 64 - __builtin_clzll(high ^ low);                 // the bits from here on are the same in all (n > 1: some differ)
-    uint64_t known = shift == 64 ? 0 : high >> shift << shift;
+    uint64_t open = some ^ all, known = all;                      // bits in which ranks differ and that are not known yet (n > 1: some); the k-th's others
     for (;;) {
-        const int next = shift > 8 ? shift - 8 : 0;
+        const int top = 64 - __builtin_clzll(open), next = top > 8 ? top - 8 : 0;
+        const uint64_t fixed = top == 64 ? 0 : ~0ull << top;
 #pragma unroll
-        for (uint32_t q = 0; q < kRoom / kThreads; ++q)
-            if (mine[q] && (shift == 64 || mine[q] >> shift == known >> shift)) atomicAdd(&s.bins[mine[q] >> next & ((1u << (shift - next)) - 1)], 1u);
+        for (uint32_t q = 0; q < ROOM / kThreads; ++q)
+            if (mine[q] && ((mine[q] ^ known) & fixed) == 0) atomicAdd(&s.bins[mine[q] >> next & 255u & ((1u << (top - next)) - 1)], 1u);
         __syncthreads();
         // thread i has bin 255 - i: what lies in it and above
         const uint32_t bin = 255 - threadIdx.x, here = s.bins[bin];
@@ -99,40 +95,44 @@ __device__ uint64_t kth_rank(TopLds& s, uint32_t n, uint32_t k) {
             s.inside = here;
         }
         __syncthreads();
-        known |= (uint64_t)s.bin << next;
+        const uint64_t digit = ((1ull << (top - next)) - 1) << next;
+        known = (known & ~digit) | (uint64_t)s.bin << next;
+        open &= ~digit & ~fixed;
         k -= s.above;
-        const bool all = s.inside == k;                           // all of the bin: nothing below matters
-        shift = next;
-        if (all || shift == 0) return known;
+        const bool whole = s.inside == k;                         // all of the bin: nothing below matters, and known has no open bit set
+        if (whole || open == 0) return known;
         __syncthreads();                                          // (s.bin is written again)
     }
 }
 
 // Leaves the k best of the list's n > k ranks in its first places, in no order; returns the lowest of them.
-__device__ uint64_t keep_best(TopLds& s, uint32_t n, uint32_t k) {
+template <uint32_t ROOM>
+__device__ uint64_t keep_best(TopLds<ROOM>& s, uint32_t n, uint32_t k) {
     const uint64_t bar = kth_rank(s, n, k);
-    uint64_t mine[kRoom / kThreads];
+    uint64_t mine[ROOM / kThreads];
 #pragma unroll
-    for (uint32_t q = 0; q < kRoom / kThreads; ++q) mine[q] = q * kThreads + threadIdx.x < n ? s.list[q * kThreads + threadIdx.x] : 0;
+    for (uint32_t q = 0; q < ROOM / kThreads; ++q) mine[q] = q * kThreads + threadIdx.x < n ? s.list[q * kThreads + threadIdx.x] : 0;
     if (threadIdx.x == 0) s.count = 0;
     __syncthreads();
 #pragma unroll
-    for (uint32_t q = 0; q < kRoom / kThreads; ++q)
+    for (uint32_t q = 0; q < ROOM / kThreads; ++q)
         if (mine[q] >= bar) s.list[atomicAdd(&s.count, 1u)] = mine[q];
     __syncthreads();
     return bar;
 }
 
-// The list's best k (all of it where it holds fewer) as pairs in ascending index order.
-template <typename F>
-__device__ void write_pairs(TopLds& s, uint32_t n, uint32_t k, F value) {
+// The list's best k (all of it where it holds fewer) as pairs in ascending index order.  A rank tells its logit, but not which zero or NaN it is.
+template <typename T, uint32_t ROOM>
+__device__ void write_pairs(TopLds<ROOM>& s, uint32_t n, uint32_t k, const T* z, uint2* pairs) {
     if (n > k) (void)keep_best(s, n, k);
     for (uint32_t q = threadIdx.x; q < k; q += kThreads) {
         const uint64_t rank = s.list[q];
-        const uint32_t mine = (uint32_t)rank;                     // the index's complement
-        uint32_t place = 0;
+        const uint32_t mine = (uint32_t)rank, key = (uint32_t)(rank >> 32);                // (mine: the index's complement)
+        uint32_t bits = key & 0x80000000u ? key & 0x7FFFFFFFu : ~key, place = 0;
+        if (bits == 0 || key == logit_key(__builtin_nanf(""))) bits = __float_as_uint((float)z[~mine]);
+#pragma unroll 8
         for (uint32_t i = 0; i < k; ++i) place += (uint32_t)s.list[i] > mine ? 1u : 0u;
-        value(place, ~mine);
+        pairs[place] = make_uint2(~mine, bits);
     }
 }
 
@@ -157,7 +157,7 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads, 4) top_logits_kernel(TopShape a) {
     constexpr uint32_t E = Pieces<T>::E, kStretch = kThreads * kPieces * E;
     using Piece = typename Pieces<T>::Piece;
-    __shared__ TopLds s;
+    __shared__ TopLds<kRoom> s;
     const uint64_t row = a.row0 + blockIdx.x;
     const uint32_t k = a.k, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
     const T* z = static_cast<const T*>(a.z) + row * a.z_ld;
@@ -165,40 +165,42 @@ __global__ void __launch_bounds__(kThreads, 4) top_logits_kernel(TopShape a) {
     const float scale = kLog2e / a.temperature;
     Spread spread = kNoSpread;
     uint64_t bar = 0;                                             // candidates: ranks above it
-    float bar_value = -__builtin_huge_valf();                     // logits below it are no candidates
-    bool first = true;
+    float bar_value = -kInf;                                      // logits below it are no candidates
+    auto raise = [&](uint64_t to) {
+        bar = to;
+        const uint32_t key = (uint32_t)(bar >> 32), bits = key & 0x80000000u ? key & 0x7FFFFFFFu : ~key;
+        bar_value = __uint_as_float(bits);
+    };
     if (threadIdx.x == 0) s.count = 0;
     uint32_t held = 0;                                            // in the list; the same in every thread
     __syncthreads();
 
-    for (uint64_t at = begin; at < end; at += kStretch) {
-        // element e of piece p: column at + (p kThreads + thread) E + e; -inf behind the end, which is never asked for
-        float v[kPieces][E];
-        const uint64_t mine = at + (uint64_t)threadIdx.x * E;
+    // Element e of piece p of a stretch: column at + (p kThreads + thread) E + e; what lies behind the end counts as minus infinity, and is no candidate.
+    auto fetch = [&](Piece (&raw)[kPieces], uint64_t at) {
+        const T* from = z + at + (uint64_t)threadIdx.x * E;
         if (at + kStretch <= end) {
-            Piece raw[kPieces];
 #pragma unroll
-            for (int p = 0; p < kPieces; ++p) raw[p] = *reinterpret_cast<const Piece*>(z + mine + (uint64_t)p * kThreads * E);
-#pragma unroll
-            for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-                for (uint32_t e = 0; e < E; ++e) v[p][e] = (float)raw[p][e];
+            for (int p = 0; p < kPieces; ++p) raw[p] = *reinterpret_cast<const Piece*>(from + (uint64_t)p * kThreads * E);
         } else {
 #pragma unroll
             for (int p = 0; p < kPieces; ++p)
 #pragma unroll
                 for (uint32_t e = 0; e < E; ++e) {
-                    const uint64_t c = mine + (uint64_t)p * kThreads * E + e;
-                    v[p][e] = c < end ? (float)z[c] : -__builtin_huge_valf();
+                    const uint64_t c = at + ((uint64_t)p * kThreads + threadIdx.x) * E + e;
+                    raw[p][e] = c < end ? z[c] : (T)-kInf;
                 }
         }
-        auto there = [&](int p, uint32_t e) { return mine + (uint64_t)p * kThreads * E + e < end; };
-        auto rank_of = [&](int p, uint32_t e) { return logit_rank(v[p][e], (uint32_t)(mine + (uint64_t)p * kThreads * E + e)); };
-        float most[kPieces];
+    };
+    auto go_through = [&](const Piece (&raw)[kPieces], uint64_t at, bool set_bar) {
+        float v[kPieces][E], most[kPieces];
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) most[p] = largest_of(v[p]);
+        for (int p = 0; p < kPieces; ++p) {
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) v[p][e] = (float)raw[p][e];
+            most[p] = largest_of(v[p]);
+        }
         add_logits(spread, v, largest_of(most), scale);
-        if (first && end - at >= (uint64_t)kThreads * kPieces * E) {
+        if (set_bar) {
             uint32_t key[kPieces];
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) key[p] = logit_key(most[p]);
@@ -208,61 +210,64 @@ __global__ void __launch_bounds__(kThreads, 4) top_logits_kernel(TopShape a) {
             uint32_t lowest = s.totals[0];
             for (int w = 1; w < kWaves; ++w) lowest = s.totals[w] < lowest ? s.totals[w] : lowest;
             __syncthreads();
-            if (lowest > 0) bar = ((uint64_t)(lowest - 1) << 32) | 0xFFFFFFFFull;         // everything of that key or a higher one passes
+            if (lowest > 0) raise(((uint64_t)(lowest - 1) << 32) | 0xFFFFFFFFull);        // everything of that key or a higher one passes
         }
-        first = false;
-        auto bar_to_value = [&] {
-            const uint32_t key = (uint32_t)(bar >> 32);
-            const uint32_t bits = key & 0x80000000u ? key & 0x7FFFFFFFu : ~key;
-            bar_value = bar == 0 ? -__builtin_huge_valf() : __uint_as_float(bits);
-        };
-        bar_to_value();
         // a logit passes if it is not below the bar's value (NaN passes) and its rank is above the bar
+        uint32_t passed = 0;
 #pragma unroll
         for (int p = 0; p < kPieces; ++p)
             if (!(most[p] < bar_value))
 #pragma unroll
-                for (uint32_t e = 0; e < E; ++e)
-                    if (!(v[p][e] < bar_value)) {
-                        const uint64_t rank = rank_of(p, e);
-                        if (rank > bar && there(p, e)) {
-                            const uint32_t place = atomicAdd(&s.count, 1u);
-                            if (place < kRoom) s.list[place] = rank;
-                        }
-                    }
+                for (uint32_t e = 0; e < E; ++e) passed |= v[p][e] < bar_value ? 0u : 1u << (p * E + e);
+        while (passed) {                                          // few: their logits are read once more
+            const uint32_t bit = __builtin_ctz(passed);
+            passed &= passed - 1;
+            const uint64_t column = at + ((uint64_t)(bit / E) * kThreads + threadIdx.x) * E + bit % E;
+            if (column >= end) continue;
+            const uint64_t rank = logit_rank((float)z[column], (uint32_t)column);
+            if (rank <= bar) continue;
+            const uint32_t place = atomicAdd(&s.count, 1u);
+            if (place < kRoom) s.list[place] = rank;
+        }
+    };
+    for (uint64_t at = begin; at < end; at += kStretch) {
+        Piece raw[kPieces];
+        fetch(raw, at);
+        go_through(raw, at, at == begin && at + kStretch <= end);
         __syncthreads();
         const uint32_t count = s.count;
         __syncthreads();
         if (count <= kRoom) {
             held = count;
             if (held > kLong) {                                   // (k <= 256: twice as many at least)
-                bar = keep_best(s, held, k);
+                raise(keep_best(s, held, k));
                 held = k;
             }
             continue;
         }
-        // too many: back to what was held, and one element of each thread at a time
+        // too many: back to what was held, and a logit of each thread at a time
         if (threadIdx.x == 0) s.count = held;
         __syncthreads();
-#pragma unroll
-        for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-            for (uint32_t e = 0; e < E; ++e) {
-                if (held + kThreads > kRoom) {
-                    bar = keep_best(s, held, k);
-                    held = k;
-                }
-                const uint64_t rank = rank_of(p, e);
-                if (rank > bar && there(p, e)) s.list[atomicAdd(&s.count, 1u)] = rank;
-                __syncthreads();
-                held = s.count;
-                __syncthreads();
+        const uint64_t to = at + kStretch < end ? at + kStretch : end;
+        for (uint64_t from = at; from < to; from += kThreads) {
+            if (held + kThreads > kRoom) {
+                raise(keep_best(s, held, k));
+                held = k;
             }
+            const uint64_t column = from + threadIdx.x;
+            if (column < to) {
+                const uint64_t rank = logit_rank((float)z[column], (uint32_t)column);
+                if (rank > bar) s.list[atomicAdd(&s.count, 1u)] = rank;
+            }
+            __syncthreads();
+            held = s.count;
+            __syncthreads();
+        }
     }
     spread = workgroup_spread<kWaves>(spread, scale, s.sums);
     __syncthreads();
     if (a.parts == 1) {
-        write_pairs(s, held, k, [&](uint32_t place, uint32_t index) { a.pairs[row * k + place] = make_uint2(index, __float_as_uint((float)z[index])); });
+        write_pairs(s, held, k, z, a.pairs + row * k);
         if (a.lse && threadIdx.x == 0) a.lse[row] = row_lse(spread, scale, a.temperature);
         return;
     }
@@ -278,7 +283,8 @@ __global__ void __launch_bounds__(kThreads, 4) top_logits_kernel(TopShape a) {
 // Joins the parts of a row.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) top_logits_join_kernel(TopShape a) {
-    __shared__ TopLds s;
+    constexpr uint32_t kRoom = 4096;                              // 16 lists of k = 64 hold some 1500
+    __shared__ TopLds<kRoom> s;
     const uint64_t row = a.row0 + blockIdx.x;
     const uint32_t k = a.k;
     const TopShape::Part* found = a.found + row * a.parts;
@@ -286,28 +292,50 @@ __global__ void __launch_bounds__(kThreads) top_logits_join_kernel(TopShape a) {
     __syncthreads();
     uint32_t held = 0;
     uint64_t bar = 0;
-    for (uint32_t p = 0; p < a.parts; ++p) {
-        const uint64_t* list = a.lists + (row * a.parts + p) * kLong;
-        const uint32_t n = found[p].held;
-        if (held + n > kRoom) {                                   // (n <= 512, k <= 256)
-            bar = keep_best(s, held, k);
-            held = k;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    uint32_t in_all = 0, mine_at = 0;                             // (parts <= 64)
+    Spread spread = kNoSpread;
+    {
+        TopShape::Part part{-kInf, 0.f, 0, 0};
+        if (lane < a.parts) part = found[lane];
+        if (wave == 0) spread = {part.max, part.sum};
+        const uint32_t n = part.held;
+        uint32_t upto = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t other = (uint32_t)__shfl_up((int)upto, o);
+            if (lane >= (uint32_t)o) upto += other;
         }
-        for (uint32_t q = threadIdx.x; q < n; q += kThreads)
-            if (list[q] > bar) s.list[atomicAdd(&s.count, 1u)] = list[q];
+        in_all = (uint32_t)__shfl((int)upto, 63);
+        mine_at = upto - n;
+    }
+    if (in_all <= kRoom) {                                        // room for all of them, one list behind the other
+        for (uint32_t p = wave; p < a.parts; p += kWaves) {
+            const uint64_t* list = a.lists + (row * a.parts + p) * kLong;
+            const uint32_t n = found[p].held, to = (uint32_t)__shfl((int)mine_at, p);
+            for (uint32_t q = lane; q < n; q += 64) s.list[to + q] = list[q];
+        }
+        held = in_all;
         __syncthreads();
-        held = s.count;
-        __syncthreads();
+    } else {
+        for (uint32_t p = 0; p < a.parts; ++p) {
+            const uint64_t* list = a.lists + (row * a.parts + p) * kLong;
+            const uint32_t n = found[p].held;
+            if (held + n > kRoom) {                               // (n <= 512, k <= 256)
+                bar = keep_best(s, held, k);
+                held = k;
+            }
+            for (uint32_t q = threadIdx.x; q < n; q += kThreads)
+                if (list[q] > bar) s.list[atomicAdd(&s.count, 1u)] = list[q];
+            __syncthreads();
+            held = s.count;
+            __syncthreads();
+        }
     }
     const T* z = static_cast<const T*>(a.z) + row * a.z_ld;
-    write_pairs(s, held, k, [&](uint32_t place, uint32_t index) { a.pairs[row * k + place] = make_uint2(index, __float_as_uint((float)z[index])); });
+    write_pairs(s, held, k, z, a.pairs + row * k);
     if (!a.lse) return;
     const float scale = kLog2e / a.temperature;
-    Spread spread = kNoSpread;
-    for (uint32_t p = threadIdx.x; p < a.parts; p += kThreads) {
-        const TopShape::Part v = found[p];
-        spread = join(spread, Spread{v.max, v.sum}, scale);
-    }
     spread = workgroup_spread<kWaves>(spread, scale, s.sums);
     if (threadIdx.x == 0) a.lse[row] = row_lse(spread, scale, a.temperature);
 }
