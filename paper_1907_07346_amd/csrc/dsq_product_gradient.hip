@@ -59,6 +59,9 @@ struct Rows {
 template <typename T, int TT, bool NARROW>
 __global__ void __launch_bounds__(kThreads, 2) product_gradient_kernel(GradientShape a) {
     constexpr int P = sizeof(T) == 4 ? 3 : 2, H = NARROW ? 2 : 1;
+    // What codes are too large by is taken off at the end, or, for fp32, every 32 rows, before sums grow: they are five times what the difference is, and so were
+    // their roundings (8192 x 5000, 16 tokens: 1.7e-6 of the result, now 8.5e-7, as sums in fp32 have).
+    constexpr bool kCentred = sizeof(T) == 4;
     constexpr uint32_t E = 16 / sizeof(T), PER = kBlockRows / E, PIECES = TT * 16 * PER / kThreads;   // 16-byte pieces of dy: elements, of a token, of a thread
     constexpr uint32_t kPitch = kBlockRows + E;                   // of a token's dy in LDS, elements
     using R = Rows<NARROW>;
@@ -194,11 +197,25 @@ __global__ void __launch_bounds__(kThreads, 2) product_gradient_kernel(GradientS
                     for (int e = 0; e < 8; ++e) d[e] = r0 + 8 * j + e < a.rows ? d[e] : 0.f;
                 Eight<__bf16> left[P];
                 split_operand<P>(d, left);
+                if constexpr (kCentred) {
+                    f32x4 from = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    off[t][h] = matrix_fma(left[p], centre_operand<__bf16>(), off[t][h]);
+                    for (int p = 0; p < P; ++p) from = matrix_fma(left[p], centre_operand<__bf16>(), from);
+                    from = -from;
 #pragma unroll
-                    for (int c = 0; c < COLS; ++c) sum[t][COLS * h + c] = matrix_fma(left[p], right[c], sum[t][COLS * h + c]);
+                    for (int c = 0; c < COLS; ++c) {
+                        f32x4 part = from;
+#pragma unroll
+                        for (int p = 0; p < P; ++p) part = matrix_fma(left[p], right[c], part);
+                        sum[t][COLS * h + c] += part;
+                    }
+                } else {
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        off[t][h] = matrix_fma(left[p], centre_operand<__bf16>(), off[t][h]);
+#pragma unroll
+                        for (int c = 0; c < COLS; ++c) sum[t][COLS * h + c] = matrix_fma(left[p], right[c], sum[t][COLS * h + c]);
+                    }
                 }
             }
         }
@@ -236,10 +253,11 @@ __global__ void __launch_bounds__(kThreads, 2) product_gradient_kernel(GradientS
         use(rows, 0, true, r0);
         __syncthreads();
     }
+    if constexpr (!kCentred)
 #pragma unroll
-    for (int t = 0; t < TT; ++t)
+        for (int t = 0; t < TT; ++t)
 #pragma unroll
-        for (int c = 0; c < 8; ++c) sum[t][c] -= off[t][NARROW ? c / 4 : 0];
+            for (int c = 0; c < 8; ++c) sum[t][c] -= off[t][NARROW ? c / 4 : 0];
 
     // join the waves, CT columns of each word at a time: [wave][column][token tile][lane], then rows of 128 columns
     constexpr int CT = 8 / TT;
