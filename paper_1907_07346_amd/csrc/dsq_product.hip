@@ -2,14 +2,18 @@
 //
 // Reading the message, 0.53 bytes a weight, is what cannot be done without, and leaves time for some four vector instructions a weight's
 // share of a lane.  Codes are bytes after half an instruction each, so x is made of bytes, too, and the products are integers: per token
-// and 128 columns ("chunk"; 64 where a block is 64), x = 2^e v with integers v of 16 bits (24 for fp32), written as two (three) signed bytes, most of which an i8 matrix instruction
-// takes as rows of their own.  All sums inside a chunk are exact; 15 sum v, which takes codes 0 .. 15 to 2 code - 15, is where they start.  What is rounded is v:
+// and 128 columns ("chunk"; 64 where a block is 64), x = 2^e v with integers v of 16 bits (24 for fp32), written as two (three) signed bytes, which an
+// i8 matrix instruction takes as rows of their own.  All sums inside a chunk are exact; 15 sum v, which takes codes 0 .. 15 to 2 code - 15, is where they start.  What is rounded is v:
 // 2^-15 (2^-23) of the largest |x| next to it at most, which the same block's scale multiplies and no code drops, against the 2^-8 or 2^-11 of
 // y's own rounding for 16-bit types (2^-24 for fp32).
-//   A wave takes 16 (or 32) rows and a chunk at a time: lane (n, j) = (l % 16, l / 16) holds 32 codes of row n (one 16-byte load) and the scale of its
-// block, which is one factor for all of the lane's results.  x's bytes lie in LDS in the order in which codes come out of a word.  Up to 8 tokens (4 for
-// fp32) each workgroup makes them itself; for more, a launch before makes them once, in work_dev.  The waves of a workgroup split its rows and, where there are few, its
-// columns (joined in LDS); where there are too few rows for the GPU, workgroups split the columns, too, and one more launch adds their sums.
+//   A wave takes 16 (or 32) rows and a chunk at a time: lane (n, j) = (l % 16, l / 16) holds 32 codes of row n and the scale of its block, which is
+// one factor for all of the lane's results.  x's bytes lie in LDS in the order in which codes come out of a word.
+//   Three kernels.  One token: product_one_kernel.  Up to two matrix instructions of tokens (16; 8 for fp32), where reading codes is most of the work:
+// product_tiles_kernel, whose workgroups make x's bytes themselves.  More tokens: product_kernel; a launch before makes x's bytes once, in work_dev,
+// and codes go straight into registers, which leaves LDS to x.  Measured, us, product_tiles_kernel against product_kernel: 2 x 65536 x 4096, bf16,
+// 42.0 : 45.5; 16 x 4096 x 16384, fp16, 19.0 : 24.8; 8 x 2048 x 2048 7.1 : 9.0; 4 x 16384 x 4096, fp32, 16.1 : 16.4; from there on 61 x 16001 x 4099,
+// bf16, 55.7 : 56.3; 64 x 65536 x 1024 31.7 : 28.0, and in blocks of 64 51.4 : 39.8; 32 x 16384 x 4096, fp32, 30.3 : 31.7.
+//   Where there are too few rows for the GPU, workgroups split the columns, too, and one more launch adds their sums.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
 
@@ -18,7 +22,6 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = kWaves * 64, kChunk = 128;   // of a workgroup; columns a wave takes at a time
 constexpr uint32_t kPanel = 64 * 1024;                            // bytes of LDS for x: two workgroups fit on a compute unit
-constexpr uint64_t kTokens = 64;                                  // of a launch
 constexpr uint64_t kGroupsOfLaunch = 1u << 22;                    // a launch dimension holds fewer than 2^32 work-items
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
@@ -36,6 +39,9 @@ struct Digits<float> {
 };
 template <typename T>
 constexpr int kTileTokens = 16 / Digits<T>::stride;               // tokens of a matrix instruction
+template <typename T>
+constexpr uint64_t kTokens = 8 * kTileTokens<T>;                  // of a launch
+constexpr int kRowTiles = 2;                                      // of 16 rows, of a wave of product_kernel
 
 struct ProductPlan {
     uint32_t row_waves;                                           // waves side by side; the other kWaves / row_waves split the columns
@@ -141,52 +147,84 @@ __device__ __forceinline__ int power_of(uint32_t bits, int exponent, float limit
     return __uint_as_float(bits) * power2_of(q) > limit ? q - 1 : q;
 }
 
-// Sixteen adjacent lanes, lane u with columns 8 u .. 8 u + 7 of a chunk, write a token's part of the chunk's record.
+// op over 8 or 16 adjacent lanes, in all of them: each lane with its mirror image, then with the others of its four.
+template <int CTRL>
+__device__ __forceinline__ uint32_t other_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
+template <int LANES, typename F>
+__device__ __forceinline__ uint32_t over_lanes(uint32_t v, F op) {
+    if (LANES == 16) v = op(v, other_lane<0x140>(v));             // row_mirror
+    v = op(v, other_lane<0x141>(v));                              // row_half_mirror
+    v = op(v, other_lane<0x4E>(v));                               // quad_perm 2 3 0 1
+    return op(v, other_lane<0xB1>(v));                            // quad_perm 1 0 3 2
+}
+
+// Eight columns of x, zero behind the last.
+template <typename T>
+struct EightOf {
+    typedef T Raw __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+};
+template <typename T>
+__device__ __forceinline__ typename EightOf<T>::Raw load_eight(const T* x, uint32_t col, uint32_t cols) {
+    using Raw = typename EightOf<T>::Raw;
+    if (col + 8 <= cols) return *reinterpret_cast<const Raw*>(x + col);
+    Raw raw;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) raw[e] = col + e < cols ? x[col + e] : (T)0.f;
+    return raw;
+}
+// The bits of the largest of eight magnitudes, of the type's width; NaN is above all.  And the bits of the same number in fp32.
+template <typename T>
+__device__ __forceinline__ uint32_t largest_bits(typename EightOf<T>::Raw raw) {
+    if constexpr (sizeof(T) == 2) {
+        typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        const u16x8 bits = __builtin_bit_cast(u16x8, raw) & (uint16_t)0x7FFF;
+        const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(bits.s01, bits.s23), __builtin_elementwise_max(bits.s45, bits.s67));
+        return m.x > m.y ? m.x : m.y;
+    } else {
+        uint32_t most = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t bits = __float_as_uint((float)raw[e]) & 0x7FFFFFFFu;
+            most = bits > most ? bits : most;
+        }
+        return most;
+    }
+}
+template <typename T>
+__device__ __forceinline__ uint32_t float_bits(uint32_t bits) {
+    if constexpr (sizeof(T) == 2) return __float_as_uint((float)__builtin_bit_cast(T, (uint16_t)bits));
+    else return bits;
+}
+
+// Sixteen adjacent lanes, lane u with columns 8 u .. 8 u + 7 of a chunk (raw), write a token's part of the chunk's record.
 template <typename T, int TT, bool NARROW>
-__device__ void make_digits(const ProductArgs& a, uint64_t chunk, uint32_t tok, uint32_t u, uint8_t* record) {
+__device__ void make_digits(uint32_t tokens, uint32_t tok, uint32_t u, typename EightOf<T>::Raw raw, uint8_t* record) {
     using D = Digits<T>;
     using R = Record<T, TT, NARROW>;
     constexpr int LANES = NARROW ? 8 : 16;                        // of a block
-    const uint32_t tokens = (uint32_t)a.tokens;
-    const uint64_t col = chunk * kChunk + 8 * u;
-    const T* x = static_cast<const T*>(a.in) + tok * a.in_ld + col;
-    float v[8];
-    if (col + 8 <= a.cols) {
-        typedef T Raw __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-        const Raw raw = *reinterpret_cast<const Raw*>(x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (float)raw[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = col + e < a.cols ? (float)x[e] : 0.f;
-    }
-    uint32_t most = 0;                                            // the bits of the largest |x|; NaN is above all
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t bits = __float_as_uint(v[e]) & 0x7FFFFFFFu;
-        most = bits > most ? bits : most;
-    }
-#pragma unroll
-    for (int o = 1; o < LANES; o <<= 1) {
-        const uint32_t other = (uint32_t)__shfl_xor((int)most, o);
-        most = other > most ? other : most;
-    }
+    // 2^power x, rounded, plus 128 in all digits but the highest: its bytes are the digits, their sign bits turned over where 128 was added
+    uint32_t most = over_lanes<LANES>(largest_bits<T>(raw), [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+    most = float_bits<T>(most);
     const int power = power_of(most, D::exponent, D::most);
-    const bool finite = most < 0x7F800000u;
+    const bool finite = most < 0x7F800000u;                       // (if not, the block counts as NaN, whatever its digits are)
     const float to = power2_of(power);
-    uint32_t bytes[D::digits][2];
-    int32_t sum[D::digits];
-#pragma unroll
-    for (int d = 0; d < D::digits; ++d) bytes[d][0] = bytes[d][1] = 0, sum[d] = 0;
+    uint32_t v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        int32_t rest = finite ? (int32_t)rintf(v[e] * to) : 0;
+        if constexpr (D::digits == 2) v[e] = __float_as_uint(fmaf((float)raw[e], to, 12582912.f + 128.f));   // 1.5 2^23: an ulp is 1
+        else v[e] = (uint32_t)(finite ? (int32_t)rintf((float)raw[e] * to) : 0) + 0x8080u;
+    }
+    uint32_t bytes[D::digits][2];                                 // the odd columns apart from the even ones
 #pragma unroll
-        for (int d = D::digits - 1; d >= 0; --d) {                // the last digit is the lowest
-            const int32_t digit = d ? (int32_t)(int8_t)rest : rest;
-            rest = (rest - digit) >> 8;
-            sum[d] += digit;
-            bytes[d][e % 2] |= ((uint32_t)digit & 255u) << (8 * (e / 2));
+    for (int o = 0; o < 2; ++o) {
+        const uint32_t a = __builtin_amdgcn_perm(v[2 + o], v[o], 0x05010400u), b = __builtin_amdgcn_perm(v[6 + o], v[4 + o], 0x05010400u);
+        bytes[D::digits - 1][o] = __builtin_amdgcn_perm(b, a, 0x05040100u) ^ 0x80808080u;
+        bytes[D::digits - 2][o] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        if constexpr (D::digits == 3) {
+            bytes[1][o] ^= 0x80808080u;
+            const uint32_t c = __builtin_amdgcn_perm(v[2 + o], v[o], 0x0C0C0602u), d = __builtin_amdgcn_perm(v[6 + o], v[4 + o], 0x0C0C0602u);
+            bytes[0][o] = __builtin_amdgcn_perm(d, c, 0x05040100u);
         }
     }
     const uint32_t t = NARROW ? u / 8 * 2 + u % 2 : u % 4, j = NARROW ? u % 8 / 2 : u / 4, rows = R::rows(tokens);
@@ -194,9 +232,10 @@ __device__ void make_digits(const ProductArgs& a, uint64_t chunk, uint32_t tok, 
     for (int d = 0; d < D::digits; ++d) {
         const uint32_t at = (((t / 2) * 4 + j) * rows + tok * D::stride + d) * 16 + 8 * (t % 2);
         *reinterpret_cast<u32x2*>(record + at) = u32x2{bytes[d][0], bytes[d][1]};
-#pragma unroll
-        for (int o = 1; o < LANES; o <<= 1) sum[d] += __shfl_xor(sum[d], o);
-        if (u % LANES == 0) R::start(record, tokens)[u / LANES * (TT * 16) + tok * D::stride + d] = -15 * sum[d];
+        constexpr int kOff = (int)0xF1F1F1F1;                     // -15 each
+        const int32_t sum = __builtin_amdgcn_sdot4((int)bytes[d][0], kOff, __builtin_amdgcn_sdot4((int)bytes[d][1], kOff, 0, false), false);
+        const uint32_t total = over_lanes<LANES>((uint32_t)sum, [](uint32_t x, uint32_t y) { return x + y; });
+        if (u % LANES == 0) R::start(record, tokens)[u / LANES * (TT * 16) + tok * D::stride + d] = (int32_t)total;
     }
     if (u % LANES == 0) R::unit(record, tokens)[u / LANES * (TT * 8) + tok] = finite ? power2_of(-power) : __builtin_nanf("");
 }
@@ -205,15 +244,68 @@ __device__ void make_digits(const ProductArgs& a, uint64_t chunk, uint32_t tok, 
 template <typename T, int TT, bool NARROW>
 __global__ void __launch_bounds__(256) product_digits_kernel(ProductShape a, uint8_t* panel) {
     const uint64_t chunk = blockIdx.x;
-    for (uint32_t tok = threadIdx.x / 16 + 16 * blockIdx.y; tok < a.tokens; tok += 16 * gridDim.y)
-        make_digits<T, TT, NARROW>(a, chunk, tok, threadIdx.x % 16, panel + chunk * Record<T, TT, NARROW>::bytes((uint32_t)a.tokens));
+    const uint32_t tok = threadIdx.x / 16 + 16 * blockIdx.y, u = threadIdx.x % 16;
+    if (tok >= a.tokens) return;
+    const T* x = static_cast<const T*>(a.in) + tok * a.in_ld;
+    make_digits<T, TT, NARROW>((uint32_t)a.tokens, tok, u, load_eight(x, (uint32_t)chunk * kChunk + 8 * u, (uint32_t)a.cols), panel + chunk * Record<T, TT, NARROW>::bytes((uint32_t)a.tokens));
 }
 
+// The products of a chunk of codes, 16 RT rows, with the chunk's record of x.  x_at: the lane's row of x in each tile.
 template <typename T, int TT, int RT, bool NARROW>
-__global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
+__device__ __forceinline__ void multiply(const Codes<NARROW> (&c)[RT], uint8_t* rec, uint32_t tokens, const uint32_t (&x_at)[TT], uint32_t j,
+                                         float (&sum)[RT][TT][4 / Digits<T>::stride]) {
     using D = Digits<T>;
     using R = Record<T, TT, NARROW>;
     constexpr int H = NARROW ? 2 : 1, PER = 4 / D::stride;        // blocks of a chunk; tokens of a lane and matrix instruction
+    const uint32_t x_rows = R::rows(tokens);
+    const i32x4* digits = R::digits(rec);
+    i32x4 codes[RT][2];
+    float unit[RT][H];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            codes[r][h] = i32x4{(int)(c[r].w[2 * h] << 1 & 0x1E1E1E1Eu), (int)(c[r].w[2 * h] >> 3 & 0x1E1E1E1Eu),
+                                (int)(c[r].w[2 * h + 1] << 1 & 0x1E1E1E1Eu), (int)(c[r].w[2 * h + 1] >> 3 & 0x1E1E1E1Eu)};
+#pragma unroll
+        for (int b = 0; b < H; ++b) unit[r][b] = c[r].scale[b] * (1.f / 15.f);
+    }
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        const i32x4 x0 = digits[x_at[t]], x1 = digits[4 * x_rows + x_at[t]];
+#pragma unroll
+        for (int b = 0; b < H; ++b) {
+            float count[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) count[i] = R::unit(rec, tokens)[b * (TT * 8) + (4 * t + j) * PER + i];
+            const i32x4 start = *reinterpret_cast<const i32x4*>(R::start(rec, tokens) + b * (TT * 16) + 16 * t + 4 * j);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                i32x4 p;
+                if constexpr (NARROW) {
+                    p = __builtin_amdgcn_mfma_i32_16x16x64_i8(b ? x1 : x0, codes[r][b], start, 0, 0, 0);
+                } else {
+                    p = __builtin_amdgcn_mfma_i32_16x16x64_i8(x0, codes[r][0], start, 0, 0, 0);
+                    p = __builtin_amdgcn_mfma_i32_16x16x64_i8(x1, codes[r][1], p, 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    float v;
+                    if constexpr (D::digits == 2) v = (float)((p[2 * i] << 8) + p[2 * i + 1]);
+                    else v = fmaf(fmaf((float)p[0], 256.f, (float)p[1]), 256.f, (float)p[2]);
+                    sum[r][t][i] = fmaf(unit[r][b] * count[i], v, sum[r][t][i]);
+                }
+            }
+        }
+    }
+}
+
+template <typename T, int TT, bool NARROW>
+__global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
+    constexpr int RT = kRowTiles;
+    using D = Digits<T>;
+    using R = Record<T, TT, NARROW>;
+    constexpr int PER = 4 / D::stride;                            // tokens of a lane and matrix instruction
     extern __shared__ __align__(16) uint8_t lds[];
     const uint32_t tokens = (uint32_t)a.tokens, x_rows = R::rows(tokens), record = R::bytes(tokens);
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane & 15, j = lane >> 4;
@@ -241,51 +333,9 @@ __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) sum[r][t][i] = 0.f;
 
-    auto use = [&](const Codes<NARROW> (&c)[RT], uint32_t chunk) {
-        uint8_t* rec = lds + chunk * record;
-        const i32x4* digits = R::digits(rec);
-        i32x4 codes[RT][2];
-        float unit[RT][H];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                codes[r][h] = i32x4{(int)(c[r].w[2 * h] << 1 & 0x1E1E1E1Eu), (int)(c[r].w[2 * h] >> 3 & 0x1E1E1E1Eu),
-                                    (int)(c[r].w[2 * h + 1] << 1 & 0x1E1E1E1Eu), (int)(c[r].w[2 * h + 1] >> 3 & 0x1E1E1E1Eu)};
-#pragma unroll
-            for (int b = 0; b < H; ++b) unit[r][b] = c[r].scale[b] * (1.f / 15.f);
-        }
-#pragma unroll
-        for (int t = 0; t < TT; ++t) {
-            const i32x4 x0 = digits[x_at[t]], x1 = digits[4 * x_rows + x_at[t]];
-#pragma unroll
-            for (int b = 0; b < H; ++b) {
-                float count[PER];
-#pragma unroll
-                for (int i = 0; i < PER; ++i) count[i] = R::unit(rec, tokens)[b * (TT * 8) + (4 * t + j) * PER + i];
-                const i32x4 start = *reinterpret_cast<const i32x4*>(R::start(rec, tokens) + b * (TT * 16) + 16 * t + 4 * j);
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    i32x4 p;
-                    if constexpr (NARROW) {
-                        p = __builtin_amdgcn_mfma_i32_16x16x64_i8(b ? x1 : x0, codes[r][b], start, 0, 0, 0);
-                    } else {
-                        p = __builtin_amdgcn_mfma_i32_16x16x64_i8(x0, codes[r][0], start, 0, 0, 0);
-                        p = __builtin_amdgcn_mfma_i32_16x16x64_i8(x1, codes[r][1], p, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int i = 0; i < PER; ++i) {
-                        float v;
-                        if constexpr (D::digits == 2) v = (float)((p[2 * i] << 8) + p[2 * i + 1]);
-                        else v = fmaf(fmaf((float)p[0], 256.f, (float)p[1]), 256.f, (float)p[2]);
-                        sum[r][t][i] = fmaf(unit[r][b] * count[i], v, sum[r][t][i]);
-                    }
-                }
-            }
-        }
-    };
+    auto use = [&](const Codes<NARROW> (&c)[RT], uint32_t chunk) { multiply<T, TT, RT, NARROW>(c, lds + chunk * record, tokens, x_at, j, sum); };
     // x goes through LDS in stages; codes of the next chunks are under way while these are multiplied
-    constexpr int AHEAD = RT == 1 ? 4 : 2;
+    constexpr int AHEAD = 2;
     Codes<NARROW> ring[AHEAD][RT];
     for (uint32_t from = 0; from < chunks; from += a.plan.stage_chunks) {
         const uint32_t count = chunks - from < a.plan.stage_chunks ? chunks - from : a.plan.stage_chunks;
@@ -301,15 +351,8 @@ __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
 #pragma unroll
             for (int s = 0; s < AHEAD; ++s) fetch(ring[s], s);
         if (from) __syncthreads();
-        if (TT == 1) {
-            for (uint32_t q = threadIdx.x / 16; q < count * tokens; q += kThreads / 16) {
-                const uint32_t tok = q / count, chunk = q % count;
-                make_digits<T, TT, NARROW>(a, c0 + from + chunk, tok, threadIdx.x % 16, lds + chunk * record);
-            }
-        } else {
-            const u32x4* src = reinterpret_cast<const u32x4*>(a.panel + (c0 + from) * record);
-            for (uint32_t q = threadIdx.x; q < count * record / 16; q += kThreads) reinterpret_cast<u32x4*>(lds)[q] = src[q];
-        }
+        const u32x4* src = reinterpret_cast<const u32x4*>(a.panel + (c0 + from) * record);
+        for (uint32_t q = threadIdx.x; q < count * record / 16; q += kThreads) reinterpret_cast<u32x4*>(lds)[q] = src[q];
         __syncthreads();
         for (uint32_t q = 0; q < mine; q += AHEAD) {
 #pragma unroll
@@ -362,6 +405,130 @@ __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
                 if (a.partial) a.partial[((uint64_t)blockIdx.y * tokens + tok) * a.rows + at] = sum[r][t][i];
                 else product_store<T>(a, at, tok, sum[r][t][i]);
             }
+}
+
+// Few tokens: codes go through LDS, too, 128 rows of 256 columns at a time, so that memory is read in rows of 128 bytes (see product_one_kernel) and a
+// compute unit has as much under way as it multiplies.  While a stage is multiplied the next one's loads are on their way into registers; then it goes into
+// the other half of the LDS.  Rows of codes are 128 bytes apart, their 16-byte pieces swapped by the row's last bits against bank conflicts.
+//   16 tokens cost some 340 instructions a stage, 5400 clocks for the two workgroups of a compute unit, in which it could read 44 KB and reads 32: x's
+// digits are a third of them.  16 x 4096 x 16384 reads 2.3 TB/s, 16 x 65536 x 4096 3.2 (44.0 us), 2 x 65536 x 4096 3.4.  Slower: two stages ahead
+// (registers; 16 x 4096 x 16384 22.8 us), workgroups of 256 rows (2 x 65536 x 4096 46.8 us).
+constexpr uint32_t kStageChunks = 2, kSlots = kStageChunks * 4;   // of a stage; 16-byte pieces of a row
+
+template <typename T, int TT, bool NARROW>
+struct Stage {
+    static constexpr uint32_t H = NARROW ? 2 : 1, rows = 16 * kWaves, codes = rows * kSlots * 16, scales = rows * kStageChunks * H * 4;
+    __host__ __device__ static uint32_t bytes(uint32_t tokens) { return codes + scales + kStageChunks * Record<T, TT, NARROW>::bytes(tokens); }
+};
+
+template <typename T, int TT, bool NARROW>
+__global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a) {
+    using S = Stage<T, TT, NARROW>;
+    static_assert(16 * kStageChunks * TT * kTileTokens<T> <= kThreads, "a thread has eight columns of x");
+    using R = Record<T, TT, NARROW>;
+    using Raw = typename EightOf<T>::Raw;
+    constexpr int PER = 4 / Digits<T>::stride, H = S::H;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const uint32_t tokens = (uint32_t)a.tokens, x_rows = R::rows(tokens), record = R::bytes(tokens), half = S::bytes(tokens);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane & 15, j = lane >> 4;
+    const uint32_t block_log2 = 31 - __builtin_clz(a.block), pitch = 4 + a.block / 2;
+    const uint64_t all_stages = (a.cols + kStageChunks * kChunk - 1) / (kStageChunks * kChunk);
+    const uint32_t cols = (uint32_t)a.cols, s0 = blockIdx.y * a.plan.part_chunks;          // (of stages here)
+    const uint32_t stages = (uint32_t)(all_stages - s0 < a.plan.part_chunks ? all_stages - s0 : a.plan.part_chunks);
+    const uint64_t first = a.row0 + (uint64_t)blockIdx.x * S::rows;
+
+    // what the thread brings: two pieces of codes, a scale, and x
+    const uint32_t slot = threadIdx.x % kSlots, tile_row = threadIdx.x / kSlots;           // and as many rows on
+    auto row_at = [&](uint32_t r) { return a.msg + (first + r < a.rows ? first + r : a.rows - 1) * a.row_bytes; };
+    const uint8_t* code_row[2] = {row_at(tile_row), row_at(tile_row + S::rows / 2)};
+    constexpr uint32_t SCALES = kStageChunks * H;                 // of a row
+    const bool has_scale = threadIdx.x < S::rows * SCALES;
+    const uint8_t* scale_row = row_at(threadIdx.x / SCALES % S::rows);
+    const uint32_t x_tok = threadIdx.x / (16 * kStageChunks), x_unit = threadIdx.x % (16 * kStageChunks);
+    const T* x_row = static_cast<const T*>(a.in) + (x_tok < tokens ? x_tok : tokens - 1) * a.in_ld;
+    struct Brought {
+        u32x4 codes[2];
+        float scale;
+        Raw x;
+    };
+    auto bring = [&](Brought& v, uint32_t s) {
+        const uint32_t col = (s0 + s) * (kStageChunks * kChunk), mine = col + 32 * slot, of_scale = col + threadIdx.x % SCALES * (kChunk / H);
+        const uint32_t at = (mine >> block_log2) * pitch + 4 + (mine & (a.block - 1)) / 2, scale_at = (of_scale >> block_log2) * pitch;   // a row is below 2^28 bytes
+        const bool whole = col + kStageChunks * kChunk <= cols;
+        if (whole) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) v.codes[i] = *reinterpret_cast<const u32x4_at4*>(code_row[i] + at);
+            v.scale = *reinterpret_cast<const float*>(scale_row + scale_at);
+            v.x = *reinterpret_cast<const Raw*>(x_row + (col + 8 * x_unit));
+        } else {                                                  // the ragged end: words that are not there are 0
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) v.codes[i][w] = mine + 8 * w < cols ? *reinterpret_cast<const uint32_t*>(code_row[i] + at + 4 * w) : 0u;
+            v.scale = of_scale < cols ? *reinterpret_cast<const float*>(scale_row + scale_at) : 0.f;
+            v.x = load_eight(x_row, col + 8 * x_unit, cols);
+        }
+    };
+    auto put = [&](const Brought& v, uint8_t* to) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t r = tile_row + S::rows / 2 * i;
+            if constexpr (NARROW) {                               // piece s of a chunk: words 4 (s % 2) .. + 3 of block s / 2, for lanes 2 (s % 2) and + 1
+                const uint32_t chunk = slot / 4, h = slot % 4 / 2, lane0 = chunk * 4 + slot % 2 * 2;
+#pragma unroll
+                for (int w = 0; w < 2; ++w)
+                    *reinterpret_cast<u32x2*>(to + (r * kSlots + ((lane0 + w) ^ (r % kSlots))) * 16 + 8 * h) = u32x2{v.codes[i][2 * w], v.codes[i][2 * w + 1]};
+            } else {
+                *reinterpret_cast<u32x4*>(to + (r * kSlots + (slot ^ (r % kSlots))) * 16) = v.codes[i];
+            }
+        }
+        if (has_scale) reinterpret_cast<float*>(to + S::codes)[threadIdx.x] = v.scale;
+        uint8_t* records = to + S::codes + S::scales;
+        if (x_tok < tokens) make_digits<T, TT, NARROW>(tokens, x_tok, x_unit % 16, v.x, records + x_unit / 16 * record);
+    };
+
+    uint32_t x_at[TT];                                            // the lane's row of x in each tile; rows that are not there repeat the last
+#pragma unroll
+    for (int t = 0; t < TT; ++t) x_at[t] = j * x_rows + (16 * t + n < x_rows ? 16 * t + n : x_rows - 1);
+    float sum[1][TT][PER];
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) sum[0][t][i] = 0.f;
+    const uint32_t my_row = wave * 16 + n;
+    auto use = [&](uint8_t* from) {
+#pragma unroll
+        for (uint32_t c = 0; c < kStageChunks; ++c) {
+            Codes<NARROW> codes[1];
+            const u32x4 v = *reinterpret_cast<const u32x4*>(from + (my_row * kSlots + ((c * 4 + j) ^ (my_row % kSlots))) * 16);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) codes[0].w[w] = v[w];
+#pragma unroll
+            for (int h = 0; h < H; ++h) codes[0].scale[h] = reinterpret_cast<const float*>(from + S::codes)[my_row * SCALES + c * H + h];
+            multiply<T, TT, 1, NARROW>(codes, from + S::codes + S::scales + c * record, tokens, x_at, j, sum);
+        }
+    };
+    // Stage s is multiplied out of one half of the LDS while stage s + 1 is on its way.  (The last one again behind the end: no branch.)
+    Brought coming;
+    bring(coming, 0);
+    put(coming, lds);
+    __syncthreads();
+    for (uint32_t s = 0; s < stages; ++s) {
+        bring(coming, s + 1 < stages ? s + 1 : s);
+        use(lds + (s & 1) * half);
+        put(coming, lds + ((s + 1) & 1) * half);
+        __syncthreads();
+    }
+    const uint64_t at = first + my_row;
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t tok = (4 * t + j) * PER + i;
+            if (at >= a.rows || tok >= tokens) continue;
+            if (a.partial) a.partial[((uint64_t)blockIdx.y * tokens + tok) * a.rows + at] = sum[0][t][i];
+            else product_store<T>(a, at, tok, sum[0][t][i]);
+        }
 }
 
 // One token: rows of codes are read whole, which costs the memory pipeline a third of what sixteen rows of 64 bytes cost a load, and meet x in
@@ -576,8 +743,7 @@ void by_tiles(int tiles, bool narrow, F f) {
     if (tiles == 1) with(std::integral_constant<int, 1>());
     else if (tiles == 2) with(std::integral_constant<int, 2>());
     else if (tiles == 4) with(std::integral_constant<int, 4>());
-    else if (tiles == 8) with(std::integral_constant<int, 8>());
-    else if constexpr (sizeof(T) == 4) with(std::integral_constant<int, 16>());
+    else with(std::integral_constant<int, 8>());
 }
 
 template <typename T>
@@ -588,14 +754,22 @@ uint32_t record_bytes(uint64_t tokens, bool narrow) {
 }
 
 template <typename T>
-constexpr int kRowTiles(int tiles) { return tiles >= 4 ? 2 : 1; }  // of 16 rows, in a wave
-
-template <typename T>
 ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens, bool narrow) {
     ProductPlan p{};
     const int tiles = product_tiles<T>(tokens);
-    const uint64_t chunks = (cols + kChunk - 1) / kChunk, height = 16 * kRowTiles<T>(tiles), row_tiles = (rows + height - 1) / height;
+    const uint64_t chunks = (cols + kChunk - 1) / kChunk, height = 16 * kRowTiles, row_tiles = (rows + height - 1) / height;
     const uint32_t record = record_bytes<T>(tokens, narrow);
+    if (tiles <= 2) {
+        // A workgroup for every compute unit, as long as there is a stage for it: 8 x 2048 x 2048, bf16, 1 part 9.6 us, 2: 9.2, 4: 7.6, 8 (128 workgroups,
+        // a stage each): 7.1.  Two of them, as long as there are four stages for each: 4 x 16384 x 4096, fp32, 2 parts (256 workgroups) 17.6 us,
+        // 4: 16.3, 8: 17.0; 16 x 4096 x 4096, blocks of 64, 8 parts (256, two stages each) 10.7, 16: 13.5.
+        const uint64_t stages = (chunks + kStageChunks - 1) / kStageChunks, groups = (rows + 16 * kWaves - 1) / (16 * kWaves);
+        p.parts = 1;
+        while (p.parts < 32 && ((groups * p.parts < 256 && stages >= 2 * p.parts) || (groups * p.parts < 512 && stages >= 8 * p.parts))) p.parts *= 2;
+        p.part_chunks = (uint32_t)((stages + p.parts - 1) / p.parts);
+        p.parts = (uint32_t)((stages + p.part_chunks - 1) / p.part_chunks);
+        return p;
+    }
     // A workgroup reads all of x for the rows it has: not more bytes of it than of codes, as far as eight waves of rows go.
     p.row_waves = 1;
     while (p.row_waves < kWaves && (record > 64 * height * p.row_waves || row_tiles / (2 * p.row_waves) >= 512)) p.row_waves *= 2;
@@ -609,34 +783,48 @@ ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens, bool nar
     return p;
 }
 
-// Scratch: the panel, then the partial sums.
+// Scratch: the panel (of product_kernel), then the partial sums.
 template <typename T>
 uint64_t panel_bytes(uint64_t cols, uint64_t tokens, bool narrow) {
-    return product_tiles<T>(tokens) == 1 ? 0 : (cols + kChunk - 1) / kChunk * record_bytes<T>(tokens, narrow);
+    return product_tiles<T>(tokens) > 2 ? (cols + kChunk - 1) / kChunk * record_bytes<T>(tokens, narrow) : 0;
 }
 template <typename T>
 uint64_t scratch_bytes(uint64_t rows, uint64_t cols, uint64_t tokens, bool narrow) {
-    const uint64_t parts = product_plan<T>(rows, cols, tokens, narrow).parts;
-    return panel_bytes<T>(cols, tokens, narrow) + (parts > 1 ? parts * tokens * rows * sizeof(float) : 0);
+    const ProductPlan plan = product_plan<T>(rows, cols, tokens, narrow);
+    return panel_bytes<T>(cols, tokens, narrow) + (plan.parts > 1 ? plan.parts * tokens * rows * sizeof(float) : 0);
+}
+
+// Launches with as many workgroups as a launch takes: launch(first row, workgroups).
+template <typename F>
+void over_rows(uint64_t rows, uint64_t height, F launch) {
+    const uint64_t groups = (rows + height - 1) / height;
+    for (uint64_t g = 0; g < groups; g += kGroupsOfLaunch) launch(g * height, (unsigned)(groups - g < kGroupsOfLaunch ? groups - g : kGroupsOfLaunch));
 }
 
 template <typename T, int TT, bool NARROW>
-void launch_product_kernels(const ProductShape& a, hipStream_t stream) {
-    constexpr int RT = kRowTiles<T>(TT);
-    using R = Record<T, TT, NARROW>;
-    const uint32_t tokens = (uint32_t)a.tokens, join = a.plan.row_waves == kWaves ? 0 : kThreads * RT * TT * (4 / Digits<T>::stride) * 4;
-    const uint32_t panel = a.plan.stage_chunks * R::bytes(tokens), bytes = panel > join ? panel : join;
-    ProductShape b = a;
-    if (TT > 1) {
-        const unsigned chunks = (unsigned)((a.cols + kChunk - 1) / kChunk);
-        hipLaunchKernelGGL((product_digits_kernel<T, TT, NARROW>), dim3(chunks, (tokens + 15) / 16), dim3(256), 0, stream, b, static_cast<uint8_t*>(a.work));
-        b.panel = static_cast<const uint8_t*>(a.work);
-    }
-    const uint64_t height = 16 * RT * a.plan.row_waves, groups = (a.rows + height - 1) / height;
-    for (uint64_t g = 0; g < groups; g += kGroupsOfLaunch) {
-        b.row0 = g * height;
-        const uint64_t here = groups - g < kGroupsOfLaunch ? groups - g : kGroupsOfLaunch;
-        hipLaunchKernelGGL((product_kernel<T, TT, RT, NARROW>), dim3((unsigned)here, a.plan.parts), dim3(kThreads), bytes, stream, b);
+void launch_product_tiles(ProductShape a, hipStream_t stream) {
+    using S = Stage<T, TT, NARROW>;
+    const uint32_t lds = 2 * S::bytes((uint32_t)a.tokens);
+    static_assert(2 * (S::codes + S::scales + kStageChunks * (4096 + 2 * TT * 96)) <= 64 * 1024, "what a launch may ask for");
+    over_rows(a.rows, S::rows, [&](uint64_t row0, unsigned groups) {
+        a.row0 = row0;
+        hipLaunchKernelGGL((product_tiles_kernel<T, TT, NARROW>), dim3(groups, a.plan.parts), dim3(kThreads), lds, stream, a);
+    });
+}
+
+template <typename T, int TT, bool NARROW>
+void launch_product_kernels(ProductShape a, hipStream_t stream) {
+    if constexpr (TT <= 2) {
+        launch_product_tiles<T, TT, NARROW>(a, stream);
+    } else {
+        const uint32_t tokens = (uint32_t)a.tokens, join = a.plan.row_waves == kWaves ? 0 : kThreads * kRowTiles * TT * (4 / Digits<T>::stride) * 4;
+        const uint32_t panel = a.plan.stage_chunks * Record<T, TT, NARROW>::bytes(tokens), lds = panel > join ? panel : join;
+        hipLaunchKernelGGL((product_digits_kernel<T, TT, NARROW>), dim3((unsigned)((a.cols + kChunk - 1) / kChunk), (tokens + 15) / 16), dim3(256), 0, stream, a, static_cast<uint8_t*>(a.work));
+        a.panel = static_cast<const uint8_t*>(a.work);
+        over_rows(a.rows, 16 * kRowTiles * a.plan.row_waves, [&](uint64_t row0, unsigned groups) {
+            a.row0 = row0;
+            hipLaunchKernelGGL((product_kernel<T, TT, NARROW>), dim3(groups, a.plan.parts), dim3(kThreads), lds, stream, a);
+        });
     }
 }
 
@@ -651,22 +839,21 @@ void launch_product_one(ProductShape a, hipStream_t stream) {
     // 16: 27.9, 32: 28.2, 64: 28.6; 4096 x 16384 8: 15.4 (512 workgroups), 16: 13.2, 32: 16.8 (128); 2048 x 2048 1: 4.1, 4: 4.7, 16: 7.6.
     const uint64_t each = a.rows / (256ull * a.plan.row_waves) / AT_ONCE * AT_ONCE;
     a.plan.wave_rows = (uint32_t)(each < AT_ONCE ? AT_ONCE : each > 32 ? 32 : each);
-    const uint64_t rows_here = (uint64_t)a.plan.row_waves * a.plan.wave_rows, groups = (a.rows + rows_here - 1) / rows_here;
+    const uint64_t rows_here = (uint64_t)a.plan.row_waves * a.plan.wave_rows;
     const uint32_t bytes = col_waves * G * (Nibbles<T>::digits * 16 + 8) + kWaves * a.plan.wave_rows * 4;
-    for (uint64_t q = 0; q < groups; q += kGroupsOfLaunch) {
-        a.row0 = q * rows_here;
-        const uint64_t here = groups - q < kGroupsOfLaunch ? groups - q : kGroupsOfLaunch;
-        hipLaunchKernelGGL((product_one_kernel<T, G>), dim3((unsigned)here), dim3(kThreads), bytes, stream, a);
-    }
+    over_rows(a.rows, rows_here, [&](uint64_t row0, unsigned groups) {
+        a.row0 = row0;
+        hipLaunchKernelGGL((product_one_kernel<T, G>), dim3(groups), dim3(kThreads), bytes, stream, a);
+    });
 }
 
 template <typename T>
 void launch_product_of(const ProductArgs& args, hipStream_t stream) {
     const bool narrow = args.block == 64;
-    for (uint64_t t0 = 0; t0 < args.tokens; t0 += kTokens) {
+    for (uint64_t t0 = 0; t0 < args.tokens; t0 += kTokens<T>) {
         ProductShape a{};
         static_cast<ProductArgs&>(a) = args;
-        a.tokens = args.tokens - t0 < kTokens ? args.tokens - t0 : kTokens;
+        a.tokens = args.tokens - t0 < kTokens<T> ? args.tokens - t0 : kTokens<T>;
         a.in = static_cast<const T*>(args.in) + t0 * args.in_ld;
         a.out = static_cast<T*>(args.out) + t0 * args.out_ld;
         if (a.tokens == 1 && a.cols > 24) {                         // (see the kernel)
@@ -680,12 +867,10 @@ void launch_product_of(const ProductArgs& args, hipStream_t stream) {
         if (a.plan.parts > 1) a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(a.work) + panel_bytes<T>(a.cols, a.tokens, narrow));
         by_tiles<T>(product_tiles<T>(a.tokens), narrow, [&](auto t, auto n) { launch_product_kernels<T, decltype(t)::value, decltype(n)::value>(a, stream); });
         if (!a.partial) continue;
-        const uint64_t groups = (a.rows + 255) / 256;
-        for (uint64_t g = 0; g < groups; g += kGroupsOfLaunch) {
-            a.row0 = g * 256;
-            const uint64_t here = groups - g < kGroupsOfLaunch ? groups - g : kGroupsOfLaunch;
-            hipLaunchKernelGGL(product_join_kernel<T>, dim3((unsigned)here, (unsigned)a.tokens), dim3(256), 0, stream, a);
-        }
+        over_rows(a.rows, 256, [&](uint64_t row0, unsigned groups) {
+            a.row0 = row0;
+            hipLaunchKernelGGL(product_join_kernel<T>, dim3(groups, (unsigned)a.tokens), dim3(256), 0, stream, a);
+        });
     }
 }
 
@@ -693,14 +878,15 @@ void launch_product_of(const ProductArgs& args, hipStream_t stream) {
 
 uint64_t product_work_bytes(const ds_matrix& m) {
     uint64_t bytes = 0;
-    auto most = [&](uint64_t tokens) {                            // of the launches: whole ones and the last
-        by_dtype(m.dtype, [&](auto kind) {
-            const uint64_t here = scratch_bytes<decltype(kind)>(m.rows, m.cols, tokens, m.block == 64);
+    by_dtype(m.dtype, [&](auto kind) {
+        using T = decltype(kind);
+        auto most = [&](uint64_t tokens) {                        // of the launches: whole ones and the last
+            const uint64_t here = scratch_bytes<T>(m.rows, m.cols, tokens, m.block == 64);
             if (here > bytes) bytes = here;
-        });
-    };
-    if (m.tokens >= kTokens) most(kTokens);
-    if (m.tokens % kTokens) most(m.tokens % kTokens);
+        };
+        if (m.tokens >= kTokens<T>) most(kTokens<T>);
+        if (m.tokens % kTokens<T>) most(m.tokens % kTokens<T>);
+    });
     return bytes;
 }
 
