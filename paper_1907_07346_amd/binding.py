@@ -241,11 +241,11 @@ def _refuse(where: str, why: str):
     raise DsqError(DS_EINVAL, where, why)
 
 
-def _on_device(where: str, **tensors):
+def _on_device(where: str, names: str, *tensors):
     here = torch.cuda.current_device()
-    for name, t in tensors.items():
-        if t is not None and not (t.is_cuda and t.get_device() == here):
-            _refuse(where, f"{name} must be on the current CUDA device")
+    for at, t in enumerate(tensors):
+        if t is not None and (not t.is_cuda or t.get_device() != here):
+            _refuse(where, f"{names.split()[at]} must be on the current CUDA device")
 
 
 def _rows_of(where: str, name: str, t: "torch.Tensor"):
@@ -266,24 +266,27 @@ def _vector(where: str, name: str, t: "Optional[torch.Tensor]", rows: int):
     return t.data_ptr()
 
 
-def _new(stream, shape, dtype):
-    """A tensor whose memory belongs to the stream that the call runs on."""
+def _new(stream, shape, dtype, like):
+    """A tensor on like's device whose memory belongs to the stream that the call runs on."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device="cuda")
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device="cuda")
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _answer(name: str, shape, args, stream):
+def _answer(name: str, shape, like, stream, *args):
     """Calls `name` with scratch memory of the call's stream; the reason of a refusal goes into the exception."""
+    if stream is not None and stream.device_index != like.get_device():
+        _refuse(name, "stream must be of the current CUDA device")
     L = lib()
+    shape = ctypes.byref(shape)
     size = getattr(L, name + "_work_bytes")(shape)
-    work = _new(stream, (size,), torch.uint8) if size else None
-    args = [shape, *args, work.data_ptr() if size else None, size, _stream_pointer(stream)]
-    st = getattr(L, name)(*args, None, 0)
+    work = _new(stream, (size,), torch.uint8, like) if size else None
+    call, end = getattr(L, name), (work.data_ptr() if size else None, size, _stream_pointer(stream))
+    st = call(shape, *args, *end, None, 0)
     if st == DS_EINVAL:                                   # (checks only: nothing has been enqueued)
         buf = ctypes.create_string_buffer(256)
-        getattr(L, name)(*args, buf, 256)
+        call(shape, *args, *end, buf, 256)
         raise DsqError(st, name, buf.value.decode())
     if st != DS_OK:
         raise DsqError(st, name)
@@ -302,14 +305,16 @@ def _through(name: str, msg: "torch.Tensor", x: "torch.Tensor", rows: int, cols:
     m = ds_matrix(rows, cols, tokens, block, _DTYPES[x.dtype])
     if msg.dtype != torch.uint8 or not msg.is_contiguous() or msg.numel() < lib().ds_matrix_bytes(ctypes.byref(m)):
         _refuse(name, "msg must be a contiguous uint8 tensor that holds the matrix")
-    _on_device(name, msg=msg, x=x, out=out)
+    _on_device(name, "msg x out", msg, x, out)
+    out_pitch = out_width
     if out is None:
-        out = _new(stream, (tokens, out_width), x.dtype)
-    elif out.dtype != x.dtype or tuple(out.shape) != (tokens, out_width):
+        out = _new(stream, (tokens, out_width), x.dtype, x)
+    elif out.dtype != x.dtype or out.shape != (tokens, out_width):
         _refuse(name, f"out must be ({tokens}, {out_width}) and of the input's dtype")
-    out_pitch = _rows_of(name, "out", out)[2]
+    else:
+        out_pitch = _rows_of(name, "out", out)[2]
     if tokens:
-        _answer(name, ctypes.byref(m), [msg.data_ptr(), x.data_ptr(), pitch, out.data_ptr(), out_pitch], stream)
+        _answer(name, m, x, stream, msg.data_ptr(), x.data_ptr(), pitch, out.data_ptr(), out_pitch)
     return out
 
 
@@ -328,13 +333,13 @@ def ds_product_gradient(msg: "torch.Tensor", dy: "torch.Tensor", cols: int, bloc
 def ds_top_logits(z: "torch.Tensor", k: int, temperature: float = 1.0, stream: Optional["torch.cuda.Stream"] = None):
     """The k largest logits of each row of z: (pairs, lse), pairs int32 (rows, k, 2) of index and float32 bits, ascending index."""
     rows, vocab, pitch = _rows_of("ds_top_logits", "z", z)
-    _on_device("ds_top_logits", z=z)
+    _on_device("ds_top_logits", "z", z)
     if not 1 <= k <= 256:
         _refuse("ds_top_logits", "k must be between 1 and 256")
-    pairs, lse = _new(stream, (rows, k, 2), torch.int32), _new(stream, (rows,), torch.float32)
+    pairs, lse = _new(stream, (rows, k, 2), torch.int32, z), _new(stream, (rows,), torch.float32, z)
     if rows:
-        _answer("ds_top_logits", ctypes.byref(ds_logits(rows, vocab, k, _DTYPES[z.dtype], temperature, 0)),
-                [z.data_ptr(), pitch, pairs.data_ptr(), lse.data_ptr()], stream)
+        _answer("ds_top_logits", ds_logits(rows, vocab, k, _DTYPES[z.dtype], temperature, 0), z, stream,
+                z.data_ptr(), pitch, pairs.data_ptr(), lse.data_ptr())
     return pairs, lse
 
 
@@ -346,22 +351,23 @@ def ds_distill(z: "torch.Tensor", pairs: "torch.Tensor", temperature: float = 1.
     rows, vocab, pitch = _rows_of("ds_distill", "z", z)
     if pairs.dtype != torch.int32 or pairs.dim() != 3 or pairs.shape[0] != rows or pairs.shape[2] != 2 or not pairs.is_contiguous():
         _refuse("ds_distill", f"pairs must be a contiguous int32 tensor ({rows}, k, 2)")
-    _on_device("ds_distill", z=z, pairs=pairs, teacher_lse=teacher_lse, weight=weight, dz=dz)
-    given = [_vector("ds_distill", "teacher_lse", teacher_lse, rows), _vector("ds_distill", "weight", weight, rows)]
-    loss = _new(stream, (rows,), torch.float32) if want_loss else None
-    dz_pitch = 0
+    _on_device("ds_distill", "z pairs teacher_lse weight dz", z, pairs, teacher_lse, weight, dz)
+    given = _vector("ds_distill", "teacher_lse", teacher_lse, rows), _vector("ds_distill", "weight", weight, rows)
+    loss = _new(stream, (rows,), torch.float32, z) if want_loss else None
+    dz_pitch = vocab if want_gradient else 0
     if want_gradient:
         if dz is None:
-            dz = _new(stream, (rows, vocab), z.dtype)
+            dz = _new(stream, (rows, vocab), z.dtype, z)
         elif dz.dtype != z.dtype or dz.shape != z.shape:
             _refuse("ds_distill", "dz must have z's shape and dtype")
-        dz_pitch = _rows_of("ds_distill", "dz", dz)[2]
+        else:
+            dz_pitch = _rows_of("ds_distill", "dz", dz)[2]
     elif dz is not None:
         _refuse("ds_distill", "dz is given but no gradient is wanted")
     if rows:
-        _answer("ds_distill", ctypes.byref(ds_logits(rows, vocab, pairs.shape[1], _DTYPES[z.dtype], temperature, 0)),
-                [z.data_ptr(), pitch, pairs.data_ptr(), *given, loss.data_ptr() if want_loss else None,
-                 dz.data_ptr() if want_gradient else None, dz_pitch], stream)
+        _answer("ds_distill", ds_logits(rows, vocab, pairs.shape[1], _DTYPES[z.dtype], temperature, 0), z, stream,
+                z.data_ptr(), pitch, pairs.data_ptr(), *given, loss.data_ptr() if want_loss else None,
+                dz.data_ptr() if want_gradient else None, dz_pitch)
     return loss, dz
 
 
