@@ -6,6 +6,9 @@
 // instruction: codes of two rows sit in the halves of a register after one byte permutation, two more instructions make operands of two (dsq_codes.h).
 // The waves of a workgroup and the workgroups of a column take different rows; the waves join in LDS, the workgroups through fp32 partial sums in
 // work_dev and a second launch.
+//   64 tokens of 32768 x 4096, bf16: 46.1 us, 1.5 TB/s of codes, where reading them takes 13.  Of a compute unit's 5200 clocks for 256 rows the matrix units
+// work 2300 and the vector units 2700, more than half of it on dy * scale, of which every 128 columns need their own: two waves fit on a SIMD and hide a part
+// of one behind the other.  Loads of a step that were all asked for at its start held up the eight waves for some 2000 clocks; next to the products they do not.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
 
@@ -14,7 +17,9 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = kWaves * 64, kChunk = 128, kStep = 32;   // of a workgroup; columns and rows a wave takes at a time
 constexpr uint32_t kBlockRows = kWaves * kStep;                   // rows the workgroup takes at a time
-constexpr uint64_t kTokens = 64;                                  // of a launch
+// Tokens of a launch: what a wave has registers for.
+template <typename T>
+constexpr uint64_t kTokens(bool narrow) { return sizeof(T) == 4 || narrow ? 32 : 64; }
 constexpr uint64_t kGroupsOfLaunch = 1u << 22;                    // a launch dimension holds fewer than 2^32 work-items
 
 struct GradientShape : ProductArgs {
@@ -72,12 +77,9 @@ __global__ void __launch_bounds__(kThreads, 2) product_gradient_kernel(GradientS
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane & 15, j = lane >> 4;
     const uint32_t tokens = (uint32_t)a.tokens;
     // Workgroups go round the eight XCDs: those of the same rows, which share cache lines, onto one of them.
-    uint64_t chunk = blockIdx.x, part = blockIdx.y;
-    if (a.parts % 8 == 0) {
-        const uint64_t id = (uint64_t)blockIdx.y * gridDim.x + blockIdx.x, q = id / 8;
-        part = id % 8 + q / gridDim.x * 8;
-        chunk = q % gridDim.x;
-    }
+    const uint64_t id = (uint64_t)blockIdx.y * gridDim.x + blockIdx.x, all = (uint64_t)gridDim.x * gridDim.y;
+    const uint64_t xcd = id % 8, mine = xcd * (all / 8) + (xcd < all % 8 ? xcd : all % 8) + id / 8;
+    const uint64_t chunk = mine % gridDim.x, part = mine / gridDim.x;
     const uint64_t col0 = (a.chunk0 + chunk) * kChunk;
     const uint64_t r_begin = part * a.part_rows, r_end = r_begin + a.part_rows < a.rows ? r_begin + a.part_rows : a.rows;
     const uint32_t blocks = (uint32_t)((r_end - r_begin + kBlockRows - 1) / kBlockRows);
@@ -97,16 +99,16 @@ __global__ void __launch_bounds__(kThreads, 2) product_gradient_kernel(GradientS
         scale_at[h] = 8 * j * (uint32_t)a.row_bytes;
         word_at[h] = scale_at[h] + at[h];
     }
-    auto fetch = [&](R& v, uint32_t b) {                          // all 256 rows are there
+    auto fetch_row = [&](R& v, uint32_t b, int e) {               // row e of the lane's eight; all 256 rows are there
         const uint64_t r0 = r_begin + (uint64_t)b * kBlockRows + wave * kStep;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-            for (int h = 0; h < H; ++h) {
-                const uint8_t* p = block[h] + (r0 + e) * a.row_bytes;
-                v.scale[h][e] = *reinterpret_cast<const float*>(p + scale_at[h]);
-                v.w[h][e] = *reinterpret_cast<const uint32_t*>(p + word_at[h]);
-            }
+        for (int h = 0; h < H; ++h) {
+            uint32_t of_scale = scale_at[h], of_word = word_at[h];
+            asm volatile("" : "+v"(of_scale), "+v"(of_word));     // 32 bits here, too: the loads add them to a scalar base
+            const uint8_t* p = block[h] + (r0 + e) * a.row_bytes;
+            v.scale[h][e] = *reinterpret_cast<const float*>(p + of_scale);
+            v.w[h][e] = *reinterpret_cast<const uint32_t*>(p + of_word);
+        }
     };
     auto fetch_tail = [&](R& v, uint32_t b) {                     // rows behind the last repeat it (dy is 0 there)
         const uint64_t r0 = r_begin + (uint64_t)b * kBlockRows + wave * kStep + 8 * j;
@@ -127,11 +129,7 @@ __global__ void __launch_bounds__(kThreads, 2) product_gradient_kernel(GradientS
         const uint32_t piece = q * kThreads + threadIdx.x, tok = piece / PER < tokens ? piece / PER : tokens - 1;
         dy_at[q] = static_cast<const T*>(a.in) + tok * a.in_ld + piece % PER * E;
     }
-    auto fetch_dy = [&](Piece (&v)[PIECES], uint32_t b) {
-        const uint64_t r0 = r_begin + (uint64_t)b * kBlockRows;
-#pragma unroll
-        for (uint32_t q = 0; q < PIECES; ++q) v[q] = *reinterpret_cast<const Piece*>(dy_at[q] + r0);
-    };
+    auto fetch_dy = [&](Piece& v, uint32_t q, uint32_t b) { v = *reinterpret_cast<const Piece*>(dy_at[q] + (r_begin + (uint64_t)b * kBlockRows)); };
     auto fetch_dy_tail = [&](Piece (&v)[PIECES], uint32_t b) {
         const uint64_t r0 = r_begin + (uint64_t)b * kBlockRows;
 #pragma unroll
@@ -158,33 +156,14 @@ __global__ void __launch_bounds__(kThreads, 2) product_gradient_kernel(GradientS
         for (int h = 0; h < H; ++h) off[t][h] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const CodeMasks masks = code_masks<__bf16>();
-    auto use = [&](const R& v, uint32_t buffer, bool ragged, uint64_t r0) {
+    auto use = [&](const R& v, uint32_t buffer, bool ragged, uint64_t r0, auto meanwhile) {   // meanwhile(c), c = 0 .. 7: next to a column's products
 #pragma unroll
         for (int h = 0; h < H; ++h) {
             constexpr int COLS = NARROW ? 4 : 8;
-            Eight<__bf16> right[COLS];
-#pragma unroll
-            for (int g = 0; g < COLS / 4; ++g) {
-                uint32_t pair[4];                                 // four columns of rows 2 q and 2 q + 1
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t select = NARROW ? (n % 2 ? 0x07060302u : 0x05040100u) : g ? 0x07060302u : 0x05040100u;
-                    pair[q] = __builtin_amdgcn_perm(v.w[h][2 * q + 1], v.w[h][2 * q], select);
-                }
-                auto column = [&](auto which) {
-                    constexpr int N = decltype(which)::value;
-                    const u32x4 codes = {code_pair<__bf16, N>(pair[0], masks), code_pair<__bf16, N>(pair[1], masks), code_pair<__bf16, N>(pair[2], masks),
-                                         code_pair<__bf16, N>(pair[3], masks)};
-                    right[4 * g + N] = __builtin_bit_cast(Eight<__bf16>, codes);
-                };
-                column(std::integral_constant<int, 0>());
-                column(std::integral_constant<int, 1>());
-                column(std::integral_constant<int, 2>());
-                column(std::integral_constant<int, 3>());
-            }
             float unit[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) unit[e] = v.scale[h][e] * kPerCode;
+            Eight<__bf16> left[TT][P];
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
                 const T* from = staged + (buffer * TT * 16 + 16 * t + n) * kPitch + wave * kStep + 8 * j;
@@ -195,46 +174,76 @@ __global__ void __launch_bounds__(kThreads, 2) product_gradient_kernel(GradientS
                 if (ragged)                                       // (a scale of the last row may be infinite)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) d[e] = r0 + 8 * j + e < a.rows ? d[e] : 0.f;
-                Eight<__bf16> left[P];
-                split_operand<P>(d, left);
-                if constexpr (kCentred) {
-                    f32x4 from = {0.f, 0.f, 0.f, 0.f};
+                split_operand<P>(d, left[t]);
+            }
+            f32x4 centre[TT];                                     // what codes are too large by
 #pragma unroll
-                    for (int p = 0; p < P; ++p) from = matrix_fma(left[p], centre_operand<__bf16>(), from);
-                    from = -from;
+            for (int t = 0; t < TT; ++t) centre[t] = kCentred ? f32x4{0.f, 0.f, 0.f, 0.f} : off[t][h];
 #pragma unroll
-                    for (int c = 0; c < COLS; ++c) {
-                        f32x4 part = from;
+            for (int p = 0; p < P; ++p)
 #pragma unroll
-                        for (int p = 0; p < P; ++p) part = matrix_fma(left[p], right[c], part);
-                        sum[t][COLS * h + c] += part;
-                    }
-                } else {
+                for (int t = 0; t < TT; ++t) centre[t] = matrix_fma(left[t][p], centre_operand<__bf16>(), centre[t]);
+            if (!kCentred)
 #pragma unroll
-                    for (int p = 0; p < P; ++p) {
-                        off[t][h] = matrix_fma(left[p], centre_operand<__bf16>(), off[t][h]);
+                for (int t = 0; t < TT; ++t) off[t][h] = centre[t];
 #pragma unroll
-                        for (int c = 0; c < COLS; ++c) sum[t][COLS * h + c] = matrix_fma(left[p], right[c], sum[t][COLS * h + c]);
-                    }
+            for (int g = 0; g < COLS / 4; ++g) {
+                uint32_t pair[4];                                 // four columns of rows 2 q and 2 q + 1
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t select = NARROW ? (n % 2 ? 0x07060302u : 0x05040100u) : g ? 0x07060302u : 0x05040100u;
+                    pair[q] = __builtin_amdgcn_perm(v.w[h][2 * q + 1], v.w[h][2 * q], select);
                 }
+                auto column = [&](auto which) {
+                    constexpr int N = decltype(which)::value;
+                    const int c = COLS * h + 4 * g + N;
+                    const u32x4 codes = {code_pair<__bf16, N>(pair[0], masks), code_pair<__bf16, N>(pair[1], masks), code_pair<__bf16, N>(pair[2], masks),
+                                         code_pair<__bf16, N>(pair[3], masks)};
+                    const Eight<__bf16> right = __builtin_bit_cast(Eight<__bf16>, codes);
+                    meanwhile(c);
+                    f32x4 part[TT];
+#pragma unroll
+                    for (int t = 0; t < TT; ++t) part[t] = kCentred ? -centre[t] : sum[t][c];
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int t = 0; t < TT; ++t) part[t] = matrix_fma(left[t][p], right, part[t]);
+#pragma unroll
+                    for (int t = 0; t < TT; ++t) sum[t][c] = kCentred ? sum[t][c] + part[t] : part[t];
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                column(std::integral_constant<int, 0>());
+                column(std::integral_constant<int, 1>());
+                column(std::integral_constant<int, 2>());
+                column(std::integral_constant<int, 3>());
             }
         }
     };
-    // Whole blocks of rows, each read while the one before is multiplied (the last once more: no branch, so that loads can be counted), ...
+    // Whole blocks of rows.  While one is multiplied the next one's codes are read, two rows next to each of the first columns' products, and the dy of the one
+    // after that, next to the others'; dy of the next one goes into LDS.  (Behind the end the last one is read again: no branch, so that loads can be counted.)
     const uint32_t whole = (uint32_t)((r_end - r_begin) / kBlockRows);
     Piece dy[PIECES];
     if (whole) {
         R rows[2];
-        fetch_dy(dy, 0);
-        fetch(rows[0], 0);
+        auto within = [&](uint32_t b) { return b < whole ? b : whole - 1; };
+#pragma unroll
+        for (uint32_t q = 0; q < PIECES; ++q) fetch_dy(dy[q], q, 0);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) fetch_row(rows[0], 0, e);
         stage_dy(dy, 0);
+#pragma unroll
+        for (uint32_t q = 0; q < PIECES; ++q) fetch_dy(dy[q], q, within(1));
         __syncthreads();
         auto step = [&](const R& now, R& next, uint32_t b) {
-            const uint32_t ahead = b + 1 < whole ? b + 1 : b;
-            fetch_dy(dy, ahead);
-            fetch(next, ahead);
-            use(now, b & 1, false, 0);
-            stage_dy(dy, (b + 1) & 1);
+            use(now, b & 1, false, 0, [&](int c) {
+                if (c == 0) stage_dy(dy, (b + 1) & 1);
+                if (c < 4) {
+                    fetch_row(next, within(b + 1), 2 * c);
+                    fetch_row(next, within(b + 1), 2 * c + 1);
+#pragma unroll
+                    for (uint32_t q = c; q < PIECES; q += 4) fetch_dy(dy[q], q, within(b + 2));
+                }
+            });
             __syncthreads();
         };
         for (uint32_t b = 0; b < whole; b += 2) {
@@ -250,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, 2) product_gradient_kernel(GradientS
         stage_dy(dy, 0);
         __syncthreads();
         const uint64_t r0 = r_begin + (uint64_t)whole * kBlockRows + wave * kStep;
-        use(rows, 0, true, r0);
+        use(rows, 0, true, r0, [](int) {});
         __syncthreads();
     }
     if constexpr (!kCentred)
@@ -308,10 +317,15 @@ __global__ void __launch_bounds__(256) product_gradient_join_kernel(GradientShap
     gradient_store<T>(a, c, t, v);
 }
 
-void gradient_plan(uint64_t rows, uint64_t cols, uint32_t& parts, uint64_t& part_rows) {
+// Workgroups split the rows until all compute units have one, and not one more, which would take as long again; where two fit into a unit's registers, two.
+// 32768 x 4096, bf16, blocks of 256, us, for 256 : 512 workgroups: 64 tokens 46.1 : 54.4 (33 columns of them, 231 : 495, 49.8 : 55.5; 264 took 82), 32 tokens
+// 28.7 : 32.6; 16 tokens 22.0 : 20.2; 16 tokens of 8192 x 5000, fp32, 14.7 : 14.6 (320: 17.9).
+void gradient_plan(uint64_t rows, uint64_t cols, uint64_t tokens, bool narrow, uint32_t& parts, uint64_t& part_rows) {
     const uint64_t chunks = (cols + kChunk - 1) / kChunk, blocks = (rows + kBlockRows - 1) / kBlockRows;
-    uint64_t p = 1;
-    while (chunks * p < 256 && blocks >= 2 * p && p < 64) p *= 2;
+    uint64_t p = (tokens <= 16 && !narrow ? 512 : 256) / chunks;
+    if (p > blocks) p = blocks;
+    if (p > 64) p = 64;
+    if (!p) p = 1;
     const uint64_t each = (blocks + p - 1) / p;
     part_rows = each * kBlockRows;
     parts = (uint32_t)((blocks + each - 1) / each);
@@ -332,21 +346,22 @@ void launch_gradient_kernel(const GradientShape& a, hipStream_t stream) {
 
 template <typename T>
 void launch_gradient_of(const ProductArgs& args, hipStream_t stream) {
-    for (uint64_t t0 = 0; t0 < args.tokens; t0 += kTokens) {
+    const bool narrow = args.block == 64;
+    const uint64_t most = kTokens<T>(narrow);
+    for (uint64_t t0 = 0; t0 < args.tokens; t0 += most) {
         GradientShape a{};
         static_cast<ProductArgs&>(a) = args;
-        a.tokens = args.tokens - t0 < kTokens ? args.tokens - t0 : kTokens;
+        a.tokens = args.tokens - t0 < most ? args.tokens - t0 : most;
         a.in = static_cast<const T*>(args.in) + t0 * args.in_ld;
         a.out = static_cast<T*>(args.out) + t0 * args.out_ld;
         a.chunks = (a.cols + kChunk - 1) / kChunk;
-        gradient_plan(a.rows, a.cols, a.parts, a.part_rows);
+        gradient_plan(a.rows, a.cols, a.tokens, narrow, a.parts, a.part_rows);
         a.partial = a.parts > 1 ? static_cast<float*>(a.work) : nullptr;
-        const bool narrow = a.block == 64;
         if (a.tokens <= 16) narrow ? launch_gradient_kernel<T, 1, true>(a, stream) : launch_gradient_kernel<T, 1, false>(a, stream);
         else if (a.tokens <= 32) narrow ? launch_gradient_kernel<T, 2, true>(a, stream) : launch_gradient_kernel<T, 2, false>(a, stream);
-        else narrow ? launch_gradient_kernel<T, 4, true>(a, stream) : launch_gradient_kernel<T, 4, false>(a, stream);
+        else if constexpr (kTokens<T>(false) > 32) launch_gradient_kernel<T, 4, false>(a, stream);
         if (!a.partial) continue;
-        a.chunk0 = 0;                                             // (parts are only for matrices of fewer than 256 chunks)
+        a.chunk0 = 0;                                             // (parts are only for matrices of at most 256 chunks)
         hipLaunchKernelGGL(product_gradient_join_kernel<T>, dim3((unsigned)((a.cols + 255) / 256), (unsigned)a.tokens), dim3(256), 0, stream, a);
     }
 }
@@ -354,10 +369,17 @@ void launch_gradient_of(const ProductArgs& args, hipStream_t stream) {
 }  // namespace
 
 uint64_t product_gradient_work_bytes(const ds_matrix& m) {
-    uint32_t parts;
-    uint64_t part_rows;
-    gradient_plan(m.rows, m.cols, parts, part_rows);
-    return parts > 1 ? (uint64_t)parts * (m.tokens < kTokens ? m.tokens : kTokens) * m.cols * sizeof(float) : 0;
+    const bool narrow = m.block == 64;
+    uint64_t most = 0, bytes = 0;
+    by_dtype(m.dtype, [&](auto kind) { most = kTokens<decltype(kind)>(narrow); });
+    for (uint64_t tokens : {m.tokens < most ? m.tokens : most, m.tokens % most}) {             // of the launches: whole ones and the last
+        uint32_t parts;
+        uint64_t part_rows;
+        gradient_plan(m.rows, m.cols, tokens, narrow, parts, part_rows);
+        const uint64_t here = parts > 1 ? parts * tokens * m.cols * sizeof(float) : 0;
+        if (here > bytes) bytes = here;
+    }
+    return bytes;
 }
 
 hipError_t launch_product_gradient(const ProductArgs& a, hipStream_t stream) {
