@@ -12,7 +12,7 @@
 // product_tiles_kernel, whose workgroups make x's bytes themselves.  More tokens: product_kernel; a launch before makes x's bytes once, in work_dev,
 // and codes go straight into registers, which leaves LDS to x.  Measured, us, product_tiles_kernel against product_kernel: 2 x 65536 x 4096, bf16,
 // 42.0 : 45.5; 16 x 4096 x 16384, fp16, 19.0 : 24.8; 8 x 2048 x 2048 7.1 : 9.0; 4 x 16384 x 4096, fp32, 16.1 : 16.4; from there on 61 x 16001 x 4099,
-// bf16, 55.7 : 56.3; 64 x 65536 x 1024 31.7 : 28.0, and in blocks of 64 51.4 : 39.8; 32 x 16384 x 4096, fp32, 30.3 : 31.7.
+// bf16, 55.7 : 46.3; 64 x 65536 x 1024 31.7 : 28.0, and in blocks of 64 51.4 : 39.8; 32 x 16384 x 4096, fp32, 30.3 : 31.7.
 //   Where there are too few rows for the GPU, workgroups split the columns, too, and one more launch adds their sums.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
@@ -753,6 +753,13 @@ uint32_t record_bytes(uint64_t tokens, bool narrow) {
     return bytes;
 }
 
+// How many workgroups split the columns, where there are so many side by side and `most` could: until there are `want`, 32 at most.
+uint32_t split(uint64_t want, uint64_t groups, uint64_t most) {
+    uint64_t parts = want / groups;
+    if (parts > most) parts = most;
+    return parts < 1 ? 1 : parts > 32 ? 32 : (uint32_t)parts;
+}
+
 template <typename T>
 ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens, bool narrow) {
     ProductPlan p{};
@@ -760,12 +767,12 @@ ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens, bool nar
     const uint64_t chunks = (cols + kChunk - 1) / kChunk, height = 16 * kRowTiles, row_tiles = (rows + height - 1) / height;
     const uint32_t record = record_bytes<T>(tokens, narrow);
     if (tiles <= 2) {
-        // A workgroup for every compute unit, as long as there is a stage for it: 8 x 2048 x 2048, bf16, 1 part 9.6 us, 2: 9.2, 4: 7.6, 8 (128 workgroups,
-        // a stage each): 7.1.  Two of them, as long as there are four stages for each: 4 x 16384 x 4096, fp32, 2 parts (256 workgroups) 17.6 us,
-        // 4: 16.3, 8: 17.0; 16 x 4096 x 4096, blocks of 64, 8 parts (256, two stages each) 10.7, 16: 13.5.
+        // Two workgroups for every compute unit where each has four stages, otherwise one where it has any: 4 x 16384 x 4096, fp32, 2 parts (256 workgroups)
+        // 17.6 us, 4: 16.2, 6: 16.8; 16 x 20000 x 4096, bf16, blocks of 64, 1 part (157) 26.0, 3: 24.0; 16 x 4096 x 4096 4 parts (128) 14.1, 8 (of two stages)
+        // 10.6, 16: 12.6; 16 x 5000 x 4096 6 parts (240) 13.2, 12: 14.5; 8 x 2048 x 2048 1 part 9.6, 8 (128 workgroups, a stage each): 7.1.
         const uint64_t stages = (chunks + kStageChunks - 1) / kStageChunks, groups = (rows + 16 * kWaves - 1) / (16 * kWaves);
-        p.parts = 1;
-        while (p.parts < 32 && ((groups * p.parts < 256 && stages >= 2 * p.parts) || (groups * p.parts < 512 && stages >= 8 * p.parts))) p.parts *= 2;
+        p.parts = split(512, groups, stages);
+        if (stages < 4 * p.parts) p.parts = split(256, groups, stages);
         p.part_chunks = (uint32_t)((stages + p.parts - 1) / p.parts);
         p.parts = (uint32_t)((stages + p.part_chunks - 1) / p.part_chunks);
         return p;
@@ -774,8 +781,10 @@ ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens, bool nar
     p.row_waves = 1;
     while (p.row_waves < kWaves && (record > 64 * height * p.row_waves || row_tiles / (2 * p.row_waves) >= 512)) p.row_waves *= 2;
     const uint64_t groups = (row_tiles + p.row_waves - 1) / p.row_waves, col_waves = kWaves / p.row_waves;
-    p.parts = 1;
-    while (groups * p.parts < 256 && chunks >= 8 * p.parts * col_waves && p.parts < 32) p.parts *= 2;
+    // Workgroups split the columns until all compute units have one, and not one more, which would take as long again, with four chunks for a wave: 61 x 16001 x
+    // 4099, bf16, 4 parts (252 workgroups) 46.3 us, 7 (441): 56.2; 64 x 65536 x 1024 1 part (256) 29.9, 2: 47.7; 20 x 1000 x 30000, fp16, 7 parts (224) 19.6,
+    // 3 (96): 23.0.
+    p.parts = split(256, groups, chunks / (4 * col_waves));
     p.part_chunks = (uint32_t)((chunks + p.parts - 1) / p.parts);
     p.parts = (uint32_t)((chunks + p.part_chunks - 1) / p.part_chunks);
     const uint32_t fit = kPanel / record;
