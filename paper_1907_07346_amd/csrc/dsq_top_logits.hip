@@ -4,9 +4,13 @@
 // below the bar cost one comparison.  When the list grows long, its k best are found, which raises the bar; when a stretch has more logits above the bar
 // than the list has room for, the stretch is gone through again, a logit of each thread at a time.  Ranks are unique (the index breaks ties), so neither the
 // bar's history nor the order in which threads append shows in the result.  The first bar comes from the first stretch: the m-th best of the largest
-// of each wave's 16-byte pieces, m = ceil(k / 4): four times m >= k logits reach the lowest of the four.
-//   Few rows are split over workgroups, whose lists and sums go through work_dev to a second launch.
-// Bound by reading the logits once where there are many rows.
+// of each wave's 16-byte pieces, m = ceil(k / 4): four times m >= k logits reach the lowest of the four, or it is minus infinity, which stands for what
+// is behind the end, and all pass.
+//   Few rows are split over workgroups, whose lists and sums go through work_dev to a second launch, which has room for all of a row's lists at once
+// (1 x 1000000, k = 100, fp32: 33.8 us; 72 where lists came one after the other).  Those two launches are mostly waiting: 1 x 131072, k = 64, bf16, 7.2 + 9.3 us,
+// where an empty launch takes 2; what the first finds is some 1500 candidates, and the second's time is three reads of memory, one behind the other, one
+// histogram and the ranks in one of its bins.
+//   Many rows are bound by reading the logits once: 2048 x 65536, fp32, k = 128, 124 us, 4.3 TB/s.
 #include "dsq_answers.h"
 #include "dsq_logits.h"
 
@@ -15,6 +19,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr uint32_t kRoom = 1024, kLong = 512;                     // candidates the list has room for, and from which on it is shortened
+constexpr uint32_t kJoinRoom = 4096;                              // candidates of a row's parts
 constexpr int kPieces = 4;                                        // 16-byte pieces of a thread in a stretch
 constexpr uint64_t kRowsOfLaunch = 1u << 22;                      // a launch dimension holds fewer than 2^32 work-items
 
@@ -22,7 +27,8 @@ struct TopShape : LogitsArgs {
     uint32_t parts;                                               // workgroups of a row
     uint64_t part_logits;                                         // a multiple of a stretch
     uint64_t row0;
-    uint64_t* lists;                                              // [row][part][kLong] ranks
+    uint32_t room;                                                // of a part's list, at least k
+    uint64_t* lists;                                              // [row][part][room] ranks
     struct Part {
         float max, sum;
         uint32_t held, unused;                                    // ranks in the list
@@ -38,13 +44,27 @@ struct TopLds {
     uint32_t totals[kWaves];
     float sums[2 * kWaves];
     uint32_t count;                                               // of the list
-    uint32_t bin, above, inside;                                  // kth_rank: the k-th's bin, ranks in higher ones and in it
+    uint32_t bin, above, inside, gathered;                        // kth_rank: the k-th's bin, ranks in higher ones and in it ...
+    uint64_t few[kThreads], kth;                                  // ... and those in it, where they are few
 };
 
+// The k-th largest of n <= kThreads ranks: a thread for each counts those above its own.
+template <uint32_t ROOM>
+__device__ __forceinline__ uint64_t kth_of_few(TopLds<ROOM>& s, const uint64_t* few, uint32_t n, uint32_t k) {
+    const uint64_t rank = threadIdx.x < n ? few[threadIdx.x] : 0;
+    uint32_t higher = 0;
+#pragma unroll 8
+    for (uint32_t i = 0; i < n; ++i) higher += few[i] > rank ? 1u : 0u;
+    if (threadIdx.x < n && higher == k - 1) s.kth = rank;
+    __syncthreads();
+    return s.kth;
+}
+
 // A number that exactly k of the list's n > k ranks reach.  Up to eight bits at a time, of those in which ranks differ: a histogram of the ranks that agree
-// with what is known of the k-th, and the bin in which the k-th lies.
+// with what is known of the k-th, and the bin in which the k-th lies, until there is a thread for each rank in the bin.
 template <uint32_t ROOM>
 __device__ uint64_t kth_rank(TopLds<ROOM>& s, uint32_t n, uint32_t k) {
+    if (n <= kThreads) return kth_of_few(s, s.list, n, k);        // (8 x 32003, k = 16, fp16: 17.8 us without it, 15.4 with it)
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
     uint64_t mine[ROOM / kThreads], some = 0, all = ~0ull;
 #pragma unroll
@@ -101,7 +121,16 @@ __device__ uint64_t kth_rank(TopLds<ROOM>& s, uint32_t n, uint32_t k) {
         k -= s.above;
         const bool whole = s.inside == k;                         // all of the bin: nothing below matters, and known has no open bit set
         if (whole || open == 0) return known;
+        const uint32_t inside = s.inside;
+        if (threadIdx.x == 0) s.gathered = 0;
         __syncthreads();                                          // (s.bin is written again)
+        if (inside > kThreads) continue;
+        const uint64_t same = ~0ull << next;
+#pragma unroll
+        for (uint32_t q = 0; q < ROOM / kThreads; ++q)
+            if (mine[q] && ((mine[q] ^ known) & same) == 0) s.few[atomicAdd(&s.gathered, 1u)] = mine[q];
+        __syncthreads();
+        return kth_of_few(s, s.few, inside, k);
     }
 }
 
@@ -233,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, 4) top_logits_kernel(TopShape a) {
     for (uint64_t at = begin; at < end; at += kStretch) {
         Piece raw[kPieces];
         fetch(raw, at);
-        go_through(raw, at, at == begin && at + kStretch <= end);
+        go_through(raw, at, at == begin);
         __syncthreads();
         const uint32_t count = s.count;
         __syncthreads();
@@ -271,67 +300,45 @@ __global__ void __launch_bounds__(kThreads, 4) top_logits_kernel(TopShape a) {
         if (a.lse && threadIdx.x == 0) a.lse[row] = row_lse(spread, scale, a.temperature);
         return;
     }
-    if (held > kLong) {
+    if (held > a.room) {
         (void)keep_best(s, held, k);
         held = k;
     }
     const uint64_t part = row * a.parts + blockIdx.y;
-    for (uint32_t q = threadIdx.x; q < held; q += kThreads) a.lists[part * kLong + q] = s.list[q];
+    for (uint32_t q = threadIdx.x; q < held; q += kThreads) a.lists[part * a.room + q] = s.list[q];
     if (threadIdx.x == 0) a.found[part] = {spread.max, spread.sum, held, 0};
 }
 
-// Joins the parts of a row.
+// Joins the parts of a row.  All their lists have room in LDS, one behind the other; 256 / parts threads bring a list, eight loads at a time.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) top_logits_join_kernel(TopShape a) {
-    constexpr uint32_t kRoom = 4096;                              // 16 lists of k = 64 hold some 1500
-    __shared__ TopLds<kRoom> s;
+    __shared__ TopLds<kJoinRoom> s;
     const uint64_t row = a.row0 + blockIdx.x;
-    const uint32_t k = a.k;
-    const TopShape::Part* found = a.found + row * a.parts;
-    if (threadIdx.x == 0) s.count = 0;
-    __syncthreads();
-    uint32_t held = 0;
-    uint64_t bar = 0;
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    uint32_t in_all = 0, mine_at = 0;                             // (parts <= 64)
-    Spread spread = kNoSpread;
-    {
-        TopShape::Part part{-kInf, 0.f, 0, 0};
-        if (lane < a.parts) part = found[lane];
-        if (wave == 0) spread = {part.max, part.sum};
-        const uint32_t n = part.held;
-        uint32_t upto = n;
+    const uint32_t k = a.k, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    TopShape::Part part{-kInf, 0.f, 0, 0};                        // of lane's part (parts <= 64)
+    if (lane < a.parts) part = a.found[row * a.parts + lane];
+    Spread spread = wave == 0 ? Spread{part.max, part.sum} : kNoSpread;
+    uint32_t upto = part.held;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t other = (uint32_t)__shfl_up((int)upto, o);
-            if (lane >= (uint32_t)o) upto += other;
-        }
-        in_all = (uint32_t)__shfl((int)upto, 63);
-        mine_at = upto - n;
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t other = (uint32_t)__shfl_up((int)upto, o);
+        if (lane >= (uint32_t)o) upto += other;
     }
-    if (in_all <= kRoom) {                                        // room for all of them, one list behind the other
-        for (uint32_t p = wave; p < a.parts; p += kWaves) {
-            const uint64_t* list = a.lists + (row * a.parts + p) * kLong;
-            const uint32_t n = found[p].held, to = (uint32_t)__shfl((int)mine_at, p);
-            for (uint32_t q = lane; q < n; q += 64) s.list[to + q] = list[q];
-        }
-        held = in_all;
-        __syncthreads();
-    } else {
-        for (uint32_t p = 0; p < a.parts; ++p) {
-            const uint64_t* list = a.lists + (row * a.parts + p) * kLong;
-            const uint32_t n = found[p].held;
-            if (held + n > kRoom) {                               // (n <= 512, k <= 256)
-                bar = keep_best(s, held, k);
-                held = k;
-            }
-            for (uint32_t q = threadIdx.x; q < n; q += kThreads)
-                if (list[q] > bar) s.list[atomicAdd(&s.count, 1u)] = list[q];
-            __syncthreads();
-            held = s.count;
-            __syncthreads();
+    const uint32_t held = (uint32_t)__shfl((int)upto, 63);
+    const uint32_t of_list = kThreads >> (32 - __builtin_clz(a.parts - 1)), p = threadIdx.x / of_list, from = threadIdx.x % of_list;   // (parts > 1)
+    const uint32_t n = (uint32_t)__shfl((int)part.held, (int)(p & 63)), to = (uint32_t)__shfl((int)upto, (int)(p & 63)) - n;
+    if (p < a.parts) {
+        const uint64_t* list = a.lists + (row * a.parts + p) * a.room;
+        for (uint32_t q = from; q < n; q += 8 * of_list) {
+            uint64_t rank[8];
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) rank[i] = list[q + i * of_list < n ? q + i * of_list : q];
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i)
+                if (q + i * of_list < n) s.list[to + q + i * of_list] = rank[i];
         }
     }
+    __syncthreads();
     const T* z = static_cast<const T*>(a.z) + row * a.z_ld;
     write_pairs(s, held, k, z, a.pairs + row * k);
     if (!a.lse) return;
@@ -340,28 +347,29 @@ __global__ void __launch_bounds__(kThreads) top_logits_join_kernel(TopShape a) {
     if (threadIdx.x == 0) a.lse[row] = row_lse(spread, scale, a.temperature);
 }
 
-// Workgroups of a row: as many as fill the GPU, each with a stretch or more.
+// Workgroups of a row: as many as fill the GPU, each with a stretch or more, and not more than can send k logits each to be joined.
 template <typename T>
-void top_plan(uint64_t rows, uint64_t vocab, uint32_t& parts, uint64_t& part_logits) {
+void top_plan(uint64_t rows, uint64_t vocab, uint32_t k, uint32_t& parts, uint64_t& part_logits, uint32_t& room) {
     constexpr uint64_t stretch = kThreads * kPieces * (16 / sizeof(T));
     const uint64_t stretches = (vocab + stretch - 1) / stretch;
     uint64_t p = rows >= 512 ? 1 : 1024 / rows;
     if (p > stretches) p = stretches;
     if (p > 64) p = 64;
+    if (p > kJoinRoom / k) p = kJoinRoom / k;
     if (p < 1) p = 1;
     const uint64_t each = (stretches + p - 1) / p;
     part_logits = each * stretch;
     parts = (uint32_t)((stretches + each - 1) / each);
+    room = kJoinRoom / parts < kLong ? kJoinRoom / parts : kLong;
 }
-
 
 template <typename T>
 void launch_top_of(const LogitsArgs& args, hipStream_t stream) {
     TopShape a{};
     static_cast<LogitsArgs&>(a) = args;
-    top_plan<T>(a.rows, a.vocab, a.parts, a.part_logits);
+    top_plan<T>(a.rows, a.vocab, a.k, a.parts, a.part_logits, a.room);
     a.lists = static_cast<uint64_t*>(a.work);
-    a.found = reinterpret_cast<TopShape::Part*>(a.lists + a.rows * a.parts * kLong);
+    a.found = reinterpret_cast<TopShape::Part*>(a.lists + a.rows * a.parts * a.room);
     for (uint64_t r = 0; r < a.rows; r += kRowsOfLaunch) {
         a.row0 = r;
         const unsigned here = (unsigned)(a.rows - r < kRowsOfLaunch ? a.rows - r : kRowsOfLaunch);
@@ -373,10 +381,10 @@ void launch_top_of(const LogitsArgs& args, hipStream_t stream) {
 }  // namespace
 
 uint64_t top_logits_work_bytes(const ds_logits& l) {
-    uint32_t parts = 1;
+    uint32_t parts = 1, room = 0;
     uint64_t part_logits;
-    by_dtype(l.dtype, [&](auto kind) { top_plan<decltype(kind)>(l.rows, l.vocab, parts, part_logits); });
-    return parts > 1 ? l.rows * parts * (kLong * sizeof(uint64_t) + sizeof(TopShape::Part)) : 0;
+    by_dtype(l.dtype, [&](auto kind) { top_plan<decltype(kind)>(l.rows, l.vocab, l.k, parts, part_logits, room); });
+    return parts > 1 ? l.rows * parts * (room * sizeof(uint64_t) + sizeof(TopShape::Part)) : 0;
 }
 
 hipError_t launch_top_logits(const LogitsArgs& a, hipStream_t stream) {
