@@ -21,7 +21,6 @@ namespace dsq {
 namespace {
 
 constexpr int kWaves = 8, kThreads = kWaves * 64, kChunk = 128;   // of a workgroup; columns a wave takes at a time
-constexpr uint32_t kPanel = 64 * 1024;                            // bytes of LDS for x: two workgroups fit on a compute unit
 constexpr uint64_t kGroupsOfLaunch = 1u << 22;                    // a launch dimension holds fewer than 2^32 work-items
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
@@ -46,7 +45,6 @@ constexpr int kRowTiles = 2;                                      // of 16 rows,
 struct ProductPlan {
     uint32_t row_waves;                                           // waves side by side; the other kWaves / row_waves split the columns
     uint32_t parts, part_chunks;                                  // workgroups that split the columns, and the chunks of each
-    uint32_t stage_chunks;                                        // chunks of x that are in LDS at a time
     uint32_t wave_rows;                                           // one token: rows of a wave
 };
 
@@ -58,15 +56,13 @@ struct ProductShape : ProductArgs {
 };
 
 // One chunk of x: the digits, [matrix instruction][j][row][16 columns]; the sums the products start from, -15 times the digits' sum, [block][row]
-// (two blocks where a block is 64 columns); and per token what v counts, 2^e.  Rows: digit d of token t is row stride t + d.
+// (two blocks where a block is 64 columns); and per token what v counts, 2^e.  Rows: digit d of token t is row stride t + d; rows of no token hold anything.
 template <typename T, int TT, bool NARROW>
 struct Record {
-    static constexpr uint32_t H = NARROW ? 2 : 1, sums = H * TT * 64, units = H * TT * 32;
-    __host__ __device__ static uint32_t rows(uint32_t tokens) { return tokens * Digits<T>::stride; }
-    __host__ __device__ static uint32_t bytes(uint32_t tokens) { return 128 * rows(tokens) + sums + units; }
+    static constexpr uint32_t H = NARROW ? 2 : 1, rows = 16 * TT, sums = H * TT * 64, units = H * TT * 32, bytes = 128 * rows + sums + units;
     __device__ static i32x4* digits(uint8_t* r) { return reinterpret_cast<i32x4*>(r); }
-    __device__ static int32_t* start(uint8_t* r, uint32_t tokens) { return reinterpret_cast<int32_t*>(r + 128 * rows(tokens)); }
-    __device__ static float* unit(uint8_t* r, uint32_t tokens) { return reinterpret_cast<float*>(r + 128 * rows(tokens) + sums); }
+    __device__ static int32_t* start(uint8_t* r) { return reinterpret_cast<int32_t*>(r + 128 * rows); }
+    __device__ static float* unit(uint8_t* r) { return reinterpret_cast<float*>(r + 128 * rows + sums); }
 };
 
 // One weight after the other, as the formula has it: for a result that is not finite.
@@ -199,7 +195,7 @@ __device__ __forceinline__ uint32_t float_bits(uint32_t bits) {
 
 // Sixteen adjacent lanes, lane u with columns 8 u .. 8 u + 7 of a chunk (raw), write a token's part of the chunk's record.
 template <typename T, int TT, bool NARROW>
-__device__ void make_digits(uint32_t tokens, uint32_t tok, uint32_t u, typename EightOf<T>::Raw raw, uint8_t* record) {
+__device__ void make_digits(uint32_t tok, uint32_t u, typename EightOf<T>::Raw raw, uint8_t* record) {
     using D = Digits<T>;
     using R = Record<T, TT, NARROW>;
     constexpr int LANES = NARROW ? 8 : 16;                        // of a block
@@ -227,7 +223,7 @@ __device__ void make_digits(uint32_t tokens, uint32_t tok, uint32_t u, typename 
             bytes[0][o] = __builtin_amdgcn_perm(d, c, 0x05040100u);
         }
     }
-    const uint32_t t = NARROW ? u / 8 * 2 + u % 2 : u % 4, j = NARROW ? u % 8 / 2 : u / 4, rows = R::rows(tokens);
+    const uint32_t t = NARROW ? u / 8 * 2 + u % 2 : u % 4, j = NARROW ? u % 8 / 2 : u / 4, rows = R::rows;
 #pragma unroll
     for (int d = 0; d < D::digits; ++d) {
         const uint32_t at = (((t / 2) * 4 + j) * rows + tok * D::stride + d) * 16 + 8 * (t % 2);
@@ -235,9 +231,9 @@ __device__ void make_digits(uint32_t tokens, uint32_t tok, uint32_t u, typename 
         constexpr int kOff = (int)0xF1F1F1F1;                     // -15 each
         const int32_t sum = __builtin_amdgcn_sdot4((int)bytes[d][0], kOff, __builtin_amdgcn_sdot4((int)bytes[d][1], kOff, 0, false), false);
         const uint32_t total = over_lanes<LANES>((uint32_t)sum, [](uint32_t x, uint32_t y) { return x + y; });
-        if (u % LANES == 0) R::start(record, tokens)[u / LANES * (TT * 16) + tok * D::stride + d] = (int32_t)total;
+        if (u % LANES == 0) R::start(record)[u / LANES * (TT * 16) + tok * D::stride + d] = (int32_t)total;
     }
-    if (u % LANES == 0) R::unit(record, tokens)[u / LANES * (TT * 8) + tok] = finite ? power2_of(-power) : __builtin_nanf("");
+    if (u % LANES == 0) R::unit(record)[u / LANES * (TT * 8) + tok] = finite ? power2_of(-power) : __builtin_nanf("");
 }
 
 // x as bytes, for all workgroups: 16 threads per chunk and token.
@@ -247,17 +243,16 @@ __global__ void __launch_bounds__(256) product_digits_kernel(ProductShape a, uin
     const uint32_t tok = threadIdx.x / 16 + 16 * blockIdx.y, u = threadIdx.x % 16;
     if (tok >= a.tokens) return;
     const T* x = static_cast<const T*>(a.in) + tok * a.in_ld;
-    make_digits<T, TT, NARROW>((uint32_t)a.tokens, tok, u, load_eight(x, (uint32_t)chunk * kChunk + 8 * u, (uint32_t)a.cols), panel + chunk * Record<T, TT, NARROW>::bytes((uint32_t)a.tokens));
+    make_digits<T, TT, NARROW>(tok, u, load_eight(x, (uint32_t)chunk * kChunk + 8 * u, (uint32_t)a.cols), panel + chunk * Record<T, TT, NARROW>::bytes);
 }
 
-// The products of a chunk of codes, 16 RT rows, with the chunk's record of x.  x_at: the lane's row of x in each tile.
+// The products of a chunk of codes, 16 RT rows, with the chunk's record of x.
 template <typename T, int TT, int RT, bool NARROW>
-__device__ __forceinline__ void multiply(const Codes<NARROW> (&c)[RT], uint8_t* rec, uint32_t tokens, const uint32_t (&x_at)[TT], uint32_t j,
+__device__ __forceinline__ void multiply(const Codes<NARROW> (&c)[RT], uint8_t* rec, uint32_t n, uint32_t j,
                                          float (&sum)[RT][TT][4 / Digits<T>::stride]) {
     using D = Digits<T>;
     using R = Record<T, TT, NARROW>;
     constexpr int H = NARROW ? 2 : 1, PER = 4 / D::stride;        // blocks of a chunk; tokens of a lane and matrix instruction
-    const uint32_t x_rows = R::rows(tokens);
     const i32x4* digits = R::digits(rec);
     i32x4 codes[RT][2];
     float unit[RT][H];
@@ -270,32 +265,51 @@ __device__ __forceinline__ void multiply(const Codes<NARROW> (&c)[RT], uint8_t* 
 #pragma unroll
         for (int b = 0; b < H; ++b) unit[r][b] = c[r].scale[b] * (1.f / 15.f);
     }
+    struct Left {
+        i32x4 x[2], start[H];
+        float count[H][PER];
+    };
+    auto load = [&](Left& v, int t) {
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        const i32x4 x0 = digits[x_at[t]], x1 = digits[4 * x_rows + x_at[t]];
+        for (int h = 0; h < 2; ++h) v.x[h] = digits[(4 * h + j) * R::rows + 16 * t + n];
 #pragma unroll
         for (int b = 0; b < H; ++b) {
-            float count[PER];
 #pragma unroll
-            for (int i = 0; i < PER; ++i) count[i] = R::unit(rec, tokens)[b * (TT * 8) + (4 * t + j) * PER + i];
-            const i32x4 start = *reinterpret_cast<const i32x4*>(R::start(rec, tokens) + b * (TT * 16) + 16 * t + 4 * j);
+            for (int i = 0; i < PER; ++i) v.count[b][i] = R::unit(rec)[b * (TT * 8) + (4 * t + j) * PER + i];
+            v.start[b] = *reinterpret_cast<const i32x4*>(R::start(rec) + b * (TT * 16) + 16 * t + 4 * j);
+        }
+    };
+    Left left[2];
+    load(left[0], 0);
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        if (t + 1 < TT) load(left[(t + 1) % 2], t + 1);
+        const Left& v = left[t % 2];
+#pragma unroll
+        for (int b = 0; b < H; ++b)
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 i32x4 p;
                 if constexpr (NARROW) {
-                    p = __builtin_amdgcn_mfma_i32_16x16x64_i8(b ? x1 : x0, codes[r][b], start, 0, 0, 0);
+                    p = __builtin_amdgcn_mfma_i32_16x16x64_i8(v.x[b], codes[r][b], v.start[b], 0, 0, 0);
                 } else {
-                    p = __builtin_amdgcn_mfma_i32_16x16x64_i8(x0, codes[r][0], start, 0, 0, 0);
-                    p = __builtin_amdgcn_mfma_i32_16x16x64_i8(x1, codes[r][1], p, 0, 0, 0);
+                    p = __builtin_amdgcn_mfma_i32_16x16x64_i8(v.x[0], codes[r][0], v.start[0], 0, 0, 0);
+                    p = __builtin_amdgcn_mfma_i32_16x16x64_i8(v.x[1], codes[r][1], p, 0, 0, 0);
                 }
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
-                    float v;
-                    if constexpr (D::digits == 2) v = (float)((p[2 * i] << 8) + p[2 * i + 1]);
-                    else v = fmaf(fmaf((float)p[0], 256.f, (float)p[1]), 256.f, (float)p[2]);
-                    sum[r][t][i] = fmaf(unit[r][b] * count[i], v, sum[r][t][i]);
+                    float w;
+                    if constexpr (D::digits == 2) w = (float)((p[2 * i] << 8) + p[2 * i + 1]);
+                    else w = fmaf(fmaf((float)p[0], 256.f, (float)p[1]), 256.f, (float)p[2]);
+                    sum[r][t][i] = fmaf(unit[r][b] * v.count[b][i], w, sum[r][t][i]);
                 }
             }
+        if constexpr (TT > 2) {                                   // what is asked for, and what is left to do, beyond the next tile takes registers
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int i = 0; i < PER; ++i) asm volatile("" : "+v"(sum[r][t][i]));
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 }
@@ -303,11 +317,13 @@ __device__ __forceinline__ void multiply(const Codes<NARROW> (&c)[RT], uint8_t* 
 template <typename T, int TT, bool NARROW>
 __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
     constexpr int RT = kRowTiles;
+    constexpr uint32_t kPieces = 3;                               // 16-byte pieces of x a thread brings
     using D = Digits<T>;
     using R = Record<T, TT, NARROW>;
     constexpr int PER = 4 / D::stride;                            // tokens of a lane and matrix instruction
     extern __shared__ __align__(16) uint8_t lds[];
-    const uint32_t tokens = (uint32_t)a.tokens, x_rows = R::rows(tokens), record = R::bytes(tokens);
+    const uint32_t tokens = (uint32_t)a.tokens;
+    constexpr uint32_t record = R::bytes;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane & 15, j = lane >> 4;
     const uint32_t row_waves = a.plan.row_waves, col_waves = kWaves / row_waves;
     const uint32_t rw = wave % row_waves, cw = wave / row_waves;
@@ -322,9 +338,6 @@ __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
         const uint64_t at = first + 16 * r + n;
         row[r] = a.msg + (at < a.rows ? at : a.rows - 1) * a.row_bytes;
     }
-    uint32_t x_at[TT];                                            // the lane's row of x in each tile; rows that are not there repeat the last
-#pragma unroll
-    for (int t = 0; t < TT; ++t) x_at[t] = j * x_rows + (16 * t + n < x_rows ? 16 * t + n : x_rows - 1);
     float sum[RT][TT][PER];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -333,44 +346,61 @@ __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) sum[r][t][i] = 0.f;
 
-    auto use = [&](const Codes<NARROW> (&c)[RT], uint32_t chunk) { multiply<T, TT, RT, NARROW>(c, lds + chunk * record, tokens, x_at, j, sum); };
-    // x goes through LDS in stages; codes of the next chunks are under way while these are multiplied
-    constexpr int AHEAD = 2;
-    Codes<NARROW> ring[AHEAD][RT];
-    for (uint32_t from = 0; from < chunks; from += a.plan.stage_chunks) {
-        const uint32_t count = chunks - from < a.plan.stage_chunks ? chunks - from : a.plan.stage_chunks;
-        const uint64_t col0 = (c0 + from) * kChunk;
-        const uint32_t whole = (uint32_t)(a.cols / kChunk - (c0 + from) < count ? a.cols / kChunk - (c0 + from) : count);   // chunks without a ragged end
-        const uint32_t mine = cw < whole ? (whole - cw + col_waves - 1) / col_waves : 0;   // of this wave
-        auto fetch = [&](Codes<NARROW> (&c)[RT], uint32_t q) {    // the wave's q-th chunk, or again its last: no branch, so that loads can be counted
-            const uint32_t chunk = cw + (q < mine ? q : mine - 1) * col_waves;
+    // A stage is a chunk for every wave beside another.  x goes through LDS, a stage ahead by way of registers, and codes are on their way two stages ahead.
+    // (Behind the end the last ones are read again: no branch, so that loads can be counted.)
+    const uint32_t record4 = record / 16, stage4 = col_waves * record4, half = col_waves * record;
+    const uint32_t whole = (uint32_t)(a.cols / kChunk > c0 ? a.cols / kChunk - c0 < chunks ? a.cols / kChunk - c0 : chunks : 0);      // chunks without a ragged end
+    const uint32_t stages = whole / col_waves, all4 = chunks * record4;   // in which every wave has a whole chunk; pieces of x in all
+    const u32x4* x_from = reinterpret_cast<const u32x4*>(a.panel + c0 * record);
+    auto bring = [&](u32x4 (&v)[kPieces], uint32_t s) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r) load_codes<NARROW>(c[r], row[r], block_log2, col0 + (uint64_t)chunk * kChunk, j);
+        for (uint32_t q = 0; q < kPieces; ++q) {
+            const uint32_t at = s * stage4 + q * kThreads + threadIdx.x;
+            v[q] = x_from[at < all4 ? at : all4 - 1];
+        }
+    };
+    auto put = [&](const u32x4 (&v)[kPieces], uint32_t s) {
+#pragma unroll
+        for (uint32_t q = 0; q < kPieces; ++q)
+            if (q * kThreads + threadIdx.x < stage4) reinterpret_cast<u32x4*>(lds + (s & 1) * half)[q * kThreads + threadIdx.x] = v[q];
+    };
+    auto use = [&](const Codes<NARROW> (&c)[RT], uint32_t s) { multiply<T, TT, RT, NARROW>(c, lds + (s & 1) * half + cw * record, n, j, sum); };
+    u32x4 x[kPieces];
+    bring(x, 0);
+    if (stages) {
+        Codes<NARROW> ring[2][RT];
+        auto fetch = [&](Codes<NARROW> (&c)[RT], uint32_t s) {
+            const uint64_t col = (c0 + (s < stages ? s : stages - 1) * col_waves + cw) * kChunk;
+#pragma unroll
+            for (int r = 0; r < RT; ++r) load_codes<NARROW>(c[r], row[r], block_log2, col, j);
         };
-        if (mine)
-#pragma unroll
-            for (int s = 0; s < AHEAD; ++s) fetch(ring[s], s);
-        if (from) __syncthreads();
-        const u32x4* src = reinterpret_cast<const u32x4*>(a.panel + (c0 + from) * record);
-        for (uint32_t q = threadIdx.x; q < count * record / 16; q += kThreads) reinterpret_cast<u32x4*>(lds)[q] = src[q];
+        fetch(ring[0], 0);
+        fetch(ring[1], 1);
+        put(x, 0);
         __syncthreads();
-        for (uint32_t q = 0; q < mine; q += AHEAD) {
+        for (uint32_t s = 0; s < stages; s += 2) {
 #pragma unroll
-            for (int s = 0; s < AHEAD; ++s) {
-                if (q + s >= mine) break;
-                Codes<NARROW> now[RT];
-#pragma unroll
-                for (int r = 0; r < RT; ++r) now[r] = ring[s][r];
-                fetch(ring[s], q + s + AHEAD);
-                use(now, cw + (q + s) * col_waves);
+            for (uint32_t o = 0; o < 2; ++o) {
+                if (s + o >= stages) break;
+                bring(x, s + o + 1);
+                use(ring[o], s + o);
+                fetch(ring[o], s + o + 2);
+                put(x, s + o + 1);
+                __syncthreads();
             }
         }
-        if (whole < count && whole % col_waves == cw) {
-            Codes<NARROW> now[RT];
+    } else {
+        put(x, 0);
+        __syncthreads();
+    }
+    if (const uint32_t chunk = stages * col_waves + cw; chunk < chunks) {          // (not of every wave)
+        Codes<NARROW> now[RT];
+        const uint64_t col = (c0 + chunk) * kChunk;
 #pragma unroll
-            for (int r = 0; r < RT; ++r) load_codes_tail<NARROW>(now[r], row[r], block_log2, col0 + (uint64_t)whole * kChunk, a.cols, j);
-            use(now, whole);
-        }
+        for (int r = 0; r < RT; ++r)
+            if (chunk < whole) load_codes<NARROW>(now[r], row[r], block_log2, col, j);
+            else load_codes_tail<NARROW>(now[r], row[r], block_log2, col, a.cols, j);
+        use(now, stages);
     }
 
     // the waves that split the columns: join in LDS
@@ -418,7 +448,7 @@ constexpr uint32_t kStageChunks = 2, kSlots = kStageChunks * 4;   // of a stage;
 template <typename T, int TT, bool NARROW>
 struct Stage {
     static constexpr uint32_t H = NARROW ? 2 : 1, rows = 16 * kWaves, codes = rows * kSlots * 16, scales = rows * kStageChunks * H * 4;
-    __host__ __device__ static uint32_t bytes(uint32_t tokens) { return codes + scales + kStageChunks * Record<T, TT, NARROW>::bytes(tokens); }
+    static constexpr uint32_t bytes = codes + scales + kStageChunks * Record<T, TT, NARROW>::bytes;
 };
 
 template <typename T, int TT, bool NARROW>
@@ -429,7 +459,8 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
     using Raw = typename EightOf<T>::Raw;
     constexpr int PER = 4 / Digits<T>::stride, H = S::H;
     extern __shared__ __align__(16) uint8_t lds[];
-    const uint32_t tokens = (uint32_t)a.tokens, x_rows = R::rows(tokens), record = R::bytes(tokens), half = S::bytes(tokens);
+    const uint32_t tokens = (uint32_t)a.tokens;
+    constexpr uint32_t record = R::bytes, half = S::bytes;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane & 15, j = lane >> 4;
     const uint32_t block_log2 = 31 - __builtin_clz(a.block), pitch = 4 + a.block / 2;
     const uint64_t all_stages = (a.cols + kStageChunks * kChunk - 1) / (kStageChunks * kChunk);
@@ -484,12 +515,9 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
         }
         if (has_scale) reinterpret_cast<float*>(to + S::codes)[threadIdx.x] = v.scale;
         uint8_t* records = to + S::codes + S::scales;
-        if (x_tok < tokens) make_digits<T, TT, NARROW>(tokens, x_tok, x_unit % 16, v.x, records + x_unit / 16 * record);
+        if (x_tok < tokens) make_digits<T, TT, NARROW>(x_tok, x_unit % 16, v.x, records + x_unit / 16 * record);
     };
 
-    uint32_t x_at[TT];                                            // the lane's row of x in each tile; rows that are not there repeat the last
-#pragma unroll
-    for (int t = 0; t < TT; ++t) x_at[t] = j * x_rows + (16 * t + n < x_rows ? 16 * t + n : x_rows - 1);
     float sum[1][TT][PER];
 #pragma unroll
     for (int t = 0; t < TT; ++t)
@@ -505,7 +533,7 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
             for (int w = 0; w < 4; ++w) codes[0].w[w] = v[w];
 #pragma unroll
             for (int h = 0; h < H; ++h) codes[0].scale[h] = reinterpret_cast<const float*>(from + S::codes)[my_row * SCALES + c * H + h];
-            multiply<T, TT, 1, NARROW>(codes, from + S::codes + S::scales + c * record, tokens, x_at, j, sum);
+            multiply<T, TT, 1, NARROW>(codes, from + S::codes + S::scales + c * record, n, j, sum);
         }
     };
     // Stage s is multiplied out of one half of the LDS while stage s + 1 is on its way.  (The last one again behind the end: no branch.)
@@ -749,7 +777,7 @@ void by_tiles(int tiles, bool narrow, F f) {
 template <typename T>
 uint32_t record_bytes(uint64_t tokens, bool narrow) {
     uint32_t bytes = 0;
-    by_tiles<T>(product_tiles<T>(tokens), narrow, [&](auto t, auto n) { bytes = Record<T, decltype(t)::value, decltype(n)::value>::bytes((uint32_t)tokens); });
+    by_tiles<T>(product_tiles<T>(tokens), narrow, [&](auto t, auto n) { bytes = Record<T, decltype(t)::value, decltype(n)::value>::bytes; });
     return bytes;
 }
 
@@ -787,8 +815,6 @@ ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens, bool nar
     p.parts = split(256, groups, chunks / (4 * col_waves));
     p.part_chunks = (uint32_t)((chunks + p.parts - 1) / p.parts);
     p.parts = (uint32_t)((chunks + p.part_chunks - 1) / p.part_chunks);
-    const uint32_t fit = kPanel / record;
-    p.stage_chunks = p.part_chunks < fit ? p.part_chunks : fit;
     return p;
 }
 
@@ -813,8 +839,8 @@ void over_rows(uint64_t rows, uint64_t height, F launch) {
 template <typename T, int TT, bool NARROW>
 void launch_product_tiles(ProductShape a, hipStream_t stream) {
     using S = Stage<T, TT, NARROW>;
-    const uint32_t lds = 2 * S::bytes((uint32_t)a.tokens);
-    static_assert(2 * (S::codes + S::scales + kStageChunks * (4096 + 2 * TT * 96)) <= 64 * 1024, "what a launch may ask for");
+    constexpr uint32_t lds = 2 * S::bytes;
+    static_assert(lds <= 64 * 1024, "what a launch may ask for");
     over_rows(a.rows, S::rows, [&](uint64_t row0, unsigned groups) {
         a.row0 = row0;
         hipLaunchKernelGGL((product_tiles_kernel<T, TT, NARROW>), dim3(groups, a.plan.parts), dim3(kThreads), lds, stream, a);
@@ -827,7 +853,7 @@ void launch_product_kernels(ProductShape a, hipStream_t stream) {
         launch_product_tiles<T, TT, NARROW>(a, stream);
     } else {
         const uint32_t tokens = (uint32_t)a.tokens, join = a.plan.row_waves == kWaves ? 0 : kThreads * kRowTiles * TT * (4 / Digits<T>::stride) * 4;
-        const uint32_t panel = a.plan.stage_chunks * Record<T, TT, NARROW>::bytes(tokens), lds = panel > join ? panel : join;
+        const uint32_t x = 2 * (kWaves / a.plan.row_waves) * Record<T, TT, NARROW>::bytes, lds = x > join ? x : join;
         hipLaunchKernelGGL((product_digits_kernel<T, TT, NARROW>), dim3((unsigned)((a.cols + kChunk - 1) / kChunk), (tokens + 15) / 16), dim3(256), 0, stream, a, static_cast<uint8_t*>(a.work));
         a.panel = static_cast<const uint8_t*>(a.work);
         over_rows(a.rows, 16 * kRowTiles * a.plan.row_waves, [&](uint64_t row0, unsigned groups) {
