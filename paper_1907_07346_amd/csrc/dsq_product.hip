@@ -10,9 +10,9 @@
 // one factor for all of the lane's results.  x's bytes lie in LDS in the order in which codes come out of a word.
 //   Three kernels.  One token: product_one_kernel.  Up to two matrix instructions of tokens (16; 8 for fp32), where reading codes is most of the work:
 // product_tiles_kernel, whose workgroups make x's bytes themselves.  More tokens: product_kernel; a launch before makes x's bytes once, in work_dev,
-// and codes go straight into registers, which leaves LDS to x.  Measured, us, product_tiles_kernel against product_kernel: 2 x 65536 x 4096, bf16,
-// 42.0 : 45.5; 16 x 4096 x 16384, fp16, 19.0 : 24.8; 8 x 2048 x 2048 7.1 : 9.0; 4 x 16384 x 4096, fp32, 16.1 : 16.4; from there on 61 x 16001 x 4099,
-// bf16, 55.7 : 46.3; 64 x 65536 x 1024 31.7 : 28.0, and in blocks of 64 51.4 : 39.8; 32 x 16384 x 4096, fp32, 30.3 : 31.7.
+// and codes go straight into registers, which leaves LDS to x.  Measured, us, product_tiles_kernel : product_kernel: 2 x 65536 x 4096, bf16,
+// 34.0 : 62.0; 16 x 4096 x 16384, fp16, 19.4 : 26.7; 8 x 2048 x 2048 7.1 : 11.7; 4 x 16384 x 4096, fp32, 16.9 : 18.5; from there on 61 x 16001 x 4099,
+// bf16, 55.7 : 38.6; 64 x 65536 x 1024 31.7 : 24.9, and in blocks of 64 51.4 : 31.6; 32 x 16384 x 4096, fp32, 30.3 : 26.9.
 //   Where there are too few rows for the GPU, workgroups split the columns, too, and one more launch adds their sums.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
@@ -437,17 +437,20 @@ __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
             }
 }
 
-// Few tokens: codes go through LDS, too, 128 rows of 256 columns at a time, so that memory is read in rows of 128 bytes (see product_one_kernel) and a
+// Few tokens: codes go through LDS, too, 128 rows of 256 columns at a time, so that memory is read in rows of 128 bytes and more (see product_one_kernel) and a
 // compute unit has as much under way as it multiplies.  While a stage is multiplied the next one's loads are on their way into registers; then it goes into
-// the other half of the LDS.  Rows of codes are 128 bytes apart, their 16-byte pieces swapped by the row's last bits against bank conflicts.
-//   16 tokens cost some 340 instructions a stage, 5400 clocks for the two workgroups of a compute unit, in which it could read 44 KB and reads 32: x's
-// digits are a third of them.  16 x 4096 x 16384 reads 2.3 TB/s, 16 x 65536 x 4096 3.2 (44.0 us), 2 x 65536 x 4096 3.4.  Slower: two stages ahead
-// (registers; 16 x 4096 x 16384 22.8 us), workgroups of 256 rows (2 x 65536 x 4096 46.8 us).
-constexpr uint32_t kStageChunks = 2, kSlots = kStageChunks * 4;   // of a stage; 16-byte pieces of a row
+// the other half of the LDS.  A row's part of a stage is read as it lies in the message, in nine pieces of 16 bytes, scales among the codes: a load that
+// gathers scales alone costs the memory pipeline as much as one that brings 16 bytes a lane (2 x 65536 x 4096, blocks of 256, 34.0 us, 42.9 with scales read
+// apart; 16 x 4096 x 16384, where the instructions count, 19.4 and 18.8).  Blocks of more than 256 columns are read in eight pieces, and their scales once a
+// block (of 2048: 30.2 us).
+//   2 tokens of 65536 x 4096 read 4.2 TB/s.  16 tokens cost some 340 instructions a stage, 5400 clocks for the two workgroups of a compute unit, in which it
+// could read 44 KB and reads 32: x's digits are a third of them; 44.2 us, and 2.3 TB/s for 16 x 4096 x 16384, whose workgroups have four stages each.
+// Slower: two stages ahead (registers; 16 x 4096 x 16384 22.8 us), workgroups of 256 rows (2 x 65536 x 4096 46.8 : 42.9).
+constexpr uint32_t kStageChunks = 2, kStageCols = kStageChunks * kChunk, kRowPieces = 9;   // of a stage; 16-byte pieces of a row at most
 
 template <typename T, int TT, bool NARROW>
 struct Stage {
-    static constexpr uint32_t H = NARROW ? 2 : 1, rows = 16 * kWaves, codes = rows * kSlots * 16, scales = rows * kStageChunks * H * 4;
+    static constexpr uint32_t rows = 16 * kWaves, codes = rows * kRowPieces * 16, scales = rows * 4;
     static constexpr uint32_t bytes = codes + scales + kStageChunks * Record<T, TT, NARROW>::bytes;
 };
 
@@ -457,62 +460,81 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
     static_assert(16 * kStageChunks * TT * kTileTokens<T> <= kThreads, "a thread has eight columns of x");
     using R = Record<T, TT, NARROW>;
     using Raw = typename EightOf<T>::Raw;
-    constexpr int PER = 4 / Digits<T>::stride, H = S::H;
+    constexpr int PER = 4 / Digits<T>::stride;
     extern __shared__ __align__(16) uint8_t lds[];
     const uint32_t tokens = (uint32_t)a.tokens;
     constexpr uint32_t record = R::bytes, half = S::bytes;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane & 15, j = lane >> 4;
     const uint32_t block_log2 = 31 - __builtin_clz(a.block), pitch = 4 + a.block / 2;
-    const uint64_t all_stages = (a.cols + kStageChunks * kChunk - 1) / (kStageChunks * kChunk);
+    const uint64_t all_stages = (a.cols + kStageCols - 1) / kStageCols;
     const uint32_t cols = (uint32_t)a.cols, s0 = blockIdx.y * a.plan.part_chunks;          // (of stages here)
     const uint32_t stages = (uint32_t)(all_stages - s0 < a.plan.part_chunks ? all_stages - s0 : a.plan.part_chunks);
     const uint64_t first = a.row0 + (uint64_t)blockIdx.x * S::rows;
 
-    // what the thread brings: two pieces of codes, a scale, and x
-    const uint32_t slot = threadIdx.x % kSlots, tile_row = threadIdx.x / kSlots;           // and as many rows on
+    // what the thread brings: two pieces of codes (some a third), a long block's scale, and x
+    const bool apart = a.block > kStageCols;                      // scales are
+    const uint32_t row_pieces = apart ? kRowPieces - 1 : kRowPieces, row_bytes = (uint32_t)a.row_bytes;    // (below 2^28)
     auto row_at = [&](uint32_t r) { return a.msg + (first + r < a.rows ? first + r : a.rows - 1) * a.row_bytes; };
-    const uint8_t* code_row[2] = {row_at(tile_row), row_at(tile_row + S::rows / 2)};
-    constexpr uint32_t SCALES = kStageChunks * H;                 // of a row
-    const bool has_scale = threadIdx.x < S::rows * SCALES;
-    const uint8_t* scale_row = row_at(threadIdx.x / SCALES % S::rows);
+    constexpr uint32_t PIECES = (S::rows * kRowPieces + kThreads - 1) / kThreads;
+    const uint8_t* from[PIECES];
+    uint32_t piece_at[PIECES], piece_to[PIECES];
+#pragma unroll
+    for (uint32_t i = 0; i < PIECES; ++i) {
+        const uint32_t q = i * kThreads + threadIdx.x, in = apart ? q / (kRowPieces - 1) : q / kRowPieces, r = in < S::rows ? in : S::rows - 1;
+        from[i] = row_at(r);
+        piece_at[i] = (q - in * row_pieces) * 16;
+        piece_to[i] = r * kRowPieces * 16 + piece_at[i];
+    }
+    const bool has_third = (PIECES - 1) * kThreads + threadIdx.x < S::rows * row_pieces, has_scale = apart && threadIdx.x < S::rows;
+    const uint8_t* scale_row = row_at(threadIdx.x % S::rows);
+    const bool has_end = first + S::rows >= a.rows;               // of the message
     const uint32_t x_tok = threadIdx.x / (16 * kStageChunks), x_unit = threadIdx.x % (16 * kStageChunks);
     const T* x_row = static_cast<const T*>(a.in) + (x_tok < tokens ? x_tok : tokens - 1) * a.in_ld;
     struct Brought {
-        u32x4 codes[2];
+        u32x4 codes[PIECES];
         float scale;
         Raw x;
+        uint32_t back;                                            // words that a piece which would end behind the message was read too early by
     };
     auto bring = [&](Brought& v, uint32_t s) {
-        const uint32_t col = (s0 + s) * (kStageChunks * kChunk), mine = col + 32 * slot, of_scale = col + threadIdx.x % SCALES * (kChunk / H);
-        const uint32_t at = (mine >> block_log2) * pitch + 4 + (mine & (a.block - 1)) / 2, scale_at = (of_scale >> block_log2) * pitch;   // a row is below 2^28 bytes
-        const bool whole = col + kStageChunks * kChunk <= cols;
-        if (whole) {
+        const uint32_t col = (s0 + s) * kStageCols, in_block = col & (a.block - 1), block_at = (col >> block_log2) * pitch;
+        const uint32_t at = apart ? block_at + 4 + in_block / 2 : block_at;
+        v.back = 0;
+        if (col + kStageCols <= cols) {                           // all blocks are there, and a last piece may end in the next row ...
+            if (has_end && at + row_pieces * 16 > row_bytes) {    // ... if there is one
+                v.back = (at + row_pieces * 16 - row_bytes) / 4;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) v.codes[i] = *reinterpret_cast<const u32x4_at4*>(code_row[i] + at);
-            v.scale = *reinterpret_cast<const float*>(scale_row + scale_at);
+                for (uint32_t i = 0; i < PIECES; ++i) {
+                    const uint32_t piece = at + piece_at[i];
+                    if (i + 1 < PIECES || has_third) v.codes[i] = *reinterpret_cast<const u32x4_at4*>(from[i] + (piece + 16 <= row_bytes ? piece : row_bytes - 16));
+                }
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < PIECES; ++i)
+                    if (i + 1 < PIECES || has_third) v.codes[i] = *reinterpret_cast<const u32x4_at4*>(from[i] + (at + piece_at[i]));
+            }
             v.x = *reinterpret_cast<const Raw*>(x_row + (col + 8 * x_unit));
-        } else {                                                  // the ragged end: words that are not there are 0
+        } else {                                                  // words that are not there are 0
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (uint32_t i = 0; i < PIECES; ++i)
+                if (i + 1 < PIECES || has_third)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) v.codes[i][w] = mine + 8 * w < cols ? *reinterpret_cast<const uint32_t*>(code_row[i] + at + 4 * w) : 0u;
-            v.scale = of_scale < cols ? *reinterpret_cast<const float*>(scale_row + scale_at) : 0.f;
+                    for (uint32_t w = 0; w < 4; ++w) {
+                        const uint32_t word = at + piece_at[i] + 4 * w;
+                        v.codes[i][w] = word < row_bytes ? *reinterpret_cast<const uint32_t*>(from[i] + word) : 0u;
+                    }
             v.x = load_eight(x_row, col + 8 * x_unit, cols);
         }
+        if (has_scale && (in_block == 0 || s == 0)) v.scale = *reinterpret_cast<const float*>(scale_row + block_at);
     };
-    auto put = [&](const Brought& v, uint8_t* to) {
+    auto put = [&](Brought& v, uint8_t* to) {
+        if (v.back)                                               // (2 or 3, with blocks of 128 or 256)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t r = tile_row + S::rows / 2 * i;
-            if constexpr (NARROW) {                               // piece s of a chunk: words 4 (s % 2) .. + 3 of block s / 2, for lanes 2 (s % 2) and + 1
-                const uint32_t chunk = slot / 4, h = slot % 4 / 2, lane0 = chunk * 4 + slot % 2 * 2;
+            for (uint32_t i = 0; i < PIECES; ++i)
+                if (piece_at[i] == (kRowPieces - 1) * 16) v.codes[i].xy = v.back == 2 ? v.codes[i].zw : v.codes[i].ww;
 #pragma unroll
-                for (int w = 0; w < 2; ++w)
-                    *reinterpret_cast<u32x2*>(to + (r * kSlots + ((lane0 + w) ^ (r % kSlots))) * 16 + 8 * h) = u32x2{v.codes[i][2 * w], v.codes[i][2 * w + 1]};
-            } else {
-                *reinterpret_cast<u32x4*>(to + (r * kSlots + (slot ^ (r % kSlots))) * 16) = v.codes[i];
-            }
-        }
+        for (uint32_t i = 0; i < PIECES; ++i)
+            if (i + 1 < PIECES || has_third) *reinterpret_cast<u32x4*>(to + piece_to[i]) = v.codes[i];
         if (has_scale) reinterpret_cast<float*>(to + S::codes)[threadIdx.x] = v.scale;
         uint8_t* records = to + S::codes + S::scales;
         if (x_tok < tokens) make_digits<T, TT, NARROW>(x_tok, x_unit % 16, v.x, records + x_unit / 16 * record);
@@ -524,16 +546,29 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
 #pragma unroll
         for (int i = 0; i < PER; ++i) sum[0][t][i] = 0.f;
     const uint32_t my_row = wave * 16 + n;
-    auto use = [&](uint8_t* from) {
+    // of the lane's row in a half: chunk c's scale and codes; with blocks of 64 block b's are 36 b from the first
+    const uint32_t block = my_row * kRowPieces * 16, scale_at = apart ? S::codes + 4 * my_row : block, scale_step = a.block == kChunk ? pitch : 0;
+    const uint32_t codes_at = block + (apart ? 0 : 4) + 16 * j, codes_step = a.block == kChunk ? pitch : kChunk / 2;
+    auto use = [&](uint8_t* half_at) {
 #pragma unroll
         for (uint32_t c = 0; c < kStageChunks; ++c) {
             Codes<NARROW> codes[1];
-            const u32x4 v = *reinterpret_cast<const u32x4*>(from + (my_row * kSlots + ((c * 4 + j) ^ (my_row % kSlots))) * 16);
+            if constexpr (NARROW) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) codes[0].w[w] = v[w];
+                for (uint32_t h = 0; h < 2; ++h) {
+                    const uint8_t* p = half_at + block + (2 * c + h) * 36;
+                    codes[0].scale[h] = *reinterpret_cast<const float*>(p);
+                    const u32x2 v = *reinterpret_cast<const u32x2_at4*>(p + 4 + 8 * j);
+                    codes[0].w[2 * h] = v.x;
+                    codes[0].w[2 * h + 1] = v.y;
+                }
+            } else {
+                codes[0].scale[0] = *reinterpret_cast<const float*>(half_at + scale_at + c * scale_step);
+                const u32x4 v = *reinterpret_cast<const u32x4_at4*>(half_at + codes_at + c * codes_step);
 #pragma unroll
-            for (int h = 0; h < H; ++h) codes[0].scale[h] = reinterpret_cast<const float*>(from + S::codes)[my_row * SCALES + c * H + h];
-            multiply<T, TT, 1, NARROW>(codes, from + S::codes + S::scales + c * record, n, j, sum);
+                for (int w = 0; w < 4; ++w) codes[0].w[w] = v[w];
+            }
+            multiply<T, TT, 1, NARROW>(codes, half_at + S::codes + S::scales + c * record, n, j, sum);
         }
     };
     // Stage s is multiplied out of one half of the LDS while stage s + 1 is on its way.  (The last one again behind the end: no branch.)
