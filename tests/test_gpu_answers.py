@@ -72,6 +72,33 @@ def test_product_and_its_gradient(tokens, rows, cols, block, dtype):
     assert torch.equal(y, b.ds_product(msg_dev, x.cuda(), rows, block)) and torch.equal(dx, b.ds_product_gradient(msg_dev, dy.cuda(), cols, block))
 
 
+# Whole stages of 256 columns for every block size, of which the matrix's last row has the last 16-byte piece end behind the message (blocks of 128
+# and 256), or its scale in an earlier stage (longer ones); more workgroups than one for the columns, and rows that end inside one of them.
+ENDS = [(2, 3, 256, 64), (3, 128, 256, 128), (4, 129, 256, 256), (5, 130, 512, 128), (8, 1, 768, 256), (9, 257, 1024, 512), (12, 300, 2048, 2048),
+        (16, 260, 2560, 1024), (7, 40, 4352, 2048), (6, 2000, 512, 256), (2, 64, 8192, 128),
+        # the gradient's rows and columns in a number of workgroups that no eight divides
+        (20, 3001, 700, 128), (11, 9000, 390, 256), (50, 2600, 1500, 512)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("tokens,rows,cols,block", ENDS)
+def test_products_of_whole_stages(tokens, rows, cols, block, dtype):
+    rng = np.random.default_rng(tokens * 7919 + rows * 31 + cols)
+    msg, codes, scales = plain.random_message(rows, cols, block, rng)
+    m, unit = plain.dense(codes, scales, block), units(scales, block, cols)
+    x, dy = normal(rng, (tokens, cols), dtype), normal(rng, (tokens, rows), dtype)
+    # what follows the matrix is no part of it: scales that are infinite and NaN
+    big = torch.full((msg.numel() + 256,), 255, dtype=torch.uint8)
+    big[:msg.numel()] = msg
+    here = big.cuda()[:msg.numel()]
+    y = b.ds_product(here, x.cuda(), rows, block)
+    want = x.double() @ m.t().contiguous()
+    check(y, want, product_tolerance(want, x.double(), unit.t().contiguous(), dtype), "y")
+    dx = b.ds_product_gradient(here, dy.cuda(), cols, block)
+    want = dy.double() @ m
+    check(dx, want, product_tolerance(want, dy.double(), unit, dtype), "dx")
+
+
 def test_gradient_is_the_transpose_and_matches_differences():
     """<dy, product(x)> = <gradient(dy), x>, and the product is linear: a difference of it along e_c is the gradient's column."""
     rng = np.random.default_rng(5)
@@ -203,6 +230,12 @@ def check_top(z, k, temperature=1.0):
                                           (33, 4097, 100), (3, 32003, 256), (2, 131072, 64), (1, 262147, 128), (600, 513, 8), (1, 9000, 255)])
 def test_top_logits(rows, vocab, k, dtype):
     check_top(normal(np.random.default_rng(rows * 7 + vocab), (rows, vocab), dtype, 3.0), k, 1.0 if k % 2 else 2.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16])
+@pytest.mark.parametrize("rows,vocab,k", [(1, 700001, 256), (2, 300000, 200), (1, 1000003, 100), (3, 9000, 2), (5, 4099, 250), (20, 33000, 256), (1, 270000, 1)])
+def test_top_logits_of_rows_in_many_parts(rows, vocab, k, dtype):
+    check_top(normal(np.random.default_rng(rows * 13 + vocab), (rows, vocab), dtype, 3.0), k, 0.5)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
