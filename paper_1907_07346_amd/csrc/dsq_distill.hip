@@ -34,16 +34,12 @@ struct Teacher {
 
 template <int WAVES>
 __device__ __forceinline__ float workgroup_total(float v, float* sums) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+    v = total_over_lanes<64>(v);
     if (WAVES == 1) return v;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x / 64] = v;
     __syncthreads();
-    v = sums[threadIdx.x & (WAVES - 1)];                          // (WAVES is a power of two)
-#pragma unroll
-    for (int o = 1; o < WAVES; o <<= 1) v += __shfl_xor(v, o);
-    return v;
+    return total_over_lanes<WAVES>(sums[threadIdx.x & (WAVES - 1)]);
 }
 
 // k <= 256: the entries are the first four waves'.

@@ -70,11 +70,38 @@ __device__ __forceinline__ float largest_of(const float (&z)[N]) {
     for (int e = 1; e < N; ++e) m = max_or_nan(m, z[e]);
     return m;
 }
-// Joins the spreads of a workgroup's WAVES * 64 threads, in an order that is always the same; every thread gets the result.  sums: 2 * WAVES floats of LDS.
+// op over 2, 4, 8 or 16 adjacent lanes, or all 64, in all of them and in an order that is always the same: a lane with its neighbour, with the other two of
+// its four, with its mirror image in eight and in sixteen, and the four sixteens one after the other.
+template <int CTRL>
+__device__ __forceinline__ float other_lane(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true)); }
+template <int LANES, typename F>
+__device__ __forceinline__ float over_lanes(float v, F op) {
+    if (LANES >= 2) v = op(v, other_lane<0xB1>(v));               // quad_perm 1 0 3 2
+    if (LANES >= 4) v = op(v, other_lane<0x4E>(v));               // quad_perm 2 3 0 1
+    if (LANES >= 8) v = op(v, other_lane<0x141>(v));              // row_half_mirror
+    if (LANES >= 16) v = op(v, other_lane<0x140>(v));             // row_mirror
+    if (LANES == 64) {
+        auto sixteen = [&](int of) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), of)); };
+        v = op(op(sixteen(0), sixteen(16)), op(sixteen(32), sixteen(48)));
+    }
+    return v;
+}
+template <int LANES>
+__device__ __forceinline__ float total_over_lanes(float v) {
+    return over_lanes<LANES>(v, [](float a, float b) { return a + b; });
+}
+// Joins the lanes' spreads as join does, but the largest first, so that each sum is scaled once (8 x 32003, fp32, k = 16, a row's whole gradient: 11.3 us with
+// joins two by two over lane shuffles).
+template <int LANES>
+__device__ __forceinline__ Spread spread_over_lanes(Spread s, float scale) {
+    const float m = over_lanes<LANES>(s.max, [](float a, float b) { return max_or_nan(a, b); });
+    return {m, total_over_lanes<LANES>(s.sum == 0.f ? 0.f : s.sum * power2(exponents(s.max, scale).at - exponents(m, scale).at))};
+}
+// Joins the spreads of a workgroup's WAVES * 64 threads; every thread gets the result.  sums: 2 * WAVES floats of LDS.
 template <int WAVES>
 __device__ Spread workgroup_spread(Spread s, float scale, float* sums) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) s = join(s, Spread{__shfl_xor(s.max, o), __shfl_xor(s.sum, o)}, scale);
+    static_assert(WAVES <= 16 && (WAVES & (WAVES - 1)) == 0);
+    s = spread_over_lanes<64>(s, scale);
     if (WAVES == 1) return s;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) {
@@ -82,11 +109,8 @@ __device__ Spread workgroup_spread(Spread s, float scale, float* sums) {
         sums[2 * (threadIdx.x / 64) + 1] = s.sum;
     }
     __syncthreads();
-    const int w = threadIdx.x & (WAVES - 1);                      // (WAVES is a power of two)
-    s = Spread{sums[2 * w], sums[2 * w + 1]};
-#pragma unroll
-    for (int o = 1; o < WAVES; o <<= 1) s = join(s, Spread{__shfl_xor(s.max, o), __shfl_xor(s.sum, o)}, scale);
-    return s;
+    const int w = threadIdx.x & (WAVES - 1);
+    return spread_over_lanes<WAVES>(Spread{sums[2 * w], sums[2 * w + 1]}, scale);
 }
 // ln of the sum of exp(z / temperature) is base + rest: the largest (0 where that is infinite) and, for what `at` was rounded to, the sum.
 struct LogSum {
