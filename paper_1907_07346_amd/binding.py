@@ -241,11 +241,13 @@ def _refuse(where: str, why: str):
     raise DsqError(DS_EINVAL, where, why)
 
 
-def _on_device(where: str, names: str, *tensors):
+def _on_device(where: str, names: str, *tensors) -> int:
+    """The current device, on which they have to be."""
     here = torch.cuda.current_device()
-    for at, t in enumerate(tensors):
-        if t is not None and (not t.is_cuda or t.get_device() != here):
-            _refuse(where, f"{names.split()[at]} must be on the current CUDA device")
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            _refuse(where, f"{names.split()[[t is other for other in tensors].index(True)]} must be on the current CUDA device")
+    return here
 
 
 def _rows_of(where: str, name: str, t: "torch.Tensor"):
@@ -274,19 +276,21 @@ def _new(stream, shape, dtype, like):
         return like.new_empty(shape, dtype=dtype)
 
 
-def _answer(name: str, shape, like, stream, *args):
-    """Calls `name` with scratch memory of the call's stream; the reason of a refusal goes into the exception."""
-    if stream is not None and stream.device_index != like.get_device():
+def _answer(name: str, work_bytes, call, shape, like, here: int, stream, *args):
+    """Makes the call with scratch memory of its stream; the reason of a refusal goes into the exception."""
+    if stream is None:
+        pointer = _raw_stream(here) if _raw_stream is not None else _stream_pointer(None)
+    elif stream.device_index != here:
         _refuse(name, "stream must be of the current CUDA device")
-    L = lib()
-    shape = ctypes.byref(shape)
-    size = getattr(L, name + "_work_bytes")(shape)
+    else:
+        pointer = stream.cuda_stream
+    size = work_bytes(shape)
     work = _new(stream, (size,), torch.uint8, like) if size else None
-    call, end = getattr(L, name), (work.data_ptr() if size else None, size, _stream_pointer(stream))
-    st = call(shape, *args, *end, None, 0)
+    at = work.data_ptr() if size else None
+    st = call(shape, *args, at, size, pointer, None, 0)
     if st == DS_EINVAL:                                   # (checks only: nothing has been enqueued)
         buf = ctypes.create_string_buffer(256)
-        call(shape, *args, *end, buf, 256)
+        call(shape, *args, at, size, pointer, buf, 256)
         raise DsqError(st, name, buf.value.decode())
     if st != DS_OK:
         raise DsqError(st, name)
@@ -296,16 +300,15 @@ def ds_matrix_bytes(rows: int, cols: int, block: int) -> int:
     return int(lib().ds_matrix_bytes(ctypes.byref(ds_matrix(rows, cols, 0, block, 0))))
 
 
-def _through(name: str, msg: "torch.Tensor", x: "torch.Tensor", rows: int, cols: int, block: int, out: "Optional[torch.Tensor]",
-             stream: Optional["torch.cuda.Stream"]):
-    width, out_width = (cols, rows) if name == "ds_product" else (rows, cols)
+def _through(name: str, work_bytes, call, msg: "torch.Tensor", x: "torch.Tensor", rows: int, cols: int, width: int, out_width: int, block: int,
+             out: "Optional[torch.Tensor]", stream: Optional["torch.cuda.Stream"]):
     tokens, got, pitch = _rows_of(name, "the input", x)
     if got != width:
         _refuse(name, f"the input must have {width} columns")
-    m = ds_matrix(rows, cols, tokens, block, _DTYPES[x.dtype])
-    if msg.dtype != torch.uint8 or not msg.is_contiguous() or msg.numel() < lib().ds_matrix_bytes(ctypes.byref(m)):
+    m = ctypes.byref(ds_matrix(rows, cols, tokens, block, _DTYPES[x.dtype]))
+    if msg.dtype != torch.uint8 or not msg.is_contiguous() or msg.numel() < _lib.ds_matrix_bytes(m):
         _refuse(name, "msg must be a contiguous uint8 tensor that holds the matrix")
-    _on_device(name, "msg x out", msg, x, out)
+    here = _on_device(name, "msg x out", msg, x, out)
     out_pitch = out_width
     if out is None:
         out = _new(stream, (tokens, out_width), x.dtype, x)
@@ -314,31 +317,35 @@ def _through(name: str, msg: "torch.Tensor", x: "torch.Tensor", rows: int, cols:
     else:
         out_pitch = _rows_of(name, "out", out)[2]
     if tokens:
-        _answer(name, m, x, stream, msg.data_ptr(), x.data_ptr(), pitch, out.data_ptr(), out_pitch)
+        _answer(name, work_bytes, call, m, x, here, stream, msg.data_ptr(), x.data_ptr(), pitch, out.data_ptr(), out_pitch)
     return out
 
 
 def ds_product(msg: "torch.Tensor", x: "torch.Tensor", rows: int, block: int, out: "Optional[torch.Tensor]" = None,
                stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
     """x (tokens, cols) through the matrix of `rows` rows held as 4-bit messages in msg (uint8): (tokens, rows) of x's dtype."""
-    return _through("ds_product", msg, x, rows, x.shape[-1], block, out, stream)
+    L, cols = lib(), x.shape[-1]
+    return _through("ds_product", L.ds_product_work_bytes, L.ds_product, msg, x, rows, cols, cols, rows, block, out, stream)
 
 
 def ds_product_gradient(msg: "torch.Tensor", dy: "torch.Tensor", cols: int, block: int, out: "Optional[torch.Tensor]" = None,
                         stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
     """The gradient of ds_product with respect to x: dy (tokens, rows) gives (tokens, cols) of dy's dtype."""
-    return _through("ds_product_gradient", msg, dy, dy.shape[-1], cols, block, out, stream)
+    L, rows = lib(), dy.shape[-1]
+    return _through("ds_product_gradient", L.ds_product_gradient_work_bytes, L.ds_product_gradient, msg, dy, rows, cols, rows, cols, block, out, stream)
 
 
 def ds_top_logits(z: "torch.Tensor", k: int, temperature: float = 1.0, stream: Optional["torch.cuda.Stream"] = None):
     """The k largest logits of each row of z: (pairs, lse), pairs int32 (rows, k, 2) of index and float32 bits, ascending index."""
     rows, vocab, pitch = _rows_of("ds_top_logits", "z", z)
-    _on_device("ds_top_logits", "z", z)
+    here = _on_device("ds_top_logits", "z", z)
     if not 1 <= k <= 256:
         _refuse("ds_top_logits", "k must be between 1 and 256")
     pairs, lse = _new(stream, (rows, k, 2), torch.int32, z), _new(stream, (rows,), torch.float32, z)
     if rows:
-        _answer("ds_top_logits", ds_logits(rows, vocab, k, _DTYPES[z.dtype], temperature, 0), z, stream,
+        L = lib()
+        _answer("ds_top_logits", L.ds_top_logits_work_bytes, L.ds_top_logits,
+                ctypes.byref(ds_logits(rows, vocab, k, _DTYPES[z.dtype], temperature, 0)), z, here, stream,
                 z.data_ptr(), pitch, pairs.data_ptr(), lse.data_ptr())
     return pairs, lse
 
@@ -351,7 +358,7 @@ def ds_distill(z: "torch.Tensor", pairs: "torch.Tensor", temperature: float = 1.
     rows, vocab, pitch = _rows_of("ds_distill", "z", z)
     if pairs.dtype != torch.int32 or pairs.dim() != 3 or pairs.shape[0] != rows or pairs.shape[2] != 2 or not pairs.is_contiguous():
         _refuse("ds_distill", f"pairs must be a contiguous int32 tensor ({rows}, k, 2)")
-    _on_device("ds_distill", "z pairs teacher_lse weight dz", z, pairs, teacher_lse, weight, dz)
+    here = _on_device("ds_distill", "z pairs teacher_lse weight dz", z, pairs, teacher_lse, weight, dz)
     given = _vector("ds_distill", "teacher_lse", teacher_lse, rows), _vector("ds_distill", "weight", weight, rows)
     loss = _new(stream, (rows,), torch.float32, z) if want_loss else None
     dz_pitch = vocab if want_gradient else 0
@@ -365,9 +372,10 @@ def ds_distill(z: "torch.Tensor", pairs: "torch.Tensor", temperature: float = 1.
     elif dz is not None:
         _refuse("ds_distill", "dz is given but no gradient is wanted")
     if rows:
-        _answer("ds_distill", ds_logits(rows, vocab, pairs.shape[1], _DTYPES[z.dtype], temperature, 0), z, stream,
-                z.data_ptr(), pitch, pairs.data_ptr(), *given, loss.data_ptr() if want_loss else None,
-                dz.data_ptr() if want_gradient else None, dz_pitch)
+        L = lib()
+        _answer("ds_distill", L.ds_distill_work_bytes, L.ds_distill,
+                ctypes.byref(ds_logits(rows, vocab, pairs.shape[1], _DTYPES[z.dtype], temperature, 0)), z, here, stream,
+                z.data_ptr(), pitch, pairs.data_ptr(), *given, loss.data_ptr() if want_loss else None, dz.data_ptr() if want_gradient else None, dz_pitch)
     return loss, dz
 
 
