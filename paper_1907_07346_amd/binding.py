@@ -477,14 +477,14 @@ class DeepSqueeze:
         """x (tokens, cols) through parameters first .. first + rows * cols - 1 of `worker` as the message of the last ds_step holds
         them (4-bit QUANT_MAXABS; first and cols multiples of the block).  Some launch plans alternate between two message buffers:
         the call then waits for the last ds_step (see ds_message_ptr)."""
-        return self._through_message("ds_product", worker, x, rows, x.shape[-1], first, out, stream)
+        return ds_product(self._matrix("ds_product", worker, rows, x.shape[-1], first), x, rows, self.cfg.comp.block, out, stream)
 
     def ds_product_gradient(self, worker: int, dy: "torch.Tensor", cols: int, first: int = 0, out: "Optional[torch.Tensor]" = None,
                             stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
         """The gradient of ds_product (same worker and parameters) with respect to x."""
-        return self._through_message("ds_product_gradient", worker, dy, dy.shape[-1], cols, first, out, stream)
+        return ds_product_gradient(self._matrix("ds_product_gradient", worker, dy.shape[-1], cols, first), dy, cols, self.cfg.comp.block, out, stream)
 
-    def _through_message(self, name, worker, x, rows, cols, first, out, stream):
+    def _matrix(self, name, worker, rows, cols, first):
         comp = self.cfg.comp
         if comp.kind != KIND_QUANT_MAXABS or comp.bits != 4:
             _refuse(name, "messages of the 4-bit block quantiser only")
@@ -496,8 +496,7 @@ class DeepSqueeze:
             _refuse(name, "first and cols must be multiples of the block and the matrix must lie inside the worker's parameters")
         msg, total = self.ds_message_ptr()
         lo = worker * (total // self.n) + first // comp.block * (4 + comp.block // 2)
-        view = torch.as_tensor(_Lent(msg + lo, ds_matrix_bytes(rows, cols, comp.block), self), device="cuda")
-        return _through(name, view, x, rows, cols, comp.block, out, stream)
+        return torch.as_tensor(_Lent(msg + lo, ds_matrix_bytes(rows, cols, comp.block), self), device="cuda")
 
     def ds_diagnostics(self) -> dict:
         out = (ctypes.c_double * 4)()
