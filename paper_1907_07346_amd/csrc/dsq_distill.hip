@@ -5,6 +5,8 @@
 // and asks for the next row's logits as it writes: 16 bytes of gradient, and the registers they came from wait for 16 bytes of logits.  Where rows
 // are longer, or too few to fill the GPU, they are split: a first launch sums the parts, a second one reads the logits again (out of the
 // memory-side cache, mostly) and writes the gradient.
+//   4096 x 131072, bf16: 439 us, 4.9 TB/s in and out; 1023 x 50001, fp16: 49 us, 4.2, in two rows of each workgroup, the first of which is waited for.  The
+// exponentials are made twice, which with their arguments is most of the instructions: of 16 bits there is no room to keep them.
 //   The listed columns are written once more, after the dense part, by the thread that has the first of the entries with that index.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
@@ -335,8 +337,8 @@ constexpr uint64_t kRowBytes = 1024 * 16 * 16;                    // of the long
 void distill_plan(uint64_t rows, uint64_t vocab, uint64_t size, uint32_t& parts, uint64_t& part_logits) {
     parts = 0;
     part_logits = vocab;
-    // One launch where it holds up: rows 8 x 32003 f32 11.3 us, and 5.0 + 7.3 split; 1 x 65536 bf16 13.3 and 4.1 + 7.1; 1 x 131072 bf16 20.9 and 4.5 + 7.1; 64 x
-    // 131072 24.5 and 9.2 + 10.5; 200 x 131072 30.8 and 13.2 + 20.1.
+    // One launch where it holds up: rows 8 x 32003 f32 9.2 us, and 4.0 + 5.5 split; 1 x 65536 bf16 11.0 and 3.6 + 5.5; 1 x 131072 bf16 18.0 and 3.4 + 5.4; 64 x
+    // 131072 22.5 and 7.0 + 9.5; 200 x 131072 27.9 and 13.1 + 20.1.
     if (vocab * size <= kRowBytes && (rows >= 128 || vocab * size <= kRowBytes / 2)) return;
     const uint64_t stretch = kPartThreads * kPartPieces * (16 / size), stretches = (vocab + stretch - 1) / stretch;
     uint64_t p = rows >= 1024 ? 1 : 1024 / rows;
@@ -347,10 +349,10 @@ void distill_plan(uint64_t rows, uint64_t vocab, uint64_t size, uint32_t& parts,
     parts = (uint32_t)((stretches + each - 1) / each);
 }
 
-// Few threads with much of a row each, so that a compute unit has several rows under way: 4096 x 32000 bf16 with 256 threads 112 us, 512 128, 1024 184;
-// 1023 x 50001 f16 with 512 50, 1024 65.  As many workgroups as run at once, each with rows of its own (RESIDENT a compute unit): 1023 x 50001 50 us, and 58 with
+// Few threads with much of a row each, so that a compute unit has several rows under way: 4096 x 32000 bf16 with 256 threads 113 us, 512 136, 1024 233;
+// 1023 x 50001 f16 with 512 49, 1024 74.  As many workgroups as run at once, each with rows of its own (RESIDENT a compute unit): 1023 x 50001 49 us, and 54 with
 // one for each row.  Where a compute unit holds one row it gains nothing, and rows of weight 0 leave some with less to do than others (RESIDENT = 0: one for
-// each row): 4096 x 131072 bf16 480 us, and 502.
+// each row): 4096 x 131072 bf16 439 us, and 471.
 template <typename T, int THREADS, int N, int RESIDENT>
 void launch_rows(const DistillShape& a, unsigned here, hipStream_t stream) {
     constexpr unsigned most = 256 * RESIDENT;

@@ -7,10 +7,11 @@
 // of each wave's 16-byte pieces, m = ceil(k / 4): four times m >= k logits reach the lowest of the four, or it is minus infinity, which stands for what
 // is behind the end, and all pass.
 //   Few rows are split over workgroups, whose lists and sums go through work_dev to a second launch, which has room for all of a row's lists at once
-// (1 x 1000000, k = 100, fp32: 33.8 us; 72 where lists came one after the other).  Those two launches are mostly waiting: 1 x 131072, k = 64, bf16, 7.2 + 9.3 us,
+// (1 x 1000000, k = 100, fp32: 33.8 us; 72 where lists came one after the other).  Those two launches are mostly waiting: 1 x 131072, k = 64, bf16, 6.0 + 8.6 us,
 // where an empty launch takes 2; what the first finds is some 1500 candidates, and the second's time is three reads of memory, one behind the other, one
 // histogram and the ranks in one of its bins.
-//   Many rows are bound by reading the logits once: 2048 x 65536, fp32, k = 128, 124 us, 4.3 TB/s.
+//   Many rows are bound by reading the logits once: 2048 x 65536, fp32, k = 128, 124 us, 4.3 TB/s, with the
+// vector units busy nearly half the time.
 #include "dsq_answers.h"
 #include "dsq_logits.h"
 
