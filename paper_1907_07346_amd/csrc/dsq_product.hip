@@ -43,9 +43,8 @@ constexpr uint64_t kTokens = 8 * kTileTokens<T>;                  // of a launch
 constexpr int kRowTiles = 2;                                      // of 16 rows, of a wave of product_kernel
 
 struct ProductPlan {
-    uint32_t row_waves;                                           // waves side by side; the other kWaves / row_waves split the columns
-    uint32_t parts, part_chunks;                                  // workgroups that split the columns, and the chunks of each
-    uint32_t wave_rows;                                           // one token: rows of a wave
+    uint32_t parts, part_chunks;                                  // workgroups that split the columns, and the chunks (product_tiles_kernel: stages) of each
+    uint32_t row_waves, wave_rows;                                // one token: waves side by side, the other kWaves / row_waves split the columns; rows of a wave
 };
 
 struct ProductShape : ProductArgs {
@@ -317,21 +316,17 @@ __device__ __forceinline__ void multiply(const Codes<NARROW> (&c)[RT], uint8_t* 
 template <typename T, int TT, bool NARROW>
 __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
     constexpr int RT = kRowTiles;
-    constexpr uint32_t kPieces = 3;                               // 16-byte pieces of x a thread brings
-    using D = Digits<T>;
     using R = Record<T, TT, NARROW>;
-    constexpr int PER = 4 / D::stride;                            // tokens of a lane and matrix instruction
+    constexpr int PER = 4 / Digits<T>::stride;                    // tokens of a lane and matrix instruction
+    constexpr uint32_t record = R::bytes, kAll = record / 16, kPieces = (kAll + kThreads - 1) / kThreads;      // x of a chunk, in 16-byte pieces; of a thread
     extern __shared__ __align__(16) uint8_t lds[];
     const uint32_t tokens = (uint32_t)a.tokens;
-    constexpr uint32_t record = R::bytes;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane & 15, j = lane >> 4;
-    const uint32_t row_waves = a.plan.row_waves, col_waves = kWaves / row_waves;
-    const uint32_t rw = wave % row_waves, cw = wave / row_waves;
     const uint64_t c0 = (uint64_t)blockIdx.y * a.plan.part_chunks, all_chunks = (a.cols + kChunk - 1) / kChunk;
     const uint32_t chunks = (uint32_t)(all_chunks - c0 < a.plan.part_chunks ? all_chunks - c0 : a.plan.part_chunks);
     const uint32_t block_log2 = 31 - __builtin_clz(a.block);
 
-    const uint64_t first = a.row0 + ((uint64_t)blockIdx.x * row_waves + rw) * (16 * RT);
+    const uint64_t first = a.row0 + ((uint64_t)blockIdx.x * kWaves + wave) * (16 * RT);
     const uint8_t* row[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {                                // rows behind the last read the last one, and are not stored
@@ -346,46 +341,42 @@ __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) sum[r][t][i] = 0.f;
 
-    // A stage is a chunk for every wave beside another.  x goes through LDS, a stage ahead by way of registers, and codes are on their way two stages ahead.
-    // (Behind the end the last ones are read again: no branch, so that loads can be counted.)
-    const uint32_t record4 = record / 16, stage4 = col_waves * record4, half = col_waves * record;
-    const uint32_t whole = (uint32_t)(a.cols / kChunk > c0 ? a.cols / kChunk - c0 < chunks ? a.cols / kChunk - c0 : chunks : 0);      // chunks without a ragged end
-    const uint32_t stages = whole / col_waves, all4 = chunks * record4;   // in which every wave has a whole chunk; pieces of x in all
+    // x goes through LDS, a chunk ahead by way of registers, and codes are on their way two chunks ahead.  (Behind the end the last ones are read again: no
+    // branch, so that loads can be counted.)
+    const uint32_t whole = chunks - (c0 + chunks == all_chunks && a.cols % kChunk ? 1 : 0);    // without the ragged end
     const u32x4* x_from = reinterpret_cast<const u32x4*>(a.panel + c0 * record);
-    auto bring = [&](u32x4 (&v)[kPieces], uint32_t s) {
+    auto bring = [&](u32x4 (&v)[kPieces], uint32_t c) {
+        const u32x4* from = x_from + (uint64_t)(c < chunks ? c : chunks - 1) * kAll;
 #pragma unroll
-        for (uint32_t q = 0; q < kPieces; ++q) {
-            const uint32_t at = s * stage4 + q * kThreads + threadIdx.x;
-            v[q] = x_from[at < all4 ? at : all4 - 1];
-        }
+        for (uint32_t q = 0; q < kPieces; ++q) v[q] = from[q * kThreads + threadIdx.x < kAll ? q * kThreads + threadIdx.x : kAll - 1];
     };
-    auto put = [&](const u32x4 (&v)[kPieces], uint32_t s) {
+    auto put = [&](const u32x4 (&v)[kPieces], uint32_t c) {
 #pragma unroll
         for (uint32_t q = 0; q < kPieces; ++q)
-            if (q * kThreads + threadIdx.x < stage4) reinterpret_cast<u32x4*>(lds + (s & 1) * half)[q * kThreads + threadIdx.x] = v[q];
+            if (q * kThreads + threadIdx.x < kAll) reinterpret_cast<u32x4*>(lds + (c & 1) * record)[q * kThreads + threadIdx.x] = v[q];
     };
-    auto use = [&](const Codes<NARROW> (&c)[RT], uint32_t s) { multiply<T, TT, RT, NARROW>(c, lds + (s & 1) * half + cw * record, n, j, sum); };
+    auto use = [&](const Codes<NARROW> (&codes)[RT], uint32_t c) { multiply<T, TT, RT, NARROW>(codes, lds + (c & 1) * record, n, j, sum); };
     u32x4 x[kPieces];
     bring(x, 0);
-    if (stages) {
+    if (whole) {
         Codes<NARROW> ring[2][RT];
-        auto fetch = [&](Codes<NARROW> (&c)[RT], uint32_t s) {
-            const uint64_t col = (c0 + (s < stages ? s : stages - 1) * col_waves + cw) * kChunk;
+        auto fetch = [&](Codes<NARROW> (&codes)[RT], uint32_t c) {
+            const uint64_t col = (c0 + (c < whole ? c : whole - 1)) * kChunk;
 #pragma unroll
-            for (int r = 0; r < RT; ++r) load_codes<NARROW>(c[r], row[r], block_log2, col, j);
+            for (int r = 0; r < RT; ++r) load_codes<NARROW>(codes[r], row[r], block_log2, col, j);
         };
         fetch(ring[0], 0);
         fetch(ring[1], 1);
         put(x, 0);
         __syncthreads();
-        for (uint32_t s = 0; s < stages; s += 2) {
+        for (uint32_t c = 0; c < whole; c += 2) {
 #pragma unroll
             for (uint32_t o = 0; o < 2; ++o) {
-                if (s + o >= stages) break;
-                bring(x, s + o + 1);
-                use(ring[o], s + o);
-                fetch(ring[o], s + o + 2);
-                put(x, s + o + 1);
+                if (c + o >= whole) break;
+                bring(x, c + o + 1);
+                use(ring[o], c + o);
+                fetch(ring[o], c + o + 2);
+                put(x, c + o + 1);
                 __syncthreads();
             }
         }
@@ -393,35 +384,11 @@ __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
         put(x, 0);
         __syncthreads();
     }
-    if (const uint32_t chunk = stages * col_waves + cw; chunk < chunks) {          // (not of every wave)
-        Codes<NARROW> now[RT];
-        const uint64_t col = (c0 + chunk) * kChunk;
+    if (whole < chunks) {
+        Codes<NARROW> codes[RT];
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-            if (chunk < whole) load_codes<NARROW>(now[r], row[r], block_log2, col, j);
-            else load_codes_tail<NARROW>(now[r], row[r], block_log2, col, a.cols, j);
-        use(now, stages);
-    }
-
-    // the waves that split the columns: join in LDS
-    if (col_waves > 1) {
-        __syncthreads();
-        float* joined = reinterpret_cast<float*>(lds);            // [wave][tile of rows][tile of tokens][token][lane]
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int t = 0; t < TT; ++t)
-#pragma unroll
-                for (int i = 0; i < PER; ++i) joined[(((wave * RT + r) * TT + t) * PER + i) * 64 + lane] = sum[r][t][i];
-        __syncthreads();
-        if (cw != 0) return;
-        for (uint32_t c = 1; c < col_waves; ++c)
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int t = 0; t < TT; ++t)
-#pragma unroll
-                    for (int i = 0; i < PER; ++i) sum[r][t][i] += joined[((((c * row_waves + rw) * RT + r) * TT + t) * PER + i) * 64 + lane];
+        for (int r = 0; r < RT; ++r) load_codes_tail<NARROW>(codes[r], row[r], block_log2, (c0 + whole) * kChunk, a.cols, j);
+        use(codes, whole);
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -824,11 +791,10 @@ uint32_t split(uint64_t want, uint64_t groups, uint64_t most) {
 }
 
 template <typename T>
-ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens, bool narrow) {
+ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens) {
     ProductPlan p{};
     const int tiles = product_tiles<T>(tokens);
-    const uint64_t chunks = (cols + kChunk - 1) / kChunk, height = 16 * kRowTiles, row_tiles = (rows + height - 1) / height;
-    const uint32_t record = record_bytes<T>(tokens, narrow);
+    const uint64_t chunks = (cols + kChunk - 1) / kChunk;
     if (tiles <= 2) {
         // Two workgroups for every compute unit where each has four stages, otherwise one where it has any: 4 x 16384 x 4096, fp32, 2 parts (256 workgroups)
         // 17.6 us, 4: 16.2, 6: 16.8; 16 x 20000 x 4096, bf16, blocks of 64, 1 part (157) 26.0, 3: 24.0; 16 x 4096 x 4096 4 parts (128) 14.1, 8 (of two stages)
@@ -840,14 +806,11 @@ ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens, bool nar
         p.parts = (uint32_t)((stages + p.part_chunks - 1) / p.part_chunks);
         return p;
     }
-    // A workgroup reads all of x for the rows it has: not more bytes of it than of codes, as far as eight waves of rows go.
-    p.row_waves = 1;
-    while (p.row_waves < kWaves && (record > 64 * height * p.row_waves || row_tiles / (2 * p.row_waves) >= 512)) p.row_waves *= 2;
-    const uint64_t groups = (row_tiles + p.row_waves - 1) / p.row_waves, col_waves = kWaves / p.row_waves;
-    // Workgroups split the columns until all compute units have one, and not one more, which would take as long again, with four chunks for a wave: 61 x 16001 x
-    // 4099, bf16, 4 parts (252 workgroups) 46.3 us, 7 (441): 56.2; 64 x 65536 x 1024 1 part (256) 29.9, 2: 47.7; 20 x 1000 x 30000, fp16, 7 parts (224) 19.6,
-    // 3 (96): 23.0.
-    p.parts = split(256, groups, chunks / (4 * col_waves));
+    const uint64_t height = 16 * kRowTiles * kWaves, groups = (rows + height - 1) / height;
+    // Workgroups split the columns until all compute units have one, and not one more, which would take as long again or add to what is joined: 61 x 16001 x
+    // 4099, bf16, 4 parts (252 workgroups) 39.1 us, 8: 48.3; 64 x 65536 x 1024 1 part (256) 25.7, 2: 41.5; 64 x 2048 x 2048, fp32, 4 parts (of four chunks) 14.5,
+    // 16 (128 workgroups, a chunk each) 11.8; 30 x 300 x 1000, bf16, 2 parts 12.7, 8: 10.8.
+    p.parts = split(256, groups, chunks);
     p.part_chunks = (uint32_t)((chunks + p.parts - 1) / p.parts);
     p.parts = (uint32_t)((chunks + p.part_chunks - 1) / p.part_chunks);
     return p;
@@ -860,7 +823,7 @@ uint64_t panel_bytes(uint64_t cols, uint64_t tokens, bool narrow) {
 }
 template <typename T>
 uint64_t scratch_bytes(uint64_t rows, uint64_t cols, uint64_t tokens, bool narrow) {
-    const ProductPlan plan = product_plan<T>(rows, cols, tokens, narrow);
+    const ProductPlan plan = product_plan<T>(rows, cols, tokens);
     return panel_bytes<T>(cols, tokens, narrow) + (plan.parts > 1 ? plan.parts * tokens * rows * sizeof(float) : 0);
 }
 
@@ -887,11 +850,12 @@ void launch_product_kernels(ProductShape a, hipStream_t stream) {
     if constexpr (TT <= 2) {
         launch_product_tiles<T, TT, NARROW>(a, stream);
     } else {
-        const uint32_t tokens = (uint32_t)a.tokens, join = a.plan.row_waves == kWaves ? 0 : kThreads * kRowTiles * TT * (4 / Digits<T>::stride) * 4;
-        const uint32_t x = 2 * (kWaves / a.plan.row_waves) * Record<T, TT, NARROW>::bytes, lds = x > join ? x : join;
-        hipLaunchKernelGGL((product_digits_kernel<T, TT, NARROW>), dim3((unsigned)((a.cols + kChunk - 1) / kChunk), (tokens + 15) / 16), dim3(256), 0, stream, a, static_cast<uint8_t*>(a.work));
+        constexpr uint32_t lds = 2 * Record<T, TT, NARROW>::bytes;
+        static_assert(lds <= 64 * 1024, "what a launch may ask for");
+        hipLaunchKernelGGL((product_digits_kernel<T, TT, NARROW>), dim3((unsigned)((a.cols + kChunk - 1) / kChunk), (unsigned)(a.tokens + 15) / 16), dim3(256), 0, stream, a,
+                           static_cast<uint8_t*>(a.work));
         a.panel = static_cast<const uint8_t*>(a.work);
-        over_rows(a.rows, 16 * kRowTiles * a.plan.row_waves, [&](uint64_t row0, unsigned groups) {
+        over_rows(a.rows, 16 * kRowTiles * kWaves, [&](uint64_t row0, unsigned groups) {
             a.row0 = row0;
             hipLaunchKernelGGL((product_kernel<T, TT, NARROW>), dim3(groups, a.plan.parts), dim3(kThreads), lds, stream, a);
         });
@@ -933,7 +897,7 @@ void launch_product_of(const ProductArgs& args, hipStream_t stream) {
             else launch_product_one<T, 64>(a, stream);
             continue;
         }
-        a.plan = product_plan<T>(a.rows, a.cols, a.tokens, narrow);
+        a.plan = product_plan<T>(a.rows, a.cols, a.tokens);
         if (a.plan.parts > 1) a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(a.work) + panel_bytes<T>(a.cols, a.tokens, narrow));
         by_tiles<T>(product_tiles<T>(a.tokens), narrow, [&](auto t, auto n) { launch_product_kernels<T, decltype(t)::value, decltype(n)::value>(a, stream); });
         if (!a.partial) continue;
