@@ -802,6 +802,7 @@ ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens) {
         const uint64_t stages = (chunks + kStageChunks - 1) / kStageChunks, groups = (rows + 16 * kWaves - 1) / (16 * kWaves);
         p.parts = split(512, groups, stages);
         if (stages < 4 * p.parts) p.parts = split(256, groups, stages);
+        if (stages < 6) p.parts = 1;                              // (a stage takes 0.76 us where there are few workgroups, the launch that joins 2.6)
         p.part_chunks = (uint32_t)((stages + p.parts - 1) / p.parts);
         p.parts = (uint32_t)((stages + p.part_chunks - 1) / p.part_chunks);
         return p;
@@ -810,11 +811,14 @@ ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens) {
     // Workgroups split the columns until all compute units have one, and not one more, which would take as long again or add to what is joined: 61 x 16001 x
     // 4099, bf16, 4 parts (252 workgroups) 39.1 us, 8: 48.3; 64 x 65536 x 1024 1 part (256) 25.7, 2: 41.5; 64 x 2048 x 2048, fp32, 4 parts (of four chunks) 14.5,
     // 16 (128 workgroups, a chunk each) 11.8; 30 x 300 x 1000, bf16, 2 parts 12.7, 8: 10.8.
-    p.parts = split(256, groups, chunks);
+    p.parts = chunks < 4 ? 1 : split(256, groups, chunks);        // (a chunk takes a microsecond where there are few workgroups, the launch that joins 2.6)
     p.part_chunks = (uint32_t)((chunks + p.parts - 1) / p.parts);
     p.parts = (uint32_t)((chunks + p.part_chunks - 1) / p.part_chunks);
     return p;
 }
+
+// product_one_kernel's calls: a row has four words.
+bool by_rows(uint64_t tokens, uint64_t cols) { return tokens == 1 && cols > 24; }
 
 // Scratch: the panel (of product_kernel), then the partial sums.
 template <typename T>
@@ -823,6 +827,7 @@ uint64_t panel_bytes(uint64_t cols, uint64_t tokens, bool narrow) {
 }
 template <typename T>
 uint64_t scratch_bytes(uint64_t rows, uint64_t cols, uint64_t tokens, bool narrow) {
+    if (by_rows(tokens, cols)) return 0;
     const ProductPlan plan = product_plan<T>(rows, cols, tokens);
     return panel_bytes<T>(cols, tokens, narrow) + (plan.parts > 1 ? plan.parts * tokens * rows * sizeof(float) : 0);
 }
@@ -890,7 +895,7 @@ void launch_product_of(const ProductArgs& args, hipStream_t stream) {
         a.tokens = args.tokens - t0 < kTokens<T> ? args.tokens - t0 : kTokens<T>;
         a.in = static_cast<const T*>(args.in) + t0 * args.in_ld;
         a.out = static_cast<T*>(args.out) + t0 * args.out_ld;
-        if (a.tokens == 1 && a.cols > 24) {                         // (see the kernel)
+        if (by_rows(a.tokens, a.cols)) {
             if (a.cols <= 4 * kLaneCols) launch_product_one<T, 4>(a, stream);
             else if (a.cols <= 16 * kLaneCols) launch_product_one<T, 16>(a, stream);
             else if (a.cols <= 32 * kLaneCols) launch_product_one<T, 32>(a, stream);
