@@ -9,6 +9,7 @@ Tolerances.  U = 2^-24 is half a unit in the last place of fp32, in which sums a
 Then comes the rounding to the output's type (answers_plain.rounding).
 """
 import math
+import types
 
 import numpy as np
 import pytest
@@ -183,6 +184,38 @@ def test_products_of_no_tokens_and_refusals():
         assert e.value.status == b.DS_EINVAL
     with pytest.raises(b.DsqError, match="overlaps"):
         b.ds_product(msg, x, 2, 64, out=x[:, :2])
+
+
+def test_products_on_a_stream_of_another_device_are_refused():
+    msg, x = torch.zeros(2 * 36, dtype=torch.uint8, device="cuda"), torch.zeros((3, 64), device="cuda")
+    other = types.SimpleNamespace(device_index=torch.cuda.current_device() + 1, cuda_stream=0)
+    for call in (lambda: b.ds_product(msg, x, 2, 64, out=torch.zeros((3, 2), device="cuda"), stream=other),
+                 lambda: b.ds_product_gradient(msg, x[:, :2].contiguous(), 64, 64, out=torch.zeros((3, 64), device="cuda"), stream=other)):
+        with pytest.raises(b.DsqError, match="stream"):
+            call()
+
+
+@pytest.mark.parametrize("tokens,dtype", [(1, BF16), (12, F16), (40, BF16), (3, F32)])
+def test_products_past_four_gigabytes(tokens, dtype):
+    """All kernels, on a message of more than 2^32 bytes that is zero but for some rows."""
+    rows, cols, block = 160_000, 52_000, 128
+    per = plain.row_bytes(cols, block)
+    assert per * rows > 1 << 32
+    rng = np.random.default_rng(tokens)
+    some = [0, 1, 77_777, (1 << 32) // per - 1, (1 << 32) // per, (1 << 32) // per + 1, rows - 130, rows - 2, rows - 1]
+    part, codes, scales = plain.random_message(len(some), cols, block, rng)
+    msg = torch.zeros(rows * per, dtype=torch.uint8, device="cuda")
+    msg.view(rows, per)[some] = part.view(len(some), per).cuda()
+    m, unit = plain.dense(codes, scales, block), units(scales, block, cols)
+    x, dy = normal(rng, (tokens, cols), dtype), normal(rng, (tokens, rows), dtype)
+    y = b.ds_product(msg, x.cuda(), rows, block)
+    want = x.double() @ m.t().contiguous()
+    check(y[:, some], want, product_tolerance(want, x.double(), unit.t().contiguous(), dtype), "y")
+    y[:, some] = 0
+    assert not y.any(), "a row of scale 0 has a product"
+    dx = b.ds_product_gradient(msg, dy.cuda(), cols, block)
+    want = dy[:, some].double() @ m
+    check(dx, want, product_tolerance(want, dy[:, some].double(), unit, dtype), "dx")
 
 
 def test_product_reads_a_message_of_more_than_four_gigabytes():
