@@ -72,16 +72,18 @@ __device__ __forceinline__ float largest_of(const float (&z)[N]) {
 }
 // op over 2, 4, 8 or 16 adjacent lanes, or all 64, in all of them and in an order that is always the same: a lane with its neighbour, with the other two of
 // its four, with its mirror image in eight and in sixteen, and the four sixteens one after the other.
-template <int CTRL>
-__device__ __forceinline__ float other_lane(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true)); }
-template <int LANES, typename F>
-__device__ __forceinline__ float over_lanes(float v, F op) {
+template <int CTRL, typename V>
+__device__ __forceinline__ V other_lane(V v) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+template <int LANES, typename V, typename F>
+__device__ __forceinline__ V over_lanes(V v, F op) {
     if (LANES >= 2) v = op(v, other_lane<0xB1>(v));               // quad_perm 1 0 3 2
     if (LANES >= 4) v = op(v, other_lane<0x4E>(v));               // quad_perm 2 3 0 1
     if (LANES >= 8) v = op(v, other_lane<0x141>(v));              // row_half_mirror
     if (LANES >= 16) v = op(v, other_lane<0x140>(v));             // row_mirror
     if (LANES == 64) {
-        auto sixteen = [&](int of) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), of)); };
+        auto sixteen = [&](int of) { return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), of)); };
         v = op(op(sixteen(0), sixteen(16)), op(sixteen(32), sixteen(48)));
     }
     return v;

@@ -75,11 +75,10 @@ __device__ uint64_t kth_rank(TopLds<ROOM>& s, uint32_t n, uint32_t k) {
         some |= mine[q];
         all &= at < n ? mine[q] : ~0ull;
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        some |= __shfl_xor((unsigned long long)some, o);
-        all &= __shfl_xor((unsigned long long)all, o);
-    }
+    auto either = [](uint32_t a, uint32_t b) { return a | b; };
+    auto both = [](uint32_t a, uint32_t b) { return a & b; };
+    some = (uint64_t)over_lanes<64>((uint32_t)(some >> 32), either) << 32 | over_lanes<64>((uint32_t)some, either);
+    all = (uint64_t)over_lanes<64>((uint32_t)(all >> 32), both) << 32 | over_lanes<64>((uint32_t)all, both);
     if (lane == 0) {
         s.edges[0][wave] = some;
         s.edges[1][wave] = all;
