@@ -313,6 +313,8 @@ __device__ __forceinline__ void multiply(const Codes<NARROW> (&c)[RT], uint8_t* 
     }
 }
 
+// More tokens: a workgroup takes 256 rows, chunk after chunk, its waves 32 rows each against the same x in LDS.  61 x 16001 x 4099, bf16, in blocks of 64: 30 us;
+// for every token, row and block four vector instructions, 45 % of the clocks, and the matrix instructions 15 %.
 template <typename T, int TT, bool NARROW>
 __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
     constexpr int RT = kRowTiles;
@@ -564,7 +566,8 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
 // One token: rows of codes are read whole, which costs the memory pipeline a third of what sixteen rows of 64 bytes cost a load, and meet x in
 // registers.  A lane keeps 32 columns of x for all the rows of its wave, G lanes hold a row, and a load takes 64 / G rows of 32 G columns.  x is
 // written in digits of four bits here, 16^d apart, 4 of them (6 for fp32), with an exponent per 32 columns: eight codes (less 8, so that they are
-// signed) meet eight digits in one instruction, 0.6 instructions a weight.  The lanes of a row are joined by a tree of lane shifts.
+// signed) meet eight digits in one instruction, 0.6 instructions a weight.  The lanes of a row are joined by a tree of lane shifts.  65536 x 4096: 24.6 us,
+// 5.8 TB/s, the vector units busy 67 % of the time.
 constexpr uint32_t kLaneCols = 32;
 template <typename T>
 struct Nibbles {
