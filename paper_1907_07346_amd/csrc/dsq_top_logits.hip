@@ -10,9 +10,9 @@
 // (1 x 1000000, k = 100, fp32: 33.8 us; 72 where lists came one after the other).  Those two launches are mostly waiting: 1 x 131072, k = 64, bf16, 6.0 + 8.6 us,
 // where an empty launch takes 2; what the first finds is some 1500 candidates, and the second's time is three reads of memory, one behind the other, one
 // histogram and the ranks in one of its bins.
-//   Many rows are bound by reading the logits once: 2048 x 65536, fp32, k = 128, 124 us, 4.3 TB/s, with the
-// vector units busy nearly half the time.
+//   Many rows: 2048 x 65536, fp32, k = 128, 110 us, 4.9 TB/s, with the vector units busy half the time; a row is a workgroup's, and 1000 rows take 58.
 #include "dsq_answers.h"
+#include "dsq_codes.h"
 #include "dsq_logits.h"
 
 namespace dsq {
@@ -187,6 +187,7 @@ __global__ void __launch_bounds__(kThreads, 4) top_logits_kernel(TopShape a) {
     constexpr uint32_t E = Pieces<T>::E, kStretch = kThreads * kPieces * E;
     using Piece = typename Pieces<T>::Piece;
     __shared__ TopLds<kRoom> s;
+    __shared__ u32x4 pieces[kPieces][kThreads];                   // of the thread: those with candidates
     const uint64_t row = a.row0 + blockIdx.x;
     const uint32_t k = a.k, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
     const T* z = static_cast<const T*>(a.z) + row * a.z_ld;
@@ -248,20 +249,36 @@ __global__ void __launch_bounds__(kThreads, 4) top_logits_kernel(TopShape a) {
             if (!(most[p] < bar_value))
 #pragma unroll
                 for (uint32_t e = 0; e < E; ++e) passed |= v[p][e] < bar_value ? 0u : 1u << (p * E + e);
-        while (passed) {                                          // few: their logits are read once more
+        // few: their pieces go into LDS, where a logit has an address (read from memory once more: 2048 x 65536, fp32, k = 128, 126 us, 113 so)
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p)
+            if (!(most[p] < bar_value)) pieces[p][threadIdx.x] = __builtin_bit_cast(u32x4, raw[p]);
+        while (passed) {
             const uint32_t bit = __builtin_ctz(passed);
             passed &= passed - 1;
             const uint64_t column = at + ((uint64_t)(bit / E) * kThreads + threadIdx.x) * E + bit % E;
             if (column >= end) continue;
-            const uint64_t rank = logit_rank((float)z[column], (uint32_t)column);
+            const uint64_t rank = logit_rank((float)reinterpret_cast<const T*>(&pieces[bit / E][threadIdx.x])[bit % E], (uint32_t)column);
             if (rank <= bar) continue;
             const uint32_t place = atomicAdd(&s.count, 1u);
             if (place < kRoom) s.list[place] = rank;
         }
     };
+    // fp32 has registers for the next stretch's logits on their way meanwhile: 1000 x 65536, k = 128, 57.6 us, 59.8 without; dtypes of 16 bits, whose stretches
+    // are twice as many numbers, have not: 300 x 50000, k = 100, fp16, 20.3 without, 23.5 with them.
+    constexpr bool kAhead = sizeof(T) == 4;
+    Piece coming[kPieces];
+    if (kAhead) fetch(coming, begin);
     for (uint64_t at = begin; at < end; at += kStretch) {
         Piece raw[kPieces];
-        fetch(raw, at);
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) raw[p] = coming[p];
+            if (at + kStretch < end) fetch(coming, at + kStretch);
+            __builtin_amdgcn_sched_barrier(0);
+        } else {
+            fetch(raw, at);
+        }
         go_through(raw, at, at == begin);
         __syncthreads();
         const uint32_t count = s.count;
