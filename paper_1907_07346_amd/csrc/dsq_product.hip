@@ -16,6 +16,7 @@
 //   Where there are too few rows for the GPU, workgroups split the columns, too, and one more launch adds their sums.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
+#include "dsq_message_reads.h"
 
 namespace dsq {
 namespace {
@@ -607,7 +608,7 @@ __global__ void __launch_bounds__(kThreads) product_one_kernel(ProductShape a) {
     const uint32_t row_waves = a.plan.row_waves, col_waves = kWaves / row_waves, rw = wave % row_waves, cw = wave / row_waves;
     const uint32_t wave_rows = a.plan.wave_rows, rows_here = row_waves * wave_rows, loads = wave_rows / AT_ONCE;
     const uint64_t first = a.row0 + (uint64_t)blockIdx.x * rows_here;
-    const uint32_t block_log2 = 31 - __builtin_clz(a.block), pitch = 4 + a.block / 2;
+    const uint32_t block_log2 = 31 - __builtin_clz(a.block);
     const uint32_t lanes = col_waves * G;                         // lanes that hold different columns ...
     i32x4* digits = reinterpret_cast<i32x4*>(lds);                // ... and their digits, [digit][lane]; then sum v and what v counts
     int32_t* sums = reinterpret_cast<int32_t*>(digits + D::digits * lanes);
@@ -617,13 +618,8 @@ __global__ void __launch_bounds__(kThreads) product_one_kernel(ProductShape a) {
     const T* x = static_cast<const T*>(a.in);
     for (uint64_t slice = 0; slice < a.cols; slice += lanes * kLaneCols) {
         const uint64_t col = slice + (cw * G + l) * kLaneCols;
-        // Lanes behind the last column read words of the first, and count for nothing.  The last lane with columns may have fewer than four
-        // words: it reads the four that end with the row instead, and has digits for its own.  (A row has four: cols > 24.)
-        const bool some = col < a.cols;
-        const uint64_t from_col = some ? col : slice;
-        auto missing_words = [&](uint64_t c) { return c < a.cols && c + 24 >= a.cols ? 4 - (uint32_t)((a.cols - c + 7) / 8) : 0u; };
-        const uint64_t scale_at = (from_col >> block_log2) * pitch;
-        const uint64_t codes_at = scale_at + 4 + (from_col & (a.block - 1)) / 2 - 4 * missing_words(col);
+        const bool some = col < a.cols;                           // (if not, the lane counts for nothing)
+        const LaneRead read = lane_read(col, a.cols, block_log2);
         struct Load {
             u32x4 w;
             float scale;
@@ -631,8 +627,8 @@ __global__ void __launch_bounds__(kThreads) product_one_kernel(ProductShape a) {
         auto fetch = [&](Load& v, uint32_t q) {                   // the q-th rows, or again the last: no branch, so that loads can be counted
             const uint64_t at = first + rw * wave_rows + (q < loads ? q : loads - 1) * AT_ONCE + g, row = at < a.rows ? at : a.rows - 1;
             const uint8_t* p = a.msg + row * a.row_bytes;
-            v.scale = *reinterpret_cast<const float*>(p + scale_at);
-            v.w = *reinterpret_cast<const u32x4_at4*>(p + codes_at);
+            v.scale = *reinterpret_cast<const float*>(p + read.scale);
+            v.w = *reinterpret_cast<const u32x4_at4*>(p + read.codes);
         };
         Load ring[AHEAD];
 #pragma unroll
@@ -681,7 +677,7 @@ __global__ void __launch_bounds__(kThreads) product_one_kernel(ProductShape a) {
                     out[d] |= ((uint32_t)digit & 15u) << (4 * e);
                 }
             }
-            const uint32_t place = (w % 4 + missing_words(slice + w / 4 * kLaneCols)) % 4;
+            const uint32_t place = (w % 4 + missing_words(slice + w / 4 * kLaneCols, a.cols)) % 4;
 #pragma unroll
             for (int d = 0; d < D::digits; ++d) reinterpret_cast<uint32_t*>(digits + d * lanes + w / 4)[place] = out[d];
 #pragma unroll
