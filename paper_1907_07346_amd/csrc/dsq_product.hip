@@ -416,7 +416,8 @@ __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
 //   2 tokens of 65536 x 4096 read 4.2 TB/s.  16 tokens cost some 340 instructions a stage, 5400 clocks for the two workgroups of a compute unit, in which it
 // could read 44 KB and reads 32: x's digits are a third of them; 44.2 us, and 2.3 TB/s for 16 x 4096 x 16384, whose workgroups have four stages each.
 // Slower: two stages ahead (registers; 16 x 4096 x 16384 22.8 us), workgroups of 256 rows (2 x 65536 x 4096 46.8 : 42.9).
-constexpr uint32_t kStageChunks = 2, kStageCols = kStageChunks * kChunk, kRowPieces = 9;   // of a stage; 16-byte pieces of a row at most
+constexpr uint32_t kStageChunks = 2, kStageCols = kStageChunks * kChunk;                   // of a stage
+static_assert(kStageCols == kStageColumns);
 
 template <typename T, int TT, bool NARROW>
 struct Stage {
@@ -442,8 +443,8 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
     const uint64_t first = a.row0 + (uint64_t)blockIdx.x * S::rows;
 
     // what the thread brings: two pieces of codes (some a third), a long block's scale, and x
-    const bool apart = a.block > kStageCols;                      // scales are
-    const uint32_t row_pieces = apart ? kRowPieces - 1 : kRowPieces, row_bytes = (uint32_t)a.row_bytes;    // (below 2^28)
+    const bool apart = scales_apart(block_log2);
+    const uint32_t row_pieces = stage_pieces(block_log2), row_bytes = (uint32_t)a.row_bytes;    // (below 2^28)
     auto row_at = [&](uint32_t r) { return a.msg + (first + r < a.rows ? first + r : a.rows - 1) * a.row_bytes; };
     constexpr uint32_t PIECES = (S::rows * kRowPieces + kThreads - 1) / kThreads;
     const uint8_t* from[PIECES];
@@ -467,16 +468,14 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
         uint32_t back;                                            // words that a piece which would end behind the message was read too early by
     };
     auto bring = [&](Brought& v, uint32_t s) {
-        const uint32_t col = (s0 + s) * kStageCols, in_block = col & (a.block - 1), block_at = (col >> block_log2) * pitch;
-        const uint32_t at = apart ? block_at + 4 + in_block / 2 : block_at;
+        const uint32_t col = (s0 + s) * kStageCols, in_block = col & (a.block - 1), block_at = stage_scale(col, block_log2), at = stage_codes(col, block_log2);
         v.back = 0;
         if (col + kStageCols <= cols) {                           // all blocks are there, and a last piece may end in the next row ...
             if (has_end && at + row_pieces * 16 > row_bytes) {    // ... if there is one
-                v.back = (at + row_pieces * 16 - row_bytes) / 4;
+                v.back = words_back(at, row_pieces, row_bytes);
 #pragma unroll
                 for (uint32_t i = 0; i < PIECES; ++i) {
-                    const uint32_t piece = at + piece_at[i];
-                    if (i + 1 < PIECES || has_third) v.codes[i] = *reinterpret_cast<const u32x4_at4*>(from[i] + (piece + 16 <= row_bytes ? piece : row_bytes - 16));
+                    if (i + 1 < PIECES || has_third) v.codes[i] = *reinterpret_cast<const u32x4_at4*>(from[i] + piece_read(at + piece_at[i], row_bytes));
                 }
             } else {
 #pragma unroll
@@ -498,10 +497,14 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
         if (has_scale && (in_block == 0 || s == 0)) v.scale = *reinterpret_cast<const float*>(scale_row + block_at);
     };
     auto put = [&](Brought& v, uint8_t* to) {
-        if (v.back)                                               // (2 or 3, with blocks of 128 or 256)
+        if (v.back)
 #pragma unroll
             for (uint32_t i = 0; i < PIECES; ++i)
-                if (piece_at[i] == (kRowPieces - 1) * 16) v.codes[i].xy = v.back == 2 ? v.codes[i].zw : v.codes[i].ww;
+                if (piece_at[i] == (kRowPieces - 1) * 16) {
+                    const Front front = moved_to_front(v.back, v.codes[i].y, v.codes[i].z, v.codes[i].w);
+                    v.codes[i].x = front.x;
+                    v.codes[i].y = front.y;
+                }
 #pragma unroll
         for (uint32_t i = 0; i < PIECES; ++i)
             if (i + 1 < PIECES || has_third) *reinterpret_cast<u32x4*>(to + piece_to[i]) = v.codes[i];

@@ -39,6 +39,34 @@ void one_token(uint64_t cols, uint32_t block_log2, uint64_t lanes) {
         }
 }
 
+// Few tokens: all whole stages of one of the matrix's last rows, or (inner) of another, whose last piece may end in the next row.
+void few_tokens(uint64_t cols, uint32_t block_log2, bool inner) {
+    const uint32_t block = 1u << block_log2, end = (uint32_t)row_bytes(cols, block), pieces = dsq::stage_pieces(block_log2);
+    const uint32_t readable = inner ? 2 * end : end;
+    for (uint32_t col = 0; col + dsq::kStageColumns <= cols; col += dsq::kStageColumns) {
+        const uint32_t at = dsq::stage_codes(col, block_log2), scale = dsq::stage_scale(col, block_log2);
+        if (scale != col / block * (4 + block / 2) || scale + 4 > end) fail("a stage's scale", cols, block, col);
+        const uint32_t back = inner ? 0 : dsq::words_back(at, pieces, end);
+        uint32_t words[4 * dsq::kRowPieces];                      // the bytes' offsets in the row that the stage's words came from
+        for (uint32_t p = 0; p < pieces; ++p) {
+            const uint32_t from = inner ? at + 16 * p : dsq::piece_read(at + 16 * p, end);
+            if (from + 16 > readable) fail("a piece behind the row", cols, block, col);
+            for (uint32_t w = 0; w < 4; ++w) words[4 * p + w] = from + 4 * w;
+            if (back && p == dsq::kRowPieces - 1) {
+                const dsq::Front f = dsq::moved_to_front(back, words[4 * p + 1], words[4 * p + 2], words[4 * p + 3]);
+                words[4 * p] = f.x;
+                words[4 * p + 1] = f.y;
+            }
+        }
+        // where the kernel looks: scales and codes of blocks of at most 256 columns one behind the other, of longer ones codes alone
+        for (uint32_t c = col; c < col + dsq::kStageColumns; c += 8) {
+            const uint32_t in = c - col, word = dsq::scales_apart(block_log2) ? in / 8 : in / block * (1 + block / 8) + 1 + in % block / 8;
+            if (words[word] != word_of(c, block)) fail("a stage's word", cols, block, c);
+            if (!dsq::scales_apart(block_log2) && words[in / block * (1 + block / 8)] != c / block * (4 + block / 2)) fail("a block's scale", cols, block, c);
+        }
+    }
+}
+
 }  // namespace
 
 int main() {
@@ -47,6 +75,10 @@ int main() {
             for (uint64_t cols = 25; cols < 2200; ++cols) one_token(cols, block_log2, lanes);
             for (uint64_t slices = 1; slices <= 3; ++slices)      // around the ends of slices
                 for (int off = -70; off <= 70; ++off) one_token(512 * 32 * slices + off, block_log2, lanes);
+        }
+        for (uint64_t cols = 256; cols < 5000; ++cols) {
+            few_tokens(cols, block_log2, false);
+            few_tokens(cols, block_log2, true);
         }
     }
     if (!failures) std::printf("message reads ok\n");
