@@ -399,7 +399,7 @@ typedef struct {
     uint64_t vocab;           /* logits per row, 1 <= vocab < 2^31                               */
     int32_t  k;               /* pairs per row, 1 <= k <= 256 (ds_top_logits: and k <= vocab)    */
     int32_t  dtype;           /* ds_dtype of the logits and of their gradient                    */
-    float    temperature;     /* logits are divided by it; finite, > 0                           */
+    float    temperature;     /* logits are divided by it; finite, > 0, not subnormal            */
     int32_t  reserved;        /* must be 0                                                       */
 } ds_logits;
 

@@ -1,4 +1,5 @@
 // Entry points of the operators on messages and logits: checks of what the caller gives.  No allocation, no exception.
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -52,7 +53,7 @@ const char* logits_fault(const ds_logits* l) {
     if (l->vocab < 1 || l->vocab >= kMost) return "vocab must be at least 1 and below 2^31";
     if (l->k < 1 || l->k > dsq::kMaxTop) return "k must be between 1 and 256";
     if (!known(l->dtype)) return "unknown dtype";
-    if (!std::isfinite(l->temperature) || !(l->temperature > 0.f)) return "temperature must be finite and positive";
+    if (!std::isfinite(l->temperature) || !(l->temperature >= FLT_MIN)) return "temperature must be finite and positive, and no subnormal number";
     if (l->reserved != 0) return "reserved must be 0";
     return nullptr;
 }

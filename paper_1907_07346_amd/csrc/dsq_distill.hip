@@ -58,7 +58,7 @@ __device__ Teacher read_teacher(const LogitsArgs& a, uint64_t row, uint2 pair, f
     if (a.teacher_lse) {
         e.log_p = logit / a.temperature - a.teacher_lse[row];
     } else {
-        const Spread s = workgroup_spread<WAVES>(e.listed ? spread_of(logit) : kNoSpread, scale, sums);
+        const Spread s = workgroup_spread<WAVES>(e.listed ? spread_of(logit, scale) : kNoSpread, scale, sums);
         const LogSum l = log_sum(s, scale);
         e.log_p = (logit - l.from) / a.temperature - l.rest;
     }
@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(THREADS) distill_row_kernel(DistillShape a) {
         T* dz = a.dz ? static_cast<T*>(a.dz) + row * a.dz_ld : nullptr;
         const uint64_t next = row + gridDim.x;
         const float next_weight = next < end ? weight_of(next) : 0.f;
-        Gradient g{{0.f, 0.f}, 0.f, 0.f};
+        Gradient g{{0.f, 0.f, false}, 0.f, 0.f};
         bool skip = weight == 0.f;                                // a padded token: its logits are not read
         Teacher teacher{};
         if (!skip) {
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(THREADS) distill_row_kernel(DistillShape a) {
                 }
                 add_logits(s, v, largest_of(most), scale);
             }
-            s = join(s, spread_of(last), scale);
+            s = join(s, spread_of(last, scale), scale);
             s = workgroup_spread<WAVES>(s, scale, sums);
             const LogSum l = log_sum(s, scale);
             if (a.loss) {
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kPartThreads) distill_part_kernel(DistillShape
     const float2 of_part = threadIdx.x < a.parts ? a.spreads[row * a.parts + threadIdx.x] : make_float2(-kInf, 0.f);   // (parts <= 256)
     bool skip = weight == 0.f;
     Teacher teacher{};
-    Gradient g{{0.f, 0.f}, 0.f, 0.f};
+    Gradient g{{0.f, 0.f, false}, 0.f, 0.f};
     if (!skip) {
         teacher = read_teacher<kPartWaves>(a, row, pair, z_pair, scale, sums);
         keep_listed(teacher, a.k, listed);

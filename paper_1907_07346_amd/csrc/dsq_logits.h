@@ -31,32 +31,41 @@ struct Spread {
     float max, sum;
 };
 constexpr Spread kNoSpread{-kInf, 0.f};
-// What exponents are made with.  Where the largest is infinite they count from 0: a row of minus infinities has sum 0, one with plus infinity an infinite
-// sum.  Where the largest is finite but not with the factor, numbers lie so far apart that only those equal to it count, with any factor.
+// What exponents are made with.  The rounding of `at` makes the largest's own term 2^-64 to 2^64 as long as |at| < 2^31.  From there on neighbours in fp32 are
+// 64 or more apart in the exponent, so that only what equals the largest counts (2^31 others add 2^-33 of it): any factor that tells them apart will do, and
+// a power of two makes its term 1.  Where the largest is infinite exponents count from 0: a row of minus infinities has sum 0, one with plus infinity an
+// infinite sum.
 struct Exponents {
     float scale, at;
+    bool alone;                                                   // only what equals the largest counts
     __device__ float operator()(float z) const { return power2(fmaf(z, scale, -at)); }
 };
 __device__ __forceinline__ Exponents exponents(float max, float scale) {
     const float at = max * scale;
-    if (fabsf(at) != kInf) return {scale, at};
-    if (fabsf(max) == kInf) return {scale, 0.f};
-    return {1.f, max};
+    if (!(fabsf(at) >= 2147483648.f)) return {scale, at, false};  // (and NaN)
+    if (fabsf(max) == kInf) return {scale, 0.f, false};
+    const uint32_t up = 380u - (__float_as_uint(max) >> 23 & 255u);                        // |max| times it lies between 2^126 and 2^127
+    const float apart = __uint_as_float((up < 254u ? up : 254u) << 23);
+    return {apart, max * apart, true};
 }
-__device__ __forceinline__ Spread spread_of(float z) { return {z, z == -kInf ? 0.f : z == kInf ? z : z == z ? 1.f : z}; }
+__device__ __forceinline__ Spread spread_of(float z, float scale) { return {z, exponents(z, scale)(z)}; }
+// The sum of s when it counts from e, the exponents of `max`, which is at least s.max.  (Exponents of another kind than e's are never subtracted from its.)
+__device__ __forceinline__ float sum_from(Spread s, float max, Exponents e, float scale) {
+    if (s.sum == 0.f || s.max == max) return s.sum;               // (an empty or all-masked side counts from 0, which may lie far above)
+    const Exponents own = exponents(s.max, scale);
+    return own.alone || e.alone ? 0.f : s.sum * power2(own.at - e.at);
+}
 __device__ __forceinline__ Spread join(Spread a, Spread b, float scale) {
-    const float m = max_or_nan(a.max, b.max), at = exponents(m, scale).at;
-    // (An empty or all-masked side has sum 0 and counts from 0, which may lie far above the other's largest.)
-    const float sa = a.sum == 0.f ? 0.f : a.sum * power2(exponents(a.max, scale).at - at);
-    const float sb = b.sum == 0.f ? 0.f : b.sum * power2(exponents(b.max, scale).at - at);
-    return {m, sa + sb};
+    const float m = max_or_nan(a.max, b.max);
+    const Exponents e = exponents(m, scale);
+    return {m, sum_from(a, m, e, scale) + sum_from(b, m, e, scale)};
 }
 // Adds M times N logits whose largest is `most` (-inf counts for nothing).
 template <int M, int N>
 __device__ __forceinline__ void add_logits(Spread& s, const float (&z)[M][N], float most, float scale) {
     const float m = max_or_nan(s.max, most);
     const Exponents e = exponents(m, scale);
-    float total = s.sum == 0.f ? 0.f : s.sum * power2(exponents(s.max, scale).at - e.at);
+    float total = sum_from(s, m, e, scale);
 #pragma unroll
     for (int i = 0; i < M; ++i)
 #pragma unroll
@@ -97,7 +106,7 @@ __device__ __forceinline__ float total_over_lanes(float v) {
 template <int LANES>
 __device__ __forceinline__ Spread spread_over_lanes(Spread s, float scale) {
     const float m = over_lanes<LANES>(s.max, [](float a, float b) { return max_or_nan(a, b); });
-    return {m, total_over_lanes<LANES>(s.sum == 0.f ? 0.f : s.sum * power2(exponents(s.max, scale).at - exponents(m, scale).at))};
+    return {m, total_over_lanes<LANES>(sum_from(s, m, exponents(m, scale), scale))};
 }
 // Joins the spreads of a workgroup's WAVES * 64 threads; every thread gets the result.  sums: 2 * WAVES floats of LDS.
 template <int WAVES>

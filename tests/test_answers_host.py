@@ -154,3 +154,11 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
                  lambda: b.ds_top_logits(x, 4), lambda: b.ds_distill(x, pairs)):
         with pytest.raises(b.DsqError, match="current CUDA device"):
             call()
+
+
+def test_subnormal_temperatures_are_refused():
+    """log2(e) over one of them is no fp32 number."""
+    for call in (top, distill):
+        st, msg = call(logits(temperature=1e-39))
+        assert st == b.DS_EINVAL and "temperature" in msg, msg
+        assert b.lib().ds_distill_work_bytes(ctypes.byref(logits(vocab=1 << 20, temperature=1e-39))) == 0
