@@ -16,7 +16,7 @@ import torch  # noqa: F401  (must be loaded before libdsq.so: one HIP runtime pe
 
 from .detgen import GRAD_KINDS
 from .workloads import (KIND_IDENTITY, KIND_QUANT_MAXABS, KIND_SIGN_MEANABS, KIND_TOPK, KIND_QUANT_L2NORM, KIND_RAND_SPARSE, KIND_GSPAR,  # noqa: F401
-                        TOPO_CSR, TOPO_RING, TOPO_TORUS2D, Config)
+                        ALGO_DEEPSQUEEZE, TOPO_CSR, TOPO_RING, TOPO_TORUS2D, Config)
 
 DS_OK, DS_EINVAL, DS_ENOMEM, DS_EHIP, DS_ESTATE = range(5)
 _STATUS = {0: "DS_OK", 1: "DS_EINVAL", 2: "DS_ENOMEM", 3: "DS_EHIP", 4: "DS_ESTATE"}
@@ -475,7 +475,7 @@ class DeepSqueeze:
     def ds_product(self, worker: int, x: "torch.Tensor", rows: int, first: int = 0, out: "Optional[torch.Tensor]" = None,
                    stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
         """x (tokens, cols) through parameters first .. first + rows * cols - 1 of `worker` as the message of the last ds_step holds
-        them (4-bit QUANT_MAXABS; first and cols multiples of the block).  Some launch plans alternate between two message buffers:
+        them (4-bit QUANT_MAXABS and DeepSqueeze's own update, whose messages are parameters; first and cols multiples of the block).  Some launch plans alternate between two message buffers:
         the call then waits for the last ds_step (see ds_message_ptr)."""
         return ds_product(self._matrix("ds_product", worker, rows, x.shape[-1], first), x, rows, self.cfg.comp.block, out, stream)
 
@@ -488,6 +488,8 @@ class DeepSqueeze:
         comp = self.cfg.comp
         if comp.kind != KIND_QUANT_MAXABS or comp.bits != 4:
             _refuse(name, "messages of the 4-bit block quantiser only")
+        if self.cfg.algo != ALGO_DEEPSQUEEZE:
+            _refuse(name, "the messages of DCD-PSGD and CHOCO-SGD are differences, no parameters")
         if not self._stepped:
             raise DsqError(DS_ESTATE, name, "no step has been taken yet")
         if not 0 <= worker < self.n:
