@@ -425,8 +425,9 @@ class DeepSqueeze:
         self._stepped = True
 
     def ds_step_raw(self, g_ptr: int, g_ld: int, stream_ptr: int = 0) -> int:
-        self._stepped = True
-        return lib().ds_step(self._h, g_ptr, g_ld, stream_ptr)
+        st = lib().ds_step(self._h, g_ptr, g_ld, stream_ptr)
+        self._stepped = self._stepped or st == DS_OK
+        return st
 
     def ds_set_mixing(self, W_csr):
         """W_csr = (rowptr int32, col int32, val float32): the mixing matrix for the following steps."""

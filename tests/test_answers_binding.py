@@ -1,4 +1,6 @@
 """What the binding of the operators on messages refuses before it asks the library: no GPU, no handle."""
+import types
+
 import pytest
 import torch
 
@@ -21,3 +23,14 @@ def test_messages_that_are_differences_are_no_matrix(algo):
         with pytest.raises(b.DsqError, match="differences") as e:
             call()
         assert e.value.status == b.DS_EINVAL
+
+
+def test_a_first_step_that_fails_leaves_no_message(monkeypatch):
+    ds, answers = handle(stepped=False), iter([b.DS_EHIP, b.DS_EINVAL, b.DS_OK, b.DS_EHIP])
+    monkeypatch.setattr(b, "lib", lambda: types.SimpleNamespace(ds_step=lambda *a: next(answers)))
+    for status, there in ((b.DS_EHIP, False), (b.DS_EINVAL, False), (b.DS_OK, True), (b.DS_EHIP, True)):
+        assert ds.ds_step_raw(0, 640) == status and ds._stepped is there
+        if not there:
+            with pytest.raises(b.DsqError) as e:
+                ds.ds_product(0, torch.zeros((1, 64)), 2)
+            assert e.value.status == b.DS_ESTATE
