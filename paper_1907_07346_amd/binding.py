@@ -303,6 +303,8 @@ def ds_matrix_bytes(rows: int, cols: int, block: int) -> int:
 def _through(name: str, work_bytes, call, msg: "torch.Tensor", x: "torch.Tensor", rows: int, cols: int, width: int, out_width: int, block: int,
              out: "Optional[torch.Tensor]", stream: Optional["torch.cuda.Stream"]):
     tokens, got, pitch = _rows_of(name, "the input", x)
+    if x.requires_grad and torch.is_grad_enabled():
+        _refuse(name, "the result would carry no graph: detach the input, and call ds_product_gradient for the way back")
     if got != width:
         _refuse(name, f"the input must have {width} columns")
     m = ctypes.byref(ds_matrix(rows, cols, tokens, block, _DTYPES[x.dtype]))
@@ -323,20 +325,22 @@ def _through(name: str, work_bytes, call, msg: "torch.Tensor", x: "torch.Tensor"
 
 def ds_product(msg: "torch.Tensor", x: "torch.Tensor", rows: int, block: int, out: "Optional[torch.Tensor]" = None,
                stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
-    """x (tokens, cols) through the matrix of `rows` rows held as 4-bit messages in msg (uint8): (tokens, rows) of x's dtype."""
+    """x (tokens, cols) through the matrix of `rows` rows held as 4-bit messages in msg (uint8): (tokens, rows) of x's dtype.  Autograd
+    does not record the call: an x that requires a gradient is refused where gradients are recorded."""
     L, cols = lib(), x.shape[-1]
     return _through("ds_product", L.ds_product_work_bytes, L.ds_product, msg, x, rows, cols, cols, rows, block, out, stream)
 
 
 def ds_product_gradient(msg: "torch.Tensor", dy: "torch.Tensor", cols: int, block: int, out: "Optional[torch.Tensor]" = None,
                         stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
-    """The gradient of ds_product with respect to x: dy (tokens, rows) gives (tokens, cols) of dy's dtype."""
+    """The gradient of ds_product with respect to x: dy (tokens, rows) gives (tokens, cols) of dy's dtype.  Not recorded either."""
     L, rows = lib(), dy.shape[-1]
     return _through("ds_product_gradient", L.ds_product_gradient_work_bytes, L.ds_product_gradient, msg, dy, rows, cols, rows, cols, block, out, stream)
 
 
 def ds_top_logits(z: "torch.Tensor", k: int, temperature: float = 1.0, stream: Optional["torch.cuda.Stream"] = None):
-    """The k largest logits of each row of z: (pairs, lse), pairs int32 (rows, k, 2) of index and float32 bits, ascending index."""
+    """The k largest logits of each row of z: (pairs, lse), pairs int32 (rows, k, 2) of index and float32 bits, ascending index.  They are
+    what a teacher sends, numbers without a graph."""
     rows, vocab, pitch = _rows_of("ds_top_logits", "z", z)
     here = _on_device("ds_top_logits", "z", z)
     if not 1 <= k <= 256:
@@ -354,7 +358,8 @@ def ds_distill(z: "torch.Tensor", pairs: "torch.Tensor", temperature: float = 1.
                weight: "Optional[torch.Tensor]" = None, want_loss: bool = True, want_gradient: bool = True,
                dz: "Optional[torch.Tensor]" = None, stream: Optional["torch.cuda.Stream"] = None):
     """The loss of each row of z against the teacher's pairs (as ds_top_logits gives them) and its gradient: (loss, dz), None for
-    what is not wanted.  dz may be given, also as z itself."""
+    what is not wanted.  dz may be given, also as z itself.  The gradient is dz and nothing else: the loss is a number without a graph,
+    and a z that has one goes on with z.backward(dz)."""
     rows, vocab, pitch = _rows_of("ds_distill", "z", z)
     if pairs.dtype != torch.int32 or pairs.dim() != 3 or pairs.shape[0] != rows or pairs.shape[2] != 2 or not pairs.is_contiguous():
         _refuse("ds_distill", f"pairs must be a contiguous int32 tensor ({rows}, k, 2)")

@@ -34,3 +34,17 @@ def test_a_first_step_that_fails_leaves_no_message(monkeypatch):
             with pytest.raises(b.DsqError) as e:
                 ds.ds_product(0, torch.zeros((1, 64)), 2)
             assert e.value.status == b.DS_ESTATE
+
+
+def test_products_that_would_drop_a_gradient_are_refused(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    msg, leaf = torch.zeros(2 * 36, dtype=torch.uint8), torch.zeros((3, 64), requires_grad=True)
+    for x in (leaf, leaf * 2):
+        for call in (lambda: b.ds_product(msg, x, 2, 64), lambda: b.ds_product_gradient(msg, x[:, :2], 64, 64)):
+            with pytest.raises(b.DsqError, match="graph") as e:
+                call()
+            assert e.value.status == b.DS_EINVAL
+            with torch.no_grad(), pytest.raises(b.DsqError, match="current CUDA device"):     # (it goes on to the next check)
+                call()
+    with pytest.raises(b.DsqError, match="current CUDA device"):
+        b.ds_product(msg, leaf.detach(), 2, 64)
