@@ -382,12 +382,14 @@ uint64_t ds_matrix_bytes(const ds_matrix* m);
 /* y[t][r] = sum over blocks (scale / 15) * sum over c of the block (2 code - 15) * x[t][c]: `tokens` vectors through the matrix.
  * msg_dev: ds_matrix_bytes(m) bytes, 4-byte aligned.  x_dev: tokens rows of pitch x_ld >= cols elements; y_dev: tokens rows of
  * pitch y_ld >= rows elements (columns behind `rows` are left as they were); both of m->dtype and aligned to their elements.  Products are summed in fp32 and
- * rounded once to dtype.  Infinities and NaN in x go where the formula takes them. */
+ * rounded once to dtype; for DS_F32, x first to multiples of 2^-31 (at most) of the largest |x| of the 128 columns around it (32 for one token), which are summed
+ * exactly.  Infinities and NaN in x go where the formula takes them. */
 uint64_t ds_product_work_bytes(const ds_matrix* m);
 ds_status ds_product(const ds_matrix* m, const void* msg_dev, const void* x_dev, uint64_t x_ld, void* y_dev, uint64_t y_ld,
                      void* work_dev, uint64_t work_bytes, void* hip_stream, char* errbuf, uint64_t errbuf_len);
 
 /* dx[t][c] = sum over r of dy[t][r] * (scale(r, c) / 15) * (2 code(r, c) - 15): the gradient of ds_product with respect to x.
+ * dy * scale / 15 is rounded before, by at most 2^-17 of itself for 16-bit dtypes and 2^-24 for DS_F32; sums are fp32, rounded once to dtype.
  * dy_dev: tokens rows of pitch dy_ld >= rows elements; dx_dev: tokens rows of pitch dx_ld >= cols elements; otherwise as ds_product. */
 uint64_t ds_product_gradient_work_bytes(const ds_matrix* m);
 ds_status ds_product_gradient(const ds_matrix* m, const void* msg_dev, const void* dy_dev, uint64_t dy_ld, void* dx_dev,

@@ -1,18 +1,19 @@
 // Products with a matrix that is held as messages (ds_product): y = x M^T, M's rows as 4-bit codes with a scale per block.
 //
 // Reading the message, 0.53 bytes a weight, is what cannot be done without, and leaves time for some four vector instructions a weight's
-// share of a lane.  Codes are bytes after half an instruction each, so x is made of bytes, too, and the products are integers: per token
-// and 128 columns ("chunk"; 64 where a block is 64), x = 2^e v with integers v of 16 bits (24 for fp32), written as two (three) signed bytes, which an
-// i8 matrix instruction takes as rows of their own.  All sums inside a chunk are exact; 15 sum v, which takes codes 0 .. 15 to 2 code - 15, is where they start.  What is rounded is v:
-// 2^-15 (2^-23) of the largest |x| next to it at most, which the same block's scale multiplies and no code drops, against the 2^-8 or 2^-11 of
-// y's own rounding for 16-bit types (2^-24 for fp32).
+// share of a lane.  16-bit types: x goes into matrix instructions as it is, a code as 0.5 + q / 32 (dsq_codes.h), which takes one vector instruction, and
+// what that is too large by is where sums start: -47/64 sum x of a block.  Products are exact and sums are fp32; a block's scale multiplies its sum.
+//   fp32: x is made of bytes, and the products are integers: per token and 128 columns ("chunk"; 64 where a block is 64), x = 2^e v with integers v of 32
+// bits, written as four signed bytes, which an i8 matrix instruction takes as rows of their own, against codes as bytes.  All sums inside a chunk are exact; 15 sum v,
+// which takes codes 0 .. 15 to 2 code - 15, is where they start.  What is rounded is v: 2^-31 of the largest |x| next to it at most, which the same
+// block's scale multiplies and no code drops: below 2^-24 of what that one contributes, 1/15 of it or more, unless a hundred of them agree in sign.
 //   A wave takes 16 (or 32) rows and a chunk at a time: lane (n, j) = (l % 16, l / 16) holds 32 codes of row n and the scale of its block, which is
-// one factor for all of the lane's results.  x's bytes lie in LDS in the order in which codes come out of a word.
-//   Three kernels.  One token: product_one_kernel.  Up to two matrix instructions of tokens (16; 8 for fp32), where reading codes is most of the work:
-// product_tiles_kernel, whose workgroups make x's bytes themselves.  More tokens: product_kernel; a launch before makes x's bytes once, in work_dev,
-// and codes go straight into registers, which leaves LDS to x.  Measured, us, product_tiles_kernel : product_kernel: 2 x 65536 x 4096, bf16,
-// 34.0 : 62.0; 16 x 4096 x 16384, fp16, 19.4 : 26.7; 8 x 2048 x 2048 7.1 : 11.7; 4 x 16384 x 4096, fp32, 16.9 : 18.5; from there on 61 x 16001 x 4099,
-// bf16, 55.7 : 38.6; 64 x 65536 x 1024 31.7 : 24.9, and in blocks of 64 51.4 : 31.6; 32 x 16384 x 4096, fp32, 30.3 : 26.9.
+// one factor for all of the lane's results.  x lies in LDS in the order in which codes come out of a word.
+//   Three kernels.  One token: product_one_kernel.  Up to 16 tokens (8 for fp32), where reading codes is most of the work:
+// product_tiles_kernel, whose workgroups lay out x themselves.  More tokens: product_kernel; a launch before lays x out once, in work_dev,
+// and codes go straight into registers, which leaves LDS to x.  Measured, us, product_tiles_kernel : product_kernel: 2 x 65536 x 4096,
+// bf16, 30.7 : 64.4; 16 x 4096 x 16384, fp16, 18.3 : 23.7; 16 x 65536 x 4096, bf16, 40.0 : 66.2; 8 x 2048 x 2048, fp32, 7.6 : 9.6; 4 x 16384 x 4096, fp32,
+// 17.3 : 20.5; one launch of product_tiles_kernel after the other: 17 x 65536 x 4096, bf16, 70.2 : 55.5; 32 tokens 79.0 : 56.2; 16 x 16384 x 4096, fp32, 38.6 : 21.7.
 //   Where there are too few rows for the GPU, workgroups split the columns, too, and one more launch adds their sums.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
@@ -26,21 +27,22 @@ constexpr uint64_t kGroupsOfLaunch = 1u << 22;                    // a launch di
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
-// How x is written as bytes: `digits` rows of a matrix instruction per token, of which `stride` are set aside.
+// What a matrix instruction's 16 rows are: tokens, or for fp32 four digits of four tokens.
 template <typename T>
-struct Digits {
-    static constexpr int digits = 2, stride = 2, exponent = 14;   // |v| <= 127 * 256 + 127, below 2^15
-    static constexpr float most = 32639.f;
-};
-template <>
-struct Digits<float> {
-    static constexpr int digits = 3, stride = 4, exponent = 22;   // |v| <= 127 (2^16 + 2^8 + 1), below 2^23
-    static constexpr float most = 8355711.f;
-};
+constexpr int kTokenRows = sizeof(T) == 4 ? 4 : 1;
 template <typename T>
-constexpr int kTileTokens = 16 / Digits<T>::stride;               // tokens of a matrix instruction
+using Coded = std::conditional_t<sizeof(T) == 4, __bf16, T>;        // (codes as a matrix instruction's numbers: of 16-bit types)
 template <typename T>
-constexpr uint64_t kTokens = 8 * kTileTokens<T>;                  // of a launch
+constexpr int kTileTokens = 16 / kTokenRows<T>;                   // tokens of a matrix instruction
+template <typename T>
+constexpr int kMostTiles = sizeof(T) == 4 ? 8 : 4;                // of a launch
+template <typename T>
+constexpr int kFewTiles = sizeof(T) == 4 ? 2 : 1;                 // of product_tiles_kernel
+template <typename T>
+constexpr uint64_t kTokens = kMostTiles<T> * kTileTokens<T>;      // of a launch
+// x of fp32 as integers: |v| <= 127 (2^24 + 2^16 + 2^8 + 1), below 2^31, and as a number of fp32.
+constexpr int kExponent = 30;
+constexpr float kMostDigits = 2139062016.f;
 constexpr int kRowTiles = 2;                                      // of 16 rows, of a wave of product_kernel
 
 struct ProductPlan {
@@ -55,14 +57,18 @@ struct ProductShape : ProductArgs {
     float* partial;                                               // parts x tokens x rows, or nullptr
 };
 
-// One chunk of x: the digits, [matrix instruction][j][row][16 columns]; the sums the products start from, -15 times the digits' sum, [block][row]
-// (two blocks where a block is 64 columns); and per token what v counts, 2^e.  Rows: digit d of token t is row stride t + d; rows of no token hold anything.
+// One chunk of x.  16-bit types: x in the order of codes, [word of a lane][j][token][8 columns], and what products start from, -kCentre sum x, [block][token].
+// fp32: the digits, [matrix instruction][j][row][16 columns] with digit d of token t in row 4 t + d; where the products start, -15 times the digits' sum,
+// [block][row]; and per token what v counts, over 2^kExponent.  (Two blocks where a block is 64 columns.)  Rows of no token hold anything.
 template <typename T, int TT, bool NARROW>
 struct Record {
-    static constexpr uint32_t H = NARROW ? 2 : 1, rows = 16 * TT, sums = H * TT * 64, units = H * TT * 32, bytes = 128 * rows + sums + units;
-    __device__ static i32x4* digits(uint8_t* r) { return reinterpret_cast<i32x4*>(r); }
-    __device__ static int32_t* start(uint8_t* r) { return reinterpret_cast<int32_t*>(r + 128 * rows); }
-    __device__ static float* unit(uint8_t* r) { return reinterpret_cast<float*>(r + 128 * rows + sums); }
+    static constexpr uint32_t H = NARROW ? 2 : 1, rows = 16 * TT;
+    static constexpr uint32_t x_bytes = (sizeof(T) == 4 ? 128 : 256) * rows, sums = H * rows * 4;
+    static constexpr uint32_t units = sizeof(T) == 4 ? H * rows : 0, bytes = x_bytes + sums + units;
+    static_assert(bytes % 16 == 0);
+    __device__ static u32x4* x(uint8_t* r) { return reinterpret_cast<u32x4*>(r); }
+    __device__ static void* start(uint8_t* r) { return r + x_bytes; }
+    __device__ static float* unit(uint8_t* r) { return reinterpret_cast<float*>(r + x_bytes + sums); }
 };
 
 // One weight after the other, as the formula has it: for a result that is not finite.
@@ -136,18 +142,19 @@ __device__ __forceinline__ void load_codes_tail(Codes<NARROW>& c, const uint8_t*
 
 // 2^p, for p from -126 to 127.
 __device__ __forceinline__ float power2_of(int p) { return __uint_as_float((uint32_t)(p + 127) << 23); }
-// The largest p for which 2^p x is below 2^(exponent + 1) and at most `limit`, of an |x| with these bits (not above 127: what is lost there is
-// below 2^-127).
-__device__ __forceinline__ int power_of(uint32_t bits, int exponent, float limit) {
-    const int p = exponent + 127 - (int)(bits >> 23), q = p > 126 ? 126 : p;
-    return __uint_as_float(bits) * power2_of(q) > limit ? q - 1 : q;
+// The largest p for which 2^p x is at most `limit`, just below 2^31, of an |x| with these bits: -97 to 149 (2^149 makes an integer of any x).
+__device__ __forceinline__ int power_of(uint32_t bits, float limit) {
+    const int p = kExponent + 127 - (int)(bits >> 23), q = p > 149 ? 149 : p;
+    return ldexpf(__uint_as_float(bits), q) > limit ? q - 1 : q;
 }
 
 // op over 8 or 16 adjacent lanes, in all of them: each lane with its mirror image, then with the others of its four.
-template <int CTRL>
-__device__ __forceinline__ uint32_t other_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
-template <int LANES, typename F>
-__device__ __forceinline__ uint32_t over_lanes(uint32_t v, F op) {
+template <int CTRL, typename V>
+__device__ __forceinline__ V other_lane(V v) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+template <int LANES, typename V, typename F>
+__device__ __forceinline__ V over_lanes(V v, F op) {
     if (LANES == 16) v = op(v, other_lane<0x140>(v));             // row_mirror
     v = op(v, other_lane<0x141>(v));                              // row_half_mirror
     v = op(v, other_lane<0x4E>(v));                               // quad_perm 2 3 0 1
@@ -168,115 +175,109 @@ __device__ __forceinline__ typename EightOf<T>::Raw load_eight(const T* x, uint3
     for (int e = 0; e < 8; ++e) raw[e] = col + e < cols ? x[col + e] : (T)0.f;
     return raw;
 }
-// The bits of the largest of eight magnitudes, of the type's width; NaN is above all.  And the bits of the same number in fp32.
-template <typename T>
-__device__ __forceinline__ uint32_t largest_bits(typename EightOf<T>::Raw raw) {
-    if constexpr (sizeof(T) == 2) {
-        typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
-        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-        const u16x8 bits = __builtin_bit_cast(u16x8, raw) & (uint16_t)0x7FFF;
-        const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(bits.s01, bits.s23), __builtin_elementwise_max(bits.s45, bits.s67));
-        return m.x > m.y ? m.x : m.y;
-    } else {
-        uint32_t most = 0;
+// The bits of the largest of N magnitudes; NaN is above all.
+template <int N>
+__device__ __forceinline__ uint32_t largest_bits(const float (&v)[N]) {
+    uint32_t most = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t bits = __float_as_uint((float)raw[e]) & 0x7FFFFFFFu;
-            most = bits > most ? bits : most;
-        }
-        return most;
+    for (int e = 0; e < N; ++e) {
+        const uint32_t bits = __float_as_uint(v[e]) & 0x7FFFFFFFu;
+        most = bits > most ? bits : most;
     }
-}
-template <typename T>
-__device__ __forceinline__ uint32_t float_bits(uint32_t bits) {
-    if constexpr (sizeof(T) == 2) return __float_as_uint((float)__builtin_bit_cast(T, (uint16_t)bits));
-    else return bits;
+    return most;
 }
 
 // Sixteen adjacent lanes, lane u with columns 8 u .. 8 u + 7 of a chunk (raw), write a token's part of the chunk's record.
 template <typename T, int TT, bool NARROW>
-__device__ void make_digits(uint32_t tok, uint32_t u, typename EightOf<T>::Raw raw, uint8_t* record) {
-    using D = Digits<T>;
+__device__ void make_record(uint32_t tok, uint32_t u, typename EightOf<T>::Raw raw, uint8_t* record) {
     using R = Record<T, TT, NARROW>;
     constexpr int LANES = NARROW ? 8 : 16;                        // of a block
-    // 2^power x, rounded, plus 128 in all digits but the highest: its bytes are the digits, their sign bits turned over where 128 was added
-    uint32_t most = over_lanes<LANES>(largest_bits<T>(raw), [](uint32_t x, uint32_t y) { return x > y ? x : y; });
-    most = float_bits<T>(most);
-    const int power = power_of(most, D::exponent, D::most);
-    const bool finite = most < 0x7F800000u;                       // (if not, the block counts as NaN, whatever its digits are)
-    const float to = power2_of(power);
-    uint32_t v[8];
+    const uint32_t t = NARROW ? u / 8 * 2 + u % 2 : u % 4, j = NARROW ? u % 8 / 2 : u / 4;
+    if constexpr (sizeof(T) == 2) {
+        R::x(record)[(4 * t + j) * R::rows + tok] = in_code_order(__builtin_bit_cast(u32x4, raw));
+        float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if constexpr (D::digits == 2) v[e] = __float_as_uint(fmaf((float)raw[e], to, 12582912.f + 128.f));   // 1.5 2^23: an ulp is 1
-        else v[e] = (uint32_t)(finite ? (int32_t)rintf((float)raw[e] * to) : 0) + 0x8080u;
-    }
-    uint32_t bytes[D::digits][2];                                 // the odd columns apart from the even ones
+        for (int e = 0; e < 8; ++e) sum += (float)raw[e];
+        sum = over_lanes<LANES>(sum, [](float x, float y) { return x + y; });
+        if (u % LANES == 0) static_cast<float*>(R::start(record))[u / LANES * R::rows + tok] = -kCentre * sum;
+    } else {
+        float x[8];
 #pragma unroll
-    for (int o = 0; o < 2; ++o) {
-        const uint32_t a = __builtin_amdgcn_perm(v[2 + o], v[o], 0x05010400u), b = __builtin_amdgcn_perm(v[6 + o], v[4 + o], 0x05010400u);
-        bytes[D::digits - 1][o] = __builtin_amdgcn_perm(b, a, 0x05040100u) ^ 0x80808080u;
-        bytes[D::digits - 2][o] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-        if constexpr (D::digits == 3) {
-            bytes[1][o] ^= 0x80808080u;
-            const uint32_t c = __builtin_amdgcn_perm(v[2 + o], v[o], 0x0C0C0602u), d = __builtin_amdgcn_perm(v[6 + o], v[4 + o], 0x0C0C0602u);
-            bytes[0][o] = __builtin_amdgcn_perm(d, c, 0x05040100u);
+        for (int e = 0; e < 8; ++e) x[e] = raw[e];
+        // 2^power x, rounded, plus 128 in all digits but the highest: its bytes are the digits, their sign bits turned over where 128 was added
+        const uint32_t most = over_lanes<LANES>(largest_bits(x), [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+        const int power = power_of(most, kMostDigits);
+        const bool finite = most < 0x7F800000u;                   // (if not, the block counts as NaN, whatever its digits are)
+        uint32_t v[8], bytes[4][2];                               // of a digit: the odd columns apart from the even ones
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (uint32_t)(finite ? (int32_t)rintf(ldexpf(x[e], power)) : 0) + 0x808080u;
+#pragma unroll
+        for (int o = 0; o < 2; ++o) {
+            const uint32_t a = __builtin_amdgcn_perm(v[2 + o], v[o], 0x05010400u), b = __builtin_amdgcn_perm(v[6 + o], v[4 + o], 0x05010400u);
+            const uint32_t c = __builtin_amdgcn_perm(v[2 + o], v[o], 0x07030602u), d = __builtin_amdgcn_perm(v[6 + o], v[4 + o], 0x07030602u);
+            bytes[3][o] = __builtin_amdgcn_perm(b, a, 0x05040100u) ^ 0x80808080u;
+            bytes[2][o] = __builtin_amdgcn_perm(b, a, 0x07060302u) ^ 0x80808080u;
+            bytes[1][o] = __builtin_amdgcn_perm(d, c, 0x05040100u) ^ 0x80808080u;
+            bytes[0][o] = __builtin_amdgcn_perm(d, c, 0x07060302u);
         }
-    }
-    const uint32_t t = NARROW ? u / 8 * 2 + u % 2 : u % 4, j = NARROW ? u % 8 / 2 : u / 4, rows = R::rows;
 #pragma unroll
-    for (int d = 0; d < D::digits; ++d) {
-        const uint32_t at = (((t / 2) * 4 + j) * rows + tok * D::stride + d) * 16 + 8 * (t % 2);
-        *reinterpret_cast<u32x2*>(record + at) = u32x2{bytes[d][0], bytes[d][1]};
-        constexpr int kOff = (int)0xF1F1F1F1;                     // -15 each
-        const int32_t sum = __builtin_amdgcn_sdot4((int)bytes[d][0], kOff, __builtin_amdgcn_sdot4((int)bytes[d][1], kOff, 0, false), false);
-        const uint32_t total = over_lanes<LANES>((uint32_t)sum, [](uint32_t x, uint32_t y) { return x + y; });
-        if (u % LANES == 0) R::start(record)[u / LANES * (TT * 16) + tok * D::stride + d] = (int32_t)total;
+        for (int d = 0; d < 4; ++d) {
+            const uint32_t at = (((t / 2) * 4 + j) * R::rows + 4 * tok + d) * 16 + 8 * (t % 2);
+            *reinterpret_cast<u32x2*>(record + at) = u32x2{bytes[d][0], bytes[d][1]};
+            constexpr int kOff = (int)0xF1F1F1F1;                 // -15 each
+            int32_t sum = __builtin_amdgcn_sdot4((int)bytes[d][0], kOff, __builtin_amdgcn_sdot4((int)bytes[d][1], kOff, 0, false), false);
+            sum = over_lanes<LANES>(sum, [](int32_t x, int32_t y) { return x + y; });
+            if (u % LANES == 0) static_cast<int32_t*>(R::start(record))[u / LANES * R::rows + 4 * tok + d] = sum;
+        }
+        if (u % LANES == 0) R::unit(record)[u / LANES * (TT * 4) + tok] = finite ? power2_of(kExponent - power) : __builtin_nanf("");
     }
-    if (u % LANES == 0) R::unit(record)[u / LANES * (TT * 8) + tok] = finite ? power2_of(-power) : __builtin_nanf("");
 }
 
-// x as bytes, for all workgroups: 16 threads per chunk and token.
+// The records, for all workgroups: 16 threads per chunk and token.
 template <typename T, int TT, bool NARROW>
-__global__ void __launch_bounds__(256) product_digits_kernel(ProductShape a, uint8_t* panel) {
+__global__ void __launch_bounds__(256) product_records_kernel(ProductShape a, uint8_t* panel) {
     const uint64_t chunk = blockIdx.x;
     const uint32_t tok = threadIdx.x / 16 + 16 * blockIdx.y, u = threadIdx.x % 16;
     if (tok >= a.tokens) return;
     const T* x = static_cast<const T*>(a.in) + tok * a.in_ld;
-    make_digits<T, TT, NARROW>(tok, u, load_eight(x, (uint32_t)chunk * kChunk + 8 * u, (uint32_t)a.cols), panel + chunk * Record<T, TT, NARROW>::bytes);
+    make_record<T, TT, NARROW>(tok, u, load_eight(x, (uint32_t)chunk * kChunk + 8 * u, (uint32_t)a.cols), panel + chunk * Record<T, TT, NARROW>::bytes);
 }
 
 // The products of a chunk of codes, 16 RT rows, with the chunk's record of x.
 template <typename T, int TT, int RT, bool NARROW>
-__device__ __forceinline__ void multiply(const Codes<NARROW> (&c)[RT], uint8_t* rec, uint32_t n, uint32_t j,
-                                         float (&sum)[RT][TT][4 / Digits<T>::stride]) {
-    using D = Digits<T>;
+__device__ __forceinline__ void multiply(const Codes<NARROW> (&c)[RT], uint8_t* rec, uint32_t n, uint32_t j, CodeMasks masks,
+                                         float (&sum)[RT][TT][4 / kTokenRows<T>]) {
     using R = Record<T, TT, NARROW>;
-    constexpr int H = NARROW ? 2 : 1, PER = 4 / D::stride;        // blocks of a chunk; tokens of a lane and matrix instruction
-    const i32x4* digits = R::digits(rec);
-    i32x4 codes[RT][2];
+    constexpr bool kInteger = sizeof(T) == 4;
+    constexpr int H = NARROW ? 2 : 1, PER = 4 / kTokenRows<T>, W = kInteger ? 2 : 4;       // blocks of a chunk; tokens of a lane; operands of a chunk
+    using Operand = std::conditional_t<kInteger, i32x4, Eight<Coded<T>>>;
+    using Sums = std::conditional_t<kInteger, i32x4, f32x4>;
+    Operand codes[RT][W];
     float unit[RT][H];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            codes[r][h] = i32x4{(int)(c[r].w[2 * h] << 1 & 0x1E1E1E1Eu), (int)(c[r].w[2 * h] >> 3 & 0x1E1E1E1Eu),
-                                (int)(c[r].w[2 * h + 1] << 1 & 0x1E1E1E1Eu), (int)(c[r].w[2 * h + 1] >> 3 & 0x1E1E1E1Eu)};
+        for (int w = 0; w < W; ++w) {
+            if constexpr (kInteger)
+                codes[r][w] = i32x4{(int)(c[r].w[2 * w] << 1 & 0x1E1E1E1Eu), (int)(c[r].w[2 * w] >> 3 & 0x1E1E1E1Eu),
+                                    (int)(c[r].w[2 * w + 1] << 1 & 0x1E1E1E1Eu), (int)(c[r].w[2 * w + 1] >> 3 & 0x1E1E1E1Eu)};
+            else codes[r][w] = code_operand<T>(c[r].w[w], masks);
+        }
 #pragma unroll
-        for (int b = 0; b < H; ++b) unit[r][b] = c[r].scale[b] * (1.f / 15.f);
+        for (int b = 0; b < H; ++b) unit[r][b] = c[r].scale[b] * (kInteger ? 1.f / 15.f : kPerCode);
     }
     struct Left {
-        i32x4 x[2], start[H];
-        float count[H][PER];
+        Operand x[W];
+        Sums start[H];
+        float count[H];
     };
     auto load = [&](Left& v, int t) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) v.x[h] = digits[(4 * h + j) * R::rows + 16 * t + n];
+        for (int w = 0; w < W; ++w) v.x[w] = __builtin_bit_cast(Operand, R::x(rec)[(4 * w + j) * R::rows + 16 * t + n]);
 #pragma unroll
         for (int b = 0; b < H; ++b) {
-#pragma unroll
-            for (int i = 0; i < PER; ++i) v.count[b][i] = R::unit(rec)[b * (TT * 8) + (4 * t + j) * PER + i];
-            v.start[b] = *reinterpret_cast<const i32x4*>(R::start(rec) + b * (TT * 16) + 16 * t + 4 * j);
+            v.start[b] = *reinterpret_cast<const Sums*>(static_cast<uint32_t*>(R::start(rec)) + b * R::rows + 16 * t + 4 * j);
+            if constexpr (kInteger) v.count[b] = R::unit(rec)[b * (TT * 4) + 4 * t + j];
         }
     };
     Left left[2];
@@ -289,22 +290,22 @@ __device__ __forceinline__ void multiply(const Codes<NARROW> (&c)[RT], uint8_t* 
         for (int b = 0; b < H; ++b)
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                i32x4 p;
-                if constexpr (NARROW) {
-                    p = __builtin_amdgcn_mfma_i32_16x16x64_i8(v.x[b], codes[r][b], v.start[b], 0, 0, 0);
-                } else {
-                    p = __builtin_amdgcn_mfma_i32_16x16x64_i8(v.x[0], codes[r][0], v.start[0], 0, 0, 0);
-                    p = __builtin_amdgcn_mfma_i32_16x16x64_i8(v.x[1], codes[r][1], p, 0, 0, 0);
-                }
+                Sums p = v.start[b];
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    float w;
-                    if constexpr (D::digits == 2) w = (float)((p[2 * i] << 8) + p[2 * i + 1]);
-                    else w = fmaf(fmaf((float)p[0], 256.f, (float)p[1]), 256.f, (float)p[2]);
-                    sum[r][t][i] = fmaf(unit[r][b] * v.count[b][i], w, sum[r][t][i]);
+                for (int w = b * (W / H); w < (b + 1) * (W / H); ++w) {
+                    if constexpr (kInteger) p = __builtin_amdgcn_mfma_i32_16x16x64_i8(v.x[w], codes[r][w], p, 0, 0, 0);
+                    else p = matrix_fma(v.x[w], codes[r][w], p);
+                }
+                if constexpr (kInteger) {                         // the factors one after the other, smallest first: no product leaves fp32's range before y does
+                    const float high = (float)((p[0] << 8) + p[1]), low = (float)((p[2] << 8) + p[3]);
+                    const float w = fmaf(high, 0x1p-14f, low * 0x1p-30f);
+                    sum[r][t][0] = fmaf(unit[r][b] * w, v.count[b], sum[r][t][0]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) sum[r][t][i] = fmaf(unit[r][b], p[i], sum[r][t][i]);
                 }
             }
-        if constexpr (TT > 2) {                                   // what is asked for, and what is left to do, beyond the next tile takes registers
+        if constexpr (TT > kFewTiles<T>) {                        // what is asked for, and left to do, beyond the next tile takes registers (32 x 65536 x 4096, bf16: 69 us)
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -314,13 +315,13 @@ __device__ __forceinline__ void multiply(const Codes<NARROW> (&c)[RT], uint8_t* 
     }
 }
 
-// More tokens: a workgroup takes 256 rows, chunk after chunk, its waves 32 rows each against the same x in LDS.  61 x 16001 x 4099, bf16, in blocks of 64: 30 us;
-// for every token, row and block four vector instructions, 45 % of the clocks, and the matrix instructions 15 %.
+// More tokens: a workgroup takes 256 rows, chunk after chunk, its waves 32 rows each against the same x in LDS.  61 x 16001 x 4099, bf16, in blocks of 64: 24.4 us,
+// vector instructions 31 % of the clocks, matrix instructions 18 %; two waves on a SIMD wait for one another at every chunk.
 template <typename T, int TT, bool NARROW>
 __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
     constexpr int RT = kRowTiles;
     using R = Record<T, TT, NARROW>;
-    constexpr int PER = 4 / Digits<T>::stride;                    // tokens of a lane and matrix instruction
+    constexpr int PER = 4 / kTokenRows<T>;                        // tokens of a lane and matrix instruction
     constexpr uint32_t record = R::bytes, kAll = record / 16, kPieces = (kAll + kThreads - 1) / kThreads;      // x of a chunk, in 16-byte pieces; of a thread
     extern __shared__ __align__(16) uint8_t lds[];
     const uint32_t tokens = (uint32_t)a.tokens;
@@ -358,7 +359,8 @@ __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
         for (uint32_t q = 0; q < kPieces; ++q)
             if (q * kThreads + threadIdx.x < kAll) reinterpret_cast<u32x4*>(lds + (c & 1) * record)[q * kThreads + threadIdx.x] = v[q];
     };
-    auto use = [&](const Codes<NARROW> (&codes)[RT], uint32_t c) { multiply<T, TT, RT, NARROW>(codes, lds + (c & 1) * record, n, j, sum); };
+    const CodeMasks masks = code_masks<Coded<T>>();
+    auto use = [&](const Codes<NARROW> (&codes)[RT], uint32_t c) { multiply<T, TT, RT, NARROW>(codes, lds + (c & 1) * record, n, j, masks, sum); };
     u32x4 x[kPieces];
     bring(x, 0);
     if (whole) {
@@ -410,12 +412,11 @@ __global__ void __launch_bounds__(kThreads) product_kernel(ProductShape a) {
 // Few tokens: codes go through LDS, too, 128 rows of 256 columns at a time, so that memory is read in rows of 128 bytes and more (see product_one_kernel) and a
 // compute unit has as much under way as it multiplies.  While a stage is multiplied the next one's loads are on their way into registers; then it goes into
 // the other half of the LDS.  A row's part of a stage is read as it lies in the message, in nine pieces of 16 bytes, scales among the codes: a load that
-// gathers scales alone costs the memory pipeline as much as one that brings 16 bytes a lane (2 x 65536 x 4096, blocks of 256, 34.0 us, 42.9 with scales read
-// apart; 16 x 4096 x 16384, where the instructions count, 19.4 and 18.8).  Blocks of more than 256 columns are read in eight pieces, and their scales once a
-// block (of 2048: 30.2 us).
-//   2 tokens of 65536 x 4096 read 4.2 TB/s.  16 tokens cost some 340 instructions a stage, 5400 clocks for the two workgroups of a compute unit, in which it
-// could read 44 KB and reads 32: x's digits are a third of them; 44.2 us, and 2.3 TB/s for 16 x 4096 x 16384, whose workgroups have four stages each.
-// Slower: two stages ahead (registers; 16 x 4096 x 16384 22.8 us), workgroups of 256 rows (2 x 65536 x 4096 46.8 : 42.9).
+// gathers scales alone costs the memory pipeline as much as one that brings 16 bytes a lane (2 x 65536 x 4096, blocks of 256, 30.7 us; with scales read
+// apart a quarter more).  Blocks of more than 256 columns are read in eight pieces, and their scales once a block (of 2048: 31.0 us).
+//   2 tokens of 65536 x 4096 read 4.6 TB/s, 16 tokens 3.6.  16 x 4096 x 16384, fp16: 14.4 us, 2.5 TB/s: 190 vector instructions of a wave and stage, 46 % of the
+// clocks, and four stages of each workgroup, of which the first one's reads have nothing beside them.
+// Slower, when x was held in digits: two stages ahead (registers; 22.8 us for 19.4), workgroups of 256 rows (2 x 65536 x 4096 46.8 for 42.9).
 constexpr uint32_t kStageChunks = 2, kStageCols = kStageChunks * kChunk;                   // of a stage
 static_assert(kStageCols == kStageColumns);
 
@@ -431,7 +432,7 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
     static_assert(16 * kStageChunks * TT * kTileTokens<T> <= kThreads, "a thread has eight columns of x");
     using R = Record<T, TT, NARROW>;
     using Raw = typename EightOf<T>::Raw;
-    constexpr int PER = 4 / Digits<T>::stride;
+    constexpr int PER = 4 / kTokenRows<T>;
     extern __shared__ __align__(16) uint8_t lds[];
     const uint32_t tokens = (uint32_t)a.tokens;
     constexpr uint32_t record = R::bytes, half = S::bytes;
@@ -510,7 +511,7 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
             if (i + 1 < PIECES || has_third) *reinterpret_cast<u32x4*>(to + piece_to[i]) = v.codes[i];
         if (has_scale) reinterpret_cast<float*>(to + S::codes)[threadIdx.x] = v.scale;
         uint8_t* records = to + S::codes + S::scales;
-        if (x_tok < tokens) make_digits<T, TT, NARROW>(x_tok, x_unit % 16, v.x, records + x_unit / 16 * record);
+        if (x_tok < tokens) make_record<T, TT, NARROW>(x_tok, x_unit % 16, v.x, records + x_unit / 16 * record);
     };
 
     float sum[1][TT][PER];
@@ -522,6 +523,7 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
     // of the lane's row in a half: chunk c's scale and codes; with blocks of 64 block b's are 36 b from the first
     const uint32_t block = my_row * kRowPieces * 16, scale_at = apart ? S::codes + 4 * my_row : block, scale_step = a.block == kChunk ? pitch : 0;
     const uint32_t codes_at = block + (apart ? 0 : 4) + 16 * j, codes_step = a.block == kChunk ? pitch : kChunk / 2;
+    const CodeMasks masks = code_masks<Coded<T>>();
     auto use = [&](uint8_t* half_at) {
 #pragma unroll
         for (uint32_t c = 0; c < kStageChunks; ++c) {
@@ -541,7 +543,7 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
 #pragma unroll
                 for (int w = 0; w < 4; ++w) codes[0].w[w] = v[w];
             }
-            multiply<T, TT, 1, NARROW>(codes, half_at + S::codes + S::scales + c * record, n, j, sum);
+            multiply<T, TT, 1, NARROW>(codes, half_at + S::codes + S::scales + c * record, n, j, masks, sum);
         }
     };
     // Stage s is multiplied out of one half of the LDS while stage s + 1 is on its way.  (The last one again behind the end: no branch.)
@@ -568,21 +570,16 @@ __global__ void __launch_bounds__(kThreads) product_tiles_kernel(ProductShape a)
 }
 
 // One token: rows of codes are read whole, which costs the memory pipeline a third of what sixteen rows of 64 bytes cost a load, and meet x in
-// registers.  A lane keeps 32 columns of x for all the rows of its wave, G lanes hold a row, and a load takes 64 / G rows of 32 G columns.  x is
-// written in digits of four bits here, 16^d apart, 4 of them (6 for fp32), with an exponent per 32 columns: eight codes (less 8, so that they are
-// signed) meet eight digits in one instruction, 0.6 instructions a weight.  The lanes of a row are joined by a tree of lane shifts.  65536 x 4096: 24.6 us,
-// 5.8 TB/s, the vector units busy 67 % of the time.
+// registers.  A lane keeps 32 columns of x for all the rows of its wave, G lanes hold a row, and a load takes 64 / G rows of 32 G columns.
+//   16-bit types: a matrix instruction of 4 x 4 blocks, lane l's operands row and column l % 4 of block l / 4, of which the lane's own product stands on the
+// diagonal, in its register l % 4; the other twelve sums are of no use and cost nothing that is short.
+//   fp32: x is written in eight signed digits of four bits, 16^d apart, with an exponent per 32 columns: eight codes (less 8, so that they are signed) meet
+// eight digits in one instruction.
+// The lanes of a row are joined by a tree of lane shifts.  65536 x 4096, bf16: 24.9 us, 5.7 TB/s, the
+// vector units busy 70 % of the time, the matrix units 16 %; fp32 31 us.
 constexpr uint32_t kLaneCols = 32;
-template <typename T>
-struct Nibbles {
-    static constexpr int digits = 4, exponent = 14;
-    static constexpr float most = 30583.f;                        // 7 (16^3 + 16^2 + 16 + 1)
-};
-template <>
-struct Nibbles<float> {
-    static constexpr int digits = 6, exponent = 22;
-    static constexpr float most = 7829367.f;
-};
+constexpr int kNibbles = 8;
+constexpr float kMostNibbles = 2004317952.f;                      // 7 (16^7 + .. + 16 + 1), as a number of fp32
 
 template <int CTRL, int ROW_MASK>
 __device__ __forceinline__ float add_shifted(float v) {
@@ -602,9 +599,73 @@ __device__ __forceinline__ float lanes_total(float v) {
     return v;
 }
 
+// What a lane has of x, in one of two forms.
+template <typename T>
+struct Own {                                                      // 16-bit types: words in the order of codes, and what a product starts from
+    u32x4 x[4];
+    float start;
+    CodeMasks masks;
+
+    // `missing` of the words that come before the lane's are read with it, and count for nothing.
+    __device__ void read(const T* x_of, uint64_t col, uint64_t cols) {
+        using Raw = typename EightOf<T>::Raw;
+        const uint32_t missing = missing_words(col, cols);
+        float sum = 0.f;
+#pragma unroll
+        for (uint32_t w = 0; w < 4; ++w) {
+            Raw raw;
+            if (col + kLaneCols <= cols) {
+                raw = *reinterpret_cast<const Raw*>(x_of + col + 8 * w);
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) {
+                    const uint64_t c = col + 8 * w + e - 8 * missing;
+                    raw[e] = w >= missing && c < cols ? x_of[c] : (T)0.f;
+                }
+            }
+            x[w] = in_code_order(__builtin_bit_cast(u32x4, raw));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += (float)raw[e];
+        }
+        start = -kCentre * sum;
+        masks = code_masks<T>();
+    }
+    __device__ float product(u32x4 words, float scale) const {
+        f32x4 p = {start, start, start, start};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const u32x4 codes = __builtin_bit_cast(u32x4, code_operand<T>(words[w], masks));
+            p = own_products<T>(codes.xy, x[w].xy, p);
+            p = own_products<T>(codes.zw, x[w].zw, p);
+        }
+        const uint32_t lane = threadIdx.x;
+        const float even = lane & 2 ? p.z : p.x, odd = lane & 2 ? p.w : p.y;
+        return scale * kPerCode * (lane & 1 ? odd : even);
+    }
+};
+template <>
+struct Own<float> {                                               // digits; sum v as high and low halves of v; what v counts, over 2^kExponent
+    i32x4 digits[kNibbles];
+    int32_t high, low;
+    float count;
+
+    __device__ float product(u32x4 words, float scale) const {
+        int32_t dot[kNibbles];
+#pragma unroll
+        for (int d = 0; d < kNibbles; ++d) dot[d] = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int d = 0; d < kNibbles; ++d) dot[d] = __builtin_amdgcn_sdot8((int32_t)(words[w] ^ 0x88888888u), digits[d][w], dot[d], false);   // code - 8
+        // sum (2 code - 15) v = 2 sum (code - 8) v + sum v
+        const int32_t upper = ((dot[7] * 16 + dot[6]) * 16 + dot[5]) * 16 + dot[4], lower = ((dot[3] * 16 + dot[2]) * 16 + dot[1]) * 16 + dot[0];
+        const float v = fmaf((float)(2 * upper + high), 0x1p-14f, (float)(2 * lower + low) * 0x1p-30f);
+        return scale * (1.f / 15.f) * v * count;                  // (one after the other: see multiply)
+    }
+};
+
 template <typename T, int G>
 __global__ void __launch_bounds__(kThreads) product_one_kernel(ProductShape a) {
-    using D = Nibbles<T>;
     constexpr int AT_ONCE = 64 / G, AHEAD = 4;                    // rows of a load, loads under way
     extern __shared__ __align__(16) uint8_t lds[];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / G, l = lane % G;
@@ -612,11 +673,8 @@ __global__ void __launch_bounds__(kThreads) product_one_kernel(ProductShape a) {
     const uint32_t wave_rows = a.plan.wave_rows, rows_here = row_waves * wave_rows, loads = wave_rows / AT_ONCE;
     const uint64_t first = a.row0 + (uint64_t)blockIdx.x * rows_here;
     const uint32_t block_log2 = 31 - __builtin_clz(a.block);
-    const uint32_t lanes = col_waves * G;                         // lanes that hold different columns ...
-    i32x4* digits = reinterpret_cast<i32x4*>(lds);                // ... and their digits, [digit][lane]; then sum v and what v counts
-    int32_t* sums = reinterpret_cast<int32_t*>(digits + D::digits * lanes);
-    float* units = reinterpret_cast<float*>(sums + lanes);
-    float* totals = units + lanes;                                // [column wave][row of the workgroup]
+    const uint32_t lanes = col_waves * G;                         // lanes that hold different columns
+    float* totals = reinterpret_cast<float*>(lds);                // [column wave][row of the workgroup]
     float* mine = totals + cw * rows_here + rw * wave_rows;
     const T* x = static_cast<const T*>(a.in);
     for (uint64_t slice = 0; slice < a.cols; slice += lanes * kLaneCols) {
@@ -636,85 +694,75 @@ __global__ void __launch_bounds__(kThreads) product_one_kernel(ProductShape a) {
         Load ring[AHEAD];
 #pragma unroll
         for (int s = 0; s < AHEAD; ++s) fetch(ring[s], s);
-
-        // the workgroup writes this stretch of x in digits: a thread takes eight columns, four threads a lane's 32
-        if (slice) __syncthreads();
-        for (uint32_t w = threadIdx.x; w < lanes * 4; w += kThreads) {
-            const uint64_t at = slice + 8 * w;
-            float v[8];
-            if (at + 8 <= a.cols) {
-                typedef T Raw __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-                const Raw raw = *reinterpret_cast<const Raw*>(x + at);
+        Own<T> own;
+        if constexpr (sizeof(T) == 2) {
+            own.read(x, col, a.cols);
+        } else {
+            // the workgroup writes this stretch of x in digits, [digit][lane]: a thread takes eight columns, four threads a lane's 32
+            i32x4* digits = reinterpret_cast<i32x4*>(totals + kWaves * wave_rows);
+            int32_t* highs = reinterpret_cast<int32_t*>(digits + kNibbles * lanes);
+            int32_t* lows = highs + lanes;
+            float* counts = reinterpret_cast<float*>(lows + lanes);
+            if (slice) __syncthreads();
+            for (uint32_t w = threadIdx.x; w < lanes * 4; w += kThreads) {
+                const uint64_t at = slice + 8 * w;
+                float v[8];
+                if (at + 8 <= a.cols) {
+                    const EightOf<float>::Raw raw = *reinterpret_cast<const EightOf<float>::Raw*>(x + at);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = (float)raw[e];
-            } else {
+                    for (int e = 0; e < 8; ++e) v[e] = raw[e];
+                } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = at + e < a.cols ? (float)x[at + e] : 0.f;
-            }
-            uint32_t most = 0;
+                    for (int e = 0; e < 8; ++e) v[e] = at + e < a.cols ? (float)x[at + e] : 0.f;
+                }
+                uint32_t most = largest_bits(v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t bits = __float_as_uint(v[e]) & 0x7FFFFFFFu;
-                most = bits > most ? bits : most;
-            }
+                for (int o = 1; o < 4; o <<= 1) {
+                    const uint32_t other = (uint32_t)__shfl_xor((int)most, o);
+                    most = other > most ? other : most;
+                }
+                const int power = power_of(most, kMostNibbles);
+                const bool finite = most < 0x7F800000u;
+                uint32_t out[kNibbles];
+                int32_t high = 0, low = 0;
 #pragma unroll
-            for (int o = 1; o < 4; o <<= 1) {
-                const uint32_t other = (uint32_t)__shfl_xor((int)most, o);
-                most = other > most ? other : most;
-            }
-            const int power = power_of(most, D::exponent, D::most);
-            const bool finite = most < 0x7F800000u;
-            const float to = power2_of(power);
-            uint32_t out[D::digits];
-            int32_t sum = 0;
+                for (int d = 0; d < kNibbles; ++d) out[d] = 0;
 #pragma unroll
-            for (int d = 0; d < D::digits; ++d) out[d] = 0;
+                for (int e = 0; e < 8; ++e) {
+                    int32_t rest = finite ? (int32_t)rintf(ldexpf(v[e], power)) : 0;
+                    high += rest >> 16;
+                    low += rest & 0xFFFF;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                int32_t rest = finite ? (int32_t)rintf(v[e] * to) : 0;
-                sum += rest;
+                    for (int d = 0; d < kNibbles; ++d) {          // the first digit is the lowest; signed, [-8, 7]
+                        const int32_t digit = (int32_t)((uint32_t)rest << 28) >> 28;
+                        rest = (rest - digit) >> 4;
+                        out[d] |= ((uint32_t)digit & 15u) << (4 * e);
+                    }
+                }
+                const uint32_t place = (w % 4 + missing_words(slice + w / 4 * kLaneCols, a.cols)) % 4;
 #pragma unroll
-                for (int d = 0; d < D::digits; ++d) {             // the first digit is the lowest; signed, [-8, 7]
-                    const int32_t digit = rest << 28 >> 28;
-                    rest = (rest - digit) >> 4;
-                    out[d] |= ((uint32_t)digit & 15u) << (4 * e);
+                for (int d = 0; d < kNibbles; ++d) reinterpret_cast<uint32_t*>(digits + d * lanes + w / 4)[place] = out[d];
+#pragma unroll
+                for (int o = 1; o < 4; o <<= 1) {
+                    high += __shfl_xor(high, o);
+                    low += __shfl_xor(low, o);
+                }
+                if (w % 4 == 0) {
+                    highs[w / 4] = high;
+                    lows[w / 4] = low;
+                    counts[w / 4] = finite ? power2_of(kExponent - power) : __builtin_nanf("");
                 }
             }
-            const uint32_t place = (w % 4 + missing_words(slice + w / 4 * kLaneCols, a.cols)) % 4;
+            __syncthreads();
+            const uint32_t from = cw * G + l;
 #pragma unroll
-            for (int d = 0; d < D::digits; ++d) reinterpret_cast<uint32_t*>(digits + d * lanes + w / 4)[place] = out[d];
-#pragma unroll
-            for (int o = 1; o < 4; o <<= 1) sum += __shfl_xor(sum, o);
-            if (w % 4 == 0) {
-                sums[w / 4] = sum;
-                units[w / 4] = finite ? power2_of(-power) * (1.f / 15.f) : __builtin_nanf("");
-            }
+            for (int d = 0; d < kNibbles; ++d) own.digits[d] = digits[d * lanes + from];
+            own.high = highs[from];
+            own.low = lows[from];
+            own.count = counts[from];
         }
-        __syncthreads();
-        i32x4 own[D::digits];
-#pragma unroll
-        for (int d = 0; d < D::digits; ++d) own[d] = digits[d * lanes + cw * G + l];
-        const int32_t start = sums[cw * G + l];
-        const float unit = units[cw * G + l];
-
         auto use = [&](const Load& v, uint32_t q) {
-            int32_t codes[4], dot[D::digits];
-#pragma unroll
-            for (int w = 0; w < 4; ++w) codes[w] = (int32_t)(v.w[w] ^ 0x88888888u);         // code - 8
-#pragma unroll
-            for (int d = 0; d < D::digits; ++d) {
-                dot[d] = 0;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) dot[d] = __builtin_amdgcn_sdot8(codes[w], own[d][w], dot[d], false);
-            }
-            float sum;                                            // sum (2 code - 15) v = 2 sum (code - 8) v + sum v
-            if constexpr (D::digits == 4) {
-                sum = (float)(2 * ((((dot[3] * 16 + dot[2]) * 16 + dot[1]) * 16) + dot[0]) + start);
-            } else {
-                const int32_t high = (dot[5] * 16 + dot[4]) * 16 + dot[3], low = (dot[2] * 16 + dot[1]) * 16 + dot[0];
-                sum = fmaf((float)high, 8192.f, (float)(2 * low + start));
-            }
-            sum = lanes_total<G>((some ? v.scale : 0.f) * unit * sum);
+            const float sum = lanes_total<G>(own.product(v.w, some ? v.scale : 0.f));
             if (l == G - 1) {
                 float* to = mine + q * AT_ONCE + g;
                 *to = slice ? *to + sum : sum;
@@ -774,6 +822,7 @@ void by_tiles(int tiles, bool narrow, F f) {
     };
     if (tiles == 1) with(std::integral_constant<int, 1>());
     else if (tiles == 2) with(std::integral_constant<int, 2>());
+    else if constexpr (kMostTiles<T> == 4) with(std::integral_constant<int, 4>());
     else if (tiles == 4) with(std::integral_constant<int, 4>());
     else with(std::integral_constant<int, 8>());
 }
@@ -797,23 +846,23 @@ ProductPlan product_plan(uint64_t rows, uint64_t cols, uint64_t tokens) {
     ProductPlan p{};
     const int tiles = product_tiles<T>(tokens);
     const uint64_t chunks = (cols + kChunk - 1) / kChunk;
-    if (tiles <= 2) {
+    if (tiles <= kFewTiles<T>) {
         // Two workgroups for every compute unit where each has four stages, otherwise one where it has any: 4 x 16384 x 4096, fp32, 2 parts (256 workgroups)
-        // 17.6 us, 4: 16.2, 6: 16.8; 16 x 20000 x 4096, bf16, blocks of 64, 1 part (157) 26.0, 3: 24.0; 16 x 4096 x 4096 4 parts (128) 14.1, 8 (of two stages)
-        // 10.6, 16: 12.6; 16 x 5000 x 4096 6 parts (240) 13.2, 12: 14.5; 8 x 2048 x 2048 1 part 9.6, 8 (128 workgroups, a stage each): 7.1.
+        // 18.6 us, 4: 17.3, 6: 19.0; 16 x 20000 x 4096, bf16, blocks of 64, 1 part (157) 20.9, 2: 23.5, 3: 21.3; 16 x 4096 x 4096 4 parts (128) 13.1, 8 (of two
+        // stages) 9.3, 16: 10.7; 16 x 5000 x 4096 6 parts (240) 10.6, 12: 12.0; 8 x 2048 x 2048 1 part 10.4, 8 (128 workgroups, a stage each): 7.0.
         const uint64_t stages = (chunks + kStageChunks - 1) / kStageChunks, groups = (rows + 16 * kWaves - 1) / (16 * kWaves);
         p.parts = split(512, groups, stages);
         if (stages < 4 * p.parts) p.parts = split(256, groups, stages);
-        if (stages < 6) p.parts = 1;                              // (a stage takes 0.76 us where there are few workgroups, the launch that joins 2.6)
+        if (stages < 6) p.parts = 1;                              // (a stage takes 1.2 us where there are few workgroups, the launch that joins 2.6)
         p.part_chunks = (uint32_t)((stages + p.parts - 1) / p.parts);
         p.parts = (uint32_t)((stages + p.part_chunks - 1) / p.part_chunks);
         return p;
     }
     const uint64_t height = 16 * kRowTiles * kWaves, groups = (rows + height - 1) / height;
     // Workgroups split the columns until all compute units have one, and not one more, which would take as long again or add to what is joined: 61 x 16001 x
-    // 4099, bf16, 4 parts (252 workgroups) 39.1 us, 8: 48.3; 64 x 65536 x 1024 1 part (256) 25.7, 2: 41.5; 64 x 2048 x 2048, fp32, 4 parts (of four chunks) 14.5,
-    // 16 (128 workgroups, a chunk each) 11.8; 30 x 300 x 1000, bf16, 2 parts 12.7, 8: 10.8.
-    p.parts = chunks < 4 ? 1 : split(256, groups, chunks);        // (a chunk takes a microsecond where there are few workgroups, the launch that joins 2.6)
+    // 4099, bf16, 3 parts 34.6 us, 4 (252 workgroups) 31.8, 8: 41.9; 64 x 65536 x 1024 1 part (256) 21.3, 2: 39.7; 64 x 2048 x 2048, fp32, 4 parts (of four
+    // chunks) 17.2, 16 (128 workgroups, a chunk each) 11.0; 30 x 300 x 1000, bf16, 2 parts 16.8, 8: 10.5.
+    p.parts = chunks < 4 ? 1 : split(256, groups, chunks);        // (a chunk takes 1.5 us where there are few workgroups, the launch that joins 2.6)
     p.part_chunks = (uint32_t)((chunks + p.parts - 1) / p.parts);
     p.parts = (uint32_t)((chunks + p.part_chunks - 1) / p.part_chunks);
     return p;
@@ -825,7 +874,7 @@ bool by_rows(uint64_t tokens, uint64_t cols) { return tokens == 1 && cols > 24; 
 // Scratch: the panel (of product_kernel), then the partial sums.
 template <typename T>
 uint64_t panel_bytes(uint64_t cols, uint64_t tokens, bool narrow) {
-    return product_tiles<T>(tokens) > 2 ? (cols + kChunk - 1) / kChunk * record_bytes<T>(tokens, narrow) : 0;
+    return product_tiles<T>(tokens) > kFewTiles<T> ? (cols + kChunk - 1) / kChunk * record_bytes<T>(tokens, narrow) : 0;
 }
 template <typename T>
 uint64_t scratch_bytes(uint64_t rows, uint64_t cols, uint64_t tokens, bool narrow) {
@@ -854,12 +903,12 @@ void launch_product_tiles(ProductShape a, hipStream_t stream) {
 
 template <typename T, int TT, bool NARROW>
 void launch_product_kernels(ProductShape a, hipStream_t stream) {
-    if constexpr (TT <= 2) {
+    if constexpr (TT <= kFewTiles<T>) {
         launch_product_tiles<T, TT, NARROW>(a, stream);
     } else {
         constexpr uint32_t lds = 2 * Record<T, TT, NARROW>::bytes;
         static_assert(lds <= 64 * 1024, "what a launch may ask for");
-        hipLaunchKernelGGL((product_digits_kernel<T, TT, NARROW>), dim3((unsigned)((a.cols + kChunk - 1) / kChunk), (unsigned)(a.tokens + 15) / 16), dim3(256), 0, stream, a,
+        hipLaunchKernelGGL((product_records_kernel<T, TT, NARROW>), dim3((unsigned)((a.cols + kChunk - 1) / kChunk), (unsigned)(a.tokens + 15) / 16), dim3(256), 0, stream, a,
                            static_cast<uint8_t*>(a.work));
         a.panel = static_cast<const uint8_t*>(a.work);
         over_rows(a.rows, 16 * kRowTiles * kWaves, [&](uint64_t row0, unsigned groups) {
@@ -876,12 +925,13 @@ void launch_product_one(ProductShape a, hipStream_t stream) {
     uint32_t col_waves = 1;
     while (col_waves < kWaves && col_waves < slices) col_waves *= 2;
     a.plan.row_waves = kWaves / col_waves;
-    // Rows enough to be worth writing x in digits for, as long as there is a workgroup for every compute unit: 65536 x 4096, bf16, 8 rows a wave 32.6 us,
-    // 16: 27.9, 32: 28.2, 64: 28.6; 4096 x 16384 8: 15.4 (512 workgroups), 16: 13.2, 32: 16.8 (128); 2048 x 2048 1: 4.1, 4: 4.7, 16: 7.6.
+    // Rows enough to be worth laying x out for, as long as there is a workgroup for every compute unit: 65536 x 4096, bf16, 8 rows a wave 31.6 us,
+    // 16: 28.4, 32: 29.1, 64: 29.4; fp32 8: 42.4, 16: 34.1, 32: 31.3, 64: 34.0; 4096 x 16384, fp16, 8: 10.3 (512 workgroups), 16: 10.0, 32: 14.2 (128);
+    // 2048 x 2048, fp32, 1: 4.6, 4: 5.5, 16: 10.1.
     const uint64_t each = a.rows / (256ull * a.plan.row_waves) / AT_ONCE * AT_ONCE;
     a.plan.wave_rows = (uint32_t)(each < AT_ONCE ? AT_ONCE : each > 32 ? 32 : each);
     const uint64_t rows_here = (uint64_t)a.plan.row_waves * a.plan.wave_rows;
-    const uint32_t bytes = col_waves * G * (Nibbles<T>::digits * 16 + 8) + kWaves * a.plan.wave_rows * 4;
+    const uint32_t bytes = kWaves * a.plan.wave_rows * 4 + (sizeof(T) == 4 ? col_waves * G * (kNibbles * 16 + 12) : 0);
     over_rows(a.rows, rows_here, [&](uint64_t row0, unsigned groups) {
         a.row0 = row0;
         hipLaunchKernelGGL((product_one_kernel<T, G>), dim3(groups), dim3(kThreads), bytes, stream, a);

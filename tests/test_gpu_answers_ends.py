@@ -46,7 +46,7 @@ def test_one_token_through_wide_rows(cols, block, dtype):
 
 # Few tokens, 256 columns at a time: a row ends with them, or a word, two or more behind them; rows below, at and above the 128 of a workgroup;
 # 66 tokens: the last two are a launch of their own.
-@pytest.mark.parametrize("dtype", [F32])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("block", [64, 128, 256, 512])
 @pytest.mark.parametrize("tokens,rows,cols", [(2, 100, 257), (8, 128, 264), (16, 129, 265), (8, 131, 513), (3, 300, 4100), (2, 40, 256), (5, 7, 520),
                                               (8, 260, 521), (66, 130, 260)])

@@ -1,0 +1,141 @@
+"""Products with inputs whose sizes differ: outliers among hidden states, columns that shrink by powers of two, numbers near the ends of
+their types.  Against 64 bits.
+
+Tolerances, U = 2^-24.
+  16-bit dtypes  x is an operand as it is, a code counts as 0.5 + q / 32 and 47/64 sum x is taken off, all in fp32: 31/30 of the largest
+                 |2 code - 15| at most.  n roundings with signs of their own, each U times a partial sum: 8 U of sum |31 x unit|.
+  fp32           x is 2^e v with integers v below 2^31, e of 128 columns (one token: 32): half a unit of v is 2^-31 of the block's largest |x| at
+                 most (limits lie just below 2^31 and twice below what x reaches), times |2 code - 15| unit for each column.  Then some eight
+                 roundings of a block's sum, and one of each partial sum of blocks: (8 + 2 sqrt(blocks)) U of sum |block's sum|.
+  the gradient   8 U and, for 16-bit dtypes, 2^-17 of sum |31 dy unit|, as in test_gpu_answers.py.
+Then the rounding to the output's type."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1907_07346_amd import binding as b
+from tests import answers_plain as plain
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+def matrix(rng, rows, cols, block, codes=None, scale=1.0):
+    msg, q, scales = plain.random_message(rows, cols, block, rng, lambda shape, r: (r.random(shape) + 0.01) * scale)
+    if codes is not None:                                         # ... of which these columns have the codes nearest zero
+        q[:, codes] = rng.integers(7, 9, (rows, len(codes)))
+        data = np.frombuffer(msg.numpy().tobytes(), np.uint8).reshape(rows, -1).copy()
+        for c in codes:
+            at = c // block * (4 + block // 2) + 4 + c % block // 2
+            low = c % 2 == 0
+            data[:, at] = (data[:, at] & (0xF0 if low else 0x0F)) | (q[:, c] if low else q[:, c] << 4)
+        msg = torch.from_numpy(data.reshape(-1))
+        assert torch.allclose(plain.decode(msg.numpy(), rows, cols, block), plain.dense(q, scales, block), rtol=1e-14, atol=0.0)
+    unit = torch.from_numpy(np.repeat(scales.astype(np.float64), block, axis=1)[:, :cols] / 15.0)
+    return msg, plain.dense(q, scales, block), unit
+
+
+def tolerance(x, m, unit, dtype, block):
+    want = x @ m.t().contiguous()
+    if dtype != F32:
+        return want, 8 * U * 31.0 * (x.abs() @ unit.t().contiguous()) + plain.rounding(want, dtype)
+    chunk = 32 if x.shape[0] == 1 else min(block, 128)
+    blocks = math.ceil(x.shape[1] / chunk)
+    grid, sums = torch.zeros_like(want), torch.zeros_like(want)
+    for lo in range(0, x.shape[1], chunk):
+        part, w = x[:, lo:lo + chunk], m[:, lo:lo + chunk].t().contiguous()
+        grid += 2.0 ** -31 * part.abs().amax(dim=1, keepdim=True) * w.abs().sum(dim=0)
+        sums += (part @ w).abs()
+    return want, grid + (8 + 2 * math.sqrt(blocks)) * U * sums + plain.rounding(want, dtype)
+
+
+def check(tokens, rows, cols, block, dtype, x, msg, m, unit, what):
+    got = b.ds_product(msg.cuda(), x.cuda(), rows, block).cpu().double()
+    want, tol = tolerance(x.double(), m, unit, dtype, block)
+    off = (got - want).abs()
+    bad = ~(off <= tol)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, by up to {(off / tol).max():.2f} of the tolerance"
+
+
+SHAPES = [(1, 200, 1000, 128), (1, 77, 4100, 64), (1, 40, 300, 2048), (1, 33, 120, 64), (2, 130, 700, 64), (8, 100, 512, 512), (8, 140, 1024, 256), (16, 64, 2048, 128),
+          (30, 100, 900, 64), (40, 300, 640, 128), (61, 90, 4099, 1024)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("tokens,rows,cols,block", SHAPES)
+def test_products_of_inputs_with_outliers(tokens, rows, cols, block, dtype):
+    rng = np.random.default_rng(tokens * 31 + cols)
+    where = list(range(5, cols, 128))                             # a column in every chunk is 100 and 3000 times the others, and meets codes near zero
+    msg, m, unit = matrix(rng, rows, cols, block, where)
+    for times in (1.0, 100.0, 3000.0):
+        x = rng.standard_normal((tokens, cols))
+        x[:, where] *= times
+        check(tokens, rows, cols, block, dtype, torch.from_numpy(x).to(dtype), msg, m, unit, f"outliers of {times}")
+    x = np.full((tokens, cols), 0.0149)                           # all of one sign, so that what they lose adds up
+    x[:, where] = 1000.0
+    check(tokens, rows, cols, block, dtype, torch.from_numpy(x).to(dtype), msg, m, unit, "one sign")
+    x = rng.standard_normal((tokens, cols)) * 2.0 ** -(np.arange(cols) % 16.0)
+    check(tokens, rows, cols, block, dtype, torch.from_numpy(x).to(dtype), msg, m, unit, "powers of two")
+
+
+@pytest.mark.parametrize("tokens", [1, 8, 40])
+@pytest.mark.parametrize("dtype,scale,size", [(F32, 1e-18, 1e-18), (F32, 1e25, 1e-35), (F32, 1e-30, 1e30), (F32, 1e30, 1e-42), (BF16, 1e-18, 1e-18), (BF16, 1e25, 1e-35),
+                                              (BF16, 1e-30, 1e30), (F16, 1.0, 3e-6), (F16, 1e6, 1e-7), (F16, 1e-3, 3e4)])
+def test_products_near_the_ends_of_the_types(tokens, dtype, scale, size):
+    """Subnormal inputs among them; no product or partial sum is beyond fp32 where y is not."""
+    rng = np.random.default_rng(tokens)
+    rows, cols, block = 50, 700, 128
+    msg, m, unit = matrix(rng, rows, cols, block, scale=scale)
+    x = torch.from_numpy(np.clip(rng.standard_normal((tokens, cols)), -2, 2) * size).to(dtype)
+    check(tokens, rows, cols, block, dtype, x, msg, m, unit, f"{scale} x {size}")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_a_token_alone_and_among_others(dtype):
+    """Tokens do not share exponents: alone, among few and among many a token's product differs by the order of its sum alone."""
+    rng = np.random.default_rng(8)
+    rows, cols, block = 150, 1500, 256
+    msg, m, unit = matrix(rng, rows, cols, block, list(range(9, cols, 200)))
+    x = torch.from_numpy(rng.standard_normal((50, cols)) * np.where(np.arange(cols) % 200 == 9, 300.0, 1.0)).to(dtype)
+    many, few = b.ds_product(msg.cuda(), x.cuda(), rows, block), b.ds_product(msg.cuda(), x[:7].cuda(), rows, block)
+    want, tol = tolerance(x.double(), m, unit, dtype, block)
+    for t in range(7):
+        one = b.ds_product(msg.cuda(), x[t:t + 1].cuda(), rows, block)
+        for y in (one[0], few[t], many[t]):
+            assert ((y.cpu().double() - want[t]).abs() <= tol[t]).all()
+
+
+def through(dy, m, unit, dtype):
+    """The gradient, and how far it may be off."""
+    want = dy @ m
+    if dtype != F32:
+        return want, (8 * U + 2.0 ** -17) * 31.0 * (dy.abs() @ unit) + plain.rounding(want, dtype)
+    # Every 32 rows some 24 roundings, each U times a partial sum of terms of 47 dy unit or so that differ in sign: the root of their squares' sum, of all rows,
+    # four times as much for the largest of many.  (A piece less would be off by 2^-17 9 / sqrt(3) of that root: as much for the first of twenty results.)
+    return want, 4 * math.sqrt(24) * 47 * U * ((dy * dy) @ (unit * unit)).sqrt() + plain.rounding(want, dtype)
+
+
+@pytest.mark.parametrize("tokens,rows,cols,block", [(3, 2000, 300, 64), (16, 1000, 500, 256), (20, 700, 1000, 128), (40, 4000, 130, 2048)])
+def test_gradients_of_fp32_keep_24_bits(tokens, rows, cols, block):
+    rng = np.random.default_rng(rows)
+    msg, m, unit = matrix(rng, rows, cols, block)
+    dy = torch.from_numpy(rng.standard_normal((tokens, rows))).float()
+    want, tol = through(dy.double(), m, unit, F32)
+    off = (b.ds_product_gradient(msg.cuda(), dy.cuda(), cols, block).cpu().double() - want).abs()
+    assert (off <= tol).all(), f"off by up to {(off / tol).max():.2f} of the tolerance"
+
+
+@pytest.mark.parametrize("tokens", [1, 8, 40])
+@pytest.mark.parametrize("dtype,scale,size", [(F32, 1e-15, 1e-12), (F32, 1e20, 1e-35), (F32, 1e-25, 1e30), (BF16, 1e-15, 1e-15), (BF16, 1e20, 1e-35), (BF16, 1e-25, 1e30),
+                                              (F16, 1.0, 3e-6), (F16, 1e6, 1e-7), (F16, 1e-3, 3e4)])
+def test_gradients_near_the_ends_of_the_types(tokens, dtype, scale, size):
+    rng = np.random.default_rng(tokens)
+    rows, cols, block = 600, 150, 64
+    msg, m, unit = matrix(rng, rows, cols, block, scale=scale)
+    dy = torch.from_numpy(np.clip(rng.standard_normal((tokens, rows)), -2, 2) * size).to(dtype)
+    want, tol = through(dy.double(), m, unit, dtype)
+    off = (b.ds_product_gradient(msg.cuda(), dy.cuda(), cols, block).cpu().double() - want).abs()
+    assert (off <= tol).all(), f"{scale} x {size}: off by up to {(off / tol).max():.2f} of the tolerance"
