@@ -187,6 +187,16 @@ __device__ __forceinline__ uint32_t largest_bits(const float (&v)[N]) {
     return most;
 }
 
+// Byte b of four words, as word b.
+__device__ __forceinline__ void transpose_bytes(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3, uint32_t (&out)[4]) {
+    const uint32_t a = __builtin_amdgcn_perm(w1, w0, 0x05010400u), b = __builtin_amdgcn_perm(w3, w2, 0x05010400u);
+    const uint32_t c = __builtin_amdgcn_perm(w1, w0, 0x07030602u), d = __builtin_amdgcn_perm(w3, w2, 0x07030602u);
+    out[0] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+    out[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    out[2] = __builtin_amdgcn_perm(d, c, 0x05040100u);
+    out[3] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+}
+
 // Sixteen adjacent lanes, lane u with columns 8 u .. 8 u + 7 of a chunk (raw), write a token's part of the chunk's record.
 template <typename T, int TT, bool NARROW>
 __device__ void make_record(uint32_t tok, uint32_t u, typename EightOf<T>::Raw raw, uint8_t* record) {
@@ -213,12 +223,10 @@ __device__ void make_record(uint32_t tok, uint32_t u, typename EightOf<T>::Raw r
         for (int e = 0; e < 8; ++e) v[e] = (uint32_t)(finite ? (int32_t)rintf(ldexpf(x[e], power)) : 0) + 0x808080u;
 #pragma unroll
         for (int o = 0; o < 2; ++o) {
-            const uint32_t a = __builtin_amdgcn_perm(v[2 + o], v[o], 0x05010400u), b = __builtin_amdgcn_perm(v[6 + o], v[4 + o], 0x05010400u);
-            const uint32_t c = __builtin_amdgcn_perm(v[2 + o], v[o], 0x07030602u), d = __builtin_amdgcn_perm(v[6 + o], v[4 + o], 0x07030602u);
-            bytes[3][o] = __builtin_amdgcn_perm(b, a, 0x05040100u) ^ 0x80808080u;
-            bytes[2][o] = __builtin_amdgcn_perm(b, a, 0x07060302u) ^ 0x80808080u;
-            bytes[1][o] = __builtin_amdgcn_perm(d, c, 0x05040100u) ^ 0x80808080u;
-            bytes[0][o] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+            uint32_t lowest_first[4];
+            transpose_bytes(v[o], v[2 + o], v[4 + o], v[6 + o], lowest_first);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) bytes[d][o] = lowest_first[3 - d] ^ (d ? 0x80808080u : 0u);
         }
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
@@ -723,21 +731,27 @@ __global__ void __launch_bounds__(kThreads) product_one_kernel(ProductShape a) {
                 }
                 const int power = power_of(most, kMostNibbles);
                 const bool finite = most < 0x7F800000u;
-                uint32_t out[kNibbles];
+                // 2^power x, rounded, plus 8 in all digits: its digits of four bits are the signed ones plus 8, whose highest bits are turned over
+                uint32_t out[kNibbles], nibbles[8];
                 int32_t high = 0, low = 0;
 #pragma unroll
-                for (int d = 0; d < kNibbles; ++d) out[d] = 0;
-#pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    int32_t rest = finite ? (int32_t)rintf(ldexpf(v[e], power)) : 0;
-                    high += rest >> 16;
-                    low += rest & 0xFFFF;
+                    const int32_t rounded = finite ? (int32_t)rintf(ldexpf(v[e], power)) : 0;
+                    high += rounded >> 16;
+                    low += rounded & 0xFFFF;
+                    nibbles[e] = ((uint32_t)rounded + 0x88888888u) ^ 0x88888888u;
+                }
+                // digit d of column e to place e of word d, the lowest digit first
 #pragma unroll
-                    for (int d = 0; d < kNibbles; ++d) {          // the first digit is the lowest; signed, [-8, 7]
-                        const int32_t digit = (int32_t)((uint32_t)rest << 28) >> 28;
-                        rest = (rest - digit) >> 4;
-                        out[d] |= ((uint32_t)digit & 15u) << (4 * e);
-                    }
+                for (int odd = 0; odd < 2; ++odd) {
+                    uint32_t pair[4], word[4];
+#pragma unroll
+                    for (int p = 0; p < 4; ++p)
+                        pair[p] = odd ? (nibbles[2 * p] >> 4 & 0x0F0F0F0Fu) | (nibbles[2 * p + 1] & 0xF0F0F0F0u)
+                                      : (nibbles[2 * p] & 0x0F0F0F0Fu) | (nibbles[2 * p + 1] << 4 & 0xF0F0F0F0u);
+                    transpose_bytes(pair[0], pair[1], pair[2], pair[3], word);
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) out[2 * b + odd] = word[b];
                 }
                 const uint32_t place = (w % 4 + missing_words(slice + w / 4 * kLaneCols, a.cols)) % 4;
 #pragma unroll
@@ -926,12 +940,14 @@ void launch_product_one(ProductShape a, hipStream_t stream) {
     while (col_waves < kWaves && col_waves < slices) col_waves *= 2;
     a.plan.row_waves = kWaves / col_waves;
     // Rows enough to be worth laying x out for, as long as there is a workgroup for every compute unit: 65536 x 4096, bf16, 8 rows a wave 31.6 us,
-    // 16: 28.4, 32: 29.1, 64: 29.4; fp32 8: 42.4, 16: 34.1, 32: 31.3, 64: 34.0; 4096 x 16384, fp16, 8: 10.3 (512 workgroups), 16: 10.0, 32: 14.2 (128);
-    // 2048 x 2048, fp32, 1: 4.6, 4: 5.5, 16: 10.1.
+    // 16: 28.4, 32: 29.1, 64: 29.4; fp32 8: 38.0, 16: 32.8, 32: 31.5, 64: 33.6; 4096 x 16384, fp16, 8: 10.3 (512 workgroups), 16: 10.0, 32: 14.2 (128);
+    // fp32 8: 15.8, 16: 14.1, 32: 18.8; 2048 x 2048, fp32, 1: 4.2, 4: 5.2, 16: 9.7.
     const uint64_t each = a.rows / (256ull * a.plan.row_waves) / AT_ONCE * AT_ONCE;
     a.plan.wave_rows = (uint32_t)(each < AT_ONCE ? AT_ONCE : each > 32 ? 32 : each);
     const uint64_t rows_here = (uint64_t)a.plan.row_waves * a.plan.wave_rows;
     const uint32_t bytes = kWaves * a.plan.wave_rows * 4 + (sizeof(T) == 4 ? col_waves * G * (kNibbles * 16 + 12) : 0);
+    if (bytes > 64 * 1024)                                        // (fp32 and more than 8192 columns: 70 KB of digits; without it a launch may ask for 64 KB)
+        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(product_one_kernel<T, G>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     over_rows(a.rows, rows_here, [&](uint64_t row0, unsigned groups) {
         a.row0 = row0;
         hipLaunchKernelGGL((product_one_kernel<T, G>), dim3(groups), dim3(kThreads), bytes, stream, a);
