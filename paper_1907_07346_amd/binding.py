@@ -276,8 +276,9 @@ def _new(stream, shape, dtype, like):
         return like.new_empty(shape, dtype=dtype)
 
 
-def _answer(name: str, work_bytes, call, shape, like, here: int, stream, *args):
-    """Makes the call with scratch memory of its stream; the reason of a refusal goes into the exception."""
+def _answer(name: str, work_bytes, call, shape, given, here: int, stream, *args):
+    """Makes the call with scratch memory of its stream; the reason of a refusal goes into the exception.  given: the caller's tensors (the
+    first is the scratch memory's pattern), whose memory, freed by its own stream, must wait for another one that the call runs on."""
     if stream is None:
         pointer = _raw_stream(here) if _raw_stream is not None else _stream_pointer(None)
     elif stream.device_index != here:
@@ -285,13 +286,17 @@ def _answer(name: str, work_bytes, call, shape, like, here: int, stream, *args):
     else:
         pointer = stream.cuda_stream
     size = work_bytes(shape)
-    work = _new(stream, (size,), torch.uint8, like) if size else None
+    work = _new(stream, (size,), torch.uint8, given[0]) if size else None
     at = work.data_ptr() if size else None
     st = call(shape, *args, at, size, pointer, None, 0)
     if st == DS_EINVAL:                                   # (checks only: nothing has been enqueued)
         buf = ctypes.create_string_buffer(256)
         call(shape, *args, at, size, pointer, buf, 256)
         raise DsqError(st, name, buf.value.decode())
+    if stream is not None:
+        for t in given:
+            if t is not None:
+                t.record_stream(stream)
     if st != DS_OK:
         raise DsqError(st, name)
 
@@ -319,7 +324,7 @@ def _through(name: str, work_bytes, call, msg: "torch.Tensor", x: "torch.Tensor"
     else:
         out_pitch = _rows_of(name, "out", out)[2]
     if tokens:
-        _answer(name, work_bytes, call, m, x, here, stream, msg.data_ptr(), x.data_ptr(), pitch, out.data_ptr(), out_pitch)
+        _answer(name, work_bytes, call, m, (x, msg, out), here, stream, msg.data_ptr(), x.data_ptr(), pitch, out.data_ptr(), out_pitch)
     return out
 
 
@@ -349,7 +354,7 @@ def ds_top_logits(z: "torch.Tensor", k: int, temperature: float = 1.0, stream: O
     if rows:
         L = lib()
         _answer("ds_top_logits", L.ds_top_logits_work_bytes, L.ds_top_logits,
-                ctypes.byref(ds_logits(rows, vocab, k, _DTYPES[z.dtype], temperature, 0)), z, here, stream,
+                ctypes.byref(ds_logits(rows, vocab, k, _DTYPES[z.dtype], temperature, 0)), (z,), here, stream,
                 z.data_ptr(), pitch, pairs.data_ptr(), lse.data_ptr())
     return pairs, lse
 
@@ -379,7 +384,7 @@ def ds_distill(z: "torch.Tensor", pairs: "torch.Tensor", temperature: float = 1.
     if rows:
         L = lib()
         _answer("ds_distill", L.ds_distill_work_bytes, L.ds_distill,
-                ctypes.byref(ds_logits(rows, vocab, pairs.shape[1], _DTYPES[z.dtype], temperature, 0)), z, here, stream,
+                ctypes.byref(ds_logits(rows, vocab, pairs.shape[1], _DTYPES[z.dtype], temperature, 0)), (z, pairs, teacher_lse, weight, dz), here, stream,
                 z.data_ptr(), pitch, pairs.data_ptr(), *given, loss.data_ptr() if want_loss else None, dz.data_ptr() if want_gradient else None, dz_pitch)
     return loss, dz
 
