@@ -383,7 +383,7 @@ uint64_t ds_matrix_bytes(const ds_matrix* m);
  * msg_dev: ds_matrix_bytes(m) bytes, 4-byte aligned.  x_dev: tokens rows of pitch x_ld >= cols elements; y_dev: tokens rows of
  * pitch y_ld >= rows elements (columns behind `rows` are left as they were); both of m->dtype and aligned to their elements.  Products are summed in fp32 and
  * rounded once to dtype; for DS_F32, x first to multiples of 2^-31 (at most) of the largest |x| of the 128 columns around it (32 for one token), which are summed
- * exactly.  Infinities and NaN in x go where the formula takes them. */
+ * exactly.  Infinities and NaN in x go where the formula takes them; results that are not finite take far longer, a thread each. */
 uint64_t ds_product_work_bytes(const ds_matrix* m);
 ds_status ds_product(const ds_matrix* m, const void* msg_dev, const void* x_dev, uint64_t x_ld, void* y_dev, uint64_t y_ld,
                      void* work_dev, uint64_t work_bytes, void* hip_stream, char* errbuf, uint64_t errbuf_len);

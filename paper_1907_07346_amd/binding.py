@@ -487,7 +487,8 @@ class DeepSqueeze:
                    stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
         """x (tokens, cols) through parameters first .. first + rows * cols - 1 of `worker` as the message of the last ds_step holds
         them (4-bit QUANT_MAXABS and DeepSqueeze's own update, whose messages are parameters; first and cols multiples of the block).  Some launch plans alternate between two message buffers:
-        the call then waits for the last ds_step (see ds_message_ptr)."""
+        the call then waits for the last ds_step (see ds_message_ptr).  Otherwise the order is the caller's: the call runs on `stream`, which
+        must be the last ds_step's or wait for it, and the next ds_step must not overtake the call."""
         return ds_product(self._matrix("ds_product", worker, rows, x.shape[-1], first), x, rows, self.cfg.comp.block, out, stream)
 
     def ds_product_gradient(self, worker: int, dy: "torch.Tensor", cols: int, first: int = 0, out: "Optional[torch.Tensor]" = None,

@@ -3,9 +3,10 @@
 // Bound by reading the logits once and writing their gradient once.  A row stays in the registers of its workgroup between the sum of exponentials
 // and the gradient (up to 256 KB: 1024 threads of 64 registers); the threads' number follows the row's length.  A workgroup takes one row after the other,
 // and asks for the next row's logits as it writes: 16 bytes of gradient, and the registers they came from wait for 16 bytes of logits.  Where rows
-// are longer, or too few to fill the GPU, they are split: a first launch sums the parts, a second one reads the logits again (out of the
-// memory-side cache, mostly) and writes the gradient.
-//   4096 x 131072, bf16: 439 us, 4.9 TB/s in and out; 1023 x 50001, fp16: 49 us, 4.2, in two rows of each workgroup, the first of which is waited for.  The
+// are longer, or too few to fill the GPU, they are split: a first launch sums the parts, a second one reads the logits again and writes the gradient.  The
+// second read comes out of the memory-side cache where the call's logits fit it (100 x 200003, bf16: 30 us), otherwise from memory: 4096 x 151936, bf16,
+// 773 us, three passes of 1.2 GB at 4.8 TB/s; 2048 x 100000, fp32, 486 us.
+//   4096 x 131072, bf16: 440 us, 4.9 TB/s in and out; 1023 x 50001, fp16: 49 us, 4.2, in two rows of each workgroup, the first of which is waited for.  The
 // exponentials are made twice, which with their arguments is most of the instructions: of 16 bits there is no room to keep them.
 //   The listed columns are written once more, after the dense part, by the thread that has the first of the entries with that index.
 #include "dsq_answers.h"

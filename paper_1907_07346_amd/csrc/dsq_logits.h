@@ -17,7 +17,6 @@ __device__ __forceinline__ uint32_t logit_key(float z) {
     return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
 }
 __device__ __forceinline__ uint64_t logit_rank(float z, uint32_t index) { return (uint64_t)logit_key(z) << 32 | (uint32_t)~index; }
-__device__ __forceinline__ uint32_t rank_index(uint64_t rank) { return ~(uint32_t)rank; }
 
 // 2^x as the hardware has it: results below 2^-126 are 0.
 __device__ __forceinline__ float power2(float x) { return __builtin_amdgcn_exp2f(x); }

