@@ -143,7 +143,8 @@ __device__ __forceinline__ void load_codes_tail(Codes<NARROW>& c, const uint8_t*
 
 // 2^p, for p from -126 to 127.
 __device__ __forceinline__ float power2_of(int p) { return __uint_as_float((uint32_t)(p + 127) << 23); }
-// The largest p for which 2^p x is at most `limit`, just below 2^31, of an |x| with these bits: -97 to 149 (2^149 makes an integer of any x).
+// The largest p for which 2^p x is at most `limit`, just below 2^31, of an |x| with these bits: -98 to 149 (2^149 makes an integer of any x).  At -98, for |x| of
+// 3.1e38 and more, 2^(kExponent - p) is infinite, and results are made in order.
 __device__ __forceinline__ int power_of(uint32_t bits, float limit) {
     const int p = kExponent + 127 - (int)(bits >> 23), q = p > 149 ? 149 : p;
     return ldexpf(__uint_as_float(bits), q) > limit ? q - 1 : q;

@@ -102,6 +102,27 @@ def test_teachers_and_students_with_a_common_offset(offset):
     assert ((loss.cpu().double() - want_loss).abs() <= tol).all(), ((loss.cpu().double() - want_loss).abs() / tol).max()
 
 
+@pytest.mark.parametrize("temperature", [0.5, 1.0, 4.0])
+def test_teachers_whose_entries_are_masked(temperature):
+    """Entries of any size of mask, beside usual ones and by themselves: alike ones share the probability."""
+    rng = np.random.default_rng(5)
+    vocab, k = 900, 130
+    values = []
+    for a, c in ((-1e10, 0.0), (-1e10, -1e10), (-1e30, -1e30), (LOWEST, LOWEST), (LOWEST, -1e38), (-1e38, LOWEST), (-2.3e38, -2.4e38), (2.4e38, 2.3e38), (-1e20, LOWEST)):
+        v = np.where(np.arange(k) < 70, a, c + (rng.standard_normal(k) if c == 0 else 0.0))
+        values += [v, rng.permutation(v)]
+    value = torch.from_numpy(np.stack(values)).float()
+    rows = value.shape[0]
+    z = torch.from_numpy(rng.standard_normal((rows, vocab))).float()
+    index = torch.from_numpy(np.stack([rng.permutation(vocab)[:k] for _ in range(rows)])).long()
+    loss, dz = b.ds_distill(z.cuda(), pack_pairs(index, value).cuda(), temperature)
+    want_loss, want = plain.distill(z, index, value, temperature)
+    rel = U * (64 + 4 * 100)
+    tol = rel * (plain.log_softmax(z.double() / temperature).exp() / temperature + want.abs()) + 2.0 ** -126 / temperature + plain.rounding(want, F32)
+    assert ((dz.cpu().double() - want).abs() <= tol).all()
+    assert ((loss.cpu().double() - want_loss).abs() <= rel * (16 + math.log(vocab))).all()       # (every -ln p and -ln q of a probable entry is below 16)
+
+
 def test_temperatures_that_have_no_reciprocal_are_refused():
     z, pairs = torch.zeros((2, 50), device="cuda"), torch.zeros((2, 3, 2), dtype=torch.int32, device="cuda")
     for call in (lambda: b.ds_top_logits(z, 3, 1e-39), lambda: b.ds_distill(z, pairs, 1e-39)):

@@ -139,3 +139,17 @@ def test_gradients_near_the_ends_of_the_types(tokens, dtype, scale, size):
     want, tol = through(dy.double(), m, unit, dtype)
     off = (b.ds_product_gradient(msg.cuda(), dy.cuda(), cols, block).cpu().double() - want).abs()
     assert (off <= tol).all(), f"{scale} x {size}: off by up to {(off / tol).max():.2f} of the tolerance"
+
+
+@pytest.mark.parametrize("tokens", [1, 5, 20])
+def test_products_of_the_largest_numbers(tokens):
+    """fp32's last binade, whose block counts by a power that fp32 does not have, next to a token and a block of ordinary numbers."""
+    rng = np.random.default_rng(tokens)
+    rows, cols, block = 70, 300, 64
+    msg, m, unit = matrix(rng, rows, cols, block, scale=1e-6)
+    x = torch.from_numpy(np.clip(rng.standard_normal((tokens, cols)), -2, 2)).float()
+    x[0, 3], x[0, 200] = 3.4e38, -3.2e38
+    got = b.ds_product(msg.cuda(), x.cuda(), rows, block).cpu().double()
+    want = x.double() @ m.t().contiguous()
+    tol = 8 * U * (x.double().abs() @ m.t().abs().contiguous()) + plain.rounding(want, F32)                   # in order: U of sum |term| a step
+    assert ((got - want).abs() <= tol).all()
