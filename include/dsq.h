@@ -389,7 +389,8 @@ ds_status ds_product(const ds_matrix* m, const void* msg_dev, const void* x_dev,
                      void* work_dev, uint64_t work_bytes, void* hip_stream, char* errbuf, uint64_t errbuf_len);
 
 /* dx[t][c] = sum over r of dy[t][r] * (scale(r, c) / 15) * (2 code(r, c) - 15): the gradient of ds_product with respect to x.
- * dy * scale / 15 is rounded before, by at most 2^-17 of itself for 16-bit dtypes and 2^-24 for DS_F32; sums are fp32, rounded once to dtype.
+ * dy * scale / 15 is rounded before, by at most 2^-17 of itself for 16-bit dtypes and 2^-24 for DS_F32, or by 2^-134 where that is more; sums are fp32,
+ * rounded once to dtype.
  * dy_dev: tokens rows of pitch dy_ld >= rows elements; dx_dev: tokens rows of pitch dx_ld >= cols elements; otherwise as ds_product. */
 uint64_t ds_product_gradient_work_bytes(const ds_matrix* m);
 ds_status ds_product_gradient(const ds_matrix* m, const void* msg_dev, const void* dy_dev, uint64_t dy_ld, void* dx_dev,

@@ -5,8 +5,8 @@
 // what that is too large by is where sums start: -47/64 sum x of a block.  Products are exact and sums are fp32; a block's scale multiplies its sum.
 //   fp32: x is made of bytes, and the products are integers: per token and 128 columns ("chunk"; 64 where a block is 64), x = 2^e v with integers v of 32
 // bits, written as four signed bytes, which an i8 matrix instruction takes as rows of their own, against codes as bytes.  All sums inside a chunk are exact; 15 sum v,
-// which takes codes 0 .. 15 to 2 code - 15, is where they start.  What is rounded is v: 2^-31 of the largest |x| next to it at most, which the same
-// block's scale multiplies and no code drops: below 2^-24 of what that one contributes, 1/15 of it or more, unless a hundred of them agree in sign.
+// which takes codes 0 .. 15 to 2 code - 15, is where they start.  What is rounded is v: by 2^-31 of the largest |x| next to it at most, of which
+// y has 1/15 of the scale or more: no rounding is above 2^-27 of what that one contributes.
 //   A wave takes 16 (or 32) rows and a chunk at a time: lane (n, j) = (l % 16, l / 16) holds 32 codes of row n and the scale of its block, which is
 // one factor for all of the lane's results.  x lies in LDS in the order in which codes come out of a word.
 //   Three kernels.  One token: product_one_kernel.  Up to 16 tokens (8 for fp32), where reading codes is most of the work:
@@ -53,7 +53,7 @@ struct ProductPlan {
 struct ProductShape : ProductArgs {
     ProductPlan plan;
     uint64_t row0;
-    const uint8_t* panel;                                         // x as bytes, one record per chunk (see Record), or nullptr
+    const uint8_t* panel;                                         // x laid out, one record per chunk (see Record), or nullptr
     float* partial;                                               // parts x tokens x rows, or nullptr
 };
 

@@ -1,7 +1,7 @@
 // The gradient of ds_product with respect to its vectors (ds_product_gradient): dx = dy M, M's rows as 4-bit codes with a scale per block.
 //
 // The sum runs over the matrix's rows, so the scales belong to what is summed: dy * scale is the other operand, made anew for every block
-// of columns and rounded to bf16 pieces (two for 16-bit dtypes, 2^-17 relative, three for fp32: 24 bits).  A wave takes 128 columns and 32
+// of columns and rounded to bf16 pieces (two for 16-bit dtypes, 2^-17 relative, three for fp32: 24 bits; the smallest bf16 is 2^-133).  A wave takes 128 columns and 32
 // rows at a time: lane (n, j) loads word n (eight columns) of rows 8 j .. 8 j + 7, and column c of all words, c = 0 .. 7, is one matrix
 // instruction: codes of two rows sit in the halves of a register after one byte permutation, two more instructions make operands of two (dsq_codes.h).
 // The waves of a workgroup and the workgroups of a column take different rows; the waves join in LDS, the workgroups through fp32 partial sums in
