@@ -69,8 +69,12 @@ __device__ Teacher read_teacher(const LogitsArgs& a, uint64_t row, uint2 pair, f
 }
 
 // The entry's share of the loss.
-__device__ __forceinline__ float listed_term(const Teacher& e, LogSum l, float temperature) {
-    return e.p != 0.f ? e.p * (e.log_p - (e.z - l.from) / temperature + l.rest) : 0.f;
+__device__ __forceinline__ float listed_term(const Teacher& e, LogSum l, float temperature, float weight) {
+    if (e.p == 0.f) return 0.f;
+    const float q = (e.z - l.from) / temperature;
+    if (fabsf(q) != kInf || fabsf(e.z) == kInf) return weight * (e.p * (e.log_p - q + l.rest));
+    // q is beyond fp32 (a mask of the lowest value, T < 1): weight p q may not be
+    return weight * (e.p * (e.log_p + l.rest)) - weight * (2.f * e.p) / temperature * (0.5f * e.z - 0.5f * l.from);
 }
 
 // The row's entries in LDS.
@@ -181,8 +185,8 @@ __global__ void __launch_bounds__(THREADS) distill_row_kernel(DistillShape a) {
             s = workgroup_spread<WAVES>(s, scale, sums);
             const LogSum l = log_sum(s, scale);
             if (a.loss) {
-                const float terms = workgroup_total<WAVES>(listed_term(teacher, l, a.temperature), sums);
-                if (threadIdx.x == 0) a.loss[row] = teacher.mass == 0.f ? 0.f : weight * terms;
+                const float terms = workgroup_total<WAVES>(listed_term(teacher, l, a.temperature, weight), sums);
+                if (threadIdx.x == 0) a.loss[row] = teacher.mass == 0.f ? 0.f : terms;
             }
             g = {exponents(s.max, scale), weight / a.temperature * teacher.mass / s.sum, weight / a.temperature};
             skip = teacher.mass == 0.f;
@@ -299,8 +303,8 @@ __global__ void __launch_bounds__(kPartThreads) distill_part_kernel(DistillShape
         const LogSum l = log_sum(s, scale);
         skip = teacher.mass == 0.f;
         if (a.loss && blockIdx.y == 0) {
-            const float terms = workgroup_total<kPartWaves>(listed_term(teacher, l, a.temperature), sums);
-            if (threadIdx.x == 0) a.loss[row] = skip ? 0.f : weight * terms;
+            const float terms = workgroup_total<kPartWaves>(listed_term(teacher, l, a.temperature, weight), sums);
+            if (threadIdx.x == 0) a.loss[row] = skip ? 0.f : terms;
         }
         g = {exponents(s.max, scale), weight / a.temperature * teacher.mass / s.sum, weight / a.temperature};
     } else if (a.loss && blockIdx.y == 0 && threadIdx.x == 0) {

@@ -4,8 +4,7 @@ exponents past what fp32 holds, teachers whose logits share a large offset.  Aga
 Tolerances.  U = 2^-24.  A term 2^((z - max) log2(e) / T) is off by 4 U d + 16 U of itself, d = (max - z) / T in units of e (the product's and the
 exponential's rounding and the sum's).  The hardware's 2^x is 0 below 2^-126: a gradient, which is a term over T and over a sum of 1 or
 more, may lack 2^-126 / T.  (Terms of 1e-38 of the largest, which 1e-40 / T left no room for.)  ln of the sum: the terms', and roundings at the size of
-the result, of max / T and of ln V.  A loss whose listed entry has -ln q = (max - z) / T past 3.4e38, which fp32 has no number for, may be infinite though p
-times it is not."""
+the result, of max / T and of ln V.  A loss past 3.4e38 has no number in fp32; p times -ln q = (max - z) / T below that has one, whatever -ln q is."""
 import math
 
 import numpy as np
@@ -62,10 +61,12 @@ def test_sums_of_logits_far_apart(dtype, vocab, temperature):
     index = torch.from_numpy(np.stack([np.sort(rng.permutation(vocab)[:k]) for _ in range(rows)])).long()
     index[:, 0] = 0                                               # ... one of which is surely not masked in some rows
     index, value = index.sort(dim=1).values, torch.from_numpy(rng.standard_normal((rows, k))).float() * temperature
-    loss, dz = b.ds_distill(z.cuda(), pack_pairs(index, value).cuda(), temperature)
-    want_loss, want = plain.distill(z, index, value, temperature)
+    weight = torch.from_numpy(2.0 ** -rng.integers(0, 9, rows)).float()
+    loss, dz = b.ds_distill(z.cuda(), pack_pairs(index, value).cuda(), temperature, weight=weight.cuda())
+    want_loss, want = plain.distill(z, index, value, temperature, weight=weight)
+    w = weight.double()
     log_q = plain.log_softmax(zd / temperature)
-    dense = log_q.exp() / temperature
+    dense = w[:, None] * log_q.exp() / temperature
     tol = U * (64 + 4 * 100) * (dense + want.abs()) + 2.0 ** -126 / temperature + plain.rounding(want, dtype)
     got = dz.cpu().double()
     over = want.abs() > 3.39e38
@@ -74,10 +75,10 @@ def test_sums_of_logits_far_apart(dtype, vocab, temperature):
     assert not bad.any(), f"dz: {[(names[i], j, got[i, j].item(), want[i, j].item()) for i, j in bad.nonzero().tolist()][:4]}"
     # the loss: sum p (ln p - ln q); ln q of a masked entry is as large as the mask
     p = torch.softmax(value.double() / temperature, dim=1)
-    size = (p * log_q.gather(1, index).abs()).sum(dim=1)
-    tol = 16 * U * size + U * (64 + 4 * 100 + 4 * math.log(vocab + 1)) + 4 * U * want_loss.abs()
+    size = w * (p * log_q.gather(1, index).abs()).sum(dim=1)
+    tol = 16 * U * size + w * U * (64 + 4 * 100 + 4 * math.log(vocab + 1)) + 4 * U * want_loss.abs()
     got = loss.cpu().double()
-    over = log_q.gather(1, index).abs().amax(dim=1) > 3.40e38
+    over = size > 3.39e38
     bad = ~((got - want_loss).abs() <= tol) & ~over
     assert not bad.any(), f"loss: {[(names[i], got[i].item(), want_loss[i].item()) for i in bad.nonzero()[:, 0].tolist()][:4]}"
 
