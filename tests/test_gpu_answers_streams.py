@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_1907_07346_amd import binding as b
+from paper_1907_07346_amd import workloads as wl
 from tests.test_gpu_answers import BF16, F32, calls
 
 pytestmark = pytest.mark.gpu
@@ -28,3 +29,19 @@ def test_inputs_freed_while_another_stream_is_busy(which, dtype):
     for a, w in zip(got, want):
         assert torch.equal(a, w), "the call read memory that belonged to others already"
     assert others
+
+
+def test_a_handles_message_on_another_stream():
+    """The message's memory is the library's own; the call's stream waits for the step's, as it has to."""
+    n, V, D = 4, 40, 128
+    cfg, keep = b.make_config(n, V * D, wl.TOPO_RING, wl.KIND_QUANT_MAXABS, 0.05, 0.3, bits=4, block=64, seed=1)
+    ds = b.DeepSqueeze(cfg, keep)
+    ds.ds_step(torch.randn((n, V * D), device="cuda", generator=torch.Generator(device="cuda").manual_seed(2)))
+    x = torch.randn((3, D), device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    want, back = ds.ds_product(1, x, V), ds.ds_product_gradient(1, x[:, :V].contiguous(), D)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got, got_back = ds.ds_product(1, x, V, stream=side), ds.ds_product_gradient(1, x[:, :V].contiguous(), D, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(got_back, back)
+    ds.ds_destroy()
