@@ -427,6 +427,52 @@ ds_status ds_distill(const ds_logits* l, const void* z_dev, uint64_t z_ld, const
                      const float* weight_dev, float* loss_dev, void* dz_dev, uint64_t dz_ld, void* work_dev, uint64_t work_bytes,
                      void* hip_stream, char* errbuf, uint64_t errbuf_len);
 
+/* ---- gradients that lie in many tensors: their norms, and clipping ---------------------------------------------------
+ *
+ * ds_step takes a worker's gradient as one row of fp32; a backward pass leaves it in many tensors, often of 16 bits.  ds_gradients_lay writes down
+ * once where they are, in device memory of the caller's; ds_gradient_norm and ds_clip then take what the tensors hold at the time of each call.
+ * Streams, work_dev and errors as for the calls above: nothing is allocated, copied, cleared or synchronised. */
+typedef struct {
+    void*    data_dev;        /* count elements, one behind the other, aligned to their type; not looked at where count is 0 */
+    uint64_t count;           /* < 2^40                                                          */
+    int32_t  dtype;           /* ds_dtype                                                        */
+    int32_t  worker;          /* whose gradient it belongs to                                    */
+} ds_tensor;
+
+/* What ds_gradients_lay returns and the calls take: plain numbers, freely copied, good as long as the table and the tensors stay where they are. */
+typedef struct {
+    void*    table_dev;
+    uint64_t table_bytes;
+    uint64_t workers, tensors, tiles;
+    uint64_t columns;         /* elements of the largest worker                                  */
+    uint64_t worker_tiles;    /* tiles of the worker that has most of them                       */
+} ds_gradients;
+
+/* Bytes of the table for `count` tensors (host array; the workers' numbers do not descend; a worker may have none) of `workers` workers,
+ * 1 <= workers < 2^20, count < 2^24, fewer than 2^40 elements a worker; 0 if something about them is invalid. */
+uint64_t ds_gradients_bytes(const ds_tensor* tensors, uint64_t count, uint64_t workers);
+/* Writes the table into table_dev (16-byte aligned), enqueued on hip_stream: a call on another stream has to wait for it.  The list is not needed
+ * afterwards. */
+ds_status ds_gradients_lay(const ds_tensor* tensors, uint64_t count, uint64_t workers, void* table_dev, uint64_t table_bytes,
+                           ds_gradients* out, void* hip_stream, char* errbuf, uint64_t errbuf_len);
+
+/* norm[w] = sqrt(sum of x^2 over all elements of worker w's tensors), summed in 64 bits and rounded once to fp32 (0 where there are none).
+ * norm_dev: `workers` floats. */
+uint64_t ds_gradient_norm_work_bytes(const ds_gradients* g);
+ds_status ds_gradient_norm(const ds_gradients* g, float* norm_dev, void* work_dev, uint64_t work_bytes, void* hip_stream, char* errbuf,
+                           uint64_t errbuf_len);
+
+/* Scales the gradient of every worker whose norm is above max_norm to it: x * max_norm / norm, in 64 bits and rounded to the type written; others stay
+ * as they are.  A gradient whose norm is not finite (an infinity or NaN in it) becomes zeros.  max_norm: >= 0; infinity scales nothing.
+ *   g_dev != NULL: the result is written to g_dev, `workers` rows of fp32 of pitch g_ld >= columns, 4-byte aligned: a worker's tensors one
+ *                  behind the other in the list's order.  What lies behind a worker's elements is left as it was; the tensors are not
+ *                  written.  g_dev must not overlap them, unless a tensor of DS_F32 lies exactly where it goes.
+ *   g_dev == NULL: in place, in the tensors (which then must not overlap each other).
+ * norm_dev: the norms before, `workers` floats, or NULL. */
+uint64_t ds_clip_work_bytes(const ds_gradients* g);
+ds_status ds_clip(const ds_gradients* g, double max_norm, float* g_dev, uint64_t g_ld, float* norm_dev, void* work_dev, uint64_t work_bytes,
+                  void* hip_stream, char* errbuf, uint64_t errbuf_len);
+
 /* Frees everything the handle owns (synchronises first).  NULL is a no-op. */
 void ds_destroy(ds_handle* h);
 

@@ -28,7 +28,8 @@ EXPORTS = ["ds_validate_config", "ds_build_topology", "ds_message_bytes", "ds_in
            "ds_step_count", "ds_plan_name", "ds_last_error", "ds_destroy", "ds_bench_copy",
            "ds_topk_candidate_rows", "ds_set_mixing", "ds_diagnostics", "ds_set_rates", "ds_workload_gradient", "ds_bench_stream", "ds_build_id", "ds_step_static", "ds_init_ex",
            "ds_matrix_bytes", "ds_product", "ds_product_work_bytes", "ds_product_gradient", "ds_product_gradient_work_bytes",
-           "ds_top_logits", "ds_top_logits_work_bytes", "ds_distill", "ds_distill_work_bytes"]
+           "ds_top_logits", "ds_top_logits_work_bytes", "ds_distill", "ds_distill_work_bytes",
+           "ds_gradients_bytes", "ds_gradients_lay", "ds_gradient_norm", "ds_gradient_norm_work_bytes", "ds_clip", "ds_clip_work_bytes"]
 
 
 # torch's current stream as the pointer the library takes.  torch.cuda.current_stream() makes a Stream object for it: 2.9 us of
@@ -75,6 +76,15 @@ class ds_matrix(ctypes.Structure):
 class ds_logits(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_uint64), ("vocab", ctypes.c_uint64), ("k", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("temperature", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class ds_tensor(ctypes.Structure):
+    _fields_ = [("data_dev", ctypes.c_void_p), ("count", ctypes.c_uint64), ("dtype", ctypes.c_int32), ("worker", ctypes.c_int32)]
+
+
+class ds_gradients(ctypes.Structure):
+    _fields_ = [("table_dev", ctypes.c_void_p), ("table_bytes", ctypes.c_uint64), ("workers", ctypes.c_uint64), ("tensors", ctypes.c_uint64),
+                ("tiles", ctypes.c_uint64), ("columns", ctypes.c_uint64), ("worker_tiles", ctypes.c_uint64)]
 
 
 class DsqError(RuntimeError):
@@ -131,7 +141,14 @@ def lib() -> ctypes.CDLL:
         L.ds_product.argtypes = L.ds_product_gradient.argtypes = [mp, vp, vp, u64, vp, u64, vp, u64, vp] + err
         L.ds_top_logits.argtypes = [lp, vp, u64, vp, vp, vp, u64, vp] + err
         L.ds_distill.argtypes = [lp, vp, u64, vp, vp, vp, vp, vp, u64, vp, u64, vp] + err
-        for name in ("ds_product", "ds_product_gradient", "ds_top_logits", "ds_distill"):
+        tp, gp = ctypes.c_void_p, ctypes.POINTER(ds_gradients)
+        L.ds_gradients_bytes.argtypes, L.ds_gradients_bytes.restype = [tp, u64, u64], u64
+        L.ds_gradients_lay.argtypes = [tp, u64, u64, vp, u64, gp, vp] + err
+        for name in ("ds_gradient_norm_work_bytes", "ds_clip_work_bytes"):
+            getattr(L, name).argtypes, getattr(L, name).restype = [gp], u64
+        L.ds_gradient_norm.argtypes = [gp, vp, vp, u64, vp] + err
+        L.ds_clip.argtypes = [gp, ctypes.c_double, vp, u64, vp, vp, u64, vp] + err
+        for name in ("ds_product", "ds_product_gradient", "ds_top_logits", "ds_distill", "ds_gradients_lay", "ds_gradient_norm", "ds_clip"):
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -387,6 +404,111 @@ def ds_distill(z: "torch.Tensor", pairs: "torch.Tensor", temperature: float = 1.
                 ctypes.byref(ds_logits(rows, vocab, pairs.shape[1], _DTYPES[z.dtype], temperature, 0)), (z, pairs, teacher_lse, weight, dz), here, stream,
                 z.data_ptr(), pitch, pairs.data_ptr(), *given, loss.data_ptr() if want_loss else None, dz.data_ptr() if want_gradient else None, dz_pitch)
     return loss, dz
+
+
+# ---- gradients in many tensors --------------------------------------------------------------------------------------
+
+class Gradients:
+    """Where the gradients of the workers lie, laid out once for ds_gradient_norm and ds_clip: `grads` is a list with a list of tensors per
+    worker, or the tensors of one (contiguous, of float32, bfloat16 or float16, on the current CUDA device).  The calls take what the tensors hold then;
+    their memory is kept as long as this is (not when a tensor's storage is resized: lay them out again).  Waits until the table is written."""
+
+    def __init__(self, grads):
+        grads = list(grads)
+        if not grads or isinstance(grads[0], torch.Tensor):
+            grads = [grads]
+        grads = [list(of) for of in grads]
+        flat = [t for of in grads for t in of]
+        for t in flat:
+            if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES or not t.is_contiguous():
+                _refuse("Gradients", "gradients must be contiguous tensors of float32, bfloat16 or float16")
+            if t.requires_grad and torch.is_grad_enabled():
+                _refuse("Gradients", "a tensor requires a gradient, which the calls do not record: detach it")
+        here = _on_device("Gradients", "gradients " * len(flat), *flat)
+        if torch.cuda.is_current_stream_capturing():
+            _refuse("Gradients", "a table cannot be laid out in a stream capture: make it before")
+        self.workers, self.device = len(grads), here
+        self.tensors = [t.detach() for t in flat]         # (of their own: what becomes of the caller's later does not free the memory)
+        sizes = np.array([t.numel() for t in flat], np.uint64)
+        worker = np.repeat(np.arange(len(grads), dtype=np.int32), [len(of) for of in grads])
+        listed = np.zeros(len(flat), np.dtype([("data", "u8"), ("count", "u8"), ("dtype", "i4"), ("worker", "i4")]))
+        listed["data"], listed["count"] = [t.data_ptr() for t in flat], sizes
+        listed["dtype"], listed["worker"] = [_DTYPES[t.dtype] for t in flat], worker
+        L, self._g = lib(), ds_gradients()
+        size = L.ds_gradients_bytes(listed.ctypes.data, len(flat), len(grads))
+        self.table = torch.empty(max(size, 16), dtype=torch.uint8, device=torch.device("cuda", here))
+        buf = ctypes.create_string_buffer(256)
+        st = L.ds_gradients_lay(listed.ctypes.data, len(flat), len(grads), self.table.data_ptr(), size, ctypes.byref(self._g),
+                                _stream_pointer(None), buf, 256)
+        if st != DS_OK:
+            raise DsqError(st, "Gradients", buf.value.decode())
+        torch.cuda.current_stream().synchronize()
+        self.columns = int(self._g.columns)
+        some = sizes > 0
+        self._lo = listed["data"][some]
+        self._hi = self._lo + sizes[some] * np.where(listed["dtype"][some] == 0, 4, 2).astype(np.uint64)
+        self._f32, self._worker = listed["dtype"][some] == 0, worker[some].astype(np.uint64)
+        before = np.concatenate([[0], np.cumsum(sizes)[:-1]]).astype(np.uint64) if len(flat) else sizes
+        first = {int(w): before[i] for i, w in reversed(list(enumerate(worker)))}
+        self._column = (before - np.array([first[int(w)] for w in worker], np.uint64))[some]
+        order = np.argsort(self._lo)
+        self._apart = bool(np.all(self._hi[order][:-1] <= self._lo[order][1:]))
+        self._span = (int(self._lo.min()), int(self._hi.max())) if some.any() else (0, 0)
+
+    def _overlapped(self, out: "torch.Tensor", pitch: int) -> bool:
+        """A tensor lies in out, and not where its elements go."""
+        lo = out.data_ptr()
+        hi = lo + 4 * ((self.workers - 1) * pitch + self.columns)
+        if hi <= self._span[0] or self._span[1] <= lo:
+            return False
+        there = np.uint64(lo) + np.uint64(4) * (self._worker * np.uint64(pitch) + self._column)
+        return bool(np.any((self._lo < hi) & (self._hi > lo) & ~(self._f32 & (self._lo == there))))
+
+
+def _gradients(name: str, grads) -> Gradients:
+    grads = grads if isinstance(grads, Gradients) else Gradients(grads)
+    if torch.cuda.current_device() != grads.device:
+        _refuse(name, "the gradients must be on the current CUDA device")
+    return grads
+
+
+def ds_gradient_norm(grads, stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
+    """The Euclidean norm of each worker's gradient over all its tensors: float32 (workers,).  grads: Gradients, or what they are made of
+    (then they are laid out for this call, which waits for it)."""
+    g = _gradients("ds_gradient_norm", grads)
+    norm = _new(stream, (g.workers,), torch.float32, g.table)
+    L = lib()
+    _answer("ds_gradient_norm", L.ds_gradient_norm_work_bytes, L.ds_gradient_norm, ctypes.byref(g._g), (g.table,) if stream is None else (g.table, *g.tensors),
+            g.device, stream, norm.data_ptr())
+    return norm
+
+
+def ds_clip(grads, max_norm: float, out: "Optional[torch.Tensor]" = None, stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
+    """Scales the gradients of workers whose norm is above max_norm to it, and returns the norms before: float32 (workers,).  With out, float32 (workers,
+    >= columns), what ds_step takes: written there, each worker's tensors one behind the other, nothing behind them; otherwise in place.  A
+    gradient that is not finite becomes zeros."""
+    g = _gradients("ds_clip", grads)
+    at, pitch = None, 0
+    if out is not None:
+        _on_device("ds_clip", "out", out)
+        if out.dtype != torch.float32 or out.dim() != 2 or out.shape[0] != g.workers or out.shape[1] < g.columns:
+            _refuse("ds_clip", f"out must be float32 ({g.workers}, at least {g.columns})")
+        if out.requires_grad and torch.is_grad_enabled():
+            _refuse("ds_clip", "out requires a gradient, which the call does not record")
+        _, cols, pitch = _rows_of("ds_clip", "out", out)
+        if g.workers > 1 and pitch < cols:
+            _refuse("ds_clip", "the rows of out must not overlap")
+        at = out.data_ptr()
+        if g.columns and g._overlapped(out, pitch):
+            _refuse("ds_clip", "out overlaps a gradient that does not lie where it goes")
+        at = at or None
+    elif not g._apart:
+        _refuse("ds_clip", "tensors that overlap cannot be scaled in place")
+    norm = _new(stream, (g.workers,), torch.float32, g.table)
+    L = lib()
+    _answer("ds_clip", L.ds_clip_work_bytes, L.ds_clip, ctypes.byref(g._g), (g.table, out) if stream is None else (g.table, out, *g.tensors), g.device, stream,
+            max_norm, at, pitch, norm.data_ptr())
+    return norm
 
 
 class _Lent:

@@ -46,6 +46,39 @@ hipError_t launch_top_logits(const LogitsArgs& a, hipStream_t stream);
 uint64_t distill_work_bytes(const ds_logits& l);
 hipError_t launch_distill(const LogitsArgs& a, hipStream_t stream);
 
+// A tensor of a worker's gradient, as the table holds it: records[tensors + 1], the last one of no elements; behind them first_tile[workers + 1], the tiles before
+// a worker's; behind those tensor_of[tiles].
+constexpr uint32_t kGradientTile = 16384;                         // elements; the last tile of a tensor has fewer
+struct TensorRecord {
+    void* data;
+    uint64_t count;
+    uint64_t column;                                              // elements of the worker's tensors before it
+    uint64_t first_tile;
+    uint32_t dtype, worker;
+    uint64_t worker_from;                                         // the tensor is the first one of this worker to `worker`, or this is worker + 1
+};
+inline uint64_t gradients_table_bytes(uint64_t workers, uint64_t tensors, uint64_t tiles) {
+    return (tensors + 1) * sizeof(TensorRecord) + (workers + 1) * sizeof(uint64_t) + tiles * sizeof(uint32_t);
+}
+struct RecordBatch {                                              // of a launch, by value
+    static constexpr uint32_t kMost = 64;
+    TensorRecord record[kMost];
+    uint64_t first, here;                                         // records before them, and how many
+};
+hipError_t launch_lay(const ds_gradients& g, const RecordBatch& batch, hipStream_t stream);
+struct ClipArgs {
+    ds_gradients g;
+    double max_norm;
+    float* out;                                                   // or NULL: in place
+    uint64_t out_ld;
+    float* norm;
+    void* work;
+};
+uint64_t gradient_norm_work_bytes(const ds_gradients& g);
+hipError_t launch_gradient_norm(const ClipArgs& a, hipStream_t stream);
+uint64_t clip_work_bytes(const ds_gradients& g);
+hipError_t launch_clip(const ClipArgs& a, hipStream_t stream);
+
 // f(T()) with the C++ type of a ds_dtype.
 template <typename F>
 auto by_dtype(int32_t dtype, F f) {

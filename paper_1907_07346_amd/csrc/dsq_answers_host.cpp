@@ -117,6 +117,48 @@ ds_status logits_call(const ds_logits* l, const void* z, uint64_t z_ld, const vo
     return DS_OK;
 }
 
+// What is wrong with a list of tensors, and the numbers that go into its ds_gradients.
+const char* tensors_fault(const ds_tensor* tensors, uint64_t count, uint64_t workers, ds_gradients& g) {
+    if (workers < 1 || workers >= (1ull << 20)) return "workers must be at least 1 and below 2^20";
+    if (count >= (1ull << 24)) return "there must be fewer than 2^24 tensors";
+    if (count && !tensors) return "the list of tensors is NULL";
+    g = ds_gradients{};
+    g.workers = workers;
+    g.tensors = count;
+    uint64_t column = 0, tiles = 0;
+    int32_t before = 0;
+    for (uint64_t i = 0; i < count; ++i) {
+        const ds_tensor& t = tensors[i];
+        if (t.worker < before || (uint64_t)t.worker >= workers) return "the tensors' workers must not descend and must be below `workers`";
+        if (!known(t.dtype)) return "unknown dtype";
+        if (t.count >= (1ull << 40)) return "a tensor must have fewer than 2^40 elements";
+        const uint64_t size = size_of(t.dtype);
+        if (t.count && !t.data_dev) return "a device pointer is NULL";
+        if (t.count && (address(t.data_dev) & (size - 1))) return "tensors must be aligned to their elements";
+        if (t.count && address(t.data_dev) > UINT64_MAX - t.count * size) return "a tensor does not fit into the address space";
+        if (t.worker != before) column = tiles = 0;
+        before = t.worker;
+        column += t.count;
+        if (column >= (1ull << 40)) return "a worker must have fewer than 2^40 elements";
+        const uint64_t of = (t.count + dsq::kGradientTile - 1) / dsq::kGradientTile;
+        tiles += of;
+        g.tiles += of;
+        if (g.tiles >= (1ull << 32) - 1) return "too many elements";
+        if (column > g.columns) g.columns = column;
+        if (tiles > g.worker_tiles) g.worker_tiles = tiles;
+    }
+    g.table_bytes = dsq::gradients_table_bytes(workers, count, g.tiles);
+    return nullptr;
+}
+
+const char* gradients_fault(const ds_gradients* g) {
+    if (!g) return "the gradients' description is NULL";
+    if (!g->table_dev || (address(g->table_dev) & 15) || g->workers < 1 || g->workers >= (1ull << 20) || g->tensors >= (1ull << 24) ||
+        g->tiles >= (1ull << 32) - 1 || g->worker_tiles > g->tiles || g->table_bytes != dsq::gradients_table_bytes(g->workers, g->tensors, g->tiles))
+        return "the gradients' description is not what ds_gradients_lay made";
+    return nullptr;
+}
+
 }  // namespace
 
 extern "C" {
@@ -199,6 +241,90 @@ ds_status ds_distill(const ds_logits* l, const void* z_dev, uint64_t z_ld, const
     a.loss = loss_dev; a.dz = dz_dev; a.dz_ld = dz_ld;
     a.work = work_dev;
     return report.done(dsq::launch_distill(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+uint64_t ds_gradients_bytes(const ds_tensor* tensors, uint64_t count, uint64_t workers) {
+    ds_gradients g;
+    return tensors_fault(tensors, count, workers, g) ? 0 : g.table_bytes;
+}
+
+ds_status ds_gradients_lay(const ds_tensor* tensors, uint64_t count, uint64_t workers, void* table_dev, uint64_t table_bytes,
+                           ds_gradients* out, void* hip_stream, char* errbuf, uint64_t errbuf_len) {
+    const Report report{errbuf, errbuf_len};
+    ds_gradients g;
+    if (const char* why = tensors_fault(tensors, count, workers, g)) return report(DS_EINVAL, "%s", why);
+    if (!out) return report(DS_EINVAL, "out is NULL");
+    if (!table_dev || table_bytes < g.table_bytes)
+        return report(DS_EINVAL, "table_dev: %llu bytes are needed, %llu given", (unsigned long long)g.table_bytes, (unsigned long long)(table_dev ? table_bytes : 0));
+    if (address(table_dev) & 15) return report(DS_EINVAL, "table_dev must be 16-byte aligned");
+    g.table_dev = table_dev;
+    dsq::RecordBatch batch{};
+    uint64_t column = 0, tile = 0, next_worker = 0;               // (workers before next_worker know their first tile)
+    int32_t before = 0;
+    for (uint64_t i = 0; i <= count; ++i) {
+        dsq::TensorRecord& r = batch.record[batch.here++];
+        if (i < count) {
+            const ds_tensor& t = tensors[i];
+            if (t.worker != before) column = 0;
+            before = t.worker;
+            r = {t.data_dev, t.count, column, tile, (uint32_t)t.dtype, (uint32_t)t.worker, next_worker};
+            column += t.count;
+            tile += (t.count + dsq::kGradientTile - 1) / dsq::kGradientTile;
+        } else {
+            r = {nullptr, 0, 0, tile, (uint32_t)DS_F32, (uint32_t)workers, next_worker};
+        }
+        next_worker = (uint64_t)r.worker + 1;
+        if (batch.here == dsq::RecordBatch::kMost || i == count) {
+            const hipError_t e = dsq::launch_lay(g, batch, static_cast<hipStream_t>(hip_stream));
+            if (e != hipSuccess) return report.done(e);
+            batch.first += batch.here;
+            batch.here = 0;
+        }
+    }
+    *out = g;
+    return report.done(hipSuccess);
+}
+
+uint64_t ds_gradient_norm_work_bytes(const ds_gradients* g) { return gradients_fault(g) ? 0 : dsq::gradient_norm_work_bytes(*g); }
+
+uint64_t ds_clip_work_bytes(const ds_gradients* g) { return gradients_fault(g) ? 0 : dsq::clip_work_bytes(*g); }
+
+ds_status ds_gradient_norm(const ds_gradients* g, float* norm_dev, void* work_dev, uint64_t work_bytes, void* hip_stream, char* errbuf,
+                           uint64_t errbuf_len) {
+    const Report report{errbuf, errbuf_len};
+    if (const char* why = gradients_fault(g)) return report(DS_EINVAL, "%s", why);
+    if (!norm_dev) return report(DS_EINVAL, "a device pointer is NULL");
+    if (address(norm_dev) & 3) return report(DS_EINVAL, "norm_dev must be 4-byte aligned");
+    if (const ds_status st = check_work(report, work_dev, work_bytes, dsq::gradient_norm_work_bytes(*g))) return st;
+    dsq::ClipArgs a{};
+    a.g = *g;
+    a.norm = norm_dev;
+    a.work = work_dev;
+    return report.done(dsq::launch_gradient_norm(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+ds_status ds_clip(const ds_gradients* g, double max_norm, float* g_dev, uint64_t g_ld, float* norm_dev, void* work_dev, uint64_t work_bytes,
+                  void* hip_stream, char* errbuf, uint64_t errbuf_len) {
+    const Report report{errbuf, errbuf_len};
+    if (const char* why = gradients_fault(g)) return report(DS_EINVAL, "%s", why);
+    if (!(max_norm >= 0.0)) return report(DS_EINVAL, "max_norm must be a number that is not negative");
+    if ((address(norm_dev) | address(g_dev)) & 3) return report(DS_EINVAL, "an array of floats must be 4-byte aligned");
+    if (g_dev) {
+        if (g_ld < g->columns) return report(DS_EINVAL, "g_ld must be at least %llu, the elements of the largest worker", (unsigned long long)g->columns);
+        uint64_t lo, hi;
+        if (!range(g_dev, g->workers, g->columns, g_ld, 4, lo, hi)) return report(DS_EINVAL, "g does not fit into the address space");
+        const uint64_t table = address(g->table_dev);
+        if (lo < table + g->table_bytes && table < hi) return report(DS_EINVAL, "g overlaps the table");
+    }
+    if (const ds_status st = check_work(report, work_dev, work_bytes, dsq::clip_work_bytes(*g))) return st;
+    dsq::ClipArgs a{};
+    a.g = *g;
+    a.max_norm = max_norm;
+    a.out = g_dev;
+    a.out_ld = g_ld;
+    a.norm = norm_dev;
+    a.work = work_dev;
+    return report.done(dsq::launch_clip(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

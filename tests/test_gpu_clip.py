@@ -1,0 +1,258 @@
+"""Norms and clipping of gradients in many tensors against plain sums in 64 bits.
+
+Tolerances.  Sums are in 64 bits (n roundings of 2^-53 each, n < 2^32: less than 2^-21 of half a unit of fp32 in the norm, 1e-13 in the factor), so that what
+counts is the rounding to the output's type, and before types of 16 bits one to fp32."""
+import math
+
+import pytest
+import torch
+
+from paper_1907_07346_amd import binding as b
+from paper_1907_07346_amd import workloads as wl
+from tests.answers_plain import rounding
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+INF, NAN = float("inf"), float("nan")
+
+
+def make(spec, seed=0, scale=1.0):
+    """A tensor per (elements, dtype, elements before it in its memory), fresh memory each."""
+    g = torch.Generator().manual_seed(seed)
+    out = []
+    for n, dtype, before in spec:
+        base = torch.full((before + n + 3,), 7.0, dtype=dtype, device="cuda")
+        base[before:before + n] = (torch.randn(n, generator=g) * scale).to(dtype).cuda()
+        out.append(base[before:before + n])
+    return out
+
+
+def plain_norms(grads):
+    return torch.tensor([math.sqrt(sum(float(t.double().square().sum()) for t in of)) for of in grads], dtype=torch.float64)
+
+
+def plain_factor(norm, max_norm):
+    if not norm < INF:
+        return 0.0
+    return max_norm / norm if norm > max_norm else 1.0
+
+
+def plain_clip(x, factor):
+    return x.double() * factor if factor else torch.zeros_like(x, dtype=torch.float64)
+
+
+def close(got, want, dtype, what):
+    got, want = got.cpu().double(), want.cpu()
+    tol = rounding(want, dtype) * (1 + 2.0 ** -20) + (0 if dtype == F32 else rounding(want, F32))
+    same = (got == want) | (torch.isnan(got) & torch.isnan(want))
+    bad = ~(same | ((got - want).abs() <= tol))
+    assert not bad.any(), f"{what}: {int(bad.sum())} off, first {got[bad][0]} for {want[bad][0]}"
+
+
+def close_norms(got, want):
+    close(got, want, F32, "norms")
+
+
+SPECS = [
+    [[(1, F32, 0)]],
+    [[(1, BF16, 1)], [(2, F16, 1)], [(3, F32, 1)]],
+    [[(7, F32, 1), (0, F32, 0), (9, BF16, 3), (1, F16, 1)], [], [(16383, F32, 0), (16384, BF16, 5), (16385, F16, 7)], [(0, F16, 0)], [(5, F32, 2)], []],
+    [[(40000, F32, 3), (1, F32, 0), (33333, BF16, 1), (17, BF16, 0), (50001, F16, 2)], [(100003, BF16, 0)]],
+    [[(n % 37 + 1, (F32, BF16, F16)[n % 3], n % 4) for n in range(300)], [(1000, F32, 0)] * 70],
+    [[(255 + w, F32, w % 2)] for w in range(150)],
+    [[(4096 * 64 + 8, F32, 0)], [(4096 * 64 + 8, BF16, 0)], [(4096 * 64 + 8, F16, 0)]],
+]
+
+
+@pytest.mark.parametrize("spec", range(len(SPECS)))
+def test_norms_and_clipping_into_rows(spec):
+    grads = [make(of, seed=100 * spec + w, scale=10.0 ** (w % 3 - 1)) for w, of in enumerate(SPECS[spec])]
+    before = [[t.clone() for t in of] for of in grads]
+    g = b.Gradients(grads)
+    want = plain_norms(grads)
+    close_norms(b.ds_gradient_norm(g), want)
+    max_norm = float(want.median()) if len(grads) > 1 else float(want[0]) / 3
+    for pitch in (max(g.columns, 1), g.columns + 5):
+        out = torch.full((len(grads), pitch), NAN, device="cuda")
+        close_norms(b.ds_clip(g, max_norm, out=out), want)
+        for w, of in enumerate(grads):
+            at, factor = 0, plain_factor(float(want[w]), max_norm)
+            for t in of:
+                close(out[w, at:at + t.numel()], plain_clip(t, factor), F32, f"worker {w}")
+                at += t.numel()
+            assert torch.isnan(out[w, at:]).all()
+    assert all(torch.equal(t, u) for of, old in zip(grads, before) for t, u in zip(of, old))
+
+
+@pytest.mark.parametrize("spec", range(len(SPECS)))
+def test_clipping_in_place(spec):
+    grads = [make(of, seed=100 * spec + w, scale=10.0 ** (w % 3 - 1)) for w, of in enumerate(SPECS[spec])]
+    before = [[t.clone() for t in of] for of in grads]
+    want = plain_norms(grads)
+    max_norm = float(want.median()) if len(grads) > 1 else float(want[0]) / 3
+    close_norms(b.ds_clip(b.Gradients(grads), max_norm), want)
+    for w, (of, old) in enumerate(zip(grads, before)):
+        for t, u in zip(of, old):
+            close(t, plain_clip(u, plain_factor(float(want[w]), max_norm)), t.dtype, f"worker {w}")
+            whole = torch.empty(0, dtype=t.dtype, device="cuda").set_(t.untyped_storage())
+            lo = t.storage_offset()
+            assert (whole[:lo] == 7.0).all() and (whole[lo + t.numel():] == 7.0).all()
+
+
+@pytest.mark.parametrize("value,dtype", [(3e38, F32), (1e-38, F32), (2.0 ** -140, F32), (3e38, BF16), (60000.0, F16), (2.0 ** -24, F16), (1e-20, F32)])
+def test_values_whose_squares_leave_fp32(value, dtype):
+    x = torch.full((20000,), value, dtype=dtype, device="cuda")
+    want = math.sqrt(20000.0) * float(x[0])
+    got = b.ds_gradient_norm([x])
+    close_norms(got, torch.tensor([want if want < 3.4028235e38 else INF], dtype=torch.float64))
+    out = torch.empty((1, 20000), device="cuda")
+    b.ds_clip([x], want / 2, out=out)                                             # (the norm's square root is held in 64 bits)
+    close(out[0], x.double() * 0.5, F32, "scaled")
+
+
+@pytest.mark.parametrize("bad", [INF, -INF, NAN])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_a_gradient_that_is_not_finite_becomes_zeros(bad, dtype):
+    grads = [make([(300, dtype, 0), (20000, dtype, 1)], seed=w) for w in range(3)]
+    grads[1][1][17777] = bad
+    keep = [t.clone() for t in grads[2]]
+    out = torch.full((3, 20300), NAN, device="cuda")
+    for max_norm in (1e9, 1.0, 0.0, INF):
+        norm = b.ds_clip(b.Gradients(grads), max_norm, out=out)
+        assert not math.isfinite(float(norm[1])) and math.isnan(float(norm[1])) == math.isnan(bad)
+        assert (out[1] == 0).all() and torch.isfinite(out).all()
+        assert (out[2] == 0).all() == (max_norm == 0.0)
+        if max_norm in (1e9, INF):
+            assert torch.equal(out[2], torch.cat(keep).float())
+    b.ds_clip(b.Gradients(grads), 1e9)
+    assert (grads[1][0] == 0).all() and (grads[1][1] == 0).all() and all(torch.equal(t, u) for t, u in zip(grads[2], keep))
+
+
+def test_a_norm_at_the_limit_scales_nothing():
+    x = torch.zeros(100, device="cuda")
+    x[3], x[90] = 3.0, 4.0
+    out = torch.empty((1, 100), device="cuda")
+    assert float(b.ds_clip([x], 5.0, out=out)) == 5.0 and torch.equal(out[0], x)
+    assert float(b.ds_clip([x], 2.5)) == 5.0 and x[3] == 1.5 and x[90] == 2.0
+
+
+def test_gradients_that_lie_in_the_result():
+    out = torch.randn((3, 5000), device="cuda")
+    before = out.clone()
+    grads = [[out[w, :1001], out[w, 1001:4000]] for w in range(3)]
+    want = plain_norms(grads)
+    close_norms(b.ds_clip(grads, 1.0, out=out), want)
+    for w in range(3):
+        close(out[w, :4000], before[w, :4000].double() / want[w], F32, "scaled")
+    assert torch.equal(out[:, 4000:], before[:, 4000:])
+    for wrong in ([[out[1, :10]], [out[0, :10]], [out[2, :10]]], [[out[w, 1:10]] for w in range(3)],
+                  [[out[0, :20].view(BF16)], [out[1, :10]], [out[2, :10]]]):
+        with pytest.raises(b.DsqError, match="overlaps"):
+            b.ds_clip(wrong, 1.0, out=out)
+    with pytest.raises(b.DsqError, match="in place"):
+        b.ds_clip([out[0, :10], out[0, 5:20]], 1.0)
+    x = torch.ones(8, device="cuda")
+    row = torch.empty((1, 16), device="cuda")
+    assert float(b.ds_clip([x, x], 2.0, out=row)) == 4.0 and (row == 0.5).all()  # the same one twice counts twice
+
+
+def test_results_that_are_refused():
+    g = b.Gradients([torch.ones(10, device="cuda"), torch.ones(3, device="cuda", dtype=F16)])
+    for out in (torch.empty((1, 12), device="cuda"), torch.empty((2, 13), device="cuda"), torch.empty(13, device="cuda"),
+                torch.empty((1, 13), device="cuda", dtype=BF16)):
+        with pytest.raises(b.DsqError, match="out must"):
+            b.ds_clip(g, 1.0, out=out)
+    with pytest.raises(b.DsqError, match="out must be on"):
+        b.ds_clip(g, 1.0, out=torch.empty((1, 13)))
+    with pytest.raises(b.DsqError, match="column stride"):
+        b.ds_clip(g, 1.0, out=torch.empty((1, 26), device="cuda")[:, ::2])
+    with pytest.raises(b.DsqError, match="records|record"):
+        b.ds_clip(g, 1.0, out=torch.empty((1, 13), device="cuda", requires_grad=True))
+    two = b.Gradients([[torch.ones(4, device="cuda")], [torch.ones(4, device="cuda")]])
+    with pytest.raises(b.DsqError, match="overlap"):
+        b.ds_clip(two, 1.0, out=torch.empty((1, 4), device="cuda").expand(2, 4))
+    for max_norm in (-1.0, NAN):
+        with pytest.raises(b.DsqError, match="max_norm"):
+            b.ds_clip(g, max_norm)
+
+
+def test_no_tensors_and_empty_ones():
+    for grads, workers in (([], 1), ([[], []], 2), ([[torch.empty(0, device="cuda")], [torch.empty(0, device="cuda", dtype=BF16)]], 2)):
+        assert b.ds_gradient_norm(grads).tolist() == [0.0] * workers
+        out = torch.full((workers, 4), 3.0, device="cuda")
+        assert b.ds_clip(grads, 1.0, out=out).tolist() == [0.0] * workers and (out == 3.0).all()
+        assert b.ds_clip(grads, 1.0).tolist() == [0.0] * workers
+
+
+def test_a_captured_call_takes_what_the_tensors_hold_then():
+    grads = [make([(5000, F32, 0), (20001, BF16, 1)], seed=w) for w in range(2)]
+    g, out = b.Gradients(grads), torch.zeros((2, 25001), device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        b.ds_clip(g, 1.0, out=out)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        norm = b.ds_clip(g, 1.0, out=out)
+        alone = b.ds_gradient_norm(g)
+        with pytest.raises(b.DsqError, match="capture"):
+            b.Gradients(grads)
+    for t in range(4):
+        for w, of in enumerate(grads):
+            for x in of:
+                x.copy_(torch.randn(x.shape, device="cuda") * (t + 1) * (0.001 if w else 1.0))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = plain_norms(grads)
+        close_norms(norm, want)
+        close_norms(alone, want)
+        rows = out.clone()
+        eager = torch.zeros_like(out)
+        b.ds_clip(g, 1.0, out=eager)
+        assert torch.equal(rows, eager)
+
+
+def test_calls_on_another_stream_and_memory_freed_meanwhile():
+    s = torch.cuda.Stream()
+    want = torch.full((1, 1 << 22), 1.0 / 2048, device="cuda")
+    for _ in range(10):
+        x = torch.ones(1 << 22, device="cuda")
+        out = torch.empty((1, 1 << 22), device="cuda")
+        s.wait_stream(torch.cuda.current_stream())
+        norm = b.ds_clip([x], 1.0, out=out, stream=s)
+        del x
+        torch.full((1 << 22,), 9.0, device="cuda")                                # may take its place
+        s.synchronize()
+        assert float(norm) == 2048.0 and torch.equal(out, want)
+
+
+def test_more_than_four_gigabytes_in_a_tensor():
+    n = 2 ** 31 + 12345
+    x = torch.ones(n, dtype=BF16, device="cuda")
+    x[-1] = 2.0
+    out = torch.zeros((1, n + 3), device="cuda")
+    want = math.sqrt(n + 3)
+    norm = b.ds_clip([x], want / 4, out=out)
+    close_norms(norm, torch.tensor([want], dtype=torch.float64))
+    assert float(out[0, 0]) == 0.25 and float(out[0, n - 1]) == 0.5 and (out[0, n:] == 0).all()
+    assert float(out[0, :n - 1].min()) == 0.25 and float(out[0, :n - 1].max()) == 0.25
+
+
+def test_steps_take_what_clipping_made():
+    """A worker's gradient in two tensors, clipped into the row that ds_step takes: the first step of D-PSGD without neighbours moves x by it."""
+    n, N = 4, 3000
+    cfg, keep = b.make_config(n=n, N=N, topo=wl.TOPO_RING, kind=wl.KIND_IDENTITY, gamma=1.0, eta=0.0)
+    ds = b.DeepSqueeze(cfg, keep)
+    g = torch.zeros((n, ds.ds_state_ptrs()[2]), device="cuda")
+    grads = [make([(1000, F32, 0), (2000, BF16, 1)], seed=w, scale=1.0 + w) for w in range(n)]
+    norm = plain_norms(grads)
+    assert (norm > 100.0).any() and (norm < 100.0).any()
+    b.ds_clip(grads, 100.0, out=g)
+    ds.ds_step(g)
+    x, _ = ds.ds_read_state(want_delta=False)
+    for w, of in enumerate(grads):
+        want = torch.cat([plain_clip(t, plain_factor(float(norm[w]), 100.0)) for t in of])
+        close(-torch.from_numpy(x[w]), want, F32, f"worker {w}")
+    assert (g[:, N:] == 0).all()
+    ds.ds_destroy()
