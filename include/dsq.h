@@ -427,6 +427,40 @@ ds_status ds_distill(const ds_logits* l, const void* z_dev, uint64_t z_ld, const
                      const float* weight_dev, float* loss_dev, void* dz_dev, uint64_t dz_ld, void* work_dev, uint64_t work_bytes,
                      void* hip_stream, char* errbuf, uint64_t errbuf_len);
 
+/* Drawing an answer: a token of every row of logits from a given random number. */
+typedef struct {
+    uint64_t rows;            /* < 2^31                                                          */
+    uint64_t vocab;           /* logits per row, 1 <= vocab < 2^31                               */
+    int32_t  dtype;           /* ds_dtype of the logits                                          */
+    int32_t  top_k;           /* >= 0; 0 (or >= vocab): all                                      */
+    float    temperature;     /* as in ds_logits, or 0: the largest logit                        */
+    float    top_p;           /* 0 <= top_p <= 1; 1: all                                         */
+    float    min_p;           /* 0 <= min_p <= 1; 0: all                                         */
+    int32_t  reserved;        /* must be 0                                                       */
+} ds_sampling;
+
+/* Parameters of rows, in place of those above: `rows` numbers each, 4-byte aligned, or NULL.  They are not checked: a temperature that is
+ * none (NaN, infinite, subnormal, 0 or below) is taken as 0, other numbers as the nearest that is allowed, NaN as all. */
+typedef struct {
+    const float*   temperature_dev;
+    const int32_t* top_k_dev;
+    const float*   top_p_dev;
+    const float*   min_p_dev;
+} ds_sampling_rows;
+
+/* The order of a row z: larger logits first, of equal ones (+0 and -0 are) the lower index.  With T = temperature and e_v = exp((z_v - max z) / T), what is kept
+ * is a beginning of that order: its first top_k; of these the fewest whose e sum up to top_p * (the sum of these); of these those with e >= min_p; the largest
+ * always.  With S the sum of e of all that is kept:
+ *   token = the first in the order at which the sum of e passes u * S,     logp = (z_token - max z) / T - ln S
+ * so that u = 0 gives the largest logit, and u drawn uniformly from [0, 1) a token with probability e / S.  At temperature 0 only the first of the order
+ * is kept.  e is held as whole multiples of 2^-51, or 2^-62 times the power of two that reaches vocab where that is more, made in 64 bits (to 4e-14), and summed exactly.
+ * u outside [0, 1) counts as the nearest number inside, NaN as 0.  Logits of minus infinity have probability 0; where some are plus infinity, only these count,
+ * and alike.  A row of minus infinities has token -1, which as an index of a pair is no entry, and logp minus infinity; a row with a NaN token -1 and logp NaN.
+ * z_dev: rows of pitch z_ld >= vocab elements, aligned to them; each: may be NULL; u_dev, token_dev: one per row; logp_dev: one per row, or NULL. */
+uint64_t ds_sample_work_bytes(const ds_sampling* s);
+ds_status ds_sample(const ds_sampling* s, const ds_sampling_rows* each, const void* z_dev, uint64_t z_ld, const float* u_dev,
+                    int32_t* token_dev, float* logp_dev, void* work_dev, uint64_t work_bytes, void* hip_stream, char* errbuf, uint64_t errbuf_len);
+
 /* ---- gradients that lie in many tensors: their norms, and clipping ---------------------------------------------------
  *
  * ds_step takes a worker's gradient as one row of fp32; a backward pass leaves it in many tensors, often of 16 bits.  ds_gradients_lay writes down

@@ -29,7 +29,7 @@ EXPORTS = ["ds_validate_config", "ds_build_topology", "ds_message_bytes", "ds_in
            "ds_topk_candidate_rows", "ds_set_mixing", "ds_diagnostics", "ds_set_rates", "ds_workload_gradient", "ds_bench_stream", "ds_build_id", "ds_step_static", "ds_init_ex",
            "ds_matrix_bytes", "ds_product", "ds_product_work_bytes", "ds_product_gradient", "ds_product_gradient_work_bytes",
            "ds_top_logits", "ds_top_logits_work_bytes", "ds_distill", "ds_distill_work_bytes",
-           "ds_gradients_bytes", "ds_gradients_lay", "ds_gradient_norm", "ds_gradient_norm_work_bytes", "ds_clip", "ds_clip_work_bytes"]
+           "ds_sample", "ds_sample_work_bytes", "ds_gradients_bytes", "ds_gradients_lay", "ds_gradient_norm", "ds_gradient_norm_work_bytes", "ds_clip", "ds_clip_work_bytes"]
 
 
 # torch's current stream as the pointer the library takes.  torch.cuda.current_stream() makes a Stream object for it: 2.9 us of
@@ -76,6 +76,15 @@ class ds_matrix(ctypes.Structure):
 class ds_logits(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_uint64), ("vocab", ctypes.c_uint64), ("k", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("temperature", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class ds_sampling(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_uint64), ("vocab", ctypes.c_uint64), ("dtype", ctypes.c_int32), ("top_k", ctypes.c_int32),
+                ("temperature", ctypes.c_float), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class ds_sampling_rows(ctypes.Structure):
+    _fields_ = [("temperature_dev", ctypes.c_void_p), ("top_k_dev", ctypes.c_void_p), ("top_p_dev", ctypes.c_void_p), ("min_p_dev", ctypes.c_void_p)]
 
 
 class ds_tensor(ctypes.Structure):
@@ -141,6 +150,9 @@ def lib() -> ctypes.CDLL:
         L.ds_product.argtypes = L.ds_product_gradient.argtypes = [mp, vp, vp, u64, vp, u64, vp, u64, vp] + err
         L.ds_top_logits.argtypes = [lp, vp, u64, vp, vp, vp, u64, vp] + err
         L.ds_distill.argtypes = [lp, vp, u64, vp, vp, vp, vp, vp, u64, vp, u64, vp] + err
+        sp = ctypes.POINTER(ds_sampling)
+        L.ds_sample_work_bytes.argtypes, L.ds_sample_work_bytes.restype = [sp], u64
+        L.ds_sample.argtypes = [sp, ctypes.POINTER(ds_sampling_rows), vp, u64, vp, vp, vp, vp, u64, vp] + err
         tp, gp = ctypes.c_void_p, ctypes.POINTER(ds_gradients)
         L.ds_gradients_bytes.argtypes, L.ds_gradients_bytes.restype = [tp, u64, u64], u64
         L.ds_gradients_lay.argtypes = [tp, u64, u64, vp, u64, gp, vp] + err
@@ -148,7 +160,7 @@ def lib() -> ctypes.CDLL:
             getattr(L, name).argtypes, getattr(L, name).restype = [gp], u64
         L.ds_gradient_norm.argtypes = [gp, vp, vp, u64, vp] + err
         L.ds_clip.argtypes = [gp, ctypes.c_double, vp, u64, vp, vp, u64, vp] + err
-        for name in ("ds_product", "ds_product_gradient", "ds_top_logits", "ds_distill", "ds_gradients_lay", "ds_gradient_norm", "ds_clip"):
+        for name in ("ds_product", "ds_product_gradient", "ds_top_logits", "ds_distill", "ds_sample", "ds_gradients_lay", "ds_gradient_norm", "ds_clip"):
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -404,6 +416,35 @@ def ds_distill(z: "torch.Tensor", pairs: "torch.Tensor", temperature: float = 1.
                 ctypes.byref(ds_logits(rows, vocab, pairs.shape[1], _DTYPES[z.dtype], temperature, 0)), (z, pairs, teacher_lse, weight, dz), here, stream,
                 z.data_ptr(), pitch, pairs.data_ptr(), *given, loss.data_ptr() if want_loss else None, dz.data_ptr() if want_gradient else None, dz_pitch)
     return loss, dz
+
+
+def ds_sample(z: "torch.Tensor", u: "torch.Tensor", temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream: Optional["torch.cuda.Stream"] = None):
+    """A token of each row of z from the random numbers u (float32, one per row, in [0, 1)): (token, logp), int32 and float32 (rows,).  Each
+    parameter is a number, or a tensor with a number per row (float32; top_k int32).  Temperature 0 takes the largest logit.  What is drawn carries no graph."""
+    rows, vocab, pitch = _rows_of("ds_sample", "z", z)
+    if u.dtype != torch.float32 or u.dim() != 1 or u.shape[0] != rows or not u.is_contiguous():
+        _refuse("ds_sample", f"u must be a contiguous float32 vector of {rows}")
+    here = _on_device("ds_sample", "z u", z, u)
+    s, each, own = ds_sampling(rows, vocab, _DTYPES[z.dtype], 0, 1.0, 1.0, 0.0, 0), None, []
+    for name, value, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                               ("min_p", min_p, torch.float32)):
+        if not isinstance(value, torch.Tensor):
+            if name == "top_k" and not (isinstance(value, (int, np.integer)) and 0 <= value < 1 << 31):
+                _refuse("ds_sample", "top_k must be a whole number of at least 0 and below 2^31")
+            setattr(s, name, value)
+            continue
+        if value.dtype != dtype or value.dim() != 1 or value.shape[0] != rows or not value.is_contiguous():
+            _refuse("ds_sample", f"{name} must be a number or a contiguous vector of {rows}, {dtype}")
+        _on_device("ds_sample", name, value)
+        each = each or ds_sampling_rows()
+        setattr(each, name + "_dev", value.data_ptr())
+        own.append(value)
+    token, logp = _new(stream, (rows,), torch.int32, z), _new(stream, (rows,), torch.float32, z)
+    if rows:
+        L = lib()
+        _answer("ds_sample", L.ds_sample_work_bytes, L.ds_sample, ctypes.byref(s), (z, u, *own), here, stream,
+                ctypes.byref(each) if each is not None else None, z.data_ptr(), pitch, u.data_ptr(), token.data_ptr(), logp.data_ptr())
+    return token, logp
 
 
 # ---- gradients in many tensors --------------------------------------------------------------------------------------

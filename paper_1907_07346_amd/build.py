@@ -14,7 +14,7 @@ SOURCES = ["dsq_tile_quant4.hip", "dsq_tile_quant2.hip", "dsq_tile_quant8.hip", 
            "dsq_team_quant4.hip", "dsq_team_quant2.hip", "dsq_team_quant8.hip", "dsq_team_sign.hip", "dsq_host.cpp", "dsq_api.hip",
            "dsq_topk_kernels.hip", "dsq_topk_resident.hip", "dsq_l2norm_kernels.hip", "dsq_workload_kernels.hip",
            "dsq_compare_quant4.hip", "dsq_compare_quant2.hip", "dsq_compare_quant8.hip", "dsq_compare_sign.hip",
-           "dsq_answers_host.cpp", "dsq_product.hip", "dsq_product_gradient.hip", "dsq_top_logits.hip", "dsq_distill.hip", "dsq_clip.hip"]
+           "dsq_answers_host.cpp", "dsq_product.hip", "dsq_product_gradient.hip", "dsq_top_logits.hip", "dsq_distill.hip", "dsq_sample.hip", "dsq_clip.hip"]
 
 # -ffp-contract=off: every fused multiply-add in the kernels is written out as fmaf, nothing else may fuse
 #  (bit-level agreement of codes and scales depends on it).  The packed-fp32 feature is switched off because

@@ -46,6 +46,20 @@ hipError_t launch_top_logits(const LogitsArgs& a, hipStream_t stream);
 uint64_t distill_work_bytes(const ds_logits& l);
 hipError_t launch_distill(const LogitsArgs& a, hipStream_t stream);
 
+struct SampleArgs {
+    const void* z;
+    uint64_t rows, vocab, z_ld;
+    int32_t dtype, top_k;
+    float temperature, top_p, min_p;
+    ds_sampling_rows each;                                        // rows' own parameters in place of these
+    const float* u;
+    int32_t* token;
+    float* logp;
+    void* work;
+};
+uint64_t sample_work_bytes(const ds_sampling& s);
+hipError_t launch_sample(const SampleArgs& a, hipStream_t stream);
+
 // A tensor of a worker's gradient, as the table holds it: records[tensors + 1], the last one of no elements; behind them first_tile[workers + 1], the tiles before
 // a worker's; behind those tensor_of[tiles].
 constexpr uint32_t kGradientTile = 16384;                         // elements; the last tile of a tensor has fewer

@@ -117,6 +117,20 @@ ds_status logits_call(const ds_logits* l, const void* z, uint64_t z_ld, const vo
     return DS_OK;
 }
 
+const char* sampling_fault(const ds_sampling* s) {
+    if (!s) return "the sampling's description is NULL";
+    if (s->rows >= kMost) return "rows must be below 2^31";
+    if (s->vocab < 1 || s->vocab >= kMost) return "vocab must be at least 1 and below 2^31";
+    if (!known(s->dtype)) return "unknown dtype";
+    if (s->top_k < 0) return "top_k must not be negative";
+    if (!(s->temperature == 0.f || (std::isfinite(s->temperature) && s->temperature >= FLT_MIN)))
+        return "temperature must be 0, or finite and positive, and no subnormal number";
+    if (!(s->top_p >= 0.f && s->top_p <= 1.f)) return "top_p must be between 0 and 1";
+    if (!(s->min_p >= 0.f && s->min_p <= 1.f)) return "min_p must be between 0 and 1";
+    if (s->reserved != 0) return "reserved must be 0";
+    return nullptr;
+}
+
 // What is wrong with a list of tensors, and the numbers that go into its ds_gradients.
 const char* tensors_fault(const ds_tensor* tensors, uint64_t count, uint64_t workers, ds_gradients& g) {
     if (workers < 1 || workers >= (1ull << 20)) return "workers must be at least 1 and below 2^20";
@@ -241,6 +255,45 @@ ds_status ds_distill(const ds_logits* l, const void* z_dev, uint64_t z_ld, const
     a.loss = loss_dev; a.dz = dz_dev; a.dz_ld = dz_ld;
     a.work = work_dev;
     return report.done(dsq::launch_distill(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+uint64_t ds_sample_work_bytes(const ds_sampling* s) { return sampling_fault(s) || s->rows == 0 ? 0 : dsq::sample_work_bytes(*s); }
+
+ds_status ds_sample(const ds_sampling* s, const ds_sampling_rows* each, const void* z_dev, uint64_t z_ld, const float* u_dev,
+                    int32_t* token_dev, float* logp_dev, void* work_dev, uint64_t work_bytes, void* hip_stream, char* errbuf, uint64_t errbuf_len) {
+    const Report report{errbuf, errbuf_len};
+    if (const char* why = sampling_fault(s)) return report(DS_EINVAL, "%s", why);
+    if (s->rows == 0) return report(DS_OK, "%s", "");
+    if (!z_dev || !u_dev || !token_dev) return report(DS_EINVAL, "a device pointer is NULL");
+    if (z_ld < s->vocab) return report(DS_EINVAL, "z_ld must be >= vocab");
+    if (address(z_dev) & (size_of(s->dtype) - 1)) return report(DS_EINVAL, "z_dev must be aligned to its elements");
+    const ds_sampling_rows own = each ? *each : ds_sampling_rows{};
+    if ((address(u_dev) | address(token_dev) | address(logp_dev) | address(own.temperature_dev) | address(own.top_k_dev) | address(own.top_p_dev) |
+         address(own.min_p_dev)) & 3)
+        return report(DS_EINVAL, "an array of a number per row must be 4-byte aligned");
+    uint64_t z_lo, z_hi;
+    if (!range(z_dev, s->rows, s->vocab, z_ld, size_of(s->dtype), z_lo, z_hi)) return report(DS_EINVAL, "z does not fit into the address space");
+    // outputs are neither inputs nor each other
+    const void* const arrays[] = {token_dev, logp_dev, u_dev, own.temperature_dev, own.top_k_dev, own.top_p_dev, own.min_p_dev};
+    for (int i = 0; i < 2; ++i) {
+        uint64_t lo, hi, other_lo, other_hi;
+        if (!arrays[i]) continue;
+        if (!range(arrays[i], 1, s->rows, s->rows, 4, lo, hi)) return report(DS_EINVAL, "an array does not fit into the address space");
+        if (lo < z_hi && z_lo < hi) return report(DS_EINVAL, "an output overlaps z");
+        for (int j = i + 1; j < 7; ++j) {
+            if (!arrays[j]) continue;
+            if (!range(arrays[j], 1, s->rows, s->rows, 4, other_lo, other_hi)) return report(DS_EINVAL, "an array does not fit into the address space");
+            if (lo < other_hi && other_lo < hi) return report(DS_EINVAL, "an output overlaps another array");
+        }
+    }
+    if (const ds_status st = check_work(report, work_dev, work_bytes, dsq::sample_work_bytes(*s))) return st;
+    dsq::SampleArgs a{};
+    a.z = z_dev; a.z_ld = z_ld;
+    a.rows = s->rows; a.vocab = s->vocab; a.dtype = s->dtype;
+    a.top_k = s->top_k; a.temperature = s->temperature; a.top_p = s->top_p; a.min_p = s->min_p;
+    a.each = own;
+    a.u = u_dev; a.token = token_dev; a.logp = logp_dev; a.work = work_dev;
+    return report.done(dsq::launch_sample(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 uint64_t ds_gradients_bytes(const ds_tensor* tensors, uint64_t count, uint64_t workers) {

@@ -94,3 +94,40 @@ def distill(z, index, value, temperature, teacher_lse=None, weight=None):
         loss[i] = weight[i] * (p[some] * (log_p[some] - log_q[at[some]])).sum()
         dz[i] = weight[i] / temperature * (p.sum() * log_q.exp()).index_add(0, at, -p)
     return loss, dz
+
+
+def sample_row(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """(token, logp) of a row (numpy, any float type), by a sorted list; parameters as the fp32 numbers they are given as."""
+    z = np.asarray(z, np.float64)
+    temperature, top_p, min_p, u = (float(np.float32(v)) for v in (temperature, top_p, min_p, u))
+    if np.isnan(z).any():
+        return -1, np.nan
+    if z.max() == -np.inf:
+        return -1, -np.inf
+    order = np.lexsort((np.arange(len(z)), -z))
+    greedy = not (2.0 ** -126 <= temperature < np.inf)
+    if greedy:
+        temperature, top_k = 1.0, 1
+    z = z[order]
+    with np.errstate(invalid="ignore", over="ignore", divide="ignore"):
+        y = np.where(z == z[0], 0.0, (z - z[0]) / temperature)
+    e = np.exp(y)
+    last = len(z) if top_k <= 0 else min(top_k, len(z))
+    mass = np.cumsum(e[:last])
+    if top_p < 1.0:
+        last = int(np.searchsorted(mass, top_p * mass[-1])) + 1 if top_p > 0 else 1
+    if min_p > 0:
+        last = min(last, int((e >= min(min_p, 1.0)).sum()))
+    mass = mass[:last]
+    u = 0.0 if not u > 0 else u
+    place = int(np.searchsorted(mass, u * mass[-1], side="right")) if u < 1 else last
+    place = min(place, int((e[:last] > 0).sum()) - 1)
+    return int(order[place]), y[place] - np.log(mass[-1])
+
+
+def sample(z, u, **parameters):
+    """(token, logp) of rows; parameters are numbers or tensors of one per row."""
+    rows = z.double().cpu().numpy()
+    of = [{k: v[i].item() if torch.is_tensor(v) else v for k, v in parameters.items()} for i in range(len(rows))]
+    got = [sample_row(rows[i], float(u[i]), **of[i]) for i in range(len(rows))]
+    return torch.tensor([t for t, _ in got], dtype=torch.int32), torch.tensor([p for _, p in got], dtype=torch.float64)
