@@ -46,15 +46,17 @@ struct Masses {
     }
 };
 
-// Which bin of the row a logit lies in: bins are numbers of the 15 leading bits of its magnitude, those below `base` as one.
+// Bins that follow the order: a logit's is the number that the 15 leading bits of its magnitude make, those below `base` as one, `top` of them above it; what lies
+// behind the last one is in it.
 struct Bins {
     int32_t base, top;
+    uint32_t last;
     __device__ __forceinline__ uint32_t operator()(float z) const {
         const uint32_t bits = __float_as_uint(z);
         int32_t c = (int32_t)(bits >> 16 & 0x7FFFu) - base;
         c = c > 0 ? c : 0;
         const uint32_t bin = (uint32_t)(top - ((int32_t)bits < 0 ? -c : c));
-        return bin < kBins - 1 ? bin : kBins - 1;
+        return bin < last ? bin : last;
     }
     // The largest and the smallest number of a bin.
     __device__ float highest(uint32_t bin) const {
@@ -67,7 +69,7 @@ struct Bins {
     }
     __device__ float lowest(uint32_t bin) const {
         const int32_t v = top - (int32_t)bin;
-        if (bin == kBins - 1) return -kInf;
+        if (bin == last) return -kInf;
         if (v > 0) return __uint_as_float((uint32_t)(base + v) << 16);
         const uint32_t bits = (uint32_t)(base - v) << 16 | 0xFFFFu;
         return -__uint_as_float(bits < 0x7F800000u ? bits : 0x7F800000u);
@@ -75,8 +77,14 @@ struct Bins {
     // The only number of a bin, if logits have 8 bits ...
     __device__ __forceinline__ float number(uint32_t bin) const { return (int32_t)bin < top ? lowest(bin) : highest(bin); }
     // ... and this is true.
-    __device__ __forceinline__ bool single(uint32_t bin) const { return bin != (uint32_t)top && bin != kBins - 1; }
+    __device__ __forceinline__ bool single(uint32_t bin) const { return bin != (uint32_t)top && bin != last; }
 };
+// Bins for rows whose largest logit and what matters below it lie between -2^12 and 2^12, whatever it is: 128 of each power of two from 2^-20 on.
+constexpr int32_t kFixedBase = (127 - 20) << 7, kFixedTop = 4095;
+constexpr uint32_t kFixedLast = 2 * kFixedTop, kFixedBins = kFixedLast + 2;                // (a multiple of the threads)
+constexpr float kFixedMost = 4096.f;
+__device__ __forceinline__ Bins fixed_bins() { return {kFixedBase, kFixedTop, kFixedLast}; }
+// Bins for any row.
 __device__ __forceinline__ Bins bins_of(float max, float temperature) {
     const int32_t m = (int32_t)(__float_as_uint(max) >> 16 & 0x7FFFu), t = (int32_t)(__float_as_uint(temperature) >> 16) - (int32_t)kOctaves;
     Bins b;
@@ -86,15 +94,17 @@ __device__ __forceinline__ Bins bins_of(float max, float temperature) {
     if (b.base > 0x7F7F) b.base = 0x7F7F;
     const int32_t c = m > b.base ? m - b.base : 0;
     b.top = max < 0.f ? -c : c;
+    b.last = kBins - 1;
     return b;
 }
 __device__ __forceinline__ float of_key(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 
+// Of a workgroup; dynamic, so that functions that are not inlined know it as LDS.
 template <int THREADS>
 struct SampleLds {
     union {
         uint64_t mass[kBins];
-        uint32_t count[2 * kBins];
+        uint32_t count[kFixedBins + 64];                          // (the last 64: see count_and_largest)
     };
     uint64_t list[kList], sorted[kList], upto[kList];             // ranks of the logits gathered; in order; the mass through each
     uint64_t part_mass[kParts];
@@ -102,10 +112,13 @@ struct SampleLds {
     uint64_t sums[THREADS / 64];
     uint32_t counts[THREADS / 64];
     float most[THREADS / 64];
-    uint64_t special[2];                                          // mass of the bins that hold several numbers, if others hold one
     uint64_t before, through;                                     // answers
     uint32_t held, bin, ahead, index;
+    float value;
 };
+extern __shared__ u32x4 sample_memory[];
+template <int THREADS>
+__device__ __forceinline__ SampleLds<THREADS>& sample_lds() { return *reinterpret_cast<SampleLds<THREADS>*>(sample_memory); }
 
 // What lies before the thread's v in the workgroup, and all of it.
 template <int THREADS, typename V>
@@ -114,7 +127,9 @@ __device__ __forceinline__ V before_thread(V v, V* sums, V& all) {
     V upto = v;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const V other = (V)__shfl_up((unsigned long long)upto, o);
+        V other;
+        if constexpr (sizeof(V) == 8) other = (V)__shfl_up((unsigned long long)upto, o);
+        else other = (V)__shfl_up((int)upto, o);
         if (lane >= (uint32_t)o) upto += other;
     }
     __syncthreads();
@@ -137,12 +152,9 @@ template <typename T, int THREADS>
 struct Row {
     static constexpr uint32_t E = Pieces<T>::E;
     using Piece = typename Pieces<T>::Piece;
-    static constexpr uint32_t kOwn = kBins / THREADS;             // bins of a thread
-    SampleLds<THREADS>& s;
     const T* z;
     uint32_t vocab;
     Masses masses;
-    Bins bins;
     float least;                                                  // logits below it have no mass
 
     // f(values, column of the first) for all 16-byte pieces; what lies behind the end is minus infinity.
@@ -169,12 +181,70 @@ struct Row {
         }
     }
 
+    // The thread's largest logit, and all of them counted in fixed bins, but for those of the last one: they are mostly masked, which would be one address for many.
+    // They go to a place of the lane's.
+    __device__ __forceinline__ float count_and_largest() const {
+        SampleLds<THREADS>& s = sample_lds<THREADS>();
+        float max = -kInf;
+        if constexpr (std::is_same_v<T, __bf16>) {                // two at a time
+            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+            typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+            const uint32_t nowhere = (kFixedBins + (threadIdx.x & 63)) * 4;
+            auto add = [&](uint32_t place) {
+                place = place != kFixedLast * 4 ? place : nowhere;
+                atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.count) + place), 1u);
+            };
+            auto two = [&](uint32_t bits) {
+                const u16x2 magnitude = __builtin_bit_cast(u16x2, bits & 0x7FFF7FFFu);
+                const u16x2 base = (uint16_t)kFixedBase, top = (uint16_t)kFixedTop;
+                u16x2 c = __builtin_elementwise_min(__builtin_elementwise_sub_sat(magnitude, base), top);
+                const u16x2 sign = __builtin_bit_cast(u16x2, __builtin_bit_cast(i16x2, bits) >> (int16_t)15);
+                c = (u16x2)(((top + sign) - (c ^ sign)) << (uint16_t)2);                   // top - c, or top + c where the sign is set; in bytes
+                const uint32_t places = __builtin_bit_cast(uint32_t, c);
+                add(places & 0xFFFFu);
+                add(places >> 16);
+                max = max_or_nan(max, max_or_nan(__uint_as_float(bits << 16), __uint_as_float(bits & 0xFFFF0000u)));
+            };
+            uint32_t at = threadIdx.x * E;
+            for (; at + (kPieces - 1) * THREADS * E + E <= vocab; at += kPieces * THREADS * E) {
+                u32x4 raw[kPieces];
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p) raw[p] = __builtin_bit_cast(u32x4, *reinterpret_cast<const Piece*>(z + at + p * THREADS * E));
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) two(raw[p][i]);
+            }
+            for (; at < vocab; at += THREADS * E) {
+                Piece raw;
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) raw[e] = at + e < vocab ? z[at + e] : (T)-kInf;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) two(__builtin_bit_cast(u32x4, raw)[i]);
+            }
+        } else {
+            const Bins fixed = fixed_bins();
+            const uint32_t nowhere = kFixedBins + (threadIdx.x & 63);
+            stream([&](const float(&v)[E], uint32_t) {
+                max = max_or_nan(max, largest_of(v));
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) {
+                    const uint32_t bin = fixed(v[e]);
+                    atomicAdd(&s.count[bin != kFixedLast ? bin : nowhere], 1u);
+                }
+            });
+        }
+        return max;
+    }
+
     // Gathers the logits from lo to hi (kList of them at most) as ranks; returns how many there are.
-    __device__ uint32_t gather(float lo, float hi) {
+    __device__ __forceinline__ uint32_t gather(float lo, float hi) const {
+        SampleLds<THREADS>& s = sample_lds<THREADS>();
         __syncthreads();
         if (threadIdx.x == 0) s.held = 0;
         __syncthreads();
         stream([&](const float(&v)[E], uint32_t at) {
+            if (!(largest_of(v) >= lo)) return;
 #pragma unroll
             for (uint32_t e = 0; e < E; ++e)
                 if (v[e] >= lo && v[e] <= hi && at + e < vocab) {
@@ -186,7 +256,8 @@ struct Row {
         return s.held;
     }
     // Puts the n gathered logits in order, with the mass through each of them, `before` included.
-    __device__ void settle(uint32_t n, uint64_t before) {
+    __device__ void settle(uint32_t n, uint64_t before) const {
+        SampleLds<THREADS>& s = sample_lds<THREADS>();
         for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
             const uint64_t mine = s.list[i];
             uint32_t place = 0;
@@ -213,7 +284,8 @@ struct Row {
         __syncthreads();
     }
     // Mass through the place in the list where mass reaches t; its index goes to s.index.
-    __device__ uint64_t list_mass(uint32_t n, uint64_t before, uint64_t t) {
+    __device__ uint64_t list_mass(uint32_t n, uint64_t before, uint64_t t) const {
+        SampleLds<THREADS>& s = sample_lds<THREADS>();
         for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
             const uint64_t here = s.upto[i];
             if (here >= t && (i ? s.upto[i - 1] : before) < t) {
@@ -227,7 +299,8 @@ struct Row {
         return through;
     }
     // Mass through the last logit of the list with z - max >= d.
-    __device__ uint64_t list_value(uint32_t n, uint64_t before, double d) {
+    __device__ uint64_t list_value(uint32_t n, uint64_t before, double d) const {
+        SampleLds<THREADS>& s = sample_lds<THREADS>();
         if (threadIdx.x == 0) s.through = before;
         __syncthreads();
         auto kept = [&](uint32_t i) { return (double)of_key((uint32_t)(s.sorted[i] >> 32)) - masses.max >= d; };
@@ -239,8 +312,63 @@ struct Row {
         return through;
     }
 
+    // The column of the nth (from 1) logit that equals `value`, from the row's beginning on until it is there.
+    __device__ void find(float value, uint64_t nth) const {
+        SampleLds<THREADS>& s = sample_lds<THREADS>();
+        uint32_t* const list = reinterpret_cast<uint32_t*>(s.list);                        // columns
+        constexpr uint32_t kRoom = 2 * kList, kStretch = kPieces * THREADS * E;
+        if (nth > kRoom) return find_nth(value, nth);
+        __syncthreads();
+        if (threadIdx.x == 0) s.held = 0;
+        __syncthreads();
+        Piece raw[kPieces], coming[kPieces];
+        auto fetch = [&](uint32_t at) {
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                const uint32_t from = at + (p * THREADS + threadIdx.x) * E;
+                if (from + E <= vocab) coming[p] = *reinterpret_cast<const Piece*>(z + from);
+                else
+#pragma unroll
+                    for (uint32_t e = 0; e < E; ++e) coming[p][e] = from + e < vocab ? z[from + e] : (T)-kInf;
+            }
+        };
+        fetch(0);
+        uint32_t held = 0;
+        for (uint32_t at = 0; at < vocab; at += kStretch) {
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) raw[p] = coming[p];
+            if (at + kStretch < vocab) fetch(at + kStretch);
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                bool some = false;
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) some |= (float)raw[p][e] == value;
+                if (!some) continue;
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e)
+                    if ((float)raw[p][e] == value) {
+                        const uint32_t place = atomicAdd(&s.held, 1u);
+                        if (place < kRoom) list[place] = at + (p * THREADS + threadIdx.x) * E + e;
+                    }
+            }
+            __syncthreads();
+            held = s.held;
+            __syncthreads();
+            if (held >= nth) break;
+        }
+        if (held > kRoom) return find_nth(value, nth);
+        for (uint32_t i = threadIdx.x; i < held; i += THREADS) {
+            const uint32_t mine = list[i];
+            uint32_t place = 0;
+#pragma unroll 8
+            for (uint32_t j = 0; j < held; ++j) place += list[j] < mine ? 1u : 0u;
+            if (place == nth - 1) s.index = mine;
+        }
+        __syncthreads();
+    }
     // The column of the nth (from 1) logit that equals `value`: each wave counts those of a stretch of the row.
-    __device__ void find_nth(float value, uint64_t nth) {
+    __device__ void find_nth(float value, uint64_t nth) const {
+        SampleLds<THREADS>& s = sample_lds<THREADS>();
         const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
         constexpr uint32_t kStep = 64 * E;
         const uint32_t stretch = ((vocab + THREADS / 64 - 1) / (THREADS / 64) + kStep - 1) / kStep * kStep;
@@ -288,19 +416,22 @@ struct Row {
     }
 
     // Logits that are all `value`, n of them (kValue), behind `before`.
-    __device__ uint64_t among_equals(Question q, float value, uint64_t n, uint64_t before, uint64_t t, double d, bool pick) {
+    __device__ uint64_t among_equals(Question q, float value, uint64_t n, uint64_t before, uint64_t t, double d, bool pick) const {
         const uint64_t mass = masses(value);
         if (q == kValue) return before + ((double)value - masses.max >= d ? n * mass : 0);
         const uint64_t nth = q == kCount ? t : (t - before + mass - 1) / mass;
-        if (pick) find_nth(value, nth);
+        if (pick) find(value, nth);
         return before + nth * mass;
     }
 
     // The answer among the logits from lo to hi: the mass through the place where their count (kCount) or the mass, that of logits before them
     // included (kMass), reaches t, or through the last with z - max >= d (kValue).
-    __device__ uint64_t through(Question q, float lo, float hi, uint64_t before, uint64_t t, double d, bool pick) {
+    __device__ uint64_t through(Question q, float lo, float hi, uint64_t before, uint64_t t, double d, bool pick) const {
+        SampleLds<THREADS>& s = sample_lds<THREADS>();
         for (;;) {
             const uint32_t n = gather(lo, hi);
+            if (q == kCount && t > n) t = n;                      // (what is below `least` was counted, too)
+            if (n == 0) return before;
             if (n <= kList) {
                 settle(n, before);
                 if (q == kValue) return list_value(n, before, d);
@@ -358,26 +489,248 @@ struct Row {
     }
 };
 
-template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS) sample_kernel(SampleShape a) {
-    constexpr bool kSingle = std::is_same_v<T, __bf16>;           // a bin is a number
-    constexpr uint32_t E = Pieces<T>::E, kOwn = kBins / THREADS;
-    __shared__ SampleLds<THREADS> s;
-    const uint64_t row = a.row0 + blockIdx.x;
-    Row<T, THREADS> r{s, static_cast<const T*>(a.z) + row * a.z_ld, (uint32_t)a.vocab, {}, {}, 0.f};
-    float temperature = a.each.temperature_dev ? a.each.temperature_dev[row] : a.temperature;
-    const int32_t top_k = a.each.top_k_dev ? a.each.top_k_dev[row] : a.top_k;
-    const float top_p = a.each.top_p_dev ? a.each.top_p_dev[row] : a.top_p, min_p = a.each.min_p_dev ? a.each.min_p_dev[row] : a.min_p;
-    uint32_t k = top_k > 0 && (uint32_t)top_k < r.vocab ? (uint32_t)top_k : 0;
-    if (!(temperature >= __FLT_MIN__ && temperature < kInf)) {    // the largest logit
-        temperature = 1.f;
-        k = 1;
+// What a row is asked for.
+struct Asked {
+    float temperature, top_p, max;
+    uint32_t k;                                                   // 0: all
+    uint64_t u;                                                   // times 2^64
+    bool by_mass, by_value;
+    double border;                                                // of z - max: by_value
+    // what the first logits must reach for top_p of a sum
+    __device__ __forceinline__ uint64_t share(uint64_t sum) const {
+        if (!(top_p > 0.f)) return 1;
+        const uint64_t p = (uint64_t)((double)top_p * 0x1p64), t = __umul64hi(p, sum) + (p * sum ? 1 : 0);
+        return t ? t : 1;
     }
-    const bool by_mass = top_p < 1.f;
+};
 
-    // the largest
+// The mass that is kept, and s.index, out of a list of everything that matters.
+template <typename T, int THREADS>
+__device__ __forceinline__ uint64_t answer_from_list(const Row<T, THREADS>& r, const Asked& a, uint32_t n) {
+    SampleLds<THREADS>& s = sample_lds<THREADS>();
+    r.settle(n, 0);
+    uint64_t sum = s.upto[a.k && a.k < n ? a.k - 1 : n - 1];
+    if (a.by_mass) sum = r.list_mass(n, 0, a.share(sum));
+    if (a.by_value) {
+        const uint64_t kept = r.list_value(n, 0, a.border);
+        sum = kept < sum ? kept : sum;
+    }
+    (void)r.list_mass(n, 0, __umul64hi(a.u, sum) + 1);
+    return sum;
+}
+
+// The bin of the k-th logit (s.bin), the logits before it (s.ahead) and up to its end (s.held): `owned` bins a thread, `own` logits in them, `before` before them.
+template <int THREADS>
+__device__ __forceinline__ void find_kth(uint32_t k, uint32_t before, uint32_t own, uint32_t owned) {
+    SampleLds<THREADS>& s = sample_lds<THREADS>();
+    if (before < k && k <= before + own) {
+        uint32_t upto = before;
+        for (uint32_t i = threadIdx.x * owned;; ++i) {
+            const uint32_t here = s.count[i];
+            if (k <= upto + here) {
+                s.bin = i;
+                s.ahead = upto;
+                s.held = upto + here;
+                break;
+            }
+            upto += here;
+        }
+    }
+    __syncthreads();
+}
+
+// Any row: bins of its own hold masses, and what lies in one of them is gathered.  k_low, k_high: the numbers of the bin of the k-th logit, if k > 0, and k_left the
+// how-manieth of it that is, 0 where this is not known yet.
+template <typename T, int THREADS>
+__device__ __attribute__((noinline)) uint64_t answer_any(Row<T, THREADS> r, Asked a, float k_low, float k_high, uint32_t k_left) {
+    constexpr uint32_t E = Pieces<T>::E, kOwn = kBins / THREADS;
+    SampleLds<THREADS>& s = sample_lds<THREADS>();
+    const Bins bins = bins_of(a.max, a.temperature);
+    __syncthreads();
+    if (a.k && !k_left) {
+        for (uint32_t i = threadIdx.x; i < kBins; i += THREADS) s.count[i] = 0;
+        __syncthreads();
+        r.stream([&](const float(&v)[E], uint32_t) {
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e)
+                if (v[e] >= r.least) atomicAdd(&s.count[bins(v[e])], 1u);
+        });
+        __syncthreads();
+        uint32_t own = 0, all;
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn; ++i) own += s.count[threadIdx.x * kOwn + i];
+        const uint32_t before = before_thread<THREADS>(own, s.counts, all);
+        if (a.k >= all) a.k = 0;
+        if (a.k) {
+            find_kth<THREADS>(a.k, before, own, kOwn);
+            const uint32_t bin = s.bin, upto = s.held;
+            k_left = a.k - s.ahead;
+            k_low = bins.lowest(bin);
+            k_high = bins.highest(bin);
+            if (k_low > r.least) r.least = k_low;
+            __syncthreads();
+            if (upto <= kList) return answer_from_list(r, a, r.gather(r.least, kInf));
+        }
+    }
+    if (a.k && k_low > r.least) r.least = k_low;
+    for (uint32_t i = threadIdx.x; i < kBins; i += THREADS) s.mass[i] = 0;
+    __syncthreads();
+    uint64_t above = 0;                                           // mass before the k-th's bin
+    r.stream([&](const float(&v)[E], uint32_t) {
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e)
+            if (v[e] >= r.least) {
+                const uint64_t mass = r.masses(v[e]);
+                atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[bins(v[e])]), (unsigned long long)mass);
+                if (a.k && v[e] > k_high) above += mass;
+            }
+    });
+    __syncthreads();
+    uint64_t own = 0, sum;
+#pragma unroll
+    for (uint32_t i = 0; i < kOwn; ++i) own += s.mass[threadIdx.x * kOwn + i];
+    const uint64_t before = before_thread<THREADS>(own, s.sums, sum);
+    if (a.k) {
+        (void)before_thread<THREADS>(above, s.sums, above);
+        sum = r.through(kCount, r.least, k_high, above, k_left, 0.0, false);
+    }
+    // the bin in which mass reaches t, or the given one, and what is asked of it
+    auto of_bin = [&](Question q, uint32_t which, uint64_t t, double d, bool pick) {
+        const bool given = q == kValue;
+        if (given ? which / kOwn == threadIdx.x : before < t && t <= before + own) {
+            uint64_t upto = before;
+            for (uint32_t i = threadIdx.x * kOwn;; ++i) {
+                const uint64_t here = s.mass[i];
+                if (given ? i == which : t <= upto + here) {
+                    s.bin = i;
+                    s.before = upto;
+                    break;
+                }
+                upto += here;
+            }
+        }
+        __syncthreads();
+        const uint32_t bin = s.bin;
+        const uint64_t ahead = s.before;
+        __syncthreads();
+        const float lo = bins.lowest(bin);
+        return r.through(q, lo > r.least ? lo : r.least, bins.highest(bin), ahead, t, d, pick);
+    };
+    if (a.by_mass) sum = of_bin(kMass, 0, a.share(sum), 0.0, false);
+    if (a.by_value) {
+        const float at = (float)(r.masses.max + a.border);
+        if (at >= r.least) {
+            const uint64_t kept = of_bin(kValue, bins(at), 0, a.border, false);
+            sum = kept < sum ? kept : sum;
+        }
+    }
+    (void)of_bin(kMass, 0, __umul64hi(a.u, sum) + 1, 0.0, true);
+    __syncthreads();
+    return sum;
+}
+
+// Rows in whose bins every logit is the same number: what is left is arithmetic, and the token the nth of a number.  Returns 0 if there are others near 0.
+template <int THREADS>
+__device__ __forceinline__ uint64_t answer_by_numbers(const Row<__bf16, THREADS>& r, const Asked& a, uint32_t k_bin, uint32_t k_left) {
+    constexpr uint32_t E = Pieces<__bf16>::E, kOwn = kFixedBins / THREADS;
+    SampleLds<THREADS>& s = sample_lds<THREADS>();
+    const Bins bins = fixed_bins();
+    if (s.count[kFixedTop]) {
+        __syncthreads();
+        if (threadIdx.x == 0) s.ahead = 0;
+        __syncthreads();
+        const float tiny = bins.highest(kFixedTop);
+        bool some = false;
+        r.stream([&](const float(&v)[E], uint32_t) {
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) some |= v[e] != 0.f && fabsf(v[e]) <= tiny;
+        });
+        if (some) s.ahead = 1;
+        __syncthreads();
+        if (s.ahead) return 0;
+    }
+    auto number = [&](uint32_t bin) { return bin == kFixedTop ? 0.f : bins.number(bin); };
+    uint64_t own = 0, sum;
+#pragma unroll 1
+    for (uint32_t i = threadIdx.x * kOwn; i < (threadIdx.x + 1) * kOwn; ++i) {
+        const uint32_t n = s.count[i];
+        if (n) own += n * r.masses(number(i));
+    }
+    const uint64_t before = before_thread<THREADS>(own, s.sums, sum);
+    // f(number, mass of each, how many, mass before them), by the thread whose bin it is: where mass reaches t, or the given one
+    auto of_bin = [&](bool given, uint32_t which, uint64_t t, auto f) {
+        if (given ? which / kOwn == threadIdx.x : before < t && t <= before + own) {
+            uint64_t upto = before;
+            for (uint32_t i = threadIdx.x * kOwn;; ++i) {
+                const uint32_t n = s.count[i];
+                const uint64_t each = n || given ? r.masses(number(i)) : 0;
+                if (given ? i == which : t <= upto + n * each) {
+                    f(number(i), each, n, upto);
+                    break;
+                }
+                upto += n * each;
+            }
+        }
+        __syncthreads();
+    };
+    auto kept = [&](auto f, bool given, uint32_t which, uint64_t t) {
+        of_bin(given, which, t, [&](float value, uint64_t each, uint32_t n, uint64_t upto) { s.through = upto + f(value, each, n, upto); });
+        const uint64_t through = s.through;
+        __syncthreads();
+        return through;
+    };
+    if (a.k) sum = kept([&](float, uint64_t each, uint32_t, uint64_t) { return k_left * each; }, true, k_bin, 0);
+    if (a.by_mass) {
+        const uint64_t t = a.share(sum);
+        sum = kept([&](float, uint64_t each, uint32_t, uint64_t upto) { return (t - upto + each - 1) / each * each; }, false, 0, t);
+    }
+    if (a.by_value) {
+        const float at = (float)(r.masses.max + a.border);
+        if (at >= r.least && at > -kFixedMost) {
+            const uint64_t to = kept([&](float value, uint64_t each, uint32_t n, uint64_t) { return (double)value - r.masses.max >= a.border ? n * each : 0; }, true, bins(at), 0);
+            sum = to < sum ? to : sum;
+        }
+    }
+    const uint64_t t = __umul64hi(a.u, sum) + 1;
+    of_bin(false, 0, t, [&](float value, uint64_t each, uint32_t, uint64_t upto) {
+        s.value = value;
+        s.before = (t - upto + each - 1) / each;
+    });
+    r.find(s.value, s.before);
+    return sum;
+}
+
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 6) sample_kernel(SampleShape a) {
+    constexpr bool kNumbers = std::is_same_v<T, __bf16>;          // a bin is a number
+    constexpr uint32_t E = Pieces<T>::E, kOwn = kFixedBins / THREADS;
+    SampleLds<THREADS>& s = sample_lds<THREADS>();
+    const uint64_t row = a.row0 + blockIdx.x;
+    Row<T, THREADS> r{static_cast<const T*>(a.z) + row * a.z_ld, (uint32_t)a.vocab, {}, 0.f};
+    Asked asked;
+    asked.temperature = a.each.temperature_dev ? a.each.temperature_dev[row] : a.temperature;
+    asked.top_p = a.each.top_p_dev ? a.each.top_p_dev[row] : a.top_p;
+    const int32_t top_k = a.each.top_k_dev ? a.each.top_k_dev[row] : a.top_k;
+    const float min_p = a.each.min_p_dev ? a.each.min_p_dev[row] : a.min_p, u = a.u[row];
+    asked.k = top_k > 0 && (uint32_t)top_k < r.vocab ? (uint32_t)top_k : 0;
+    if (!(asked.temperature >= __FLT_MIN__ && asked.temperature < kInf)) {                 // the largest logit
+        asked.temperature = 1.f;
+        asked.k = 1;
+    }
+    asked.by_mass = asked.top_p < 1.f;
+    asked.u = !(u > 0.f) ? 0 : u >= 1.f ? ~0ull : (uint64_t)((double)u * 0x1p64);
+
+    // the largest, and how many logits are in each of the fixed bins
+    const bool few = r.vocab <= kList, counted = !few && (kNumbers || asked.k);
     float max = -kInf;
-    r.stream([&](const float(&v)[E], uint32_t) { max = max_or_nan(max, largest_of(v)); });
+    if (counted) {
+        u32x4* const clear = reinterpret_cast<u32x4*>(s.count);
+        for (uint32_t i = threadIdx.x; i < kFixedBins / 4; i += THREADS) clear[i] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+        max = r.count_and_largest();
+    } else {
+        r.stream([&](const float(&v)[E], uint32_t) { max = max_or_nan(max, largest_of(v)); });
+    }
     max = over_lanes<64>(max, [](float x, float y) { return max_or_nan(x, y); });
     if ((threadIdx.x & 63) == 0) s.most[threadIdx.x / 64] = max;
     __syncthreads();
@@ -390,169 +743,63 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(SampleShape a) {
         }
         return;
     }
-    const bool infinite = max == kInf, by_value = min_p > 0.f && !infinite;                // (infinite ones are alike)
-    const double t64 = (double)temperature;
+    const bool infinite = max == kInf;
+    const double t64 = (double)asked.temperature;
     r.masses.max = (double)max;
     r.masses.scale = 1.44269504088896340736 / t64;
     r.masses.least = infinite ? 0.0 : -1000.0;
     r.masses.bits = 62 - (r.vocab > 1 ? 32 - __builtin_clz(r.vocab - 1) : 0);
     if (r.masses.bits > 51) r.masses.bits = 51;
-    r.bins = bins_of(max, temperature);
     // below: masses of less than half of a unit.  (In 32 bits: off by less than what one unit more of the exponent allows for.)
     r.least = infinite ? kInf : fmaxf((float)((double)max - (r.masses.bits + 2) * 0.69314718055994530942 * t64 - fabs((double)max) * 0x1p-20), -__FLT_MAX__);
-    const double border = !by_value ? -kInf : t64 * log((double)(min_p < 1.f ? min_p : 1.f));    // of z - max
-    const float u = a.u[row];
-    const uint64_t u64 = !(u > 0.f) ? 0 : u >= 1.f ? ~0ull : (uint64_t)((double)u * 0x1p64);
-    // what the first logits must reach for top_p of S
-    auto share = [&](uint64_t sum) {
-        if (!(top_p > 0.f)) return (uint64_t)1;
-        const uint64_t p64 = (uint64_t)((double)top_p * 0x1p64), low = p64 * sum;
-        const uint64_t t = __umul64hi(p64, sum) + (low ? 1 : 0);
-        return t ? t : (uint64_t)1;
-    };
-    auto answer = [&](uint64_t sum) {                             // s.index is the token's
-        if (threadIdx.x != 0) return;
-        const uint32_t index = s.index;
-        a.token[row] = (int32_t)index;
-        const double y = infinite ? 0.0 : ((double)(float)r.z[index] - (double)max) / t64;
-        if (a.logp) a.logp[row] = (float)(y - log(ldexp((double)sum, -r.masses.bits)));
-    };
-    // everything that matters is in the list
-    auto answer_from_list = [&](uint32_t n) {
-        r.settle(n, 0);
-        uint64_t sum = s.upto[k && k < n ? k - 1 : n - 1];
-        if (by_mass) sum = r.list_mass(n, 0, share(sum));
-        if (by_value) {
-            const uint64_t kept = r.list_value(n, 0, border);
-            sum = kept < sum ? kept : sum;
-        }
-        (void)r.list_mass(n, 0, __umul64hi(u64, sum) + 1);
-        answer(sum);
-    };
-    if (r.vocab <= kList) return answer_from_list(r.gather(r.least, kInf));
-
-    // counts of the bins
-    uint32_t k_bin = 0, k_left = 0;                               // the bin of the k-th logit, and the how-manieth of it that is
-    uint32_t count_before = 0, held = 0;
-    if (kSingle || k) {
-        for (uint32_t i = threadIdx.x; i < kBins; i += THREADS) s.count[i] = 0;
-        if (threadIdx.x < 2) s.special[threadIdx.x] = 0;
-        __syncthreads();
-        r.stream([&](const float(&v)[E], uint32_t) {
-#pragma unroll
-            for (uint32_t e = 0; e < E; ++e)
-                if (v[e] >= r.least) {
-                    const uint32_t bin = r.bins(v[e]);
-                    atomicAdd(&s.count[bin], 1u);
-                    if (kSingle && !r.bins.single(bin))
-                        atomicAdd(reinterpret_cast<unsigned long long*>(&s.special[bin == kBins - 1]), (unsigned long long)r.masses(v[e]));
-                }
-        });
-        __syncthreads();
-        uint32_t own = 0;
+    asked.max = max;
+    asked.by_value = min_p > 0.f && !infinite;                    // (infinite ones are alike)
+    asked.border = asked.by_value ? t64 * log((double)(min_p < 1.f ? min_p : 1.f)) : -kInf;
+    const bool fixed = counted && max < kFixedMost && r.least > -kFixedMost;
+    bool listed = few;                                            // everything that matters lies above r.least, and the list has room for it
+    if (asked.by_value && !asked.by_mass && !few) {               // no other filter needs what this one leaves out
+        const float at = (float)((double)max + asked.border), below = at - fabsf(at) * 0x1p-20f;
+        if (below > r.least) r.least = below;
+    }
+    float k_low = 0.f, k_high = 0.f;
+    uint32_t k_bin = 0, k_left = 0;
+    if (fixed && asked.k) {
+        uint32_t own = 0, all;
 #pragma unroll
         for (uint32_t i = 0; i < kOwn; ++i) own += s.count[threadIdx.x * kOwn + i];
-        count_before = before_thread<THREADS>(own, s.counts, held);
-        if (k >= held) k = 0;
-        if (k) {
-            if (count_before < k && k <= count_before + own) {
-                uint32_t upto = count_before;
-                for (uint32_t i = 0; i < kOwn; ++i) {
-                    const uint32_t here = s.count[threadIdx.x * kOwn + i];
-                    if (k <= upto + here) {
-                        s.bin = threadIdx.x * kOwn + i;
-                        s.ahead = upto;
-                        s.held = upto + here;
-                        break;
-                    }
-                    upto += here;
-                }
-            }
-            __syncthreads();
+        const uint32_t before = before_thread<THREADS>(own, s.counts, all);
+        if (asked.k >= all) asked.k = 0;
+        if (asked.k) {
+            find_kth<THREADS>(asked.k, before, own, kOwn);
             k_bin = s.bin;
-            k_left = k - s.ahead;
-            const uint32_t above = s.held;
+            k_left = asked.k - s.ahead;
+            listed = s.held <= kList;
+            k_low = fixed_bins().lowest(k_bin);
+            k_high = fixed_bins().highest(k_bin);
             __syncthreads();
-            if (above <= kList) return answer_from_list(r.gather(r.bins.lowest(k_bin) > r.least ? r.bins.lowest(k_bin) : r.least, kInf));
-            if (!kSingle && r.bins.lowest(k_bin) > r.least) r.least = r.bins.lowest(k_bin);
+            if (listed && k_low > r.least) r.least = k_low;
         }
     }
-    // masses of the bins
-    if constexpr (!kSingle) {
-        for (uint32_t i = threadIdx.x; i < kBins; i += THREADS) s.mass[i] = 0;
-        __syncthreads();
-        r.stream([&](const float(&v)[E], uint32_t) {
-#pragma unroll
-            for (uint32_t e = 0; e < E; ++e)
-                if (v[e] >= r.least)
-                    atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[r.bins(v[e])]), (unsigned long long)r.masses(v[e]));
-        });
-        __syncthreads();
-    }
-    auto mass_of = [&](uint32_t bin) -> uint64_t {
-        if constexpr (kSingle) {
-            if (!r.bins.single(bin)) return s.special[bin == kBins - 1];
-            const uint32_t n = s.count[bin];
-            return n ? n * r.masses(r.bins.number(bin)) : 0;
-        } else {
-            return s.mass[bin];
-        }
-    };
-    uint64_t own = 0, sum;
-#pragma unroll 1
-    for (uint32_t i = 0; i < kOwn; ++i) own += mass_of(threadIdx.x * kOwn + i);
-    const uint64_t mass_before = before_thread<THREADS>(own, s.sums, sum);
-    // s.bin and s.before: the bin in which mass reaches t, or the given one, and the mass before it
-    auto find = [&](bool given, uint32_t which, uint64_t t) {
-        const bool mine = given ? which / kOwn == threadIdx.x : mass_before < t && t <= mass_before + own;
-        if (mine) {
-            uint64_t upto = mass_before;
-            for (uint32_t i = threadIdx.x * kOwn;; ++i) {
-                const uint64_t here = mass_of(i);
-                if (given ? i == which : t <= upto + here) {
-                    s.bin = i;
-                    s.before = upto;
-                    break;
-                }
-                upto += here;
-            }
-        }
-        __syncthreads();
-    };
-    auto through = [&](Question q, uint64_t t, double d, bool pick) {
-        const uint32_t bin = s.bin;
-        const uint64_t before = s.before;
-        __syncthreads();
-        const float hi = r.bins.highest(bin), lo = r.bins.lowest(bin);
-        if (kSingle && r.bins.single(bin)) {
-            const float value = r.bins.number(bin);
-            const uint32_t n = s.count[bin];
-            if (!pick || n > kList) return r.among_equals(q, value, n, before, t, d, pick);
-            return r.through(q, value, value, before, t, d, pick);
-        }
-        return r.through(q, lo > r.least ? lo : r.least, hi, before, t, d, pick);
-    };
-    if (k) {
-        find(true, k_bin, 0);
-        sum = through(kCount, k_left, 0.0, false);
-    }
-    if (by_mass) {
-        const uint64_t t = share(sum);
-        find(false, 0, t);
-        sum = through(kMass, t, 0.0, false);
-    }
-    if (by_value) {
-        const float at = (float)(r.masses.max + border);
-        if (at >= r.least) {
-            find(true, r.bins(at), 0);
-            const uint64_t kept = through(kValue, 0, border, false);
-            sum = kept < sum ? kept : sum;
+    uint64_t sum = 0;
+    bool done = false;
+    if (listed || (!kNumbers && asked.by_value && !asked.by_mass && !asked.k)) {
+        const uint32_t n = r.gather(r.least, kInf);
+        if (n <= kList) {
+            sum = answer_from_list(r, asked, n);
+            done = true;
         }
     }
-    const uint64_t t = __umul64hi(u64, sum) + 1;
-    find(false, 0, t);
-    (void)through(kMass, t, 0.0, true);
-    answer(sum);
+    if constexpr (kNumbers)
+        if (!done && fixed) {
+            sum = answer_by_numbers<THREADS>(r, asked, k_bin, k_left);
+            done = sum != 0;
+        }
+    if (!done) sum = answer_any(r, asked, k_low, k_high, k_left);
+    if (threadIdx.x != 0) return;
+    const uint32_t index = s.index;
+    a.token[row] = (int32_t)index;
+    const double y = infinite ? 0.0 : ((double)(float)r.z[index] - (double)max) / t64;
+    if (a.logp) a.logp[row] = (float)(y - log(ldexp((double)sum, -r.masses.bits)));
 }
 
 template <typename T>
@@ -562,8 +809,8 @@ void launch_sample_of(const SampleArgs& args, hipStream_t stream) {
     for (uint64_t r = 0; r < a.rows; r += kRowsOfLaunch) {
         a.row0 = r;
         const unsigned here = (unsigned)(a.rows - r < kRowsOfLaunch ? a.rows - r : kRowsOfLaunch);
-        if (a.vocab <= 16384) hipLaunchKernelGGL((sample_kernel<T, 256>), dim3(here), dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((sample_kernel<T, 512>), dim3(here), dim3(512), 0, stream, a);
+        if (a.vocab <= 16384) hipLaunchKernelGGL((sample_kernel<T, 256>), dim3(here), dim3(256), sizeof(SampleLds<256>), stream, a);
+        else hipLaunchKernelGGL((sample_kernel<T, 512>), dim3(here), dim3(512), sizeof(SampleLds<512>), stream, a);
     }
 }
 
