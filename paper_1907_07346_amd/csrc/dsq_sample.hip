@@ -15,8 +15,8 @@ namespace dsq {
 namespace {
 
 constexpr uint64_t kRowsOfLaunch = 1u << 21;                      // a launch dimension holds fewer than 2^32 work-items
-constexpr uint32_t kBins = 4096, kList = 512, kParts = 256;       // bins of a row; logits that are ranked at once; bins of a bin
-constexpr uint32_t kAbove = 1536, kOctaves = 1024;                // bins for the logits of the largest one's sign; how far below T they are told apart
+constexpr uint32_t kBins = 2048, kList = 512, kParts = 256;       // bins of a row; logits that are ranked at once; bins of a bin
+constexpr uint32_t kAbove = 768, kOctaves = 1024;                 // bins for the logits of the largest one's sign; how far below T they are told apart
 constexpr int kPieces = 4;                                        // 16-byte pieces that a thread asks for at a time
 
 struct SampleShape : SampleArgs {
@@ -45,6 +45,14 @@ struct Masses {
         return (uint64_t)__double_as_longlong(v) & ((1ull << 52) - 1);
     }
 };
+
+// A number that is the same in every lane, where it costs no register of each.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(uniform(__float_as_uint(v))); }
+__device__ __forceinline__ double uniform(double v) {
+    const uint64_t bits = (uint64_t)__double_as_longlong(v);
+    return __longlong_as_double((long long)((uint64_t)uniform((uint32_t)(bits >> 32)) << 32 | uniform((uint32_t)bits)));
+}
 
 // Bins that follow the order: a logit's is the number that the 15 leading bits of its magnitude make, those below `base` as one, `top` of them above it; what lies
 // behind the last one is in it.
@@ -79,10 +87,13 @@ struct Bins {
     // ... and this is true.
     __device__ __forceinline__ bool single(uint32_t bin) const { return bin != (uint32_t)top && bin != last; }
 };
-// Bins for rows whose largest logit and what matters below it lie between -2^12 and 2^12, whatever it is: 128 of each power of two from 2^-20 on.
-constexpr int32_t kFixedBase = (127 - 20) << 7, kFixedTop = 4095;
-constexpr uint32_t kFixedLast = 2 * kFixedTop, kFixedBins = kFixedLast + 2;                // (a multiple of the threads)
-constexpr float kFixedMost = 4096.f;
+// Bins for rows whose largest logit and what matters below it lie between -4080 and 4080, whatever it is: 128 of each power of two from 2^-20 on.  What lies
+// beyond is mostly masked and would be one address for many: each lane has a bin of its own for it, 64 at either end.
+constexpr int32_t kFixedBase = (127 - 20) << 7, kFixedSide = 4095, kFixedTop = kFixedSide + 63;
+constexpr uint32_t kFixedFirst = 63, kFixedLast = kFixedTop + kFixedSide, kFixedCounts = (kFixedLast + 64 + 3) / 4 * 4;
+constexpr uint32_t kFixedBins = 8192;                             // from kFixedFirst on: those with an answer in them, and two
+constexpr uint32_t kGroups = kFixedBins / 16;
+constexpr float kFixedMost = 4080.f;                              // the first number of those
 __device__ __forceinline__ Bins fixed_bins() { return {kFixedBase, kFixedTop, kFixedLast}; }
 // Bins for any row.
 __device__ __forceinline__ Bins bins_of(float max, float temperature) {
@@ -99,16 +110,19 @@ __device__ __forceinline__ Bins bins_of(float max, float temperature) {
 }
 __device__ __forceinline__ float of_key(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 
-// Of a workgroup; dynamic, so that functions that are not inlined know it as LDS.
 template <int THREADS>
 struct SampleLds {
     union {
-        uint64_t mass[kBins];
-        uint32_t count[kFixedBins + 64];                          // (the last 64: see count_and_largest)
+        uint32_t count[kFixedCounts];
+        uint32_t columns[2 * kList];                              // of a number, when counts are done with
+        struct {
+            uint64_t list[kList], sorted[kList], upto[kList];     // ranks of the logits gathered; in order; the mass through each
+            uint64_t mass[kBins];
+            uint64_t part_mass[kParts];
+            uint32_t part_count[kParts];
+        };
     };
-    uint64_t list[kList], sorted[kList], upto[kList];             // ranks of the logits gathered; in order; the mass through each
-    uint64_t part_mass[kParts];
-    uint32_t part_count[kParts];
+    uint64_t group[kGroups];                                      // counts or masses of sixteen fixed bins each, and then of all before
     uint64_t sums[THREADS / 64];
     uint32_t counts[THREADS / 64];
     float most[THREADS / 64];
@@ -116,9 +130,12 @@ struct SampleLds {
     uint32_t held, bin, ahead, index;
     float value;
 };
-extern __shared__ u32x4 sample_memory[];
-template <int THREADS>
-__device__ __forceinline__ SampleLds<THREADS>& sample_lds() { return *reinterpret_cast<SampleLds<THREADS>*>(sample_memory); }
+// Of a kernel, and of the functions that it calls: one for each, so that it has an address that is known.
+template <typename T, int THREADS>
+__device__ __forceinline__ SampleLds<THREADS>& sample_lds() {
+    __shared__ SampleLds<THREADS> s;
+    return s;
+}
 
 // What lies before the thread's v in the workgroup, and all of it.
 template <int THREADS, typename V>
@@ -146,10 +163,67 @@ __device__ __forceinline__ V before_thread(V v, V* sums, V& all) {
     return before + upto - v;
 }
 
+// The column of the nth (from 1) logit that equals `value`: each wave counts those of a stretch of the row.
+template <typename T, int THREADS>
+__device__ __attribute__((noinline)) void find_nth(const T* z, uint32_t vocab, float value, uint64_t nth) {
+    constexpr uint32_t E = Pieces<T>::E;
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    constexpr uint32_t kStep = 64 * E;
+    const uint32_t stretch = ((vocab + THREADS / 64 - 1) / (THREADS / 64) + kStep - 1) / kStep * kStep;
+    const uint64_t begin = (uint64_t)wave * stretch;
+    const uint32_t from = begin < vocab ? (uint32_t)begin : vocab, to = vocab - from < stretch ? vocab : from + stretch;
+    auto equal = [&](uint32_t at) {                           // bits of the lane's elements that are it
+        uint32_t bits = 0;
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e)
+            if (at + e < to && (float)z[at + e] == value) bits |= 1u << e;
+        return bits;
+    };
+    uint32_t mine = 0, all;
+    for (uint32_t at = from + lane * E; at < to; at += kStep) mine += (uint32_t)__popc(equal(at));
+    uint64_t before = before_thread<THREADS>(mine, s.counts, all);
+    before = (uint64_t)(uint32_t)__shfl((int)before, 0);      // of the wave
+    const uint32_t of_wave = s.counts[wave];
+    if (nth <= before || nth > before + of_wave) {
+        __syncthreads();
+        return;
+    }
+    uint64_t left = nth - before;
+    for (uint32_t base = from; base < to; base += kStep) {
+        const uint32_t at = base + lane * E, bits = at < to ? equal(at) : 0;
+        uint32_t upto = (uint32_t)__popc(bits);
+        const uint32_t own = upto;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t other = (uint32_t)__shfl_up((int)upto, o);
+            if (lane >= (uint32_t)o) upto += other;
+        }
+        const uint32_t total = (uint32_t)__shfl((int)upto, 63);
+        if (left > total) {
+            left -= total;
+            continue;
+        }
+        if (left <= upto && left > upto - own) {
+            uint32_t rest = bits;
+            for (uint64_t i = left - (upto - own); i > 1; --i) rest &= rest - 1;
+            s.index = at + (uint32_t)__builtin_ctz(rest);
+        }
+        break;
+    }
+    __syncthreads();
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint64_t other_lane64(uint64_t v) {
+    return (uint64_t)other_lane<CTRL>((uint32_t)(v >> 32)) << 32 | other_lane<CTRL>((uint32_t)v);
+}
+
 enum Question { kCount, kMass, kValue };                          // at which place do count or mass reach a number, or logits a value
 
 template <typename T, int THREADS>
 struct Row {
+    static constexpr bool kNumbers = std::is_same_v<T, __bf16>;   // a bin is a number
     static constexpr uint32_t E = Pieces<T>::E;
     using Piece = typename Pieces<T>::Piece;
     const T* z;
@@ -181,29 +255,25 @@ struct Row {
         }
     }
 
-    // The thread's largest logit, and all of them counted in fixed bins, but for those of the last one: they are mostly masked, which would be one address for many.
-    // They go to a place of the lane's.
-    __device__ __forceinline__ float count_and_largest() const {
-        SampleLds<THREADS>& s = sample_lds<THREADS>();
-        float max = -kInf;
-        if constexpr (std::is_same_v<T, __bf16>) {                // two at a time
+    // Counts logits in fixed bins.  Returns the thread's largest one; of bf16, whose bins tell it, the largest magnitudes of either half of its words.
+    __device__ __forceinline__ uint32_t count_fixed() const {
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+        auto add = [&](uint32_t place) { atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.count) + place), 1u); };
+        const uint32_t most = kFixedSide + (threadIdx.x & 63);
+        if constexpr (kNumbers) {                                 // two at a time
             typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
             typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
-            const uint32_t nowhere = (kFixedBins + (threadIdx.x & 63)) * 4;
-            auto add = [&](uint32_t place) {
-                place = place != kFixedLast * 4 ? place : nowhere;
-                atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.count) + place), 1u);
-            };
+            const u16x2 base = (uint16_t)kFixedBase, side = (uint16_t)most, top = (uint16_t)(4 * kFixedTop);
+            u16x2 largest = 0;
             auto two = [&](uint32_t bits) {
                 const u16x2 magnitude = __builtin_bit_cast(u16x2, bits & 0x7FFF7FFFu);
-                const u16x2 base = (uint16_t)kFixedBase, top = (uint16_t)kFixedTop;
-                u16x2 c = __builtin_elementwise_min(__builtin_elementwise_sub_sat(magnitude, base), top);
+                largest = __builtin_elementwise_max(largest, magnitude);
+                u16x2 c = __builtin_elementwise_min(__builtin_elementwise_sub_sat(magnitude, base), side);
                 const u16x2 sign = __builtin_bit_cast(u16x2, __builtin_bit_cast(i16x2, bits) >> (int16_t)15);
-                c = (u16x2)(((top + sign) - (c ^ sign)) << (uint16_t)2);                   // top - c, or top + c where the sign is set; in bytes
+                c = (u16x2)(((sign - (c ^ sign)) << (uint16_t)2) + top);                   // top - c, or top + c where the sign is set; in bytes
                 const uint32_t places = __builtin_bit_cast(uint32_t, c);
                 add(places & 0xFFFFu);
                 add(places >> 16);
-                max = max_or_nan(max, max_or_nan(__uint_as_float(bits << 16), __uint_as_float(bits & 0xFFFF0000u)));
             };
             uint32_t at = threadIdx.x * E;
             for (; at + (kPieces - 1) * THREADS * E + E <= vocab; at += kPieces * THREADS * E) {
@@ -222,24 +292,91 @@ struct Row {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) two(__builtin_bit_cast(u32x4, raw)[i]);
             }
+            return __builtin_bit_cast(uint32_t, largest);
         } else {
-            const Bins fixed = fixed_bins();
-            const uint32_t nowhere = kFixedBins + (threadIdx.x & 63);
+            float max = -kInf;
             stream([&](const float(&v)[E], uint32_t) {
                 max = max_or_nan(max, largest_of(v));
 #pragma unroll
                 for (uint32_t e = 0; e < E; ++e) {
-                    const uint32_t bin = fixed(v[e]);
-                    atomicAdd(&s.count[bin != kFixedLast ? bin : nowhere], 1u);
+                    const uint32_t bits = __float_as_uint(v[e]), sign = (uint32_t)((int32_t)bits >> 31);
+                    uint32_t c = __builtin_elementwise_sub_sat(bits >> 16 & 0x7FFFu, (uint32_t)kFixedBase);
+                    c = c < most ? c : most;
+                    add((sign - (c ^ sign) + kFixedTop) * 4);
                 }
             });
+            return __float_as_uint(max);
         }
-        return max;
+    }
+    __device__ __forceinline__ uint32_t fixed_count(uint32_t bin) const { return bin < kFixedLast ? sample_lds<T, THREADS>().count[bin] : 0; }
+    // s.group: what of(bin, its count) gives for sixteen bins, summed up over all groups before.  Returns the sum of all.
+    template <typename F>
+    __device__ __forceinline__ uint64_t sum_groups(F of) const {
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+#pragma unroll 1
+        for (uint32_t i = threadIdx.x; i < kFixedBins; i += THREADS) {
+            const uint32_t n = fixed_count(kFixedFirst + i);
+            uint64_t sum = 0;
+            if (__ballot(n != 0)) {
+                if (n) sum = of(kFixedFirst + i, n);
+                sum += other_lane64<0xB1>(sum);
+                sum += other_lane64<0x4E>(sum);
+                sum += other_lane64<0x141>(sum);
+                sum += other_lane64<0x140>(sum);
+            }
+            if ((threadIdx.x & 15) == 0) s.group[i / 16] = sum;
+        }
+        __syncthreads();
+        constexpr uint32_t kEach = kGroups / THREADS;
+        uint64_t own[kEach], sum = 0, all;
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) {
+            own[i] = s.group[threadIdx.x * kEach + i];
+            sum += own[i];
+        }
+        uint64_t before = before_thread<THREADS>(sum, s.sums, all);
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) {
+            s.group[threadIdx.x * kEach + i] = before;
+            before += own[i];
+        }
+        __syncthreads();
+        return all;
+    }
+    // In a wave: the bin in which the sum reaches t (1 <= t <= all), or `bin` itself, what of(bin, count) gives for it and what lies before it.
+    struct FoundBin {
+        uint32_t bin;
+        uint64_t here, before;
+    };
+    template <typename F>
+    __device__ __forceinline__ FoundBin find_bin(bool given, uint32_t bin, uint64_t t, F of) const {
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+        const uint32_t lane = threadIdx.x & 63;
+        uint32_t group;
+        if (given) {
+            group = (bin - kFixedFirst) / 16;
+        } else {
+            group = 0;
+#pragma unroll
+            for (uint32_t i = 0; i < kGroups; i += 64) group += (uint32_t)__popcll(__ballot(s.group[i + lane] < t));
+            --group;                                              // (the first group has nothing before it)
+        }
+        const uint32_t mine = kFixedFirst + group * 16 + (lane & 15), n = fixed_count(mine);
+        const uint64_t here = n ? of(mine, n) : 0, ahead = s.group[group];
+        uint64_t upto = here;
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) {
+            const uint64_t other = (uint64_t)__shfl_up((unsigned long long)upto, o, 16);
+            if ((lane & 15) >= (uint32_t)o) upto += other;
+        }
+        upto += ahead;
+        const uint32_t at = given ? (bin - kFixedFirst) % 16 : (uint32_t)__builtin_ctzll(__ballot(upto >= t));
+        return {kFixedFirst + group * 16 + at, (uint64_t)__shfl((unsigned long long)here, (int)at), (uint64_t)__shfl((unsigned long long)(upto - here), (int)at)};
     }
 
     // Gathers the logits from lo to hi (kList of them at most) as ranks; returns how many there are.
     __device__ __forceinline__ uint32_t gather(float lo, float hi) const {
-        SampleLds<THREADS>& s = sample_lds<THREADS>();
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
         __syncthreads();
         if (threadIdx.x == 0) s.held = 0;
         __syncthreads();
@@ -257,7 +394,7 @@ struct Row {
     }
     // Puts the n gathered logits in order, with the mass through each of them, `before` included.
     __device__ void settle(uint32_t n, uint64_t before) const {
-        SampleLds<THREADS>& s = sample_lds<THREADS>();
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
         for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
             const uint64_t mine = s.list[i];
             uint32_t place = 0;
@@ -285,7 +422,7 @@ struct Row {
     }
     // Mass through the place in the list where mass reaches t; its index goes to s.index.
     __device__ uint64_t list_mass(uint32_t n, uint64_t before, uint64_t t) const {
-        SampleLds<THREADS>& s = sample_lds<THREADS>();
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
         for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
             const uint64_t here = s.upto[i];
             if (here >= t && (i ? s.upto[i - 1] : before) < t) {
@@ -300,7 +437,7 @@ struct Row {
     }
     // Mass through the last logit of the list with z - max >= d.
     __device__ uint64_t list_value(uint32_t n, uint64_t before, double d) const {
-        SampleLds<THREADS>& s = sample_lds<THREADS>();
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
         if (threadIdx.x == 0) s.through = before;
         __syncthreads();
         auto kept = [&](uint32_t i) { return (double)of_key((uint32_t)(s.sorted[i] >> 32)) - masses.max >= d; };
@@ -313,23 +450,51 @@ struct Row {
     }
 
     // The column of the nth (from 1) logit that equals `value`, from the row's beginning on until it is there.
-    __device__ void find(float value, uint64_t nth) const {
-        SampleLds<THREADS>& s = sample_lds<THREADS>();
-        uint32_t* const list = reinterpret_cast<uint32_t*>(s.list);                        // columns
+    __device__ __forceinline__ void find(float value, uint64_t nth) const {
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
         constexpr uint32_t kRoom = 2 * kList, kStretch = kPieces * THREADS * E;
-        if (nth > kRoom) return find_nth(value, nth);
+        if (nth > kRoom) return find_nth<T, THREADS>(z, vocab, value, nth);
         __syncthreads();
         if (threadIdx.x == 0) s.held = 0;
         __syncthreads();
-        Piece raw[kPieces], coming[kPieces];
+        // equal numbers are equal bits, but for the sign of 0
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        uint32_t bits, keep = ~0u;
+        if constexpr (sizeof(T) == 2) {
+            bits = __builtin_bit_cast(uint16_t, (T)value) * 0x10001u;
+            if (value == 0.f) keep = 0x7FFF7FFFu;
+        } else {
+            bits = __float_as_uint(value);
+            if (value == 0.f) keep = 0x7FFFFFFFu;
+        }
+        bits &= keep;
+        auto is = [&](u32x4 raw, uint32_t e) {
+            if constexpr (sizeof(T) == 2) return (((raw[e / 2] & keep) ^ bits) >> (16 * (e & 1)) & 0xFFFFu) == 0;
+            else return ((raw[e] & keep) ^ bits) == 0;
+        };
+        auto any = [&](u32x4 raw) {
+            u32x4 d;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[i] = (raw[i] & keep) ^ bits;
+            if constexpr (sizeof(T) == 2) {
+                auto least = [](uint32_t x, uint32_t y) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y))); };
+                const uint32_t m = least(least(d[0], d[1]), least(d[2], d[3]));
+                return (m & 0xFFFFu) == 0 || m < 0x10000u;
+            } else {
+                return d[0] == 0 || d[1] == 0 || d[2] == 0 || d[3] == 0;
+            }
+        };
+        u32x4 raw[kPieces], coming[kPieces];
         auto fetch = [&](uint32_t at) {
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) {
                 const uint32_t from = at + (p * THREADS + threadIdx.x) * E;
-                if (from + E <= vocab) coming[p] = *reinterpret_cast<const Piece*>(z + from);
+                Piece piece;
+                if (from + E <= vocab) piece = *reinterpret_cast<const Piece*>(z + from);
                 else
 #pragma unroll
-                    for (uint32_t e = 0; e < E; ++e) coming[p][e] = from + e < vocab ? z[from + e] : (T)-kInf;
+                    for (uint32_t e = 0; e < E; ++e) piece[e] = from + e < vocab ? z[from + e] : (T)-kInf;
+                coming[p] = __builtin_bit_cast(u32x4, piece);
             }
         };
         fetch(0);
@@ -340,15 +505,12 @@ struct Row {
             if (at + kStretch < vocab) fetch(at + kStretch);
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) {
-                bool some = false;
-#pragma unroll
-                for (uint32_t e = 0; e < E; ++e) some |= (float)raw[p][e] == value;
-                if (!some) continue;
+                if (!any(raw[p])) continue;
 #pragma unroll
                 for (uint32_t e = 0; e < E; ++e)
-                    if ((float)raw[p][e] == value) {
+                    if (is(raw[p], e)) {
                         const uint32_t place = atomicAdd(&s.held, 1u);
-                        if (place < kRoom) list[place] = at + (p * THREADS + threadIdx.x) * E + e;
+                        if (place < kRoom) s.columns[place] = at + (p * THREADS + threadIdx.x) * E + e;
                     }
             }
             __syncthreads();
@@ -356,65 +518,16 @@ struct Row {
             __syncthreads();
             if (held >= nth) break;
         }
-        if (held > kRoom) return find_nth(value, nth);
+        if (held > kRoom) return find_nth<T, THREADS>(z, vocab, value, nth);
         for (uint32_t i = threadIdx.x; i < held; i += THREADS) {
-            const uint32_t mine = list[i];
+            const uint32_t mine = s.columns[i];
             uint32_t place = 0;
 #pragma unroll 8
-            for (uint32_t j = 0; j < held; ++j) place += list[j] < mine ? 1u : 0u;
+            for (uint32_t j = 0; j < held; ++j) place += s.columns[j] < mine ? 1u : 0u;
             if (place == nth - 1) s.index = mine;
         }
         __syncthreads();
     }
-    // The column of the nth (from 1) logit that equals `value`: each wave counts those of a stretch of the row.
-    __device__ void find_nth(float value, uint64_t nth) const {
-        SampleLds<THREADS>& s = sample_lds<THREADS>();
-        const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-        constexpr uint32_t kStep = 64 * E;
-        const uint32_t stretch = ((vocab + THREADS / 64 - 1) / (THREADS / 64) + kStep - 1) / kStep * kStep;
-        const uint64_t begin = (uint64_t)wave * stretch;
-        const uint32_t from = begin < vocab ? (uint32_t)begin : vocab, to = vocab - from < stretch ? vocab : from + stretch;
-        auto equal = [&](uint32_t at) {                           // bits of the lane's elements that are it
-            uint32_t bits = 0;
-#pragma unroll
-            for (uint32_t e = 0; e < E; ++e)
-                if (at + e < to && (float)z[at + e] == value) bits |= 1u << e;
-            return bits;
-        };
-        uint32_t mine = 0, all;
-        for (uint32_t at = from + lane * E; at < to; at += kStep) mine += (uint32_t)__popc(equal(at));
-        uint64_t before = before_thread<THREADS>(mine, s.counts, all);
-        before = (uint64_t)(uint32_t)__shfl((int)before, 0);      // of the wave
-        const uint32_t of_wave = s.counts[wave];
-        if (nth <= before || nth > before + of_wave) {
-            __syncthreads();
-            return;
-        }
-        uint64_t left = nth - before;
-        for (uint32_t base = from; base < to; base += kStep) {
-            const uint32_t at = base + lane * E, bits = at < to ? equal(at) : 0;
-            uint32_t upto = (uint32_t)__popc(bits);
-            const uint32_t own = upto;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const uint32_t other = (uint32_t)__shfl_up((int)upto, o);
-                if (lane >= (uint32_t)o) upto += other;
-            }
-            const uint32_t total = (uint32_t)__shfl((int)upto, 63);
-            if (left > total) {
-                left -= total;
-                continue;
-            }
-            if (left <= upto && left > upto - own) {
-                uint32_t rest = bits;
-                for (uint64_t i = left - (upto - own); i > 1; --i) rest &= rest - 1;
-                s.index = at + (uint32_t)__builtin_ctz(rest);
-            }
-            break;
-        }
-        __syncthreads();
-    }
-
     // Logits that are all `value`, n of them (kValue), behind `before`.
     __device__ uint64_t among_equals(Question q, float value, uint64_t n, uint64_t before, uint64_t t, double d, bool pick) const {
         const uint64_t mass = masses(value);
@@ -423,71 +536,73 @@ struct Row {
         if (pick) find(value, nth);
         return before + nth * mass;
     }
-
-    // The answer among the logits from lo to hi: the mass through the place where their count (kCount) or the mass, that of logits before them
-    // included (kMass), reaches t, or through the last with z - max >= d (kValue).
-    __device__ uint64_t through(Question q, float lo, float hi, uint64_t before, uint64_t t, double d, bool pick) const {
-        SampleLds<THREADS>& s = sample_lds<THREADS>();
-        for (;;) {
-            const uint32_t n = gather(lo, hi);
-            if (q == kCount && t > n) t = n;                      // (what is below `least` was counted, too)
-            if (n == 0) return before;
-            if (n <= kList) {
-                settle(n, before);
-                if (q == kValue) return list_value(n, before, d);
-                if (q == kMass) return list_mass(n, before, t);
-                return s.upto[t - 1];
-            }
-            if (lo == hi) return among_equals(q, lo, n, before, t, d, pick);
-            // too many: bins of their own
-            const uint32_t first = logit_key(hi), last = logit_key(lo);
-            int shift = 0;
-            while ((first - last) >> shift >= kParts) ++shift;
-            __syncthreads();
-            for (uint32_t i = threadIdx.x; i < kParts; i += THREADS) {
-                s.part_mass[i] = 0;
-                s.part_count[i] = 0;
-            }
-            __syncthreads();
-            stream([&](const float(&v)[E], uint32_t at) {
-#pragma unroll
-                for (uint32_t e = 0; e < E; ++e)
-                    if (v[e] >= lo && v[e] <= hi && at + e < vocab) {
-                        const uint32_t part = (first - logit_key(v[e])) >> shift;
-                        atomicAdd(&s.part_count[part], 1u);
-                        atomicAdd(reinterpret_cast<unsigned long long*>(&s.part_mass[part]), (unsigned long long)masses(v[e]));
-                    }
-            });
-            __syncthreads();
-            const uint64_t mass = threadIdx.x < kParts ? s.part_mass[threadIdx.x] : 0;
-            const uint32_t count = threadIdx.x < kParts ? s.part_count[threadIdx.x] : 0;
-            uint64_t all_mass;
-            uint32_t all_count;
-            const uint64_t mass_before = before + before_thread<THREADS>(mass, s.sums, all_mass);
-            const uint32_t ahead = before_thread<THREADS>(count, s.counts, all_count);
-            bool here;
-            if (q == kCount) here = ahead < t && t <= (uint64_t)ahead + count;
-            else if (q == kMass) here = mass_before < t && t <= mass_before + mass;
-            else {
-                float border = (float)(masses.max + d);
-                border = border > hi ? hi : border < lo ? lo : border;
-                here = threadIdx.x == (first - logit_key(border)) >> shift;
-            }
-            if (here) {
-                s.bin = threadIdx.x;
-                s.before = mass_before;
-                s.ahead = ahead;
-            }
-            __syncthreads();
-            const uint32_t high = first - (s.bin << shift), low = high - ((1u << shift) - 1);
-            hi = of_key(high == 0x7FFFFFFFu ? high - 1 : high);   // (-0 has the key of +0, which is above)
-            lo = high - last < (1u << shift) ? of_key(last) : of_key(low);
-            before = s.before;
-            if (q == kCount) t -= s.ahead;
-            __syncthreads();
-        }
-    }
 };
+
+// The answer among the logits from lo to hi: the mass through the place where their count (kCount) or the mass, that of logits before them
+// included (kMass), reaches t, or through the last with z - max >= d (kValue).
+template <typename T, int THREADS>
+__device__ __attribute__((noinline)) uint64_t through(Row<T, THREADS> r, Question q, float lo, float hi, uint64_t before, uint64_t t, double d, bool pick) {
+    constexpr uint32_t E = Pieces<T>::E;
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+    for (;;) {
+        const uint32_t n = r.gather(lo, hi);
+        if (q == kCount && t > n) t = n;                      // (what is below `least` was counted, too)
+        if (n == 0) return before;
+        if (n <= kList) {
+            r.settle(n, before);
+            if (q == kValue) return r.list_value(n, before, d);
+            if (q == kMass) return r.list_mass(n, before, t);
+            return s.upto[t - 1];
+        }
+        if (lo == hi) return r.among_equals(q, lo, n, before, t, d, pick);
+        // too many: bins of their own
+        const uint32_t first = logit_key(hi), last = logit_key(lo);
+        int shift = 0;
+        while ((first - last) >> shift >= kParts) ++shift;
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < kParts; i += THREADS) {
+            s.part_mass[i] = 0;
+            s.part_count[i] = 0;
+        }
+        __syncthreads();
+        r.stream([&](const float(&v)[E], uint32_t at) {
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e)
+                if (v[e] >= lo && v[e] <= hi && at + e < r.vocab) {
+                    const uint32_t part = (first - logit_key(v[e])) >> shift;
+                    atomicAdd(&s.part_count[part], 1u);
+                    atomicAdd(reinterpret_cast<unsigned long long*>(&s.part_mass[part]), (unsigned long long)r.masses(v[e]));
+                }
+        });
+        __syncthreads();
+        const uint64_t mass = threadIdx.x < kParts ? s.part_mass[threadIdx.x] : 0;
+        const uint32_t count = threadIdx.x < kParts ? s.part_count[threadIdx.x] : 0;
+        uint64_t all_mass;
+        uint32_t all_count;
+        const uint64_t mass_before = before + before_thread<THREADS>(mass, s.sums, all_mass);
+        const uint32_t ahead = before_thread<THREADS>(count, s.counts, all_count);
+        bool here;
+        if (q == kCount) here = ahead < t && t <= (uint64_t)ahead + count;
+        else if (q == kMass) here = mass_before < t && t <= mass_before + mass;
+        else {
+            float border = (float)(r.masses.max + d);
+            border = border > hi ? hi : border < lo ? lo : border;
+            here = threadIdx.x == (first - logit_key(border)) >> shift;
+        }
+        if (here) {
+            s.bin = threadIdx.x;
+            s.before = mass_before;
+            s.ahead = ahead;
+        }
+        __syncthreads();
+        const uint32_t high = first - (s.bin << shift), low = high - ((1u << shift) - 1);
+        hi = of_key(high == 0x7FFFFFFFu ? high - 1 : high);   // (-0 has the key of +0, which is above)
+        lo = high - last < (1u << shift) ? of_key(last) : of_key(low);
+        before = s.before;
+        if (q == kCount) t -= s.ahead;
+        __syncthreads();
+    }
+}
 
 // What a row is asked for.
 struct Asked {
@@ -507,7 +622,7 @@ struct Asked {
 // The mass that is kept, and s.index, out of a list of everything that matters.
 template <typename T, int THREADS>
 __device__ __forceinline__ uint64_t answer_from_list(const Row<T, THREADS>& r, const Asked& a, uint32_t n) {
-    SampleLds<THREADS>& s = sample_lds<THREADS>();
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
     r.settle(n, 0);
     uint64_t sum = s.upto[a.k && a.k < n ? a.k - 1 : n - 1];
     if (a.by_mass) sum = r.list_mass(n, 0, a.share(sum));
@@ -519,14 +634,15 @@ __device__ __forceinline__ uint64_t answer_from_list(const Row<T, THREADS>& r, c
     return sum;
 }
 
-// The bin of the k-th logit (s.bin), the logits before it (s.ahead) and up to its end (s.held): `owned` bins a thread, `own` logits in them, `before` before them.
-template <int THREADS>
-__device__ __forceinline__ void find_kth(uint32_t k, uint32_t before, uint32_t own, uint32_t owned) {
-    SampleLds<THREADS>& s = sample_lds<THREADS>();
+// The bin of the k-th logit (s.bin), the logits before it (s.ahead) and up to its end (s.held): the thread's bins begin with `first` and have `own` logits, and
+// there are `before` before them; count(bin).
+template <typename T, int THREADS, typename C>
+__device__ __forceinline__ void find_kth(uint32_t k, uint32_t before, uint32_t own, uint32_t first, C count) {
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
     if (before < k && k <= before + own) {
         uint32_t upto = before;
-        for (uint32_t i = threadIdx.x * owned;; ++i) {
-            const uint32_t here = s.count[i];
+        for (uint32_t i = first;; ++i) {
+            const uint32_t here = count(i);
             if (k <= upto + here) {
                 s.bin = i;
                 s.ahead = upto;
@@ -542,9 +658,11 @@ __device__ __forceinline__ void find_kth(uint32_t k, uint32_t before, uint32_t o
 // Any row: bins of its own hold masses, and what lies in one of them is gathered.  k_low, k_high: the numbers of the bin of the k-th logit, if k > 0, and k_left the
 // how-manieth of it that is, 0 where this is not known yet.
 template <typename T, int THREADS>
-__device__ __attribute__((noinline)) uint64_t answer_any(Row<T, THREADS> r, Asked a, float k_low, float k_high, uint32_t k_left) {
+__device__ __attribute__((noinline)) uint64_t answer_any(Row<T, THREADS> r, float temperature, float top_p, float max, uint32_t k, uint64_t u, double border,
+                                                           float k_low, float k_high, uint32_t k_left) {
+    Asked a{temperature, top_p, max, k, u, top_p < 1.f, border != -kInf, border};
     constexpr uint32_t E = Pieces<T>::E, kOwn = kBins / THREADS;
-    SampleLds<THREADS>& s = sample_lds<THREADS>();
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
     const Bins bins = bins_of(a.max, a.temperature);
     __syncthreads();
     if (a.k && !k_left) {
@@ -562,7 +680,7 @@ __device__ __attribute__((noinline)) uint64_t answer_any(Row<T, THREADS> r, Aske
         const uint32_t before = before_thread<THREADS>(own, s.counts, all);
         if (a.k >= all) a.k = 0;
         if (a.k) {
-            find_kth<THREADS>(a.k, before, own, kOwn);
+            find_kth<T, THREADS>(a.k, before, own, threadIdx.x * kOwn, [&](uint32_t i) { return s.count[i]; });
             const uint32_t bin = s.bin, upto = s.held;
             k_left = a.k - s.ahead;
             k_low = bins.lowest(bin);
@@ -592,7 +710,7 @@ __device__ __attribute__((noinline)) uint64_t answer_any(Row<T, THREADS> r, Aske
     const uint64_t before = before_thread<THREADS>(own, s.sums, sum);
     if (a.k) {
         (void)before_thread<THREADS>(above, s.sums, above);
-        sum = r.through(kCount, r.least, k_high, above, k_left, 0.0, false);
+        sum = through(r, kCount, r.least, k_high, above, k_left, 0.0, false);
     }
     // the bin in which mass reaches t, or the given one, and what is asked of it
     auto of_bin = [&](Question q, uint32_t which, uint64_t t, double d, bool pick) {
@@ -614,7 +732,7 @@ __device__ __attribute__((noinline)) uint64_t answer_any(Row<T, THREADS> r, Aske
         const uint64_t ahead = s.before;
         __syncthreads();
         const float lo = bins.lowest(bin);
-        return r.through(q, lo > r.least ? lo : r.least, bins.highest(bin), ahead, t, d, pick);
+        return through(r, q, lo > r.least ? lo : r.least, bins.highest(bin), ahead, t, d, pick);
     };
     if (a.by_mass) sum = of_bin(kMass, 0, a.share(sum), 0.0, false);
     if (a.by_value) {
@@ -629,82 +747,81 @@ __device__ __attribute__((noinline)) uint64_t answer_any(Row<T, THREADS> r, Aske
     return sum;
 }
 
-// Rows in whose bins every logit is the same number: what is left is arithmetic, and the token the nth of a number.  Returns 0 if there are others near 0.
-template <int THREADS>
-__device__ __forceinline__ uint64_t answer_by_numbers(const Row<__bf16, THREADS>& r, const Asked& a, uint32_t k_bin, uint32_t k_left) {
-    constexpr uint32_t E = Pieces<__bf16>::E, kOwn = kFixedBins / THREADS;
-    SampleLds<THREADS>& s = sample_lds<THREADS>();
+// Rows in whose bins every logit is the same number: what is left is arithmetic, and the token the nth of a number.  Returns 0 if the answer hangs on what lies
+// around 0, which may be several.
+template <typename T, int THREADS>
+__device__ __forceinline__ uint64_t answer_by_numbers(const Row<T, THREADS>& r, const Asked& a, uint32_t k_bin, uint32_t k_left) {
+    constexpr uint32_t E = Pieces<T>::E;
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
     const Bins bins = fixed_bins();
+    uint64_t zeros = 0;
     if (s.count[kFixedTop]) {
-        __syncthreads();
-        if (threadIdx.x == 0) s.ahead = 0;
-        __syncthreads();
         const float tiny = bins.highest(kFixedTop);
+        uint64_t mine = 0;
         bool some = false;
         r.stream([&](const float(&v)[E], uint32_t) {
 #pragma unroll
-            for (uint32_t e = 0; e < E; ++e) some |= v[e] != 0.f && fabsf(v[e]) <= tiny;
+            for (uint32_t e = 0; e < E; ++e)
+                if (fabsf(v[e]) <= tiny) {
+                    mine += r.masses(v[e]);
+                    some |= v[e] != 0.f;
+                }
         });
         if (some) s.ahead = 1;
-        __syncthreads();
-        if (s.ahead) return 0;
+        (void)before_thread<THREADS>(mine, s.sums, zeros);
     }
-    auto number = [&](uint32_t bin) { return bin == kFixedTop ? 0.f : bins.number(bin); };
-    uint64_t own = 0, sum;
-#pragma unroll 1
-    for (uint32_t i = threadIdx.x * kOwn; i < (threadIdx.x + 1) * kOwn; ++i) {
-        const uint32_t n = s.count[i];
-        if (n) own += n * r.masses(number(i));
-    }
-    const uint64_t before = before_thread<THREADS>(own, s.sums, sum);
-    // f(number, mass of each, how many, mass before them), by the thread whose bin it is: where mass reaches t, or the given one
-    auto of_bin = [&](bool given, uint32_t which, uint64_t t, auto f) {
-        if (given ? which / kOwn == threadIdx.x : before < t && t <= before + own) {
-            uint64_t upto = before;
-            for (uint32_t i = threadIdx.x * kOwn;; ++i) {
-                const uint32_t n = s.count[i];
-                const uint64_t each = n || given ? r.masses(number(i)) : 0;
-                if (given ? i == which : t <= upto + n * each) {
-                    f(number(i), each, n, upto);
-                    break;
-                }
-                upto += n * each;
+    auto number = [&](uint32_t bin) { return bin == (uint32_t)kFixedTop ? 0.f : bins.number(bin); };
+    auto mass = [&](uint32_t bin, uint32_t n) { return bin == (uint32_t)kFixedTop ? zeros : n * r.masses(bins.number(bin)); };
+    uint64_t sum = r.sum_groups(mass);
+    if (threadIdx.x < 64) {
+        bool known = true;
+        auto each_of = [&](uint32_t bin) {
+            const uint64_t each = r.masses(number(bin));
+            if (bin == (uint32_t)kFixedTop && s.ahead) known = false;
+            return each;
+        };
+        if (a.k) {
+            const auto f = r.find_bin(true, k_bin, 0, mass);
+            sum = f.before + k_left * each_of(k_bin);
+        }
+        if (a.by_mass) {
+            const uint64_t t = a.share(sum);
+            const auto f = r.find_bin(false, 0, t, mass);
+            const uint64_t each = each_of(f.bin);
+            if (known) sum = f.before + (t - f.before + each - 1) / each * each;
+        }
+        if (a.by_value && known) {
+            const float at = (float)(r.masses.max + a.border);
+            if (at >= r.least && at > -kFixedMost) {
+                const uint32_t bin = bins(at);
+                const auto f = r.find_bin(true, bin, 0, mass);
+                if (bin == (uint32_t)kFixedTop && f.here) (void)each_of(bin);
+                const uint64_t to = f.before + ((double)number(bin) - r.masses.max >= a.border ? f.here : 0);
+                sum = to < sum ? to : sum;
             }
         }
-        __syncthreads();
-    };
-    auto kept = [&](auto f, bool given, uint32_t which, uint64_t t) {
-        of_bin(given, which, t, [&](float value, uint64_t each, uint32_t n, uint64_t upto) { s.through = upto + f(value, each, n, upto); });
-        const uint64_t through = s.through;
-        __syncthreads();
-        return through;
-    };
-    if (a.k) sum = kept([&](float, uint64_t each, uint32_t, uint64_t) { return k_left * each; }, true, k_bin, 0);
-    if (a.by_mass) {
-        const uint64_t t = a.share(sum);
-        sum = kept([&](float, uint64_t each, uint32_t, uint64_t upto) { return (t - upto + each - 1) / each * each; }, false, 0, t);
-    }
-    if (a.by_value) {
-        const float at = (float)(r.masses.max + a.border);
-        if (at >= r.least && at > -kFixedMost) {
-            const uint64_t to = kept([&](float value, uint64_t each, uint32_t n, uint64_t) { return (double)value - r.masses.max >= a.border ? n * each : 0; }, true, bins(at), 0);
-            sum = to < sum ? to : sum;
+        if (known) {
+            const uint64_t t = __umul64hi(a.u, sum) + 1;
+            const auto f = r.find_bin(false, 0, t, mass);
+            const uint64_t each = each_of(f.bin);
+            if (known && threadIdx.x == 0) {
+                s.value = number(f.bin);
+                s.before = (t - f.before + each - 1) / each;
+            }
         }
+        if (threadIdx.x == 0) s.through = known ? sum : 0;
     }
-    const uint64_t t = __umul64hi(a.u, sum) + 1;
-    of_bin(false, 0, t, [&](float value, uint64_t each, uint32_t, uint64_t upto) {
-        s.value = value;
-        s.before = (t - upto + each - 1) / each;
-    });
-    r.find(s.value, s.before);
+    __syncthreads();
+    sum = s.through;
+    if (sum) r.find(s.value, s.before);
     return sum;
 }
 
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS, 6) sample_kernel(SampleShape a) {
-    constexpr bool kNumbers = std::is_same_v<T, __bf16>;          // a bin is a number
-    constexpr uint32_t E = Pieces<T>::E, kOwn = kFixedBins / THREADS;
-    SampleLds<THREADS>& s = sample_lds<THREADS>();
+__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 8 : 4) sample_kernel(SampleShape a) {
+    constexpr bool kNumbers = Row<T, THREADS>::kNumbers;
+    constexpr uint32_t E = Pieces<T>::E;
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
     const uint64_t row = a.row0 + blockIdx.x;
     Row<T, THREADS> r{static_cast<const T*>(a.z) + row * a.z_ld, (uint32_t)a.vocab, {}, 0.f};
     Asked asked;
@@ -723,19 +840,45 @@ __global__ void __launch_bounds__(THREADS, 6) sample_kernel(SampleShape a) {
     // the largest, and how many logits are in each of the fixed bins
     const bool few = r.vocab <= kList, counted = !few && (kNumbers || asked.k);
     float max = -kInf;
+    bool known = !counted || !kNumbers;                           // max is the largest, or will be
     if (counted) {
         u32x4* const clear = reinterpret_cast<u32x4*>(s.count);
-        for (uint32_t i = threadIdx.x; i < kFixedBins / 4; i += THREADS) clear[i] = u32x4{0, 0, 0, 0};
+        for (uint32_t i = threadIdx.x; i < kFixedCounts / 4; i += THREADS) clear[i] = u32x4{0, 0, 0, 0};
+        if (threadIdx.x == 0) {
+            s.held = s.ahead = 0;                                 // (ahead: there are numbers around 0 that are not 0)
+            s.bin = ~0u;
+        }
         __syncthreads();
-        max = r.count_and_largest();
-    } else {
-        r.stream([&](const float(&v)[E], uint32_t) { max = max_or_nan(max, largest_of(v)); });
-    }
-    max = over_lanes<64>(max, [](float x, float y) { return max_or_nan(x, y); });
-    if ((threadIdx.x & 63) == 0) s.most[threadIdx.x / 64] = max;
-    __syncthreads();
+        const uint32_t largest = r.count_fixed();
+        if constexpr (kNumbers) {
+            // no number is beyond the bins (NaN is), and the first that is not empty tells the largest, unless it is the one around 0
+            __syncthreads();
+            uint32_t first = ~0u;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) max = max_or_nan(max, s.most[w]);
+            for (uint32_t i = 0; i < kFixedBins; i += THREADS) {
+                const uint32_t bin = kFixedFirst + i + threadIdx.x;
+                if (r.fixed_count(bin) && bin < first) first = bin;
+            }
+            first = over_lanes<64>(first, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
+            if ((threadIdx.x & 63) == 0) atomicMin(&s.bin, first);
+            if ((largest & 0xFFFFu) > 0x7F80u || largest >> 16 > 0x7F80u || (threadIdx.x < 64 && s.count[threadIdx.x] != 0)) s.held = 1;
+            __syncthreads();
+            known = s.bin != ~0u && s.bin != (uint32_t)kFixedTop && !s.held;
+            if (known) max = fixed_bins().number(s.bin);
+            __syncthreads();
+        } else {
+            max = __uint_as_float(largest);
+        }
+    }
+    if (!counted || (kNumbers && !known)) r.stream([&](const float(&v)[E], uint32_t) { max = max_or_nan(max, largest_of(v)); });
+    if (!kNumbers || !counted || !known) {
+        max = over_lanes<64>(max, [](float x, float y) { return max_or_nan(x, y); });
+        if ((threadIdx.x & 63) == 0) s.most[threadIdx.x / 64] = max;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) max = max_or_nan(max, s.most[w]);
+    }
+    max = uniform(max);
     if (max != max || max == -kInf) {                             // no answer
         if (threadIdx.x == 0) {
             a.token[row] = -1;
@@ -746,7 +889,7 @@ __global__ void __launch_bounds__(THREADS, 6) sample_kernel(SampleShape a) {
     const bool infinite = max == kInf;
     const double t64 = (double)asked.temperature;
     r.masses.max = (double)max;
-    r.masses.scale = 1.44269504088896340736 / t64;
+    r.masses.scale = uniform(1.44269504088896340736 / t64);
     r.masses.least = infinite ? 0.0 : -1000.0;
     r.masses.bits = 62 - (r.vocab > 1 ? 32 - __builtin_clz(r.vocab - 1) : 0);
     if (r.masses.bits > 51) r.masses.bits = 51;
@@ -764,20 +907,18 @@ __global__ void __launch_bounds__(THREADS, 6) sample_kernel(SampleShape a) {
     float k_low = 0.f, k_high = 0.f;
     uint32_t k_bin = 0, k_left = 0;
     if (fixed && asked.k) {
-        uint32_t own = 0, all;
-#pragma unroll
-        for (uint32_t i = 0; i < kOwn; ++i) own += s.count[threadIdx.x * kOwn + i];
-        const uint32_t before = before_thread<THREADS>(own, s.counts, all);
+        auto count = [](uint32_t, uint32_t n) { return (uint64_t)n; };
+        const uint64_t all = r.sum_groups(count);
         if (asked.k >= all) asked.k = 0;
         if (asked.k) {
-            find_kth<THREADS>(asked.k, before, own, kOwn);
-            k_bin = s.bin;
-            k_left = asked.k - s.ahead;
-            listed = s.held <= kList;
+            const auto f = r.find_bin(false, 0, asked.k, count);  // (in every wave)
+            k_bin = uniform(f.bin);
+            k_left = asked.k - uniform((uint32_t)f.before);
+            listed = f.before + f.here <= kList;
             k_low = fixed_bins().lowest(k_bin);
             k_high = fixed_bins().highest(k_bin);
-            __syncthreads();
             if (listed && k_low > r.least) r.least = k_low;
+            __syncthreads();
         }
     }
     uint64_t sum = 0;
@@ -791,10 +932,10 @@ __global__ void __launch_bounds__(THREADS, 6) sample_kernel(SampleShape a) {
     }
     if constexpr (kNumbers)
         if (!done && fixed) {
-            sum = answer_by_numbers<THREADS>(r, asked, k_bin, k_left);
+            sum = answer_by_numbers(r, asked, k_bin, k_left);
             done = sum != 0;
         }
-    if (!done) sum = answer_any(r, asked, k_low, k_high, k_left);
+    if (!done) sum = answer_any(r, asked.temperature, asked.top_p, max, asked.k, asked.u, asked.border, k_low, k_high, k_left);
     if (threadIdx.x != 0) return;
     const uint32_t index = s.index;
     a.token[row] = (int32_t)index;
@@ -809,8 +950,8 @@ void launch_sample_of(const SampleArgs& args, hipStream_t stream) {
     for (uint64_t r = 0; r < a.rows; r += kRowsOfLaunch) {
         a.row0 = r;
         const unsigned here = (unsigned)(a.rows - r < kRowsOfLaunch ? a.rows - r : kRowsOfLaunch);
-        if (a.vocab <= 16384) hipLaunchKernelGGL((sample_kernel<T, 256>), dim3(here), dim3(256), sizeof(SampleLds<256>), stream, a);
-        else hipLaunchKernelGGL((sample_kernel<T, 512>), dim3(here), dim3(512), sizeof(SampleLds<512>), stream, a);
+        if (a.vocab <= 16384) hipLaunchKernelGGL((sample_kernel<T, 256>), dim3(here), dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((sample_kernel<T, 512>), dim3(here), dim3(512), 0, stream, a);
     }
 }
 
