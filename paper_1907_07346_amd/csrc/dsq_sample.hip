@@ -219,6 +219,238 @@ __device__ __forceinline__ uint64_t other_lane64(uint64_t v) {
     return (uint64_t)other_lane<CTRL>((uint32_t)(v >> 32)) << 32 | other_lane<CTRL>((uint32_t)v);
 }
 
+// A row of which the thread keeps N 16-byte pieces in registers between the passes; what does not fit comes from memory, or its caches, again, the last of it
+// first: it is the likeliest to be there.
+template <typename T, int THREADS, int N>
+struct Kept {
+    static constexpr bool kNumbers = std::is_same_v<T, __bf16>;
+    static constexpr uint32_t E = Pieces<T>::E, kHeld = N * THREADS;                       // pieces of a row that are held
+    using Piece = typename Pieces<T>::Piece;
+    const T* z;
+    uint32_t vocab, whole;                                        // whole: pieces without the ragged end
+    u32x4 held[N];
+    T last;                                                       // of the ragged end
+
+    __device__ __forceinline__ u32x4 load(uint32_t piece) const { return __builtin_bit_cast(u32x4, *reinterpret_cast<const Piece*>(z + piece * E)); }
+    static constexpr uint32_t kNothing = sizeof(T) == 4 ? 0xFF800000u : kNumbers ? 0xFF80FF80u : 0xFC00FC00u;             // minus infinity
+    __device__ __forceinline__ static u32x4 nothing() { return u32x4{kNothing, kNothing, kNothing, kNothing}; }
+    __device__ __forceinline__ Kept(const T* row, uint32_t length) : z(row), vocab(length), whole(length / E) {
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+            held[p] = nothing();
+            if (p * THREADS + threadIdx.x < whole) held[p] = load(p * THREADS + threadIdx.x);
+        }
+        last = whole * E + threadIdx.x < vocab ? z[whole * E + threadIdx.x] : (T)-kInf;
+    }
+    __device__ __forceinline__ uint32_t last_column() const { return whole * E + threadIdx.x; }
+    // f(piece, its first column) for what is held ...
+    template <typename F>
+    __device__ __forceinline__ void of_held(F f) const {
+#pragma unroll
+        for (int p = 0; p < N; ++p)
+            if (p * THREADS < whole) f(held[p], (p * THREADS + threadIdx.x) * E);
+    }
+    // ... and for stretch i of what is not
+    static constexpr uint32_t kStretch = kPieces * THREADS;
+    __device__ __forceinline__ uint32_t stretches() const { return whole > kHeld ? (whole - kHeld + kStretch - 1) / kStretch : 0; }
+    __device__ __forceinline__ void fetch(u32x4 (&raw)[kPieces], uint32_t i) const {
+        const uint32_t first = kHeld + i * kStretch + threadIdx.x;
+        if (kHeld + (i + 1) * kStretch <= whole) {
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) raw[p] = load(first + p * THREADS);
+        } else {
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                raw[p] = nothing();
+                if (first + p * THREADS < whole) raw[p] = load(first + p * THREADS);
+            }
+        }
+    }
+    __device__ __forceinline__ static uint32_t column(uint32_t i, int p) { return (kHeld + i * kStretch + p * THREADS + threadIdx.x) * E; }
+
+    __device__ __forceinline__ static void values(u32x4 raw, float (&v)[E]) {
+        const Piece piece = __builtin_bit_cast(Piece, raw);
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e) v[e] = (float)piece[e];
+    }
+    // The thread's largest logit.
+    __device__ __forceinline__ float largest() const {
+        float max = (float)last;
+        auto f = [&](u32x4 raw, uint32_t) {
+            float v[E];
+            values(raw, v);
+            max = max_or_nan(max, largest_of(v));
+        };
+        of_held(f);
+        for (uint32_t i = 0, n = stretches(); i < n; ++i) {
+            u32x4 raw[kPieces];
+            fetch(raw, i);
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) f(raw[p], 0);
+        }
+        return max;
+    }
+    // Counts logits in fixed bins.  Returns the thread's largest one; of bf16, whose bins tell it, the largest magnitudes of either half of its words.
+    __device__ __forceinline__ uint32_t count_fixed() const {
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+        auto add = [&](uint32_t place) { atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.count) + place), 1u); };
+        const uint32_t most = kFixedSide + (threadIdx.x & 63);
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+        u16x2 magnitudes = 0;
+        float max = -kInf;
+        auto f = [&](u32x4 raw) {
+            if constexpr (kNumbers) {                             // two at a time
+                const u16x2 base = (uint16_t)kFixedBase, side = (uint16_t)most, top = (uint16_t)(4 * kFixedTop);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t bits = raw[i];                 // (a cast of the element itself would be one of the first)
+                    const u16x2 magnitude = __builtin_bit_cast(u16x2, bits & 0x7FFF7FFFu);
+                    magnitudes = __builtin_elementwise_max(magnitudes, magnitude);
+                    u16x2 c = __builtin_elementwise_min(__builtin_elementwise_sub_sat(magnitude, base), side);
+                    const u16x2 sign = __builtin_bit_cast(u16x2, __builtin_bit_cast(i16x2, bits) >> (int16_t)15);
+                    c = (u16x2)(((sign - (c ^ sign)) << (uint16_t)2) + top);               // top - c, or top + c where the sign is set; in bytes
+                    const uint32_t places = __builtin_bit_cast(uint32_t, c);
+                    add(places & 0xFFFFu);
+                    add(places >> 16);
+                }
+            } else {
+                float v[E];
+                values(raw, v);
+                max = max_or_nan(max, largest_of(v));
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) {
+                    const uint32_t bits = __float_as_uint(v[e]), sign = (uint32_t)((int32_t)bits >> 31);
+                    uint32_t c = __builtin_elementwise_sub_sat(bits >> 16 & 0x7FFFu, (uint32_t)kFixedBase);
+                    c = c < most ? c : most;
+                    add((sign - (c ^ sign) + kFixedTop) * 4);
+                }
+            }
+        };
+        of_held([&](u32x4 raw, uint32_t) { f(raw); });
+        for (uint32_t i = 0, n = stretches(); i < n; ++i) {
+            u32x4 raw[kPieces];
+            fetch(raw, i);
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) f(raw[p]);
+        }
+        if (whole * E < vocab) {
+            u32x4 end = nothing();
+            if constexpr (sizeof(T) == 4) end[0] = __builtin_bit_cast(uint32_t, last);
+            else end[0] = (end[0] & 0xFFFF0000u) | __builtin_bit_cast(uint16_t, last);
+            f(end);
+        }
+        return kNumbers ? __builtin_bit_cast(uint32_t, magnitudes) : __float_as_uint(max);
+    }
+    // Gathers the logits from lo on (kList of them at most) as ranks; returns how many there are.
+    __device__ __forceinline__ uint32_t gather(float lo) const {
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+        __syncthreads();
+        if (threadIdx.x == 0) s.held = 0;
+        __syncthreads();
+        auto one = [&](float v, uint32_t column) {
+            if (v >= lo) {
+                const uint32_t place = atomicAdd(&s.held, 1u);
+                if (place < kList) s.list[place] = logit_rank(v, column);
+            }
+        };
+        auto f = [&](u32x4 raw, uint32_t first) {
+            float v[E];
+            values(raw, v);
+            if (!(largest_of(v) >= lo)) return;
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) one(v[e], first + e);
+        };
+        of_held(f);
+        for (uint32_t i = stretches(); i-- > 0;) {
+            u32x4 raw[kPieces];
+            fetch(raw, i);
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) f(raw[p], column(i, p));
+        }
+        if (whole * E < vocab) one((float)last, last_column());
+        __syncthreads();
+        return s.held;
+    }
+    // The column of the nth (from 1) of the n logits that equal `value`: from the front among those held, or from the row's end.
+    __device__ __forceinline__ void find(float value, uint64_t nth, uint32_t n) const {
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+        constexpr uint32_t kRoom = 2 * kList;
+        // equal numbers are equal bits, but for the sign of 0
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        uint32_t bits, keep = ~0u;
+        if constexpr (sizeof(T) == 2) {
+            bits = __builtin_bit_cast(uint16_t, (T)value) * 0x10001u;
+            if (value == 0.f) keep = 0x7FFF7FFFu;
+        } else {
+            bits = __float_as_uint(value);
+            if (value == 0.f) keep = 0x7FFFFFFFu;
+        }
+        bits &= keep;
+        auto append = [&](uint32_t column) {
+            const uint32_t place = atomicAdd(&s.held, 1u);
+            if (place < kRoom) s.columns[place] = column;
+        };
+        auto f = [&](u32x4 raw, uint32_t first) {
+            u32x4 d;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[i] = (raw[i] & keep) ^ bits;
+            if constexpr (sizeof(T) == 2) {
+                auto least = [](uint32_t x, uint32_t y) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y))); };
+                const uint32_t m = least(least(d[0], d[1]), least(d[2], d[3]));
+                if ((m & 0xFFFFu) != 0 && m >= 0x10000u) return;
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e)
+                    if ((d[e / 2] >> (16 * (e & 1)) & 0xFFFFu) == 0) append(first + e);
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e)
+                    if (d[e] == 0) append(first + e);
+            }
+        };
+        auto clear = [&] {
+            __syncthreads();
+            if (threadIdx.x == 0) s.held = 0;
+            __syncthreads();
+        };
+        const uint32_t rest = stretches();
+        clear();
+        of_held(f);
+        auto end = [&] {
+            if (whole * E < vocab && (float)last == value) append(last_column());
+        };
+        if (!rest) end();
+        __syncthreads();
+        uint32_t found = s.held;
+        bool forward = true;
+        if (rest && nth > found) {
+            forward = false;
+            nth = n - nth + 1;
+            clear();
+            end();
+            for (uint32_t i = rest; i-- > 0;) {
+                u32x4 raw[kPieces];
+                fetch(raw, i);
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p) f(raw[p], column(i, p));
+                __syncthreads();
+                found = s.held;
+                __syncthreads();
+                if (found >= nth) break;
+            }
+        }
+        if (found > kRoom) return find_nth<T, THREADS>(z, vocab, value, forward ? nth : n - nth + 1);
+        for (uint32_t i = threadIdx.x; i < found; i += THREADS) {
+            const uint32_t mine = s.columns[i];
+            uint32_t place = 0;
+#pragma unroll 8
+            for (uint32_t j = 0; j < found; ++j) place += (s.columns[j] < mine) == forward ? 1u : 0u;
+            if (place == (forward ? nth - 1 : nth)) s.index = mine;                        // (backwards it counts itself)
+        }
+        __syncthreads();
+    }
+};
+
 enum Question { kCount, kMass, kValue };                          // at which place do count or mass reach a number, or logits a value
 
 template <typename T, int THREADS>
@@ -255,59 +487,6 @@ struct Row {
         }
     }
 
-    // Counts logits in fixed bins.  Returns the thread's largest one; of bf16, whose bins tell it, the largest magnitudes of either half of its words.
-    __device__ __forceinline__ uint32_t count_fixed() const {
-        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
-        auto add = [&](uint32_t place) { atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.count) + place), 1u); };
-        const uint32_t most = kFixedSide + (threadIdx.x & 63);
-        if constexpr (kNumbers) {                                 // two at a time
-            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-            typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
-            const u16x2 base = (uint16_t)kFixedBase, side = (uint16_t)most, top = (uint16_t)(4 * kFixedTop);
-            u16x2 largest = 0;
-            auto two = [&](uint32_t bits) {
-                const u16x2 magnitude = __builtin_bit_cast(u16x2, bits & 0x7FFF7FFFu);
-                largest = __builtin_elementwise_max(largest, magnitude);
-                u16x2 c = __builtin_elementwise_min(__builtin_elementwise_sub_sat(magnitude, base), side);
-                const u16x2 sign = __builtin_bit_cast(u16x2, __builtin_bit_cast(i16x2, bits) >> (int16_t)15);
-                c = (u16x2)(((sign - (c ^ sign)) << (uint16_t)2) + top);                   // top - c, or top + c where the sign is set; in bytes
-                const uint32_t places = __builtin_bit_cast(uint32_t, c);
-                add(places & 0xFFFFu);
-                add(places >> 16);
-            };
-            uint32_t at = threadIdx.x * E;
-            for (; at + (kPieces - 1) * THREADS * E + E <= vocab; at += kPieces * THREADS * E) {
-                u32x4 raw[kPieces];
-#pragma unroll
-                for (int p = 0; p < kPieces; ++p) raw[p] = __builtin_bit_cast(u32x4, *reinterpret_cast<const Piece*>(z + at + p * THREADS * E));
-#pragma unroll
-                for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) two(raw[p][i]);
-            }
-            for (; at < vocab; at += THREADS * E) {
-                Piece raw;
-#pragma unroll
-                for (uint32_t e = 0; e < E; ++e) raw[e] = at + e < vocab ? z[at + e] : (T)-kInf;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) two(__builtin_bit_cast(u32x4, raw)[i]);
-            }
-            return __builtin_bit_cast(uint32_t, largest);
-        } else {
-            float max = -kInf;
-            stream([&](const float(&v)[E], uint32_t) {
-                max = max_or_nan(max, largest_of(v));
-#pragma unroll
-                for (uint32_t e = 0; e < E; ++e) {
-                    const uint32_t bits = __float_as_uint(v[e]), sign = (uint32_t)((int32_t)bits >> 31);
-                    uint32_t c = __builtin_elementwise_sub_sat(bits >> 16 & 0x7FFFu, (uint32_t)kFixedBase);
-                    c = c < most ? c : most;
-                    add((sign - (c ^ sign) + kFixedTop) * 4);
-                }
-            });
-            return __float_as_uint(max);
-        }
-    }
     __device__ __forceinline__ uint32_t fixed_count(uint32_t bin) const { return bin < kFixedLast ? sample_lds<T, THREADS>().count[bin] : 0; }
     // s.group: what of(bin, its count) gives for sixteen bins, summed up over all groups before.  Returns the sum of all.
     template <typename F>
@@ -449,91 +628,12 @@ struct Row {
         return through;
     }
 
-    // The column of the nth (from 1) logit that equals `value`, from the row's beginning on until it is there.
-    __device__ __forceinline__ void find(float value, uint64_t nth) const {
-        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
-        constexpr uint32_t kRoom = 2 * kList, kStretch = kPieces * THREADS * E;
-        if (nth > kRoom) return find_nth<T, THREADS>(z, vocab, value, nth);
-        __syncthreads();
-        if (threadIdx.x == 0) s.held = 0;
-        __syncthreads();
-        // equal numbers are equal bits, but for the sign of 0
-        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-        uint32_t bits, keep = ~0u;
-        if constexpr (sizeof(T) == 2) {
-            bits = __builtin_bit_cast(uint16_t, (T)value) * 0x10001u;
-            if (value == 0.f) keep = 0x7FFF7FFFu;
-        } else {
-            bits = __float_as_uint(value);
-            if (value == 0.f) keep = 0x7FFFFFFFu;
-        }
-        bits &= keep;
-        auto is = [&](u32x4 raw, uint32_t e) {
-            if constexpr (sizeof(T) == 2) return (((raw[e / 2] & keep) ^ bits) >> (16 * (e & 1)) & 0xFFFFu) == 0;
-            else return ((raw[e] & keep) ^ bits) == 0;
-        };
-        auto any = [&](u32x4 raw) {
-            u32x4 d;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) d[i] = (raw[i] & keep) ^ bits;
-            if constexpr (sizeof(T) == 2) {
-                auto least = [](uint32_t x, uint32_t y) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y))); };
-                const uint32_t m = least(least(d[0], d[1]), least(d[2], d[3]));
-                return (m & 0xFFFFu) == 0 || m < 0x10000u;
-            } else {
-                return d[0] == 0 || d[1] == 0 || d[2] == 0 || d[3] == 0;
-            }
-        };
-        u32x4 raw[kPieces], coming[kPieces];
-        auto fetch = [&](uint32_t at) {
-#pragma unroll
-            for (int p = 0; p < kPieces; ++p) {
-                const uint32_t from = at + (p * THREADS + threadIdx.x) * E;
-                Piece piece;
-                if (from + E <= vocab) piece = *reinterpret_cast<const Piece*>(z + from);
-                else
-#pragma unroll
-                    for (uint32_t e = 0; e < E; ++e) piece[e] = from + e < vocab ? z[from + e] : (T)-kInf;
-                coming[p] = __builtin_bit_cast(u32x4, piece);
-            }
-        };
-        fetch(0);
-        uint32_t held = 0;
-        for (uint32_t at = 0; at < vocab; at += kStretch) {
-#pragma unroll
-            for (int p = 0; p < kPieces; ++p) raw[p] = coming[p];
-            if (at + kStretch < vocab) fetch(at + kStretch);
-#pragma unroll
-            for (int p = 0; p < kPieces; ++p) {
-                if (!any(raw[p])) continue;
-#pragma unroll
-                for (uint32_t e = 0; e < E; ++e)
-                    if (is(raw[p], e)) {
-                        const uint32_t place = atomicAdd(&s.held, 1u);
-                        if (place < kRoom) s.columns[place] = at + (p * THREADS + threadIdx.x) * E + e;
-                    }
-            }
-            __syncthreads();
-            held = s.held;
-            __syncthreads();
-            if (held >= nth) break;
-        }
-        if (held > kRoom) return find_nth<T, THREADS>(z, vocab, value, nth);
-        for (uint32_t i = threadIdx.x; i < held; i += THREADS) {
-            const uint32_t mine = s.columns[i];
-            uint32_t place = 0;
-#pragma unroll 8
-            for (uint32_t j = 0; j < held; ++j) place += s.columns[j] < mine ? 1u : 0u;
-            if (place == nth - 1) s.index = mine;
-        }
-        __syncthreads();
-    }
     // Logits that are all `value`, n of them (kValue), behind `before`.
     __device__ uint64_t among_equals(Question q, float value, uint64_t n, uint64_t before, uint64_t t, double d, bool pick) const {
         const uint64_t mass = masses(value);
         if (q == kValue) return before + ((double)value - masses.max >= d ? n * mass : 0);
         const uint64_t nth = q == kCount ? t : (t - before + mass - 1) / mass;
-        if (pick) find(value, nth);
+        if (pick) find_nth<T, THREADS>(z, vocab, value, nth);
         return before + nth * mass;
     }
 };
@@ -749,8 +849,8 @@ __device__ __attribute__((noinline)) uint64_t answer_any(Row<T, THREADS> r, floa
 
 // Rows in whose bins every logit is the same number: what is left is arithmetic, and the token the nth of a number.  Returns 0 if the answer hangs on what lies
 // around 0, which may be several.
-template <typename T, int THREADS>
-__device__ __forceinline__ uint64_t answer_by_numbers(const Row<T, THREADS>& r, const Asked& a, uint32_t k_bin, uint32_t k_left) {
+template <typename T, int THREADS, int N>
+__device__ __forceinline__ uint64_t answer_by_numbers(const Row<T, THREADS>& r, const Kept<T, THREADS, N>& kept, const Asked& a, uint32_t k_bin, uint32_t k_left) {
     constexpr uint32_t E = Pieces<T>::E;
     SampleLds<THREADS>& s = sample_lds<T, THREADS>();
     const Bins bins = fixed_bins();
@@ -807,20 +907,20 @@ __device__ __forceinline__ uint64_t answer_by_numbers(const Row<T, THREADS>& r, 
             if (known && threadIdx.x == 0) {
                 s.value = number(f.bin);
                 s.before = (t - f.before + each - 1) / each;
+                s.ahead = s.count[f.bin];
             }
         }
         if (threadIdx.x == 0) s.through = known ? sum : 0;
     }
     __syncthreads();
     sum = s.through;
-    if (sum) r.find(s.value, s.before);
+    if (sum) kept.find(s.value, s.before, s.ahead);
     return sum;
 }
 
-template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 8 : 4) sample_kernel(SampleShape a) {
+template <typename T, int THREADS, int N, int WAVES>
+__global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
     constexpr bool kNumbers = Row<T, THREADS>::kNumbers;
-    constexpr uint32_t E = Pieces<T>::E;
     SampleLds<THREADS>& s = sample_lds<T, THREADS>();
     const uint64_t row = a.row0 + blockIdx.x;
     Row<T, THREADS> r{static_cast<const T*>(a.z) + row * a.z_ld, (uint32_t)a.vocab, {}, 0.f};
@@ -834,6 +934,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 8 : 4) sample_kernel
         asked.temperature = 1.f;
         asked.k = 1;
     }
+    const Kept<T, THREADS, N> kept(r.z, r.vocab);
+    if (threadIdx.x == 0) s.index = 0;
     asked.by_mass = asked.top_p < 1.f;
     asked.u = !(u > 0.f) ? 0 : u >= 1.f ? ~0ull : (uint64_t)((double)u * 0x1p64);
 
@@ -849,7 +951,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 8 : 4) sample_kernel
             s.bin = ~0u;
         }
         __syncthreads();
-        const uint32_t largest = r.count_fixed();
+        const uint32_t largest = kept.count_fixed();
         if constexpr (kNumbers) {
             // no number is beyond the bins (NaN is), and the first that is not empty tells the largest, unless it is the one around 0
             __syncthreads();
@@ -870,7 +972,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 8 : 4) sample_kernel
             max = __uint_as_float(largest);
         }
     }
-    if (!counted || (kNumbers && !known)) r.stream([&](const float(&v)[E], uint32_t) { max = max_or_nan(max, largest_of(v)); });
+    if (!counted || (kNumbers && !known)) max = kept.largest();
     if (!kNumbers || !counted || !known) {
         max = over_lanes<64>(max, [](float x, float y) { return max_or_nan(x, y); });
         if ((threadIdx.x & 63) == 0) s.most[threadIdx.x / 64] = max;
@@ -924,7 +1026,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 8 : 4) sample_kernel
     uint64_t sum = 0;
     bool done = false;
     if (listed || (!kNumbers && asked.by_value && !asked.by_mass && !asked.k)) {
-        const uint32_t n = r.gather(r.least, kInf);
+        const uint32_t n = kept.gather(r.least);
         if (n <= kList) {
             sum = answer_from_list(r, asked, n);
             done = true;
@@ -932,7 +1034,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 8 : 4) sample_kernel
     }
     if constexpr (kNumbers)
         if (!done && fixed) {
-            sum = answer_by_numbers(r, asked, k_bin, k_left);
+            sum = answer_by_numbers(r, kept, asked, k_bin, k_left);
             done = sum != 0;
         }
     if (!done) sum = answer_any(r, asked.temperature, asked.top_p, max, asked.k, asked.u, asked.border, k_low, k_high, k_left);
@@ -943,6 +1045,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 8 : 4) sample_kernel
     if (a.logp) a.logp[row] = (float)(y - log(ldexp((double)sum, -r.masses.bits)));
 }
 
+template <int V>
+using Int = std::integral_constant<int, V>;
+
 template <typename T>
 void launch_sample_of(const SampleArgs& args, hipStream_t stream) {
     SampleShape a{};
@@ -950,8 +1055,11 @@ void launch_sample_of(const SampleArgs& args, hipStream_t stream) {
     for (uint64_t r = 0; r < a.rows; r += kRowsOfLaunch) {
         a.row0 = r;
         const unsigned here = (unsigned)(a.rows - r < kRowsOfLaunch ? a.rows - r : kRowsOfLaunch);
-        if (a.vocab <= 16384) hipLaunchKernelGGL((sample_kernel<T, 256>), dim3(here), dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((sample_kernel<T, 512>), dim3(here), dim3(512), 0, stream, a);
+        auto launch = [&](auto threads, auto pieces, auto waves) {
+            hipLaunchKernelGGL((sample_kernel<T, decltype(threads)::value, decltype(pieces)::value, decltype(waves)::value>), dim3(here), dim3(threads.value), 0, stream, a);
+        };
+        if (a.vocab * sizeof(T) <= 256 * 8 * 16) launch(Int<256>(), Int<8>(), Int<4>());
+        else launch(Int<512>(), Int<16>(), Int<4>());
     }
 }
 
