@@ -117,7 +117,7 @@ struct SampleLds {
         uint32_t columns[2 * kList];                              // of a number, when counts are done with
         struct {
             uint64_t list[kList], sorted[kList], upto[kList];     // ranks of the logits gathered; in order; the mass through each
-            uint64_t mass[kBins];
+            uint64_t mass[kBins];                                 // of bins, and then what lies before them
             uint64_t part_mass[kParts];
             uint32_t part_count[kParts];
         };
@@ -127,7 +127,7 @@ struct SampleLds {
     uint32_t counts[THREADS / 64];
     float most[THREADS / 64];
     uint64_t before, through;                                     // answers
-    uint32_t held, bin, ahead, index;
+    uint32_t held, bin, ahead, least, index;
     float value;
 };
 // Of a kernel, and of the functions that it calls: one for each, so that it has an address that is known.
@@ -137,18 +137,41 @@ __device__ __forceinline__ SampleLds<THREADS>& sample_lds() {
     return s;
 }
 
+// The sum of the lanes up to the own one, by register permutations: one, two, four and eight lanes on in sixteen, then a sixteen's last to the next one's, and that of 32
+// to the rest.
+template <int CTRL, int ROWS, typename V>
+__device__ __forceinline__ V add_other(V v) {
+    if constexpr (sizeof(V) == 8) {
+        const uint32_t high = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xF, false);
+        return v + ((uint64_t)high << 32 | (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false));
+    } else {
+        return v + (V)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
+    }
+}
+template <typename V>
+__device__ __forceinline__ V upto_lane(V v) {
+    v = add_other<0x111, 0xF>(v);                                 // row_shr 1, 2, 4, 8
+    v = add_other<0x112, 0xF>(v);
+    v = add_other<0x114, 0xF>(v);
+    v = add_other<0x118, 0xF>(v);
+    v = add_other<0x142, 0xA>(v);                                 // row_bcast 15, 31
+    return add_other<0x143, 0xC>(v);
+}
+__device__ __forceinline__ uint64_t of_lane(uint64_t v, uint32_t lane) {
+    return (uint64_t)__builtin_amdgcn_readlane((uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)v, lane);
+}
+
+__device__ __forceinline__ void wave_sync() {                     // what lanes wrote to LDS before is read by others after
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+}
+
 // What lies before the thread's v in the workgroup, and all of it.
 template <int THREADS, typename V>
 __device__ __forceinline__ V before_thread(V v, V* sums, V& all) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    V upto = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        V other;
-        if constexpr (sizeof(V) == 8) other = (V)__shfl_up((unsigned long long)upto, o);
-        else other = (V)__shfl_up((int)upto, o);
-        if (lane >= (uint32_t)o) upto += other;
-    }
+    const V upto = upto_lane(v);
     __syncthreads();
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
@@ -342,14 +365,32 @@ struct Kept {
         }
         return kNumbers ? __builtin_bit_cast(uint32_t, magnitudes) : __float_as_uint(max);
     }
-    // Gathers the logits from lo on (kList of them at most) as ranks; returns how many there are.
-    __device__ __forceinline__ uint32_t gather(float lo) const {
+    // f(logit) for all of them.
+    template <typename F>
+    __device__ __forceinline__ void of_all(F f) const {
+        auto piece = [&](u32x4 raw) {
+            float v[E];
+            values(raw, v);
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) f(v[e]);
+        };
+        of_held([&](u32x4 raw, uint32_t) { piece(raw); });
+        for (uint32_t i = stretches(); i-- > 0;) {
+            u32x4 raw[kPieces];
+            fetch(raw, i);
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) piece(raw[p]);
+        }
+        f((float)last);
+    }
+    // Gathers the logits from lo to hi (kList of them at most) as ranks; returns how many there are.
+    __device__ __forceinline__ uint32_t gather(float lo, float hi) const {
         SampleLds<THREADS>& s = sample_lds<T, THREADS>();
         __syncthreads();
         if (threadIdx.x == 0) s.held = 0;
         __syncthreads();
         auto one = [&](float v, uint32_t column) {
-            if (v >= lo) {
+            if (v >= lo && v <= hi) {
                 const uint32_t place = atomicAdd(&s.held, 1u);
                 if (place < kList) s.list[place] = logit_rank(v, column);
             }
@@ -488,39 +529,39 @@ struct Row {
     }
 
     __device__ __forceinline__ uint32_t fixed_count(uint32_t bin) const { return bin < kFixedLast ? sample_lds<T, THREADS>().count[bin] : 0; }
-    // s.group: what of(bin, its count) gives for sixteen bins, summed up over all groups before.  Returns the sum of all.
+    // s.group, which is cleared: what of(bin, its count) gives for sixteen bins.
     template <typename F>
-    __device__ __forceinline__ uint64_t sum_groups(F of) const {
+    __device__ __forceinline__ void sum_groups(F of) const {
         SampleLds<THREADS>& s = sample_lds<T, THREADS>();
 #pragma unroll 1
         for (uint32_t i = threadIdx.x; i < kFixedBins; i += THREADS) {
             const uint32_t n = fixed_count(kFixedFirst + i);
-            uint64_t sum = 0;
-            if (__ballot(n != 0)) {
-                if (n) sum = of(kFixedFirst + i, n);
-                sum += other_lane64<0xB1>(sum);
-                sum += other_lane64<0x4E>(sum);
-                sum += other_lane64<0x141>(sum);
-                sum += other_lane64<0x140>(sum);
-            }
-            if ((threadIdx.x & 15) == 0) s.group[i / 16] = sum;
+            if (n) atomicAdd(reinterpret_cast<unsigned long long*>(&s.group[i / 16]), (unsigned long long)of(kFixedFirst + i, n));
         }
         __syncthreads();
-        constexpr uint32_t kEach = kGroups / THREADS;
-        uint64_t own[kEach], sum = 0, all;
+    }
+    // In the first wave: what lies before each of the groups takes their place.  Returns the sum of all.
+    __device__ __forceinline__ uint64_t sum_before_groups() const {
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+        constexpr uint32_t kEach = kGroups / 64;
+        uint64_t own[kEach], sum = 0;
 #pragma unroll
         for (uint32_t i = 0; i < kEach; ++i) {
             own[i] = s.group[threadIdx.x * kEach + i];
             sum += own[i];
         }
-        uint64_t before = before_thread<THREADS>(sum, s.sums, all);
+        const uint64_t upto = upto_lane(sum), all = of_lane(upto, 63);
+        uint64_t before = upto - sum;
 #pragma unroll
         for (uint32_t i = 0; i < kEach; ++i) {
             s.group[threadIdx.x * kEach + i] = before;
             before += own[i];
         }
-        __syncthreads();
+        wave_sync();
         return all;
+    }
+    __device__ __forceinline__ void clear_groups() const {
+        for (uint32_t i = threadIdx.x; i < kGroups; i += THREADS) sample_lds<T, THREADS>().group[i] = 0;
     }
     // In a wave: the bin in which the sum reaches t (1 <= t <= all), or `bin` itself, what of(bin, count) gives for it and what lies before it.
     struct FoundBin {
@@ -542,15 +583,13 @@ struct Row {
         }
         const uint32_t mine = kFixedFirst + group * 16 + (lane & 15), n = fixed_count(mine);
         const uint64_t here = n ? of(mine, n) : 0, ahead = s.group[group];
-        uint64_t upto = here;
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) {
-            const uint64_t other = (uint64_t)__shfl_up((unsigned long long)upto, o, 16);
-            if ((lane & 15) >= (uint32_t)o) upto += other;
-        }
+        uint64_t upto = add_other<0x111, 0xF>(here);              // (each sixteen lanes by themselves)
+        upto = add_other<0x112, 0xF>(upto);
+        upto = add_other<0x114, 0xF>(upto);
+        upto = add_other<0x118, 0xF>(upto);
         upto += ahead;
-        const uint32_t at = given ? (bin - kFixedFirst) % 16 : (uint32_t)__builtin_ctzll(__ballot(upto >= t));
-        return {kFixedFirst + group * 16 + at, (uint64_t)__shfl((unsigned long long)here, (int)at), (uint64_t)__shfl((unsigned long long)(upto - here), (int)at)};
+        const uint32_t at = uniform(given ? (bin - kFixedFirst) % 16 : (uint32_t)__builtin_ctzll(__ballot(upto >= t)));
+        return {kFixedFirst + group * 16 + at, of_lane(here, at), of_lane(upto - here, at)};
     }
 
     // Gathers the logits from lo to hi (kList of them at most) as ranks; returns how many there are.
@@ -709,7 +748,7 @@ struct Asked {
     float temperature, top_p, max;
     uint32_t k;                                                   // 0: all
     uint64_t u;                                                   // times 2^64
-    bool by_mass, by_value;
+    bool by_mass, by_value, infinite;
     double border;                                                // of z - max: by_value
     // what the first logits must reach for top_p of a sum
     __device__ __forceinline__ uint64_t share(uint64_t sum) const {
@@ -718,6 +757,45 @@ struct Asked {
         return t ? t : 1;
     }
 };
+__device__ __forceinline__ Asked asked_of(const SampleShape& a, uint64_t row) {
+    Asked q{};
+    q.temperature = a.each.temperature_dev ? a.each.temperature_dev[row] : a.temperature;
+    q.top_p = a.each.top_p_dev ? a.each.top_p_dev[row] : a.top_p;
+    const int32_t top_k = a.each.top_k_dev ? a.each.top_k_dev[row] : a.top_k;
+    q.k = top_k > 0 && (uint64_t)top_k < a.vocab ? (uint32_t)top_k : 0;
+    if (!(q.temperature >= __FLT_MIN__ && q.temperature < kInf)) {                         // the largest logit
+        q.temperature = 1.f;
+        q.k = 1;
+    }
+    q.by_mass = q.top_p < 1.f;
+    return q;
+}
+// What depends on the row's largest logit, which is a number or plus infinity.
+__device__ __forceinline__ void ask(const SampleShape& a, uint64_t row, float max, Asked& q, Masses& masses, float& least) {
+    const double t = (double)q.temperature;
+    const float min_p = a.each.min_p_dev ? a.each.min_p_dev[row] : a.min_p, u = a.u[row];
+    q.max = max;
+    q.infinite = max == kInf;
+    q.by_value = min_p > 0.f && !q.infinite;                      // (infinite ones are alike)
+    q.border = q.by_value ? t * log((double)(min_p < 1.f ? min_p : 1.f)) : -kInf;
+    q.u = !(u > 0.f) ? 0 : u >= 1.f ? ~0ull : (uint64_t)((double)u * 0x1p64);
+    masses.max = (double)max;
+    masses.scale = uniform(1.44269504088896340736 / t);
+    masses.least = q.infinite ? 0.0 : -1000.0;
+    masses.bits = 62 - (a.vocab > 1 ? 64 - __builtin_clzll(a.vocab - 1) : 0);
+    if (masses.bits > 51) masses.bits = 51;
+    // below: masses of less than half of a unit.  (In 32 bits: off by less than what one unit more of the exponent allows for.)
+    least = q.infinite ? kInf : fmaxf((float)((double)max - (masses.bits + 2) * 0.69314718055994530942 * t - fabs((double)max) * 0x1p-20), -__FLT_MAX__);
+}
+__device__ __forceinline__ void no_answer(const SampleShape& a, uint64_t row, float max) {
+    a.token[row] = -1;
+    if (a.logp) a.logp[row] = max;
+}
+__device__ __forceinline__ void write_answer(const SampleShape& a, uint64_t row, const Asked& q, const Masses& masses, uint32_t index, float z, uint64_t sum) {
+    a.token[row] = (int32_t)index;
+    const double y = q.infinite ? 0.0 : ((double)z - (double)q.max) / (double)q.temperature;
+    if (a.logp) a.logp[row] = (float)(y - log(ldexp((double)sum, -masses.bits)));
+}
 
 // The mass that is kept, and s.index, out of a list of everything that matters.
 template <typename T, int THREADS>
@@ -732,6 +810,55 @@ __device__ __forceinline__ uint64_t answer_from_list(const Row<T, THREADS>& r, c
     }
     (void)r.list_mass(n, 0, __umul64hi(a.u, sum) + 1);
     return sum;
+}
+
+// The same, and the answer written: the workgroup puts the list in order, its first wave does the rest.
+template <typename T, int THREADS>
+__device__ __forceinline__ void finish_from_list(const SampleShape& shape, uint64_t row, const Row<T, THREADS>& r, const Asked& a, uint32_t n) {
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+    if (n * 4 <= THREADS) {                                       // four threads for each
+        const uint32_t i = threadIdx.x / 4;
+        const uint64_t mine = i < n ? s.list[i] : 0;
+        uint32_t place = 0;
+#pragma unroll 4
+        for (uint32_t j = threadIdx.x & 3; j < n; j += 4) place += s.list[j] > mine ? 1u : 0u;
+        place = over_lanes<4>(place, [](uint32_t x, uint32_t y) { return x + y; });
+        if (i < n && (threadIdx.x & 3) == 0) s.sorted[place] = mine;
+    } else {
+        for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
+            const uint64_t mine = s.list[i];
+            uint32_t place = 0;
+#pragma unroll 8
+            for (uint32_t j = 0; j < n; ++j) place += s.list[j] > mine ? 1u : 0u;
+            s.sorted[place] = mine;
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    const uint32_t each = (n + 63) / 64, first = threadIdx.x * each;                       // in their order: `each` of a lane
+    uint64_t sum = 0;
+    for (uint32_t i = first; i < first + each && i < n; ++i) {
+        sum += r.masses(of_key((uint32_t)(s.sorted[i] >> 32)));
+        s.upto[i] = sum;
+    }
+    const uint64_t before = upto_lane(sum) - sum;
+    for (uint32_t i = first; i < first + each && i < n; ++i) s.upto[i] += before;
+    wave_sync();
+    // places at which f is true, which are the first ones
+    auto places = [&](auto f) {
+        uint32_t all = 0;
+        for (uint32_t i = 0; i < n; i += 64) all += (uint32_t)__popcll(__ballot(i + threadIdx.x < n && f(i + threadIdx.x)));
+        return all;
+    };
+    auto reached = [&](uint64_t t) { return places([&](uint32_t i) { return s.upto[i] < t; }); };
+    sum = s.upto[a.k && a.k < n ? a.k - 1 : n - 1];
+    if (a.by_mass) sum = s.upto[reached(a.share(sum))];
+    if (a.by_value) {
+        const uint64_t kept = s.upto[places([&](uint32_t i) { return (double)of_key((uint32_t)(s.sorted[i] >> 32)) - r.masses.max >= a.border; }) - 1];
+        sum = kept < sum ? kept : sum;
+    }
+    const uint64_t token = s.sorted[reached(__umul64hi(a.u, sum) + 1)];
+    if (threadIdx.x == 0) write_answer(shape, row, a, r.masses, ~(uint32_t)token, of_key((uint32_t)(token >> 32)), sum);
 }
 
 // The bin of the k-th logit (s.bin), the logits before it (s.ahead) and up to its end (s.held): the thread's bins begin with `first` and have `own` logits, and
@@ -760,7 +887,7 @@ __device__ __forceinline__ void find_kth(uint32_t k, uint32_t before, uint32_t o
 template <typename T, int THREADS>
 __device__ __attribute__((noinline)) uint64_t answer_any(Row<T, THREADS> r, float temperature, float top_p, float max, uint32_t k, uint64_t u, double border,
                                                            float k_low, float k_high, uint32_t k_left) {
-    Asked a{temperature, top_p, max, k, u, top_p < 1.f, border != -kInf, border};
+    Asked a{temperature, top_p, max, k, u, top_p < 1.f, border != -kInf, max == kInf, border};
     constexpr uint32_t E = Pieces<T>::E, kOwn = kBins / THREADS;
     SampleLds<THREADS>& s = sample_lds<T, THREADS>();
     const Bins bins = bins_of(a.max, a.temperature);
@@ -872,8 +999,9 @@ __device__ __forceinline__ uint64_t answer_by_numbers(const Row<T, THREADS>& r, 
     }
     auto number = [&](uint32_t bin) { return bin == (uint32_t)kFixedTop ? 0.f : bins.number(bin); };
     auto mass = [&](uint32_t bin, uint32_t n) { return bin == (uint32_t)kFixedTop ? zeros : n * r.masses(bins.number(bin)); };
-    uint64_t sum = r.sum_groups(mass);
+    r.sum_groups(mass);
     if (threadIdx.x < 64) {
+        uint64_t sum = r.sum_before_groups();
         bool known = true;
         auto each_of = [&](uint32_t bin) {
             const uint64_t each = r.masses(number(bin));
@@ -913,8 +1041,86 @@ __device__ __forceinline__ uint64_t answer_by_numbers(const Row<T, THREADS>& r, 
         if (threadIdx.x == 0) s.through = known ? sum : 0;
     }
     __syncthreads();
-    sum = s.through;
+    const uint64_t sum = s.through;
     if (sum) kept.find(s.value, s.before, s.ahead);
+    return sum;
+}
+
+// Rows of any numbers between the fixed bins' ends: masses of four bins at a time, and lists of what lies in those that matter.  Returns 0 if a list is too short.
+template <typename T, int THREADS, int N>
+__device__ __forceinline__ uint64_t answer_by_masses(const Row<T, THREADS>& r, const Kept<T, THREADS, N>& kept, const Asked& a, float k_low, float k_high, uint32_t k_left) {
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+    static_assert(kBins * 4 == kFixedBins && kBins == 64 * 32);
+    const Bins bins = fixed_bins();
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < kBins; i += THREADS) s.mass[i] = 0;
+    __syncthreads();
+    const float from = a.k && k_low > r.least ? k_low : r.least;
+    uint64_t above = 0, sum;                                      // above: mass before the k-th logit's bin
+    kept.of_all([&](float v) {
+        if (v >= from) {
+            const uint64_t mass = r.masses(v);
+            atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[(bins(v) - kFixedFirst) / 4]), (unsigned long long)mass);
+            if (a.k && v > k_high) above += mass;
+        }
+    });
+    __syncthreads();
+    constexpr uint32_t kOwn = kBins / THREADS;
+    uint64_t own[kOwn], mine = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kOwn; ++i) {
+        own[i] = s.mass[threadIdx.x * kOwn + i];
+        mine += own[i];
+    }
+    uint64_t before = before_thread<THREADS>(mine, s.sums, sum);
+#pragma unroll
+    for (uint32_t i = 0; i < kOwn; ++i) {
+        s.mass[threadIdx.x * kOwn + i] = before;
+        before += own[i];
+    }
+    __syncthreads();
+    uint32_t loaded = ~0u, n = 0;
+    uint64_t ahead = 0;
+    // the list of bin g, or of the k-th's
+    auto load = [&](uint32_t g) {
+        if (g == loaded) return;
+        loaded = g;
+        ahead = s.mass[g];
+        const float low = bins.lowest(kFixedFirst + 4 * g + 3);
+        n = kept.gather(low > from ? low : from, bins.highest(kFixedFirst + 4 * g));
+        if (n && n <= kList) r.settle(n, ahead);
+    };
+    // the bin in which mass reaches t
+    auto find = [&](uint64_t t) {
+        const uint32_t lane = threadIdx.x & 63, thirty = (uint32_t)__popcll(__ballot(s.mass[lane * 32] < t)) - 1;
+        return uniform(thirty * 32 + (uint32_t)__popcll(__ballot(lane < 32 && s.mass[thirty * 32 + (lane & 31)] < t)) - 1);
+    };
+    if (a.k) {
+        (void)before_thread<THREADS>(above, s.sums, above);
+        n = kept.gather(from, k_high);
+        if (n > kList) return 0;
+        if (n) r.settle(n, above);
+        sum = n ? s.upto[k_left < n ? k_left - 1 : n - 1] : above;
+    }
+    if (a.by_mass) {
+        const uint64_t t = a.share(sum);
+        load(find(t));
+        if (n > kList) return 0;
+        sum = r.list_mass(n, ahead, t);
+    }
+    if (a.by_value) {
+        const float at = (float)(r.masses.max + a.border);
+        if (at >= from) {
+            load((bins(at) - kFixedFirst) / 4);
+            if (n > kList) return 0;
+            const uint64_t to = n ? r.list_value(n, ahead, a.border) : ahead;
+            sum = to < sum ? to : sum;
+        }
+    }
+    const uint64_t t = __umul64hi(a.u, sum) + 1;
+    load(find(t));
+    if (n > kList) return 0;
+    (void)r.list_mass(n, ahead, t);
     return sum;
 }
 
@@ -924,21 +1130,9 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
     SampleLds<THREADS>& s = sample_lds<T, THREADS>();
     const uint64_t row = a.row0 + blockIdx.x;
     Row<T, THREADS> r{static_cast<const T*>(a.z) + row * a.z_ld, (uint32_t)a.vocab, {}, 0.f};
-    Asked asked;
-    asked.temperature = a.each.temperature_dev ? a.each.temperature_dev[row] : a.temperature;
-    asked.top_p = a.each.top_p_dev ? a.each.top_p_dev[row] : a.top_p;
-    const int32_t top_k = a.each.top_k_dev ? a.each.top_k_dev[row] : a.top_k;
-    const float min_p = a.each.min_p_dev ? a.each.min_p_dev[row] : a.min_p, u = a.u[row];
-    asked.k = top_k > 0 && (uint32_t)top_k < r.vocab ? (uint32_t)top_k : 0;
-    if (!(asked.temperature >= __FLT_MIN__ && asked.temperature < kInf)) {                 // the largest logit
-        asked.temperature = 1.f;
-        asked.k = 1;
-    }
     const Kept<T, THREADS, N> kept(r.z, r.vocab);
+    Asked asked = asked_of(a, row);
     if (threadIdx.x == 0) s.index = 0;
-    asked.by_mass = asked.top_p < 1.f;
-    asked.u = !(u > 0.f) ? 0 : u >= 1.f ? ~0ull : (uint64_t)((double)u * 0x1p64);
-
     // the largest, and how many logits are in each of the fixed bins
     const bool few = r.vocab <= kList, counted = !few && (kNumbers || asked.k);
     float max = -kInf;
@@ -946,6 +1140,7 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
     if (counted) {
         u32x4* const clear = reinterpret_cast<u32x4*>(s.count);
         for (uint32_t i = threadIdx.x; i < kFixedCounts / 4; i += THREADS) clear[i] = u32x4{0, 0, 0, 0};
+        r.clear_groups();
         if (threadIdx.x == 0) {
             s.held = s.ahead = 0;                                 // (ahead: there are numbers around 0 that are not 0)
             s.bin = ~0u;
@@ -981,25 +1176,11 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
         for (int w = 0; w < THREADS / 64; ++w) max = max_or_nan(max, s.most[w]);
     }
     max = uniform(max);
-    if (max != max || max == -kInf) {                             // no answer
-        if (threadIdx.x == 0) {
-            a.token[row] = -1;
-            if (a.logp) a.logp[row] = max;
-        }
+    if (max != max || max == -kInf) {
+        if (threadIdx.x == 0) no_answer(a, row, max);
         return;
     }
-    const bool infinite = max == kInf;
-    const double t64 = (double)asked.temperature;
-    r.masses.max = (double)max;
-    r.masses.scale = uniform(1.44269504088896340736 / t64);
-    r.masses.least = infinite ? 0.0 : -1000.0;
-    r.masses.bits = 62 - (r.vocab > 1 ? 32 - __builtin_clz(r.vocab - 1) : 0);
-    if (r.masses.bits > 51) r.masses.bits = 51;
-    // below: masses of less than half of a unit.  (In 32 bits: off by less than what one unit more of the exponent allows for.)
-    r.least = infinite ? kInf : fmaxf((float)((double)max - (r.masses.bits + 2) * 0.69314718055994530942 * t64 - fabs((double)max) * 0x1p-20), -__FLT_MAX__);
-    asked.max = max;
-    asked.by_value = min_p > 0.f && !infinite;                    // (infinite ones are alike)
-    asked.border = asked.by_value ? t64 * log((double)(min_p < 1.f ? min_p : 1.f)) : -kInf;
+    ask(a, row, max, asked, r.masses, r.least);
     const bool fixed = counted && max < kFixedMost && r.least > -kFixedMost;
     bool listed = few;                                            // everything that matters lies above r.least, and the list has room for it
     if (asked.by_value && !asked.by_mass && !few) {               // no other filter needs what this one leaves out
@@ -1010,39 +1191,306 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
     uint32_t k_bin = 0, k_left = 0;
     if (fixed && asked.k) {
         auto count = [](uint32_t, uint32_t n) { return (uint64_t)n; };
-        const uint64_t all = r.sum_groups(count);
-        if (asked.k >= all) asked.k = 0;
-        if (asked.k) {
-            const auto f = r.find_bin(false, 0, asked.k, count);  // (in every wave)
-            k_bin = uniform(f.bin);
-            k_left = asked.k - uniform((uint32_t)f.before);
-            listed = f.before + f.here <= kList;
+        r.sum_groups(count);
+        if (threadIdx.x < 64) {
+            const uint64_t all = r.sum_before_groups();
+            uint32_t bin = ~0u, ahead = 0, upto = 0;
+            if (asked.k < all) {
+                const auto f = r.find_bin(false, 0, asked.k, count);
+                bin = f.bin;
+                ahead = (uint32_t)f.before;
+                upto = (uint32_t)(f.before + f.here);
+            }
+            if (threadIdx.x == 0) {
+                s.bin = bin;
+                s.least = ahead;
+                s.held = upto;
+            }
+        }
+        __syncthreads();
+        k_bin = uniform(s.bin);
+        if (k_bin == ~0u) {
+            asked.k = 0;
+        } else {
+            k_left = asked.k - uniform(s.least);
+            listed = uniform(s.held) <= kList;
             k_low = fixed_bins().lowest(k_bin);
             k_high = fixed_bins().highest(k_bin);
             if (listed && k_low > r.least) r.least = k_low;
-            __syncthreads();
         }
+        r.clear_groups();
+        __syncthreads();
     }
     uint64_t sum = 0;
     bool done = false;
     if (listed || (!kNumbers && asked.by_value && !asked.by_mass && !asked.k)) {
-        const uint32_t n = kept.gather(r.least);
-        if (n <= kList) {
-            sum = answer_from_list(r, asked, n);
-            done = true;
-        }
+        const uint32_t n = kept.gather(r.least, kInf);
+        if (n <= kList) return finish_from_list(a, row, r, asked, n);
     }
     if constexpr (kNumbers)
         if (!done && fixed) {
             sum = answer_by_numbers(r, kept, asked, k_bin, k_left);
             done = sum != 0;
         }
+    if constexpr (!kNumbers && N <= 8)
+        if (!done && max < kFixedMost && r.least > -kFixedMost && (!asked.k || k_left)) {
+            sum = answer_by_masses(r, kept, asked, k_low, k_high, k_left);
+            done = sum != 0;
+        }
     if (!done) sum = answer_any(r, asked.temperature, asked.top_p, max, asked.k, asked.u, asked.border, k_low, k_high, k_left);
-    if (threadIdx.x != 0) return;
-    const uint32_t index = s.index;
-    a.token[row] = (int32_t)index;
-    const double y = infinite ? 0.0 : ((double)(float)r.z[index] - (double)max) / t64;
-    if (a.logp) a.logp[row] = (float)(y - log(ldexp((double)sum, -r.masses.bits)));
+    if (threadIdx.x == 0) write_answer(a, row, asked, r.masses, s.index, (float)r.z[s.index], sum);
+}
+
+// Short rows: a wave each, with the row in LDS.  Bins are linear between what is looked for and divided again as long as more than 64 different logits lie in
+// the one that matters.
+constexpr uint32_t kWaveBins = 256, kWaveRows = 4;
+template <uint32_t ROOM>
+struct WaveLds {
+    uint64_t mass[kWaveBins], list[64];
+    uint32_t count[kWaveBins];
+    float z[ROOM];
+};
+template <typename T, uint32_t ROOM>
+__global__ void __launch_bounds__(64 * kWaveRows) sample_wave_kernel(SampleShape a, uint64_t rows_end) {
+    constexpr uint32_t E = Pieces<T>::E, kOwn = kWaveBins / 64, kStep = 4 * 64;
+    using Piece = typename Pieces<T>::Piece;
+    __shared__ WaveLds<ROOM> lds[kWaveRows];
+    WaveLds<ROOM>& s = lds[threadIdx.x / 64];
+    const uint32_t lane = threadIdx.x & 63, vocab = (uint32_t)a.vocab;
+    const uint64_t row = a.row0 + (uint64_t)blockIdx.x * kWaveRows + uniform(threadIdx.x / 64);
+    if (row >= rows_end) return;
+    const T* z = static_cast<const T*>(a.z) + row * a.z_ld;
+    const uint32_t end = (vocab + kStep - 1) / kStep * kStep;    // filled with minus infinity
+    float max = -kInf;
+    for (uint32_t at = lane * E; at < end; at += 64 * E) {
+        float v[E];
+        if (at + E <= vocab) {
+            const Piece piece = *reinterpret_cast<const Piece*>(z + at);
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) v[e] = (float)piece[e];
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) v[e] = at + e < vocab ? (float)z[at + e] : -kInf;
+        }
+        max = max_or_nan(max, largest_of(v));
+#pragma unroll
+        for (uint32_t e = 0; e < E; e += 4) *reinterpret_cast<f32x4*>(s.z + at + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+    }
+    Asked q = asked_of(a, row);
+    // f(logit, column), kept together four times 64 at once; the first ones first
+    auto of_all = [&](auto f) {
+#pragma unroll 1
+        for (uint32_t at = lane; at < end; at += kStep) {
+            float x[4];
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) x[i] = s.z[at + i * 64];
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) f(x[i], at + i * 64);
+        }
+    };
+    auto smaller = [](float x, float y) { return x < y ? x : y; };
+    auto larger = [](float x, float y) { return x > y ? x : y; };
+    auto plus = [](uint32_t x, uint32_t y) { return x + y; };
+    max = uniform(over_lanes<64>(max, [](float x, float y) { return max_or_nan(x, y); }));
+    wave_sync();
+    if (max != max || max == -kInf) {
+        if (lane == 0) no_answer(a, row, max);
+        return;
+    }
+    Masses masses;
+    float least;
+    ask(a, row, max, q, masses, least);
+    if (q.infinite) {                                             // as zeros among minus infinities
+        for (uint32_t at = lane; at < end; at += 64) s.z[at] = s.z[at] == kInf ? 0.f : -kInf;
+        masses.max = 0.0;
+        masses.least = -1000.0;
+        least = 0.f;
+        wave_sync();
+    }
+    auto distance = [&](float x) { return masses.max - (double)x; };
+
+    // bins of the logits from lo to hi, at level 0 from the lowest that has mass to the largest
+    float lo = kInf, hi = q.infinite ? 0.f : max;
+    uint32_t n = 0;
+    of_all([&](float x, uint32_t) {
+        if (x >= least) {
+            lo = smaller(lo, x);
+            ++n;
+        }
+    });
+    lo = uniform(over_lanes<64>(lo, smaller));
+    n = uniform(over_lanes<64>(n, plus));
+    if (q.k >= n) q.k = 0;
+    double from, scale;
+    auto set_bins = [&] {
+        from = distance(hi);
+        scale = uniform((kWaveBins - 0.5) / (distance(lo) - from));                        // (infinite where they are the same: not used)
+    };
+    auto bin_of = [&](float x) { return (uint32_t)((distance(x) - from) * scale); };
+    uint64_t own[kOwn], before;                                   // masses of the lane's bins, and before them
+    uint32_t own_count[kOwn], count_before;
+    auto fill_bins = [&] {
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn; ++i) {
+            s.mass[i * 64 + lane] = 0;
+            s.count[i * 64 + lane] = 0;
+        }
+        wave_sync();
+        of_all([&](float x, uint32_t) {
+            if (x >= lo && x <= hi) {
+                const uint32_t bin = bin_of(x);
+                atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[bin]), (unsigned long long)masses(x));
+                atomicAdd(&s.count[bin], 1u);
+            }
+        });
+        wave_sync();
+        uint64_t sum = 0;
+        uint32_t count = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn; ++i) {
+            own[i] = s.mass[lane * kOwn + i];
+            own_count[i] = s.count[lane * kOwn + i];
+            sum += own[i];
+            count += own_count[i];
+        }
+        before = upto_lane(sum) - sum;
+        count_before = upto_lane(count) - count;
+        wave_sync();
+    };
+    const float lowest = lo, highest = hi;
+    uint32_t index = 0;
+    float value = 0.f;
+    uint64_t sum = 0;
+    bool whole = false;                                           // the bins are those of level 0
+    for (int step = 0; step < 4; ++step) {                        // top_k, top_p, min_p, the token
+        if ((step == 0 && !q.k && lowest != highest) || (step == 1 && !q.by_mass) || (step == 2 && !q.by_value)) {
+            if (step != 0) continue;
+        }
+        lo = lowest;
+        hi = highest;
+        uint64_t ahead = 0, t = step == 0 ? q.k : step == 1 ? q.share(sum) : __umul64hi(q.u, sum) + 1;
+        uint32_t here = n;                                        // logits from lo to hi
+        bool first = true;
+        uint64_t through = 0;
+        for (;;) {
+            if (lo == hi) {                                       // all the same number
+                const uint64_t each = masses(lo);
+                const uint64_t nth = step == 0 ? (q.k ? t : here) : step == 2 ? (-distance(lo) >= q.border ? here : 0) : (t - ahead + each - 1) / each;
+                through = ahead + nth * each;
+                if (step == 3) {
+                    uint32_t left = (uint32_t)nth;
+                    value = lo;
+                    of_all([&](float x, uint32_t column) {
+                        const uint64_t those = __ballot(x == lo);
+                        const uint32_t all = (uint32_t)__popcll(those);
+                        if (left && left <= all) {
+                            const uint32_t below = __builtin_amdgcn_mbcnt_hi((uint32_t)(those >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)those, 0));
+                            index = (uint32_t)__builtin_amdgcn_readlane(column, __builtin_ctzll(__ballot(x == lo && below == left - 1)));
+                        }
+                        left = left <= all ? 0 : left - all;
+                    });
+                }
+                break;
+            }
+            if (here <= 64) {                                     // one of them a lane, in their order
+                uint32_t held = 0;
+                of_all([&](float x, uint32_t column) {
+                    const bool in = x >= lo && x <= hi;
+                    const uint64_t those = __ballot(in);
+                    if (in) s.list[held + __builtin_amdgcn_mbcnt_hi((uint32_t)(those >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)those, 0))] = logit_rank(x, column);
+                    held += (uint32_t)__popcll(those);
+                });
+                wave_sync();
+                const uint64_t mine = lane < here ? s.list[lane] : 0;
+                uint32_t place = 0;
+                for (uint32_t j = 0; j < here; ++j) place += s.list[j] > mine ? 1u : 0u;
+                wave_sync();
+                if (lane < here) s.list[place] = mine;
+                wave_sync();
+                const uint64_t rank = lane < here ? s.list[lane] : 0;
+                const float x = of_key((uint32_t)(rank >> 32));
+                const uint64_t upto = ahead + upto_lane(lane < here ? masses(x) : 0);
+                wave_sync();
+                uint32_t at;                                      // of the last that is kept, or of the token; here: none
+                if (step == 0) at = (q.k ? (uint32_t)t : here) - 1;
+                else if (step == 2) at = (uint32_t)__popcll(__ballot(lane < here && -distance(x) >= q.border)) - 1;
+                else at = (uint32_t)__builtin_ctzll(__ballot(lane < here && upto >= t));
+                through = at == ~0u ? ahead : of_lane(upto, at);
+                if (step == 3) {
+                    index = ~(uint32_t)__builtin_amdgcn_readlane((uint32_t)rank, at);
+                    value = uniform(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), at)));
+                }
+                break;
+            }
+            if (!(first && whole)) {
+                set_bins();
+                fill_bins();
+                whole = first;
+            }
+            if (step == 0 && !q.k) {                              // all of it
+                uint64_t mine = 0;
+#pragma unroll
+                for (uint32_t i = 0; i < kOwn; ++i) mine += own[i];
+                through = of_lane(before + mine, 63);
+                break;
+            }
+            // the bin
+            uint32_t which = 0, inside = 0;
+            uint64_t upto = ahead + before;
+            bool it = false;
+            if (step == 2) {
+                const double d = -q.border;
+                const uint32_t bin = d <= from ? 0 : (d - from) * scale >= kWaveBins ? kWaveBins - 1 : (uint32_t)((d - from) * scale);
+#pragma unroll
+                for (uint32_t i = 0; i < kOwn; ++i) {
+                    if (lane * kOwn + i == bin) {
+                        it = true;
+                        which = i;
+                        inside = own_count[i];
+                    }
+                    if (!it) upto += own[i];
+                }
+            } else {
+                uint32_t counted = count_before;
+#pragma unroll
+                for (uint32_t i = 0; i < kOwn; ++i) {
+                    const bool reached = step == 0 ? counted < t && t <= counted + own_count[i] : upto < t && t <= upto + own[i];
+                    if (reached && !it) {
+                        it = true;
+                        which = i;
+                        inside = own_count[i];
+                    }
+                    if (!it) {
+                        upto += own[i];
+                        counted += own_count[i];
+                    }
+                }
+                if (step == 0 && it) t -= counted;
+            }
+            const uint32_t owner = (uint32_t)__builtin_ctzll(__ballot(it));
+            const uint32_t bin = owner * kOwn + (uint32_t)__builtin_amdgcn_readlane(which, owner);
+            here = (uint32_t)__builtin_amdgcn_readlane(inside, owner);
+            ahead = of_lane(upto, owner);
+            if (step == 0) t = of_lane(t, owner);
+            if (here == 0) {
+                through = ahead;
+                break;
+            }
+            float low = kInf, high = -kInf;
+            of_all([&](float x, uint32_t) {
+                if (x >= lo && x <= hi && bin_of(x) == bin) {
+                    low = smaller(low, x);
+                    high = larger(high, x);
+                }
+            });
+            lo = uniform(over_lanes<64>(low, smaller));
+            hi = uniform(over_lanes<64>(high, larger));
+            first = false;
+        }
+        if (step == 2) sum = through < sum ? through : sum;
+        else if (step < 2) sum = through;
+    }
+    if (lane == 0) write_answer(a, row, q, masses, index, value, sum);
 }
 
 template <int V>
@@ -1058,7 +1506,12 @@ void launch_sample_of(const SampleArgs& args, hipStream_t stream) {
         auto launch = [&](auto threads, auto pieces, auto waves) {
             hipLaunchKernelGGL((sample_kernel<T, decltype(threads)::value, decltype(pieces)::value, decltype(waves)::value>), dim3(here), dim3(threads.value), 0, stream, a);
         };
-        if (a.vocab * sizeof(T) <= 256 * 8 * 16) launch(Int<256>(), Int<8>(), Int<4>());
+        auto launch_waves = [&](auto room) {
+            hipLaunchKernelGGL((sample_wave_kernel<T, decltype(room)::value>), dim3((here + kWaveRows - 1) / kWaveRows), dim3(64 * kWaveRows), 0, stream, a, r + here);
+        };
+        if (a.vocab <= 512) launch_waves(Int<512>());
+        else if (a.vocab <= 2048) launch_waves(Int<2048>());
+        else if (a.vocab * sizeof(T) <= 256 * 8 * 16) launch(Int<256>(), Int<8>(), Int<4>());
         else launch(Int<512>(), Int<16>(), Int<4>());
     }
 }
