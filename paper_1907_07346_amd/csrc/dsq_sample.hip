@@ -313,14 +313,19 @@ struct Kept {
         }
         return max;
     }
-    // Counts logits in fixed bins.  Returns the thread's largest one; of bf16, whose bins tell it, the largest magnitudes of either half of its words.
-    __device__ __forceinline__ uint32_t count_fixed() const {
+    // Counts logits in fixed bins.  Returns the thread's largest one; of bf16, whose bins tell it, the first bin in which it counted one, and whether it met a NaN.
+    struct Counted {
+        float max;
+        uint32_t first;
+        bool nan;
+    };
+    __device__ __forceinline__ Counted count_fixed() const {
         SampleLds<THREADS>& s = sample_lds<T, THREADS>();
         auto add = [&](uint32_t place) { atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.count) + place), 1u); };
         const uint32_t most = kFixedSide + (threadIdx.x & 63);
         typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
         typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
-        u16x2 magnitudes = 0;
+        u16x2 magnitudes = 0, places = (uint16_t)0xFFFF;
         float max = -kInf;
         auto f = [&](u32x4 raw) {
             if constexpr (kNumbers) {                             // two at a time
@@ -333,9 +338,10 @@ struct Kept {
                     u16x2 c = __builtin_elementwise_min(__builtin_elementwise_sub_sat(magnitude, base), side);
                     const u16x2 sign = __builtin_bit_cast(u16x2, __builtin_bit_cast(i16x2, bits) >> (int16_t)15);
                     c = (u16x2)(((sign - (c ^ sign)) << (uint16_t)2) + top);               // top - c, or top + c where the sign is set; in bytes
-                    const uint32_t places = __builtin_bit_cast(uint32_t, c);
-                    add(places & 0xFFFFu);
-                    add(places >> 16);
+                    places = __builtin_elementwise_min(places, c);
+                    const uint32_t at = __builtin_bit_cast(uint32_t, c);
+                    add(at & 0xFFFFu);
+                    add(at >> 16);
                 }
             } else {
                 float v[E];
@@ -363,7 +369,8 @@ struct Kept {
             else end[0] = (end[0] & 0xFFFF0000u) | __builtin_bit_cast(uint16_t, last);
             f(end);
         }
-        return kNumbers ? __builtin_bit_cast(uint32_t, magnitudes) : __float_as_uint(max);
+        const uint16_t first = places[0] < places[1] ? places[0] : places[1];
+        return {max, first / 4u, magnitudes[0] > 0x7F80 || magnitudes[1] > 0x7F80};
     }
     // f(logit) for all of them.
     template <typename F>
@@ -389,10 +396,19 @@ struct Kept {
         __syncthreads();
         if (threadIdx.x == 0) s.held = 0;
         __syncthreads();
+        // a thread's first two wait in registers, so that a wave asks for places but once
+        uint64_t some[2] = {0, 0};
+        uint32_t mine = 0;
         auto one = [&](float v, uint32_t column) {
             if (v >= lo && v <= hi) {
-                const uint32_t place = atomicAdd(&s.held, 1u);
-                if (place < kList) s.list[place] = logit_rank(v, column);
+                const uint64_t rank = logit_rank(v, column);
+                if (mine == 0) some[0] = rank;
+                else if (mine == 1) some[1] = rank;
+                else {
+                    const uint32_t place = atomicAdd(&s.held, 1u);
+                    if (place < kList) s.list[place] = rank;
+                }
+                ++mine;
             }
         };
         auto f = [&](u32x4 raw, uint32_t first) {
@@ -410,6 +426,14 @@ struct Kept {
             for (int p = 0; p < kPieces; ++p) f(raw[p], column(i, p));
         }
         if (whole * E < vocab) one((float)last, last_column());
+        const uint32_t waiting = mine < 2 ? mine : 2, upto = upto_lane(waiting), all = (uint32_t)__builtin_amdgcn_readlane(upto, 63);
+        if (all) {
+            uint32_t place = 0;
+            if ((threadIdx.x & 63) == 0) place = atomicAdd(&s.held, all);
+            place = uniform(place) + upto - waiting;
+            if (waiting > 0 && place < kList) s.list[place] = some[0];
+            if (waiting > 1 && place + 1 < kList) s.list[place + 1] = some[1];
+        }
         __syncthreads();
         return s.held;
     }
@@ -771,9 +795,8 @@ __device__ __forceinline__ Asked asked_of(const SampleShape& a, uint64_t row) {
     return q;
 }
 // What depends on the row's largest logit, which is a number or plus infinity.
-__device__ __forceinline__ void ask(const SampleShape& a, uint64_t row, float max, Asked& q, Masses& masses, float& least) {
+__device__ __forceinline__ void ask(const SampleShape& a, float max, float u, float min_p, Asked& q, Masses& masses, float& least) {
     const double t = (double)q.temperature;
-    const float min_p = a.each.min_p_dev ? a.each.min_p_dev[row] : a.min_p, u = a.u[row];
     q.max = max;
     q.infinite = max == kInf;
     q.by_value = min_p > 0.f && !q.infinite;                      // (infinite ones are alike)
@@ -1137,34 +1160,27 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
     const bool few = r.vocab <= kList, counted = !few && (kNumbers || asked.k);
     float max = -kInf;
     bool known = !counted || !kNumbers;                           // max is the largest, or will be
+    uint32_t first = 0;                                           // counted: the bin of the largest
+    const float u_given = a.u[row], min_p = a.each.min_p_dev ? a.each.min_p_dev[row] : a.min_p;       // (asked for with the row)
     if (counted) {
         u32x4* const clear = reinterpret_cast<u32x4*>(s.count);
         for (uint32_t i = threadIdx.x; i < kFixedCounts / 4; i += THREADS) clear[i] = u32x4{0, 0, 0, 0};
         r.clear_groups();
-        if (threadIdx.x == 0) {
-            s.held = s.ahead = 0;                                 // (ahead: there are numbers around 0 that are not 0)
-            s.bin = ~0u;
-        }
+        if (threadIdx.x == 0) s.held = s.ahead = 0;               // (ahead: there are numbers around 0 that are not 0)
         __syncthreads();
-        const uint32_t largest = kept.count_fixed();
+        const auto c = kept.count_fixed();
+        max = c.max;
         if constexpr (kNumbers) {
             // no number is beyond the bins (NaN is), and the first that is not empty tells the largest, unless it is the one around 0
+            first = over_lanes<64>(c.first, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
+            if ((threadIdx.x & 63) == 0) s.counts[threadIdx.x / 64] = first;
+            if (c.nan) s.held = 1;
             __syncthreads();
-            uint32_t first = ~0u;
 #pragma unroll
-            for (uint32_t i = 0; i < kFixedBins; i += THREADS) {
-                const uint32_t bin = kFixedFirst + i + threadIdx.x;
-                if (r.fixed_count(bin) && bin < first) first = bin;
-            }
-            first = over_lanes<64>(first, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
-            if ((threadIdx.x & 63) == 0) atomicMin(&s.bin, first);
-            if ((largest & 0xFFFFu) > 0x7F80u || largest >> 16 > 0x7F80u || (threadIdx.x < 64 && s.count[threadIdx.x] != 0)) s.held = 1;
-            __syncthreads();
-            known = s.bin != ~0u && s.bin != (uint32_t)kFixedTop && !s.held;
-            if (known) max = fixed_bins().number(s.bin);
-            __syncthreads();
-        } else {
-            max = __uint_as_float(largest);
+            for (int w = 0; w < THREADS / 64; ++w) first = s.counts[w] < first ? s.counts[w] : first;
+            first = uniform(first);
+            known = first > kFixedFirst && first < kFixedLast && first != (uint32_t)kFixedTop && uniform(s.held) == 0;
+            if (known) max = fixed_bins().number(first);
         }
     }
     if (!counted || (kNumbers && !known)) max = kept.largest();
@@ -1180,7 +1196,7 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
         if (threadIdx.x == 0) no_answer(a, row, max);
         return;
     }
-    ask(a, row, max, asked, r.masses, r.least);
+    ask(a, max, u_given, min_p, asked, r.masses, r.least);
     const bool fixed = counted && max < kFixedMost && r.least > -kFixedMost;
     bool listed = few;                                            // everything that matters lies above r.least, and the list has room for it
     if (asked.by_value && !asked.by_mass && !few) {               // no other filter needs what this one leaves out
@@ -1190,36 +1206,58 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
     float k_low = 0.f, k_high = 0.f;
     uint32_t k_bin = 0, k_left = 0;
     if (fixed && asked.k) {
-        auto count = [](uint32_t, uint32_t n) { return (uint64_t)n; };
-        r.sum_groups(count);
-        if (threadIdx.x < 64) {
-            const uint64_t all = r.sum_before_groups();
-            uint32_t bin = ~0u, ahead = 0, upto = 0;
-            if (asked.k < all) {
-                const auto f = r.find_bin(false, 0, asked.k, count);
-                bin = f.bin;
-                ahead = (uint32_t)f.before;
-                upto = (uint32_t)(f.before + f.here);
-            }
-            if (threadIdx.x == 0) {
-                s.bin = bin;
-                s.least = ahead;
-                s.held = upto;
+        // from the largest one's bin on, 64 bins at a time, every wave by itself; where that is long, by groups
+        uint32_t ahead = 0, here = 0;
+        bool there = false;
+        k_bin = kNumbers && known ? first : uniform(fixed_bins()(max));
+        for (int step = 0; step < 12 && !there && k_bin < kFixedLast; ++step) {
+            const uint32_t n = r.fixed_count(k_bin + (threadIdx.x & 63)), upto = upto_lane(n), all = (uint32_t)__builtin_amdgcn_readlane(upto, 63);
+            if (ahead + all >= asked.k) {
+                const uint32_t at = (uint32_t)__builtin_ctzll(__ballot(ahead + upto >= asked.k));
+                here = (uint32_t)__builtin_amdgcn_readlane(n, at);
+                ahead += (uint32_t)__builtin_amdgcn_readlane(upto, at) - here;
+                k_bin += at;
+                there = true;
+            } else {
+                ahead += all;
+                k_bin += 64;
             }
         }
-        __syncthreads();
-        k_bin = uniform(s.bin);
-        if (k_bin == ~0u) {
+        if (!there && k_bin >= kFixedLast) {                      // there are no more than k
             asked.k = 0;
-        } else {
-            k_left = asked.k - uniform(s.least);
-            listed = uniform(s.held) <= kList;
+        } else if (!there) {
+            auto count = [](uint32_t, uint32_t n) { return (uint64_t)n; };
+            r.sum_groups(count);
+            if (threadIdx.x < 64) {
+                const uint64_t all = r.sum_before_groups();
+                uint32_t bin = ~0u;
+                if (asked.k < all) {
+                    const auto f = r.find_bin(false, 0, asked.k, count);
+                    bin = f.bin;
+                    ahead = (uint32_t)f.before;
+                    here = (uint32_t)f.here;
+                }
+                if (threadIdx.x == 0) {
+                    s.bin = bin;
+                    s.least = ahead;
+                    s.held = here;
+                }
+            }
+            __syncthreads();
+            k_bin = uniform(s.bin);
+            ahead = uniform(s.least);
+            here = uniform(s.held);
+            if (k_bin == ~0u) asked.k = 0;
+            r.clear_groups();
+            __syncthreads();
+        }
+        if (asked.k) {
+            k_left = asked.k - ahead;
+            listed = ahead + here <= kList;
             k_low = fixed_bins().lowest(k_bin);
             k_high = fixed_bins().highest(k_bin);
             if (listed && k_low > r.least) r.least = k_low;
         }
-        r.clear_groups();
-        __syncthreads();
     }
     uint64_t sum = 0;
     bool done = false;
@@ -1277,6 +1315,7 @@ __global__ void __launch_bounds__(64 * kWaveRows) sample_wave_kernel(SampleShape
         for (uint32_t e = 0; e < E; e += 4) *reinterpret_cast<f32x4*>(s.z + at + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
     }
     Asked q = asked_of(a, row);
+    const float u = a.u[row], min_p = a.each.min_p_dev ? a.each.min_p_dev[row] : a.min_p;
     // f(logit, column), kept together four times 64 at once; the first ones first
     auto of_all = [&](auto f) {
 #pragma unroll 1
@@ -1299,7 +1338,7 @@ __global__ void __launch_bounds__(64 * kWaveRows) sample_wave_kernel(SampleShape
     }
     Masses masses;
     float least;
-    ask(a, row, max, q, masses, least);
+    ask(a, max, u, min_p, q, masses, least);
     if (q.infinite) {                                             // as zeros among minus infinities
         for (uint32_t at = lane; at < end; at += 64) s.z[at] = s.z[at] == kInf ? 0.f : -kInf;
         masses.max = 0.0;
