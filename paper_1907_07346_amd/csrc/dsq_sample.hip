@@ -114,12 +114,22 @@ template <int THREADS>
 struct SampleLds {
     union {
         uint32_t count[kFixedCounts];
-        uint32_t columns[2 * kList];                              // of a number, when counts are done with
         struct {
-            uint64_t list[kList], sorted[kList], upto[kList];     // ranks of the logits gathered; in order; the mass through each
+            uint64_t list[kList];                                 // ranks of the logits gathered
+            union {
+                struct {
+                    uint64_t sorted[kList], upto[kList];          // in order; the mass through each
+                };
+                u32x4 queue[kList];                               // pieces with something to gather, before that
+            };
+            union {
+                struct {
+                    uint64_t part_mass[kParts];
+                    uint32_t part_count[kParts];
+                };
+                uint32_t queue_column[kList];                     // of their first logits
+            };
             uint64_t mass[kBins];                                 // of bins, and then what lies before them
-            uint64_t part_mass[kParts];
-            uint32_t part_count[kParts];
         };
     };
     uint64_t group[kGroups];                                      // counts or masses of sixteen fixed bins each, and then of all before
@@ -127,7 +137,7 @@ struct SampleLds {
     uint32_t counts[THREADS / 64];
     float most[THREADS / 64];
     uint64_t before, through;                                     // answers
-    uint32_t held, bin, ahead, least, index;
+    uint32_t held, queued, bin, ahead, least, index;
     float value;
 };
 // Of a kernel, and of the functions that it calls: one for each, so that it has an address that is known.
@@ -390,57 +400,75 @@ struct Kept {
         }
         f((float)last);
     }
-    // Gathers the logits from lo to hi (kList of them at most) as ranks; returns how many there are.
-    __device__ __forceinline__ uint32_t gather(float lo, float hi) const {
+    // What is rare is looked for in two steps, so that the code for each piece is short: pieces with some of it, by test(piece), go into a queue (queue, for M of them), and
+    // is(logit) tells for the queue's logits from piece `from` on which ones go to add(logit, column) (expand).
+    __device__ __forceinline__ void clear_queue() const {
         SampleLds<THREADS>& s = sample_lds<T, THREADS>();
         __syncthreads();
-        if (threadIdx.x == 0) s.held = 0;
+        if (threadIdx.x == 0) s.held = s.queued = 0;
         __syncthreads();
-        // a thread's first two wait in registers, so that a wave asks for places but once
-        uint64_t some[2] = {0, 0};
-        uint32_t mine = 0;
-        auto one = [&](float v, uint32_t column) {
-            if (v >= lo && v <= hi) {
-                const uint64_t rank = logit_rank(v, column);
-                if (mine == 0) some[0] = rank;
-                else if (mine == 1) some[1] = rank;
-                else {
-                    const uint32_t place = atomicAdd(&s.held, 1u);
-                    if (place < kList) s.list[place] = rank;
+    }
+    template <int M, typename F, typename C>
+    __device__ __forceinline__ void queue(const u32x4 (&raw)[M], C column_of, F test) const {
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+        uint32_t mask = 0;
+#pragma unroll
+        for (int p = 0; p < M; ++p) mask |= test(raw[p]) ? 1u << p : 0u;
+        if (!__ballot(mask != 0)) return;
+        const uint32_t mine = (uint32_t)__popc(mask), upto = upto_lane(mine), all = (uint32_t)__builtin_amdgcn_readlane(upto, 63);
+        uint32_t place = 0;
+        if ((threadIdx.x & 63) == 0) place = atomicAdd(&s.queued, all);
+        place = uniform(place) + upto - mine;
+#pragma unroll
+        for (int p = 0; p < M; ++p)
+            if (mask >> p & 1u) {
+                if (place < kList) {
+                    s.queue[place] = raw[p];
+                    s.queue_column[place] = column_of(p);
                 }
-                ++mine;
+                ++place;
             }
-        };
-        auto f = [&](u32x4 raw, uint32_t first) {
+    }
+    template <typename F, typename A>
+    __device__ __forceinline__ uint32_t expand(uint32_t from, F is, A add) const {
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+        __syncthreads();
+        const uint32_t queued = s.queued;
+        if (queued <= kList)
+            for (uint32_t i = from * E + threadIdx.x; i < queued * E; i += THREADS) {
+                const float v = (float)reinterpret_cast<const T*>(&s.queue[i / E])[i % E];
+                if (is(v)) add(v, s.queue_column[i / E] + i % E);
+            }
+        __syncthreads();
+        return queued;
+    }
+    // Gathers the logits from lo to hi as ranks; returns how many there are, or more than kList.
+    __device__ __forceinline__ uint32_t gather(float lo, float hi) const {
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+        clear_queue();
+        auto test = [&](u32x4 raw) {
             float v[E];
             values(raw, v);
-            if (!(largest_of(v) >= lo)) return;
-#pragma unroll
-            for (uint32_t e = 0; e < E; ++e) one(v[e], first + e);
+            return largest_of(v) >= lo;
         };
-        of_held(f);
+        auto is = [&](float v) { return v >= lo && v <= hi; };
+        auto add = [&](float v, uint32_t column) {
+            const uint32_t place = atomicAdd(&s.held, 1u);
+            if (place < kList) s.list[place] = logit_rank(v, column);
+        };
+        queue(held, [&](int p) { return (p * THREADS + threadIdx.x) * E; }, test);
         for (uint32_t i = stretches(); i-- > 0;) {
             u32x4 raw[kPieces];
             fetch(raw, i);
-#pragma unroll
-            for (int p = 0; p < kPieces; ++p) f(raw[p], column(i, p));
+            queue(raw, [&](int p) { return column(i, p); }, test);
         }
-        if (whole * E < vocab) one((float)last, last_column());
-        const uint32_t waiting = mine < 2 ? mine : 2, upto = upto_lane(waiting), all = (uint32_t)__builtin_amdgcn_readlane(upto, 63);
-        if (all) {
-            uint32_t place = 0;
-            if ((threadIdx.x & 63) == 0) place = atomicAdd(&s.held, all);
-            place = uniform(place) + upto - waiting;
-            if (waiting > 0 && place < kList) s.list[place] = some[0];
-            if (waiting > 1 && place + 1 < kList) s.list[place + 1] = some[1];
-        }
-        __syncthreads();
-        return s.held;
+        if (whole * E < vocab && is((float)last)) add((float)last, last_column());
+        const uint32_t queued = expand(0, is, add);
+        return queued <= kList ? s.held : queued;
     }
     // The column of the nth (from 1) of the n logits that equal `value`: from the front among those held, or from the row's end.
     __device__ __forceinline__ void find(float value, uint64_t nth, uint32_t n) const {
         SampleLds<THREADS>& s = sample_lds<T, THREADS>();
-        constexpr uint32_t kRoom = 2 * kList;
         // equal numbers are equal bits, but for the sign of 0
         typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
         uint32_t bits, keep = ~0u;
@@ -452,65 +480,54 @@ struct Kept {
             if (value == 0.f) keep = 0x7FFFFFFFu;
         }
         bits &= keep;
-        auto append = [&](uint32_t column) {
-            const uint32_t place = atomicAdd(&s.held, 1u);
-            if (place < kRoom) s.columns[place] = column;
-        };
-        auto f = [&](u32x4 raw, uint32_t first) {
+        auto test = [&](u32x4 raw) {
             u32x4 d;
 #pragma unroll
             for (int i = 0; i < 4; ++i) d[i] = (raw[i] & keep) ^ bits;
             if constexpr (sizeof(T) == 2) {
                 auto least = [](uint32_t x, uint32_t y) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y))); };
                 const uint32_t m = least(least(d[0], d[1]), least(d[2], d[3]));
-                if ((m & 0xFFFFu) != 0 && m >= 0x10000u) return;
-#pragma unroll
-                for (uint32_t e = 0; e < E; ++e)
-                    if ((d[e / 2] >> (16 * (e & 1)) & 0xFFFFu) == 0) append(first + e);
+                return (m & 0xFFFFu) == 0 || m < 0x10000u;
             } else {
-#pragma unroll
-                for (uint32_t e = 0; e < E; ++e)
-                    if (d[e] == 0) append(first + e);
+                return d[0] == 0 || d[1] == 0 || d[2] == 0 || d[3] == 0;
             }
         };
-        auto clear = [&] {
-            __syncthreads();
-            if (threadIdx.x == 0) s.held = 0;
-            __syncthreads();
+        auto is = [&](float v) { return v == value; };
+        auto add = [&](float, uint32_t column) {
+            const uint32_t place = atomicAdd(&s.held, 1u);
+            if (place < kList) s.list[place] = column;
         };
         const uint32_t rest = stretches();
-        clear();
-        of_held(f);
+        clear_queue();
+        queue(held, [&](int p) { return (p * THREADS + threadIdx.x) * E; }, test);
         auto end = [&] {
-            if (whole * E < vocab && (float)last == value) append(last_column());
+            if (whole * E < vocab && is((float)last)) add(0.f, last_column());
         };
         if (!rest) end();
-        __syncthreads();
-        uint32_t found = s.held;
+        uint32_t queued = expand(0, is, add), found = s.held;
         bool forward = true;
-        if (rest && nth > found) {
+        if (rest && queued <= kList && nth > found) {
             forward = false;
             nth = n - nth + 1;
-            clear();
+            clear_queue();
             end();
+            queued = 0;
             for (uint32_t i = rest; i-- > 0;) {
                 u32x4 raw[kPieces];
                 fetch(raw, i);
-#pragma unroll
-                for (int p = 0; p < kPieces; ++p) f(raw[p], column(i, p));
-                __syncthreads();
+                queue(raw, [&](int p) { return column(i, p); }, test);
+                queued = expand(queued, is, add);
                 found = s.held;
-                __syncthreads();
-                if (found >= nth) break;
+                if (found >= nth || queued > kList) break;
             }
         }
-        if (found > kRoom) return find_nth<T, THREADS>(z, vocab, value, forward ? nth : n - nth + 1);
+        if (queued > kList || found > kList) return find_nth<T, THREADS>(z, vocab, value, forward ? nth : n - nth + 1);
         for (uint32_t i = threadIdx.x; i < found; i += THREADS) {
-            const uint32_t mine = s.columns[i];
+            const uint64_t mine = s.list[i];
             uint32_t place = 0;
 #pragma unroll 8
-            for (uint32_t j = 0; j < found; ++j) place += (s.columns[j] < mine) == forward ? 1u : 0u;
-            if (place == (forward ? nth - 1 : nth)) s.index = mine;                        // (backwards it counts itself)
+            for (uint32_t j = 0; j < found; ++j) place += (s.list[j] < mine) == forward ? 1u : 0u;
+            if (place == (forward ? nth - 1 : nth)) s.index = (uint32_t)mine;              // (backwards it counts itself)
         }
         __syncthreads();
     }
