@@ -438,6 +438,8 @@ def ds_sample(z: "torch.Tensor", u: "torch.Tensor", temperature=1.0, top_k=0, to
         _on_device("ds_sample", name, value)
         each = each or ds_sampling_rows()
         setattr(each, name + "_dev", value.data_ptr())
+        if name == "top_k":
+            s.top_k = 1                                       # (some rows have one: see include/dsq.h)
         own.append(value)
     token, logp = _new(stream, (rows,), torch.int32, z), _new(stream, (rows,), torch.float32, z)
     if rows:

@@ -1086,17 +1086,90 @@ __device__ __forceinline__ uint64_t answer_by_numbers(const Row<T, THREADS>& r, 
     return sum;
 }
 
-// Rows of any numbers between the fixed bins' ends: masses of four bins at a time, and lists of what lies in those that matter.  Returns 0 if a list is too short.
+// The bin in which mass reaches t; s.mass holds what lies before each.
+template <typename T, int THREADS>
+__device__ __forceinline__ uint32_t bin_at_mass(uint64_t t) {
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+    const uint32_t lane = threadIdx.x & 63, thirty = (uint32_t)__popcll(__ballot(s.mass[lane * 32] < t)) - 1;
+    return uniform(thirty * 32 + (uint32_t)__popcll(__ballot(lane < 32 && s.mass[thirty * 32 + (lane & 31)] < t)) - 1);
+}
+// What lies before each bin takes the masses' place; returns the sum of all.
+template <typename T, int THREADS>
+__device__ __forceinline__ uint64_t sum_before_bins() {
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+    static_assert(kBins == 64 * 32);
+    constexpr uint32_t kOwn = kBins / THREADS;
+    uint64_t own[kOwn], mine = 0, all;
+#pragma unroll
+    for (uint32_t i = 0; i < kOwn; ++i) {
+        own[i] = s.mass[threadIdx.x * kOwn + i];
+        mine += own[i];
+    }
+    uint64_t before = before_thread<THREADS>(mine, s.sums, all);
+#pragma unroll
+    for (uint32_t i = 0; i < kOwn; ++i) {
+        s.mass[threadIdx.x * kOwn + i] = before;
+        before += own[i];
+    }
+    __syncthreads();
+    return all;
+}
+
+// The mass that is kept, and s.index, out of bins and of lists of what lies in those that matter.  s.mass: what lies before each bin; sum: of the first top_k, or if k_left > 0 the
+// k_left-th logit from k_low to k_high, with `above` before them, is the last of these; gather(lo, hi) makes a list of the logits from lo to hi, none of them below `from`; bin(v),
+// low(bin), high(bin).  Returns 0 if a list is too short.
+template <typename T, int THREADS, typename G, typename B, typename L, typename H>
+__device__ __forceinline__ uint64_t answer_by_bins(const Row<T, THREADS>& r, const Asked& a, uint64_t sum, float k_low, float k_high, uint32_t k_left, uint64_t above, float from, G gather, B bin,
+                                                   L low, H high) {
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+    uint32_t loaded = ~0u, n = 0;
+    uint64_t ahead = 0;
+    auto load = [&](uint32_t g) {
+        if (g == loaded) return;
+        loaded = g;
+        ahead = s.mass[g];
+        n = gather(low(g) > from ? low(g) : from, high(g));
+        if (n && n <= kList) r.settle(n, ahead);
+    };
+    if (k_left) {
+        n = gather(k_low > from ? k_low : from, k_high);
+        if (n > kList) return 0;
+        if (n) r.settle(n, above);
+        sum = n ? s.upto[k_left < n ? k_left - 1 : n - 1] : above;
+    }
+    for (int step = 1; step < 4; ++step) {                        // top_p, min_p, the token
+        if ((step == 1 && !a.by_mass) || (step == 2 && !a.by_value)) continue;
+        const uint64_t t = step == 1 ? a.share(sum) : __umul64hi(a.u, sum) + 1;
+        if (step == 2) {
+            const float at = (float)(r.masses.max + a.border);
+            if (at < from) continue;
+            load(bin(at));
+        } else {
+            load(bin_at_mass<T, THREADS>(t));
+        }
+        if (n > kList) return 0;
+        if (step == 2) {
+            const uint64_t to = n ? r.list_value(n, ahead, a.border) : ahead;
+            sum = to < sum ? to : sum;
+        } else {
+            const uint64_t to = r.list_mass(n, ahead, t);
+            if (step == 1) sum = to;
+        }
+    }
+    return sum;
+}
+
+// Rows of any numbers between the fixed bins' ends: masses of four bins at a time.
 template <typename T, int THREADS, int N>
 __device__ __forceinline__ uint64_t answer_by_masses(const Row<T, THREADS>& r, const Kept<T, THREADS, N>& kept, const Asked& a, float k_low, float k_high, uint32_t k_left) {
     SampleLds<THREADS>& s = sample_lds<T, THREADS>();
-    static_assert(kBins * 4 == kFixedBins && kBins == 64 * 32);
+    static_assert(kBins * 4 == kFixedBins);
     const Bins bins = fixed_bins();
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < kBins; i += THREADS) s.mass[i] = 0;
     __syncthreads();
     const float from = a.k && k_low > r.least ? k_low : r.least;
-    uint64_t above = 0, sum;                                      // above: mass before the k-th logit's bin
+    uint64_t above = 0;                                           // mass before the k-th logit's bin
     kept.of_all([&](float v) {
         if (v >= from) {
             const uint64_t mass = r.masses(v);
@@ -1105,63 +1178,11 @@ __device__ __forceinline__ uint64_t answer_by_masses(const Row<T, THREADS>& r, c
         }
     });
     __syncthreads();
-    constexpr uint32_t kOwn = kBins / THREADS;
-    uint64_t own[kOwn], mine = 0;
-#pragma unroll
-    for (uint32_t i = 0; i < kOwn; ++i) {
-        own[i] = s.mass[threadIdx.x * kOwn + i];
-        mine += own[i];
-    }
-    uint64_t before = before_thread<THREADS>(mine, s.sums, sum);
-#pragma unroll
-    for (uint32_t i = 0; i < kOwn; ++i) {
-        s.mass[threadIdx.x * kOwn + i] = before;
-        before += own[i];
-    }
-    __syncthreads();
-    uint32_t loaded = ~0u, n = 0;
-    uint64_t ahead = 0;
-    // the list of bin g, or of the k-th's
-    auto load = [&](uint32_t g) {
-        if (g == loaded) return;
-        loaded = g;
-        ahead = s.mass[g];
-        const float low = bins.lowest(kFixedFirst + 4 * g + 3);
-        n = kept.gather(low > from ? low : from, bins.highest(kFixedFirst + 4 * g));
-        if (n && n <= kList) r.settle(n, ahead);
-    };
-    // the bin in which mass reaches t
-    auto find = [&](uint64_t t) {
-        const uint32_t lane = threadIdx.x & 63, thirty = (uint32_t)__popcll(__ballot(s.mass[lane * 32] < t)) - 1;
-        return uniform(thirty * 32 + (uint32_t)__popcll(__ballot(lane < 32 && s.mass[thirty * 32 + (lane & 31)] < t)) - 1);
-    };
-    if (a.k) {
-        (void)before_thread<THREADS>(above, s.sums, above);
-        n = kept.gather(from, k_high);
-        if (n > kList) return 0;
-        if (n) r.settle(n, above);
-        sum = n ? s.upto[k_left < n ? k_left - 1 : n - 1] : above;
-    }
-    if (a.by_mass) {
-        const uint64_t t = a.share(sum);
-        load(find(t));
-        if (n > kList) return 0;
-        sum = r.list_mass(n, ahead, t);
-    }
-    if (a.by_value) {
-        const float at = (float)(r.masses.max + a.border);
-        if (at >= from) {
-            load((bins(at) - kFixedFirst) / 4);
-            if (n > kList) return 0;
-            const uint64_t to = n ? r.list_value(n, ahead, a.border) : ahead;
-            sum = to < sum ? to : sum;
-        }
-    }
-    const uint64_t t = __umul64hi(a.u, sum) + 1;
-    load(find(t));
-    if (n > kList) return 0;
-    (void)r.list_mass(n, ahead, t);
-    return sum;
+    const uint64_t sum = sum_before_bins<T, THREADS>();
+    if (a.k) (void)before_thread<THREADS>(above, s.sums, above);
+    return answer_by_bins(
+        r, a, sum, k_low, k_high, a.k ? k_left : 0, above, from, [&](float lo, float hi) { return kept.gather(lo, hi); }, [&](float v) { return (bins(v) - kFixedFirst) / 4; },
+        [&](uint32_t g) { return bins.lowest(kFixedFirst + 4 * g + 3); }, [&](uint32_t g) { return bins.highest(kFixedFirst + 4 * g); });
 }
 
 template <typename T, int THREADS, int N, int WAVES>
@@ -1549,13 +1570,269 @@ __global__ void __launch_bounds__(64 * kWaveRows) sample_wave_kernel(SampleShape
     if (lane == 0) write_answer(a, row, q, masses, index, value, sum);
 }
 
+// Few long rows are split over workgroups, in four launches: the largest of each part; masses (and counts, for top_k) in bins of the row, added up in memory; which bins matter, as
+// far as they tell, and the logits in them into a list of the row; the answer out of bins and list.
+constexpr uint32_t kSplitThreads = 256, kSplitRoom = 2048;        // room: of a row's list
+struct SplitRow {
+    uint64_t mass[kBins];
+    uint64_t list[kSplitRoom];
+    uint32_t count[kBins];
+    float most[64];                                               // of parts
+    uint32_t held, k_bin, k_left, unused;
+};
+struct SplitShape : SampleShape {
+    SplitRow* rows_of;
+    uint32_t parts, part_logits;                                  // parts <= 64; part_logits: a multiple of what 16 bytes hold
+};
+template <typename T>
+__device__ __forceinline__ Row<T, kSplitThreads> part_of(const SplitShape& a) {
+    const uint32_t begin = blockIdx.x * a.part_logits, vocab = (uint32_t)a.vocab;
+    Row<T, kSplitThreads> r{};
+    r.z = static_cast<const T*>(a.z) + (a.row0 + blockIdx.y) * a.z_ld + begin;
+    r.vocab = vocab - begin < a.part_logits ? vocab - begin : a.part_logits;
+    return r;
+}
+__device__ __forceinline__ float split_largest(const SplitShape& a, const SplitRow& w) {
+    const uint32_t lane = threadIdx.x & 63;
+    return uniform(over_lanes<64>(lane < a.parts ? w.most[lane] : -kInf, [](float x, float y) { return max_or_nan(x, y); }));
+}
+template <typename T>
+__device__ __forceinline__ void split_ask(const SplitShape& a, float max, Asked& q, Masses& masses, float& least) {
+    const uint64_t row = a.row0 + blockIdx.y;
+    q = asked_of(a, row);
+    ask(a, max, a.u[row], a.each.min_p_dev ? a.each.min_p_dev[row] : a.min_p, q, masses, least);
+}
+
+// What lies in memory since the launch before is asked for at once, before anything is made of it: a read takes a microsecond.
+struct SplitMasses {
+    static constexpr uint32_t kEach = kBins / kSplitThreads;
+    uint64_t mass[kEach];
+    __device__ __forceinline__ explicit SplitMasses(const SplitRow& w) {
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) mass[i] = w.mass[i * kSplitThreads + threadIdx.x];
+    }
+    __device__ __forceinline__ void put(uint64_t* to) const {
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) to[i * kSplitThreads + threadIdx.x] = mass[i];
+        __syncthreads();
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kSplitThreads) sample_most_kernel(SplitShape a) {
+    constexpr uint32_t E = Pieces<T>::E;
+    __shared__ float most[kSplitThreads / 64];
+    SplitRow& w = a.rows_of[blockIdx.y];
+    const auto r = part_of<T>(a);
+    for (uint32_t i = blockIdx.x * kSplitThreads + threadIdx.x; i < kBins; i += gridDim.x * kSplitThreads) {
+        w.mass[i] = 0;
+        w.count[i] = 0;
+    }
+    float max = -kInf;
+    r.stream([&](const float(&v)[E], uint32_t) { max = max_or_nan(max, largest_of(v)); });
+    max = over_lanes<64>(max, [](float x, float y) { return max_or_nan(x, y); });
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x / 64] = max;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (uint32_t i = 1; i < kSplitThreads / 64; ++i) max = max_or_nan(max, most[i]);
+    w.most[blockIdx.x] = max;
+    if (blockIdx.x == 0) w.held = 0;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSplitThreads) sample_bins_kernel(SplitShape a) {
+    constexpr uint32_t E = Pieces<T>::E;
+    __shared__ uint64_t mass[kBins];
+    __shared__ uint32_t count[kBins];
+    SplitRow& w = a.rows_of[blockIdx.y];
+    for (uint32_t i = threadIdx.x; i < kBins; i += kSplitThreads) {
+        mass[i] = 0;
+        count[i] = 0;
+    }
+    const float max = split_largest(a, w);
+    if (max != max || max == -kInf) return;
+    auto r = part_of<T>(a);
+    Asked q;
+    split_ask<T>(a, max, q, r.masses, r.least);
+    const Bins bins = bins_of(max, q.temperature);
+    __syncthreads();
+    r.stream([&](const float(&v)[E], uint32_t) {
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e)
+            if (v[e] >= r.least) {
+                const uint32_t bin = bins(v[e]);
+                atomicAdd(reinterpret_cast<unsigned long long*>(&mass[bin]), (unsigned long long)r.masses(v[e]));
+                if (q.k) atomicAdd(&count[bin], 1u);
+            }
+    });
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < kBins; i += kSplitThreads) {
+        if (mass[i]) atomicAdd(reinterpret_cast<unsigned long long*>(&w.mass[i]), (unsigned long long)mass[i]);
+        if (count[i]) atomicAdd(&w.count[i], count[i]);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSplitThreads) sample_sift_kernel(SplitShape a) {
+    constexpr uint32_t E = Pieces<T>::E;
+    SampleLds<kSplitThreads>& s = sample_lds<T, kSplitThreads>();
+    SplitRow& w = a.rows_of[blockIdx.y];
+    const SplitMasses masses(w);
+    const float max = split_largest(a, w);
+    if (max != max || max == -kInf) return;
+    auto r = part_of<T>(a);
+    Asked q;
+    split_ask<T>(a, max, q, r.masses, r.least);
+    const Bins bins = bins_of(max, q.temperature);
+    uint32_t k_bin = 0, k_left = 0;
+    if (q.k) {
+        uint32_t* const count = reinterpret_cast<uint32_t*>(s.queue);
+        uint32_t own = 0, all;
+        for (uint32_t i = threadIdx.x; i < kBins; i += kSplitThreads) count[i] = w.count[i];
+        __syncthreads();
+        constexpr uint32_t kOwn = kBins / kSplitThreads;
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn; ++i) own += count[threadIdx.x * kOwn + i];
+        const uint32_t before = before_thread<kSplitThreads>(own, s.counts, all);
+        if (q.k >= all) q.k = 0;
+        if (q.k) {
+            find_kth<T, kSplitThreads>(q.k, before, own, threadIdx.x * kOwn, [&](uint32_t i) { return count[i]; });
+            k_bin = s.bin;
+            k_left = q.k - s.ahead;
+        }
+    }
+    masses.put(s.mass);
+    const uint64_t all = sum_before_bins<T, kSplitThreads>();
+    auto end_of = [&](uint32_t bin) { return bin + 1 < kBins ? s.mass[bin + 1] : all; };
+    // what is kept lies between these two, and what decides it in these bins
+    uint64_t fewest = all, most = all;
+    uint32_t p_from = 1, p_to = 0, value_bin = ~0u;
+    if (k_left) {
+        fewest = s.mass[k_bin] ? s.mass[k_bin] : 1;
+        most = end_of(k_bin);
+    }
+    if (q.by_mass) {
+        p_from = bin_at_mass<T, kSplitThreads>(q.share(fewest));
+        p_to = bin_at_mass<T, kSplitThreads>(q.share(most));
+        fewest = s.mass[p_from] ? s.mass[p_from] : 1;
+        most = end_of(p_to);
+    }
+    if (q.by_value) {
+        const float at = (float)(r.masses.max + q.border);
+        if (at >= r.least) {
+            value_bin = bins(at);
+            const uint64_t before = s.mass[value_bin] ? s.mass[value_bin] : 1, end = end_of(value_bin);
+            fewest = before < fewest ? before : fewest;
+            most = end < most ? end : most;
+        }
+    }
+    const uint32_t from = bin_at_mass<T, kSplitThreads>(__umul64hi(q.u, fewest) + 1), to = bin_at_mass<T, kSplitThreads>(__umul64hi(q.u, most) + 1);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        w.k_bin = k_bin;
+        w.k_left = k_left;
+    }
+    // the part's into LDS, where masses are done with, and then with one request for places into the row's
+    __syncthreads();
+    if (threadIdx.x == 0) s.held = 0;
+    __syncthreads();
+    const uint32_t begin = blockIdx.x * a.part_logits;
+    r.stream([&](const float(&v)[E], uint32_t at) {
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e)
+            if (v[e] >= r.least) {
+                const uint32_t bin = bins(v[e]);
+                if ((bin >= from && bin <= to) || (bin >= p_from && bin <= p_to) || bin == value_bin || (k_left && bin == k_bin)) {
+                    const uint32_t place = atomicAdd(&s.held, 1u);
+                    if (place < kBins) s.mass[place] = logit_rank(v[e], begin + at + e);
+                }
+            }
+    });
+    __syncthreads();
+    const uint32_t held = s.held;
+    if (held == 0) return;
+    if (threadIdx.x == 0) s.ahead = atomicAdd(&w.held, held);
+    __syncthreads();
+    const uint32_t first = s.ahead;
+    for (uint32_t i = threadIdx.x; i < held && i < kBins && first + i < kSplitRoom; i += kSplitThreads) w.list[first + i] = s.mass[i];
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSplitThreads, 4) sample_split_kernel(SplitShape a) {
+    SampleLds<kSplitThreads>& s = sample_lds<T, kSplitThreads>();
+    SplitRow& w = a.rows_of[blockIdx.y];
+    const uint64_t row = a.row0 + blockIdx.y;
+    const SplitMasses masses(w);
+    constexpr uint32_t kEach = kSplitRoom / kSplitThreads;
+    uint64_t rank[kEach];                                         // the thread's part of the list
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) rank[i] = w.list[i * kSplitThreads + threadIdx.x];
+    const uint32_t listed = w.held, k_bin = w.k_bin, k_left = w.k_left;
+    const float max = split_largest(a, w);
+    if (max != max || max == -kInf) {
+        if (threadIdx.x == 0) no_answer(a, row, max);
+        return;
+    }
+    Row<T, kSplitThreads> r{static_cast<const T*>(a.z) + row * a.z_ld, (uint32_t)a.vocab, {}, 0.f};
+    Asked q;
+    split_ask<T>(a, max, q, r.masses, r.least);
+    const Bins bins = bins_of(max, q.temperature);
+    if (threadIdx.x == 0) s.index = 0;
+    masses.put(s.mass);
+    const uint64_t all = sum_before_bins<T, kSplitThreads>();
+    auto gather = [&](float lo, float hi) {
+        __syncthreads();
+        if (threadIdx.x == 0) s.held = 0;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) {
+            const float v = of_key((uint32_t)(rank[i] >> 32));
+            if (i * kSplitThreads + threadIdx.x < listed && v >= lo && v <= hi) {
+                const uint32_t place = atomicAdd(&s.held, 1u);
+                if (place < kList) s.list[place] = rank[i];
+            }
+        }
+        __syncthreads();
+        return s.held;
+    };
+    uint64_t sum = 0;
+    if (listed <= kSplitRoom)
+        sum = answer_by_bins(
+            r, q, all, bins.lowest(k_bin), bins.highest(k_bin), k_left, s.mass[k_bin], r.least, gather, [&](float v) { return bins(v); }, [&](uint32_t g) { return bins.lowest(g); },
+            [&](uint32_t g) { return bins.highest(g); });
+    if (!sum) sum = answer_any(r, q.temperature, q.top_p, max, q.k, q.u, q.border, 0.f, 0.f, 0u);
+    if (threadIdx.x == 0) write_answer(a, row, q, r.masses, s.index, (float)r.z[s.index], sum);
+}
+
+// Workgroups of a row, 1 for none.  Of bf16, and where top_k or min_p alone leave little, a workgroup by itself reads a row twice at most: 1 x 131072, bf16, top_p, 22 us,
+// split 30; 4 x 131072, fp32, min_p, 14.5 and 24.6.  Otherwise it reads it four times and makes masses of all of it: 1 x 131072, fp32, top_p, 88 us, split 25; 32 x 40000 42 and 34; 4 x 20000 25 and 28.
+uint32_t sample_parts(const ds_sampling& l) {
+    const uint64_t size = l.dtype == DS_F32 ? 4 : 2, bytes = l.vocab * size;
+    const bool few_left = l.dtype == DS_BF16 || l.top_k > 0 || (l.min_p > 0.f && l.top_p >= 1.f);
+    if (l.rows > 32 || bytes < (few_left ? 1u << 20 : 1u << 17)) return 1;
+    const uint64_t p = (bytes + 16383) / 16384;
+    return (uint32_t)(p < 64 ? p : 64);
+}
+
 template <int V>
 using Int = std::integral_constant<int, V>;
 
 template <typename T>
 void launch_sample_of(const SampleArgs& args, hipStream_t stream) {
-    SampleShape a{};
+    SplitShape a{};
     static_cast<SampleArgs&>(a) = args;
+    a.parts = a.work ? sample_parts({a.rows, a.vocab, a.dtype, a.top_k, a.temperature, a.top_p, a.min_p, 0}) : 1;
+    if (a.parts > 1) {
+        constexpr uint64_t E = Pieces<T>::E;
+        a.rows_of = static_cast<SplitRow*>(a.work);
+        a.part_logits = (uint32_t)(((a.vocab + a.parts - 1) / a.parts + E - 1) / E * E);
+        a.parts = (uint32_t)((a.vocab + a.part_logits - 1) / a.part_logits);
+        const dim3 grid(a.parts, (unsigned)a.rows), block(kSplitThreads);
+        hipLaunchKernelGGL(sample_most_kernel<T>, grid, block, 0, stream, a);
+        hipLaunchKernelGGL(sample_bins_kernel<T>, grid, block, 0, stream, a);
+        hipLaunchKernelGGL(sample_sift_kernel<T>, grid, block, 0, stream, a);
+        hipLaunchKernelGGL(sample_split_kernel<T>, dim3(1, (unsigned)a.rows), block, 0, stream, a);
+        return;
+    }
     for (uint64_t r = 0; r < a.rows; r += kRowsOfLaunch) {
         a.row0 = r;
         const unsigned here = (unsigned)(a.rows - r < kRowsOfLaunch ? a.rows - r : kRowsOfLaunch);
@@ -1574,7 +1851,9 @@ void launch_sample_of(const SampleArgs& args, hipStream_t stream) {
 
 }  // namespace
 
-uint64_t sample_work_bytes(const ds_sampling&) { return 0; }
+uint64_t sample_work_bytes(const ds_sampling& s) {
+    return sample_parts(s) > 1 ? s.rows * sizeof(SplitRow) : 0;
+}
 
 hipError_t launch_sample(const SampleArgs& a, hipStream_t stream) {
     by_dtype(a.dtype, [&](auto kind) { launch_sample_of<decltype(kind)>(a, stream); });
