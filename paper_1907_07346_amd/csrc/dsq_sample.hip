@@ -535,6 +535,31 @@ struct Kept {
 
 enum Question { kCount, kMass, kValue };                          // at which place do count or mass reach a number, or logits a value
 
+// Puts s.list's n ranks (n <= kList) in order into s.sorted: each goes where as many are above it.  Of few, four threads count for each.  (Numbers that go
+// to all lanes from a register by v_readlane instead of from LDS: 64 x 30000, k = 400, 24 us, and 17.)
+template <typename T, int THREADS>
+__device__ __forceinline__ void sort_list(uint32_t n) {
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+    if (n * 4 <= THREADS) {
+        const uint32_t i = threadIdx.x / 4;
+        const uint64_t mine = i < n ? s.list[i] : 0;
+        uint32_t place = 0;
+#pragma unroll 4
+        for (uint32_t j = threadIdx.x & 3; j < n; j += 4) place += s.list[j] > mine ? 1u : 0u;
+        place = over_lanes<4>(place, [](uint32_t x, uint32_t y) { return x + y; });
+        if (i < n && (threadIdx.x & 3) == 0) s.sorted[place] = mine;
+    } else {
+        for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
+            const uint64_t mine = s.list[i];
+            uint32_t place = 0;
+#pragma unroll 8
+            for (uint32_t j = 0; j < n; ++j) place += s.list[j] > mine ? 1u : 0u;
+            s.sorted[place] = mine;
+        }
+    }
+    __syncthreads();
+}
+
 template <typename T, int THREADS>
 struct Row {
     static constexpr bool kNumbers = std::is_same_v<T, __bf16>;   // a bin is a number
@@ -654,14 +679,7 @@ struct Row {
     // Puts the n gathered logits in order, with the mass through each of them, `before` included.
     __device__ void settle(uint32_t n, uint64_t before) const {
         SampleLds<THREADS>& s = sample_lds<T, THREADS>();
-        for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
-            const uint64_t mine = s.list[i];
-            uint32_t place = 0;
-#pragma unroll 8
-            for (uint32_t j = 0; j < n; ++j) place += s.list[j] > mine ? 1u : 0u;
-            s.sorted[place] = mine;
-        }
-        __syncthreads();
+        sort_list<T, THREADS>(n);
         constexpr uint32_t kEach = kList / THREADS;
         uint64_t mass[kEach], sum = 0;
 #pragma unroll
@@ -856,24 +874,7 @@ __device__ __forceinline__ uint64_t answer_from_list(const Row<T, THREADS>& r, c
 template <typename T, int THREADS>
 __device__ __forceinline__ void finish_from_list(const SampleShape& shape, uint64_t row, const Row<T, THREADS>& r, const Asked& a, uint32_t n) {
     SampleLds<THREADS>& s = sample_lds<T, THREADS>();
-    if (n * 4 <= THREADS) {                                       // four threads for each
-        const uint32_t i = threadIdx.x / 4;
-        const uint64_t mine = i < n ? s.list[i] : 0;
-        uint32_t place = 0;
-#pragma unroll 4
-        for (uint32_t j = threadIdx.x & 3; j < n; j += 4) place += s.list[j] > mine ? 1u : 0u;
-        place = over_lanes<4>(place, [](uint32_t x, uint32_t y) { return x + y; });
-        if (i < n && (threadIdx.x & 3) == 0) s.sorted[place] = mine;
-    } else {
-        for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
-            const uint64_t mine = s.list[i];
-            uint32_t place = 0;
-#pragma unroll 8
-            for (uint32_t j = 0; j < n; ++j) place += s.list[j] > mine ? 1u : 0u;
-            s.sorted[place] = mine;
-        }
-    }
-    __syncthreads();
+    sort_list<T, THREADS>(n);
     if (threadIdx.x >= 64) return;
     const uint32_t each = (n + 63) / 64, first = threadIdx.x * each;                       // in their order: `each` of a lane
     uint64_t sum = 0;
@@ -1842,8 +1843,10 @@ void launch_sample_of(const SampleArgs& args, hipStream_t stream) {
         auto launch_waves = [&](auto room) {
             hipLaunchKernelGGL((sample_wave_kernel<T, decltype(room)::value>), dim3((here + kWaveRows - 1) / kWaveRows), dim3(64 * kWaveRows), 0, stream, a, r + here);
         };
+        // A wave for a row: 64 x 500, fp32, top_p, 11.1 us (a workgroup 23), 4000 x 500 18.6 (111).  Above, for many rows of which masses have to be made: 4000 x 2000, fp32, top_p, 47.6
+        // (53.8); but 1024 x 2000 24.7 (17.6), and 4000 x 2000, bf16, top_k, 54 (33).
         if (a.vocab <= 512) launch_waves(Int<512>());
-        else if (a.vocab <= 2048) launch_waves(Int<2048>());
+        else if (a.vocab <= 2048 && a.rows >= 2048 && a.top_k == 0 && !std::is_same_v<T, __bf16>) launch_waves(Int<2048>());
         else if (a.vocab * sizeof(T) <= 256 * 8 * 16) launch(Int<256>(), Int<8>(), Int<4>());
         else launch(Int<512>(), Int<16>(), Int<4>());
     }
