@@ -442,16 +442,29 @@ struct Kept {
         __syncthreads();
         return queued;
     }
-    // Gathers the logits from lo to hi as ranks; returns how many there are, or more than kList.
+    // Gathers logits as ranks, those from lo to hi or those of which is(logit) is true; returns how many there are, or more than kList.
     __device__ __forceinline__ uint32_t gather(float lo, float hi) const {
-        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
-        clear_queue();
-        auto test = [&](u32x4 raw) {
+        return gather_if([&](u32x4 raw) {
             float v[E];
             values(raw, v);
             return largest_of(v) >= lo;
-        };
-        auto is = [&](float v) { return v >= lo && v <= hi; };
+        }, [&](float v) { return v >= lo && v <= hi; });
+    }
+    template <typename F>
+    __device__ __forceinline__ uint32_t gather_those(F is) const {
+        return gather_if([&](u32x4 raw) {
+            float v[E];
+            values(raw, v);
+            bool some = false;
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) some |= is(v[e]);
+            return some;
+        }, is);
+    }
+    template <typename S, typename F>
+    __device__ __forceinline__ uint32_t gather_if(S test, F is) const {
+        SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+        clear_queue();
         auto add = [&](float v, uint32_t column) {
             const uint32_t place = atomicAdd(&s.held, 1u);
             if (place < kList) s.list[place] = logit_rank(v, column);
@@ -1116,6 +1129,85 @@ __device__ __forceinline__ uint64_t sum_before_bins() {
     return all;
 }
 
+// The bins that tell what is kept and which the token is, as far as bins tell: s.mass holds what lies before each, `all` in all; k_left: if > 0 the k-th logit lies in k_bin.
+struct Wanted {
+    uint32_t from, to, p_from, p_to, value, k;                    // of the token, of top_p (from > to: none), of min_p and top_k (~0: none)
+    uint64_t value_before;
+    __device__ __forceinline__ bool operator()(uint32_t bin) const {
+        return (bin >= from && bin <= to) || (bin >= p_from && bin <= p_to) || bin == value || bin == k;
+    }
+};
+template <typename T, int THREADS, typename B>
+__device__ __forceinline__ Wanted wanted_bins(const Asked& q, uint64_t all, double max, float least, uint32_t k_bin, uint32_t k_left, B bin_of) {
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+    auto end_of = [&](uint32_t bin) { return bin + 1 < kBins ? s.mass[bin + 1] : all; };
+    auto some = [](uint64_t v) { return v ? v : (uint64_t)1; };
+    uint64_t fewest = all, most = all;                            // what is kept lies between these two
+    Wanted w{0, 0, 1, 0, ~0u, ~0u, 0};
+    if (k_left) {
+        w.k = k_bin;
+        fewest = some(s.mass[k_bin]);
+        most = end_of(k_bin);
+    }
+    if (q.by_mass) {
+        w.p_from = bin_at_mass<T, THREADS>(q.share(fewest));
+        w.p_to = bin_at_mass<T, THREADS>(q.share(most));
+        fewest = some(s.mass[w.p_from]);
+        most = end_of(w.p_to);
+    }
+    if (q.by_value) {
+        const float at = (float)(max + q.border);
+        if (at >= least) {
+            w.value = bin_of(at);
+            w.value_before = s.mass[w.value];
+            const uint64_t before = some(w.value_before), end = end_of(w.value);
+            fewest = before < fewest ? before : fewest;
+            most = end < most ? end : most;
+        }
+    }
+    w.from = bin_at_mass<T, THREADS>(__umul64hi(q.u, fewest) + 1);
+    w.to = bin_at_mass<T, THREADS>(__umul64hi(q.u, most) + 1);
+    return w;
+}
+// Writes the answer out of a list of the n <= kList logits in the wanted bins (without top_k): put in order by the workgroup, the rest by its first wave.
+template <typename T, int THREADS, typename B>
+__device__ __forceinline__ void finish_from_bins(const SampleShape& shape, uint64_t row, const Row<T, THREADS>& r, const Asked& a, const Wanted& wanted, uint64_t all, uint32_t n, B bin_of) {
+    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+    sort_list<T, THREADS>(n);
+    if (threadIdx.x >= 64) return;
+    const uint32_t each = (n + 63) / 64, first = threadIdx.x * each;                       // in their order: `each` of a lane
+    auto value = [&](uint32_t i) { return of_key((uint32_t)(s.sorted[i] >> 32)); };
+    uint64_t sum = 0;
+    for (uint32_t i = first; i < first + each && i < n; ++i) {
+        sum += r.masses(value(i));
+        s.upto[i] = sum;
+    }
+    const uint64_t before = upto_lane(sum) - sum;
+    for (uint32_t i = first; i < first + each && i < n; ++i) s.upto[i] += before;
+    wave_sync();
+    // the list's sums leave out what lies between its bins: a bin's first logit puts that right, in the place of what lies before the bin
+    for (uint32_t i = first; i < first + each && i < n; ++i)
+        if (i == 0 || bin_of(value(i)) != bin_of(value(i - 1))) s.mass[bin_of(value(i))] -= i ? s.upto[i - 1] : 0;
+    wave_sync();
+    for (uint32_t i = first; i < first + each && i < n; ++i) s.upto[i] += s.mass[bin_of(value(i))];
+    wave_sync();
+    auto places = [&](auto f) {                                   // at which f is true, which are the first ones
+        uint32_t count = 0;
+        for (uint32_t i = 0; i < n; i += 64) count += (uint32_t)__popcll(__ballot(i + threadIdx.x < n && f(i + threadIdx.x)));
+        return count;
+    };
+    auto reached = [&](uint64_t t) { return places([&](uint32_t i) { return s.upto[i] < t; }); };
+    sum = all;
+    if (a.by_mass) sum = s.upto[reached(a.share(sum))];
+    if (wanted.value != ~0u) {
+        const uint32_t kept = places([&](uint32_t i) { return (double)value(i) - r.masses.max >= a.border; });
+        const uint64_t to = kept && bin_of(value(kept - 1)) == wanted.value ? s.upto[kept - 1] : wanted.value_before;
+        sum = to < sum ? to : sum;
+    }
+    const uint64_t token = s.sorted[reached(__umul64hi(a.u, sum) + 1)];
+    if (threadIdx.x == 0) write_answer(shape, row, a, r.masses, ~(uint32_t)token, of_key((uint32_t)(token >> 32)), sum);
+}
+
 // The mass that is kept, and s.index, out of bins and of lists of what lies in those that matter.  s.mass: what lies before each bin; sum: of the first top_k, or if k_left > 0 the
 // k_left-th logit from k_low to k_high, with `above` before them, is the last of these; gather(lo, hi) makes a list of the logits from lo to hi, none of them below `from`; bin(v),
 // low(bin), high(bin).  Returns 0 if a list is too short.
@@ -1160,30 +1252,32 @@ __device__ __forceinline__ uint64_t answer_by_bins(const Row<T, THREADS>& r, con
     return sum;
 }
 
-// Rows of any numbers between the fixed bins' ends: masses of four bins at a time.
+// Rows of any numbers between the fixed bins' ends, without top_k: masses of four bins at a time.  Returns false if the list is too short.
 template <typename T, int THREADS, int N>
-__device__ __forceinline__ uint64_t answer_by_masses(const Row<T, THREADS>& r, const Kept<T, THREADS, N>& kept, const Asked& a, float k_low, float k_high, uint32_t k_left) {
+__device__ __forceinline__ bool finish_by_masses(const SampleShape& shape, uint64_t row, const Row<T, THREADS>& r, const Kept<T, THREADS, N>& kept, const Asked& a) {
     SampleLds<THREADS>& s = sample_lds<T, THREADS>();
     static_assert(kBins * 4 == kFixedBins);
     const Bins bins = fixed_bins();
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < kBins; i += THREADS) s.mass[i] = 0;
     __syncthreads();
-    const float from = a.k && k_low > r.least ? k_low : r.least;
-    uint64_t above = 0;                                           // mass before the k-th logit's bin
     kept.of_all([&](float v) {
-        if (v >= from) {
-            const uint64_t mass = r.masses(v);
-            atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[(bins(v) - kFixedFirst) / 4]), (unsigned long long)mass);
-            if (a.k && v > k_high) above += mass;
-        }
+        if (v >= r.least) atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[(bins(v) - kFixedFirst) / 4]), (unsigned long long)r.masses(v));
     });
     __syncthreads();
-    const uint64_t sum = sum_before_bins<T, THREADS>();
-    if (a.k) (void)before_thread<THREADS>(above, s.sums, above);
-    return answer_by_bins(
-        r, a, sum, k_low, k_high, a.k ? k_left : 0, above, from, [&](float lo, float hi) { return kept.gather(lo, hi); }, [&](float v) { return (bins(v) - kFixedFirst) / 4; },
-        [&](uint32_t g) { return bins.lowest(kFixedFirst + 4 * g + 3); }, [&](uint32_t g) { return bins.highest(kFixedFirst + 4 * g); });
+    const uint64_t all = sum_before_bins<T, THREADS>();
+    auto bin_of = [&](float v) { return (bins(v) - kFixedFirst) / 4; };
+    const Wanted wanted = wanted_bins<T, THREADS>(a, all, r.masses.max, r.least, 0, 0, bin_of);
+    // as limits of logits: the token's bins, and those of top_p and of min_p
+    auto low = [&](uint32_t g) { return fmaxf(bins.lowest(kFixedFirst + 4 * g + 3), r.least); };
+    auto high = [&](uint32_t g) { return bins.highest(kFixedFirst + 4 * g); };
+    const float lo0 = low(wanted.to), hi0 = high(wanted.from), none = kInf;
+    const float lo1 = a.by_mass ? low(wanted.p_to) : none, hi1 = a.by_mass ? high(wanted.p_from) : -none;
+    const float lo2 = wanted.value != ~0u ? low(wanted.value) : none, hi2 = wanted.value != ~0u ? high(wanted.value) : -none;
+    const uint32_t n = kept.gather_those([&](float v) { return (v >= lo0 && v <= hi0) || (v >= lo1 && v <= hi1) || (v >= lo2 && v <= hi2); });
+    if (n > kList) return false;
+    finish_from_bins(shape, row, r, a, wanted, all, n, bin_of);
+    return true;
 }
 
 template <typename T, int THREADS, int N, int WAVES>
@@ -1310,10 +1404,8 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
             done = sum != 0;
         }
     if constexpr (!kNumbers && N <= 8)
-        if (!done && max < kFixedMost && r.least > -kFixedMost && (!asked.k || k_left)) {
-            sum = answer_by_masses(r, kept, asked, k_low, k_high, k_left);
-            done = sum != 0;
-        }
+        if (max < kFixedMost && r.least > -kFixedMost && !asked.k)
+            if (finish_by_masses(a, row, r, kept, asked)) return;
     if (!done) sum = answer_any(r, asked.temperature, asked.top_p, max, asked.k, asked.u, asked.border, k_low, k_high, k_left);
     if (threadIdx.x == 0) write_answer(a, row, asked, r.masses, s.index, (float)r.z[s.index], sum);
 }
@@ -1704,30 +1796,7 @@ __global__ void __launch_bounds__(kSplitThreads) sample_sift_kernel(SplitShape a
     }
     masses.put(s.mass);
     const uint64_t all = sum_before_bins<T, kSplitThreads>();
-    auto end_of = [&](uint32_t bin) { return bin + 1 < kBins ? s.mass[bin + 1] : all; };
-    // what is kept lies between these two, and what decides it in these bins
-    uint64_t fewest = all, most = all;
-    uint32_t p_from = 1, p_to = 0, value_bin = ~0u;
-    if (k_left) {
-        fewest = s.mass[k_bin] ? s.mass[k_bin] : 1;
-        most = end_of(k_bin);
-    }
-    if (q.by_mass) {
-        p_from = bin_at_mass<T, kSplitThreads>(q.share(fewest));
-        p_to = bin_at_mass<T, kSplitThreads>(q.share(most));
-        fewest = s.mass[p_from] ? s.mass[p_from] : 1;
-        most = end_of(p_to);
-    }
-    if (q.by_value) {
-        const float at = (float)(r.masses.max + q.border);
-        if (at >= r.least) {
-            value_bin = bins(at);
-            const uint64_t before = s.mass[value_bin] ? s.mass[value_bin] : 1, end = end_of(value_bin);
-            fewest = before < fewest ? before : fewest;
-            most = end < most ? end : most;
-        }
-    }
-    const uint32_t from = bin_at_mass<T, kSplitThreads>(__umul64hi(q.u, fewest) + 1), to = bin_at_mass<T, kSplitThreads>(__umul64hi(q.u, most) + 1);
+    const Wanted wanted = wanted_bins<T, kSplitThreads>(q, all, r.masses.max, r.least, k_bin, k_left, bins);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         w.k_bin = k_bin;
         w.k_left = k_left;
@@ -1741,8 +1810,7 @@ __global__ void __launch_bounds__(kSplitThreads) sample_sift_kernel(SplitShape a
 #pragma unroll
         for (uint32_t e = 0; e < E; ++e)
             if (v[e] >= r.least) {
-                const uint32_t bin = bins(v[e]);
-                if ((bin >= from && bin <= to) || (bin >= p_from && bin <= p_to) || bin == value_bin || (k_left && bin == k_bin)) {
+                if (wanted(bins(v[e]))) {
                     const uint32_t place = atomicAdd(&s.held, 1u);
                     if (place < kBins) s.mass[place] = logit_rank(v[e], begin + at + e);
                 }
@@ -1796,6 +1864,14 @@ __global__ void __launch_bounds__(kSplitThreads, 4) sample_split_kernel(SplitSha
         return s.held;
     };
     uint64_t sum = 0;
+    if (listed <= kList && !k_left) {
+        const Wanted wanted = wanted_bins<T, kSplitThreads>(q, all, r.masses.max, r.least, 0, 0, bins);
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i)
+            if (i * kSplitThreads + threadIdx.x < listed) s.list[i * kSplitThreads + threadIdx.x] = rank[i];
+        __syncthreads();
+        return finish_from_bins(a, row, r, q, wanted, all, listed, bins);
+    }
     if (listed <= kSplitRoom)
         sum = answer_by_bins(
             r, q, all, bins.lowest(k_bin), bins.highest(k_bin), k_left, s.mass[k_bin], r.least, gather, [&](float v) { return bins(v); }, [&](uint32_t g) { return bins.lowest(g); },
