@@ -247,11 +247,6 @@ __device__ __attribute__((noinline)) void find_nth(const T* z, uint32_t vocab, f
     __syncthreads();
 }
 
-template <int CTRL>
-__device__ __forceinline__ uint64_t other_lane64(uint64_t v) {
-    return (uint64_t)other_lane<CTRL>((uint32_t)(v >> 32)) << 32 | other_lane<CTRL>((uint32_t)v);
-}
-
 // A row of which the thread keeps N 16-byte pieces in registers between the passes; what does not fit comes from memory, or its caches, again, the last of it
 // first: it is the likeliest to be there.
 template <typename T, int THREADS, int N>
@@ -612,10 +607,18 @@ struct Row {
     template <typename F>
     __device__ __forceinline__ void sum_groups(F of) const {
         SampleLds<THREADS>& s = sample_lds<T, THREADS>();
+        constexpr uint32_t kOwn = kFixedBins / THREADS, kAtOnce = 16;
 #pragma unroll 1
-        for (uint32_t i = threadIdx.x; i < kFixedBins; i += THREADS) {
-            const uint32_t n = fixed_count(kFixedFirst + i);
-            if (n) atomicAdd(reinterpret_cast<unsigned long long*>(&s.group[i / 16]), (unsigned long long)of(kFixedFirst + i, n));
+        for (uint32_t from = 0; from < kOwn; from += kAtOnce) {
+            uint32_t n[kAtOnce];
+#pragma unroll
+            for (uint32_t i = 0; i < kAtOnce; ++i) n[i] = fixed_count(kFixedFirst + (from + i) * THREADS + threadIdx.x);
+#pragma unroll
+            for (uint32_t i = 0; i < kAtOnce; ++i)
+                if (n[i]) {
+                    const uint32_t at = (from + i) * THREADS + threadIdx.x;
+                    atomicAdd(reinterpret_cast<unsigned long long*>(&s.group[at / 16]), (unsigned long long)of(kFixedFirst + at, n[i]));
+                }
         }
         __syncthreads();
     }
@@ -1129,26 +1132,19 @@ __device__ __forceinline__ uint64_t sum_before_bins() {
     return all;
 }
 
-// The bins that tell what is kept and which the token is, as far as bins tell: s.mass holds what lies before each, `all` in all; k_left: if > 0 the k-th logit lies in k_bin.
+// The bins that tell what is kept and which the token is, as far as bins tell, without top_k: s.mass holds what lies before each, `all` in all.
 struct Wanted {
-    uint32_t from, to, p_from, p_to, value, k;                    // of the token, of top_p (from > to: none), of min_p and top_k (~0: none)
+    uint32_t from, to, p_from, p_to, value;                       // of the token, of top_p (from > to: none) and of min_p (~0: none)
     uint64_t value_before;
-    __device__ __forceinline__ bool operator()(uint32_t bin) const {
-        return (bin >= from && bin <= to) || (bin >= p_from && bin <= p_to) || bin == value || bin == k;
-    }
+    __device__ __forceinline__ bool operator()(uint32_t bin) const { return (bin >= from && bin <= to) || (bin >= p_from && bin <= p_to) || bin == value; }
 };
 template <typename T, int THREADS, typename B>
-__device__ __forceinline__ Wanted wanted_bins(const Asked& q, uint64_t all, double max, float least, uint32_t k_bin, uint32_t k_left, B bin_of) {
+__device__ __forceinline__ Wanted wanted_bins(const Asked& q, uint64_t all, double max, float least, B bin_of) {
     SampleLds<THREADS>& s = sample_lds<T, THREADS>();
     auto end_of = [&](uint32_t bin) { return bin + 1 < kBins ? s.mass[bin + 1] : all; };
     auto some = [](uint64_t v) { return v ? v : (uint64_t)1; };
     uint64_t fewest = all, most = all;                            // what is kept lies between these two
-    Wanted w{0, 0, 1, 0, ~0u, ~0u, 0};
-    if (k_left) {
-        w.k = k_bin;
-        fewest = some(s.mass[k_bin]);
-        most = end_of(k_bin);
-    }
+    Wanted w{0, 0, 1, 0, ~0u, 0};
     if (q.by_mass) {
         w.p_from = bin_at_mass<T, THREADS>(q.share(fewest));
         w.p_to = bin_at_mass<T, THREADS>(q.share(most));
@@ -1169,7 +1165,7 @@ __device__ __forceinline__ Wanted wanted_bins(const Asked& q, uint64_t all, doub
     w.to = bin_at_mass<T, THREADS>(__umul64hi(q.u, most) + 1);
     return w;
 }
-// Writes the answer out of a list of the n <= kList logits in the wanted bins (without top_k): put in order by the workgroup, the rest by its first wave.
+// Writes the answer out of a list of the n <= kList logits in the wanted bins: put in order by the workgroup, the rest by its first wave.
 template <typename T, int THREADS, typename B>
 __device__ __forceinline__ void finish_from_bins(const SampleShape& shape, uint64_t row, const Row<T, THREADS>& r, const Asked& a, const Wanted& wanted, uint64_t all, uint32_t n, B bin_of) {
     SampleLds<THREADS>& s = sample_lds<T, THREADS>();
@@ -1208,50 +1204,6 @@ __device__ __forceinline__ void finish_from_bins(const SampleShape& shape, uint6
     if (threadIdx.x == 0) write_answer(shape, row, a, r.masses, ~(uint32_t)token, of_key((uint32_t)(token >> 32)), sum);
 }
 
-// The mass that is kept, and s.index, out of bins and of lists of what lies in those that matter.  s.mass: what lies before each bin; sum: of the first top_k, or if k_left > 0 the
-// k_left-th logit from k_low to k_high, with `above` before them, is the last of these; gather(lo, hi) makes a list of the logits from lo to hi, none of them below `from`; bin(v),
-// low(bin), high(bin).  Returns 0 if a list is too short.
-template <typename T, int THREADS, typename G, typename B, typename L, typename H>
-__device__ __forceinline__ uint64_t answer_by_bins(const Row<T, THREADS>& r, const Asked& a, uint64_t sum, float k_low, float k_high, uint32_t k_left, uint64_t above, float from, G gather, B bin,
-                                                   L low, H high) {
-    SampleLds<THREADS>& s = sample_lds<T, THREADS>();
-    uint32_t loaded = ~0u, n = 0;
-    uint64_t ahead = 0;
-    auto load = [&](uint32_t g) {
-        if (g == loaded) return;
-        loaded = g;
-        ahead = s.mass[g];
-        n = gather(low(g) > from ? low(g) : from, high(g));
-        if (n && n <= kList) r.settle(n, ahead);
-    };
-    if (k_left) {
-        n = gather(k_low > from ? k_low : from, k_high);
-        if (n > kList) return 0;
-        if (n) r.settle(n, above);
-        sum = n ? s.upto[k_left < n ? k_left - 1 : n - 1] : above;
-    }
-    for (int step = 1; step < 4; ++step) {                        // top_p, min_p, the token
-        if ((step == 1 && !a.by_mass) || (step == 2 && !a.by_value)) continue;
-        const uint64_t t = step == 1 ? a.share(sum) : __umul64hi(a.u, sum) + 1;
-        if (step == 2) {
-            const float at = (float)(r.masses.max + a.border);
-            if (at < from) continue;
-            load(bin(at));
-        } else {
-            load(bin_at_mass<T, THREADS>(t));
-        }
-        if (n > kList) return 0;
-        if (step == 2) {
-            const uint64_t to = n ? r.list_value(n, ahead, a.border) : ahead;
-            sum = to < sum ? to : sum;
-        } else {
-            const uint64_t to = r.list_mass(n, ahead, t);
-            if (step == 1) sum = to;
-        }
-    }
-    return sum;
-}
-
 // Rows of any numbers between the fixed bins' ends, without top_k: masses of four bins at a time.  Returns false if the list is too short.
 template <typename T, int THREADS, int N>
 __device__ __forceinline__ bool finish_by_masses(const SampleShape& shape, uint64_t row, const Row<T, THREADS>& r, const Kept<T, THREADS, N>& kept, const Asked& a) {
@@ -1267,7 +1219,7 @@ __device__ __forceinline__ bool finish_by_masses(const SampleShape& shape, uint6
     __syncthreads();
     const uint64_t all = sum_before_bins<T, THREADS>();
     auto bin_of = [&](float v) { return (bins(v) - kFixedFirst) / 4; };
-    const Wanted wanted = wanted_bins<T, THREADS>(a, all, r.masses.max, r.least, 0, 0, bin_of);
+    const Wanted wanted = wanted_bins<T, THREADS>(a, all, r.masses.max, r.least, bin_of);
     // as limits of logits: the token's bins, and those of top_p and of min_p
     auto low = [&](uint32_t g) { return fmaxf(bins.lowest(kFixedFirst + 4 * g + 3), r.least); };
     auto high = [&](uint32_t g) { return bins.highest(kFixedFirst + 4 * g); };
@@ -1290,7 +1242,7 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
     Asked asked = asked_of(a, row);
     if (threadIdx.x == 0) s.index = 0;
     // the largest, and how many logits are in each of the fixed bins
-    const bool few = r.vocab <= kList, counted = !few && (kNumbers || asked.k);
+    const bool counted = kNumbers || asked.k;
     float max = -kInf;
     bool known = !counted || !kNumbers;                           // max is the largest, or will be
     uint32_t first = 0;                                           // counted: the bin of the largest
@@ -1331,9 +1283,9 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
     }
     ask(a, max, u_given, min_p, asked, r.masses, r.least);
     const bool fixed = counted && max < kFixedMost && r.least > -kFixedMost;
-    bool listed = few;                                            // everything that matters lies above r.least, and the list has room for it
-    if (asked.by_value && !asked.by_mass && !few) {               // no other filter needs what this one leaves out
-        const float at = (float)((double)max + asked.border), below = at - fabsf(at) * 0x1p-20f;
+    bool listed = false;                                          // everything that matters lies above r.least, and the list has room for it
+    if (asked.by_value && !asked.by_mass) {                       // no other filter needs what this one leaves out
+        const float at = (float)((double)max + asked.border), below = at - (fabsf(at) + fabsf(max)) * 0x1p-20f;
         if (below > r.least) r.least = below;
     }
     float k_low = 0.f, k_high = 0.f;
@@ -1663,15 +1615,14 @@ __global__ void __launch_bounds__(64 * kWaveRows) sample_wave_kernel(SampleShape
     if (lane == 0) write_answer(a, row, q, masses, index, value, sum);
 }
 
-// Few long rows are split over workgroups, in four launches: the largest of each part; masses (and counts, for top_k) in bins of the row, added up in memory; which bins matter, as
-// far as they tell, and the logits in them into a list of the row; the answer out of bins and list.
-constexpr uint32_t kSplitThreads = 256, kSplitRoom = 2048;        // room: of a row's list
+// Few long rows are split over workgroups, in four launches: the largest of each part; masses in bins of the row, added up in memory; which bins matter, as far as they tell, and the
+// logits in them into a list of the row; the answer out of bins and list.  A row with a top_k after all (of its own), or with a list too long, is the last launch's alone.
+constexpr uint32_t kSplitThreads = 256;
 struct SplitRow {
     uint64_t mass[kBins];
-    uint64_t list[kSplitRoom];
-    uint32_t count[kBins];
+    uint64_t list[kList];
     float most[64];                                               // of parts
-    uint32_t held, k_bin, k_left, unused;
+    uint32_t held, unused[3];
 };
 struct SplitShape : SampleShape {
     SplitRow* rows_of;
@@ -1717,10 +1668,7 @@ __global__ void __launch_bounds__(kSplitThreads) sample_most_kernel(SplitShape a
     __shared__ float most[kSplitThreads / 64];
     SplitRow& w = a.rows_of[blockIdx.y];
     const auto r = part_of<T>(a);
-    for (uint32_t i = blockIdx.x * kSplitThreads + threadIdx.x; i < kBins; i += gridDim.x * kSplitThreads) {
-        w.mass[i] = 0;
-        w.count[i] = 0;
-    }
+    for (uint32_t i = blockIdx.x * kSplitThreads + threadIdx.x; i < kBins; i += gridDim.x * kSplitThreads) w.mass[i] = 0;
     float max = -kInf;
     r.stream([&](const float(&v)[E], uint32_t) { max = max_or_nan(max, largest_of(v)); });
     max = over_lanes<64>(max, [](float x, float y) { return max_or_nan(x, y); });
@@ -1736,12 +1684,8 @@ template <typename T>
 __global__ void __launch_bounds__(kSplitThreads) sample_bins_kernel(SplitShape a) {
     constexpr uint32_t E = Pieces<T>::E;
     __shared__ uint64_t mass[kBins];
-    __shared__ uint32_t count[kBins];
     SplitRow& w = a.rows_of[blockIdx.y];
-    for (uint32_t i = threadIdx.x; i < kBins; i += kSplitThreads) {
-        mass[i] = 0;
-        count[i] = 0;
-    }
+    for (uint32_t i = threadIdx.x; i < kBins; i += kSplitThreads) mass[i] = 0;
     const float max = split_largest(a, w);
     if (max != max || max == -kInf) return;
     auto r = part_of<T>(a);
@@ -1752,17 +1696,11 @@ __global__ void __launch_bounds__(kSplitThreads) sample_bins_kernel(SplitShape a
     r.stream([&](const float(&v)[E], uint32_t) {
 #pragma unroll
         for (uint32_t e = 0; e < E; ++e)
-            if (v[e] >= r.least) {
-                const uint32_t bin = bins(v[e]);
-                atomicAdd(reinterpret_cast<unsigned long long*>(&mass[bin]), (unsigned long long)r.masses(v[e]));
-                if (q.k) atomicAdd(&count[bin], 1u);
-            }
+            if (v[e] >= r.least) atomicAdd(reinterpret_cast<unsigned long long*>(&mass[bins(v[e])]), (unsigned long long)r.masses(v[e]));
     });
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < kBins; i += kSplitThreads) {
+    for (uint32_t i = threadIdx.x; i < kBins; i += kSplitThreads)
         if (mass[i]) atomicAdd(reinterpret_cast<unsigned long long*>(&w.mass[i]), (unsigned long long)mass[i]);
-        if (count[i]) atomicAdd(&w.count[i], count[i]);
-    }
 }
 
 template <typename T>
@@ -1777,30 +1715,9 @@ __global__ void __launch_bounds__(kSplitThreads) sample_sift_kernel(SplitShape a
     Asked q;
     split_ask<T>(a, max, q, r.masses, r.least);
     const Bins bins = bins_of(max, q.temperature);
-    uint32_t k_bin = 0, k_left = 0;
-    if (q.k) {
-        uint32_t* const count = reinterpret_cast<uint32_t*>(s.queue);
-        uint32_t own = 0, all;
-        for (uint32_t i = threadIdx.x; i < kBins; i += kSplitThreads) count[i] = w.count[i];
-        __syncthreads();
-        constexpr uint32_t kOwn = kBins / kSplitThreads;
-#pragma unroll
-        for (uint32_t i = 0; i < kOwn; ++i) own += count[threadIdx.x * kOwn + i];
-        const uint32_t before = before_thread<kSplitThreads>(own, s.counts, all);
-        if (q.k >= all) q.k = 0;
-        if (q.k) {
-            find_kth<T, kSplitThreads>(q.k, before, own, threadIdx.x * kOwn, [&](uint32_t i) { return count[i]; });
-            k_bin = s.bin;
-            k_left = q.k - s.ahead;
-        }
-    }
     masses.put(s.mass);
     const uint64_t all = sum_before_bins<T, kSplitThreads>();
-    const Wanted wanted = wanted_bins<T, kSplitThreads>(q, all, r.masses.max, r.least, k_bin, k_left, bins);
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        w.k_bin = k_bin;
-        w.k_left = k_left;
-    }
+    const Wanted wanted = wanted_bins<T, kSplitThreads>(q, all, r.masses.max, r.least, bins);
     // the part's into LDS, where masses are done with, and then with one request for places into the row's
     __syncthreads();
     if (threadIdx.x == 0) s.held = 0;
@@ -1822,7 +1739,7 @@ __global__ void __launch_bounds__(kSplitThreads) sample_sift_kernel(SplitShape a
     if (threadIdx.x == 0) s.ahead = atomicAdd(&w.held, held);
     __syncthreads();
     const uint32_t first = s.ahead;
-    for (uint32_t i = threadIdx.x; i < held && i < kBins && first + i < kSplitRoom; i += kSplitThreads) w.list[first + i] = s.mass[i];
+    for (uint32_t i = threadIdx.x; i < held && i < kBins && first + i < kList; i += kSplitThreads) w.list[first + i] = s.mass[i];
 }
 
 template <typename T>
@@ -1831,11 +1748,11 @@ __global__ void __launch_bounds__(kSplitThreads, 4) sample_split_kernel(SplitSha
     SplitRow& w = a.rows_of[blockIdx.y];
     const uint64_t row = a.row0 + blockIdx.y;
     const SplitMasses masses(w);
-    constexpr uint32_t kEach = kSplitRoom / kSplitThreads;
+    constexpr uint32_t kEach = kList / kSplitThreads;
     uint64_t rank[kEach];                                         // the thread's part of the list
 #pragma unroll
     for (uint32_t i = 0; i < kEach; ++i) rank[i] = w.list[i * kSplitThreads + threadIdx.x];
-    const uint32_t listed = w.held, k_bin = w.k_bin, k_left = w.k_left;
+    const uint32_t listed = w.held;
     const float max = split_largest(a, w);
     if (max != max || max == -kInf) {
         if (threadIdx.x == 0) no_answer(a, row, max);
@@ -1844,48 +1761,29 @@ __global__ void __launch_bounds__(kSplitThreads, 4) sample_split_kernel(SplitSha
     Row<T, kSplitThreads> r{static_cast<const T*>(a.z) + row * a.z_ld, (uint32_t)a.vocab, {}, 0.f};
     Asked q;
     split_ask<T>(a, max, q, r.masses, r.least);
+    if (q.k || listed > kList) {
+        if (threadIdx.x == 0) s.index = 0;
+        const uint64_t sum = answer_any(r, q.temperature, q.top_p, max, q.k, q.u, q.border, 0.f, 0.f, 0u);
+        if (threadIdx.x == 0) write_answer(a, row, q, r.masses, s.index, (float)r.z[s.index], sum);
+        return;
+    }
     const Bins bins = bins_of(max, q.temperature);
-    if (threadIdx.x == 0) s.index = 0;
     masses.put(s.mass);
     const uint64_t all = sum_before_bins<T, kSplitThreads>();
-    auto gather = [&](float lo, float hi) {
-        __syncthreads();
-        if (threadIdx.x == 0) s.held = 0;
-        __syncthreads();
+    const Wanted wanted = wanted_bins<T, kSplitThreads>(q, all, r.masses.max, r.least, bins);
 #pragma unroll
-        for (uint32_t i = 0; i < kEach; ++i) {
-            const float v = of_key((uint32_t)(rank[i] >> 32));
-            if (i * kSplitThreads + threadIdx.x < listed && v >= lo && v <= hi) {
-                const uint32_t place = atomicAdd(&s.held, 1u);
-                if (place < kList) s.list[place] = rank[i];
-            }
-        }
-        __syncthreads();
-        return s.held;
-    };
-    uint64_t sum = 0;
-    if (listed <= kList && !k_left) {
-        const Wanted wanted = wanted_bins<T, kSplitThreads>(q, all, r.masses.max, r.least, 0, 0, bins);
-#pragma unroll
-        for (uint32_t i = 0; i < kEach; ++i)
-            if (i * kSplitThreads + threadIdx.x < listed) s.list[i * kSplitThreads + threadIdx.x] = rank[i];
-        __syncthreads();
-        return finish_from_bins(a, row, r, q, wanted, all, listed, bins);
-    }
-    if (listed <= kSplitRoom)
-        sum = answer_by_bins(
-            r, q, all, bins.lowest(k_bin), bins.highest(k_bin), k_left, s.mass[k_bin], r.least, gather, [&](float v) { return bins(v); }, [&](uint32_t g) { return bins.lowest(g); },
-            [&](uint32_t g) { return bins.highest(g); });
-    if (!sum) sum = answer_any(r, q.temperature, q.top_p, max, q.k, q.u, q.border, 0.f, 0.f, 0u);
-    if (threadIdx.x == 0) write_answer(a, row, q, r.masses, s.index, (float)r.z[s.index], sum);
+    for (uint32_t i = 0; i < kEach; ++i)
+        if (i * kSplitThreads + threadIdx.x < listed) s.list[i * kSplitThreads + threadIdx.x] = rank[i];
+    __syncthreads();
+    finish_from_bins(a, row, r, q, wanted, all, listed, bins);
 }
 
 // Workgroups of a row, 1 for none.  Of bf16, and where top_k or min_p alone leave little, a workgroup by itself reads a row twice at most: 1 x 131072, bf16, top_p, 22 us,
 // split 30; 4 x 131072, fp32, min_p, 14.5 and 24.6.  Otherwise it reads it four times and makes masses of all of it: 1 x 131072, fp32, top_p, 88 us, split 25; 32 x 40000 42 and 34; 4 x 20000 25 and 28.
 uint32_t sample_parts(const ds_sampling& l) {
     const uint64_t size = l.dtype == DS_F32 ? 4 : 2, bytes = l.vocab * size;
-    const bool few_left = l.dtype == DS_BF16 || l.top_k > 0 || (l.min_p > 0.f && l.top_p >= 1.f);
-    if (l.rows > 32 || bytes < (few_left ? 1u << 20 : 1u << 17)) return 1;
+    const bool few_left = l.dtype == DS_BF16 || (l.min_p > 0.f && l.top_p >= 1.f);
+    if (l.top_k > 0 || l.rows > 32 || bytes < (few_left ? 1u << 20 : 1u << 17)) return 1;
     const uint64_t p = (bytes + 16383) / 16384;
     return (uint32_t)(p < 64 ? p : 64);
 }
@@ -1919,10 +1817,11 @@ void launch_sample_of(const SampleArgs& args, hipStream_t stream) {
         auto launch_waves = [&](auto room) {
             hipLaunchKernelGGL((sample_wave_kernel<T, decltype(room)::value>), dim3((here + kWaveRows - 1) / kWaveRows), dim3(64 * kWaveRows), 0, stream, a, r + here);
         };
+        constexpr bool kWaves = !std::is_same_v<T, __bf16>;
         // A wave for a row: 64 x 500, fp32, top_p, 11.1 us (a workgroup 23), 4000 x 500 18.6 (111).  Above, for many rows of which masses have to be made: 4000 x 2000, fp32, top_p, 47.6
         // (53.8); but 1024 x 2000 24.7 (17.6), and 4000 x 2000, bf16, top_k, 54 (33).
         if (a.vocab <= 512) launch_waves(Int<512>());
-        else if (a.vocab <= 2048 && a.rows >= 2048 && a.top_k == 0 && !std::is_same_v<T, __bf16>) launch_waves(Int<2048>());
+        else if (kWaves && a.vocab <= 2048 && a.rows >= 2048 && a.top_k == 0) launch_waves(Int<kWaves ? 2048 : 512>());
         else if (a.vocab * sizeof(T) <= 256 * 8 * 16) launch(Int<256>(), Int<8>(), Int<4>());
         else launch(Int<512>(), Int<16>(), Int<4>());
     }

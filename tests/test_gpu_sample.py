@@ -219,6 +219,40 @@ def test_no_rows_and_results_without_logp():
     assert torch.equal(token[:3], b.ds_sample(z, u)[0]) and (token[3:] == 77).all()
 
 
+def test_rows_with_a_top_k_that_the_shape_does_not_tell_of():
+    """top_k_dev beside top_k = 0 in C: right all the same."""
+    import ctypes
+    for dtype, vocab in ((F32, 40000), (F16, 70000), (BF16, 5000)):
+        z, u, k = normal(4, vocab, dtype, seed=27), uniform(4, 7), torch.tensor([0, 3, 700, 50], dtype=torch.int32)
+        own, uc, kc = z.cuda(), u.cuda(), k.cuda()
+        shape = b.ds_sampling(4, vocab, {F32: 0, BF16: 1, F16: 2}[dtype], 0, 1.0, 0.9, 0.0, 0)
+        each = b.ds_sampling_rows(None, kc.data_ptr(), None, None)
+        size = b.lib().ds_sample_work_bytes(ctypes.byref(shape))
+        work = torch.empty(max(size, 16), dtype=torch.uint8, device="cuda")
+        token, logp = torch.empty(4, dtype=torch.int32, device="cuda"), torch.empty(4, device="cuda")
+        assert b.lib().ds_sample(ctypes.byref(shape), ctypes.byref(each), own.data_ptr(), vocab, uc.data_ptr(), token.data_ptr(), logp.data_ptr(), work.data_ptr(),
+                                 size, torch.cuda.current_stream().cuda_stream, None, 0) == b.DS_OK
+        same((token, logp), plain.sample(z, u, top_k=k, top_p=0.9), vocab)
+
+
+SPLIT = [(1, 131072, F32), (3, 65536, F16), (32, 33001, F32), (2, 600001, BF16)]
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", SPLIT)
+def test_rows_that_are_split(rows, vocab, dtype):
+    z, u = normal(rows, vocab, dtype, seed=28), uniform(rows, 9)
+    for f in (dict(), dict(top_p=0.9), dict(top_p=0.999, min_p=1e-4), dict(temperature=0.3, top_p=0.5), dict(temperature=40.0), dict(min_p=0.9, top_p=0.99)):
+        check(z, u, **f)
+    z[0] = -INF
+    if rows > 1:
+        z[1, vocab // 3] = NAN
+    if rows > 2:
+        z[2, 5] = z[2, vocab - 1] = INF
+    check(z, u, top_p=0.9)
+    check(torch.full_like(z, 0.5), u, top_p=0.7)                                  # more ties than lists have room for
+    check(torch.round(normal(rows, vocab, dtype, seed=29)), u, top_p=0.8)
+
+
 @pytest.mark.parametrize("rows,vocab", [(3, 300), (2, 40000), (1, 131072)])
 def test_a_captured_call_draws_from_what_it_finds(rows, vocab):
     z, u = torch.zeros((rows, vocab), dtype=BF16, device="cuda"), torch.zeros(rows, device="cuda")
