@@ -314,7 +314,7 @@ def _answer(name: str, work_bytes, call, shape, given, here: int, stream, *args)
         _refuse(name, "stream must be of the current CUDA device")
     else:
         pointer = stream.cuda_stream
-    size = work_bytes(shape)
+    size = work_bytes if type(work_bytes) is int else work_bytes(shape)
     work = _new(stream, (size,), torch.uint8, given[0]) if size else None
     at = work.data_ptr() if size else None
     st = call(shape, *args, at, size, pointer, None, 0)
@@ -328,6 +328,7 @@ def _answer(name: str, work_bytes, call, shape, given, here: int, stream, *args)
                 t.record_stream(stream)
     if st != DS_OK:
         raise DsqError(st, name)
+    return pointer
 
 
 def ds_matrix_bytes(rows: int, cols: int, block: int) -> int:
@@ -431,7 +432,7 @@ def ds_sample(z: "torch.Tensor", u: "torch.Tensor", temperature=1.0, top_k=0, to
         if not isinstance(value, torch.Tensor):
             if name == "top_k" and not (isinstance(value, (int, np.integer)) and 0 <= value < 1 << 31):
                 _refuse("ds_sample", "top_k must be a whole number of at least 0 and below 2^31")
-            setattr(s, name, value)
+            setattr(s, name, int(value) if name == "top_k" else float(value))
             continue
         if value.dtype != dtype or value.dim() != 1 or value.shape[0] != rows or not value.is_contiguous():
             _refuse("ds_sample", f"{name} must be a number or a contiguous vector of {rows}, {dtype}")
@@ -485,7 +486,10 @@ class Gradients:
                                 _stream_pointer(None), buf, 256)
         if st != DS_OK:
             raise DsqError(st, "Gradients", buf.value.decode())
-        torch.cuda.current_stream().synchronize()
+        made_on = torch.cuda.current_stream()
+        made_on.synchronize()
+        self._made_on = made_on.cuda_stream
+        self._work = int(L.ds_gradient_norm_work_bytes(ctypes.byref(self._g))), int(L.ds_clip_work_bytes(ctypes.byref(self._g)))
         self.columns = int(self._g.columns)
         some = sizes > 0
         self._lo = listed["data"][some]
@@ -498,9 +502,17 @@ class Gradients:
         self._apart = bool(np.all(self._hi[order][:-1] <= self._lo[order][1:]))
         self._span = (int(self._lo.min()), int(self._hi.max())) if some.any() else (0, 0)
 
-    def _overlapped(self, out: "torch.Tensor", pitch: int) -> bool:
-        """A tensor lies in out, and not where its elements go."""
-        lo = out.data_ptr()
+    def _lent(self, pointer: int, stream: Optional["torch.cuda.Stream"]):
+        """The memory of table and tensors, freed by the stream it is of, must wait for another one that a call ran on."""
+        if pointer == self._made_on:
+            return
+        if stream is None:
+            stream = torch.cuda.current_stream()
+        for t in (self.table, *self.tensors):
+            t.record_stream(stream)
+
+    def _overlapped(self, lo: int, pitch: int) -> bool:
+        """A tensor lies in the rows of this pitch from address lo on, and not where its elements go."""
         hi = lo + 4 * ((self.workers - 1) * pitch + self.columns)
         if hi <= self._span[0] or self._span[1] <= lo:
             return False
@@ -508,49 +520,41 @@ class Gradients:
         return bool(np.any((self._lo < hi) & (self._hi > lo) & ~(self._f32 & (self._lo == there))))
 
 
-def _gradients(name: str, grads) -> Gradients:
-    grads = grads if isinstance(grads, Gradients) else Gradients(grads)
-    if torch.cuda.current_device() != grads.device:
-        _refuse(name, "the gradients must be on the current CUDA device")
-    return grads
-
-
 def ds_gradient_norm(grads, stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
     """The Euclidean norm of each worker's gradient over all its tensors: float32 (workers,).  grads: Gradients, or what they are made of
     (then they are laid out for this call, which waits for it)."""
-    g = _gradients("ds_gradient_norm", grads)
+    g, L = grads if type(grads) is Gradients else Gradients(grads), lib()
+    here = _on_device("ds_gradient_norm", "gradients", g.table)
     norm = _new(stream, (g.workers,), torch.float32, g.table)
-    L = lib()
-    _answer("ds_gradient_norm", L.ds_gradient_norm_work_bytes, L.ds_gradient_norm, ctypes.byref(g._g), (g.table,) if stream is None else (g.table, *g.tensors),
-            g.device, stream, norm.data_ptr())
+    pointer = _answer("ds_gradient_norm", g._work[0], L.ds_gradient_norm, ctypes.byref(g._g), (g.table,), here, stream, norm.data_ptr())
+    g._lent(pointer, stream)
     return norm
 
 
 def ds_clip(grads, max_norm: float, out: "Optional[torch.Tensor]" = None, stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
     """Scales the gradients of workers whose norm is above max_norm to it, and returns the norms before: float32 (workers,).  With out, float32 (workers,
     >= columns), what ds_step takes: written there, each worker's tensors one behind the other, nothing behind them; otherwise in place.  A
-    gradient that is not finite becomes zeros."""
-    g = _gradients("ds_clip", grads)
+    gradient that is not finite becomes zeros.  Autograd records neither."""
+    g, L = grads if type(grads) is Gradients else Gradients(grads), lib()
+    here = _on_device("ds_clip", "gradients out", g.table, out)
     at, pitch = None, 0
     if out is not None:
-        _on_device("ds_clip", "out", out)
-        if out.dtype != torch.float32 or out.dim() != 2 or out.shape[0] != g.workers or out.shape[1] < g.columns:
+        rows, cols, pitch = _rows_of("ds_clip", "out", out)
+        if out.dtype != torch.float32 or rows != g.workers or cols < g.columns:
             _refuse("ds_clip", f"out must be float32 ({g.workers}, at least {g.columns})")
         if out.requires_grad and torch.is_grad_enabled():
             _refuse("ds_clip", "out requires a gradient, which the call does not record")
-        _, cols, pitch = _rows_of("ds_clip", "out", out)
-        if g.workers > 1 and pitch < cols:
+        if rows > 1 and pitch < cols:
             _refuse("ds_clip", "the rows of out must not overlap")
         at = out.data_ptr()
-        if g.columns and g._overlapped(out, pitch):
+        if g.columns and g._overlapped(at, pitch):
             _refuse("ds_clip", "out overlaps a gradient that does not lie where it goes")
         at = at or None
     elif not g._apart:
         _refuse("ds_clip", "tensors that overlap cannot be scaled in place")
     norm = _new(stream, (g.workers,), torch.float32, g.table)
-    L = lib()
-    _answer("ds_clip", L.ds_clip_work_bytes, L.ds_clip, ctypes.byref(g._g), (g.table, out) if stream is None else (g.table, out, *g.tensors), g.device, stream,
-            max_norm, at, pitch, norm.data_ptr())
+    pointer = _answer("ds_clip", g._work[1], L.ds_clip, ctypes.byref(g._g), (g.table, out), here, stream, max_norm, at, pitch, norm.data_ptr())
+    g._lent(pointer, stream)
     return norm
 
 

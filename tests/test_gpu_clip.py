@@ -159,7 +159,7 @@ def test_gradients_that_lie_in_the_result():
 def test_results_that_are_refused():
     g = b.Gradients([torch.ones(10, device="cuda"), torch.ones(3, device="cuda", dtype=F16)])
     for out in (torch.empty((1, 12), device="cuda"), torch.empty((2, 13), device="cuda"), torch.empty(13, device="cuda"),
-                torch.empty((1, 13), device="cuda", dtype=BF16)):
+                torch.empty((1, 13), device="cuda", dtype=BF16), torch.empty((1, 13), device="cuda", dtype=torch.float64)):
         with pytest.raises(b.DsqError, match="out must"):
             b.ds_clip(g, 1.0, out=out)
     with pytest.raises(b.DsqError, match="out must be on"):
@@ -225,6 +225,24 @@ def test_calls_on_another_stream_and_memory_freed_meanwhile():
         torch.full((1 << 22,), 9.0, device="cuda")                                # may take its place
         s.synchronize()
         assert float(norm) == 2048.0 and torch.equal(out, want)
+
+
+def test_a_table_that_another_current_stream_uses_and_that_is_freed_meanwhile():
+    s = torch.cuda.Stream()
+    for _ in range(10):
+        x = [torch.ones(1 << 18, device="cuda") for _ in range(8)]
+        g = b.Gradients(x)
+        out = torch.empty((1, 1 << 21), device="cuda")
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            norm = b.ds_clip(g, 1.0, out=out)
+            alone = b.ds_gradient_norm(g)
+        size = g.table.numel()
+        del x, g
+        [torch.full((1 << 18,), 9.0, device="cuda") for _ in range(8)], torch.full((size,), 255, dtype=torch.uint8, device="cuda")     # may take their places
+        s.synchronize()
+        want = math.sqrt(2.0 ** 21)
+        assert abs(float(norm) - want) < 1e-3 and float(alone) == float(norm) and float((out - 1.0 / want).abs().max()) <= 2.0 ** -24 / want
 
 
 def test_more_than_four_gigabytes_in_a_tensor():

@@ -127,9 +127,9 @@ def laid(sizes, at, pitch=None):
 def test_results_over_gradients():
     out = torch.zeros((2, 12))
     at = out.data_ptr()
-    assert not laid([10, 10], [at, at + 48])._overlapped(out, 12)                 # where they go
-    assert laid([10, 10], [at, at + 40])._overlapped(out, 12)
-    assert laid([10, 10], [at + 4, BIG])._overlapped(out, 12)
-    assert not laid([10, 10], [at - 40, at + 4 * 22])._overlapped(out, 12)        # before it, and behind the last row's elements
-    assert laid([10, 10], [at - 36, BIG])._overlapped(out, 12)
-    assert laid([10, 10], [at + 48, at])._overlapped(out, 12)                     # the wrong rows
+    assert not laid([10, 10], [at, at + 48])._overlapped(at, 12)                  # where they go
+    assert laid([10, 10], [at, at + 40])._overlapped(at, 12)
+    assert laid([10, 10], [at + 4, BIG])._overlapped(at, 12)
+    assert not laid([10, 10], [at - 40, at + 4 * 22])._overlapped(at, 12)         # before it, and behind the last row's elements
+    assert laid([10, 10], [at - 36, BIG])._overlapped(at, 12)
+    assert laid([10, 10], [at + 48, at])._overlapped(at, 12)                      # the wrong rows
