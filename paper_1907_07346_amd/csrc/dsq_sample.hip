@@ -147,6 +147,16 @@ __device__ __forceinline__ SampleLds<THREADS>& sample_lds() {
     return s;
 }
 
+// a's low (or high) 16 bits times b's, as signed numbers, and c.
+template <bool A_HIGH, bool B_HIGH>
+__device__ __forceinline__ uint32_t multiply_add_16(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    if constexpr (A_HIGH && B_HIGH) asm("v_mad_i32_i16 %0, %1, %2, %3 op_sel:[1,1,0,0]" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    else if constexpr (A_HIGH) asm("v_mad_i32_i16 %0, %1, %2, %3 op_sel:[1,0,0,0]" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    else asm("v_mad_i32_i16 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
+}
+
 // The sum of the lanes up to the own one, by register permutations: one, two, four and eight lanes on in sixteen, then a sixteen's last to the next one's, and that of 32
 // to the rest.
 template <int CTRL, int ROWS, typename V>
@@ -318,35 +328,31 @@ struct Kept {
         }
         return max;
     }
-    // Counts logits in fixed bins.  Returns the thread's largest one; of bf16, whose bins tell it, the first bin in which it counted one, and whether it met a NaN.
+    // Counts logits in fixed bins.  Returns the thread's largest one; of bf16, whose bins tell it, whether it met a NaN.
     struct Counted {
         float max;
-        uint32_t first;
         bool nan;
     };
     __device__ __forceinline__ Counted count_fixed() const {
         SampleLds<THREADS>& s = sample_lds<T, THREADS>();
         auto add = [&](uint32_t place) { atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.count) + place), 1u); };
-        const uint32_t most = kFixedSide + (threadIdx.x & 63);
+        const uint32_t most = kFixedSide + (threadIdx.x & 63), top = 4 * kFixedTop;        // (places are in bytes)
         typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-        typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
-        u16x2 magnitudes = 0, places = (uint16_t)0xFFFF;
+        u16x2 magnitudes = 0;
         float max = -kInf;
+        const float least_magnitude = __uint_as_float((uint32_t)kFixedBase << 16), most_magnitude = __uint_as_float((kFixedBase + most) << 16);
         auto f = [&](u32x4 raw) {
             if constexpr (kNumbers) {                             // two at a time
-                const u16x2 base = (uint16_t)kFixedBase, side = (uint16_t)most, top = (uint16_t)(4 * kFixedTop);
+                const u16x2 base = (uint16_t)kFixedBase, side = (uint16_t)most;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint32_t bits = raw[i];                 // (a cast of the element itself would be one of the first)
                     const u16x2 magnitude = __builtin_bit_cast(u16x2, bits & 0x7FFF7FFFu);
                     magnitudes = __builtin_elementwise_max(magnitudes, magnitude);
-                    u16x2 c = __builtin_elementwise_min(__builtin_elementwise_sub_sat(magnitude, base), side);
-                    const u16x2 sign = __builtin_bit_cast(u16x2, __builtin_bit_cast(i16x2, bits) >> (int16_t)15);
-                    c = (u16x2)(((sign - (c ^ sign)) << (uint16_t)2) + top);               // top - c, or top + c where the sign is set; in bytes
-                    places = __builtin_elementwise_min(places, c);
-                    const uint32_t at = __builtin_bit_cast(uint32_t, c);
-                    add(at & 0xFFFFu);
-                    add(at >> 16);
+                    const uint32_t c = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_elementwise_sub_sat(magnitude, base), side));
+                    const uint32_t step = __builtin_bit_cast(uint32_t, (u16x2)((__builtin_bit_cast(u16x2, bits) >> (uint16_t)15) * (uint16_t)8 + (uint16_t)-4));
+                    add(multiply_add_16<false, false>(c, step, top));                      // top - 4 c, or top + 4 c where the sign is set
+                    add(multiply_add_16<true, true>(c, step, top));
                 }
             } else {
                 float v[E];
@@ -354,10 +360,9 @@ struct Kept {
                 max = max_or_nan(max, largest_of(v));
 #pragma unroll
                 for (uint32_t e = 0; e < E; ++e) {
-                    const uint32_t bits = __float_as_uint(v[e]), sign = (uint32_t)((int32_t)bits >> 31);
-                    uint32_t c = __builtin_elementwise_sub_sat(bits >> 16 & 0x7FFFu, (uint32_t)kFixedBase);
-                    c = c < most ? c : most;
-                    add((sign - (c ^ sign) + kFixedTop) * 4);
+                    const uint32_t magnitude = __float_as_uint(__builtin_amdgcn_fmed3f(fabsf(v[e]), least_magnitude, most_magnitude));
+                    const uint32_t step = (__float_as_uint(v[e]) >> 31) * 8 - 4;
+                    add(multiply_add_16<true, false>(magnitude - ((uint32_t)kFixedBase << 16), step, top));
                 }
             }
         };
@@ -374,8 +379,7 @@ struct Kept {
             else end[0] = (end[0] & 0xFFFF0000u) | __builtin_bit_cast(uint16_t, last);
             f(end);
         }
-        const uint16_t first = places[0] < places[1] ? places[0] : places[1];
-        return {max, first / 4u, magnitudes[0] > 0x7F80 || magnitudes[1] > 0x7F80};
+        return {max, magnitudes[0] > 0x7F80 || magnitudes[1] > 0x7F80};
     }
     // f(logit) for all of them.
     template <typename F>
@@ -603,6 +607,28 @@ struct Row {
     }
 
     __device__ __forceinline__ uint32_t fixed_count(uint32_t bin) const { return bin < kFixedLast ? sample_lds<T, THREADS>().count[bin] : 0; }
+    // The first fixed bin with a logit in it, which each wave looks for by itself, eight powers of two at a time.
+    __device__ __forceinline__ uint32_t first_bin() const {
+        const u32x4* const four = reinterpret_cast<const u32x4*>(sample_lds<T, THREADS>().count);
+        constexpr uint32_t kFours = kFixedCounts / 4, kAtOnce = 4;
+#pragma unroll 1
+        for (uint32_t from = 0; from < kFours; from += 64 * kAtOnce) {
+            u32x4 n[kAtOnce];
+#pragma unroll
+            for (uint32_t i = 0; i < kAtOnce; ++i) {
+                const uint32_t at = from + i * 64 + (threadIdx.x & 63);
+                n[i] = at < kFours ? four[at] : u32x4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < kAtOnce; ++i) {
+                const uint64_t some = __ballot((n[i][0] | n[i][1] | n[i][2] | n[i][3]) != 0);
+                if (!some) continue;
+                const uint32_t lane = (uint32_t)__builtin_ctzll(some), mine = n[i][0] ? 0u : n[i][1] ? 1u : n[i][2] ? 2u : 3u;
+                return uniform((from + i * 64 + lane) * 4 + (uint32_t)__builtin_amdgcn_readlane(mine, lane));
+            }
+        }
+        return kFixedLast;
+    }
     // s.group, which is cleared: what of(bin, its count) gives for sixteen bins.
     template <typename F>
     __device__ __forceinline__ void sum_groups(F of) const {
@@ -1257,13 +1283,9 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
         max = c.max;
         if constexpr (kNumbers) {
             // no number is beyond the bins (NaN is), and the first that is not empty tells the largest, unless it is the one around 0
-            first = over_lanes<64>(c.first, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
-            if ((threadIdx.x & 63) == 0) s.counts[threadIdx.x / 64] = first;
             if (c.nan) s.held = 1;
             __syncthreads();
-#pragma unroll
-            for (int w = 0; w < THREADS / 64; ++w) first = s.counts[w] < first ? s.counts[w] : first;
-            first = uniform(first);
+            first = r.first_bin();
             known = first > kFixedFirst && first < kFixedLast && first != (uint32_t)kFixedTop && uniform(s.held) == 0;
             if (known) max = fixed_bins().number(first);
         }
