@@ -496,8 +496,7 @@ class Gradients:
         self._hi = self._lo + sizes[some] * np.where(listed["dtype"][some] == 0, 4, 2).astype(np.uint64)
         self._f32, self._worker = listed["dtype"][some] == 0, worker[some].astype(np.uint64)
         before = np.concatenate([[0], np.cumsum(sizes)[:-1]]).astype(np.uint64) if len(flat) else sizes
-        first = {int(w): before[i] for i, w in reversed(list(enumerate(worker)))}
-        self._column = (before - np.array([first[int(w)] for w in worker], np.uint64))[some]
+        self._column = (before - before[np.searchsorted(worker, worker)])[some]            # (the workers' numbers do not descend)
         order = np.argsort(self._lo)
         self._apart = bool(np.all(self._hi[order][:-1] <= self._lo[order][1:]))
         self._span = (int(self._lo.min()), int(self._hi.max())) if some.any() else (0, 0)

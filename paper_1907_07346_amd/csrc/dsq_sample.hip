@@ -6,7 +6,18 @@
 //   Masses exp((z - max) / T) are whole numbers of 2^-kBits or so, made in 64 bits: their sums are exact, so that they depend on no order, may be made with
 // atomics, and differ from the formula's by less than 1e-13 of the largest one's mass per logit.  (A token is wrong where u comes closer to a border than the sums
 // are off: with sums in 32 bits in one row of ten of 131072 logits.)
-//   A workgroup takes a row, and reads it again for each stage: the largest; the bins; what lies in the bins that matter.
+//   How a row is gone about, by its type, length and number:
+// - up to 512 logits, a wave each, the row in LDS (sample_wave_kernel);
+// - a workgroup each (sample_kernel), which keeps 32 KB or 128 KB of the row in registers, so that what needs another look at it need not ask memory: passes over a
+//   row are bound by what the chip's fabric carries (about 6.6 TB/s), and caches behind it are no faster.  bf16, and rows with a top_k, count logits in fixed bins while they
+//   come in.  A bin of bf16 is a number: sums, filters and the token's value are arithmetic on counts, and the last look finds the nth logit of that value.  For a top_k the walk from
+//   the largest bin on ends at the k-th's, and what lies above goes into a list that is put in order.  Rows with min_p alone are listed after the first look.  Rows of fp32 and fp16 that
+//   need sums of everything make masses of all logits: 64-bit arithmetic bounds these;
+// - few long rows by several workgroups, four launches (sample_most_kernel and behind it);
+// - everything that this leaves open (lists that are too long, ties beyond them, largest logits beyond 4080) by answer_any, at leisure.
+//   Calls, us, and what a pass over the logits takes at 6.63 TB/s: 1 x 32000, bf16, k = 50, p = 0.95, 10 (a launch, two trips to memory, twenty barriers); 256 x 32003, fp32, min_p, 13 (4.9);
+// 1024 x 131072, bf16, p = 0.95, 84 (40); 2048 x 65536, fp32, k = 100, p = 0.9, 118 (81); 4096 x 131072, bf16, 263 (162).  The last one's vector units are busy for 54 % of
+// the clocks and its LDS, where a count is an atomic of 64 lanes that meet in banks and in popular bins, for another 54 %, in two workgroups of a compute unit that overlap in part.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
 #include "dsq_logits.h"
@@ -328,7 +339,8 @@ struct Kept {
         }
         return max;
     }
-    // Counts logits in fixed bins.  Returns the thread's largest one; of bf16, whose bins tell it, whether it met a NaN.
+    // Counts logits in fixed bins; with places as multiples of a sign's step added to the middle, eight vector instructions for two bf16 logits (twelve, with two's complements and the least place of
+    // each thread kept: 4096 x 131072 268 us, so 263).  Returns the thread's largest one; of bf16, whose bins tell it, whether it met a NaN.
     struct Counted {
         float max;
         bool nan;
