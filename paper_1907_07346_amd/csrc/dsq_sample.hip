@@ -16,8 +16,10 @@
 // - few long rows by several workgroups, four launches (sample_most_kernel and behind it);
 // - everything that this leaves open (lists that are too long, ties beyond them, largest logits beyond 4080) by answer_any, at leisure.
 //   Calls, us, and what a pass over the logits takes at 6.63 TB/s: 1 x 32000, bf16, k = 50, p = 0.95, 10 (a launch, two trips to memory, twenty barriers); 256 x 32003, fp32, min_p, 13 (4.9);
-// 1024 x 131072, bf16, p = 0.95, 84 (40); 2048 x 65536, fp32, k = 100, p = 0.9, 118 (81); 4096 x 131072, bf16, 263 (162).  The last one's vector units are busy for 54 % of
-// the clocks and its LDS, where a count is an atomic of 64 lanes that meet in banks and in popular bins, for another 54 %, in two workgroups of a compute unit that overlap in part.
+// 1024 x 131072, bf16, p = 0.95, 84 (40); 2048 x 65536, fp32, k = 100, p = 0.9, 118 (81); 4096 x 131072, bf16, 258 (162).  Of the last one's 63000
+// clocks a row, with two workgroups on a compute unit, counting takes 27000: an atomic of 64 lanes on LDS takes 9 clocks, 6 of them because lanes meet in banks.  The rest is a chain of
+// short phases (masses of bins 6400, the token's place in the row 10000), in which the other workgroup counts.  Three workgroups of 256 threads and 16 pieces: 245, but 1024 x 131072 88 -> 99 and
+// 2048 x 65536, fp32, 118 -> 141; three of 512 and 8 pieces, which read more of a row twice, 292.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
 #include "dsq_logits.h"
@@ -378,10 +380,15 @@ struct Kept {
                 }
             }
         };
+        const uint32_t n = stretches();
+        u32x4 ahead[kPieces];                                     // (a stretch is on its way while what comes before it is counted: 4096 x 131072, bf16, 263 us, so 258)
+        if (n) fetch(ahead, 0);
         of_held([&](u32x4 raw, uint32_t) { f(raw); });
-        for (uint32_t i = 0, n = stretches(); i < n; ++i) {
+        for (uint32_t i = 0; i < n; ++i) {
             u32x4 raw[kPieces];
-            fetch(raw, i);
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) raw[p] = ahead[p];
+            if (i + 1 < n) fetch(ahead, i + 1);
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) f(raw[p]);
         }
