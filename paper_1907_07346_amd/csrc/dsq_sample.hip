@@ -8,7 +8,7 @@
 // are off: with sums in 32 bits in one row of ten of 131072 logits.)
 //   How a row is gone about, by its type, length and number:
 // - up to 512 logits, a wave each, the row in LDS (sample_wave_kernel);
-// - a workgroup each (sample_kernel), which keeps 32 KB or 128 KB of the row in registers, so that what needs another look at it need not ask memory: passes over a
+// - a workgroup each (sample_kernel), which keeps 32 to 128 KB of the row in registers, so that what needs another look at it need not ask memory: passes over a
 //   row are bound by what the chip's fabric carries (about 6.6 TB/s), and caches behind it are no faster.  bf16, and rows with a top_k, count logits in fixed bins while they
 //   come in.  A bin of bf16 is a number: sums, filters and the token's value are arithmetic on counts, and the last look finds the nth logit of that value.  For a top_k the walk from
 //   the largest bin on ends at the k-th's, and what lies above goes into a list that is put in order.  Rows with min_p alone are listed after the first look.  Rows of fp32 and fp16 that
@@ -16,10 +16,9 @@
 // - few long rows by several workgroups, four launches (sample_most_kernel and behind it);
 // - everything that this leaves open (lists that are too long, ties beyond them, largest logits beyond 4080) by answer_any, at leisure.
 //   Calls, us, and what a pass over the logits takes at 6.63 TB/s: 1 x 32000, bf16, k = 50, p = 0.95, 10 (a launch, two trips to memory, twenty barriers); 256 x 32003, fp32, min_p, 13 (4.9);
-// 1024 x 131072, bf16, p = 0.95, 84 (40); 2048 x 65536, fp32, k = 100, p = 0.9, 118 (81); 4096 x 131072, bf16, 258 (162).  Of the last one's 63000
-// clocks a row, with two workgroups on a compute unit, counting takes 27000: an atomic of 64 lanes on LDS takes 9 clocks, 6 of them because lanes meet in banks.  The rest is a chain of
-// short phases (masses of bins 6400, the token's place in the row 10000), in which the other workgroup counts.  Three workgroups of 256 threads and 16 pieces: 245, but 1024 x 131072 88 -> 99 and
-// 2048 x 65536, fp32, 118 -> 141; three of 512 and 8 pieces, which read more of a row twice, 292.
+// 1024 x 131072, bf16, p = 0.95, 84 (40); 2048 x 65536, fp32, k = 100, p = 0.9, 118 (81); 4096 x 131072, bf16, 245 (162).  Of the last one's 63000
+// clocks a row, with two workgroups of 512 threads on a compute unit, counting takes 27000: an atomic of 64 lanes on LDS takes 9 clocks, 6 of them because lanes meet in banks.  The rest is a chain of
+// short phases (masses of bins 6400, the token's place in the row 10000), in which the other workgroup counts.  Three workgroups of 256 threads: 245.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
 #include "dsq_logits.h"
@@ -1396,7 +1395,7 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
             sum = answer_by_numbers(r, kept, asked, k_bin, k_left);
             done = sum != 0;
         }
-    if constexpr (!kNumbers && N <= 8)
+    if constexpr (!kNumbers && (N <= 8 || (N <= 16 && WAVES <= 3)))                        // (others have no registers left)
         if (max < kFixedMost && r.least > -kFixedMost && !asked.k)
             if (finish_by_masses(a, row, r, kept, asked)) return;
     if (!done) sum = answer_any(r, asked.temperature, asked.top_p, max, asked.k, asked.u, asked.border, k_low, k_high, k_left);
@@ -1861,9 +1860,17 @@ void launch_sample_of(const SampleArgs& args, hipStream_t stream) {
         constexpr bool kWaves = !std::is_same_v<T, __bf16>;
         // A wave for a row: 64 x 500, fp32, top_p, 11.1 us (a workgroup 23), 4000 x 500 18.6 (111).  Above, for many rows of which masses have to be made: 4000 x 2000, fp32, top_p, 47.6
         // (53.8); but 1024 x 2000 24.7 (17.6), and 4000 x 2000, bf16, top_k, 54 (33).
+        const uint64_t bytes = a.vocab * sizeof(T);
+        const bool many = a.rows > 512, sums = kWaves && a.top_k == 0 && !(a.min_p > 0.f && a.top_p >= 1.f);
         if (a.vocab <= 512) launch_waves(Int<512>());
         else if (kWaves && a.vocab <= 2048 && a.rows >= 2048 && a.top_k == 0) launch_waves(Int<kWaves ? 2048 : 512>());
-        else if (a.vocab * sizeof(T) <= 256 * 8 * 16) launch(Int<256>(), Int<8>(), Int<4>());
+        else if (bytes <= 256 * 8 * 16) launch(Int<256>(), Int<8>(), Int<4>());
+        // Of rows that a workgroup of 256 holds, three are on a compute unit instead of two, so that one counts while others go through the short phases behind that: 4096 x 16000, fp32,
+        // k = 50, 73 us, so 49; 4096 x 32003, fp16, min_p, 76 and 59; 8000 x 32003, bf16, 230 and 195; but 1 x 32003, fp16, top_p, 39.6 and 46.6, 512 x 20000, bf16, 19.2 and 20.8.  Where masses of all
+        // logits are made there is room for it in line, too (`answer_any` otherwise): 4096 x 16000, fp32, p = 0.9, 331 and 166; 4096 x 32003 465 and 325; but 4096 x 60000, fp16, 606 and 637.
+        else if (many && (bytes <= 256 * 16 * 16 || (sums && a.vocab <= 32768))) launch(Int<256>(), Int<16>(), Int<3>());
+        // Longer ones: 4096 x 24000, fp32, k = 50, 86 and 71; 2048 x 50001, bf16, 84.5 and 81, 4096 x 131072 256 and 245; but 4096 x 28000, fp32, min_p, 78 and 85, 2048 x 131072, bf16, 141 and 145.
+        else if (bytes <= 256 * 24 * 16 ? a.rows > 1024 : !kWaves && a.rows >= (bytes <= 1u << 17 ? 2048u : 4096u)) launch(Int<256>(), Int<24>(), Int<3>());
         else launch(Int<512>(), Int<16>(), Int<4>());
     }
 }

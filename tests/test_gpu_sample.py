@@ -235,6 +235,28 @@ def test_rows_with_a_top_k_that_the_shape_does_not_tell_of():
         same((token, logp), plain.sample(z, u, top_k=k, top_p=0.9), vocab)
 
 
+MANY = [(513, 8193, F32), (600, 32003, F32), (513, 32767, F16), (700, 16385, BF16), (1025, 24001, F32), (1030, 49152, F16), (1100, 40001, BF16), (2049, 65535, BF16), (4097, 70001, BF16)]
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", MANY)
+def test_many_rows_are_as_few_are(rows, vocab, dtype):
+    """How rows are divided goes by their number: the same answers, bit for bit, as of a few at a time, and the formula's for some."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    z = (torch.randn((rows, vocab), generator=g, device="cuda") * 3).to(dtype)
+    u = torch.rand(rows, generator=g, device="cuda")
+    z[3], z[5, 7], z[6, 9], z[8] = -INF, NAN, INF, 1.5
+    z[9, ::2] = torch.finfo(dtype).min
+    z[10] = torch.round(z[10])
+    z[11] *= 1e-6
+    some = torch.tensor([*range(14), rows // 2, rows - 1])
+    for f in (dict(), dict(top_p=0.9), dict(top_k=50, top_p=0.95), dict(top_k=5000), dict(min_p=0.05), dict(top_p=0.97, min_p=0.001, temperature=1.7)):
+        token, logp = b.ds_sample(z, u, **f)
+        for i in range(0, rows, 500):
+            few_token, few_logp = b.ds_sample(z[i:i + 500], u[i:i + 500], **f)
+            assert torch.equal(few_token, token[i:i + 500]) and torch.equal(few_logp.view(torch.int32), logp[i:i + 500].view(torch.int32))
+        same((token[some.cuda()], logp[some.cuda()]), plain.sample(z.cpu()[some], u.cpu()[some], **f), vocab)
+
+
 SPLIT = [(1, 131072, F32), (3, 65536, F16), (32, 33001, F32), (2, 600001, BF16)]
 
 
