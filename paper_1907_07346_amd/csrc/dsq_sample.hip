@@ -496,31 +496,20 @@ struct Kept {
         const uint32_t queued = expand(0, is, add);
         return queued <= kList ? s.held : queued;
     }
-    // The column of the nth (from 1) of the n logits that equal `value`: from the front among those held, or from the row's end.
+    // The column of the nth (from 1) of the n logits, of bf16, that equal `value`: from the front among those held, or from the row's end.
     __device__ __forceinline__ void find(float value, uint64_t nth, uint32_t n) const {
+        static_assert(kNumbers);
         SampleLds<THREADS>& s = sample_lds<T, THREADS>();
         // equal numbers are equal bits, but for the sign of 0
         typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-        uint32_t bits, keep = ~0u;
-        if constexpr (sizeof(T) == 2) {
-            bits = __builtin_bit_cast(uint16_t, (T)value) * 0x10001u;
-            if (value == 0.f) keep = 0x7FFF7FFFu;
-        } else {
-            bits = __float_as_uint(value);
-            if (value == 0.f) keep = 0x7FFFFFFFu;
-        }
-        bits &= keep;
+        const uint32_t keep = value == 0.f ? 0x7FFF7FFFu : ~0u, bits = __builtin_bit_cast(uint16_t, (T)value) * 0x10001u & keep;
         auto test = [&](u32x4 raw) {
             u32x4 d;
 #pragma unroll
             for (int i = 0; i < 4; ++i) d[i] = (raw[i] & keep) ^ bits;
-            if constexpr (sizeof(T) == 2) {
-                auto least = [](uint32_t x, uint32_t y) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y))); };
-                const uint32_t m = least(least(d[0], d[1]), least(d[2], d[3]));
-                return (m & 0xFFFFu) == 0 || m < 0x10000u;
-            } else {
-                return d[0] == 0 || d[1] == 0 || d[2] == 0 || d[3] == 0;
-            }
+            auto least = [](uint32_t x, uint32_t y) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y))); };
+            const uint32_t m = least(least(d[0], d[1]), least(d[2], d[3]));
+            return (m & 0xFFFFu) == 0 || m < 0x10000u;
         };
         auto is = [&](float v) { return v == value; };
         auto add = [&](float, uint32_t column) {
