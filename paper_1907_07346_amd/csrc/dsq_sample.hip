@@ -22,6 +22,7 @@
 #include "dsq_answers.h"
 #include "dsq_codes.h"
 #include "dsq_logits.h"
+#include "dsq_sample_bins.h"
 
 namespace dsq {
 namespace {
@@ -1391,9 +1392,9 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
     if (threadIdx.x == 0) write_answer(a, row, asked, r.masses, s.index, (float)r.z[s.index], sum);
 }
 
-// Short rows: a wave each, with the row in LDS.  Bins are linear between what is looked for and divided again as long as more than 64 different logits lie in
+// Short rows: a wave each, with the row in LDS.  Bins are linear between what is looked for and divided again as long as more than 64 logits that are not alike lie in
 // the one that matters.
-constexpr uint32_t kWaveBins = 256, kWaveRows = 4;
+constexpr uint32_t kWaveRows = 4;
 template <uint32_t ROOM>
 struct WaveLds {
     uint64_t mass[kWaveBins], list[64];
@@ -1458,7 +1459,8 @@ __global__ void __launch_bounds__(64 * kWaveRows) sample_wave_kernel(SampleShape
         least = 0.f;
         wave_sync();
     }
-    auto distance = [&](float x) { return masses.max - (double)x; };
+    LinearBins bin_of{masses.max, 0.0, 0.0};
+    auto distance = [&](float x) { return bin_of.distance(x); };
 
     // bins of the logits from lo to hi, at level 0 from the lowest that has mass to the largest
     float lo = kInf, hi = q.infinite ? 0.f : max;
@@ -1472,12 +1474,6 @@ __global__ void __launch_bounds__(64 * kWaveRows) sample_wave_kernel(SampleShape
     lo = uniform(over_lanes<64>(lo, smaller));
     n = uniform(over_lanes<64>(n, plus));
     if (q.k >= n) q.k = 0;
-    double from, scale;
-    auto set_bins = [&] {
-        from = distance(hi);
-        scale = uniform((kWaveBins - 0.5) / (distance(lo) - from));                        // (infinite where they are the same: not used)
-    };
-    auto bin_of = [&](float x) { return (uint32_t)((distance(x) - from) * scale); };
     uint64_t own[kOwn], before;                                   // masses of the lane's bins, and before them
     uint32_t own_count[kOwn], count_before;
     auto fill_bins = [&] {
@@ -1521,15 +1517,26 @@ __global__ void __launch_bounds__(64 * kWaveRows) sample_wave_kernel(SampleShape
         hi = highest;
         uint64_t ahead = 0, t = step == 0 ? q.k : step == 1 ? q.share(sum) : __umul64hi(q.u, sum) + 1;
         uint32_t here = n;                                        // logits from lo to hi
-        bool first = true;
+        bool first = true, one = lo == hi;                        // one: logits from lo to hi are alike (at first, when hi is the largest: equal)
         uint64_t through = 0;
         for (;;) {
-            if (lo == hi) {                                       // all the same number
+            if (__builtin_expect(one, 0)) {                       // all of the same mass
                 const uint64_t each = masses(lo);
                 const uint64_t nth = step == 0 ? (q.k ? t : here) : step == 2 ? (-distance(lo) >= q.border ? here : 0) : (t - ahead + each - 1) / each;
                 through = ahead + nth * each;
                 if (step == 3) {
                     uint32_t left = (uint32_t)nth;
+                    if (lo != hi) {                               // which number it is, and the how-manieth of these
+                        auto above = [&](uint32_t key) {          // logits from this key to hi
+                            uint32_t count = 0;
+                            of_all([&](float x, uint32_t) { count += x <= hi && logit_key(x) >= key ? 1u : 0u; });
+                            return uniform(over_lanes<64>(count, plus));
+                        };
+                        NthKey keys{logit_key(lo), logit_key(hi)};
+                        while (!keys.done()) keys.counted(above(keys.tried()) >= left);
+                        left -= above(keys.low + 1);
+                        lo = of_key(keys.low);
+                    }
                     value = lo;
                     of_all([&](float x, uint32_t column) {
                         const uint64_t those = __ballot(x == lo);
@@ -1574,7 +1581,8 @@ __global__ void __launch_bounds__(64 * kWaveRows) sample_wave_kernel(SampleShape
                 break;
             }
             if (!(first && whole)) {
-                set_bins();
+                bin_of.set(lo, hi);
+                bin_of.scale = uniform(bin_of.scale);
                 fill_bins();
                 whole = first;
             }
@@ -1591,7 +1599,8 @@ __global__ void __launch_bounds__(64 * kWaveRows) sample_wave_kernel(SampleShape
             bool it = false;
             if (step == 2) {
                 const double d = -q.border;
-                const uint32_t bin = d <= from ? 0 : (d - from) * scale >= kWaveBins ? kWaveBins - 1 : (uint32_t)((d - from) * scale);
+                const double place = (d - bin_of.from) * bin_of.scale;
+                const uint32_t bin = place <= 0.0 ? 0 : place >= kWaveBins ? kWaveBins - 1 : (uint32_t)place;
 #pragma unroll
                 for (uint32_t i = 0; i < kOwn; ++i) {
                     if (lane * kOwn + i == bin) {
@@ -1637,6 +1646,7 @@ __global__ void __launch_bounds__(64 * kWaveRows) sample_wave_kernel(SampleShape
             lo = uniform(over_lanes<64>(low, smaller));
             hi = uniform(over_lanes<64>(high, larger));
             first = false;
+            one = bin_of.alike(lo, hi);
         }
         if (step == 2) sum = through < sum ? through : sum;
         else if (step < 2) sum = through;
