@@ -901,7 +901,7 @@ __device__ __forceinline__ void no_answer(const SampleShape& a, uint64_t row, fl
 }
 __device__ __forceinline__ void write_answer(const SampleShape& a, uint64_t row, const Asked& q, const Masses& masses, uint32_t index, float z, uint64_t sum) {
     a.token[row] = (int32_t)index;
-    const double y = q.infinite ? 0.0 : ((double)z - (double)q.max) / (double)q.temperature;
+    const double y = q.infinite ? 0.0 : ((double)z - (double)q.max) / (double)q.temperature + 0.0;   // (-0 beside +0: not -0, whichever is taken for the largest)
     if (a.logp) a.logp[row] = (float)(y - log(ldexp((double)sum, -masses.bits)));
 }
 
