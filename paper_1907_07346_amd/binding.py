@@ -488,7 +488,7 @@ class Gradients:
             raise DsqError(st, "Gradients", buf.value.decode())
         made_on = torch.cuda.current_stream()
         made_on.synchronize()
-        self._made_on = made_on.cuda_stream
+        self._made_on, self._lent_to = made_on.cuda_stream, set()
         self._work = int(L.ds_gradient_norm_work_bytes(ctypes.byref(self._g))), int(L.ds_clip_work_bytes(ctypes.byref(self._g)))
         self.columns = int(self._g.columns)
         some = sizes > 0
@@ -502,13 +502,16 @@ class Gradients:
         self._span = (int(self._lo.min()), int(self._hi.max())) if some.any() else (0, 0)
 
     def _lent(self, pointer: int, stream: Optional["torch.cuda.Stream"]):
-        """The memory of table and tensors, freed by the stream it is of, must wait for another one that a call ran on."""
-        if pointer == self._made_on:
+        """The memory of table and tensors, freed by the stream it is of, must wait for another one that a call ran on: one that was given, as in every call (the
+        tensors may be of a third, wherever the table was laid), or a current one that the table was not laid on.  Once for each: what is freed waits for all that
+        its streams have been asked for by then."""
+        if pointer in self._lent_to or (stream is None and pointer == self._made_on):
             return
         if stream is None:
             stream = torch.cuda.current_stream()
         for t in (self.table, *self.tensors):
             t.record_stream(stream)
+        self._lent_to.add(pointer)
 
     def _overlapped(self, lo: int, pitch: int) -> bool:
         """A tensor lies in the rows of this pitch from address lo on, and not where its elements go."""
