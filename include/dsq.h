@@ -441,7 +441,8 @@ typedef struct {
 
 /* Parameters of rows, in place of those above: `rows` numbers each, 4-byte aligned, or NULL.  They are not checked: a temperature that is
  * none (NaN, infinite, subnormal, 0 or below) is taken as 0, other numbers as the nearest that is allowed, NaN as all.  (How the work is divided, and so
- * ds_sample_work_bytes, goes by the numbers above all the same: top_k > 0 beside top_k_dev says that most rows have one.) */
+ * ds_sample_work_bytes, goes by the numbers above all the same: top_k > 0 beside top_k_dev, or top_p < 1 beside top_p_dev, says that most rows have one;
+ * min_p > 0 beside min_p_dev that all have; temperature 0 beside temperature_dev that all are such.) */
 typedef struct {
     const float*   temperature_dev;
     const int32_t* top_k_dev;
