@@ -538,7 +538,7 @@ def ds_gradient_norm(grads, stream: Optional["torch.cuda.Stream"] = None) -> "to
 def ds_clip(grads, max_norm: float, out: "Optional[torch.Tensor]" = None, stream: Optional["torch.cuda.Stream"] = None) -> "torch.Tensor":
     """Scales the gradients of workers whose norm is above max_norm to it, and returns the norms before: float32 (workers,).  With out, float32 (workers,
     >= columns), what ds_step takes: written there, each worker's tensors one behind the other, nothing behind them; otherwise in place.  A
-    gradient that is not finite becomes zeros.  Autograd records neither."""
+    gradient that is not finite becomes zeros.  Autograd records neither, but counts both as a change in place: a graph that has saved them refuses to go backward."""
     g, L = grads if type(grads) is Gradients else Gradients(grads), lib()
     here = _on_device("ds_clip", "gradients out", g.table, out)
     at, pitch = None, 0
@@ -558,6 +558,7 @@ def ds_clip(grads, max_norm: float, out: "Optional[torch.Tensor]" = None, stream
         _refuse("ds_clip", "tensors that overlap cannot be scaled in place")
     norm = _new(stream, (g.workers,), torch.float32, g.table)
     pointer = _answer("ds_clip", g._work[1], L.ds_clip, ctypes.byref(g._g), (g.table, out), here, stream, max_norm, at, pitch, norm.data_ptr())
+    torch.autograd.graph.increment_version(g.tensors if out is None else out)    # (a graph that has saved them must notice; 1280 tensors take 27 us)
     g._lent(pointer, stream)
     return norm
 

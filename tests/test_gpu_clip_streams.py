@@ -28,3 +28,16 @@ def test_tensors_of_another_stream_than_the_tables(in_place, at_once):
         assert in_place or bool((out == 1.0 / 2048).all()), "the call read memory that belonged to others already"
         assert all(bool((t == 9.0).all()) for t in others), "the call wrote to memory that belonged to others already"
         del others
+
+
+def test_gradients_that_a_graph_has_saved():
+    """A second derivative whose first was clipped in place: refused, not wrong."""
+    x = torch.randn(5000, device="cuda", requires_grad=True)
+    grad, = torch.autograd.grad((x ** 3).sum(), x, create_graph=True)
+    again = (grad * grad).sum()                       # saves grad
+    with torch.no_grad():
+        b.ds_gradient_norm([grad])
+        torch.autograd.grad(again, x, retain_graph=True)
+        b.ds_clip([grad], 1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(again, x)

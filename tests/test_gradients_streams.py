@@ -28,6 +28,7 @@ def laid(monkeypatch):
     g.workers, g.columns, g._g, g._work, g._apart, g._made_on, g._lent_to = 1, 4, b.ds_gradients(), (0, 0), True, 7, set()
     g.table, g.tensors = Held(), [Held(), Held()]
     monkeypatch.setattr(b, "_on_device", lambda *a: 0)
+    monkeypatch.setattr(torch.autograd.graph, "increment_version", lambda tensors: None)      # (stand-ins have none)
     monkeypatch.setattr(b, "_new", lambda stream, shape, dtype, like: torch.zeros(shape, dtype=dtype))
     monkeypatch.setattr(b, "lib", lambda: types.SimpleNamespace(ds_gradient_norm=lambda *a: b.DS_OK, ds_clip=lambda *a: b.DS_OK))
 
