@@ -1374,21 +1374,17 @@ __global__ void __launch_bounds__(THREADS, WAVES) sample_kernel(SampleShape a) {
             if (listed && k_low > r.least) r.least = k_low;
         }
     }
-    uint64_t sum = 0;
-    bool done = false;
     if (listed || (!kNumbers && asked.by_value && !asked.by_mass && !asked.k)) {
         const uint32_t n = kept.gather(r.least, kInf);
         if (n <= kList) return finish_from_list(a, row, r, asked, n);
     }
+    uint64_t sum = 0;
     if constexpr (kNumbers)
-        if (!done && fixed) {
-            sum = answer_by_numbers(r, kept, asked, k_bin, k_left);
-            done = sum != 0;
-        }
+        if (fixed) sum = answer_by_numbers(r, kept, asked, k_bin, k_left);
     if constexpr (!kNumbers && (N <= 8 || (N <= 16 && WAVES <= 3)))                        // (others have no registers left)
         if (max < kFixedMost && r.least > -kFixedMost && !asked.k)
             if (finish_by_masses(a, row, r, kept, asked)) return;
-    if (!done) sum = answer_any(r, asked.temperature, asked.top_p, max, asked.k, asked.u, asked.border, k_low, k_high, k_left);
+    if (!sum) sum = answer_any(r, asked.temperature, asked.top_p, max, asked.k, asked.u, asked.border, k_low, k_high, k_left);
     if (threadIdx.x == 0) write_answer(a, row, asked, r.masses, s.index, (float)r.z[s.index], sum);
 }
 
@@ -1509,10 +1505,8 @@ __global__ void __launch_bounds__(64 * kWaveRows) sample_wave_kernel(SampleShape
     float value = 0.f;
     uint64_t sum = 0;
     bool whole = false;                                           // the bins are those of level 0
-    for (int step = 0; step < 4; ++step) {                        // top_k, top_p, min_p, the token
-        if ((step == 0 && !q.k && lowest != highest) || (step == 1 && !q.by_mass) || (step == 2 && !q.by_value)) {
-            if (step != 0) continue;
-        }
+    for (int step = 0; step < 4; ++step) {                        // top_k, or the sum of all that others start from; top_p, min_p, the token
+        if ((step == 1 && !q.by_mass) || (step == 2 && !q.by_value)) continue;
         lo = lowest;
         hi = highest;
         uint64_t ahead = 0, t = step == 0 ? q.k : step == 1 ? q.share(sum) : __umul64hi(q.u, sum) + 1;
