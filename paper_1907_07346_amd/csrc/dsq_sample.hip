@@ -3,22 +3,24 @@
 // A row's order (larger first, of equal ones the lower index) is never made.  Every filter keeps a beginning of it, so that all that is needed of a filter is the
 // mass of what it keeps, and the token is where the mass passes u times the smallest of these.  Each is one question: at which place of the order do count
 // or mass reach a number?  Bins that follow the order answer it but for what lies in one bin, whose logits are then gathered, ranked and summed.
-//   Masses exp((z - max) / T) are whole numbers of 2^-kBits or so, made in 64 bits: their sums are exact, so that they depend on no order, may be made with
-// atomics, and differ from the formula's by less than 1e-13 of the largest one's mass per logit.  (A token is wrong where u comes closer to a border than the sums
-// are off: with sums in 32 bits in one row of ten of 131072 logits.)
+//   Masses exp((z - max) / T) are whole numbers of 2^-bits, made in 64 bits: their sums are exact, so that they depend on no order, may be made with
+// atomics, and differ from the formula's by 4e-14 of each mass and half a unit of 2^-bits a logit (bits: 51, and from 2^11 logits on 62 less those of their number: 45 for 131072).  (A token is
+// wrong where u comes closer to a border than the sums are off: with sums in 32 bits in one row of ten of 131072 logits.)
 //   How a row is gone about, by its type, length and number:
-// - up to 512 logits, a wave each, the row in LDS (sample_wave_kernel);
+// - up to 512 logits, and in many rows of fp32 and fp16 without a top_k up to 2048, a wave each, the row in LDS (sample_wave_kernel).  Vector instructions bound it: 222 a logit of 500, which
+//   keep the vector units busy for 73 % of the clocks;
 // - a workgroup each (sample_kernel), which keeps 32 to 128 KB of the row in registers, so that what needs another look at it need not ask memory: passes over a
 //   row are bound by what the chip's fabric carries (about 6.6 TB/s), and caches behind it are no faster.  bf16, and rows with a top_k, count logits in fixed bins while they
 //   come in.  A bin of bf16 is a number: sums, filters and the token's value are arithmetic on counts, and the last look finds the nth logit of that value.  For a top_k the walk from
 //   the largest bin on ends at the k-th's, and what lies above goes into a list that is put in order.  Rows with min_p alone are listed after the first look.  Rows of fp32 and fp16 that
-//   need sums of everything make masses of all logits: 64-bit arithmetic bounds these;
+//   need sums of everything make masses of all logits.  In line (up to 32768 logits of many rows) 65 vector instructions a logit, 18 of them the 64-bit exponential's, bound these: 4096 x 32003, fp32,
+//   top_p, 322 us, vector units 74 % of the clocks, LDS 23 %, 1.9 readings.  Out of line (answer_any) a row is read 4.6 times, from memory: 4096 x 65536, 762 us for 5.0 GB, 6.5 TB/s;
 // - few long rows by several workgroups, four launches (sample_most_kernel and behind it);
 // - everything that this leaves open (lists that are too long, ties beyond them, largest logits beyond 4080) by answer_any, at leisure.
 //   Calls, us, and what a pass over the logits takes at 6.63 TB/s: 1 x 32000, bf16, k = 50, p = 0.95, 10 (a launch, two trips to memory, twenty barriers); 256 x 32003, fp32, min_p, 13 (4.9);
-// 1024 x 131072, bf16, p = 0.95, 84 (40); 2048 x 65536, fp32, k = 100, p = 0.9, 118 (81); 4096 x 131072, bf16, 245 (162).  Of the last one's 63000
-// clocks a row, with two workgroups of 512 threads on a compute unit, counting takes 27000: an atomic of 64 lanes on LDS takes 9 clocks, 6 of them because lanes meet in banks.  The rest is a chain of
-// short phases (masses of bins 6400, the token's place in the row 10000), in which the other workgroup counts.  Three workgroups of 256 threads: 245.
+// 1024 x 131072, bf16, p = 0.95, 84 (40); 2048 x 65536, fp32, k = 100, p = 0.9, 118 (81); 4096 x 131072, bf16, 246 (162).  The last one as two workgroups of 512 threads on a compute unit
+// takes 252 us, 63000 clocks a row.  Of these counting takes 27000: an atomic of 64 lanes on LDS takes 9 clocks, 6 of them because lanes meet in banks.  The rest is a chain of
+// short phases (masses of bins 6400, the token's place in the row 10000), in which the other workgroup counts, or, of three of 256 threads, as it runs, the other two.
 #include "dsq_answers.h"
 #include "dsq_codes.h"
 #include "dsq_logits.h"
@@ -1860,10 +1862,11 @@ void launch_sample_of(const SampleArgs& args, hipStream_t stream) {
         else if (kWaves && a.vocab <= 2048 && a.rows >= 2048 && a.top_k == 0) launch_waves(Int<kWaves ? 2048 : 512>());
         else if (bytes <= 256 * 8 * 16) launch(Int<256>(), Int<8>(), Int<4>());
         // Of rows that a workgroup of 256 holds, three are on a compute unit instead of two, so that one counts while others go through the short phases behind that: 4096 x 16000, fp32,
-        // k = 50, 73 us, so 49; 4096 x 32003, fp16, min_p, 76 and 59; 8000 x 32003, bf16, 230 and 195; but 1 x 32003, fp16, top_p, 39.6 and 46.6, 512 x 20000, bf16, 19.2 and 20.8.  Where masses of all
-        // logits are made there is room for it in line, too (`answer_any` otherwise): 4096 x 16000, fp32, p = 0.9, 331 and 166; 4096 x 32003 465 and 325; but 4096 x 60000, fp16, 606 and 637.
+        // k = 50, 68 us, so 59; 4096 x 32003, fp16, min_p, 71 and 51; 8000 x 32003, bf16, 227 and 193; but 1 x 32003, fp16, top_p, 36.6 and 38.0, 512 x 20000, bf16, 17.8 and 19.3.  Where masses of all
+        // logits are made there is room for it in line, too (`answer_any` otherwise): 4096 x 16000, fp32, p = 0.9, 329 and 162; 4096 x 32003 462 and 322; but 4096 x 60000, fp16, 604 and 638.
         else if (many && (bytes <= 256 * 16 * 16 || (sums && a.vocab <= 32768))) launch(Int<256>(), Int<16>(), Int<3>());
-        // Longer ones: 4096 x 24000, fp32, k = 50, 86 and 71; 2048 x 50001, bf16, 84.5 and 81, 4096 x 131072 256 and 245; but 4096 x 28000, fp32, min_p, 78 and 85, 2048 x 131072, bf16, 141 and 145.
+        // Longer ones: 4096 x 24000, fp32, k = 50, 83 and 69; 2048 x 50001, bf16, 78.3 and 75.6; 4096 x 131072 252 and 246, 6144 rows 358 and 345, 8192 469 and 457; but 4096 x 28000, fp32, min_p, 78 and 84;
+        // 1024 x 131072, bf16, 82 and 87, 2048 137 and 142, 3500 215 and 217.
         else if (bytes <= 256 * 24 * 16 ? a.rows > 1024 : !kWaves && a.rows >= (bytes <= 1u << 17 ? 2048u : 4096u)) launch(Int<256>(), Int<24>(), Int<3>());
         else launch(Int<512>(), Int<16>(), Int<4>());
     }
